@@ -286,6 +286,140 @@ int dense_decode_step(const loki_layout* layout, const void* q, const void* k_fu
                       void* out, void* stream);
 
 /*
+ * Rotary positions for the queries and keys of new tokens (the step in front of Algorithm 1 lines
+ * 2-4; the basis P may be fitted to keys with or without them).  The first rotary_dims columns
+ * of every head are rotary_dims / 2 pairs (a, b), columns (i, i + rotary_dims / 2) or, interleaved,
+ * (2 i, 2 i + 1); pair i of a token at position t becomes
+ *     scale (a cos x - b sin x),  scale (b cos x + a sin x),    x = t frequencies[i],
+ * the other columns stay as they are.  The angle is formed and reduced in fp64, the rest is fp32 with
+ * one rounding to the storage type.  Only B, Hq, Hkv, D and dtype of the layout are used.
+ *
+ *   q, k, v   the tensors to take along (in == NULL: not there; v is carried over unturned). Element
+ *             (b, token j, head h, column c) lies at in + b in_batch + j in_token + h in_head + c and goes
+ *             to the same sum of the out strides (elements of the storage type, multiples of 16 bytes, at
+ *             least 0; two tokens' or heads' outputs must not overlap).  out may be in with the same strides, else the two
+ *             must not overlap.  q_out as the decode calls take it is [B, Hq, D], k_new of
+ *             loki_rotate_keys [B, Hkv, n_new, D], k_new of loki_decode_step [B, m, Hkv, D].
+ *   positions device int32 [B, n_new]
+ *   rows      device int32 [B, n_new] or NULL.  When given, token j's key and value go to row
+ *             rows[b, j] in place of j along out_token, straight into a cache [B, Hkv, n_rows, D]; a row outside
+ *             [0, n_rows) is not written (padded tokens).  Two tokens of a sequence must not share a row.
+ *   frequencies  device fp64 [rotary_dims / 2], radians per position (loki_rotary_frequencies)
+ *   rotary_dims  even, 2 .. D
+ *   inverse   not 0: the angles' signs are turned, which undoes a rotation (with scale 1) and is
+ *             the gradient of one (with its scale).
+ */
+typedef struct {
+  const void* in;
+  void* out;
+  int64_t in_batch, in_token, in_head;
+  int64_t out_batch, out_token, out_head;
+} loki_rotary_tensor;
+
+typedef struct {
+  loki_rotary_tensor q, k, v;
+  const int32_t* positions;
+  const int32_t* rows;
+  const double* frequencies;
+  int32_t n_rows;
+  int32_t rotary_dims;
+  int32_t interleaved;
+  int32_t inverse;
+  float scale;
+} loki_rotary_args;
+
+int loki_rotary(const loki_layout* layout, int n_new, const loki_rotary_args* args, void* stream);
+
+/*
+ * The frequencies of loki_rotary, host only: f_i = base^(-2 i / rotary_dims), i < rotary_dims / 2, for
+ * contexts `factor` times as long as the original_context they were learnt for by
+ *   NONE    as they are
+ *   LINEAR  f_i / factor
+ *   BASE    the base times factor^(R / (R - 2)): the first pair keeps its frequency, the last one is divided
+ *           by factor (R = rotary_dims > 2)
+ *   BANDS   by the turns n_i = original_context f_i / (2 pi) a pair makes in the original context: above `high`
+ *           as they are, below `low` divided by factor, between them a mix linear in n_i (low < high)
+ *   RAMP    a mix linear in i, from as they are up to the pair that makes `high` turns (rounded down) to divided
+ *           by factor from the pair that makes `low` turns (rounded up); *scale = 0.1 ln(factor) + 1
+ * frequencies: host fp64 [rotary_dims / 2]; scale: host, may be NULL, 1 unless stated.  factor >= 1, base > 1.
+ */
+enum { LOKI_ROTARY_NONE = 0, LOKI_ROTARY_LINEAR = 1, LOKI_ROTARY_BASE = 2, LOKI_ROTARY_BANDS = 3, LOKI_ROTARY_RAMP = 4 };
+int loki_rotary_frequencies(int rotary_dims, double base, int scaling, double factor, double original_context, double low,
+                            double high, double* frequencies, float* scale);
+
+/*
+ * dense_decode_step that also adds up what its rows were worth: with p the softmax weights,
+ *     weights_out[b, h, s] = weights_in[b, h, s] + sum over the query heads of KV head h of p[s]
+ * for the rows s < seq_lens[b]; later entries of weights_out are not written.
+ *   seq_lens    device int32 [B], 0 <= seq_lens[b] <= S_max (clamped); NULL: S_max.  A sequence without rows
+ *               gives zeros in `out`.
+ *   weights_in  device fp32 [B, Hkv, S_cap] or NULL (zeros); weights_out likewise, may be weights_in
+ *   workspace   >= dense_weights_workspace_bytes(layout, S_max), 256-byte aligned
+ * A workspace sized for an S_max also serves shorter ones.
+ */
+int dense_weights_workspace_bytes(const loki_layout* layout, int S_max, size_t* bytes);
+int dense_decode_weights(const loki_layout* layout, const void* q, const void* k_full, const void* v, int S_max,
+                         const int32_t* seq_lens, const float* weights_in, float* weights_out, void* workspace,
+                         size_t workspace_bytes, void* out, void* stream);
+
+/*
+ * Eviction by accumulated attention weight.  Of every (sequence b, KV head h) with more than `budget` rows
+ * the first `sinks`, the newest `recent` and, of those between, the ones with the largest weights go on, `budget`
+ * in all, in their order; of equal weights the lowest rows.  Sequences of at most `budget` rows
+ * keep all of theirs.  The cache is that of the layout: klo, khi, v, or with d_split == D an unsplit one (klo =
+ * k_full, khi = NULL).
+ *   seq_lens   device int32 [B], 0 <= seq_lens[b] <= S_max (clamped); NULL: S_max
+ *   weights    device fp32 [B, Hkv, S_cap] (no NaN); moved along with the rows when in place
+ *   klo_out .. weights_out   the cache that the kept rows go to, rows 0 .. of [B, Hkv, S_cap_out, .],
+ *              S_cap_out >= min(budget, S_max); later rows are not written.  weights_out may be NULL.  The two caches must
+ *              not overlap.  All NULL: in place, row j from row idx[j] >= j; later rows stay as they are.
+ *   lens_out   device int32 [B] or NULL: rows kept, min(seq_lens[b], budget).  May be seq_lens.
+ *   out_idx    device int32 [B, Hkv, budget] or NULL: the rows kept, ascending, -1 behind them
+ *   page_table .. as in loki_step_args: klo, khi, v are paged pools (out caches are never; weights neither). A
+ *              page belongs to one sequence when in place.
+ *   workspace  >= loki_evict_workspace_bytes(layout, S_max, budget), 256-byte aligned
+ * 0 <= sinks, 0 <= recent, 1 <= budget, sinks + recent <= budget.
+ */
+typedef struct {
+  const int32_t* seq_lens;
+  float* weights;
+  void* klo;
+  void* khi;
+  void* v;
+  void* klo_out;
+  void* khi_out;
+  void* v_out;
+  float* weights_out;
+  int32_t* lens_out;
+  int32_t* out_idx;
+  const int32_t* page_table;
+  int32_t S_cap_out;
+  int32_t page_rows;
+  int32_t pages_per_seq;
+  int32_t n_pages;
+} loki_evict_args;
+
+int loki_evict_workspace_bytes(const loki_layout* layout, int S_max, int budget, size_t* bytes);
+int loki_evict(const loki_layout* layout, const loki_evict_args* args, int S_max, int budget, int sinks, int recent,
+               void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * dense_decode_step for sequences that all begin with the same prefix_rows rows (a system prompt, a document),
+ * held once: sequence b attends over the prefix and its own first seq_lens[b] rows,
+ *     out = softmax(q [K_prefix; K_b]^T / sqrt(D)) [V_prefix; V_b].
+ *   k_prefix, v_prefix  [Hkv, prefix_cap, D]; 0 <= prefix_rows <= prefix_cap, NULL allowed for 0 rows
+ *   k_full, v           [B, Hkv, S_cap, D], the sequences' own rows; NULL allowed for S_max = 0
+ *   S_max, seq_lens     0 <= S_max <= S_cap; device int32 [B], 0 <= seq_lens[b] <= S_max (clamped); NULL: S_max.
+ *                       A sequence with no row at all gives zeros.
+ *   workspace           >= dense_shared_workspace_bytes(layout, prefix_rows, S_max), 256-byte aligned
+ * The prefix is read once for the whole batch.  Batches with several prefixes take one call for each.
+ */
+int dense_shared_workspace_bytes(const loki_layout* layout, int prefix_rows, int S_max, size_t* bytes);
+int dense_decode_shared(const loki_layout* layout, const void* q, const void* k_prefix, const void* v_prefix, int prefix_rows,
+                        int prefix_cap, const void* k_full, const void* v, int S_max, const int32_t* seq_lens, void* workspace,
+                        size_t workspace_bytes, void* out, void* stream);
+
+/*
  * Appendix E, Algorithm 2 (PCAAttn, the variant the paper tried and set aside): the
  * attention weights come from the first d rotated columns alone, over all S rows,
  *   out = softmax(qhat[:d] Klo^T / sqrt(D)) V,

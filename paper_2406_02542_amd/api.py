@@ -20,6 +20,7 @@ SELECT_PER_QUERY_HEAD, SELECT_PER_KV_GROUP = 0, 1
 PATH_SPLIT, PATH_FUSED, PATH_CLUSTER, PATH_MASK = 0x100, 0x200, 0x300, 0x300
 WORKSPACE_ZEROED = 0x400
 PROFILE_MAX_KERNELS = 8
+ROTARY_NONE, ROTARY_LINEAR, ROTARY_BASE, ROTARY_BANDS, ROTARY_RAMP = 0, 1, 2, 3, 4
 
 
 class LokiError(RuntimeError):
@@ -34,6 +35,27 @@ class Layout(ctypes.Structure):
     _fields_ = [("B", ctypes.c_int32), ("Hq", ctypes.c_int32), ("Hkv", ctypes.c_int32),
                 ("D", ctypes.c_int32), ("d_split", ctypes.c_int32), ("S_cap", ctypes.c_int32),
                 ("dtype", ctypes.c_int32)]
+
+
+class RotaryTensor(ctypes.Structure):
+    """Mirror of ``loki_rotary_tensor``."""
+    _fields_ = [("in_", ctypes.c_void_p), ("out", ctypes.c_void_p)] + [
+        (n, ctypes.c_int64) for n in ("in_batch", "in_token", "in_head", "out_batch", "out_token", "out_head")]
+
+
+class RotaryArgs(ctypes.Structure):
+    """Mirror of ``loki_rotary_args``."""
+    _fields_ = [("q", RotaryTensor), ("k", RotaryTensor), ("v", RotaryTensor), ("positions", ctypes.c_void_p),
+                ("rows", ctypes.c_void_p), ("frequencies", ctypes.c_void_p), ("n_rows", ctypes.c_int32),
+                ("rotary_dims", ctypes.c_int32), ("interleaved", ctypes.c_int32), ("inverse", ctypes.c_int32),
+                ("scale", ctypes.c_float)]
+
+
+class EvictArgs(ctypes.Structure):
+    """Mirror of ``loki_evict_args``."""
+    _fields_ = [(n, ctypes.c_void_p) for n in ("seq_lens", "weights", "klo", "khi", "v", "klo_out", "khi_out", "v_out",
+                                               "weights_out", "lens_out", "out_idx", "page_table")] + [
+        (n, ctypes.c_int32) for n in ("S_cap_out", "page_rows", "pages_per_seq", "n_pages")]
 
 
 _lib = None
@@ -83,6 +105,23 @@ def lib() -> ctypes.CDLL:
     L.loki_layer_width.argtypes = [vp, i32, i32, ctypes.c_float, i32, vp, vp, vp]
     L.loki_index_jaccard.restype = i32
     L.loki_index_jaccard.argtypes = [vp, vp, i32, i32, vp, vp]
+    L.loki_rotary.restype = i32
+    L.loki_rotary.argtypes = [LP, i32, ctypes.POINTER(RotaryArgs), vp]
+    L.loki_rotary_frequencies.restype = i32
+    L.loki_rotary_frequencies.argtypes = [i32, ctypes.c_double, i32, ctypes.c_double, ctypes.c_double, ctypes.c_double, ctypes.c_double,
+                                          vp, ctypes.POINTER(ctypes.c_float)]
+    L.dense_weights_workspace_bytes.restype = i32
+    L.dense_weights_workspace_bytes.argtypes = [LP, i32, ctypes.POINTER(sz)]
+    L.dense_decode_weights.restype = i32
+    L.dense_decode_weights.argtypes = [LP, vp, vp, vp, i32, vp, vp, vp, vp, sz, vp, vp]
+    L.loki_evict_workspace_bytes.restype = i32
+    L.loki_evict_workspace_bytes.argtypes = [LP, i32, i32, ctypes.POINTER(sz)]
+    L.loki_evict.restype = i32
+    L.loki_evict.argtypes = [LP, ctypes.POINTER(EvictArgs), i32, i32, i32, i32, vp, sz, vp]
+    L.dense_shared_workspace_bytes.restype = i32
+    L.dense_shared_workspace_bytes.argtypes = [LP, i32, i32, ctypes.POINTER(sz)]
+    L.dense_decode_shared.restype = i32
+    L.dense_decode_shared.argtypes = [LP, vp, vp, vp, i32, i32, vp, vp, i32, vp, vp, sz, vp, vp]
     L.dense_decode_attn.restype = i32
     L.dense_decode_attn.argtypes = [LP, vp, vp, vp, i32, vp, sz, vp, vp]
     L.loki_profile_create.restype = i32
@@ -357,6 +396,169 @@ def dense_decode_attn(layout: Layout, q: torch.Tensor, k_full: torch.Tensor, v: 
         workspace.numel() if workspace is not None else 0,
         _ptr(out, "out", dt, nq),
         _stream_ptr(stream)), "dense_decode_attn")
+
+
+def loki_rotary_frequencies(rotary_dims: int, base: float = 10000.0, scaling: int = ROTARY_NONE, factor: float = 1.0,
+                            original_context: float = 0.0, low: float = 0.0, high: float = 0.0, device="cuda"):
+    """(frequencies, scale): the fp64 tensor [rotary_dims / 2] that ``loki_rotary`` takes, and its scale."""
+    f = torch.empty(max(int(rotary_dims), 2) // 2, dtype=torch.float64)
+    scale = ctypes.c_float(1.0)
+    _check(lib().loki_rotary_frequencies(rotary_dims, base, scaling, factor, original_context, low, high, f.data_ptr(),
+                                         ctypes.byref(scale)), "loki_rotary_frequencies")
+    return f.to(device), scale.value
+
+
+def _rotary_pair(t: RotaryTensor, name: str, x: torch.Tensor, y: torch.Tensor, dt: torch.dtype, B: int, n: int, heads: int,
+                 rows: int, head_major: bool) -> None:
+    """x [B, n, heads, D] to y: the same, or head-major [B, heads, rows, D]; any strides with whole rows."""
+    if y is None:
+        raise ValueError(f"{name} needs its output")
+    D = 128
+    if not (x.is_cuda and y.is_cuda):
+        raise ValueError(f"{name} must live on the GPU")
+    if x.dtype != dt or y.dtype != dt:
+        raise ValueError(f"{name} must have dtype {dt}, got {x.dtype} and {y.dtype}")
+    if tuple(x.shape) != (B, n, heads, D):
+        raise ValueError(f"{name} must be [{B}, {n}, {heads}, {D}], got {tuple(x.shape)}")
+    if tuple(y.shape) != ((B, heads, rows, D) if head_major else (B, n, heads, D)):
+        raise ValueError(f"{name}'s output has the wrong shape {tuple(y.shape)}")
+    sx, sy = x.stride(), y.stride()
+    if sx[3] != 1 or sy[3] != 1:
+        raise ValueError(f"{name}: the columns of a row must be next to each other")
+    t.in_, t.out = x.data_ptr(), y.data_ptr()
+    t.in_batch, t.in_token, t.in_head = sx[0], sx[1], sx[2]
+    t.out_batch, t.out_token, t.out_head = (sy[0], sy[2], sy[1]) if head_major else (sy[0], sy[1], sy[2])
+
+
+def loki_rotary(layout: Layout, positions: torch.Tensor, frequencies: torch.Tensor, q: Optional[torch.Tensor] = None,
+                q_out: Optional[torch.Tensor] = None, k: Optional[torch.Tensor] = None, k_out: Optional[torch.Tensor] = None,
+                v: Optional[torch.Tensor] = None, v_out: Optional[torch.Tensor] = None, rows: Optional[torch.Tensor] = None,
+                interleaved: bool = False, inverse: bool = False, scale: float = 1.0, token_major: bool = False,
+                stream=None) -> None:
+    """Rotary positions: ``q``, ``k``, ``v`` [B, n, heads, D] with any strides of whole rows (slices of one
+    projection's output, for instance), ``q_out`` the same shape, ``k_out`` and ``v_out`` [B, Hkv, n, D] as
+    ``loki_rotate_keys`` takes them, or with ``rows`` [B, n] the caches [B, Hkv, S_cap, D]; token_major:
+    [B, n, Hkv, D], as ``loki_decode_step`` takes its new tokens (and in place, given the inputs)."""
+    B, n = positions.shape
+    if B != layout.B:
+        raise ValueError(f"positions must be [{layout.B}, n], got {tuple(positions.shape)}")
+    if token_major and rows is not None:
+        raise ValueError("rows belong to head-major caches")
+    dt = torch.float32 if layout.dtype == LOKI_F32 else torch.bfloat16
+    a = RotaryArgs()
+    n_rows = n
+    if rows is not None:
+        out = k_out if k_out is not None else v_out
+        if out is None:
+            raise ValueError("rows without a key or value output")
+        n_rows = out.shape[2]
+    if q is not None:
+        _rotary_pair(a.q, "q", q, q_out, dt, B, n, layout.Hq, n, False)
+    if k is not None:
+        _rotary_pair(a.k, "k", k, k_out, dt, B, n, layout.Hkv, n_rows, not token_major)
+    if v is not None:
+        _rotary_pair(a.v, "v", v, v_out, dt, B, n, layout.Hkv, n_rows, not token_major)
+    a.positions = _ptr(positions, "positions", torch.int32, B * n)
+    a.rows = _ptr(rows, "rows", torch.int32, B * n)
+    a.frequencies = _ptr(frequencies, "frequencies", torch.float64, 1)
+    a.n_rows, a.rotary_dims, a.scale = n_rows, 2 * frequencies.numel(), scale
+    a.interleaved, a.inverse = interleaved, inverse
+    _check(lib().loki_rotary(ctypes.byref(layout), n, ctypes.byref(a), _stream_ptr(stream)), "loki_rotary")
+
+
+def dense_weights_workspace_bytes(layout: Layout, S_max: int) -> int:
+    n = ctypes.c_size_t()
+    _check(lib().dense_weights_workspace_bytes(ctypes.byref(layout), S_max, ctypes.byref(n)), "dense_weights_workspace_bytes")
+    return n.value
+
+
+def dense_decode_weights(layout: Layout, q: torch.Tensor, k_full: torch.Tensor, v: torch.Tensor, S_max: int,
+                         seq_lens: Optional[torch.Tensor], weights_in: Optional[torch.Tensor], weights_out: torch.Tensor,
+                         workspace: torch.Tensor, out: torch.Tensor, stream=None) -> None:
+    """``dense_decode_step`` that adds every row's softmax weight to its running total [B, Hkv, S_cap]."""
+    dt = _torch_dtype(layout)
+    rows = layout.B * layout.Hkv * layout.S_cap
+    nq = layout.B * layout.Hq * layout.D
+    _check(lib().dense_decode_weights(
+        ctypes.byref(layout),
+        _ptr(q, "q", dt, nq),
+        _ptr(k_full, "k_full", dt, rows * layout.D),
+        _ptr(v, "v", dt, rows * layout.D),
+        S_max,
+        _ptr(seq_lens, "seq_lens", torch.int32, layout.B),
+        _ptr(weights_in, "weights_in", torch.float32, rows),
+        _ptr(weights_out, "weights_out", torch.float32, rows),
+        _ptr(workspace, "workspace", torch.uint8), workspace.numel(),
+        _ptr(out, "out", dt, nq),
+        _stream_ptr(stream)), "dense_decode_weights")
+
+
+def loki_evict_workspace_bytes(layout: Layout, S_max: int, budget: int) -> int:
+    n = ctypes.c_size_t()
+    _check(lib().loki_evict_workspace_bytes(ctypes.byref(layout), S_max, budget, ctypes.byref(n)), "loki_evict_workspace_bytes")
+    return n.value
+
+
+def loki_evict(layout: Layout, weights: torch.Tensor, klo: torch.Tensor, khi: Optional[torch.Tensor], v: torch.Tensor,
+               S_max: int, budget: int, sinks: int, recent: int, workspace: torch.Tensor,
+               seq_lens: Optional[torch.Tensor] = None, klo_out: Optional[torch.Tensor] = None,
+               khi_out: Optional[torch.Tensor] = None, v_out: Optional[torch.Tensor] = None,
+               weights_out: Optional[torch.Tensor] = None, lens_out: Optional[torch.Tensor] = None,
+               out_idx: Optional[torch.Tensor] = None, page_table: Optional[torch.Tensor] = None, page_rows: int = 0,
+               n_pages: int = 0, stream=None) -> None:
+    """Without ``klo_out`` in place; else the kept rows go to [B, Hkv, S_cap_out, width] caches.  An unsplit cache
+    (layout.d_split == D): ``klo`` holds the keys, ``khi`` is None.  With ``page_table`` the cache is paged."""
+    dt = _torch_dtype(layout)
+    units, D, d = layout.B * layout.Hkv, layout.D, layout.d_split
+    cache_rows = (n_pages * layout.Hkv * page_rows) if page_table is not None else units * layout.S_cap
+    cap_out = klo_out.numel() // (units * d) if klo_out is not None else 0
+    a = EvictArgs(
+        _ptr(seq_lens, "seq_lens", torch.int32, layout.B),
+        _ptr(weights, "weights", torch.float32, units * layout.S_cap),
+        _ptr(klo, "klo", dt, cache_rows * d),
+        _ptr(khi, "khi", dt, cache_rows * (D - d)),
+        _ptr(v, "v", dt, cache_rows * D),
+        _ptr(klo_out, "klo_out", dt, units * cap_out * d),
+        _ptr(khi_out, "khi_out", dt, units * cap_out * (D - d)),
+        _ptr(v_out, "v_out", dt, units * cap_out * D),
+        _ptr(weights_out, "weights_out", torch.float32, units * cap_out),
+        _ptr(lens_out, "lens_out", torch.int32, layout.B),
+        _ptr(out_idx, "out_idx", torch.int32, units * budget),
+        _ptr(page_table, "page_table", torch.int32, layout.B),
+        cap_out, page_rows, (page_table.numel() // layout.B) if page_table is not None else 0, n_pages)
+    _check(lib().loki_evict(ctypes.byref(layout), ctypes.byref(a), S_max, budget, sinks, recent,
+                            _ptr(workspace, "workspace", torch.uint8), workspace.numel(), _stream_ptr(stream)), "loki_evict")
+
+
+def dense_shared_workspace_bytes(layout: Layout, prefix_rows: int, S_max: int) -> int:
+    n = ctypes.c_size_t()
+    _check(lib().dense_shared_workspace_bytes(ctypes.byref(layout), prefix_rows, S_max, ctypes.byref(n)),
+           "dense_shared_workspace_bytes")
+    return n.value
+
+
+def dense_decode_shared(layout: Layout, q: torch.Tensor, k_prefix: Optional[torch.Tensor], v_prefix: Optional[torch.Tensor],
+                        prefix_rows: int, k_full: Optional[torch.Tensor], v: Optional[torch.Tensor], S_max: int,
+                        seq_lens: Optional[torch.Tensor], workspace: torch.Tensor, out: torch.Tensor, stream=None) -> None:
+    """``dense_decode_step`` behind a prefix [Hkv, prefix_cap, D] that all sequences share."""
+    dt = _torch_dtype(layout)
+    H, D = layout.Hkv, layout.D
+    rows = layout.B * H * layout.S_cap if S_max > 0 else 0
+    nq = layout.B * layout.Hq * D
+    cap = k_prefix.numel() // (H * D) if k_prefix is not None else 0
+    _check(lib().dense_decode_shared(
+        ctypes.byref(layout),
+        _ptr(q, "q", dt, nq),
+        _ptr(k_prefix, "k_prefix", dt, H * cap * D),
+        _ptr(v_prefix, "v_prefix", dt, H * cap * D),
+        prefix_rows, cap,
+        _ptr(k_full, "k_full", dt, rows * D),
+        _ptr(v, "v", dt, rows * D),
+        S_max,
+        _ptr(seq_lens, "seq_lens", torch.int32, layout.B),
+        _ptr(workspace, "workspace", torch.uint8), workspace.numel(),
+        _ptr(out, "out", dt, nq),
+        _stream_ptr(stream)), "dense_decode_shared")
 
 
 def loki_pca_attn(layout: Layout, q: torch.Tensor, P: torch.Tensor, klo: torch.Tensor,

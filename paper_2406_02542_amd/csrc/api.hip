@@ -4,6 +4,8 @@
 
 #include <hip/hip_runtime.h>
 
+#include <math.h>
+
 #include <atomic>
 #include <new>
 
@@ -673,6 +675,276 @@ int dense_decode_step(const loki_layout* layout, const void* q, const void* k_fu
                       int S_max, const int32_t* seq_lens, void* workspace, size_t workspace_bytes,
                       void* out, void* stream) {
   return dense_impl(layout, q, k_full, v, S_max, seq_lens, workspace, workspace_bytes, out, stream);
+}
+
+// ---- rotary positions, weighed rows and their eviction, shared prefixes ---------------------------
+static int rotary_tensor(const loki_rotary_tensor& x, int heads, int epc, RotaryTensor* t) {
+  if (x.in == nullptr) return LOKI_OK;
+  if (x.out == nullptr) return LOKI_ERR_INVALID_ARG;
+  const int64_t st[6] = {x.in_batch, x.in_token, x.in_head, x.out_batch, x.out_token, x.out_head};
+  for (int64_t v : st) {
+    if (v < 0) return LOKI_ERR_INVALID_ARG;
+    if (v % epc != 0) return LOKI_ERR_ALIGNMENT;
+  }
+  if (!aligned16(x.in) || !aligned16(x.out)) return LOKI_ERR_ALIGNMENT;
+  *t = RotaryTensor{x.in, x.out, heads, x.in_batch, x.in_token, x.in_head, x.out_batch, x.out_token, x.out_head};
+  return LOKI_OK;
+}
+
+int loki_rotary(const loki_layout* layout, int n_new, const loki_rotary_args* args, void* stream) {
+  Shape s;
+  loki_layout L;
+  if (!layout || !args) return LOKI_ERR_INVALID_ARG;
+  L = *layout;
+  L.d_split = 128;  // not used
+  int rc = check_layout(&L, &s);
+  if (rc != LOKI_OK) return rc;
+  if (n_new < 1 || (long long)n_new * s.B > (1 << 30)) return LOKI_ERR_INVALID_ARG;
+  if (!args->positions || !args->frequencies) return LOKI_ERR_INVALID_ARG;
+  if (args->rotary_dims < 2 || args->rotary_dims > 128 || args->rotary_dims % 2 != 0) return LOKI_ERR_INVALID_ARG;
+  if (!args->q.in && !args->k.in && !args->v.in) return LOKI_ERR_INVALID_ARG;
+  if (args->rows && args->n_rows < 1) return LOKI_ERR_INVALID_ARG;
+  if ((reinterpret_cast<uintptr_t>(args->positions) & 3u) || (reinterpret_cast<uintptr_t>(args->rows) & 3u) ||
+      (reinterpret_cast<uintptr_t>(args->frequencies) & 7u))
+    return LOKI_ERR_ALIGNMENT;
+  RotaryArgs a{};
+  const int epc = 16 / s.elem_bytes;
+  if ((rc = rotary_tensor(args->q, s.Hq, epc, &a.q)) != LOKI_OK) return rc;
+  if ((rc = rotary_tensor(args->k, s.Hkv, epc, &a.k)) != LOKI_OK) return rc;
+  if ((rc = rotary_tensor(args->v, s.Hkv, epc, &a.v)) != LOKI_OK) return rc;
+  a.positions = args->positions;
+  a.rows = args->rows;
+  a.freqs = args->frequencies;
+  a.n = n_new;
+  a.total = n_new * s.B;
+  a.n_rows = args->n_rows;
+  a.R = args->rotary_dims;
+  a.interleaved = args->interleaved != 0;
+  a.inverse = args->inverse != 0;
+  a.scale = args->scale;
+  hipStream_t st = static_cast<hipStream_t>(stream);
+  StageTimer tm(st);
+  tm.begin("rotary");
+  const hipError_t e = launch_rotary(s, a, st);
+  tm.end();
+  return e == hipSuccess ? LOKI_OK : LOKI_ERR_HIP;
+}
+
+int loki_rotary_frequencies(int rotary_dims, double base, int scaling, double factor, double original_context, double low,
+                            double high, double* frequencies, float* scale) {
+  const int R = rotary_dims;
+  if (!frequencies || R < 2 || R > 128 || R % 2 != 0) return LOKI_ERR_INVALID_ARG;
+  if (!(base > 1.0) || !(base < 1e30)) return LOKI_ERR_INVALID_ARG;
+  if (scaling < LOKI_ROTARY_NONE || scaling > LOKI_ROTARY_RAMP) return LOKI_ERR_INVALID_ARG;
+  if (scaling != LOKI_ROTARY_NONE && !(factor >= 1.0 && factor < 1e30)) return LOKI_ERR_INVALID_ARG;
+  const bool mixed = scaling == LOKI_ROTARY_BANDS || scaling == LOKI_ROTARY_RAMP;
+  if (mixed && !(original_context > 0.0 && low > 0.0 && high > low && high < 1e30)) return LOKI_ERR_INVALID_ARG;
+  if (scaling == LOKI_ROTARY_BASE && R == 2) return LOKI_ERR_INVALID_ARG;
+  const double two_pi = 6.283185307179586476925;
+  if (scaling == LOKI_ROTARY_BASE) base *= pow(factor, (double)R / (R - 2));
+  double from = 0.0, to = 0.0;  // RAMP: the pairs between which the mix changes
+  if (scaling == LOKI_ROTARY_RAMP) {
+    // pair i makes original_context base^(-2 i / R) / (2 pi) turns
+    from = floor(R * log(original_context / (two_pi * high)) / (2.0 * log(base)));
+    to = ceil(R * log(original_context / (two_pi * low)) / (2.0 * log(base)));
+    from = from < 0.0 ? 0.0 : from;
+    to = to > R - 1.0 ? R - 1.0 : to;
+    if (!(to > from)) to = from + 0.001;  // a step
+  }
+  for (int i = 0; i < R / 2; ++i) {
+    const double f = pow(base, -2.0 * i / R);
+    double keep = 1.0;  // share of the pair's own frequency; the rest is divided by factor
+    if (scaling == LOKI_ROTARY_LINEAR) keep = 0.0;
+    if (scaling == LOKI_ROTARY_BANDS) keep = (original_context * f / two_pi - low) / (high - low);
+    if (scaling == LOKI_ROTARY_RAMP) keep = 1.0 - (i - from) / (to - from);
+    keep = keep < 0.0 ? 0.0 : keep > 1.0 ? 1.0 : keep;
+    frequencies[i] = keep == 1.0 ? f : f * keep + f / factor * (1.0 - keep);
+  }
+  if (scale) *scale = scaling == LOKI_ROTARY_RAMP ? (float)(0.1 * log(factor) + 1.0) : 1.0f;
+  return LOKI_OK;
+}
+
+// The layout of an unsplit cache.
+static int check_dense_layout(const loki_layout* layout, Shape* s) {
+  if (!layout) return LOKI_ERR_INVALID_ARG;
+  loki_layout L = *layout;
+  L.d_split = 128;
+  return check_layout(&L, s);
+}
+
+struct PartsPlan {
+  float *partial, *logits;
+  size_t total;
+};
+// Parts of every head's result and, for the weights, every row's logits.
+static PartsPlan plan_parts(const Shape& s, int nparts, bool weights, void* base) {
+  PartsPlan w{};
+  const size_t heads = (size_t)s.B * s.Hq;
+  const size_t parts = align_up(heads * nparts * kPartStride * sizeof(float), 256);
+  w.partial = static_cast<float*>(base);
+  w.logits = base && weights ? reinterpret_cast<float*>(static_cast<char*>(base) + parts) : nullptr;
+  w.total = parts + (weights ? align_up(heads * weigh_logits_pitch(s.S) * sizeof(float), 256) : 0);
+  return w;
+}
+
+int dense_weights_workspace_bytes(const loki_layout* layout, int S_max, size_t* bytes) {
+  Shape s;
+  const int rc = check_dense_layout(layout, &s);
+  if (rc != LOKI_OK) return rc;
+  if (!bytes || S_max < 1 || S_max > s.S_cap) return LOKI_ERR_INVALID_ARG;
+  s.S = S_max;
+  *bytes = plan_parts(s, weigh_splits(s), true, nullptr).total;
+  return LOKI_OK;
+}
+
+int dense_decode_weights(const loki_layout* layout, const void* q, const void* k_full, const void* v, int S_max,
+                         const int32_t* seq_lens, const float* weights_in, float* weights_out, void* workspace,
+                         size_t workspace_bytes, void* out, void* stream) {
+  Shape s;
+  const int rc = check_dense_layout(layout, &s);
+  if (rc != LOKI_OK) return rc;
+  if (!q || !k_full || !v || !weights_out || !out || !workspace) return LOKI_ERR_INVALID_ARG;
+  if (S_max < 1 || S_max > s.S_cap) return LOKI_ERR_INVALID_ARG;
+  if (!aligned16(q) || !aligned16(k_full) || !aligned16(v) || !aligned16(out) || !aligned16(weights_in) || !aligned16(weights_out))
+    return LOKI_ERR_ALIGNMENT;
+  if (!aligned256(workspace) || (reinterpret_cast<uintptr_t>(seq_lens) & 3u)) return LOKI_ERR_ALIGNMENT;
+  s.S = S_max;
+  s.rg.seq_lens = seq_lens;
+  const int nsplit = weigh_splits(s);
+  const PartsPlan w = plan_parts(s, nsplit, true, workspace);
+  if (w.total > workspace_bytes) return LOKI_ERR_WORKSPACE;
+  hipStream_t st = static_cast<hipStream_t>(stream);
+  StageTimer tm(st);
+  tm.begin("dense_parts");
+  hipError_t e = launch_parts(s, nsplit, nsplit, q, k_full, v, w.partial, w.logits, st);
+  tm.end();
+  if (e != hipSuccess) return LOKI_ERR_HIP;
+  tm.begin("weigh_merge");
+  e = launch_weigh_merge(s, nsplit, 0, w.partial, w.logits, weights_in, weights_out, out, st);
+  tm.end();
+  return e == hipSuccess ? LOKI_OK : LOKI_ERR_HIP;
+}
+
+static size_t evict_list_bytes(const Shape& s, int budget) { return align_up((size_t)s.B * s.Hkv * budget * sizeof(int32_t), 256); }
+
+int loki_evict_workspace_bytes(const loki_layout* layout, int S_max, int budget, size_t* bytes) {
+  Shape s;
+  const int rc = check_layout(layout, &s);
+  if (rc != LOKI_OK) return rc;
+  if (!bytes || S_max < 1 || S_max > s.S_cap || budget < 1) return LOKI_ERR_INVALID_ARG;
+  *bytes = evict_list_bytes(s, budget) + align_up((size_t)s.B * s.Hkv * sizeof(int32_t), 256);
+  return LOKI_OK;
+}
+
+int loki_evict(const loki_layout* layout, const loki_evict_args* args, int S_max, int budget, int sinks, int recent,
+               void* workspace, size_t workspace_bytes, void* stream) {
+  Shape s;
+  size_t need = 0;
+  int rc = check_layout(layout, &s);
+  if (rc != LOKI_OK) return rc;
+  if ((rc = loki_evict_workspace_bytes(layout, S_max, budget, &need)) != LOKI_OK) return rc;
+  if (!args || !workspace || !args->weights || !args->klo || !args->v) return LOKI_ERR_INVALID_ARG;
+  if (s.d < 128 && !args->khi) return LOKI_ERR_INVALID_ARG;
+  if (sinks < 0 || recent < 0 || (long long)sinks + recent > budget) return LOKI_ERR_INVALID_ARG;
+  const bool moves = args->klo_out || args->khi_out || args->v_out || args->weights_out;
+  if (moves) {
+    if (!args->klo_out || !args->v_out || (s.d < 128 && !args->khi_out)) return LOKI_ERR_INVALID_ARG;
+    if (args->S_cap_out < (budget < S_max ? budget : S_max)) return LOKI_ERR_INVALID_ARG;
+    if (args->klo_out == args->klo || args->v_out == args->v || (s.d < 128 && args->khi_out == args->khi) ||
+        args->weights_out == args->weights)
+      return LOKI_ERR_INVALID_ARG;
+  }
+  const void* wide[] = {args->klo, args->khi, args->v, args->klo_out, args->khi_out, args->v_out};
+  for (const void* p : wide)
+    if (!aligned16(p)) return LOKI_ERR_ALIGNMENT;
+  const void* words[] = {args->seq_lens, args->weights, args->weights_out, args->lens_out, args->out_idx};
+  for (const void* p : words)
+    if (reinterpret_cast<uintptr_t>(p) & 3u) return LOKI_ERR_ALIGNMENT;
+  if (!aligned256(workspace)) return LOKI_ERR_ALIGNMENT;
+  EvictArgs a{};
+  if (args->page_table) {
+    rc = paging_from_args(args->page_table, args->page_rows, args->pages_per_seq, args->n_pages, s.Hkv, S_max, &a.pg);
+    if (rc != LOKI_OK) return rc;
+  }
+  if (need > workspace_bytes) return LOKI_ERR_WORKSPACE;
+  a.seq_lens = args->seq_lens;
+  a.weights = args->weights;
+  a.klo = args->klo;
+  a.khi = args->khi;
+  a.v = args->v;
+  a.klo_out = args->klo_out;
+  a.khi_out = args->khi_out;
+  a.v_out = args->v_out;
+  a.weights_out = args->weights_out;
+  a.lens_out = args->lens_out;
+  a.Hkv = s.Hkv;
+  a.S_cap = s.S_cap;
+  a.S_cap_out = args->S_cap_out;
+  a.S_max = S_max;
+  a.budget = budget;
+  a.sinks = sinks;
+  a.recent = recent;
+  a.nlo = s.d * s.elem_bytes / 16;
+  int32_t* kept = reinterpret_cast<int32_t*>(static_cast<char*>(workspace) + evict_list_bytes(s, budget));
+  int32_t* list = args->out_idx ? args->out_idx : static_cast<int32_t*>(workspace);
+  hipStream_t st = static_cast<hipStream_t>(stream);
+  StageTimer tm(st);
+  tm.begin("evict_select");
+  hipError_t e = launch_evict_select(s, a, list, kept, st);
+  tm.end();
+  if (e != hipSuccess) return LOKI_ERR_HIP;
+  tm.begin("evict_move");
+  e = launch_evict_move(s, a, list, kept, st);
+  tm.end();
+  return e == hipSuccess ? LOKI_OK : LOKI_ERR_HIP;
+}
+
+int dense_shared_workspace_bytes(const loki_layout* layout, int prefix_rows, int S_max, size_t* bytes) {
+  Shape s;
+  const int rc = check_dense_layout(layout, &s);
+  if (rc != LOKI_OK) return rc;
+  if (!bytes || prefix_rows < 0 || S_max < 0 || S_max > s.S_cap) return LOKI_ERR_INVALID_ARG;
+  s.S = S_max;
+  *bytes = plan_parts(s, (S_max > 0 ? weigh_splits(s) : 0) + prefix_splits(s, prefix_rows), false, nullptr).total;
+  return LOKI_OK;
+}
+
+int dense_decode_shared(const loki_layout* layout, const void* q, const void* k_prefix, const void* v_prefix, int prefix_rows,
+                        int prefix_cap, const void* k_full, const void* v, int S_max, const int32_t* seq_lens, void* workspace,
+                        size_t workspace_bytes, void* out, void* stream) {
+  Shape s;
+  const int rc = check_dense_layout(layout, &s);
+  if (rc != LOKI_OK) return rc;
+  if (!q || !out || !workspace) return LOKI_ERR_INVALID_ARG;
+  if (prefix_rows < 0 || prefix_rows > prefix_cap || S_max < 0 || S_max > s.S_cap) return LOKI_ERR_INVALID_ARG;
+  if ((prefix_rows > 0 && (!k_prefix || !v_prefix)) || (S_max > 0 && (!k_full || !v))) return LOKI_ERR_INVALID_ARG;
+  if (!aligned16(q) || !aligned16(k_prefix) || !aligned16(v_prefix) || !aligned16(k_full) || !aligned16(v) || !aligned16(out))
+    return LOKI_ERR_ALIGNMENT;
+  if (!aligned256(workspace) || (reinterpret_cast<uintptr_t>(seq_lens) & 3u)) return LOKI_ERR_ALIGNMENT;
+  s.S = S_max;
+  s.rg.seq_lens = seq_lens;
+  const int nsplit = S_max > 0 ? weigh_splits(s) : 0, shared = prefix_splits(s, prefix_rows);
+  const PartsPlan w = plan_parts(s, nsplit + shared, false, workspace);
+  if (w.total > workspace_bytes) return LOKI_ERR_WORKSPACE;
+  hipStream_t st = static_cast<hipStream_t>(stream);
+  StageTimer tm(st);
+  hipError_t e = hipSuccess;
+  if (shared > 0) {
+    tm.begin("prefix_parts");
+    e = launch_prefix(s, nsplit, shared, nsplit + shared, q, k_prefix, v_prefix, prefix_rows, prefix_cap, w.partial, st);
+    tm.end();
+    if (e != hipSuccess) return LOKI_ERR_HIP;
+  }
+  if (nsplit > 0) {
+    tm.begin("dense_parts");
+    e = launch_parts(s, nsplit, nsplit + shared, q, k_full, v, w.partial, nullptr, st);
+    tm.end();
+    if (e != hipSuccess) return LOKI_ERR_HIP;
+  }
+  tm.begin("merge");
+  e = launch_weigh_merge(s, nsplit, shared, w.partial, nullptr, nullptr, nullptr, out, st);
+  tm.end();
+  return e == hipSuccess ? LOKI_OK : LOKI_ERR_HIP;
 }
 
 int loki_pca_attn(const loki_layout* layout, const void* q, const float* P, const void* klo,

@@ -65,6 +65,11 @@ __device__ __forceinline__ RowAddr make_row_addr(const void* k_a, const void* k_
   return ra;
 }
 
+// What else is done with the logits (times log2 e) of the rows that are there: nothing, unless the caller asks.
+struct NoLogits {
+  static constexpr bool kAny = false;
+};
+
 // One trip: R rows of this lane group (ok: the row exists), their chunks and saved scores loaded.
 template <typename T, int NH, int R, bool REUSE_LO>
 __device__ __forceinline__ void attend_trip(AttendAcc<T, NH>& acc, const float (&qr)[NH][T::EPC], const uint4 (&kraw)[R],
@@ -124,13 +129,14 @@ __device__ __forceinline__ void attend_trip(AttendAcc<T, NH>& acc, const float (
 // 4, S = 12800, k = 400 46.4 / 47.3, S = 13300, k = 831 62.7 / 64.0.
 // STREAM: rows are loaded past the caches (row_loads).  ROWS: rows per lane group and trip.
 template <typename T, int NH, int NGROUPS, bool GATHER, bool REUSE_LO, bool SCORE_BY_ROW = false, bool APART = false, bool STREAM = false,
-          int ROWS = kRowsInFlight>
+          int ROWS = kRowsInFlight, typename Logits = NoLogits>
 __device__ __forceinline__ void attend_rows(AttendAcc<T, NH>& acc, const float (&qr)[NH][T::EPC],
                                             const RowAddr& ra, const int32_t* s_idx,
-                                            const float* s_a, int gid, int r0, int r1) {
+                                            const float* s_a, int gid, int r0, int r1, Logits logits = {}) {
   constexpr int EPC = T::EPC;
   constexpr int LPRV = kD / EPC;
   constexpr int R = ROWS;
+  static_assert(!(APART && Logits::kAny), "a trip's logits are handed on here only");
   static_assert(!REUSE_LO || NH == 1, "score reuse needs one query head per selection");
   for (int t0 = r0; t0 < r1; t0 += NGROUPS * R) {
     bool ok[R];
@@ -169,6 +175,7 @@ __device__ __forceinline__ void attend_rows(AttendAcc<T, NH>& acc, const float (
           p = group_allreduce_sum<LPRV>(p);
           if constexpr (REUSE_LO) p += alo[j];
           logit[g][j] = ok[j] ? p * kSoftmaxScaleLog2 : kNegBig;
+          if constexpr (Logits::kAny) logits(g, t0 + j * NGROUPS + gid, ok[j], logit[g][j]);
         }
       }
       float vf[R][EPC];

@@ -135,10 +135,12 @@ struct AmRoundRobin {
 // not, of which an instruction takes 64 bytes of 16 rows, half lines: 16 sequences of 32/8 heads, S =
 // 16384, dense, neither 129.6 us, values 116.7, both 118.3; one selection per group, 96 units, S =
 // 6073, d = 16 39.2, 36.4, 44.6.
-template <bool GATHER, int KSTEPS, int QT, bool STREAM_V, typename Steps, typename Complete>
+// logits: what else is done with a step's logits (times log2 e; NoLogits: nothing).
+template <bool GATHER, int KSTEPS, int QT, bool STREAM_V, typename Steps, typename Complete, typename Logits = NoLogits>
 __device__ __forceinline__ void am_attend_rows(const AmAddr<KSTEPS>& ad,
                                                const am_bf16x8_t (&bq)[KSTEPS][QT],
-                                               const int32_t* s_idx, int r0, Steps steps, AmState& st, Complete complete) {
+                                               const int32_t* s_idx, int r0, Steps steps, AmState& st, Complete complete,
+                                               Logits logits = {}) {
   const int lane = threadIdx.x & 63;
   const int r16 = lane & 15, kgrp = lane >> 4;
   int base, end;
@@ -215,6 +217,10 @@ __device__ __forceinline__ void am_attend_rows(const AmAddr<KSTEPS>& ad,
         logit[t][i] = ok ? s_acc[t][i] * kSoftmaxScaleLog2 : kNegBig;
         smax = fmaxf(smax, logit[t][i]);
       }
+    if constexpr (Logits::kAny) {  // entries b0 + 16 t + 4 kgrp .. + 3 of head r16; those at or past r1 are not there
+#pragma unroll
+      for (int t = 0; t < 2; ++t) logits(r16, b0 + 16 * t + 4 * kgrp, make_float4(logit[t][0], logit[t][1], logit[t][2], logit[t][3]));
+    }
     smax = fmaxf(smax, __shfl_xor(smax, 16));
     smax = fmaxf(smax, __shfl_xor(smax, 32));
     const float m_new = fmaxf(st.m_run, smax);

@@ -1,0 +1,282 @@
+// Eviction from a cache by accumulated attention weight: of every (sequence, KV head) the first `sinks` rows,
+// the newest `recent` ones and between them those with the largest totals go on, `budget` rows in all, in
+// their order; equal totals keep the lowest row.
+//
+// Two launches.  (1) evict_select_kernel, one block per unit: the totals as order-preserving integers in
+// registers, the smallest one kept found by three radix passes over LDS histograms, the list written in
+// ascending order.  Latency bounds it: a pass is a few barriers.  (2) evict_move_kernel: the listed rows to
+// their new places, bound by memory; a row is read once and written once.  In place row j comes from list[j]
+// >= j: a block owns a slice of the unit's columns, walks the list upwards and writes a run of rows only when
+// all of its sources have been read; the sources of later runs lie behind it.
+#include "common.h"
+
+namespace loki {
+
+constexpr int kEvThreads = 1024;
+constexpr int kEvWaves = kEvThreads / 64;
+constexpr int kEvBins = 2048;  // 11-bit digits: 32 bits in three passes of 11, 11 and 10
+
+__device__ __forceinline__ int evict_rows(const int32_t* seq_lens, int b, int S_max) {
+  return seq_lens == nullptr ? S_max : min(max(seq_lens[b], 0), S_max);
+}
+
+// NK: keys per lane held in registers (rows up to 1024 NK); 0: read again in every pass.
+template <int NK>
+__global__ __launch_bounds__(kEvThreads) void evict_select_kernel(EvictArgs a, int32_t* __restrict__ list /* [units, budget] */,
+                                                                  int32_t* __restrict__ kept_rows /* [units] */) {
+  __shared__ uint32_t s_hist[kEvBins];
+  __shared__ uint32_t s_wave[kEvWaves];
+  __shared__ uint32_t s_pick[2];
+  const int unit = blockIdx.x, b = unit / a.Hkv, h = unit - b * a.Hkv;
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int len = evict_rows(a.seq_lens, b, a.S_max), kept = min(len, a.budget);
+  int32_t* out = list + (size_t)unit * a.budget;
+  if (tid == 0) kept_rows[unit] = kept;
+  for (int i = kept + tid; i < a.budget; i += kEvThreads) out[i] = -1;
+  if (len <= a.budget) {  // (uniform for the block)
+    for (int i = tid; i < len; i += kEvThreads) out[i] = i;
+    return;
+  }
+  const int c0 = a.sinks, c1 = len - a.recent;  // rows whose totals decide: at least one, len > budget
+  const uint32_t need = (uint32_t)(a.budget - a.sinks - a.recent);
+
+  // wave w holds rows [w seg, (w + 1) seg), lane by lane in rounds of 64
+  const int seg = ((len + kEvThreads - 1) / kEvThreads) * 64, rounds = seg / 64, first = wave * seg + lane;
+  const float* w = a.weights + (size_t)unit * a.S_cap;
+  auto load = [&](int i) -> uint32_t {
+    const int row = first + 64 * i;
+    const bool in = row >= c0 && row < c1;
+    return in ? max(float_to_key(w[row]), 1u) : 0u;  // 0: no candidate
+  };
+  uint32_t reg[NK > 0 ? NK : 1];
+  if constexpr (NK > 0) {
+#pragma unroll
+    for (int i = 0; i < NK; ++i) reg[i] = i < rounds ? load(i) : 0u;
+  }
+  auto each = [&](auto f) __attribute__((always_inline)) {  // f(round, key), in ascending order of the wave's rows
+    if constexpr (NK > 0) {
+#pragma unroll
+      for (int i = 0; i < NK; ++i)
+        if (i < rounds) f(i, reg[i]);
+    } else {
+      for (int i = 0; i < rounds; ++i) f(i, load(i));
+    }
+  };
+
+  // The need-th largest key, digit by digit.  Rows of total zero, of which a cache can hold many, are counted by
+  // ballots: as atomics they would queue at one bin.
+  uint32_t prefix = 0, left = need;  // left: how many of the keys that begin with `prefix` are kept
+  const uint32_t zero_key = 0x80000000u;
+  bool all = need == 0u;
+#pragma unroll
+  for (int pass = 0; pass < 3; ++pass) {
+    const int shift = pass == 0 ? 21 : pass == 1 ? 10 : 0;
+    const uint32_t mask = pass == 2 ? 0x3ffu : 0x7ffu;
+    if (all) break;  // (uniform: `need` is the block's)
+    s_hist[tid] = 0u;
+    s_hist[tid + kEvThreads] = 0u;
+    __syncthreads();
+    uint32_t zeros = 0;
+    each([&](int, uint32_t key) {
+      const bool hit = key != 0u && (pass == 0 || (key >> (pass == 1 ? 21 : 10)) == prefix);
+      zeros += (uint32_t)__popcll(__ballot(hit && key == zero_key));
+      if (hit && key != zero_key) atomicAdd(&s_hist[(key >> shift) & mask], 1u);
+    });
+    if (lane == 0 && zeros != 0u) atomicAdd(&s_hist[(zero_key >> shift) & mask], zeros);
+    __syncthreads();
+    // thread t owns the bins 2047 - 2 t and 2046 - 2 t: the keys of a larger bin come before them
+    const int hi = kEvBins - 1 - 2 * tid;
+    const uint32_t n_hi = s_hist[hi], n_lo = s_hist[hi - 1];
+    const uint32_t incl = wave_inclusive_scan_u32(n_hi + n_lo);
+    if (lane == 63) s_wave[wave] = incl;
+    __syncthreads();
+    uint32_t before = incl - (n_hi + n_lo);
+    for (int i = 0; i < wave; ++i) before += s_wave[i];
+    if (before < left && left <= before + n_hi) {
+      s_pick[0] = (uint32_t)hi;
+      s_pick[1] = left - before;
+    } else if (before + n_hi < left && left <= before + n_hi + n_lo) {
+      s_pick[0] = (uint32_t)(hi - 1);
+      s_pick[1] = left - before - n_hi;
+    }
+    __syncthreads();
+    prefix = pass == 0 ? s_pick[0] : pass == 1 ? (prefix << 11) | s_pick[0] : (prefix << 10) | s_pick[0];
+    left = s_pick[1];
+    __syncthreads();
+  }
+  const uint32_t last = all ? 0xffffffffu : prefix;  // kept: keys above it, and the first `left` equal to it
+  const uint32_t equal_kept = all ? 0u : left;
+
+  // kept rows and equal keys of every wave's segment, then each wave writes its part of the list
+  auto kind = [&](int i, uint32_t key, bool& sure, bool& equal) {
+    const int row = first + 64 * i;
+    sure = row < len && (row < c0 || row >= c1 || (!all && key > last));
+    equal = !all && key == last && key != 0u;
+  };
+  uint32_t n_sure = 0, n_equal = 0;
+  each([&](int i, uint32_t key) {
+    bool sure, equal;
+    kind(i, key, sure, equal);
+    n_sure += (uint32_t)__popcll(__ballot(sure));
+    n_equal += (uint32_t)__popcll(__ballot(equal));
+  });
+  if (lane == 0) {
+    s_wave[wave] = n_sure;
+    s_hist[wave] = n_equal;
+  }
+  __syncthreads();
+  uint32_t at = 0, eq = 0;  // list entries and equal keys before this wave's segment
+  for (int i = 0; i < wave; ++i) {
+    const uint32_t e = s_hist[i];
+    at += s_wave[i] + (min(eq + e, equal_kept) - min(eq, equal_kept));
+    eq += e;
+  }
+  const unsigned long long below = (1ull << lane) - 1ull;
+  each([&](int i, uint32_t key) {
+    bool sure, equal;
+    kind(i, key, sure, equal);
+    const unsigned long long m_equal = __ballot(equal);
+    const bool keep = sure || (equal && eq + (uint32_t)__popcll(m_equal & below) < equal_kept);
+    const unsigned long long m = __ballot(keep);
+    if (keep) out[at + (uint32_t)__popcll(m & below)] = first + 64 * i;
+    at += (uint32_t)__popcll(m);
+    eq += (uint32_t)__popcll(m_equal);
+  });
+}
+
+// One 16-byte chunk of a row: c < nk: chunk c of the key row (the first nlo in klo, the rest in khi), else of the value row.
+struct EvictSide {
+  char *klo, *khi, *v;
+  int S_cap;
+};
+__device__ __forceinline__ char* evict_chunk(const EvictSide& x, long long row, int c, int nk, int nlo) {
+  if (c >= nk) return x.v + (row * nk + (c - nk)) * 16;
+  return c < nlo ? x.klo + (row * nlo + c) * 16 : x.khi + (row * (nk - nlo) + (c - nlo)) * 16;
+}
+
+constexpr int kMvThreads = 256;
+constexpr int kMvInFlight = 8;
+
+// Into another cache: a block takes `rows` list entries of one unit.
+template <int CHUNKS>  // 16-byte chunks of a key and a value row together
+__global__ __launch_bounds__(kMvThreads) void evict_copy_kernel(EvictArgs a, const int32_t* __restrict__ list,
+                                                                const int32_t* __restrict__ kept_rows, int rows) {
+  const int unit = blockIdx.y, b = unit / a.Hkv, h = unit - b * a.Hkv, tid = threadIdx.x;
+  const int kept = kept_rows[unit];
+  const int j0 = blockIdx.x * rows, j1 = min(kept, j0 + rows);
+  if (blockIdx.x == 0 && h == 0 && tid == 0 && a.lens_out != nullptr) a.lens_out[b] = kept;
+  if (j0 >= j1) return;
+  const int32_t* from = list + (size_t)unit * a.budget;
+  const EvictSide src{(char*)a.klo, (char*)a.khi, (char*)a.v, a.S_cap};
+  const EvictSide dst{(char*)a.klo_out, (char*)a.khi_out, (char*)a.v_out, a.S_cap_out};
+  const long long out0 = (long long)unit * a.S_cap_out;
+  const int items = (j1 - j0) * CHUNKS;
+  for (int i0 = tid; i0 < items; i0 += kMvThreads * kMvInFlight) {
+    uint4 x[kMvInFlight];
+#pragma unroll
+    for (int u = 0; u < kMvInFlight; ++u) {
+      const int i = i0 + u * kMvThreads;
+      if (i < items)
+        x[u] = load16(evict_chunk(src, cache_row(a.pg, b, h, a.Hkv, a.S_cap, from[j0 + i / CHUNKS]), i % CHUNKS, CHUNKS / 2, a.nlo));
+    }
+#pragma unroll
+    for (int u = 0; u < kMvInFlight; ++u) {
+      const int i = i0 + u * kMvThreads;
+      if (i < items) *reinterpret_cast<uint4*>(evict_chunk(dst, out0 + j0 + i / CHUNKS, i % CHUNKS, CHUNKS / 2, a.nlo)) = x[u];
+    }
+  }
+  if (a.weights_out != nullptr)
+    for (int j = j0 + tid; j < j1; j += kMvThreads) a.weights_out[out0 + j] = a.weights[(size_t)unit * a.S_cap + from[j]];
+}
+
+// Every source of a run has been read, by all waves, before one of its rows is overwritten.
+__device__ __forceinline__ void evict_all_read() {
+  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+  __syncthreads();
+}
+
+constexpr int kIpThreads = 512;
+constexpr int kIpSlice = 8;  // chunks of a slice: a 128-byte line
+constexpr int kIpRows = kIpThreads / kIpSlice;
+
+// In place: a block takes one slice of the unit's columns; the block behind the last slice moves the totals.
+__global__ __launch_bounds__(kIpThreads) void evict_compact_kernel(EvictArgs a, const int32_t* __restrict__ list,
+                                                                   const int32_t* __restrict__ kept_rows, int chunks) {
+  const int unit = blockIdx.y, b = unit / a.Hkv, h = unit - b * a.Hkv, tid = threadIdx.x;
+  const int kept = kept_rows[unit];
+  const int slices = chunks / kIpSlice;
+  const int32_t* from = list + (size_t)unit * a.budget;
+  if ((int)blockIdx.x == slices) {
+    if (h == 0 && tid == 0 && a.lens_out != nullptr) a.lens_out[b] = kept;
+    float* w = a.weights + (size_t)unit * a.S_cap;
+    for (int j0 = 0; j0 < kept; j0 += kIpThreads * 4) {  // (uniform)
+      float x[4];
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {
+        const int j = j0 + u * kIpThreads + tid;
+        x[u] = j < kept ? w[from[j]] : 0.f;
+      }
+      evict_all_read();
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {
+        const int j = j0 + u * kIpThreads + tid;
+        if (j < kept) w[j] = x[u];
+      }
+    }
+    return;
+  }
+  const EvictSide x{(char*)a.klo, (char*)a.khi, (char*)a.v, a.S_cap};
+  const int c = (int)blockIdx.x * kIpSlice + tid % kIpSlice, r = tid / kIpSlice;
+  const int nk = chunks / 2;
+  constexpr int U = kMvInFlight;
+  for (int j0 = 0; j0 < kept; j0 += kIpRows * U) {  // (uniform)
+    uint4 y[U];
+    int at[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int j = j0 + u * kIpRows + r;
+      at[u] = j < kept ? from[j] : j;
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int j = j0 + u * kIpRows + r;
+      if (at[u] != j) y[u] = load16(evict_chunk(x, cache_row(a.pg, b, h, a.Hkv, a.S_cap, at[u]), c, nk, a.nlo));
+    }
+    evict_all_read();
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int j = j0 + u * kIpRows + r;
+      if (at[u] != j) *reinterpret_cast<uint4*>(evict_chunk(x, cache_row(a.pg, b, h, a.Hkv, a.S_cap, j), c, nk, a.nlo)) = y[u];
+    }
+  }
+}
+
+hipError_t launch_evict_select(const Shape& s, const EvictArgs& a, int32_t* list, int32_t* kept, hipStream_t st) {
+  const dim3 grid(s.B * s.Hkv), block(kEvThreads);
+  if (a.S_max <= 4 * kEvThreads)
+    hipLaunchKernelGGL((evict_select_kernel<4>), grid, block, 0, st, a, list, kept);
+  else if (a.S_max <= 16 * kEvThreads)
+    hipLaunchKernelGGL((evict_select_kernel<16>), grid, block, 0, st, a, list, kept);
+  else if (a.S_max <= 48 * kEvThreads)
+    hipLaunchKernelGGL((evict_select_kernel<48>), grid, block, 0, st, a, list, kept);
+  else
+    hipLaunchKernelGGL((evict_select_kernel<0>), grid, block, 0, st, a, list, kept);
+  return hipGetLastError();
+}
+
+hipError_t launch_evict_move(const Shape& s, const EvictArgs& a, const int32_t* list, const int32_t* kept, hipStream_t st) {
+  const int units = s.B * s.Hkv, chunks = 2 * kD * s.elem_bytes / 16;
+  if (a.klo_out == nullptr) {
+    hipLaunchKernelGGL(evict_compact_kernel, dim3(chunks / kIpSlice + 1, units), dim3(kIpThreads), 0, st, a, list, kept, chunks);
+    return hipGetLastError();
+  }
+  const int rows = kMvThreads * kMvInFlight / chunks;
+  const dim3 grid((a.budget + rows - 1) / rows, units), block(kMvThreads);
+  if (s.dtype == 0)
+    hipLaunchKernelGGL((evict_copy_kernel<64>), grid, block, 0, st, a, list, kept, rows);
+  else
+    hipLaunchKernelGGL((evict_copy_kernel<32>), grid, block, 0, st, a, list, kept, rows);
+  return hipGetLastError();
+}
+
+}  // namespace loki

@@ -235,6 +235,51 @@ hipError_t launch_layer_width(const float* eigenvalues, int n, int Dn, float v_p
                               float* mean_rank, int32_t* d_out, hipStream_t st);
 hipError_t launch_jaccard(const int32_t* a, const int32_t* b, int n_lists, int k, float* out,
                           hipStream_t st);
+// Rotary positions (rotary.hip): one of the tensors that a launch takes along; strides in elements.
+struct RotaryTensor {
+  const void* in = nullptr;
+  void* out = nullptr;
+  int heads = 0;  // 0: not there
+  long long in_batch = 0, in_token = 0, in_head = 0, out_batch = 0, out_token = 0, out_head = 0;
+};
+struct RotaryArgs {
+  RotaryTensor q, k, v;      // v is not turned
+  const int32_t* positions;  // [B, n]
+  const int32_t* rows;       // [B, n] or null: the token's own number; q's rows are never asked for
+  const double* freqs;       // [R / 2] radians per position
+  int n, total, n_rows, R;   // total = B n
+  int interleaved, inverse;
+  float scale;
+  int tokens, heads_per_block;  // (the launcher's)
+};
+hipError_t launch_rotary(const Shape& s, RotaryArgs a, hipStream_t st);
+// Eviction (evict.hip).  klo_out null: in place.
+struct EvictArgs {
+  const int32_t* seq_lens;
+  float* weights;  // [B, Hkv, S_cap]
+  void *klo, *khi, *v;
+  void *klo_out, *khi_out, *v_out;
+  float* weights_out;
+  int32_t* lens_out;
+  int Hkv, S_cap, S_cap_out, S_max, budget, sinks, recent, nlo;  // nlo: 16-byte chunks of a row of klo
+  Paging pg;       // of the source
+};
+hipError_t launch_evict_select(const Shape& s, const EvictArgs& a, int32_t* list, int32_t* kept, hipStream_t st);
+hipError_t launch_evict_move(const Shape& s, const EvictArgs& a, const int32_t* list, const int32_t* kept, hipStream_t st);
+// Attention over a cache in parts (weigh.hip): parts of a head's result, merged by a launch of its own.
+constexpr int kPartStride = kD + 4;  // o[128], m (of logits times log2 e), l, two unused: rows of whole 16 bytes
+int weigh_splits(const Shape& s);
+size_t weigh_logits_pitch(int S_max);
+// logits [B Hq, pitch] or null; seq_lens entries from 0 on
+hipError_t launch_parts(const Shape& s, int nsplit, int nparts, const void* q, const void* k_full, const void* v, float* partial,
+                        float* logits, hipStream_t st);
+// The sequences' parts, and behind them `shared` parts that every head has; weights_out null: only `out`.
+hipError_t launch_weigh_merge(const Shape& s, int nsplit, int shared, const float* partial, const float* logits,
+                              const float* weights_in, float* weights_out, void* out, hipStream_t st);
+// Attention of every query of the batch over one prefix (shared.hip): parts nsplit .. nsplit + splits - 1 of nparts.
+int prefix_splits(const Shape& s, int prefix_rows);
+hipError_t launch_prefix(const Shape& s, int first, int splits, int nparts, const void* q, const void* k_prefix, const void* v_prefix,
+                         int prefix_rows, int prefix_cap, float* partial, hipStream_t st);
 hipError_t launch_rotate(const Shape& s, const void* k_new, const float* P, void* klo, void* khi,
                          int pos, int n_new, hipStream_t st);
 

@@ -1,0 +1,208 @@
+// Rotary positions for the queries and keys of new tokens (the step in front of Algorithm 1 lines 2-4 of
+// arXiv 2406.02542: q and k are rotated by their positions before they are cached).
+//
+// The first R columns of a head are R / 2 pairs (a, b); pair i of a token at position t becomes
+//   s (a cos - b sin), s (b cos + a sin)   with the angle t f_i (its sign turned for the inverse, which is
+// the gradient of the forward rotation too).  Memory bounds it: every element is read and written once, for
+// about one multiply-add each.
+//
+// A block owns kTokens tokens (or a share of one token's heads when there are few tokens) and works out their
+// R / 2 angles once, into LDS, for all heads.  The angle in quarter turns is reduced in 64 bits: 32 would
+// leave a position of 100 000 with angles off by 4e-3.  A lane group then takes rows (token, head) in turn,
+// each lane two 16-byte chunks that hold both halves of its pairs, four rows in flight.
+#include "common.h"
+
+namespace loki {
+
+constexpr int kRotThreads = 256;
+constexpr int kRotInFlight = 4;
+constexpr int kRotMaxTokens = 4;  // of a block: one angle per thread with 64 pairs
+
+// cos and sin of x quarter turns, |x| reduced here; fp32 results.  Taylor polynomials on [-pi/4, pi/4]: the first
+// term left out is below 2^-29.
+__device__ __forceinline__ float2 cos_sin_quarters(double x) {
+  const double k = rint(x);
+  const float th = (float)(x - k) * 1.57079632679489662f, t2 = th * th;
+  float s = fmaf(t2, 2.7557319224e-6f, -1.9841269841e-4f);
+  s = fmaf(s, t2, 8.3333333333e-3f);
+  s = fmaf(s, t2, -1.6666666667e-1f);
+  s = fmaf(s * t2, th, th);
+  float c = fmaf(t2, -2.7557319224e-7f, 2.4801587302e-5f);
+  c = fmaf(c, t2, -1.3888888889e-3f);
+  c = fmaf(c, t2, 4.1666666667e-2f);
+  c = fmaf(c, t2, -0.5f);
+  c = fmaf(c, t2, 1.0f);
+  const int quarter = (int)((long long)k & 3);
+  const float cs = quarter & 1 ? s : c, sn = quarter & 1 ? c : s;
+  return make_float2(quarter == 1 || quarter == 2 ? -cs : cs, quarter >= 2 ? -sn : sn);
+}
+
+template <typename T>
+__device__ __forceinline__ uint4 pack_chunk(const float (&f)[T::EPC]) {
+  if constexpr (T::EPC == 8)
+    return make_uint4(BF16::round2(f[0], f[1]), BF16::round2(f[2], f[3]), BF16::round2(f[4], f[5]), BF16::round2(f[6], f[7]));
+  else
+    return make_uint4(__float_as_uint(f[0]), __float_as_uint(f[1]), __float_as_uint(f[2]), __float_as_uint(f[3]));
+}
+
+// STYLE: 0 pairs (i, i + R / 2), R / 2 a multiple of a chunk; 1 pairs (2 i, 2 i + 1); 2 as 0, any even R.
+template <typename T, int STYLE>
+__global__ __launch_bounds__(kRotThreads) void rotary_kernel(RotaryArgs a) {
+  using ST = typename T::store_t;
+  constexpr int EPC = T::EPC;
+  constexpr int kLanes = kD / EPC / 2;  // lanes of a row: two chunks each
+  constexpr int kGroups = kRotThreads / kLanes;
+  __shared__ float2 s_cs[kRotMaxTokens][kD / 2];
+  const int tid = threadIdx.x, p = tid % kLanes, gid = tid / kLanes;
+  const int pairs = a.R / 2, tok0 = blockIdx.x * a.tokens, ntok = min(a.tokens, a.total - tok0);
+
+  for (int i = tid; i < ntok * pairs; i += kRotThreads) {
+    const int t = i / pairs, f = i - t * pairs;
+    const double quarters = (double)a.positions[tok0 + t] * (a.freqs[f] * 0.63661977236758134308);  // 2 / pi
+    float2 cs = cos_sin_quarters(quarters);
+    cs.x *= a.scale;
+    cs.y *= a.inverse ? -a.scale : a.scale;
+    s_cs[t][f] = cs;
+  }
+  __syncthreads();
+
+  // the two chunks of this lane: a pair of rotated ones, or two of the columns behind R
+  int c0, c1;
+  if (STYLE == 0) {
+    const int np = pairs / EPC;
+    c0 = p < np ? p : 2 * p;
+    c1 = p < np ? p + np : 2 * p + 1;
+  } else {
+    c0 = p;
+    c1 = p + kLanes;
+  }
+  const int heads = a.q.heads + a.k.heads + a.v.heads;
+  const int h0 = blockIdx.y * a.heads_per_block, hn = min(a.heads_per_block, heads - h0);
+  const int items = ntok * hn;
+
+  for (int i0 = gid; i0 < items; i0 += kGroups * kRotInFlight) {
+    uint4 raw[kRotInFlight][2];
+    ST* dst[kRotInFlight];
+    int tok[kRotInFlight];
+    bool turn[kRotInFlight];
+#pragma unroll
+    for (int u = 0; u < kRotInFlight; ++u) {
+      const int i = i0 + u * kGroups;
+      dst[u] = nullptr;
+      turn[u] = false;
+      tok[u] = 0;
+      raw[u][0] = raw[u][1] = make_uint4(0, 0, 0, 0);
+      if (i < items) {
+        tok[u] = i / hn;
+        int h = h0 + i - tok[u] * hn;
+        const int t = tok0 + tok[u], b = t / a.n, j = t - b * a.n;
+        const bool is_q = h < a.q.heads;
+        if (!is_q) h -= a.q.heads;
+        const bool is_k = !is_q && h < a.k.heads;
+        if (!is_q && !is_k) h -= a.k.heads;
+        const RotaryTensor& x = is_q ? a.q : is_k ? a.k : a.v;
+        int row = j;
+        if (!is_q && a.rows != nullptr) row = a.rows[t];
+        const ST* src = static_cast<const ST*>(x.in) + (b * x.in_batch + j * x.in_token + h * x.in_head);
+        raw[u][0] = load16(src + c0 * EPC);
+        raw[u][1] = load16(src + c1 * EPC);
+        turn[u] = is_q || is_k;
+        if (is_q || a.rows == nullptr || (row >= 0 && row < a.n_rows))
+          dst[u] = static_cast<ST*>(x.out) + (b * x.out_batch + row * x.out_token + h * x.out_head);
+        if constexpr (STYLE == 2) {
+          // partners that no chunk boundary respects, element by element; read before anything of the row is written
+          if (turn[u]) {
+#pragma unroll
+            for (int half = 0; half < 2; ++half) {
+              float x0[EPC];
+              T::unpack(raw[u][half], x0);
+#pragma unroll
+              for (int e = 0; e < EPC; ++e) {
+                const int col = (half ? c1 : c0) * EPC + e;
+                if (col < a.R) {
+                  const bool first = col < pairs;
+                  const float2 cs = s_cs[tok[u]][first ? col : col - pairs];
+                  const float other = T::load1(src + (first ? col + pairs : col - pairs));
+                  x0[e] = first ? x0[e] * cs.x - other * cs.y : x0[e] * cs.x + other * cs.y;
+                }
+              }
+              raw[u][half] = pack_chunk<T>(x0);
+            }
+          }
+        }
+      }
+    }
+#pragma unroll
+    for (int u = 0; u < kRotInFlight; ++u) {
+      if constexpr (STYLE == 0) {
+        if (turn[u] && c1 * EPC < a.R) {
+          float x0[EPC], x1[EPC], y0[EPC], y1[EPC];
+          T::unpack(raw[u][0], x0);
+          T::unpack(raw[u][1], x1);
+#pragma unroll
+          for (int e = 0; e < EPC; ++e) {
+            const float2 cs = s_cs[tok[u]][c0 * EPC + e];
+            y0[e] = x0[e] * cs.x - x1[e] * cs.y;
+            y1[e] = x1[e] * cs.x + x0[e] * cs.y;
+          }
+          raw[u][0] = pack_chunk<T>(y0);
+          raw[u][1] = pack_chunk<T>(y1);
+        }
+      } else if constexpr (STYLE == 1) {
+        if (turn[u]) {
+#pragma unroll
+          for (int half = 0; half < 2; ++half) {
+            float x0[EPC];
+            T::unpack(raw[u][half], x0);
+#pragma unroll
+            for (int e = 0; e < EPC; e += 2) {
+              const int col = (half ? c1 : c0) * EPC + e;
+              if (col < a.R) {
+                const float2 cs = s_cs[tok[u]][col / 2];
+                const float x = x0[e], y = x0[e + 1];
+                x0[e] = x * cs.x - y * cs.y;
+                x0[e + 1] = y * cs.x + x * cs.y;
+              }
+            }
+            raw[u][half] = pack_chunk<T>(x0);
+          }
+        }
+      }
+      if (dst[u] != nullptr) {
+        *reinterpret_cast<uint4*>(dst[u] + c0 * EPC) = raw[u][0];
+        *reinterpret_cast<uint4*>(dst[u] + c1 * EPC) = raw[u][1];
+      }
+    }
+  }
+}
+
+template <typename T>
+static hipError_t launch_rotary_t(const RotaryArgs& a, dim3 grid, int style, hipStream_t st) {
+  const dim3 block(kRotThreads);
+  if (style == 0)
+    hipLaunchKernelGGL((rotary_kernel<T, 0>), grid, block, 0, st, a);
+  else if (style == 1)
+    hipLaunchKernelGGL((rotary_kernel<T, 1>), grid, block, 0, st, a);
+  else
+    hipLaunchKernelGGL((rotary_kernel<T, 2>), grid, block, 0, st, a);
+  return hipGetLastError();
+}
+
+hipError_t launch_rotary(const Shape& s, RotaryArgs a, hipStream_t st) {
+  const int epc = 16 / s.elem_bytes, heads = a.q.heads + a.k.heads + a.v.heads;
+  // few tokens: the heads of a token are spread over blocks until every CU has one or a lane group has one row
+  a.tokens = a.total >= kRotMaxTokens * device_cus() ? kRotMaxTokens : 1;
+  a.heads_per_block = heads;
+  const int groups = kRotThreads / (kD / epc / 2);
+  if (a.tokens == 1) {
+    int splits = device_cus() / a.total;
+    const int most = (heads + groups - 1) / groups;
+    if (splits > most) splits = most;
+    if (splits > 1) a.heads_per_block = (heads + splits - 1) / splits;
+  }
+  const dim3 grid((a.total + a.tokens - 1) / a.tokens, (heads + a.heads_per_block - 1) / a.heads_per_block);
+  const int style = a.interleaved ? 1 : (a.R / 2) % epc == 0 ? 0 : 2;
+  return s.dtype == 0 ? launch_rotary_t<F32>(a, grid, style, st) : launch_rotary_t<BF16>(a, grid, style, st);
+}
+
+}  // namespace loki
