@@ -65,11 +65,273 @@ __global__ __launch_bounds__(kPfThreads) void prefix_kernel(const void* __restri
   }
 }
 
+// ---- bf16, more than 16 query rows per KV head: matrix cores on tiles that the block's waves share -------------
+// A wave holds QG groups of 32 query rows (their columns as operands in registers, 32 a group, and their outputs, 64) and
+// takes steps of 32 keys:
+//   S^T[key, query] = K Q^T      v_mfma_f32_32x32x16_bf16, A = 16 bytes of a key row, B = the queries
+//   weights                      a lane has 16 of the 32 keys of ONE query, so maximum, sum and the rescaling of its outputs
+//                                are the lane's own but for one exchange with lane ^ 32
+//   O^T[column, query] += V^T P^T    B = the weights as they come out of the first product: the order of the keys in a
+//                                product is free, so A takes the same one, rows read column-wise by the transposing LDS load
+// K and V tiles of KT keys go through LDS once for the block's four waves, WQ of which hold different queries and WK = 4 / WQ
+// different keys of the tile; the next tile is loaded into registers while this one is used.  16-byte chunks are stored at
+// places exchanged by the row's number, so that neither the key rows (stride 256 bytes) nor the four rows of a transposing
+// load meet in a bank.
+// The reference of the exponentials follows the running maximum only when that has grown by 2^8: the outputs (half of the
+// registers) are rescaled a few times per run instead of in most steps, and weights up to 2^8 lose nothing in fp32.
+typedef float pf_f32x16_t __attribute__((ext_vector_type(16)));
+typedef short pf_s16x4_t __attribute__((ext_vector_type(4)));
+typedef __attribute__((address_space(3))) pf_s16x4_t pf_lds_s16x4_t;
+constexpr float kPfGrowth = 8.0f;
+
+template <int WQ>
+constexpr int pf_tile_keys() {
+  return WQ == 1 ? 128 : 64;
+}
+
+// LDS: two pairs of tiles; at the end, where waves have other keys of the same queries, what half of them hand over.
+template <int QG, int WQ>
+constexpr int pf_lds_bytes() {
+  const int tiles = 4 * pf_tile_keys<WQ>() * 256, merge = WQ == kPfWaves ? 0 : kPfWaves * QG * 32 * 8 + kPfWaves / 2 * QG * 64 * 256;
+  return tiles > merge ? tiles : merge;
+}
+
+template <int QG, int WQ>
+__global__ __launch_bounds__(kPfThreads, QG == 2 ? 1 : 2) void prefix_mfma_kernel(
+    const uint16_t* __restrict__ k, const uint16_t* __restrict__ v, const uint16_t* __restrict__ qv, float* __restrict__ partial,
+    int M, int G, int Hq, int rows, int cap, int run, int first, int nparts) {
+  constexpr int WK = kPfWaves / WQ, KT = pf_tile_keys<WQ>(), kSteps = KT / (32 * WK), kChunks = KT / 16;
+  constexpr int kTileBytes = KT * 256;
+  extern __shared__ __align__(16) char smem[];  // [2][K tile, V tile]
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int l32 = lane & 31, half = lane >> 5, l16 = lane & 15;
+  const int wq = wave % WQ, wk = wave / WQ;
+  const int split = blockIdx.x, h = blockIdx.z;
+  const int q0 = (blockIdx.y * WQ + wq) * (QG * 32);
+  const int r0 = split * run, r1 = min(rows, r0 + run);
+  const int tiles = (r1 - r0 + KT - 1) / KT;
+
+  am_bf16x8_t q[QG][8];
+#pragma unroll
+  for (int g = 0; g < QG; ++g) {
+    const int r = min(q0 + 32 * g + l32, M - 1);
+    const uint16_t* src = qv + prefix_head(r, h, G, Hq) * kD + 8 * half;
+#pragma unroll
+    for (int ks = 0; ks < 8; ++ks) q[g][ks] = __builtin_bit_cast(am_bf16x8_t, load16(src + 16 * ks));
+  }
+  const uint16_t* kh = k + (size_t)h * cap * kD;
+  const uint16_t* vh = v + (size_t)h * cap * kD;
+
+  uint4 kst[kChunks], vst[kChunks];
+  auto load = [&](int t) __attribute__((always_inline)) {
+#pragma unroll
+    for (int j = 0; j < kChunks; ++j) {
+      const int at = tid + kPfThreads * j;
+      const size_t off = (size_t)min(r0 + t * KT + (at >> 4), r1 - 1) * kD + (at & 15) * 8;  // past the end: the last row again
+      kst[j] = load16(kh + off);
+      vst[j] = load16(vh + off);
+    }
+  };
+  auto store = [&](int b) __attribute__((always_inline)) {
+    char* base = smem + b * 2 * kTileBytes;
+#pragma unroll
+    for (int j = 0; j < kChunks; ++j) {
+      const int at = tid + kPfThreads * j, row = at >> 4, c = at & 15;
+      *reinterpret_cast<uint4*>(base + row * 256 + ((c ^ (row & 15)) * 16)) = kst[j];
+      *reinterpret_cast<uint4*>(base + kTileBytes + row * 256 + ((c ^ ((row & 7) << 1)) * 16)) = vst[j];
+    }
+  };
+
+  float m[QG], l[QG];
+  pf_f32x16_t o[QG][4];
+#pragma unroll
+  for (int g = 0; g < QG; ++g) {
+    m[g] = kNegBig;
+    l[g] = 0.f;
+#pragma unroll
+    for (int c = 0; c < 4; ++c) o[g][c] = pf_f32x16_t{};
+  }
+  const int k_at = l32 * 256 + ((half ^ (l32 & 15)) * 16);
+  const int v_row = 4 * half + (l16 >> 2);
+  const int v_at = kTileBytes + v_row * 256 + (((((lane >> 4) & 1) * 2 + ((l16 & 3) >> 1)) ^ ((v_row & 7) << 1)) * 16) + (l16 & 1) * 8;
+
+  // one step: 32 keys of the tile in buffer `base`, of which the first `there` exist
+  auto step = [&](const char* base, int there) __attribute__((always_inline)) {
+    pf_f32x16_t s[QG];
+#pragma unroll
+    for (int g = 0; g < QG; ++g) s[g] = pf_f32x16_t{};
+#pragma unroll
+    for (int ks = 0; ks < 8; ++ks) {
+      const am_bf16x8_t a = __builtin_bit_cast(am_bf16x8_t, *reinterpret_cast<const uint4*>(base + (k_at ^ (ks * 32))));
+#pragma unroll
+      for (int g = 0; g < QG; ++g) s[g] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, q[g][ks], s[g], 0, 0, 0);
+    }
+    uint32_t hi[QG][8], lo[QG][8];
+#pragma unroll
+    for (int g = 0; g < QG; ++g) {
+      if (there < 32) {  // (uniform: the run's last step)
+#pragma unroll
+        for (int i = 0; i < 16; ++i)
+          if (8 * (i >> 2) + 4 * half + (i & 3) >= there) s[g][i] = kNegBig;
+      }
+      float top = s[g][0];
+#pragma unroll
+      for (int i = 1; i < 16; ++i) top = fmaxf(top, s[g][i]);
+      top = fmaxf(top, __shfl_xor(top, 32)) * kSoftmaxScaleLog2;
+      const bool grown = top > m[g] + kPfGrowth;
+      if (__ballot(grown) != 0ull) {
+        const float mn = grown ? top : m[g], corr = fast_exp2(m[g] - mn);
+        m[g] = mn;
+        l[g] *= corr;
+#pragma unroll
+        for (int c = 0; c < 4; ++c)
+#pragma unroll
+          for (int i = 0; i < 16; ++i) o[g][c][i] *= corr;
+      }
+      float p[16], sum = 0.f;
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        p[i] = fast_exp2(fmaf(s[g][i], kSoftmaxScaleLog2, -m[g]));
+        sum += p[i];
+      }
+      l[g] += sum;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        hi[g][i] = BF16::round2(p[2 * i], p[2 * i + 1]);
+        lo[g][i] = BF16::round2(p[2 * i] - __uint_as_float(hi[g][i] << 16), p[2 * i + 1] - __uint_as_float(hi[g][i] & 0xffff0000u));
+      }
+    }
+#pragma unroll
+    for (int ks = 0; ks < 2; ++ks)
+#pragma unroll
+      for (int c = 0; c < 4; ++c) {
+        const char* at = base + (v_at ^ (c * 64)) + ks * 4096;
+        const pf_s16x4_t x = __builtin_amdgcn_ds_read_tr16_b64_v4i16((pf_lds_s16x4_t*)(at));
+        const pf_s16x4_t y = __builtin_amdgcn_ds_read_tr16_b64_v4i16((pf_lds_s16x4_t*)(at + 2048));
+        const am_bf16x8_t a = __builtin_bit_cast(am_bf16x8_t, __builtin_shufflevector(x, y, 0, 1, 2, 3, 4, 5, 6, 7));
+#pragma unroll
+        for (int g = 0; g < QG; ++g) {
+          const am_bf16x8_t b_lo = __builtin_bit_cast(am_bf16x8_t, make_uint4(lo[g][4 * ks], lo[g][4 * ks + 1], lo[g][4 * ks + 2], lo[g][4 * ks + 3]));
+          const am_bf16x8_t b_hi = __builtin_bit_cast(am_bf16x8_t, make_uint4(hi[g][4 * ks], hi[g][4 * ks + 1], hi[g][4 * ks + 2], hi[g][4 * ks + 3]));
+          o[g][c] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b_lo, o[g][c], 0, 0, 0);
+          o[g][c] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b_hi, o[g][c], 0, 0, 0);
+        }
+      }
+  };
+
+  load(0);
+  store(0);
+  __syncthreads();
+  for (int t = 0; t < tiles; ++t) {
+    if (t + 1 < tiles) load(t + 1);
+    const char* base = smem + (t & 1) * 2 * kTileBytes;
+#pragma unroll
+    for (int s = 0; s < kSteps; ++s) {
+      const int key = (s * WK + wk) * 32, there = r1 - r0 - t * KT - key;
+      if (there > 0) step(base + key * 256, there);  // (uniform for the wave)
+    }
+    if (t + 1 < tiles) store((t + 1) & 1);
+    __syncthreads();
+  }
+
+  // both halves of a query's keys; then the waves that had other keys of the same queries
+#pragma unroll
+  for (int g = 0; g < QG; ++g) l[g] += __shfl_xor(l[g], 32);
+  if constexpr (WK > 1) {
+    float* ml = reinterpret_cast<float*>(smem);  // [wave][QG][32] (max, sum)
+    float4* ob = reinterpret_cast<float4*>(smem + kPfWaves * QG * 32 * 8);  // [wave of the upper half][QG][4][4][lane]
+#pragma unroll
+    for (int g = 0; g < QG; ++g)
+      if (half == 0) *reinterpret_cast<float2*>(ml + ((wave * QG + g) * 32 + l32) * 2) = make_float2(m[g], l[g]);
+    __syncthreads();
+#pragma unroll
+    for (int g = 0; g < QG; ++g) {
+      float mn = kNegBig, ls = 0.f;
+#pragma unroll
+      for (int w = 0; w < WK; ++w) mn = fmaxf(mn, ml[(((w * WQ + wq) * QG + g) * 32 + l32) * 2]);
+#pragma unroll
+      for (int w = 0; w < WK; ++w) {
+        const float2 x = *reinterpret_cast<const float2*>(ml + (((w * WQ + wq) * QG + g) * 32 + l32) * 2);
+        ls = fmaf(x.y, fast_exp2(x.x - mn), ls);
+      }
+      const float f = fast_exp2(m[g] - mn);
+      m[g] = mn;
+      l[g] = ls;
+#pragma unroll
+      for (int c = 0; c < 4; ++c)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) o[g][c][i] *= f;
+    }
+#pragma unroll
+    for (int n = WK / 2; n >= 1; n /= 2) {
+      if (wk >= n && wk < 2 * n) {
+        float4* dst = ob + (size_t)((wk - n) * WQ + wq) * QG * 16 * 64;
+#pragma unroll
+        for (int g = 0; g < QG; ++g)
+#pragma unroll
+          for (int c = 0; c < 4; ++c)
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+              dst[((g * 4 + c) * 4 + i) * 64 + lane] = make_float4(o[g][c][4 * i], o[g][c][4 * i + 1], o[g][c][4 * i + 2], o[g][c][4 * i + 3]);
+      }
+      __syncthreads();
+      if (wk < n) {
+        const float4* src = ob + (size_t)(wk * WQ + wq) * QG * 16 * 64;
+#pragma unroll
+        for (int g = 0; g < QG; ++g)
+#pragma unroll
+          for (int c = 0; c < 4; ++c)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              const float4 x = src[((g * 4 + c) * 4 + i) * 64 + lane];
+              o[g][c][4 * i] += x.x;
+              o[g][c][4 * i + 1] += x.y;
+              o[g][c][4 * i + 2] += x.z;
+              o[g][c][4 * i + 3] += x.w;
+            }
+      }
+      __syncthreads();
+    }
+    if (wk != 0) return;
+  }
+#pragma unroll
+  for (int g = 0; g < QG; ++g) {
+    const int r = q0 + 32 * g + l32;
+    if (r < M) {
+      float* pr = partial + (prefix_head(r, h, G, Hq) * nparts + first + split) * kPartStride;
+#pragma unroll
+      for (int c = 0; c < 4; ++c)
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          *reinterpret_cast<float4*>(pr + 32 * c + 8 * i + 4 * half) =
+              make_float4(o[g][c][4 * i], o[g][c][4 * i + 1], o[g][c][4 * i + 2], o[g][c][4 * i + 3]);
+      if (half == 0) *reinterpret_cast<float2*>(pr + kD) = make_float2(m[g], l[g]);
+    }
+  }
+}
+
+// The block's queries and tiles for M query rows: as few blocks of queries as possible, and waves on different keys where
+// they do not fill four waves.
+struct PrefixShape {
+  int queries, keys, blocks_per_cu;  // of a block; keys: what a run is a multiple of
+};
+static PrefixShape prefix_shape(const Shape& s) {
+  const int M = s.B * s.G;
+  if (s.dtype == 0) return {8, 32, 4};
+  if (M <= 16) return {16, 128, 4};
+  if (M <= 32) return {32, 128, 1};
+  if (M <= 64) return {64, 128, 1};
+  if (M <= 128) return {128, 64, 1};
+  return {256, 64, 1};
+}
+
 static int prefix_run(const Shape& s, int rows) {
-  const int tiles = s.Hkv * ((s.B * s.G + 15) / 16);
-  int n = (4 * device_cus() + tiles - 1) / tiles;
+  const PrefixShape ps = prefix_shape(s);
+  const int tiles = s.Hkv * ((s.B * s.G + ps.queries - 1) / ps.queries);
+  int n = ps.blocks_per_cu * device_cus() / tiles;
+  if (n < 1) n = 1;
   const int run = (rows + n - 1) / n;
-  return (run + 127) / 128 * 128;
+  return (run + ps.keys - 1) / ps.keys * ps.keys;
 }
 
 int prefix_splits(const Shape& s, int prefix_rows) {
@@ -78,16 +340,38 @@ int prefix_splits(const Shape& s, int prefix_rows) {
   return (prefix_rows + run - 1) / run;
 }
 
+template <int QG, int WQ>
+static hipError_t launch_prefix_mfma(const Shape& s, int first, int splits, int nparts, const void* q, const void* k, const void* v,
+                                     int rows, int cap, float* partial, hipStream_t st) {
+  static std::atomic<unsigned long long> raised{0};
+  constexpr int bytes = pf_lds_bytes<QG, WQ>();
+  const hipError_t e = allow_dynamic_lds(reinterpret_cast<const void*>(&prefix_mfma_kernel<QG, WQ>), bytes, raised);
+  if (e != hipSuccess) return e;
+  const int M = s.B * s.G, nq = QG * WQ * 32;
+  hipLaunchKernelGGL((prefix_mfma_kernel<QG, WQ>), dim3(splits, (M + nq - 1) / nq, s.Hkv), dim3(kPfThreads), bytes, st,
+                     static_cast<const uint16_t*>(k), static_cast<const uint16_t*>(v), static_cast<const uint16_t*>(q), partial, M, s.G,
+                     s.Hq, rows, cap, prefix_run(s, rows), first, nparts);
+  return hipGetLastError();
+}
+
 hipError_t launch_prefix(const Shape& s, int first, int splits, int nparts, const void* q, const void* k, const void* v, int rows,
                          int cap, float* partial, hipStream_t st) {
-  const int M = s.B * s.G, run = prefix_run(s, rows);
-  if (s.dtype == 0)
+  const int M = s.B * s.G, run = prefix_run(s, rows), nq = prefix_shape(s).queries;
+  if (s.dtype == 0) {
     hipLaunchKernelGGL((prefix_kernel<F32, 8>), dim3(splits, (M + 7) / 8, s.Hkv), dim3(kPfThreads), 0, st, k, v, q, partial, M, s.G,
                        s.Hq, rows, cap, run, first, nparts);
-  else
-    hipLaunchKernelGGL((prefix_kernel<BF16, 16>), dim3(splits, (M + 15) / 16, s.Hkv), dim3(kPfThreads), 0, st, k, v, q, partial, M,
-                       s.G, s.Hq, rows, cap, run, first, nparts);
-  return hipGetLastError();
+    return hipGetLastError();
+  }
+  switch (nq) {
+    case 16:
+      hipLaunchKernelGGL((prefix_kernel<BF16, 16>), dim3(splits, (M + 15) / 16, s.Hkv), dim3(kPfThreads), 0, st, k, v, q, partial, M,
+                         s.G, s.Hq, rows, cap, run, first, nparts);
+      return hipGetLastError();
+    case 32: return launch_prefix_mfma<1, 1>(s, first, splits, nparts, q, k, v, rows, cap, partial, st);
+    case 64: return launch_prefix_mfma<2, 1>(s, first, splits, nparts, q, k, v, rows, cap, partial, st);
+    case 128: return launch_prefix_mfma<2, 2>(s, first, splits, nparts, q, k, v, rows, cap, partial, st);
+    default: return launch_prefix_mfma<2, 4>(s, first, splits, nparts, q, k, v, rows, cap, partial, st);
+  }
 }
 
 }  // namespace loki
