@@ -117,7 +117,10 @@ __global__ __launch_bounds__(kPfThreads, QG == 2 ? 1 : 2) void prefix_mfma_kerne
     const int r = min(q0 + 32 * g + l32, M - 1);
     const uint16_t* src = qv + prefix_head(r, h, G, Hq) * kD + 8 * half;
 #pragma unroll
-    for (int ks = 0; ks < 8; ++ks) q[g][ks] = __builtin_bit_cast(am_bf16x8_t, load16(src + 16 * ks));
+    for (int ks = 0; ks < 8; ++ks) {
+      q[g][ks] = __builtin_bit_cast(am_bf16x8_t, load16(src + 16 * ks));
+      if constexpr (QG == 2) asm volatile("" : "+a"(q[g][ks]));  // in accumulation registers: the others are for the loads
+    }
   }
   const uint16_t* kh = k + (size_t)h * cap * kD;
   const uint16_t* vh = v + (size_t)h * cap * kD;
@@ -155,8 +158,8 @@ __global__ __launch_bounds__(kPfThreads, QG == 2 ? 1 : 2) void prefix_mfma_kerne
   const int v_row = 4 * half + (l16 >> 2);
   const int v_at = kTileBytes + v_row * 256 + (((((lane >> 4) & 1) * 2 + ((l16 & 3) >> 1)) ^ ((v_row & 7) << 1)) * 16) + (l16 & 1) * 8;
 
-  // one step: 32 keys of the tile in buffer `base`, of which the first `there` exist
-  auto step = [&](const char* base, int there) __attribute__((always_inline)) {
+  // one step: 32 keys of the tile in buffer `base`; ENDS: only the first `there` exist
+  auto step = [&](const char* base, int there, auto ends) __attribute__((always_inline)) {
     pf_f32x16_t s[QG];
 #pragma unroll
     for (int g = 0; g < QG; ++g) s[g] = pf_f32x16_t{};
@@ -169,7 +172,7 @@ __global__ __launch_bounds__(kPfThreads, QG == 2 ? 1 : 2) void prefix_mfma_kerne
     uint32_t hi[QG][8], lo[QG][8];
 #pragma unroll
     for (int g = 0; g < QG; ++g) {
-      if (there < 32) {  // (uniform: the run's last step)
+      if constexpr (decltype(ends)::value) {
 #pragma unroll
         for (int i = 0; i < 16; ++i)
           if (8 * (i >> 2) + 4 * half + (i & 3) >= there) s[g][i] = kNegBig;
@@ -187,6 +190,11 @@ __global__ __launch_bounds__(kPfThreads, QG == 2 ? 1 : 2) void prefix_mfma_kerne
         for (int c = 0; c < 4; ++c)
 #pragma unroll
           for (int i = 0; i < 16; ++i) o[g][c][i] *= corr;
+        // (the outputs stay in accumulation registers on both ways past here: else all of them are copied in every step)
+        if constexpr (QG == 2) {
+#pragma unroll
+          for (int c = 0; c < 4; ++c) asm volatile("" : "+a"(o[g][c]));
+        }
       }
       float p[16], sum = 0.f;
 #pragma unroll
@@ -222,17 +230,19 @@ __global__ __launch_bounds__(kPfThreads, QG == 2 ? 1 : 2) void prefix_mfma_kerne
   load(0);
   store(0);
   __syncthreads();
-  for (int t = 0; t < tiles; ++t) {
-    if (t + 1 < tiles) load(t + 1);
+  for (int t = 0; t < tiles - 1; ++t) {
+    load(t + 1);
     const char* base = smem + (t & 1) * 2 * kTileBytes;
 #pragma unroll
-    for (int s = 0; s < kSteps; ++s) {
-      const int key = (s * WK + wk) * 32, there = r1 - r0 - t * KT - key;
-      if (there > 0) step(base + key * 256, there);  // (uniform for the wave)
-    }
-    if (t + 1 < tiles) store((t + 1) & 1);
+    for (int s = 0; s < kSteps; ++s) step(base + (s * WK + wk) * 32 * 256, 32, std::false_type{});
+    store((t + 1) & 1);
     __syncthreads();
   }
+  for (int s = 0; s < kSteps; ++s) {
+    const int key = (s * WK + wk) * 32, there = r1 - r0 - (tiles - 1) * KT - key;
+    if (there > 0) step(smem + ((tiles - 1) & 1) * 2 * kTileBytes + key * 256, there, std::true_type{});  // (uniform for the wave)
+  }
+  __syncthreads();
 
   // both halves of a query's keys; then the waves that had other keys of the same queries
 #pragma unroll
