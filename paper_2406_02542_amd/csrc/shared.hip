@@ -84,23 +84,23 @@ typedef short pf_s16x4_t __attribute__((ext_vector_type(4)));
 typedef __attribute__((address_space(3))) pf_s16x4_t pf_lds_s16x4_t;
 constexpr float kPfGrowth = 8.0f;
 
-template <int WQ>
+template <int WAVES, int WQ>
 constexpr int pf_tile_keys() {
-  return WQ == 1 ? 128 : 64;
+  return WAVES / WQ == 4 ? 128 : 64;
 }
 
 // LDS: two pairs of tiles; at the end, where waves have other keys of the same queries, what half of them hand over.
-template <int QG, int WQ>
+template <int QG, int WAVES, int WQ>
 constexpr int pf_lds_bytes() {
-  const int tiles = 4 * pf_tile_keys<WQ>() * 256, merge = WQ == kPfWaves ? 0 : kPfWaves * QG * 32 * 8 + kPfWaves / 2 * QG * 64 * 256;
+  const int tiles = 4 * pf_tile_keys<WAVES, WQ>() * 256, merge = WQ == WAVES ? 0 : WAVES * QG * 32 * 8 + WAVES / 2 * QG * 64 * 256;
   return tiles > merge ? tiles : merge;
 }
 
-template <int QG, int WQ>
-__global__ __launch_bounds__(kPfThreads, QG == 2 ? 1 : 2) void prefix_mfma_kernel(
+template <int QG, int WAVES, int WQ>
+__global__ __launch_bounds__(64 * WAVES, QG == 2 ? 1 : 2) void prefix_mfma_kernel(
     const uint16_t* __restrict__ k, const uint16_t* __restrict__ v, const uint16_t* __restrict__ qv, float* __restrict__ partial,
     int M, int G, int Hq, int rows, int cap, int run, int first, int nparts) {
-  constexpr int WK = kPfWaves / WQ, KT = pf_tile_keys<WQ>(), kSteps = KT / (32 * WK), kChunks = KT / 16;
+  constexpr int kThreads = 64 * WAVES, WK = WAVES / WQ, KT = pf_tile_keys<WAVES, WQ>(), kSteps = KT / (32 * WK), kChunks = KT * 16 / kThreads;
   constexpr int kTileBytes = KT * 256;
   extern __shared__ __align__(16) char smem[];  // [2][K tile, V tile]
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -129,7 +129,7 @@ __global__ __launch_bounds__(kPfThreads, QG == 2 ? 1 : 2) void prefix_mfma_kerne
   auto load = [&](int t) __attribute__((always_inline)) {
 #pragma unroll
     for (int j = 0; j < kChunks; ++j) {
-      const int at = tid + kPfThreads * j;
+      const int at = tid + kThreads * j;
       const size_t off = (size_t)min(r0 + t * KT + (at >> 4), r1 - 1) * kD + (at & 15) * 8;  // past the end: the last row again
       kst[j] = load16(kh + off);
       vst[j] = load16(vh + off);
@@ -139,7 +139,7 @@ __global__ __launch_bounds__(kPfThreads, QG == 2 ? 1 : 2) void prefix_mfma_kerne
     char* base = smem + b * 2 * kTileBytes;
 #pragma unroll
     for (int j = 0; j < kChunks; ++j) {
-      const int at = tid + kPfThreads * j, row = at >> 4, c = at & 15;
+      const int at = tid + kThreads * j, row = at >> 4, c = at & 15;
       *reinterpret_cast<uint4*>(base + row * 256 + ((c ^ (row & 15)) * 16)) = kst[j];
       *reinterpret_cast<uint4*>(base + kTileBytes + row * 256 + ((c ^ ((row & 7) << 1)) * 16)) = vst[j];
     }
@@ -249,7 +249,7 @@ __global__ __launch_bounds__(kPfThreads, QG == 2 ? 1 : 2) void prefix_mfma_kerne
   for (int g = 0; g < QG; ++g) l[g] += __shfl_xor(l[g], 32);
   if constexpr (WK > 1) {
     float* ml = reinterpret_cast<float*>(smem);  // [wave][QG][32] (max, sum)
-    float4* ob = reinterpret_cast<float4*>(smem + kPfWaves * QG * 32 * 8);  // [wave of the upper half][QG][4][4][lane]
+    float4* ob = reinterpret_cast<float4*>(smem + WAVES * QG * 32 * 8);  // [wave of the upper half][QG][4][4][lane]
 #pragma unroll
     for (int g = 0; g < QG; ++g)
       if (half == 0) *reinterpret_cast<float2*>(ml + ((wave * QG + g) * 32 + l32) * 2) = make_float2(m[g], l[g]);
@@ -350,15 +350,15 @@ int prefix_splits(const Shape& s, int prefix_rows) {
   return (prefix_rows + run - 1) / run;
 }
 
-template <int QG, int WQ>
+template <int QG, int WAVES, int WQ>
 static hipError_t launch_prefix_mfma(const Shape& s, int first, int splits, int nparts, const void* q, const void* k, const void* v,
                                      int rows, int cap, float* partial, hipStream_t st) {
   static std::atomic<unsigned long long> raised{0};
-  constexpr int bytes = pf_lds_bytes<QG, WQ>();
-  const hipError_t e = allow_dynamic_lds(reinterpret_cast<const void*>(&prefix_mfma_kernel<QG, WQ>), bytes, raised);
+  constexpr int bytes = pf_lds_bytes<QG, WAVES, WQ>();
+  const hipError_t e = allow_dynamic_lds(reinterpret_cast<const void*>(&prefix_mfma_kernel<QG, WAVES, WQ>), bytes, raised);
   if (e != hipSuccess) return e;
   const int M = s.B * s.G, nq = QG * WQ * 32;
-  hipLaunchKernelGGL((prefix_mfma_kernel<QG, WQ>), dim3(splits, (M + nq - 1) / nq, s.Hkv), dim3(kPfThreads), bytes, st,
+  hipLaunchKernelGGL((prefix_mfma_kernel<QG, WAVES, WQ>), dim3(splits, (M + nq - 1) / nq, s.Hkv), dim3(64 * WAVES), bytes, st,
                      static_cast<const uint16_t*>(k), static_cast<const uint16_t*>(v), static_cast<const uint16_t*>(q), partial, M, s.G,
                      s.Hq, rows, cap, prefix_run(s, rows), first, nparts);
   return hipGetLastError();
@@ -377,10 +377,10 @@ hipError_t launch_prefix(const Shape& s, int first, int splits, int nparts, cons
       hipLaunchKernelGGL((prefix_kernel<BF16, 16>), dim3(splits, (M + 15) / 16, s.Hkv), dim3(kPfThreads), 0, st, k, v, q, partial, M,
                          s.G, s.Hq, rows, cap, run, first, nparts);
       return hipGetLastError();
-    case 32: return launch_prefix_mfma<1, 1>(s, first, splits, nparts, q, k, v, rows, cap, partial, st);
-    case 64: return launch_prefix_mfma<2, 1>(s, first, splits, nparts, q, k, v, rows, cap, partial, st);
-    case 128: return launch_prefix_mfma<2, 2>(s, first, splits, nparts, q, k, v, rows, cap, partial, st);
-    default: return launch_prefix_mfma<2, 4>(s, first, splits, nparts, q, k, v, rows, cap, partial, st);
+    case 32: return launch_prefix_mfma<1, 4, 1>(s, first, splits, nparts, q, k, v, rows, cap, partial, st);
+    case 64: return launch_prefix_mfma<2, 4, 1>(s, first, splits, nparts, q, k, v, rows, cap, partial, st);
+    case 128: return launch_prefix_mfma<2, 4, 2>(s, first, splits, nparts, q, k, v, rows, cap, partial, st);
+    default: return launch_prefix_mfma<1, 8, 8>(s, first, splits, nparts, q, k, v, rows, cap, partial, st);
   }
 }
 
