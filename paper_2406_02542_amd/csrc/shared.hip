@@ -10,9 +10,8 @@ constexpr int kPfThreads = 256;
 constexpr int kPfWaves = kPfThreads / 64;
 
 // Row of q (and of the partial results) that query row r of KV head h is: r = b G + g.
-__device__ __forceinline__ size_t prefix_head(int r, int h, int G, int Hq) {
-  const int b = r / G;
-  return (size_t)b * Hq + h * G + (r - b * G);
+__device__ __forceinline__ size_t prefix_head(int r, int h, int G, int Hq) {  // (G is a power of two)
+  return (size_t)(r >> (31 - __builtin_clz(G))) * Hq + h * G + (r & (G - 1));
 }
 
 template <typename T, int NQ>
@@ -82,7 +81,8 @@ __global__ __launch_bounds__(kPfThreads) void prefix_kernel(const void* __restri
 typedef float pf_f32x16_t __attribute__((ext_vector_type(16)));
 typedef short pf_s16x4_t __attribute__((ext_vector_type(4)));
 typedef __attribute__((address_space(3))) pf_s16x4_t pf_lds_s16x4_t;
-constexpr float kPfGrowth = 8.0f;
+typedef __bf16 pf_bf16x2_t __attribute__((ext_vector_type(2)));
+constexpr float kPfGrowth = 256.0f;
 
 template <int WAVES, int WQ>
 constexpr int pf_tile_keys() {
@@ -141,7 +141,7 @@ __global__ __launch_bounds__(64 * WAVES, QG == 2 ? 1 : 2) void prefix_mfma_kerne
     for (int j = 0; j < kChunks; ++j) {
       const int at = tid + kThreads * j, row = at >> 4, c = at & 15;
       *reinterpret_cast<uint4*>(base + row * 256 + ((c ^ (row & 15)) * 16)) = kst[j];
-      *reinterpret_cast<uint4*>(base + kTileBytes + row * 256 + ((c ^ ((row & 7) << 1)) * 16)) = vst[j];
+      *reinterpret_cast<uint4*>(base + kTileBytes + row * 256 + ((c ^ ((row & 3) << 2)) * 16)) = vst[j];
     }
   };
 
@@ -156,20 +156,33 @@ __global__ __launch_bounds__(64 * WAVES, QG == 2 ? 1 : 2) void prefix_mfma_kerne
   }
   const int k_at = l32 * 256 + ((half ^ (l32 & 15)) * 16);
   const int v_row = 4 * half + (l16 >> 2);
-  const int v_at = kTileBytes + v_row * 256 + (((((lane >> 4) & 1) * 2 + ((l16 & 3) >> 1)) ^ ((v_row & 7) << 1)) * 16) + (l16 & 1) * 8;
+  const int v_at = kTileBytes + v_row * 256 + (((((lane >> 4) & 1) * 2 + ((l16 & 3) >> 1)) ^ ((v_row & 3) << 2)) * 16) + (l16 & 1) * 8;
 
   // one step: 32 keys of the tile in buffer `base`; ENDS: only the first `there` exist
   auto step = [&](const char* base, int there, auto ends) __attribute__((always_inline)) {
+    // the operands of a product are asked for together and ahead: left to itself the compiler waits for each in turn
+    am_bf16x8_t ka[8], va[2][4];
+#pragma unroll
+    for (int ks = 0; ks < 8; ++ks) ka[ks] = __builtin_bit_cast(am_bf16x8_t, *reinterpret_cast<const uint4*>(base + (k_at ^ (ks * 32))));
+    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+    for (int ks = 0; ks < 2; ++ks)
+#pragma unroll
+      for (int c = 0; c < 4; ++c) {
+        const char* at = base + (v_at ^ (c * 64)) + ks * 4096;
+        const pf_s16x4_t x = __builtin_amdgcn_ds_read_tr16_b64_v4i16((pf_lds_s16x4_t*)(at));
+        const pf_s16x4_t y = __builtin_amdgcn_ds_read_tr16_b64_v4i16((pf_lds_s16x4_t*)(at + 2048));
+        va[ks][c] = __builtin_bit_cast(am_bf16x8_t, __builtin_shufflevector(x, y, 0, 1, 2, 3, 4, 5, 6, 7));
+      }
     pf_f32x16_t s[QG];
 #pragma unroll
     for (int g = 0; g < QG; ++g) s[g] = pf_f32x16_t{};
 #pragma unroll
-    for (int ks = 0; ks < 8; ++ks) {
-      const am_bf16x8_t a = __builtin_bit_cast(am_bf16x8_t, *reinterpret_cast<const uint4*>(base + (k_at ^ (ks * 32))));
+    for (int ks = 0; ks < 8; ++ks)
 #pragma unroll
-      for (int g = 0; g < QG; ++g) s[g] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, q[g][ks], s[g], 0, 0, 0);
-    }
-    uint32_t hi[QG][8], lo[QG][8];
+      for (int g = 0; g < QG; ++g) s[g] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(ka[ks], q[g][ks], s[g], 0, 0, 0);
+    __builtin_amdgcn_sched_barrier(0);
+    uint32_t w[QG][8];
 #pragma unroll
     for (int g = 0; g < QG; ++g) {
       if constexpr (decltype(ends)::value) {
@@ -177,13 +190,22 @@ __global__ __launch_bounds__(64 * WAVES, QG == 2 ? 1 : 2) void prefix_mfma_kerne
         for (int i = 0; i < 16; ++i)
           if (8 * (i >> 2) + 4 * half + (i & 3) >= there) s[g][i] = kNegBig;
       }
-      float top = s[g][0];
+      float sum;
+      auto weights = [&]() __attribute__((always_inline)) {
+        sum = 0.f;
 #pragma unroll
-      for (int i = 1; i < 16; ++i) top = fmaxf(top, s[g][i]);
-      top = fmaxf(top, __shfl_xor(top, 32)) * kSoftmaxScaleLog2;
-      const bool grown = top > m[g] + kPfGrowth;
-      if (__ballot(grown) != 0ull) {
-        const float mn = grown ? top : m[g], corr = fast_exp2(m[g] - mn);
+        for (int i = 0; i < 8; ++i) {
+          w[g][i] = BF16::round2(fast_exp2(fmaf(s[g][2 * i], kSoftmaxScaleLog2, -m[g])), fast_exp2(fmaf(s[g][2 * i + 1], kSoftmaxScaleLog2, -m[g])));
+          sum = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(pf_bf16x2_t, w[g][i]), __builtin_bit_cast(pf_bf16x2_t, 0x3f803f80u), sum, false);
+        }
+      };
+      weights();
+      if (__ballot(!(sum <= kPfGrowth)) != 0ull) {
+        float top = s[g][0];
+#pragma unroll
+        for (int i = 1; i < 16; ++i) top = fmaxf(top, s[g][i]);
+        top = fmaxf(top, __shfl_xor(top, 32)) * kSoftmaxScaleLog2;
+        const float mn = fmaxf(m[g], top), corr = fast_exp2(m[g] - mn);
         m[g] = mn;
         l[g] *= corr;
 #pragma unroll
@@ -195,36 +217,18 @@ __global__ __launch_bounds__(64 * WAVES, QG == 2 ? 1 : 2) void prefix_mfma_kerne
 #pragma unroll
           for (int c = 0; c < 4; ++c) asm volatile("" : "+a"(o[g][c]));
         }
-      }
-      float p[16], sum = 0.f;
-#pragma unroll
-      for (int i = 0; i < 16; ++i) {
-        p[i] = fast_exp2(fmaf(s[g][i], kSoftmaxScaleLog2, -m[g]));
-        sum += p[i];
+        weights();
       }
       l[g] += sum;
-#pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        hi[g][i] = BF16::round2(p[2 * i], p[2 * i + 1]);
-        lo[g][i] = BF16::round2(p[2 * i] - __uint_as_float(hi[g][i] << 16), p[2 * i + 1] - __uint_as_float(hi[g][i] & 0xffff0000u));
-      }
     }
 #pragma unroll
     for (int ks = 0; ks < 2; ++ks)
 #pragma unroll
-      for (int c = 0; c < 4; ++c) {
-        const char* at = base + (v_at ^ (c * 64)) + ks * 4096;
-        const pf_s16x4_t x = __builtin_amdgcn_ds_read_tr16_b64_v4i16((pf_lds_s16x4_t*)(at));
-        const pf_s16x4_t y = __builtin_amdgcn_ds_read_tr16_b64_v4i16((pf_lds_s16x4_t*)(at + 2048));
-        const am_bf16x8_t a = __builtin_bit_cast(am_bf16x8_t, __builtin_shufflevector(x, y, 0, 1, 2, 3, 4, 5, 6, 7));
+      for (int c = 0; c < 4; ++c)
 #pragma unroll
-        for (int g = 0; g < QG; ++g) {
-          const am_bf16x8_t b_lo = __builtin_bit_cast(am_bf16x8_t, make_uint4(lo[g][4 * ks], lo[g][4 * ks + 1], lo[g][4 * ks + 2], lo[g][4 * ks + 3]));
-          const am_bf16x8_t b_hi = __builtin_bit_cast(am_bf16x8_t, make_uint4(hi[g][4 * ks], hi[g][4 * ks + 1], hi[g][4 * ks + 2], hi[g][4 * ks + 3]));
-          o[g][c] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b_lo, o[g][c], 0, 0, 0);
-          o[g][c] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b_hi, o[g][c], 0, 0, 0);
-        }
-      }
+        for (int g = 0; g < QG; ++g)
+          o[g][c] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
+              va[ks][c], __builtin_bit_cast(am_bf16x8_t, make_uint4(w[g][4 * ks], w[g][4 * ks + 1], w[g][4 * ks + 2], w[g][4 * ks + 3])), o[g][c], 0, 0, 0);
   };
 
   load(0);
@@ -304,19 +308,31 @@ __global__ __launch_bounds__(64 * WAVES, QG == 2 ? 1 : 2) void prefix_mfma_kerne
     }
     if (wk != 0) return;
   }
+  // a lane has four columns of one query at a time: through LDS, so that a store takes four half rows
+  char* mine = smem + wave * 8192;  // [32 queries][64 columns], 16-byte chunks exchanged as the keys'
 #pragma unroll
   for (int g = 0; g < QG; ++g) {
-    const int r = q0 + 32 * g + l32;
-    if (r < M) {
-      float* pr = partial + (prefix_head(r, h, G, Hq) * nparts + first + split) * kPartStride;
 #pragma unroll
-      for (int c = 0; c < 4; ++c)
+    for (int pass = 0; pass < 2; ++pass) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
-          *reinterpret_cast<float4*>(pr + 32 * c + 8 * i + 4 * half) =
-              make_float4(o[g][c][4 * i], o[g][c][4 * i + 1], o[g][c][4 * i + 2], o[g][c][4 * i + 3]);
-      if (half == 0) *reinterpret_cast<float2*>(pr + kD) = make_float2(m[g], l[g]);
+      for (int c = 0; c < 2; ++c)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const pf_f32x16_t& x = o[g][2 * pass + c];
+          *reinterpret_cast<float4*>(mine + l32 * 256 + (((8 * c + 2 * i + half) ^ l16) * 16)) = make_float4(x[4 * i], x[4 * i + 1], x[4 * i + 2], x[4 * i + 3]);
+        }
+      __builtin_amdgcn_wave_barrier();
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        const int row = 4 * j + (lane >> 4), r = q0 + 32 * g + row;
+        const float4 x = *reinterpret_cast<const float4*>(mine + row * 256 + ((l16 ^ (row & 15)) * 16));
+        if (r < M) *reinterpret_cast<float4*>(partial + (prefix_head(r, h, G, Hq) * nparts + first + split) * kPartStride + 64 * pass + 4 * l16) = x;
+      }
+      __builtin_amdgcn_wave_barrier();
     }
+    const int r = q0 + 32 * g + l32;
+    if (half == 0 && r < M)
+      *reinterpret_cast<float2*>(partial + (prefix_head(r, h, G, Hq) * nparts + first + split) * kPartStride + kD) = make_float2(m[g], l[g]);
   }
 }
 
@@ -378,8 +394,8 @@ hipError_t launch_prefix(const Shape& s, int first, int splits, int nparts, cons
                          s.G, s.Hq, rows, cap, run, first, nparts);
       return hipGetLastError();
     case 32: return launch_prefix_mfma<1, 4, 1>(s, first, splits, nparts, q, k, v, rows, cap, partial, st);
-    case 64: return launch_prefix_mfma<2, 4, 1>(s, first, splits, nparts, q, k, v, rows, cap, partial, st);
-    case 128: return launch_prefix_mfma<2, 4, 2>(s, first, splits, nparts, q, k, v, rows, cap, partial, st);
+    case 64: return launch_prefix_mfma<1, 8, 2>(s, first, splits, nparts, q, k, v, rows, cap, partial, st);
+    case 128: return launch_prefix_mfma<1, 8, 4>(s, first, splits, nparts, q, k, v, rows, cap, partial, st);
     default: return launch_prefix_mfma<1, 8, 8>(s, first, splits, nparts, q, k, v, rows, cap, partial, st);
   }
 }

@@ -108,7 +108,59 @@ struct PartList {
   __device__ __forceinline__ const float* at(int i) const { return p + (size_t)(i < live ? i : nsplit + i - live) * kPartStride; }
 };
 
-// blockIdx.x < row_blocks: totals of kMgRows rows; behind them two heads' outputs each.
+// The outputs: a block joins the parts of one head.  32 lanes take a part's row, 16 bytes each, so a block's 8 lane
+// groups go through the parts eight at a time with a running maximum of their own, and meet in LDS.
+template <typename T>
+__device__ __forceinline__ void merge_head(const PartList& pl, typename T::store_t* out) {
+  constexpr int kGroups = kMgThreads / 32, U = 4;
+  __shared__ __align__(16) float s_o[kGroups][kD];
+  __shared__ float2 s_ml[kGroups];
+  const int tid = threadIdx.x, lane = tid & 31, grp = tid >> 5;
+  float m = kNegBig, l = 0.f;
+  float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+  for (int i0 = grp; i0 < pl.n; i0 += kGroups * U) {
+    float2 ml[U];
+    float4 x[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const bool ok = i0 + u * kGroups < pl.n;
+      const float* p = pl.at(ok ? i0 + u * kGroups : i0);
+      ml[u] = *reinterpret_cast<const float2*>(p + kD);
+      x[u] = *reinterpret_cast<const float4*>(p + 4 * lane);
+      if (!ok) ml[u] = make_float2(kNegBig, 0.f);
+    }
+    float mn = m;
+#pragma unroll
+    for (int u = 0; u < U; ++u) mn = fmaxf(mn, ml[u].x);
+    const float c = fast_exp2(m - mn);
+    l *= c;
+    o = make_float4(o.x * c, o.y * c, o.z * c, o.w * c);
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const float f = i0 + u * kGroups < pl.n ? fast_exp2(ml[u].x - mn) : 0.f;
+      l = fmaf(ml[u].y, f, l);
+      o = make_float4(fmaf(x[u].x, f, o.x), fmaf(x[u].y, f, o.y), fmaf(x[u].z, f, o.z), fmaf(x[u].w, f, o.w));
+    }
+    m = mn;
+  }
+  *reinterpret_cast<float4*>(&s_o[grp][4 * lane]) = o;
+  if (lane == 0) s_ml[grp] = make_float2(m, l);
+  __syncthreads();
+  if (tid < kD) {
+    float mn = kNegBig, ls = 0.f, os = 0.f;
+#pragma unroll
+    for (int g = 0; g < kGroups; ++g) mn = fmaxf(mn, s_ml[g].x);
+#pragma unroll
+    for (int g = 0; g < kGroups; ++g) {
+      const float f = fast_exp2(s_ml[g].x - mn);
+      ls = fmaf(s_ml[g].y, f, ls);
+      os = fmaf(s_o[g][tid], f, os);
+    }
+    T::store1(out + tid, ls > 0.f ? os / ls : 0.f);  // (no row at all: zeros)
+  }
+}
+
+// blockIdx.x < row_blocks: totals of kMgRows rows; behind them one head's output each.
 template <typename T, int NH>
 __global__ __launch_bounds__(kMgThreads) void weigh_merge_kernel(const float* __restrict__ partial, const float* __restrict__ logits,
                                                                  size_t pitch, const float* weights_in, float* weights_out,
@@ -118,11 +170,15 @@ __global__ __launch_bounds__(kMgThreads) void weigh_merge_kernel(const float* __
   const int unit = blockIdx.y, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int len = part_rows_held(rg, unit / Hkv, S_max), run = part_run(len, nsplit);
   const int live = (len + run - 1) / run, nparts = nsplit + shared;
-  const bool rows = (int)blockIdx.x < row_blocks;
-  const int r0 = (int)blockIdx.x * kMgRows;
-  if (rows && r0 >= len) return;  // uniform for the block
   const size_t head0 = (size_t)unit * NH;
-  // wave w joins heads w, w + 4, .. : a lane for every 64th part
+  if ((int)blockIdx.x >= row_blocks) {
+    const size_t head = head0 + blockIdx.x - row_blocks;
+    merge_head<T>(PartList{partial + head * nparts * kPartStride, live, nsplit, live + shared}, out + head * kD);
+    return;
+  }
+  const int r0 = (int)blockIdx.x * kMgRows;
+  if (r0 >= len) return;  // uniform for the block
+  // wave w joins the maxima and sums of heads w, w + 4, .. : a lane for every 64th part
   for (int g = wave; g < NH; g += kMgThreads / 64) {
     const PartList pl{partial + (head0 + g) * nparts * kPartStride, live, nsplit, live + shared};
     float m = kNegBig, l = 0.f;
@@ -140,43 +196,22 @@ __global__ __launch_bounds__(kMgThreads) void weigh_merge_kernel(const float* __
     }
     if (lane == 0) {
       s_max[g] = m;
-      s_inv[g] = l > 0.f ? 1.0f / l : 0.f;  // (no row at all: zeros)
+      s_inv[g] = 1.0f / l;
     }
   }
   __syncthreads();
-  if (rows) {
-    const float* lg = logits + head0 * pitch;
-    const size_t w0 = (size_t)unit * S_cap;
+  const float* lg = logits + head0 * pitch;
+  const size_t w0 = (size_t)unit * S_cap;
 #pragma unroll
-    for (int u = 0; u < kMgRows / kMgThreads; ++u) {
-      const int r = r0 + u * kMgThreads + tid;
-      if (r < len) {
-        float w = weights_in != nullptr ? weights_in[w0 + r] : 0.f;
+  for (int u = 0; u < kMgRows / kMgThreads; ++u) {
+    const int r = r0 + u * kMgThreads + tid;
+    if (r < len) {
+      float w = weights_in != nullptr ? weights_in[w0 + r] : 0.f;
 #pragma unroll
-        for (int g = 0; g < NH; ++g) w = fmaf(fast_exp2(lg[g * pitch + r] - s_max[g]), s_inv[g], w);
-        weights_out[w0 + r] = w;
-      }
+      for (int g = 0; g < NH; ++g) w = fmaf(fast_exp2(lg[g * pitch + r] - s_max[g]), s_inv[g], w);
+      weights_out[w0 + r] = w;
     }
-    return;
   }
-  const int g = ((int)blockIdx.x - row_blocks) * (kMgThreads / kD) + tid / kD, col = tid % kD;
-  if (g >= NH) return;
-  const PartList pl{partial + (head0 + g) * nparts * kPartStride, live, nsplit, live + shared};
-  const float M = s_max[g];
-  float o = 0.f;
-  constexpr int U = 8;
-  for (int i0 = 0; i0 < pl.n; i0 += U) {
-    float mi[U], oi[U];
-#pragma unroll
-    for (int u = 0; u < U; ++u) {
-      const float* p = pl.at(min(i0 + u, pl.n - 1));
-      mi[u] = i0 + u < pl.n ? p[kD] : kNegBig;
-      oi[u] = i0 + u < pl.n ? p[col] : 0.f;
-    }
-#pragma unroll
-    for (int u = 0; u < U; ++u) o = fmaf(oi[u], fast_exp2(mi[u] - M), o);
-  }
-  T::store1(out + (head0 + g) * kD + col, o * s_inv[g]);
 }
 
 // Parts of a sequence: about four blocks per CU, of at least 64 rows.
@@ -230,8 +265,7 @@ template <typename T>
 static hipError_t launch_merge_t(const Shape& s, int nsplit, int shared, const float* partial, const float* logits,
                                  const float* weights_in, float* weights_out, void* out, hipStream_t st) {
   const int row_blocks = weights_out != nullptr ? (s.S + kMgRows - 1) / kMgRows : 0;
-  const int per = kMgThreads / kD;
-  const dim3 grid(row_blocks + (s.G + per - 1) / per, s.B * s.Hkv), block(kMgThreads);
+  const dim3 grid(row_blocks + s.G, s.B * s.Hkv), block(kMgThreads);
   auto* o = static_cast<typename T::store_t*>(out);
 #define LOKI_MERGE(NH)                                                                                                     \
   hipLaunchKernelGGL((weigh_merge_kernel<T, NH>), grid, block, 0, st, partial, logits, weigh_logits_pitch(s.S), weights_in, \

@@ -7,15 +7,16 @@ import torch
 DT = {"f32": torch.float32, "bf16": torch.bfloat16}
 
 
-def attend64(q, k, v):
+def attend64(q, k, v, weight_step=2.0 ** -16):
     """q [G, D], k and v [n, D] (any float type): (output [G, D], weights [G, n], bound of the output, bound of a weight
     relative to itself) in 64 bits; n == 0: zeros.
 
     A logit is a sum of D products: in any order its rounding is at most D 2^-24 of the sum of their magnitudes, and two
     roundings of the scale; a weight 2^x moves by that much relative to itself, numerator and denominator, and by the
     exponential's own 2^-22 each, and the denominator by a sum of n terms, of which no chain is longer than n / 8 + 64.  An
-    output is a sum of n products of such weights, with 2^-16 for weights that enter a matrix product in two 16-bit
-    terms of 8 bits each, relative to the sum of the products' magnitudes."""
+    output is a sum of n products of such weights, relative to the sum of the products' magnitudes.  weight_step: what
+    the weights are off as a matrix product takes them: 2^-16 in two bf16 terms of 8 bits each, 2 2^-8 in one (half a
+    step, 2^-8, of every weight in the numerator, and as much in the denominator, which adds up the rounded ones)."""
     n, D = k.shape
     q, k, v = q.double(), k.double(), v.double()
     if n == 0:
@@ -26,7 +27,7 @@ def attend64(q, k, v):
     size = float((q.abs() @ k.abs().t().contiguous()).max()) / math.sqrt(D)
     chain = (n / 8 + 64) * 2.0 ** -24
     rel = 2 * ((D + 2) * 2.0 ** -24 * size + 2.0 ** -22) + chain
-    return p @ v, p, (p @ v.abs()) * (rel + chain + 2.0 ** -16), rel
+    return p @ v, p, (p @ v.abs()) * (rel + chain + weight_step), rel
 
 
 def worst(got, ref, bound, dtype):

@@ -7,6 +7,7 @@ from paper_2406_02542_amd import api
 from tests.attention_bound import DT, attend64, worst
 from tests.test_gpu_evict import kept_rows
 from tests.test_gpu_rotary import turned
+from tests.test_gpu_shared_prefix import ONE_TERM
 
 pytestmark = pytest.mark.gpu
 
@@ -98,6 +99,6 @@ def test_a_batch_behind_a_prefix_is_the_dense_step_over_both(dtype):
     for b in range(B):
         for h in range(Hkv):
             n = P + int(lens[b])
-            ref, _, bound, _ = attend64(last[b, h * G:(h + 1) * G], kk[b, h, :n], vv[b, h, :n])
+            ref, _, bound, _ = attend64(last[b, h * G:(h + 1) * G], kk[b, h, :n], vv[b, h, :n], ONE_TERM[dtype])
             assert worst(out[b, h * G:(h + 1) * G], ref, bound, dtype) <= 0
             assert worst(dense[b, h * G:(h + 1) * G], ref, bound, dtype) <= 0
