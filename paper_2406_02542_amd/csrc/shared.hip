@@ -14,53 +14,179 @@ __device__ __forceinline__ size_t prefix_head(int r, int h, int G, int Hq) {  //
   return (size_t)(r >> (31 - __builtin_clz(G))) * Hq + h * G + (r & (G - 1));
 }
 
-template <typename T, int NQ>
-__global__ __launch_bounds__(kPfThreads) void prefix_kernel(const void* __restrict__ k, const void* __restrict__ v,
-                                                            const void* __restrict__ qv, float* __restrict__ partial, int M, int G,
-                                                            int Hq, int rows, int cap, int run, int first, int nparts) {
-  using ST = typename T::store_t;
-  __shared__ __align__(16) MergeSmem<kPfWaves, NQ> s_merge;
-  const int split = blockIdx.x, q0 = blockIdx.y * NQ, h = blockIdx.z, tid = threadIdx.x;
+// ---- fp32: matrix cores straight from registers ------------------------------------------------------------------
+// A wave takes steps of 16 keys and holds QG groups of 16 query rows:
+//   S^T[key, query] = K Q^T         v_mfma_f32_16x16x4_f32; lane (key, c) loads 16 bytes of its key's row at a time, columns
+//                                   16 j + 4 c .. + 3, one for each of four products, and the queries the same columns
+//   O^T[column, query] += V^T P^T   the weights as they come out of the first product are operand i's keys 4 c + i; lane (m, c)
+//                                   loads 16 bytes of each of these rows, columns 4 m .. + 3 of either half
+// A step's keys and values are in registers before it begins.  The block's waves take steps in turn and are joined in LDS.
+typedef float pf_f32x4_t __attribute__((ext_vector_type(4)));
+constexpr int kPfSteps = 16;       // keys of a step
+constexpr float kPfGrowth = 256.0f;  // the reference of the exponentials follows the maximum when weights sum up to more
+
+template <int QG>
+__global__ __launch_bounds__(kPfThreads, QG == 1 ? 3 : QG == 2 ? 2 : 1) void prefix_f32_kernel(
+    const float* __restrict__ k, const float* __restrict__ v, const float* __restrict__ qv, float* __restrict__ partial, int M, int G,
+    int Hq, int rows, int cap, int run, int first, int nparts) {
+  __shared__ __align__(16) float s_o[kPfWaves / 2][QG][32][64];
+  __shared__ float2 s_ml[kPfWaves][QG][16];
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int l16 = lane & 15, c4 = lane >> 4;
+  const int split = blockIdx.x, h = blockIdx.z, q0 = blockIdx.y * (QG * 16);
   const int r0 = split * run, r1 = min(rows, r0 + run);
-  const ST* q = static_cast<const ST*>(qv);
-  if constexpr (T::EPC == 8) {
-    const int lane = tid & 63, r16 = lane & 15, kgrp = lane >> 4;
-    const bool there = q0 + r16 < M;
-    am_bf16x8_t bq[4][1];
+  const float* kh = k + (size_t)h * cap * kD + 4 * c4;
+  const float* vh = v + (size_t)h * cap * kD + 4 * l16;
+
+  float4 q[QG][8];
 #pragma unroll
-    for (int step = 0; step < 4; ++step) {
-      uint4 raw = load16(q + prefix_head(there ? q0 + r16 : 0, h, G, Hq) * kD + 32 * step + 8 * kgrp);
-      if (!there) raw = make_uint4(0, 0, 0, 0);
-      bq[step][0] = __builtin_bit_cast(am_bf16x8_t, raw);
-    }
-    const AmAddr<4> ad = am_make_addr<4, false>(k, nullptr, v, (size_t)h, cap, kD);
-    AmState st;
-    st.init();
-    am_attend_rows<false, 4, 1, false>(ad, bq, nullptr, r0, AmRoundRobin<kPfWaves>(r0, r1), st, [] {});
-    am_publish<NQ, kPfWaves>(st, s_merge);
-  } else {
-    constexpr int EPC = T::EPC, LPRV = kD / EPC, RPW = 64 / LPRV;
-    const int lane = tid & 63, wave = tid >> 6, c = lane % LPRV;
-    float qr[NQ][EPC];
+  for (int g = 0; g < QG; ++g) {
+    const float* src = qv + prefix_head(min(q0 + 16 * g + l16, M - 1), h, G, Hq) * kD + 4 * c4;
 #pragma unroll
-    for (int g = 0; g < NQ; ++g) T::unpack(load16(q + prefix_head(min(q0 + g, M - 1), h, G, Hq) * kD + c * EPC), qr[g]);
-    const RowAddr ra = make_row_addr<T, false>(k, nullptr, v, (size_t)h, cap, kD, c);
-    AttendAcc<T, NQ> acc;
-    acc.init();
-    attend_rows<T, NQ, kPfWaves * RPW, false, false>(acc, qr, ra, nullptr, nullptr, wave * RPW + lane / LPRV, r0, r1);
-    attend_publish<T, NQ, kPfWaves>(acc, s_merge);
+    for (int j = 0; j < 8; ++j) q[g][j] = *reinterpret_cast<const float4*>(src + 16 * j);
   }
-  for (int i = tid; i < NQ * kD; i += kPfThreads) {
-    const int g = i / kD, col = i % kD;
-    if (q0 + g >= M) continue;
-    float mn, ls, os;
-    attend_merged<kPfWaves, NQ>(s_merge, g, col, mn, ls, os);
-    float* pr = partial + (prefix_head(q0 + g, h, G, Hq) * nparts + first + split) * kPartStride;
-    pr[col] = os;
-    if (col == 0) {
-      pr[kD] = mn;
-      pr[kD + 1] = ls;
+  float m[QG], l[QG];
+  pf_f32x4_t o[QG][8];
+#pragma unroll
+  for (int g = 0; g < QG; ++g) {
+    m[g] = kNegBig;
+    l[g] = 0.f;
+#pragma unroll
+    for (int c = 0; c < 8; ++c) o[g][c] = pf_f32x4_t{};
+  }
+  float4 kr[8], vr[4][2];
+  auto load_k = [&](int at) __attribute__((always_inline)) {  // (past the end: the last row again)
+    const float* p = kh + (size_t)min(at + l16, r1 - 1) * kD;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) kr[j] = *reinterpret_cast<const float4*>(p + 16 * j);
+  };
+  auto load_v = [&](int at) __attribute__((always_inline)) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const float* p = vh + (size_t)min(at + 4 * c4 + i, r1 - 1) * kD;
+      vr[i][0] = *reinterpret_cast<const float4*>(p);
+      vr[i][1] = *reinterpret_cast<const float4*>(p + 64);
     }
+  };
+  int at = r0 + wave * kPfSteps;
+  if (at < r1) {  // (uniform for the wave)
+    load_k(at);
+    load_v(at);
+  }
+  for (; at < r1; at += kPfWaves * kPfSteps) {
+    pf_f32x4_t s[QG];
+#pragma unroll
+    for (int g = 0; g < QG; ++g) s[g] = pf_f32x4_t{};
+#pragma unroll
+    for (int j = 0; j < 8; ++j)
+#pragma unroll
+      for (int g = 0; g < QG; ++g) {
+        s[g] = __builtin_amdgcn_mfma_f32_16x16x4f32(kr[j].x, q[g][j].x, s[g], 0, 0, 0);
+        s[g] = __builtin_amdgcn_mfma_f32_16x16x4f32(kr[j].y, q[g][j].y, s[g], 0, 0, 0);
+        s[g] = __builtin_amdgcn_mfma_f32_16x16x4f32(kr[j].z, q[g][j].z, s[g], 0, 0, 0);
+        s[g] = __builtin_amdgcn_mfma_f32_16x16x4f32(kr[j].w, q[g][j].w, s[g], 0, 0, 0);
+      }
+    load_k(at + kPfWaves * kPfSteps);
+#pragma unroll
+    for (int g = 0; g < QG; ++g) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) s[g][i] = at + 4 * c4 + i < r1 ? s[g][i] * kSoftmaxScaleLog2 : kNegBig;
+      float p[4], sum;
+      auto weights = [&]() __attribute__((always_inline)) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) p[i] = fast_exp2(s[g][i] - m[g]);
+        sum = (p[0] + p[1]) + (p[2] + p[3]);
+      };
+      weights();
+      if (__ballot(!(sum <= kPfGrowth)) != 0ull) {
+        float top = fmaxf(fmaxf(s[g][0], s[g][1]), fmaxf(s[g][2], s[g][3]));
+        top = fmaxf(top, __shfl_xor(top, 16));
+        top = fmaxf(top, __shfl_xor(top, 32));
+        const float mn = fmaxf(m[g], top), corr = fast_exp2(m[g] - mn);
+        m[g] = mn;
+        l[g] *= corr;
+#pragma unroll
+        for (int c = 0; c < 8; ++c)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) o[g][c][i] *= corr;
+        weights();
+      }
+      l[g] += sum;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) s[g][i] = p[i];
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+      for (int g = 0; g < QG; ++g)
+#pragma unroll
+        for (int c = 0; c < 2; ++c) {
+          o[g][4 * c] = __builtin_amdgcn_mfma_f32_16x16x4f32(vr[i][c].x, s[g][i], o[g][4 * c], 0, 0, 0);
+          o[g][4 * c + 1] = __builtin_amdgcn_mfma_f32_16x16x4f32(vr[i][c].y, s[g][i], o[g][4 * c + 1], 0, 0, 0);
+          o[g][4 * c + 2] = __builtin_amdgcn_mfma_f32_16x16x4f32(vr[i][c].z, s[g][i], o[g][4 * c + 2], 0, 0, 0);
+          o[g][4 * c + 3] = __builtin_amdgcn_mfma_f32_16x16x4f32(vr[i][c].w, s[g][i], o[g][4 * c + 3], 0, 0, 0);
+        }
+    load_v(at + kPfWaves * kPfSteps);
+  }
+
+  // the four waves' shares of the keys
+#pragma unroll
+  for (int g = 0; g < QG; ++g) {
+    l[g] += __shfl_xor(l[g], 16);
+    l[g] += __shfl_xor(l[g], 32);
+    if (c4 == 0) s_ml[wave][g][l16] = make_float2(m[g], l[g]);
+  }
+  __syncthreads();
+#pragma unroll
+  for (int g = 0; g < QG; ++g) {
+    float mn = kNegBig, ls = 0.f;
+#pragma unroll
+    for (int w = 0; w < kPfWaves; ++w) mn = fmaxf(mn, s_ml[w][g][l16].x);
+#pragma unroll
+    for (int w = 0; w < kPfWaves; ++w) ls = fmaf(s_ml[w][g][l16].y, fast_exp2(s_ml[w][g][l16].x - mn), ls);
+    const float f = fast_exp2(m[g] - mn);
+    m[g] = mn;
+    l[g] = ls;
+#pragma unroll
+    for (int c = 0; c < 8; ++c)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) o[g][c][i] *= f;
+  }
+#pragma unroll
+  for (int n = kPfWaves / 2; n >= 1; n /= 2) {
+    if (wave >= n && wave < 2 * n) {
+#pragma unroll
+      for (int g = 0; g < QG; ++g)
+#pragma unroll
+        for (int c = 0; c < 8; ++c)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) s_o[wave - n][g][4 * c + i][lane] = o[g][c][i];
+    }
+    __syncthreads();
+    if (wave < n) {
+#pragma unroll
+      for (int g = 0; g < QG; ++g)
+#pragma unroll
+        for (int c = 0; c < 8; ++c)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) o[g][c][i] += s_o[wave][g][4 * c + i][lane];
+    }
+    __syncthreads();
+  }
+  if (wave != 0) return;
+  // o[4 c + t][i] is column 64 c + 4 (4 c4 + i) + t of query l16
+#pragma unroll
+  for (int g = 0; g < QG; ++g) {
+    const int r = q0 + 16 * g + l16;
+    if (r >= M) continue;
+    float* pr = partial + (prefix_head(r, h, G, Hq) * nparts + first + split) * kPartStride;
+#pragma unroll
+    for (int c = 0; c < 2; ++c)
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        *reinterpret_cast<float4*>(pr + 64 * c + 16 * c4 + 4 * i) =
+            make_float4(o[g][4 * c][i], o[g][4 * c + 1][i], o[g][4 * c + 2][i], o[g][4 * c + 3][i]);
+    if (c4 == 0) *reinterpret_cast<float2*>(pr + kD) = make_float2(m[g], l[g]);
   }
 }
 
@@ -82,7 +208,6 @@ typedef float pf_f32x16_t __attribute__((ext_vector_type(16)));
 typedef short pf_s16x4_t __attribute__((ext_vector_type(4)));
 typedef __attribute__((address_space(3))) pf_s16x4_t pf_lds_s16x4_t;
 typedef __bf16 pf_bf16x2_t __attribute__((ext_vector_type(2)));
-constexpr float kPfGrowth = 256.0f;
 
 template <int WAVES, int WQ>
 constexpr int pf_tile_keys() {
@@ -343,8 +468,7 @@ struct PrefixShape {
 };
 static PrefixShape prefix_shape(const Shape& s) {
   const int M = s.B * s.G;
-  if (s.dtype == 0) return {8, 32, 4};
-  if (M <= 16) return {16, 128, 4};
+  if (s.dtype == 0) return M <= 16 ? PrefixShape{16, 64, 3} : M <= 32 ? PrefixShape{32, 64, 2} : PrefixShape{64, 64, 1};
   if (M <= 32) return {32, 128, 1};
   if (M <= 64) return {64, 128, 1};
   if (M <= 128) return {128, 64, 1};
@@ -380,24 +504,30 @@ static hipError_t launch_prefix_mfma(const Shape& s, int first, int splits, int 
   return hipGetLastError();
 }
 
+template <int QG>
+static hipError_t launch_prefix_f32(const Shape& s, int first, int splits, int nparts, const void* q, const void* k, const void* v,
+                                    int rows, int cap, float* partial, hipStream_t st) {
+  const int M = s.B * s.G, nq = QG * 16;
+  hipLaunchKernelGGL((prefix_f32_kernel<QG>), dim3(splits, (M + nq - 1) / nq, s.Hkv), dim3(kPfThreads), 0, st,
+                     static_cast<const float*>(k), static_cast<const float*>(v), static_cast<const float*>(q), partial, M, s.G, s.Hq,
+                     rows, cap, prefix_run(s, rows), first, nparts);
+  return hipGetLastError();
+}
+
 hipError_t launch_prefix(const Shape& s, int first, int splits, int nparts, const void* q, const void* k, const void* v, int rows,
                          int cap, float* partial, hipStream_t st) {
-  const int M = s.B * s.G, run = prefix_run(s, rows), nq = prefix_shape(s).queries;
+  const int nq = prefix_shape(s).queries;
+#define LOKI_PREFIX(f) return f(s, first, splits, nparts, q, k, v, rows, cap, partial, st)
   if (s.dtype == 0) {
-    hipLaunchKernelGGL((prefix_kernel<F32, 8>), dim3(splits, (M + 7) / 8, s.Hkv), dim3(kPfThreads), 0, st, k, v, q, partial, M, s.G,
-                       s.Hq, rows, cap, run, first, nparts);
-    return hipGetLastError();
+    if (nq == 16) LOKI_PREFIX(launch_prefix_f32<1>);
+    if (nq == 32) LOKI_PREFIX(launch_prefix_f32<2>);
+    LOKI_PREFIX(launch_prefix_f32<4>);
   }
-  switch (nq) {
-    case 16:
-      hipLaunchKernelGGL((prefix_kernel<BF16, 16>), dim3(splits, (M + 15) / 16, s.Hkv), dim3(kPfThreads), 0, st, k, v, q, partial, M,
-                         s.G, s.Hq, rows, cap, run, first, nparts);
-      return hipGetLastError();
-    case 32: return launch_prefix_mfma<1, 4, 1>(s, first, splits, nparts, q, k, v, rows, cap, partial, st);
-    case 64: return launch_prefix_mfma<1, 8, 2>(s, first, splits, nparts, q, k, v, rows, cap, partial, st);
-    case 128: return launch_prefix_mfma<1, 8, 4>(s, first, splits, nparts, q, k, v, rows, cap, partial, st);
-    default: return launch_prefix_mfma<1, 8, 8>(s, first, splits, nparts, q, k, v, rows, cap, partial, st);
-  }
+  if (nq == 32) LOKI_PREFIX((launch_prefix_mfma<1, 4, 1>));
+  if (nq == 64) LOKI_PREFIX((launch_prefix_mfma<1, 8, 2>));
+  if (nq == 128) LOKI_PREFIX((launch_prefix_mfma<1, 8, 4>));
+  LOKI_PREFIX((launch_prefix_mfma<1, 8, 8>));
+#undef LOKI_PREFIX
 }
 
 }  // namespace loki
