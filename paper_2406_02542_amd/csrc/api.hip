@@ -773,17 +773,22 @@ static int check_dense_layout(const loki_layout* layout, Shape* s) {
 }
 
 struct PartsPlan {
-  float *partial, *logits;
+  float *partial, *prefix, *logits;
   size_t total;
 };
-// Parts of every head's result and, for the weights, every row's logits.
-static PartsPlan plan_parts(const Shape& s, int nparts, bool weights, void* base) {
+// Parts of every head's result, nsplit of its sequence and `shared` of the prefix, and for the weights every row's logits.
+static PartsPlan plan_parts(const Shape& s, int nsplit, int shared, bool weights, void* base) {
   PartsPlan w{};
   const size_t heads = (size_t)s.B * s.Hq;
-  const size_t parts = align_up(heads * nparts * kPartStride * sizeof(float), 256);
-  w.partial = static_cast<float*>(base);
-  w.logits = base && weights ? reinterpret_cast<float*>(static_cast<char*>(base) + parts) : nullptr;
-  w.total = parts + (weights ? align_up(heads * weigh_logits_pitch(s.S) * sizeof(float), 256) : 0);
+  const size_t own = align_up(heads * nsplit * kPartStride * sizeof(float), 256);
+  const size_t prefix = align_up(heads * shared * kPartStride * sizeof(float), 256);
+  char* p = static_cast<char*>(base);
+  if (p) {
+    w.partial = reinterpret_cast<float*>(p);
+    w.prefix = reinterpret_cast<float*>(p + own);
+    w.logits = weights ? reinterpret_cast<float*>(p + own + prefix) : nullptr;
+  }
+  w.total = own + prefix + (weights ? align_up(heads * weigh_logits_pitch(s.S) * sizeof(float), 256) : 0);
   return w;
 }
 
@@ -793,7 +798,7 @@ int dense_weights_workspace_bytes(const loki_layout* layout, int S_max, size_t* 
   if (rc != LOKI_OK) return rc;
   if (!bytes || S_max < 1 || S_max > s.S_cap) return LOKI_ERR_INVALID_ARG;
   s.S = S_max;
-  *bytes = plan_parts(s, weigh_splits(s), true, nullptr).total;
+  *bytes = plan_parts(s, weigh_splits(s), 0, true, nullptr).total;
   return LOKI_OK;
 }
 
@@ -811,16 +816,16 @@ int dense_decode_weights(const loki_layout* layout, const void* q, const void* k
   s.S = S_max;
   s.rg.seq_lens = seq_lens;
   const int nsplit = weigh_splits(s);
-  const PartsPlan w = plan_parts(s, nsplit, true, workspace);
+  const PartsPlan w = plan_parts(s, nsplit, 0, true, workspace);
   if (w.total > workspace_bytes) return LOKI_ERR_WORKSPACE;
   hipStream_t st = static_cast<hipStream_t>(stream);
   StageTimer tm(st);
   tm.begin("dense_parts");
-  hipError_t e = launch_parts(s, nsplit, nsplit, q, k_full, v, w.partial, w.logits, st);
+  hipError_t e = launch_parts(s, nsplit, q, k_full, v, w.partial, w.logits, st);
   tm.end();
   if (e != hipSuccess) return LOKI_ERR_HIP;
   tm.begin("weigh_merge");
-  e = launch_weigh_merge(s, nsplit, 0, w.partial, w.logits, weights_in, weights_out, out, st);
+  e = launch_weigh_merge(s, nsplit, 0, w.partial, nullptr, w.logits, weights_in, weights_out, out, st);
   tm.end();
   return e == hipSuccess ? LOKI_OK : LOKI_ERR_HIP;
 }
@@ -905,7 +910,7 @@ int dense_shared_workspace_bytes(const loki_layout* layout, int prefix_rows, int
   if (rc != LOKI_OK) return rc;
   if (!bytes || prefix_rows < 0 || S_max < 0 || S_max > s.S_cap) return LOKI_ERR_INVALID_ARG;
   s.S = S_max;
-  *bytes = plan_parts(s, (S_max > 0 ? weigh_splits(s) : 0) + prefix_splits(s, prefix_rows), false, nullptr).total;
+  *bytes = plan_parts(s, S_max > 0 ? weigh_splits(s) : 0, prefix_splits(s, prefix_rows), false, nullptr).total;
   return LOKI_OK;
 }
 
@@ -924,25 +929,25 @@ int dense_decode_shared(const loki_layout* layout, const void* q, const void* k_
   s.S = S_max;
   s.rg.seq_lens = seq_lens;
   const int nsplit = S_max > 0 ? weigh_splits(s) : 0, shared = prefix_splits(s, prefix_rows);
-  const PartsPlan w = plan_parts(s, nsplit + shared, false, workspace);
+  const PartsPlan w = plan_parts(s, nsplit, shared, false, workspace);
   if (w.total > workspace_bytes) return LOKI_ERR_WORKSPACE;
   hipStream_t st = static_cast<hipStream_t>(stream);
   StageTimer tm(st);
   hipError_t e = hipSuccess;
   if (shared > 0) {
     tm.begin("prefix_parts");
-    e = launch_prefix(s, nsplit, shared, nsplit + shared, q, k_prefix, v_prefix, prefix_rows, prefix_cap, w.partial, st);
+    e = launch_prefix(s, shared, q, k_prefix, v_prefix, prefix_rows, prefix_cap, w.prefix, st);
     tm.end();
     if (e != hipSuccess) return LOKI_ERR_HIP;
   }
   if (nsplit > 0) {
     tm.begin("dense_parts");
-    e = launch_parts(s, nsplit, nsplit + shared, q, k_full, v, w.partial, nullptr, st);
+    e = launch_parts(s, nsplit, q, k_full, v, w.partial, nullptr, st);
     tm.end();
     if (e != hipSuccess) return LOKI_ERR_HIP;
   }
   tm.begin("merge");
-  e = launch_weigh_merge(s, nsplit, shared, w.partial, nullptr, nullptr, nullptr, out, st);
+  e = launch_weigh_merge(s, nsplit, shared, w.partial, w.prefix, nullptr, nullptr, nullptr, out, st);
   tm.end();
   return e == hipSuccess ? LOKI_OK : LOKI_ERR_HIP;
 }

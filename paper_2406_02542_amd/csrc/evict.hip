@@ -20,14 +20,26 @@ __device__ __forceinline__ int evict_rows(const int32_t* seq_lens, int b, int S_
   return seq_lens == nullptr ? S_max : min(max(seq_lens[b], 0), S_max);
 }
 
+// A row as the selection sees it: kForced goes on whatever happens, kNoRow is none (or one whose total does not count).
+constexpr uint32_t kNoRow = 0u, kForced = 0xffffffffu;
+constexpr uint32_t kZeroTotal = 0x80000000u;  // float_to_key(0)
+
+// What the waves before this one hold, of s_wave[wave].
+__device__ __forceinline__ uint32_t before_wave(const uint32_t* s_wave, int wave) {
+  const int lane = threadIdx.x & 63;
+  const uint32_t x = lane < kEvWaves ? s_wave[lane] : 0u;
+  const uint32_t incl = wave_inclusive_scan_u32(x);
+  return (uint32_t)(__builtin_amdgcn_readlane((int)incl, wave) - __builtin_amdgcn_readlane((int)x, wave));
+}
+
 // NK: keys per lane held in registers (rows up to 1024 NK); 0: read again in every pass.
 template <int NK>
 __global__ __launch_bounds__(kEvThreads) void evict_select_kernel(EvictArgs a, int32_t* __restrict__ list /* [units, budget] */,
                                                                   int32_t* __restrict__ kept_rows /* [units] */) {
   __shared__ uint32_t s_hist[kEvBins];
-  __shared__ uint32_t s_wave[kEvWaves];
-  __shared__ uint32_t s_pick[2];
-  const int unit = blockIdx.x, b = unit / a.Hkv, h = unit - b * a.Hkv;
+  __shared__ uint32_t s_wave[2][kEvWaves];
+  __shared__ uint32_t s_pick[3];
+  const int unit = blockIdx.x, b = unit / a.Hkv;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int len = evict_rows(a.seq_lens, b, a.S_max), kept = min(len, a.budget);
   int32_t* out = list + (size_t)unit * a.budget;
@@ -37,21 +49,26 @@ __global__ __launch_bounds__(kEvThreads) void evict_select_kernel(EvictArgs a, i
     for (int i = tid; i < len; i += kEvThreads) out[i] = i;
     return;
   }
-  const int c0 = a.sinks, c1 = len - a.recent;  // rows whose totals decide: at least one, len > budget
+  const int c0 = a.sinks, c1 = len - a.recent;  // rows whose totals decide: more than are needed, as len > budget
   const uint32_t need = (uint32_t)(a.budget - a.sinks - a.recent);
 
   // wave w holds rows [w seg, (w + 1) seg), lane by lane in rounds of 64
-  const int seg = ((len + kEvThreads - 1) / kEvThreads) * 64, rounds = seg / 64, first = wave * seg + lane;
+  const int rounds = (len + kEvThreads - 1) / kEvThreads, first = wave * rounds * 64 + lane;
   const float* w = a.weights + (size_t)unit * a.S_cap;
-  auto load = [&](int i) -> uint32_t {
+  // (no branch around the loads: each would be waited for by itself)
+  auto load = [&](int i) -> float { return w[min(first + 64 * i, len - 1)]; };
+  auto key_of = [&](int i, float x) -> uint32_t {
     const int row = first + 64 * i;
-    const bool in = row >= c0 && row < c1;
-    return in ? max(float_to_key(w[row]), 1u) : 0u;  // 0: no candidate
+    const uint32_t key = min(max(float_to_key(x), 1u), kForced - 1u);
+    return row >= len ? kNoRow : row >= c0 && row < c1 ? key : kForced;
   };
   uint32_t reg[NK > 0 ? NK : 1];
   if constexpr (NK > 0) {
+    float x[NK];
 #pragma unroll
-    for (int i = 0; i < NK; ++i) reg[i] = i < rounds ? load(i) : 0u;
+    for (int i = 0; i < NK; ++i) x[i] = load(i);
+#pragma unroll
+    for (int i = 0; i < NK; ++i) reg[i] = key_of(i, x[i]);
   }
   auto each = [&](auto f) __attribute__((always_inline)) {  // f(round, key), in ascending order of the wave's rows
     if constexpr (NK > 0) {
@@ -59,84 +76,83 @@ __global__ __launch_bounds__(kEvThreads) void evict_select_kernel(EvictArgs a, i
       for (int i = 0; i < NK; ++i)
         if (i < rounds) f(i, reg[i]);
     } else {
-      for (int i = 0; i < rounds; ++i) f(i, load(i));
+      for (int i = 0; i < rounds; ++i) f(i, key_of(i, load(i)));
     }
   };
 
   // The need-th largest key, digit by digit.  Rows of total zero, of which a cache can hold many, are counted by
-  // ballots: as atomics they would queue at one bin.
-  uint32_t prefix = 0, left = need;  // left: how many of the keys that begin with `prefix` are kept
-  const uint32_t zero_key = 0x80000000u;
-  bool all = need == 0u;
+  // ballots, once: as atomics they would queue at one bin.
+  uint32_t last = kForced - 1u, equal_kept = 0u;  // kept: keys above `last`, and the first equal_kept of those equal to it
+  bool all_equal = true;                          // (which are all of them)
+  if (need > 0u) {
+    uint32_t prefix = 0u, left = need, zeros = 0u;  // left: how many of the keys that begin with `prefix` are kept
 #pragma unroll
-  for (int pass = 0; pass < 3; ++pass) {
-    const int shift = pass == 0 ? 21 : pass == 1 ? 10 : 0;
-    const uint32_t mask = pass == 2 ? 0x3ffu : 0x7ffu;
-    if (all) break;  // (uniform: `need` is the block's)
-    s_hist[tid] = 0u;
-    s_hist[tid + kEvThreads] = 0u;
-    __syncthreads();
-    uint32_t zeros = 0;
-    each([&](int, uint32_t key) {
-      const bool hit = key != 0u && (pass == 0 || (key >> (pass == 1 ? 21 : 10)) == prefix);
-      zeros += (uint32_t)__popcll(__ballot(hit && key == zero_key));
-      if (hit && key != zero_key) atomicAdd(&s_hist[(key >> shift) & mask], 1u);
-    });
-    if (lane == 0 && zeros != 0u) atomicAdd(&s_hist[(zero_key >> shift) & mask], zeros);
-    __syncthreads();
-    // thread t owns the bins 2047 - 2 t and 2046 - 2 t: the keys of a larger bin come before them
-    const int hi = kEvBins - 1 - 2 * tid;
-    const uint32_t n_hi = s_hist[hi], n_lo = s_hist[hi - 1];
-    const uint32_t incl = wave_inclusive_scan_u32(n_hi + n_lo);
-    if (lane == 63) s_wave[wave] = incl;
-    __syncthreads();
-    uint32_t before = incl - (n_hi + n_lo);
-    for (int i = 0; i < wave; ++i) before += s_wave[i];
-    if (before < left && left <= before + n_hi) {
-      s_pick[0] = (uint32_t)hi;
-      s_pick[1] = left - before;
-    } else if (before + n_hi < left && left <= before + n_hi + n_lo) {
-      s_pick[0] = (uint32_t)(hi - 1);
-      s_pick[1] = left - before - n_hi;
+    for (int pass = 0; pass < 3; ++pass) {
+      const int shift = pass == 0 ? 21 : pass == 1 ? 10 : 0;
+      const uint32_t mask = pass == 2 ? 0x3ffu : 0x7ffu;
+      s_hist[tid] = 0u;
+      s_hist[tid + kEvThreads] = 0u;
+      __syncthreads();
+      each([&](int, uint32_t key) {
+        if (pass == 0) {
+          zeros += (uint32_t)__popcll(__ballot(key == kZeroTotal));
+          if (key - 1u < kForced - 1u && key != kZeroTotal) atomicAdd(&s_hist[key >> 21], 1u);
+        } else if ((key >> (pass == 1 ? 21 : 10)) == prefix && key != kForced && key != kZeroTotal) {
+          atomicAdd(&s_hist[(key >> shift) & mask], 1u);
+        }
+      });
+      if (lane == 0 && zeros != 0u && (pass == 0 || (kZeroTotal >> (pass == 1 ? 21 : 10)) == prefix))
+        atomicAdd(&s_hist[(kZeroTotal >> shift) & mask], zeros);
+      __syncthreads();
+      // thread t owns the bins 2047 - 2 t and 2046 - 2 t: the keys of a larger bin come before them
+      const int hi = kEvBins - 1 - 2 * tid;
+      const uint2 n = *reinterpret_cast<const uint2*>(&s_hist[hi - 1]);  // (x: the lower bin)
+      const uint32_t incl = wave_inclusive_scan_u32(n.x + n.y);
+      if (lane == 63) s_wave[pass & 1][wave] = incl;
+      __syncthreads();
+      const uint32_t before = before_wave(s_wave[pass & 1], wave) + incl - (n.x + n.y);
+      if (before < left && left <= before + n.x + n.y) {
+        const bool upper = left <= before + n.y;
+        s_pick[0] = (uint32_t)(upper ? hi : hi - 1);
+        s_pick[1] = left - before - (upper ? 0u : n.y);
+        s_pick[2] = upper ? n.y : n.x;
+      }
+      __syncthreads();
+      prefix = pass == 0 ? s_pick[0] : pass == 1 ? (prefix << 11) | s_pick[0] : (prefix << 10) | s_pick[0];
+      left = s_pick[1];
     }
-    __syncthreads();
-    prefix = pass == 0 ? s_pick[0] : pass == 1 ? (prefix << 11) | s_pick[0] : (prefix << 10) | s_pick[0];
-    left = s_pick[1];
-    __syncthreads();
+    last = prefix;
+    equal_kept = left;
+    all_equal = s_pick[2] == left;
   }
-  const uint32_t last = all ? 0xffffffffu : prefix;  // kept: keys above it, and the first `left` equal to it
-  const uint32_t equal_kept = all ? 0u : left;
 
-  // kept rows and equal keys of every wave's segment, then each wave writes its part of the list
-  auto kind = [&](int i, uint32_t key, bool& sure, bool& equal) {
-    const int row = first + 64 * i;
-    sure = row < len && (row < c0 || row >= c1 || (!all && key > last));
-    equal = !all && key == last && key != 0u;
-  };
+  // kept rows of every wave's segment, then each wave writes its part of the list; equal keys that do not all stay are
+  // counted too
+  if (all_equal && need > 0u) --last;  // (a key is at least 1) all of them are above it then
   uint32_t n_sure = 0, n_equal = 0;
-  each([&](int i, uint32_t key) {
-    bool sure, equal;
-    kind(i, key, sure, equal);
-    n_sure += (uint32_t)__popcll(__ballot(sure));
-    n_equal += (uint32_t)__popcll(__ballot(equal));
-  });
+  each([&](int, uint32_t key) { n_sure += (uint32_t)__popcll(__ballot(key > last)); });
+  if (!all_equal) each([&](int, uint32_t key) { n_equal += (uint32_t)__popcll(__ballot(key == last)); });
+  __syncthreads();
   if (lane == 0) {
-    s_wave[wave] = n_sure;
-    s_hist[wave] = n_equal;
+    s_wave[0][wave] = n_sure;
+    s_wave[1][wave] = n_equal;
   }
   __syncthreads();
-  uint32_t at = 0, eq = 0;  // list entries and equal keys before this wave's segment
-  for (int i = 0; i < wave; ++i) {
-    const uint32_t e = s_hist[i];
-    at += s_wave[i] + (min(eq + e, equal_kept) - min(eq, equal_kept));
-    eq += e;
+  uint32_t at = before_wave(s_wave[0], wave);
+  if (all_equal) {
+    each([&](int i, uint32_t key) {
+      const unsigned long long m = __ballot(key > last);
+      if (key > last) out[at + __builtin_amdgcn_mbcnt_hi((uint32_t)(m >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)m, 0u))] = first + 64 * i;
+      at += (uint32_t)__popcll(m);
+    });
+    return;
   }
+  uint32_t eq = before_wave(s_wave[1], wave);  // equal keys before this wave's segment; as many of them stay as there is room for
+  at += min(eq, equal_kept);
   const unsigned long long below = (1ull << lane) - 1ull;
   each([&](int i, uint32_t key) {
-    bool sure, equal;
-    kind(i, key, sure, equal);
-    const unsigned long long m_equal = __ballot(equal);
-    const bool keep = sure || (equal && eq + (uint32_t)__popcll(m_equal & below) < equal_kept);
+    const unsigned long long m_equal = __ballot(key == last);
+    const bool keep = key > last || (key == last && eq + (uint32_t)__popcll(m_equal & below) < equal_kept);
     const unsigned long long m = __ballot(keep);
     if (keep) out[at + (uint32_t)__popcll(m & below)] = first + 64 * i;
     at += (uint32_t)__popcll(m);
@@ -172,13 +188,13 @@ __global__ __launch_bounds__(kMvThreads) void evict_copy_kernel(EvictArgs a, con
   const long long out0 = (long long)unit * a.S_cap_out;
   const int items = (j1 - j0) * CHUNKS;
   for (int i0 = tid; i0 < items; i0 += kMvThreads * kMvInFlight) {
+    int at[kMvInFlight];
     uint4 x[kMvInFlight];
 #pragma unroll
-    for (int u = 0; u < kMvInFlight; ++u) {
-      const int i = i0 + u * kMvThreads;
-      if (i < items)
-        x[u] = load16(evict_chunk(src, cache_row(a.pg, b, h, a.Hkv, a.S_cap, from[j0 + i / CHUNKS]), i % CHUNKS, CHUNKS / 2, a.nlo));
-    }
+    for (int u = 0; u < kMvInFlight; ++u) at[u] = from[j0 + min(i0 + u * kMvThreads, items - 1) / CHUNKS];
+#pragma unroll
+    for (int u = 0; u < kMvInFlight; ++u)
+      x[u] = load16(evict_chunk(src, cache_row(a.pg, b, h, a.Hkv, a.S_cap, at[u]), (i0 + u * kMvThreads) % CHUNKS, CHUNKS / 2, a.nlo));
 #pragma unroll
     for (int u = 0; u < kMvInFlight; ++u) {
       const int i = i0 + u * kMvThreads;

@@ -270,16 +270,16 @@ hipError_t launch_evict_move(const Shape& s, const EvictArgs& a, const int32_t* 
 constexpr int kPartStride = kD + 4;  // o[128], m (of logits times log2 e), l, two unused: rows of whole 16 bytes
 int weigh_splits(const Shape& s);
 size_t weigh_logits_pitch(int S_max);
-// logits [B Hq, pitch] or null; seq_lens entries from 0 on
-hipError_t launch_parts(const Shape& s, int nsplit, int nparts, const void* q, const void* k_full, const void* v, float* partial,
-                        float* logits, hipStream_t st);
-// The sequences' parts, and behind them `shared` parts that every head has; weights_out null: only `out`.
-hipError_t launch_weigh_merge(const Shape& s, int nsplit, int shared, const float* partial, const float* logits,
-                              const float* weights_in, float* weights_out, void* out, hipStream_t st);
-// Attention of every query of the batch over one prefix (shared.hip): parts nsplit .. nsplit + splits - 1 of nparts.
+// Runs of rows, nsplit B places for each query head; logits [B Hq, pitch] or null; seq_lens entries from 0 on.
+hipError_t launch_parts(const Shape& s, int nsplit, const void* q, const void* k_full, const void* v, float* partial, float* logits,
+                        hipStream_t st);
+// The sequences' parts with `prefix`'s, `shared` for each of the B Hq heads; weights_out null: only `out`.
+hipError_t launch_weigh_merge(const Shape& s, int nsplit, int shared, const float* partial, const float* prefix,
+                              const float* logits, const float* weights_in, float* weights_out, void* out, hipStream_t st);
+// Attention of every query of the batch over one prefix (shared.hip): `splits` parts for each of the B Hq heads.
 int prefix_splits(const Shape& s, int prefix_rows);
-hipError_t launch_prefix(const Shape& s, int first, int splits, int nparts, const void* q, const void* k_prefix, const void* v_prefix,
-                         int prefix_rows, int prefix_cap, float* partial, hipStream_t st);
+hipError_t launch_prefix(const Shape& s, int splits, const void* q, const void* k_prefix, const void* v_prefix, int prefix_rows,
+                         int prefix_cap, float* partial, hipStream_t st);
 hipError_t launch_rotate(const Shape& s, const void* k_new, const float* P, void* klo, void* khi,
                          int pos, int n_new, hipStream_t st);
 

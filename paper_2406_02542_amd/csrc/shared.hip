@@ -28,7 +28,7 @@ constexpr float kPfGrowth = 256.0f;  // the reference of the exponentials follow
 template <int QG>
 __global__ __launch_bounds__(kPfThreads, QG == 1 ? 3 : QG == 2 ? 2 : 1) void prefix_f32_kernel(
     const float* __restrict__ k, const float* __restrict__ v, const float* __restrict__ qv, float* __restrict__ partial, int M, int G,
-    int Hq, int rows, int cap, int run, int first, int nparts) {
+    int Hq, int rows, int cap, int run) {
   __shared__ __align__(16) float s_o[kPfWaves / 2][QG][32][64];
   __shared__ float2 s_ml[kPfWaves][QG][16];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -179,7 +179,7 @@ __global__ __launch_bounds__(kPfThreads, QG == 1 ? 3 : QG == 2 ? 2 : 1) void pre
   for (int g = 0; g < QG; ++g) {
     const int r = q0 + 16 * g + l16;
     if (r >= M) continue;
-    float* pr = partial + (prefix_head(r, h, G, Hq) * nparts + first + split) * kPartStride;
+    float* pr = partial + (prefix_head(r, h, G, Hq) * gridDim.x + split) * kPartStride;
 #pragma unroll
     for (int c = 0; c < 2; ++c)
 #pragma unroll
@@ -224,7 +224,7 @@ constexpr int pf_lds_bytes() {
 template <int QG, int WAVES, int WQ>
 __global__ __launch_bounds__(64 * WAVES, QG == 2 ? 1 : 2) void prefix_mfma_kernel(
     const uint16_t* __restrict__ k, const uint16_t* __restrict__ v, const uint16_t* __restrict__ qv, float* __restrict__ partial,
-    int M, int G, int Hq, int rows, int cap, int run, int first, int nparts) {
+    int M, int G, int Hq, int rows, int cap, int run) {
   constexpr int kThreads = 64 * WAVES, WK = WAVES / WQ, KT = pf_tile_keys<WAVES, WQ>(), kSteps = KT / (32 * WK), kChunks = KT * 16 / kThreads;
   constexpr int kTileBytes = KT * 256;
   extern __shared__ __align__(16) char smem[];  // [2][K tile, V tile]
@@ -451,13 +451,13 @@ __global__ __launch_bounds__(64 * WAVES, QG == 2 ? 1 : 2) void prefix_mfma_kerne
       for (int j = 0; j < 8; ++j) {
         const int row = 4 * j + (lane >> 4), r = q0 + 32 * g + row;
         const float4 x = *reinterpret_cast<const float4*>(mine + row * 256 + ((l16 ^ (row & 15)) * 16));
-        if (r < M) *reinterpret_cast<float4*>(partial + (prefix_head(r, h, G, Hq) * nparts + first + split) * kPartStride + 64 * pass + 4 * l16) = x;
+        if (r < M) *reinterpret_cast<float4*>(partial + (prefix_head(r, h, G, Hq) * gridDim.x + split) * kPartStride + 64 * pass + 4 * l16) = x;
       }
       __builtin_amdgcn_wave_barrier();
     }
     const int r = q0 + 32 * g + l32;
     if (half == 0 && r < M)
-      *reinterpret_cast<float2*>(partial + (prefix_head(r, h, G, Hq) * nparts + first + split) * kPartStride + kD) = make_float2(m[g], l[g]);
+      *reinterpret_cast<float2*>(partial + (prefix_head(r, h, G, Hq) * gridDim.x + split) * kPartStride + kD) = make_float2(m[g], l[g]);
   }
 }
 
@@ -491,7 +491,7 @@ int prefix_splits(const Shape& s, int prefix_rows) {
 }
 
 template <int QG, int WAVES, int WQ>
-static hipError_t launch_prefix_mfma(const Shape& s, int first, int splits, int nparts, const void* q, const void* k, const void* v,
+static hipError_t launch_prefix_mfma(const Shape& s, int splits, const void* q, const void* k, const void* v,
                                      int rows, int cap, float* partial, hipStream_t st) {
   static std::atomic<unsigned long long> raised{0};
   constexpr int bytes = pf_lds_bytes<QG, WAVES, WQ>();
@@ -500,24 +500,24 @@ static hipError_t launch_prefix_mfma(const Shape& s, int first, int splits, int 
   const int M = s.B * s.G, nq = QG * WQ * 32;
   hipLaunchKernelGGL((prefix_mfma_kernel<QG, WAVES, WQ>), dim3(splits, (M + nq - 1) / nq, s.Hkv), dim3(64 * WAVES), bytes, st,
                      static_cast<const uint16_t*>(k), static_cast<const uint16_t*>(v), static_cast<const uint16_t*>(q), partial, M, s.G,
-                     s.Hq, rows, cap, prefix_run(s, rows), first, nparts);
+                     s.Hq, rows, cap, prefix_run(s, rows));
   return hipGetLastError();
 }
 
 template <int QG>
-static hipError_t launch_prefix_f32(const Shape& s, int first, int splits, int nparts, const void* q, const void* k, const void* v,
+static hipError_t launch_prefix_f32(const Shape& s, int splits, const void* q, const void* k, const void* v,
                                     int rows, int cap, float* partial, hipStream_t st) {
   const int M = s.B * s.G, nq = QG * 16;
   hipLaunchKernelGGL((prefix_f32_kernel<QG>), dim3(splits, (M + nq - 1) / nq, s.Hkv), dim3(kPfThreads), 0, st,
                      static_cast<const float*>(k), static_cast<const float*>(v), static_cast<const float*>(q), partial, M, s.G, s.Hq,
-                     rows, cap, prefix_run(s, rows), first, nparts);
+                     rows, cap, prefix_run(s, rows));
   return hipGetLastError();
 }
 
-hipError_t launch_prefix(const Shape& s, int first, int splits, int nparts, const void* q, const void* k, const void* v, int rows,
+hipError_t launch_prefix(const Shape& s, int splits, const void* q, const void* k, const void* v, int rows,
                          int cap, float* partial, hipStream_t st) {
   const int nq = prefix_shape(s).queries;
-#define LOKI_PREFIX(f) return f(s, first, splits, nparts, q, k, v, rows, cap, partial, st)
+#define LOKI_PREFIX(f) return f(s, splits, q, k, v, rows, cap, partial, st)
   if (s.dtype == 0) {
     if (nq == 16) LOKI_PREFIX(launch_prefix_f32<1>);
     if (nq == 32) LOKI_PREFIX(launch_prefix_f32<2>);
