@@ -116,6 +116,16 @@ __device__ inline uint4 load16_hint(const void* p) {
   }
 }
 
+template <bool STREAM>
+__device__ inline void store16_hint(void* p, const uint4& x) {
+  if constexpr (STREAM) {
+    typedef unsigned int u32x4_t __attribute__((ext_vector_type(4)));
+    __builtin_nontemporal_store(__builtin_bit_cast(u32x4_t, x), reinterpret_cast<u32x4_t*>(p));
+  } else {
+    *reinterpret_cast<uint4*>(p) = x;
+  }
+}
+
 // f(form) for the form (see RowLoads) that a launch takes, up to MAX.  The hint is part of the instruction, so
 // a kernel holds what it does behind the choice once for each: the single launches their whole body (two loops in
 // one body, of which the block takes one, cost them 23 to 108 registers that do not fit), and no kernel exists

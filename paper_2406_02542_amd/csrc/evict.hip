@@ -172,17 +172,18 @@ __device__ __forceinline__ char* evict_chunk(const EvictSide& x, long long row, 
 
 constexpr int kMvThreads = 256;
 constexpr int kMvInFlight = 8;
+constexpr int kBothPast = 2;  // (kThroughCaches 0, kPastCaches 1: the loads)
 
-// Into another cache: a block takes `rows` list entries of one unit.
-template <int CHUNKS>  // 16-byte chunks of a key and a value row together
+// Into another cache: a block takes `rows` list entries of one unit (behind the kept ones the list holds -1).
+// FORM: kThroughCaches, loads past the caches, loads and stores past them (launch_evict_move).
+template <int CHUNKS, int FORM>  // CHUNKS: of 16 bytes, of a key and a value row together
 __global__ __launch_bounds__(kMvThreads) void evict_copy_kernel(EvictArgs a, const int32_t* __restrict__ list,
                                                                 const int32_t* __restrict__ kept_rows, int rows) {
   const int unit = blockIdx.y, b = unit / a.Hkv, h = unit - b * a.Hkv, tid = threadIdx.x;
-  const int kept = kept_rows[unit];
-  const int j0 = blockIdx.x * rows, j1 = min(kept, j0 + rows);
-  if (blockIdx.x == 0 && h == 0 && tid == 0 && a.lens_out != nullptr) a.lens_out[b] = kept;
-  if (j0 >= j1) return;
+  const int j0 = blockIdx.x * rows, j1 = min(a.budget, j0 + rows);
+  if (blockIdx.x == 0 && h == 0 && tid == 0 && a.lens_out != nullptr) a.lens_out[b] = kept_rows[unit];
   const int32_t* from = list + (size_t)unit * a.budget;
+  if (from[j0] < 0) return;  // uniform for the block
   const EvictSide src{(char*)a.klo, (char*)a.khi, (char*)a.v, a.S_cap};
   const EvictSide dst{(char*)a.klo_out, (char*)a.khi_out, (char*)a.v_out, a.S_cap_out};
   const long long out0 = (long long)unit * a.S_cap_out;
@@ -194,15 +195,16 @@ __global__ __launch_bounds__(kMvThreads) void evict_copy_kernel(EvictArgs a, con
     for (int u = 0; u < kMvInFlight; ++u) at[u] = from[j0 + min(i0 + u * kMvThreads, items - 1) / CHUNKS];
 #pragma unroll
     for (int u = 0; u < kMvInFlight; ++u)
-      x[u] = load16(evict_chunk(src, cache_row(a.pg, b, h, a.Hkv, a.S_cap, at[u]), (i0 + u * kMvThreads) % CHUNKS, CHUNKS / 2, a.nlo));
+      x[u] = load16_hint<FORM != kThroughCaches>(
+          evict_chunk(src, cache_row(a.pg, b, h, a.Hkv, a.S_cap, max(at[u], 0)), (i0 + u * kMvThreads) % CHUNKS, CHUNKS / 2, a.nlo));
 #pragma unroll
     for (int u = 0; u < kMvInFlight; ++u) {
       const int i = i0 + u * kMvThreads;
-      if (i < items) *reinterpret_cast<uint4*>(evict_chunk(dst, out0 + j0 + i / CHUNKS, i % CHUNKS, CHUNKS / 2, a.nlo)) = x[u];
+      if (i < items && at[u] >= 0) store16_hint<FORM == kBothPast>(evict_chunk(dst, out0 + j0 + i / CHUNKS, i % CHUNKS, CHUNKS / 2, a.nlo), x[u]);
     }
   }
   if (a.weights_out != nullptr)
-    for (int j = j0 + tid; j < j1; j += kMvThreads) a.weights_out[out0 + j] = a.weights[(size_t)unit * a.S_cap + from[j]];
+    for (int j = j0 + tid; j < j1 && from[j] >= 0; j += kMvThreads) a.weights_out[out0 + j] = a.weights[(size_t)unit * a.S_cap + from[j]];
 }
 
 // Every source of a run has been read, by all waves, before one of its rows is overwritten.
@@ -288,10 +290,23 @@ hipError_t launch_evict_move(const Shape& s, const EvictArgs& a, const int32_t* 
   }
   const int rows = kMvThreads * kMvInFlight / chunks;
   const dim3 grid((a.budget + rows - 1) / rows, units), block(kMvThreads);
-  if (s.dtype == 0)
-    hipLaunchKernelGGL((evict_copy_kernel<64>), grid, block, 0, st, a, list, kept, rows);
-  else
-    hipLaunchKernelGGL((evict_copy_kernel<32>), grid, block, 0, st, a, list, kept, rows);
+  // By the bytes that go on: rows read once, from 48 MB past the caches, from 120 MB written past them too.  us through /
+  // loads / both past: 34 MB 21.8 / 23.0 / 22.5, 67 39.4 / 33.5 / 35.2, 92 52.4 / 44.8 / 46.8, 134 72.2 / 68.6 / 64.1.
+  const double moved = (double)units * (a.budget < a.S_max ? a.budget : a.S_max) * 16 * chunks;
+  const int form = moved < 48e6 ? kThroughCaches : moved < 120e6 ? kPastCaches : kBothPast;
+#define LOKI_EVICT_COPY(C)                                                                                            \
+  if (form == kThroughCaches)                                                                                         \
+    hipLaunchKernelGGL((evict_copy_kernel<C, kThroughCaches>), grid, block, 0, st, a, list, kept, rows);              \
+  else if (form == kPastCaches)                                                                                       \
+    hipLaunchKernelGGL((evict_copy_kernel<C, kPastCaches>), grid, block, 0, st, a, list, kept, rows);                 \
+  else                                                                                                                \
+    hipLaunchKernelGGL((evict_copy_kernel<C, kBothPast>), grid, block, 0, st, a, list, kept, rows)
+  if (s.dtype == 0) {
+    LOKI_EVICT_COPY(64);
+  } else {
+    LOKI_EVICT_COPY(32);
+  }
+#undef LOKI_EVICT_COPY
   return hipGetLastError();
 }
 

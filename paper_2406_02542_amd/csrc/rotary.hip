@@ -8,14 +8,14 @@
 //
 // A block owns kTokens tokens (or a share of one token's heads when there are few tokens) and works out their
 // R / 2 angles once, into LDS, for all heads.  The angle in quarter turns is reduced in 64 bits: 32 would
-// leave a position of 100 000 with angles off by 4e-3.  A lane group then takes rows (token, head) in turn,
-// each lane two 16-byte chunks that hold both halves of its pairs, four rows in flight.
+// leave a position of 100 000 with angles off by 4e-3.  A lane group then takes heads of one token in turn,
+// each lane two 16-byte chunks that hold both halves of its pairs, with their angles in registers, four rows in flight.
 #include "common.h"
 
 namespace loki {
 
 constexpr int kRotThreads = 256;
-constexpr int kRotInFlight = 4;
+constexpr int kRotInFlight = 6;
 constexpr int kRotMaxTokens = 4;  // of a block: one angle per thread with 64 pairs
 
 // cos and sin of x quarter turns, |x| reduced here; fp32 results.  Taylor polynomials on [-pi/4, pi/4]: the first
@@ -46,88 +46,87 @@ __device__ __forceinline__ uint4 pack_chunk(const float (&f)[T::EPC]) {
 }
 
 // STYLE: 0 pairs (i, i + R / 2), R / 2 a multiple of a chunk; 1 pairs (2 i, 2 i + 1); 2 as 0, any even R.
-template <typename T, int STYLE>
+// STREAM: rows are loaded and stored past the caches (launch_rotary).
+template <typename T, int STYLE, bool STREAM>
 __global__ __launch_bounds__(kRotThreads) void rotary_kernel(RotaryArgs a) {
   using ST = typename T::store_t;
   constexpr int EPC = T::EPC;
   constexpr int kLanes = kD / EPC / 2;  // lanes of a row: two chunks each
   constexpr int kGroups = kRotThreads / kLanes;
+  constexpr int kAngles = STYLE == 2 ? 1 : EPC;  // of a lane
   __shared__ float2 s_cs[kRotMaxTokens][kD / 2];
   const int tid = threadIdx.x, p = tid % kLanes, gid = tid / kLanes;
   const int pairs = a.R / 2, tok0 = blockIdx.x * a.tokens, ntok = min(a.tokens, a.total - tok0);
+  // this lane group's token, and its heads h0 + first, h0 + first + step, ..
+  const int mine = gid & (a.tokens - 1), first = gid / a.tokens, step = kGroups / a.tokens;
+  const int heads = a.q.heads + a.k.heads + a.v.heads;
+  const int h0 = blockIdx.y * a.heads_per_block, h1 = min(h0 + a.heads_per_block, heads);
+  const int t = tok0 + min(mine, ntok - 1), b = t / a.n, j = t - b * a.n;
+  const int row = a.rows != nullptr ? a.rows[t] : j;
 
   for (int i = tid; i < ntok * pairs; i += kRotThreads) {
-    const int t = i / pairs, f = i - t * pairs;
-    const double quarters = (double)a.positions[tok0 + t] * (a.freqs[f] * 0.63661977236758134308);  // 2 / pi
+    const int u = i / pairs, f = i - u * pairs;
+    const double quarters = (double)a.positions[tok0 + u] * (a.freqs[f] * 0.63661977236758134308);  // 2 / pi
     float2 cs = cos_sin_quarters(quarters);
     cs.x *= a.scale;
     cs.y *= a.inverse ? -a.scale : a.scale;
-    s_cs[t][f] = cs;
+    s_cs[u][f] = cs;
   }
   __syncthreads();
+  if (mine >= ntok) return;
 
-  // the two chunks of this lane: a pair of rotated ones, or two of the columns behind R
-  int c0, c1;
+  // the two chunks of this lane: a pair of rotated ones, or two of the columns behind R; and their angles
+  int c0 = p, c1 = p + kLanes;
   if (STYLE == 0) {
     const int np = pairs / EPC;
-    c0 = p < np ? p : 2 * p;
-    c1 = p < np ? p + np : 2 * p + 1;
-  } else {
-    c0 = p;
-    c1 = p + kLanes;
+    c0 = p < np ? p : p + np;
+    c1 = p < np ? p + np : p + kLanes;
   }
-  const int heads = a.q.heads + a.k.heads + a.v.heads;
-  const int h0 = blockIdx.y * a.heads_per_block, hn = min(a.heads_per_block, heads - h0);
-  const int items = ntok * hn;
+  float2 cs[kAngles];
+#pragma unroll
+  for (int e = 0; e < kAngles; ++e) {
+    if (STYLE == 0) cs[e] = s_cs[mine][min(c0 * EPC + e, pairs - 1)];
+    if (STYLE == 1) cs[e] = s_cs[mine][min((e < EPC / 2 ? c0 : c1) * (EPC / 2) + e % (EPC / 2), pairs - 1)];
+  }
+  const bool in_r = STYLE != 0 || c1 * EPC < a.R;  // (STYLE 0: both chunks or none)
+  const bool row_there = a.rows == nullptr || (row >= 0 && row < a.n_rows);
 
-  for (int i0 = gid; i0 < items; i0 += kGroups * kRotInFlight) {
+  for (int i0 = h0 + first; i0 < h1; i0 += step * kRotInFlight) {
     uint4 raw[kRotInFlight][2];
     ST* dst[kRotInFlight];
-    int tok[kRotInFlight];
     bool turn[kRotInFlight];
 #pragma unroll
     for (int u = 0; u < kRotInFlight; ++u) {
-      const int i = i0 + u * kGroups;
-      dst[u] = nullptr;
-      turn[u] = false;
-      tok[u] = 0;
-      raw[u][0] = raw[u][1] = make_uint4(0, 0, 0, 0);
-      if (i < items) {
-        tok[u] = i / hn;
-        int h = h0 + i - tok[u] * hn;
-        const int t = tok0 + tok[u], b = t / a.n, j = t - b * a.n;
-        const bool is_q = h < a.q.heads;
-        if (!is_q) h -= a.q.heads;
-        const bool is_k = !is_q && h < a.k.heads;
-        if (!is_q && !is_k) h -= a.k.heads;
-        const RotaryTensor& x = is_q ? a.q : is_k ? a.k : a.v;
-        int row = j;
-        if (!is_q && a.rows != nullptr) row = a.rows[t];
-        const ST* src = static_cast<const ST*>(x.in) + (b * x.in_batch + j * x.in_token + h * x.in_head);
-        raw[u][0] = load16(src + c0 * EPC);
-        raw[u][1] = load16(src + c1 * EPC);
-        turn[u] = is_q || is_k;
-        if (is_q || a.rows == nullptr || (row >= 0 && row < a.n_rows))
-          dst[u] = static_cast<ST*>(x.out) + (b * x.out_batch + row * x.out_token + h * x.out_head);
-        if constexpr (STYLE == 2) {
-          // partners that no chunk boundary respects, element by element; read before anything of the row is written
-          if (turn[u]) {
+      int h = min(i0 + u * step, h1 - 1);
+      const bool is_q = h < a.q.heads;
+      if (!is_q) h -= a.q.heads;
+      const bool is_k = !is_q && h < a.k.heads;
+      if (!is_q && !is_k) h -= a.k.heads;
+      const RotaryTensor& x = is_q ? a.q : is_k ? a.k : a.v;
+      const ST* src = static_cast<const ST*>(x.in) + (b * x.in_batch + j * x.in_token + h * x.in_head);
+      raw[u][0] = load16_hint<STREAM>(src + c0 * EPC);
+      raw[u][1] = load16_hint<STREAM>(src + c1 * EPC);
+      turn[u] = in_r && (is_q || is_k);
+      dst[u] = static_cast<ST*>(x.out) + (b * x.out_batch + (is_q ? j : row) * x.out_token + h * x.out_head);
+      if (i0 + u * step >= h1 || !(is_q || row_there)) dst[u] = nullptr;
+      if constexpr (STYLE == 2) {
+        // partners that no chunk boundary respects, element by element; read before anything of the row is written
+        if (turn[u]) {
 #pragma unroll
-            for (int half = 0; half < 2; ++half) {
-              float x0[EPC];
-              T::unpack(raw[u][half], x0);
+          for (int half = 0; half < 2; ++half) {
+            float x0[EPC];
+            T::unpack(raw[u][half], x0);
 #pragma unroll
-              for (int e = 0; e < EPC; ++e) {
-                const int col = (half ? c1 : c0) * EPC + e;
-                if (col < a.R) {
-                  const bool first = col < pairs;
-                  const float2 cs = s_cs[tok[u]][first ? col : col - pairs];
-                  const float other = T::load1(src + (first ? col + pairs : col - pairs));
-                  x0[e] = first ? x0[e] * cs.x - other * cs.y : x0[e] * cs.x + other * cs.y;
-                }
+            for (int e = 0; e < EPC; ++e) {
+              const int col = (half ? c1 : c0) * EPC + e;
+              if (col < a.R) {
+                const bool lower = col < pairs;
+                const float2 y = s_cs[mine][lower ? col : col - pairs];
+                const float other = T::load1(src + (lower ? col + pairs : col - pairs));
+                x0[e] = lower ? x0[e] * y.x - other * y.y : x0[e] * y.x + other * y.y;
               }
-              raw[u][half] = pack_chunk<T>(x0);
             }
+            raw[u][half] = pack_chunk<T>(x0);
           }
         }
       }
@@ -135,15 +134,14 @@ __global__ __launch_bounds__(kRotThreads) void rotary_kernel(RotaryArgs a) {
 #pragma unroll
     for (int u = 0; u < kRotInFlight; ++u) {
       if constexpr (STYLE == 0) {
-        if (turn[u] && c1 * EPC < a.R) {
+        if (turn[u]) {
           float x0[EPC], x1[EPC], y0[EPC], y1[EPC];
           T::unpack(raw[u][0], x0);
           T::unpack(raw[u][1], x1);
 #pragma unroll
           for (int e = 0; e < EPC; ++e) {
-            const float2 cs = s_cs[tok[u]][c0 * EPC + e];
-            y0[e] = x0[e] * cs.x - x1[e] * cs.y;
-            y1[e] = x1[e] * cs.x + x0[e] * cs.y;
+            y0[e] = x0[e] * cs[e].x - x1[e] * cs[e].y;
+            y1[e] = x1[e] * cs[e].x + x0[e] * cs[e].y;
           }
           raw[u][0] = pack_chunk<T>(y0);
           raw[u][1] = pack_chunk<T>(y1);
@@ -156,12 +154,11 @@ __global__ __launch_bounds__(kRotThreads) void rotary_kernel(RotaryArgs a) {
             T::unpack(raw[u][half], x0);
 #pragma unroll
             for (int e = 0; e < EPC; e += 2) {
-              const int col = (half ? c1 : c0) * EPC + e;
-              if (col < a.R) {
-                const float2 cs = s_cs[tok[u]][col / 2];
-                const float x = x0[e], y = x0[e + 1];
-                x0[e] = x * cs.x - y * cs.y;
-                x0[e + 1] = y * cs.x + x * cs.y;
+              if ((half ? c1 : c0) * EPC + e < a.R) {
+                const float2 y = cs[(half * EPC + e) / 2];
+                const float x = x0[e], z = x0[e + 1];
+                x0[e] = x * y.x - z * y.y;
+                x0[e + 1] = z * y.x + x * y.y;
               }
             }
             raw[u][half] = pack_chunk<T>(x0);
@@ -169,29 +166,32 @@ __global__ __launch_bounds__(kRotThreads) void rotary_kernel(RotaryArgs a) {
         }
       }
       if (dst[u] != nullptr) {
-        *reinterpret_cast<uint4*>(dst[u] + c0 * EPC) = raw[u][0];
-        *reinterpret_cast<uint4*>(dst[u] + c1 * EPC) = raw[u][1];
+        store16_hint<STREAM>(dst[u] + c0 * EPC, raw[u][0]);
+        store16_hint<STREAM>(dst[u] + c1 * EPC, raw[u][1]);
       }
     }
   }
 }
 
-template <typename T>
+template <typename T, bool STREAM>
 static hipError_t launch_rotary_t(const RotaryArgs& a, dim3 grid, int style, hipStream_t st) {
   const dim3 block(kRotThreads);
   if (style == 0)
-    hipLaunchKernelGGL((rotary_kernel<T, 0>), grid, block, 0, st, a);
+    hipLaunchKernelGGL((rotary_kernel<T, 0, STREAM>), grid, block, 0, st, a);
   else if (style == 1)
-    hipLaunchKernelGGL((rotary_kernel<T, 1>), grid, block, 0, st, a);
+    hipLaunchKernelGGL((rotary_kernel<T, 1, STREAM>), grid, block, 0, st, a);
   else
-    hipLaunchKernelGGL((rotary_kernel<T, 2>), grid, block, 0, st, a);
+    hipLaunchKernelGGL((rotary_kernel<T, 2, false>), grid, block, 0, st, a);
   return hipGetLastError();
 }
 
 hipError_t launch_rotary(const Shape& s, RotaryArgs a, hipStream_t st) {
   const int epc = 16 / s.elem_bytes, heads = a.q.heads + a.k.heads + a.v.heads;
   // few tokens: the heads of a token are spread over blocks until every CU has one or a lane group has one row
-  a.tokens = a.total >= kRotMaxTokens * device_cus() ? kRotMaxTokens : 1;
+  // (us with 4, 2 and 1 tokens a block: 8 x 2048 of 32/8 bf16 heads 69, 78, 115: the angles are worked out by a few lanes; 3 x
+  // 1111 of 24/24 fp32 heads 56, 54, 51, 4 x 1024 of 32/8 39, 38, 42: larger blocks leave the last round uneven)
+  const int tokens = s.dtype == 0 ? 2 : kRotMaxTokens;
+  a.tokens = a.total >= tokens * device_cus() ? tokens : 1;
   a.heads_per_block = heads;
   const int groups = kRotThreads / (kD / epc / 2);
   if (a.tokens == 1) {
@@ -202,7 +202,12 @@ hipError_t launch_rotary(const Shape& s, RotaryArgs a, hipStream_t st) {
   }
   const dim3 grid((a.total + a.tokens - 1) / a.tokens, (heads + a.heads_per_block - 1) / a.heads_per_block);
   const int style = a.interleaved ? 1 : (a.R / 2) % epc == 0 ? 0 : 2;
-  return s.dtype == 0 ? launch_rotary_t<F32>(a, grid, style, st) : launch_rotary_t<BF16>(a, grid, style, st);
+  // From 100 MB read and written on, past the caches.  us through / past: 88 MB 18.5 / 18.8, 101 22.4 / 20.8, 157 34.5 / 30.2,
+  // 202 41.9 / 38.0, 246 50.1 / 46.0, 403 77.6 / 72.8.
+  const bool past = 2.0 * a.total * heads * kD * s.elem_bytes >= 100e6;
+  if (s.dtype == 0)
+    return past ? launch_rotary_t<F32, true>(a, grid, style, st) : launch_rotary_t<F32, false>(a, grid, style, st);
+  return past ? launch_rotary_t<BF16, true>(a, grid, style, st) : launch_rotary_t<BF16, false>(a, grid, style, st);
 }
 
 }  // namespace loki
