@@ -10,7 +10,7 @@ PKG_DIR = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(PKG_DIR, "csrc")
 LIB_PATH = os.path.join(PKG_DIR, "libloki.so")
 SOURCES = ["api.hip", "score.hip", "select.hip", "select_attend.hip", "attend.hip", "attend_mfma.hip", "fused.hip", "fused_f32.hip", "fused_gqa.hip", "fused_gqa_cluster.hip", "rotate.hip", "calibrate.hip", "eigensolver.hip", "rotary.hip", "weigh.hip", "evict.hip", "shared.hip"]
-HEADERS = ["common.h", "launch.h", "block_order.h", "score_impl.h", "select_impl.h", "attend_impl.h", "fused_impl.h", "score_mfma_impl.h", "attend_mfma_impl.h", "fused_gqa_impl.h", "cluster_impl.h", "eigensolver.h", os.path.join("..", "..", "include", "loki.h")]
+HEADERS = ["common.h", "launch.h", "block_order.h", "score_impl.h", "select_impl.h", "attend_impl.h", "fused_impl.h", "score_mfma_impl.h", "attend_mfma_impl.h", "parts_impl.h", "fused_gqa_impl.h", "cluster_impl.h", "eigensolver.h", os.path.join("..", "..", "include", "loki.h")]
 
 # -packed-fp32-ops is switched off on purpose: the compiler must not form v_pk_*_f32.
 HIPCC_FLAGS = [

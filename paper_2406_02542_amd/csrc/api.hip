@@ -910,7 +910,7 @@ int dense_shared_workspace_bytes(const loki_layout* layout, int prefix_rows, int
   if (rc != LOKI_OK) return rc;
   if (!bytes || prefix_rows < 0 || S_max < 0 || S_max > s.S_cap) return LOKI_ERR_INVALID_ARG;
   s.S = S_max;
-  *bytes = plan_parts(s, S_max > 0 ? weigh_splits(s) : 0, prefix_splits(s, prefix_rows), false, nullptr).total;
+  *bytes = plan_parts(s, shared_own_splits(s), prefix_splits(s, prefix_rows), false, nullptr).total;
   return LOKI_OK;
 }
 
@@ -928,24 +928,15 @@ int dense_decode_shared(const loki_layout* layout, const void* q, const void* k_
   if (!aligned256(workspace) || (reinterpret_cast<uintptr_t>(seq_lens) & 3u)) return LOKI_ERR_ALIGNMENT;
   s.S = S_max;
   s.rg.seq_lens = seq_lens;
-  const int nsplit = S_max > 0 ? weigh_splits(s) : 0, shared = prefix_splits(s, prefix_rows);
+  const int nsplit = shared_own_splits(s), shared = prefix_splits(s, prefix_rows);
   const PartsPlan w = plan_parts(s, nsplit, shared, false, workspace);
   if (w.total > workspace_bytes) return LOKI_ERR_WORKSPACE;
   hipStream_t st = static_cast<hipStream_t>(stream);
   StageTimer tm(st);
-  hipError_t e = hipSuccess;
-  if (shared > 0) {
-    tm.begin("prefix_parts");
-    e = launch_prefix(s, shared, q, k_prefix, v_prefix, prefix_rows, prefix_cap, w.prefix, st);
-    tm.end();
-    if (e != hipSuccess) return LOKI_ERR_HIP;
-  }
-  if (nsplit > 0) {
-    tm.begin("dense_parts");
-    e = launch_parts(s, nsplit, q, k_full, v, w.partial, nullptr, st);
-    tm.end();
-    if (e != hipSuccess) return LOKI_ERR_HIP;
-  }
+  tm.begin("shared_parts");
+  hipError_t e = launch_shared(s, shared, nsplit, q, k_prefix, v_prefix, prefix_rows, prefix_cap, k_full, v, w.prefix, w.partial, st);
+  tm.end();
+  if (e != hipSuccess) return LOKI_ERR_HIP;
   tm.begin("merge");
   e = launch_weigh_merge(s, nsplit, shared, w.partial, w.prefix, nullptr, nullptr, nullptr, out, st);
   tm.end();

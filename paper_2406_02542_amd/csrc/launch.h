@@ -276,10 +276,12 @@ hipError_t launch_parts(const Shape& s, int nsplit, const void* q, const void* k
 // The sequences' parts with `prefix`'s, `shared` for each of the B Hq heads; weights_out null: only `out`.
 hipError_t launch_weigh_merge(const Shape& s, int nsplit, int shared, const float* partial, const float* prefix,
                               const float* logits, const float* weights_in, float* weights_out, void* out, hipStream_t st);
-// Attention of every query of the batch over one prefix (shared.hip): `splits` parts for each of the B Hq heads.
+// Attention of a batch over one prefix and over its own rows (shared.hip): `splits` parts of the prefix for each of the B Hq
+// heads, nsplit B places for each query head's own.
 int prefix_splits(const Shape& s, int prefix_rows);
-hipError_t launch_prefix(const Shape& s, int splits, const void* q, const void* k_prefix, const void* v_prefix, int prefix_rows,
-                         int prefix_cap, float* partial, hipStream_t st);
+int shared_own_splits(const Shape& s);
+hipError_t launch_shared(const Shape& s, int splits, int nsplit, const void* q, const void* k_prefix, const void* v_prefix,
+                         int prefix_rows, int prefix_cap, const void* k, const void* v, float* prefix, float* partial, hipStream_t st);
 hipError_t launch_rotate(const Shape& s, const void* k_new, const float* P, void* klo, void* khi,
                          int pos, int n_new, hipStream_t st);
 

@@ -1,16 +1,30 @@
 // Attention of a whole batch over the prefix that its sequences share (Section 2, Eq. 1 of arXiv 2406.02542, the
-// part of the rows that is the same for all): the prefix's keys and values are held once, and the B G query rows
-// of a KV head meet each of them in one product.  A run of the prefix leaves (max, sum, output) per query row, which
-// weigh_merge_kernel joins with the parts of the sequence's own rows.
-#include "attend_mfma_impl.h"
+// part of the rows that is the same for all) and over the rows of its own that each sequence has: the prefix's keys and
+// values are held once, and the M = B G query rows of a KV head meet each of them in one product.
+//
+// One launch of two kinds of blocks: a run of the prefix for a tile of query rows (below), and a run of a sequence's own rows
+// for its G heads (parts_impl.h).  Each leaves (max, sum, output) per query row, which weigh_merge_kernel joins.  Few
+// query rows: memory bounds it (16 of 32/8 heads behind 65536 rows: 268 MB in 43 us).  From about 200 on the
+// matrix cores do: the prefix is then read once by the chip for 4 M D operations a row.
+#include "parts_impl.h"
 
 namespace loki {
 
 constexpr int kPfThreads = 256;
 constexpr int kPfWaves = kPfThreads / 64;
 
-// Row of q (and of the partial results) that query row r of KV head h is: r = b G + g.
-__device__ __forceinline__ size_t prefix_head(int r, int h, int G, int Hq) {  // (G is a power of two)
+struct PrefixArgs {
+  const void *k, *v;  // [Hkv, cap, 128]
+  float* partial;     // [B Hq, splits] parts
+  int M, G, Hq, rows, cap, run, splits, tiles;
+};
+// Which run of the prefix, which tile of query rows, which KV head a block takes.
+struct PrefixAt {
+  int split, tile, h;
+};
+
+// Row of q (and of the partial results) that query row r of KV head h is: r = b G + g (G is a power of two).
+__device__ __forceinline__ size_t prefix_head(int r, int h, int G, int Hq) {
   return (size_t)(r >> (31 - __builtin_clz(G))) * Hq + h * G + (r & (G - 1));
 }
 
@@ -21,22 +35,27 @@ __device__ __forceinline__ size_t prefix_head(int r, int h, int G, int Hq) {  //
 //   O^T[column, query] += V^T P^T   the weights as they come out of the first product are operand i's keys 4 c + i; lane (m, c)
 //                                   loads 16 bytes of each of these rows, columns 4 m .. + 3 of either half
 // A step's keys and values are in registers before it begins.  The block's waves take steps in turn and are joined in LDS.
+// 64 sequences of 64/8 heads behind 16384 rows: 324 us, 106 TFLOP/s.
 typedef float pf_f32x4_t __attribute__((ext_vector_type(4)));
 constexpr int kPfSteps = 16;       // keys of a step
 constexpr float kPfGrowth = 256.0f;  // the reference of the exponentials follows the maximum when weights sum up to more
 
 template <int QG>
-__global__ __launch_bounds__(kPfThreads, QG == 1 ? 3 : QG == 2 ? 2 : 1) void prefix_f32_kernel(
-    const float* __restrict__ k, const float* __restrict__ v, const float* __restrict__ qv, float* __restrict__ partial, int M, int G,
-    int Hq, int rows, int cap, int run) {
-  __shared__ __align__(16) float s_o[kPfWaves / 2][QG][32][64];
-  __shared__ float2 s_ml[kPfWaves][QG][16];
+struct PrefixF32Smem {
+  float o[kPfWaves / 2][QG][32][64];
+  float2 ml[kPfWaves][QG][16];
+};
+template <int QG>
+__device__ __forceinline__ void prefix_f32_body(char* smem, const PrefixAt& block, const float* __restrict__ qv, const PrefixArgs& a) {
+  auto& s_o = reinterpret_cast<PrefixF32Smem<QG>*>(smem)->o;
+  auto& s_ml = reinterpret_cast<PrefixF32Smem<QG>*>(smem)->ml;
+  const int M = a.M, G = a.G, Hq = a.Hq;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int l16 = lane & 15, c4 = lane >> 4;
-  const int split = blockIdx.x, h = blockIdx.z, q0 = blockIdx.y * (QG * 16);
-  const int r0 = split * run, r1 = min(rows, r0 + run);
-  const float* kh = k + (size_t)h * cap * kD + 4 * c4;
-  const float* vh = v + (size_t)h * cap * kD + 4 * l16;
+  const int split = block.split, h = block.h, q0 = block.tile * (QG * 16);
+  const int r0 = split * a.run, r1 = min(a.rows, r0 + a.run);
+  const float* kh = static_cast<const float*>(a.k) + (size_t)h * a.cap * kD + 4 * c4;
+  const float* vh = static_cast<const float*>(a.v) + (size_t)h * a.cap * kD + 4 * l16;
 
   float4 q[QG][8];
 #pragma unroll
@@ -179,7 +198,7 @@ __global__ __launch_bounds__(kPfThreads, QG == 1 ? 3 : QG == 2 ? 2 : 1) void pre
   for (int g = 0; g < QG; ++g) {
     const int r = q0 + 16 * g + l16;
     if (r >= M) continue;
-    float* pr = partial + (prefix_head(r, h, G, Hq) * gridDim.x + split) * kPartStride;
+    float* pr = a.partial + (prefix_head(r, h, G, Hq) * a.splits + split) * kPartStride;
 #pragma unroll
     for (int c = 0; c < 2; ++c)
 #pragma unroll
@@ -190,20 +209,26 @@ __global__ __launch_bounds__(kPfThreads, QG == 1 ? 3 : QG == 2 ? 2 : 1) void pre
   }
 }
 
-// ---- bf16, more than 16 query rows per KV head: matrix cores on tiles that the block's waves share -------------
-// A wave holds QG groups of 32 query rows (their columns as operands in registers, 32 a group, and their outputs, 64) and
-// takes steps of 32 keys:
+// ---- bf16: matrix cores on tiles that the block's waves share ------------------------------------------------------
+// A wave holds 32 query rows (their columns as operands in 32 registers, and their outputs in 64) and takes steps of 32 keys:
 //   S^T[key, query] = K Q^T      v_mfma_f32_32x32x16_bf16, A = 16 bytes of a key row, B = the queries
-//   weights                      a lane has 16 of the 32 keys of ONE query, so maximum, sum and the rescaling of its outputs
-//                                are the lane's own but for one exchange with lane ^ 32
+//   weights                      a lane has 16 of the 32 keys of ONE query, so the sum and the rescaling of its outputs are the
+//                                lane's own
 //   O^T[column, query] += V^T P^T    B = the weights as they come out of the first product: the order of the keys in a
 //                                product is free, so A takes the same one, rows read column-wise by the transposing LDS load
-// K and V tiles of KT keys go through LDS once for the block's four waves, WQ of which hold different queries and WK = 4 / WQ
+// K and V tiles of KT keys go through LDS once for the block's waves, WQ of which hold different queries and WK = WAVES / WQ
 // different keys of the tile; the next tile is loaded into registers while this one is used.  16-byte chunks are stored at
 // places exchanged by the row's number, so that neither the key rows (stride 256 bytes) nor the four rows of a transposing
-// load meet in a bank.
-// The reference of the exponentials follows the running maximum only when that has grown by 2^8: the outputs (half of the
-// registers) are rescaled a few times per run instead of in most steps, and weights up to 2^8 lose nothing in fp32.
+// load meet in a bank (no conflict is counted).  Eight waves of 32 queries keep two on a SIMD, whose products and
+// exponentials overlap: four waves of 64 queries, each with the registers of a SIMD to itself, take 130 us where these take 113.
+// The weights enter the second product as ONE bf16 each: half a step, 2^-8, of each weight, which their sum, that of the
+// rounded weights, shares; over many rows the errors average to the size of the output's own rounding.  In two terms, as where
+// memory bounds an attention, the second product is twice as long (64 sequences of 64/8 heads behind 32768 rows: 97 us, 79 so).
+// The reference of the exponentials follows the running maximum only when a step's weights sum up to more than 2^8: the
+// outputs are rescaled a few times per run instead of in most steps, weights up to 2^8 lose nothing, and neither the
+// maximum nor an exchange between lanes is needed in the other steps.
+// Measured: 64 sequences of 64/8 heads behind P rows, 18 us + 1.9 us per 1024 rows (1.1 PFLOP/s; a large product reaches 1.2
+// on this card): the constant part is a launch, the queries, and 528 bytes per query row and run written.
 typedef float pf_f32x16_t __attribute__((ext_vector_type(16)));
 typedef short pf_s16x4_t __attribute__((ext_vector_type(4)));
 typedef __attribute__((address_space(3))) pf_s16x4_t pf_lds_s16x4_t;
@@ -215,40 +240,32 @@ constexpr int pf_tile_keys() {
 }
 
 // LDS: two pairs of tiles; at the end, where waves have other keys of the same queries, what half of them hand over.
-template <int QG, int WAVES, int WQ>
+template <int WAVES, int WQ>
 constexpr int pf_lds_bytes() {
-  const int tiles = 4 * pf_tile_keys<WAVES, WQ>() * 256, merge = WQ == WAVES ? 0 : WAVES * QG * 32 * 8 + WAVES / 2 * QG * 64 * 256;
+  const int tiles = 4 * pf_tile_keys<WAVES, WQ>() * 256, merge = WQ == WAVES ? 0 : WAVES * 32 * 8 + WAVES / 2 * 64 * 256;
   return tiles > merge ? tiles : merge;
 }
 
-template <int QG, int WAVES, int WQ>
-__global__ __launch_bounds__(64 * WAVES, QG == 2 ? 1 : 2) void prefix_mfma_kernel(
-    const uint16_t* __restrict__ k, const uint16_t* __restrict__ v, const uint16_t* __restrict__ qv, float* __restrict__ partial,
-    int M, int G, int Hq, int rows, int cap, int run) {
+template <int WAVES, int WQ>
+__device__ __forceinline__ void prefix_mfma_body(char* smem /* [2][K tile, V tile] */, const PrefixAt& block,
+                                                 const uint16_t* __restrict__ qv, const PrefixArgs& a) {
   constexpr int kThreads = 64 * WAVES, WK = WAVES / WQ, KT = pf_tile_keys<WAVES, WQ>(), kSteps = KT / (32 * WK), kChunks = KT * 16 / kThreads;
   constexpr int kTileBytes = KT * 256;
-  extern __shared__ __align__(16) char smem[];  // [2][K tile, V tile]
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int l32 = lane & 31, half = lane >> 5, l16 = lane & 15;
   const int wq = wave % WQ, wk = wave / WQ;
-  const int split = blockIdx.x, h = blockIdx.z;
-  const int q0 = (blockIdx.y * WQ + wq) * (QG * 32);
-  const int r0 = split * run, r1 = min(rows, r0 + run);
+  const int h = block.h, q0 = (block.tile * WQ + wq) * 32;
+  const int r0 = block.split * a.run, r1 = min(a.rows, r0 + a.run);
   const int tiles = (r1 - r0 + KT - 1) / KT;
 
-  am_bf16x8_t q[QG][8];
+  am_bf16x8_t q[8];
+  {
+    const uint16_t* src = qv + prefix_head(min(q0 + l32, a.M - 1), h, a.G, a.Hq) * kD + 8 * half;
 #pragma unroll
-  for (int g = 0; g < QG; ++g) {
-    const int r = min(q0 + 32 * g + l32, M - 1);
-    const uint16_t* src = qv + prefix_head(r, h, G, Hq) * kD + 8 * half;
-#pragma unroll
-    for (int ks = 0; ks < 8; ++ks) {
-      q[g][ks] = __builtin_bit_cast(am_bf16x8_t, load16(src + 16 * ks));
-      if constexpr (QG == 2) asm volatile("" : "+a"(q[g][ks]));  // in accumulation registers: the others are for the loads
-    }
+    for (int ks = 0; ks < 8; ++ks) q[ks] = __builtin_bit_cast(am_bf16x8_t, load16(src + 16 * ks));
   }
-  const uint16_t* kh = k + (size_t)h * cap * kD;
-  const uint16_t* vh = v + (size_t)h * cap * kD;
+  const uint16_t* kh = static_cast<const uint16_t*>(a.k) + (size_t)h * a.cap * kD;
+  const uint16_t* vh = static_cast<const uint16_t*>(a.v) + (size_t)h * a.cap * kD;
 
   uint4 kst[kChunks], vst[kChunks];
   auto load = [&](int t) __attribute__((always_inline)) {
@@ -270,22 +287,16 @@ __global__ __launch_bounds__(64 * WAVES, QG == 2 ? 1 : 2) void prefix_mfma_kerne
     }
   };
 
-  float m[QG], l[QG];
-  pf_f32x16_t o[QG][4];
+  float m = kNegBig, l = 0.f;
+  pf_f32x16_t o[4];
 #pragma unroll
-  for (int g = 0; g < QG; ++g) {
-    m[g] = kNegBig;
-    l[g] = 0.f;
-#pragma unroll
-    for (int c = 0; c < 4; ++c) o[g][c] = pf_f32x16_t{};
-  }
-  const int k_at = l32 * 256 + ((half ^ (l32 & 15)) * 16);
+  for (int c = 0; c < 4; ++c) o[c] = pf_f32x16_t{};
+  const int k_at = l32 * 256 + ((half ^ l16) * 16);
   const int v_row = 4 * half + (l16 >> 2);
   const int v_at = kTileBytes + v_row * 256 + (((((lane >> 4) & 1) * 2 + ((l16 & 3) >> 1)) ^ ((v_row & 3) << 2)) * 16) + (l16 & 1) * 8;
 
   // one step: 32 keys of the tile in buffer `base`; ENDS: only the first `there` exist
   auto step = [&](const char* base, int there, auto ends) __attribute__((always_inline)) {
-    // the operands of a product are asked for together and ahead: left to itself the compiler waits for each in turn
     am_bf16x8_t ka[8], va[2][4];
 #pragma unroll
     for (int ks = 0; ks < 8; ++ks) ka[ks] = __builtin_bit_cast(am_bf16x8_t, *reinterpret_cast<const uint4*>(base + (k_at ^ (ks * 32))));
@@ -299,61 +310,47 @@ __global__ __launch_bounds__(64 * WAVES, QG == 2 ? 1 : 2) void prefix_mfma_kerne
         const pf_s16x4_t y = __builtin_amdgcn_ds_read_tr16_b64_v4i16((pf_lds_s16x4_t*)(at + 2048));
         va[ks][c] = __builtin_bit_cast(am_bf16x8_t, __builtin_shufflevector(x, y, 0, 1, 2, 3, 4, 5, 6, 7));
       }
-    pf_f32x16_t s[QG];
+    pf_f32x16_t s = pf_f32x16_t{};
 #pragma unroll
-    for (int g = 0; g < QG; ++g) s[g] = pf_f32x16_t{};
-#pragma unroll
-    for (int ks = 0; ks < 8; ++ks)
-#pragma unroll
-      for (int g = 0; g < QG; ++g) s[g] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(ka[ks], q[g][ks], s[g], 0, 0, 0);
+    for (int ks = 0; ks < 8; ++ks) s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(ka[ks], q[ks], s, 0, 0, 0);
     __builtin_amdgcn_sched_barrier(0);
-    uint32_t w[QG][8];
+    if constexpr (decltype(ends)::value) {
 #pragma unroll
-    for (int g = 0; g < QG; ++g) {
-      if constexpr (decltype(ends)::value) {
-#pragma unroll
-        for (int i = 0; i < 16; ++i)
-          if (8 * (i >> 2) + 4 * half + (i & 3) >= there) s[g][i] = kNegBig;
-      }
-      float sum;
-      auto weights = [&]() __attribute__((always_inline)) {
-        sum = 0.f;
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          w[g][i] = BF16::round2(fast_exp2(fmaf(s[g][2 * i], kSoftmaxScaleLog2, -m[g])), fast_exp2(fmaf(s[g][2 * i + 1], kSoftmaxScaleLog2, -m[g])));
-          sum = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(pf_bf16x2_t, w[g][i]), __builtin_bit_cast(pf_bf16x2_t, 0x3f803f80u), sum, false);
-        }
-      };
-      weights();
-      if (__ballot(!(sum <= kPfGrowth)) != 0ull) {
-        float top = s[g][0];
-#pragma unroll
-        for (int i = 1; i < 16; ++i) top = fmaxf(top, s[g][i]);
-        top = fmaxf(top, __shfl_xor(top, 32)) * kSoftmaxScaleLog2;
-        const float mn = fmaxf(m[g], top), corr = fast_exp2(m[g] - mn);
-        m[g] = mn;
-        l[g] *= corr;
-#pragma unroll
-        for (int c = 0; c < 4; ++c)
-#pragma unroll
-          for (int i = 0; i < 16; ++i) o[g][c][i] *= corr;
-        // (the outputs stay in accumulation registers on both ways past here: else all of them are copied in every step)
-        if constexpr (QG == 2) {
-#pragma unroll
-          for (int c = 0; c < 4; ++c) asm volatile("" : "+a"(o[g][c]));
-        }
-        weights();
-      }
-      l[g] += sum;
+      for (int i = 0; i < 16; ++i)
+        if (8 * (i >> 2) + 4 * half + (i & 3) >= there) s[i] = kNegBig;
     }
+    uint32_t w[8];
+    float sum;
+    auto weights = [&]() __attribute__((always_inline)) {
+      sum = 0.f;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        w[i] = BF16::round2(fast_exp2(fmaf(s[2 * i], kSoftmaxScaleLog2, -m)), fast_exp2(fmaf(s[2 * i + 1], kSoftmaxScaleLog2, -m)));
+        sum = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(pf_bf16x2_t, w[i]), __builtin_bit_cast(pf_bf16x2_t, 0x3f803f80u), sum, false);
+      }
+    };
+    weights();
+    if (__ballot(!(sum <= kPfGrowth)) != 0ull) {
+      float top = s[0];
+#pragma unroll
+      for (int i = 1; i < 16; ++i) top = fmaxf(top, s[i]);
+      top = fmaxf(top, __shfl_xor(top, 32)) * kSoftmaxScaleLog2;
+      const float mn = fmaxf(m, top), corr = fast_exp2(m - mn);
+      m = mn;
+      l *= corr;
+#pragma unroll
+      for (int c = 0; c < 4; ++c)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) o[c][i] *= corr;
+      weights();
+    }
+    l += sum;
 #pragma unroll
     for (int ks = 0; ks < 2; ++ks)
 #pragma unroll
       for (int c = 0; c < 4; ++c)
-#pragma unroll
-        for (int g = 0; g < QG; ++g)
-          o[g][c] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
-              va[ks][c], __builtin_bit_cast(am_bf16x8_t, make_uint4(w[g][4 * ks], w[g][4 * ks + 1], w[g][4 * ks + 2], w[g][4 * ks + 3])), o[g][c], 0, 0, 0);
+        o[c] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(va[ks][c], __builtin_bit_cast(am_bf16x8_t, make_uint4(w[4 * ks], w[4 * ks + 1], w[4 * ks + 2], w[4 * ks + 3])),
+                                                       o[c], 0, 0, 0);
   };
 
   load(0);
@@ -374,60 +371,50 @@ __global__ __launch_bounds__(64 * WAVES, QG == 2 ? 1 : 2) void prefix_mfma_kerne
   __syncthreads();
 
   // both halves of a query's keys; then the waves that had other keys of the same queries
-#pragma unroll
-  for (int g = 0; g < QG; ++g) l[g] += __shfl_xor(l[g], 32);
+  l += __shfl_xor(l, 32);
   if constexpr (WK > 1) {
-    float* ml = reinterpret_cast<float*>(smem);  // [wave][QG][32] (max, sum)
-    float4* ob = reinterpret_cast<float4*>(smem + WAVES * QG * 32 * 8);  // [wave of the upper half][QG][4][4][lane]
-#pragma unroll
-    for (int g = 0; g < QG; ++g)
-      if (half == 0) *reinterpret_cast<float2*>(ml + ((wave * QG + g) * 32 + l32) * 2) = make_float2(m[g], l[g]);
+    float2* ml = reinterpret_cast<float2*>(smem);                       // [wave][32] (max, sum)
+    float4* ob = reinterpret_cast<float4*>(smem + WAVES * 32 * 8);      // [wave of the upper half][4][4][lane]
+    if (half == 0) ml[wave * 32 + l32] = make_float2(m, l);
     __syncthreads();
+    float mn = kNegBig, ls = 0.f;
 #pragma unroll
-    for (int g = 0; g < QG; ++g) {
-      float mn = kNegBig, ls = 0.f;
+    for (int w = 0; w < WK; ++w) mn = fmaxf(mn, ml[(w * WQ + wq) * 32 + l32].x);
 #pragma unroll
-      for (int w = 0; w < WK; ++w) mn = fmaxf(mn, ml[(((w * WQ + wq) * QG + g) * 32 + l32) * 2]);
-#pragma unroll
-      for (int w = 0; w < WK; ++w) {
-        const float2 x = *reinterpret_cast<const float2*>(ml + (((w * WQ + wq) * QG + g) * 32 + l32) * 2);
-        ls = fmaf(x.y, fast_exp2(x.x - mn), ls);
-      }
-      const float f = fast_exp2(m[g] - mn);
-      m[g] = mn;
-      l[g] = ls;
-#pragma unroll
-      for (int c = 0; c < 4; ++c)
-#pragma unroll
-        for (int i = 0; i < 16; ++i) o[g][c][i] *= f;
+    for (int w = 0; w < WK; ++w) {
+      const float2 x = ml[(w * WQ + wq) * 32 + l32];
+      ls = fmaf(x.y, fast_exp2(x.x - mn), ls);
     }
+    const float f = fast_exp2(m - mn);
+    m = mn;
+    l = ls;
+#pragma unroll
+    for (int c = 0; c < 4; ++c)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) o[c][i] *= f;
 #pragma unroll
     for (int n = WK / 2; n >= 1; n /= 2) {
       if (wk >= n && wk < 2 * n) {
-        float4* dst = ob + (size_t)((wk - n) * WQ + wq) * QG * 16 * 64;
+        float4* dst = ob + ((wk - n) * WQ + wq) * 16 * 64;
 #pragma unroll
-        for (int g = 0; g < QG; ++g)
+        for (int c = 0; c < 4; ++c)
 #pragma unroll
-          for (int c = 0; c < 4; ++c)
-#pragma unroll
-            for (int i = 0; i < 4; ++i)
-              dst[((g * 4 + c) * 4 + i) * 64 + lane] = make_float4(o[g][c][4 * i], o[g][c][4 * i + 1], o[g][c][4 * i + 2], o[g][c][4 * i + 3]);
+          for (int i = 0; i < 4; ++i)
+            dst[(c * 4 + i) * 64 + lane] = make_float4(o[c][4 * i], o[c][4 * i + 1], o[c][4 * i + 2], o[c][4 * i + 3]);
       }
       __syncthreads();
       if (wk < n) {
-        const float4* src = ob + (size_t)(wk * WQ + wq) * QG * 16 * 64;
+        const float4* src = ob + (wk * WQ + wq) * 16 * 64;
 #pragma unroll
-        for (int g = 0; g < QG; ++g)
+        for (int c = 0; c < 4; ++c)
 #pragma unroll
-          for (int c = 0; c < 4; ++c)
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-              const float4 x = src[((g * 4 + c) * 4 + i) * 64 + lane];
-              o[g][c][4 * i] += x.x;
-              o[g][c][4 * i + 1] += x.y;
-              o[g][c][4 * i + 2] += x.z;
-              o[g][c][4 * i + 3] += x.w;
-            }
+          for (int i = 0; i < 4; ++i) {
+            const float4 x = src[(c * 4 + i) * 64 + lane];
+            o[c][4 * i] += x.x;
+            o[c][4 * i + 1] += x.y;
+            o[c][4 * i + 2] += x.z;
+            o[c][4 * i + 3] += x.w;
+          }
       }
       __syncthreads();
     }
@@ -436,33 +423,67 @@ __global__ __launch_bounds__(64 * WAVES, QG == 2 ? 1 : 2) void prefix_mfma_kerne
   // a lane has four columns of one query at a time: through LDS, so that a store takes four half rows
   char* mine = smem + wave * 8192;  // [32 queries][64 columns], 16-byte chunks exchanged as the keys'
 #pragma unroll
-  for (int g = 0; g < QG; ++g) {
+  for (int pass = 0; pass < 2; ++pass) {
 #pragma unroll
-    for (int pass = 0; pass < 2; ++pass) {
+    for (int c = 0; c < 2; ++c)
 #pragma unroll
-      for (int c = 0; c < 2; ++c)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const pf_f32x16_t& x = o[g][2 * pass + c];
-          *reinterpret_cast<float4*>(mine + l32 * 256 + (((8 * c + 2 * i + half) ^ l16) * 16)) = make_float4(x[4 * i], x[4 * i + 1], x[4 * i + 2], x[4 * i + 3]);
-        }
-      __builtin_amdgcn_wave_barrier();
-#pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        const int row = 4 * j + (lane >> 4), r = q0 + 32 * g + row;
-        const float4 x = *reinterpret_cast<const float4*>(mine + row * 256 + ((l16 ^ (row & 15)) * 16));
-        if (r < M) *reinterpret_cast<float4*>(partial + (prefix_head(r, h, G, Hq) * gridDim.x + split) * kPartStride + 64 * pass + 4 * l16) = x;
+      for (int i = 0; i < 4; ++i) {
+        const pf_f32x16_t& x = o[2 * pass + c];
+        *reinterpret_cast<float4*>(mine + l32 * 256 + (((8 * c + 2 * i + half) ^ l16) * 16)) = make_float4(x[4 * i], x[4 * i + 1], x[4 * i + 2], x[4 * i + 3]);
       }
-      __builtin_amdgcn_wave_barrier();
+    __builtin_amdgcn_wave_barrier();
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      const int row = 4 * j + (lane >> 4), r = q0 + row;
+      const float4 x = *reinterpret_cast<const float4*>(mine + row * 256 + ((l16 ^ (row & 15)) * 16));
+      if (r < a.M) *reinterpret_cast<float4*>(a.partial + (prefix_head(r, h, a.G, a.Hq) * a.splits + block.split) * kPartStride + 64 * pass + 4 * l16) = x;
     }
-    const int r = q0 + 32 * g + l32;
-    if (half == 0 && r < M)
-      *reinterpret_cast<float2*>(partial + (prefix_head(r, h, G, Hq) * gridDim.x + split) * kPartStride + kD) = make_float2(m[g], l[g]);
+    __builtin_amdgcn_wave_barrier();
   }
+  const int r = q0 + l32;
+  if (half == 0 && r < a.M)
+    *reinterpret_cast<float2*>(a.partial + (prefix_head(r, h, a.G, a.Hq) * a.splits + block.split) * kPartStride + kD) = make_float2(m, l);
+}
+
+// ---- the launch -----------------------------------------------------------------------------------------------
+// The sequences' own rows: q, their parts and how they are dealt out.
+struct OwnArgs {
+  const void *k, *v;
+  float* partial;
+  int B, Hkv, S_cap, S_max, nsplit;
+  Ragged rg;
+};
+
+// Blocks [0, splits tiles Hkv): the prefix; behind them X = nsplit B blocks for every KV head.  (Neighbours in the grid are
+// runs of the prefix, so the tiles of a run, which read the same rows, go to one XCD where the runs are a multiple of 8.)
+// KIND: bf16: WQ; fp32: -QG.
+template <typename T, int NH, int WAVES, int KIND>
+__global__ __launch_bounds__(64 * WAVES, KIND == -1 ? 3 : KIND == -4 ? 1 : 2) void shared_kernel(const void* __restrict__ q, PrefixArgs pa, OwnArgs oa) {
+  extern __shared__ __align__(16) char smem[];
+  const int prefix_blocks = pa.splits * pa.tiles * oa.Hkv;
+  if ((int)blockIdx.x < prefix_blocks) {
+    const int id = blockIdx.x, rest = id / pa.splits;
+    const PrefixAt block{id - rest * pa.splits, rest % pa.tiles, rest / pa.tiles};
+    if constexpr (T::EPC == 8)
+      prefix_mfma_body<WAVES, KIND>(smem, block, static_cast<const uint16_t*>(q), pa);
+    else
+      prefix_f32_body<-KIND>(smem, block, static_cast<const float*>(q), pa);
+    return;
+  }
+  const int X = oa.nsplit * oa.B, id = (int)blockIdx.x - prefix_blocks, h = id / X, x = id - h * X;
+  const Dealt d = deal_runs(oa.rg, oa.B, oa.S_max, oa.nsplit);
+  const RunAt at = find_run(oa.rg, oa.B, oa.S_max, d.run, x);
+  if (at.b >= oa.B) return;  // uniform for the block
+  const int form_now = oa.rg.loads.form == kByLengths ? form_of(oa.rg.loads, {d.total, 0.f}) : oa.rg.loads.form;
+  auto& s_merge = *reinterpret_cast<MergeSmem<WAVES, NH>*>(smem);
+  with_form<kPastCaches>(form_now, [&](auto form) __attribute__((always_inline)) {
+    parts_body<T, NH, false, decltype(form)::value != kThroughCaches, WAVES>(s_merge, nullptr, at, d.run, h, x, X, oa.k, oa.v, q, oa.partial,
+                                                                             nullptr, 0, oa.Hkv, oa.S_cap);
+  });
 }
 
 // The block's queries and tiles for M query rows: as few blocks of queries as possible, and waves on different keys where
-// they do not fill four waves.
+// they do not fill them.
 struct PrefixShape {
   int queries, keys, blocks_per_cu;  // of a block; keys: what a run is a multiple of
 };
@@ -475,10 +496,14 @@ static PrefixShape prefix_shape(const Shape& s) {
   return {256, 64, 1};
 }
 
+static int prefix_tiles(const Shape& s) {
+  const int nq = prefix_shape(s).queries;
+  return (s.B * s.G + nq - 1) / nq;
+}
+
 static int prefix_run(const Shape& s, int rows) {
   const PrefixShape ps = prefix_shape(s);
-  const int tiles = s.Hkv * ((s.B * s.G + ps.queries - 1) / ps.queries);
-  int n = ps.blocks_per_cu * device_cus() / tiles;
+  int n = ps.blocks_per_cu * device_cus() / (s.Hkv * prefix_tiles(s));
   if (n < 1) n = 1;
   const int run = (rows + n - 1) / n;
   return (run + ps.keys - 1) / ps.keys * ps.keys;
@@ -490,44 +515,71 @@ int prefix_splits(const Shape& s, int prefix_rows) {
   return (prefix_rows + run - 1) / run;
 }
 
-template <int QG, int WAVES, int WQ>
-static hipError_t launch_prefix_mfma(const Shape& s, int splits, const void* q, const void* k, const void* v,
-                                     int rows, int cap, float* partial, hipStream_t st) {
+// One launch for the prefix and the sequences' own rows while the latter are few: a launch less, but their blocks then have
+// the registers and LDS of the prefix's and eight waves fill a CU.  us in one / in two launches: 3 sequences of 32/8 heads behind
+// 700 rows with 30 of their own 10.4 / 15.4, 8 behind 2048 with 300 (10 MB) 14.2 / 18.6; 8 of 32/16 heads behind 4096 with 500
+// (33 MB) 23.5 / 22.0, 32 of 32/8 with 1500 (197 MB) 44.5 / 41.3, 16 of 32/32 with 2048 (537 MB) 99.6 / 76.6.
+static bool in_one_launch(const Shape& s) {
+  return (double)s.B * s.Hkv * s.S * (2 * kD * s.elem_bytes) < 24e6;
+}
+
+// Runs of a sequence's own rows: blocks of 8 waves take 256 rows to have a step for each.
+int shared_own_splits(const Shape& s) {
+  if (s.S < 1) return 0;
+  if (!in_one_launch(s)) return weigh_splits(s);
+  const int units = s.B * s.Hkv, waves = s.dtype == 0 || prefix_shape(s).queries == 32 ? 4 : 8;
+  int n = ((s.dtype == 0 ? 8 : 24 / waves) * device_cus() + units - 1) / units;
+  const int most = (s.S + 32 * waves - 1) / (32 * waves);
+  if (n > most) n = most;
+  return n < 1 ? 1 : n;
+}
+
+template <typename T, int NH, int WAVES, int KIND>
+static hipError_t launch_shared_k(const Shape& s, const void* q, const PrefixArgs& pa, const OwnArgs& oa, hipStream_t st) {
   static std::atomic<unsigned long long> raised{0};
-  constexpr int bytes = pf_lds_bytes<QG, WAVES, WQ>();
-  const hipError_t e = allow_dynamic_lds(reinterpret_cast<const void*>(&prefix_mfma_kernel<QG, WAVES, WQ>), bytes, raised);
+  int bytes = (int)sizeof(MergeSmem<WAVES, NH>);
+  if constexpr (T::EPC == 8)
+    bytes = max(bytes, pf_lds_bytes<WAVES, KIND>());
+  else
+    bytes = max(bytes, (int)sizeof(PrefixF32Smem<-KIND>));
+  const hipError_t e = allow_dynamic_lds(reinterpret_cast<const void*>(&shared_kernel<T, NH, WAVES, KIND>), bytes, raised);
   if (e != hipSuccess) return e;
-  const int M = s.B * s.G, nq = QG * WQ * 32;
-  hipLaunchKernelGGL((prefix_mfma_kernel<QG, WAVES, WQ>), dim3(splits, (M + nq - 1) / nq, s.Hkv), dim3(64 * WAVES), bytes, st,
-                     static_cast<const uint16_t*>(k), static_cast<const uint16_t*>(v), static_cast<const uint16_t*>(q), partial, M, s.G,
-                     s.Hq, rows, cap, prefix_run(s, rows));
+  const int blocks = pa.splits * pa.tiles * s.Hkv + oa.nsplit * s.B * s.Hkv;
+  if (blocks < 1) return hipSuccess;  // no rows at all
+  hipLaunchKernelGGL((shared_kernel<T, NH, WAVES, KIND>), dim3(blocks), dim3(64 * WAVES), bytes, st, q, pa, oa);
   return hipGetLastError();
 }
 
-template <int QG>
-static hipError_t launch_prefix_f32(const Shape& s, int splits, const void* q, const void* k, const void* v,
-                                    int rows, int cap, float* partial, hipStream_t st) {
-  const int M = s.B * s.G, nq = QG * 16;
-  hipLaunchKernelGGL((prefix_f32_kernel<QG>), dim3(splits, (M + nq - 1) / nq, s.Hkv), dim3(kPfThreads), 0, st,
-                     static_cast<const float*>(k), static_cast<const float*>(v), static_cast<const float*>(q), partial, M, s.G, s.Hq,
-                     rows, cap, prefix_run(s, rows));
-  return hipGetLastError();
-}
-
-hipError_t launch_prefix(const Shape& s, int splits, const void* q, const void* k, const void* v, int rows,
-                         int cap, float* partial, hipStream_t st) {
+template <int NH>
+static hipError_t launch_shared_nh(const Shape& s, const void* q, const PrefixArgs& pa, const OwnArgs& oa, hipStream_t st) {
   const int nq = prefix_shape(s).queries;
-#define LOKI_PREFIX(f) return f(s, splits, q, k, v, rows, cap, partial, st)
   if (s.dtype == 0) {
-    if (nq == 16) LOKI_PREFIX(launch_prefix_f32<1>);
-    if (nq == 32) LOKI_PREFIX(launch_prefix_f32<2>);
-    LOKI_PREFIX(launch_prefix_f32<4>);
+    if (nq == 16) return launch_shared_k<F32, NH, 4, -1>(s, q, pa, oa, st);
+    if (nq == 32) return launch_shared_k<F32, NH, 4, -2>(s, q, pa, oa, st);
+    return launch_shared_k<F32, NH, 4, -4>(s, q, pa, oa, st);
   }
-  if (nq == 32) LOKI_PREFIX((launch_prefix_mfma<1, 4, 1>));
-  if (nq == 64) LOKI_PREFIX((launch_prefix_mfma<1, 8, 2>));
-  if (nq == 128) LOKI_PREFIX((launch_prefix_mfma<1, 8, 4>));
-  LOKI_PREFIX((launch_prefix_mfma<1, 8, 8>));
-#undef LOKI_PREFIX
+  if (nq == 32) return launch_shared_k<BF16, NH, 4, 1>(s, q, pa, oa, st);
+  if (nq == 64) return launch_shared_k<BF16, NH, 8, 2>(s, q, pa, oa, st);
+  if (nq == 128) return launch_shared_k<BF16, NH, 8, 4>(s, q, pa, oa, st);
+  return launch_shared_k<BF16, NH, 8, 8>(s, q, pa, oa, st);
+}
+
+hipError_t launch_shared(const Shape& s, int splits, int nsplit, const void* q, const void* k_prefix, const void* v_prefix, int rows,
+                         int cap, const void* k, const void* v, float* prefix, float* partial, hipStream_t st) {
+  const PrefixArgs pa{k_prefix, v_prefix, prefix, s.B * s.G, s.G, s.Hq, rows, cap, splits > 0 ? prefix_run(s, rows) : 0, splits, splits > 0 ? prefix_tiles(s) : 0};
+  const bool apart = nsplit > 0 && !in_one_launch(s);
+  if (apart) {
+    const hipError_t e = launch_parts(s, nsplit, q, k, v, partial, nullptr, st);
+    if (e != hipSuccess || splits == 0) return e;
+  }
+  const OwnArgs oa{k, v, partial, s.B, s.Hkv, s.S_cap, s.S, apart ? 0 : nsplit, with_loads(s, kEveryRow)};
+  switch (s.G) {
+    case 1: return launch_shared_nh<1>(s, q, pa, oa, st);
+    case 2: return launch_shared_nh<2>(s, q, pa, oa, st);
+    case 4: return launch_shared_nh<4>(s, q, pa, oa, st);
+    case 8: return launch_shared_nh<8>(s, q, pa, oa, st);
+    default: return hipErrorInvalidValue;
+  }
 }
 
 }  // namespace loki
