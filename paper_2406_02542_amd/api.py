@@ -8,6 +8,7 @@ from __future__ import annotations
 
 import ctypes
 import os
+import struct
 from typing import Optional
 
 import torch
@@ -106,7 +107,7 @@ def lib() -> ctypes.CDLL:
     L.loki_index_jaccard.restype = i32
     L.loki_index_jaccard.argtypes = [vp, vp, i32, i32, vp, vp]
     L.loki_rotary.restype = i32
-    L.loki_rotary.argtypes = [LP, i32, ctypes.POINTER(RotaryArgs), vp]
+    L.loki_rotary.argtypes = [LP, i32, vp, vp]
     L.loki_rotary_frequencies.restype = i32
     L.loki_rotary_frequencies.argtypes = [i32, ctypes.c_double, i32, ctypes.c_double, ctypes.c_double, ctypes.c_double, ctypes.c_double,
                                           vp, ctypes.POINTER(ctypes.c_float)]
@@ -117,7 +118,7 @@ def lib() -> ctypes.CDLL:
     L.loki_evict_workspace_bytes.restype = i32
     L.loki_evict_workspace_bytes.argtypes = [LP, i32, i32, ctypes.POINTER(sz)]
     L.loki_evict.restype = i32
-    L.loki_evict.argtypes = [LP, ctypes.POINTER(EvictArgs), i32, i32, i32, i32, vp, sz, vp]
+    L.loki_evict.argtypes = [LP, vp, i32, i32, i32, i32, vp, sz, vp]
     L.dense_shared_workspace_bytes.restype = i32
     L.dense_shared_workspace_bytes.argtypes = [LP, i32, i32, ctypes.POINTER(sz)]
     L.dense_decode_shared.restype = i32
@@ -184,7 +185,7 @@ def _ptr(t: Optional[torch.Tensor], name: str, dtype: Optional[torch.dtype] = No
         raise ValueError(f"{name} must live on the GPU")
     if not t.is_contiguous():
         raise ValueError(f"{name} must be contiguous")
-    if dtype is not None and t.dtype != dtype:
+    if dtype is not None and t.dtype is not dtype:
         raise ValueError(f"{name} must have dtype {dtype}, got {t.dtype}")
     if numel is not None and t.numel() < numel:
         raise ValueError(f"{name} holds {t.numel()} elements, the call reads/writes {numel}")
@@ -408,26 +409,37 @@ def loki_rotary_frequencies(rotary_dims: int, base: float = 10000.0, scaling: in
     return f.to(device), scale.value
 
 
-def _rotary_pair(t: RotaryTensor, name: str, x: torch.Tensor, y: torch.Tensor, dt: torch.dtype, B: int, n: int, heads: int,
-                 rows: int, head_major: bool) -> None:
-    """x [B, n, heads, D] to y: the same, or head-major [B, heads, rows, D]; any strides with whole rows."""
+def _refuse_rotary(name: str, x: torch.Tensor, y: Optional[torch.Tensor], shape, out_shape, dt: torch.dtype) -> None:
     if y is None:
         raise ValueError(f"{name} needs its output")
-    D = 128
     if not (x.is_cuda and y.is_cuda):
         raise ValueError(f"{name} must live on the GPU")
     if x.dtype != dt or y.dtype != dt:
         raise ValueError(f"{name} must have dtype {dt}, got {x.dtype} and {y.dtype}")
-    if tuple(x.shape) != (B, n, heads, D):
-        raise ValueError(f"{name} must be [{B}, {n}, {heads}, {D}], got {tuple(x.shape)}")
-    if tuple(y.shape) != ((B, heads, rows, D) if head_major else (B, n, heads, D)):
-        raise ValueError(f"{name}'s output has the wrong shape {tuple(y.shape)}")
-    sx, sy = x.stride(), y.stride()
-    if sx[3] != 1 or sy[3] != 1:
-        raise ValueError(f"{name}: the columns of a row must be next to each other")
-    t.in_, t.out = x.data_ptr(), y.data_ptr()
-    t.in_batch, t.in_token, t.in_head = sx[0], sx[1], sx[2]
-    t.out_batch, t.out_token, t.out_head = (sy[0], sy[2], sy[1]) if head_major else (sy[0], sy[1], sy[2])
+    if x.shape != shape:
+        raise ValueError(f"{name} must be {list(shape)}, got {tuple(x.shape)}")
+    if y.shape != out_shape:
+        raise ValueError(f"{name}'s output must be {list(out_shape)}, got {tuple(y.shape)}")
+    raise ValueError(f"{name}: the columns of a row must be next to each other")
+
+
+_NOT_THERE = (0,) * 8
+
+
+def _rotary_tensor(name: str, x: Optional[torch.Tensor], y: Optional[torch.Tensor], shape, out_shape, dt: torch.dtype, head_major: bool):
+    """The members of a ``loki_rotary_tensor``: x [B, n, heads, D] to y, of the same shape or head-major
+    [B, heads, rows, D], both with any strides of whole rows."""
+    if x is None:
+        return _NOT_THERE
+    if y is not None and x.is_cuda and y.is_cuda and x.dtype is dt and y.dtype is dt and x.shape == shape and y.shape == out_shape:
+        ib, it, ih, ic = x.stride()
+        ob, ot, oh, oc = y.stride()
+        if ic == 1 and oc == 1:
+            return (x.data_ptr(), y.data_ptr(), ib, it, ih, ob, oh, ot) if head_major else (x.data_ptr(), y.data_ptr(), ib, it, ih, ob, ot, oh)
+    _refuse_rotary(name, x, y, shape, out_shape, dt)
+
+
+_rotary_pack = struct.Struct("PPqqqqqq" * 3 + "PPPiiiif4x").pack  # RotaryArgs, filled in one go
 
 
 def loki_rotary(layout: Layout, positions: torch.Tensor, frequencies: torch.Tensor, q: Optional[torch.Tensor] = None,
@@ -442,28 +454,25 @@ def loki_rotary(layout: Layout, positions: torch.Tensor, frequencies: torch.Tens
     B, n = positions.shape
     if B != layout.B:
         raise ValueError(f"positions must be [{layout.B}, n], got {tuple(positions.shape)}")
-    if token_major and rows is not None:
-        raise ValueError("rows belong to head-major caches")
-    dt = torch.float32 if layout.dtype == LOKI_F32 else torch.bfloat16
-    a = RotaryArgs()
+    dt = _torch_dtype(layout)
+    Hq, H = layout.Hq, layout.Hkv
     n_rows = n
     if rows is not None:
         out = k_out if k_out is not None else v_out
-        if out is None:
-            raise ValueError("rows without a key or value output")
+        if out is None or token_major:
+            raise ValueError("rows are those of a head-major key or value output")
         n_rows = out.shape[2]
-    if q is not None:
-        _rotary_pair(a.q, "q", q, q_out, dt, B, n, layout.Hq, n, False)
-    if k is not None:
-        _rotary_pair(a.k, "k", k, k_out, dt, B, n, layout.Hkv, n_rows, not token_major)
-    if v is not None:
-        _rotary_pair(a.v, "v", v, v_out, dt, B, n, layout.Hkv, n_rows, not token_major)
-    a.positions = _ptr(positions, "positions", torch.int32, B * n)
-    a.rows = _ptr(rows, "rows", torch.int32, B * n)
-    a.frequencies = _ptr(frequencies, "frequencies", torch.float64, 1)
-    a.n_rows, a.rotary_dims, a.scale = n_rows, 2 * frequencies.numel(), scale
-    a.interleaved, a.inverse = interleaved, inverse
-    _check(lib().loki_rotary(ctypes.byref(layout), n, ctypes.byref(a), _stream_ptr(stream)), "loki_rotary")
+    q_shape, shape = (B, n, Hq, 128), (B, n, H, 128)
+    out_shape = shape if token_major else (B, H, n_rows, 128)
+    args = _rotary_pack(
+        *_rotary_tensor("q", q, q_out, q_shape, q_shape, dt, False),
+        *_rotary_tensor("k", k, k_out, shape, out_shape, dt, not token_major),
+        *_rotary_tensor("v", v, v_out, shape, out_shape, dt, not token_major),
+        _ptr(positions, "positions", torch.int32, 1),
+        0 if rows is None else _ptr(rows, "rows", torch.int32, B * n),
+        _ptr(frequencies, "frequencies", torch.float64, 1),
+        n_rows, 2 * frequencies.numel(), interleaved, inverse, scale)
+    _check(lib().loki_rotary(ctypes.byref(layout), n, args, _stream_ptr(stream)), "loki_rotary")
 
 
 def dense_weights_workspace_bytes(layout: Layout, S_max: int) -> int:
@@ -499,6 +508,9 @@ def loki_evict_workspace_bytes(layout: Layout, S_max: int, budget: int) -> int:
     return n.value
 
 
+_evict_pack = struct.Struct("P" * 12 + "iiii").pack  # EvictArgs
+
+
 def loki_evict(layout: Layout, weights: torch.Tensor, klo: torch.Tensor, khi: Optional[torch.Tensor], v: torch.Tensor,
                S_max: int, budget: int, sinks: int, recent: int, workspace: torch.Tensor,
                seq_lens: Optional[torch.Tensor] = None, klo_out: Optional[torch.Tensor] = None,
@@ -512,21 +524,21 @@ def loki_evict(layout: Layout, weights: torch.Tensor, klo: torch.Tensor, khi: Op
     units, D, d = layout.B * layout.Hkv, layout.D, layout.d_split
     cache_rows = (n_pages * layout.Hkv * page_rows) if page_table is not None else units * layout.S_cap
     cap_out = klo_out.numel() // (units * d) if klo_out is not None else 0
-    a = EvictArgs(
-        _ptr(seq_lens, "seq_lens", torch.int32, layout.B),
+    args = _evict_pack(
+        _ptr(seq_lens, "seq_lens", torch.int32, layout.B) or 0,
         _ptr(weights, "weights", torch.float32, units * layout.S_cap),
         _ptr(klo, "klo", dt, cache_rows * d),
-        _ptr(khi, "khi", dt, cache_rows * (D - d)),
+        _ptr(khi, "khi", dt, cache_rows * (D - d)) or 0,
         _ptr(v, "v", dt, cache_rows * D),
-        _ptr(klo_out, "klo_out", dt, units * cap_out * d),
-        _ptr(khi_out, "khi_out", dt, units * cap_out * (D - d)),
-        _ptr(v_out, "v_out", dt, units * cap_out * D),
-        _ptr(weights_out, "weights_out", torch.float32, units * cap_out),
-        _ptr(lens_out, "lens_out", torch.int32, layout.B),
-        _ptr(out_idx, "out_idx", torch.int32, units * budget),
-        _ptr(page_table, "page_table", torch.int32, layout.B),
+        _ptr(klo_out, "klo_out", dt, units * cap_out * d) or 0,
+        _ptr(khi_out, "khi_out", dt, units * cap_out * (D - d)) or 0,
+        _ptr(v_out, "v_out", dt, units * cap_out * D) or 0,
+        _ptr(weights_out, "weights_out", torch.float32, units * cap_out) or 0,
+        _ptr(lens_out, "lens_out", torch.int32, layout.B) or 0,
+        _ptr(out_idx, "out_idx", torch.int32, units * budget) or 0,
+        _ptr(page_table, "page_table", torch.int32, layout.B) or 0,
         cap_out, page_rows, (page_table.numel() // layout.B) if page_table is not None else 0, n_pages)
-    _check(lib().loki_evict(ctypes.byref(layout), ctypes.byref(a), S_max, budget, sinks, recent,
+    _check(lib().loki_evict(ctypes.byref(layout), args, S_max, budget, sinks, recent,
                             _ptr(workspace, "workspace", torch.uint8), workspace.numel(), _stream_ptr(stream)), "loki_evict")
 
 

@@ -209,6 +209,14 @@ __device__ __forceinline__ float wave_sum_f32(float x) {
   return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(x), 63));
 }
 
+// The maximum over the wave, the same in every lane, without LDS.
+__device__ __forceinline__ float wave_max_f32(float x) {
+  x = group_allreduce_max<16>(x);
+  x = fmaxf(x, __uint_as_float(dpp_u32<0x142, 0xa, false>(__float_as_uint(x))));  // (as wave_sum_f32; lanes left out see 0:
+  x = fmaxf(x, __uint_as_float(dpp_u32<0x143, 0xc, false>(__float_as_uint(x))));  // only lane 63's way there is taken)
+  return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(x), 63));
+}
+
 // The rows of a batch's entries and the rows they keep, added up; every wave for itself, lane l entries l, l + 64, ..
 struct RowSums {
   float rows, kept;

@@ -112,7 +112,19 @@ __global__ __launch_bounds__(kMgThreads) void weigh_merge_kernel(const float* __
   }
   const int r0 = (int)blockIdx.x * kMgRows;
   if (r0 >= len) return;  // uniform for the block
-  // wave w joins the maxima and sums of heads w, w + 4, .. : a lane for every 64th part
+  // the rows' logits and totals are asked for before the runs' maxima and sums are joined
+  const float* lg = logits + head0 * pitch;
+  const size_t w0 = (size_t)unit * S_cap;
+  constexpr int U = kMgRows / kMgThreads;
+  float x[U][NH], w[U];
+#pragma unroll
+  for (int u = 0; u < U; ++u) {
+    const int r = min(r0 + u * kMgThreads + tid, len - 1);
+    w[u] = weights_in != nullptr ? weights_in[w0 + r] : 0.f;
+#pragma unroll
+    for (int g = 0; g < NH; ++g) x[u][g] = lg[g * pitch + r];
+  }
+  // wave w joins heads w, w + 4, .. : a lane for every 64th part
   for (int g = wave; g < NH; g += kMgThreads / 64) {
     const PartList pl = parts(g);
     float m = kNegBig, l = 0.f;
@@ -122,39 +134,31 @@ __global__ __launch_bounds__(kMgThreads) void weigh_merge_kernel(const float* __
       l = l * fast_exp2(m - mn) + ml.y * fast_exp2(ml.x - mn);
       m = mn;
     }
-#pragma unroll
-    for (int off = 1; off < 64; off <<= 1) {
-      const float m2 = __shfl_xor(m, off), l2 = __shfl_xor(l, off), mn = fmaxf(m, m2);
-      l = l * fast_exp2(m - mn) + l2 * fast_exp2(m2 - mn);
-      m = mn;
-    }
+    const float top = wave_max_f32(m);
+    l = wave_sum_f32(l * fast_exp2(m - top));
     if (lane == 0) {
-      s_max[g] = m;
+      s_max[g] = top;
       s_inv[g] = 1.0f / l;
     }
   }
   __syncthreads();
-  const float* lg = logits + head0 * pitch;
-  const size_t w0 = (size_t)unit * S_cap;
 #pragma unroll
-  for (int u = 0; u < kMgRows / kMgThreads; ++u) {
+  for (int u = 0; u < U; ++u) {
     const int r = r0 + u * kMgThreads + tid;
-    if (r < len) {
-      float w = weights_in != nullptr ? weights_in[w0 + r] : 0.f;
 #pragma unroll
-      for (int g = 0; g < NH; ++g) w = fmaf(fast_exp2(lg[g * pitch + r] - s_max[g]), s_inv[g], w);
-      weights_out[w0 + r] = w;
-    }
+    for (int g = 0; g < NH; ++g) w[u] = fmaf(fast_exp2(x[u][g] - s_max[g]), s_inv[g], w[u]);
+    if (r < len) weights_out[w0 + r] = w[u];
   }
 }
 
-// Runs of a sequence: about four blocks per CU in bf16, eight in fp32, of at least 64 rows.  us with 2, 4, 6, 8 and 12
+// Runs of a sequence: about four blocks per CU in bf16, eight in fp32, of at least 64 rows or 128.  us with 2, 4, 6, 8 and 12
 // per CU: 16 sequences of 32/8 bf16 heads up to 16384 rows 162, 144, 147, 145, 148; 5 of 24 fp32 heads up to 2311 rows
 // 43.5, 41.2, 38.4, 38.3, 38.8.
 int weigh_splits(const Shape& s) {
   const int units = s.B * s.Hkv;
   int n = ((s.dtype == 1 ? 4 : 8) * device_cus() + units - 1) / units;
-  const int most = (s.S + 63) / 64;
+  const int rows = s.dtype == 1 && s.G >= 4 ? 128 : 64;  // a step of the matrix cores for every wave
+  const int most = (s.S + rows - 1) / rows;
   if (n > most) n = most;
   return n < 1 ? 1 : n;
 }
