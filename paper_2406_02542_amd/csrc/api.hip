@@ -810,9 +810,12 @@ int dense_decode_weights(const loki_layout* layout, const void* q, const void* k
   if (rc != LOKI_OK) return rc;
   if (!q || !k_full || !v || !weights_out || !out || !workspace) return LOKI_ERR_INVALID_ARG;
   if (S_max < 1 || S_max > s.S_cap) return LOKI_ERR_INVALID_ARG;
-  if (!aligned16(q) || !aligned16(k_full) || !aligned16(v) || !aligned16(out) || !aligned16(weights_in) || !aligned16(weights_out))
+  if (!aligned16(q) || !aligned16(k_full) || !aligned16(v) || !aligned16(out))
     return LOKI_ERR_ALIGNMENT;
-  if (!aligned256(workspace) || (reinterpret_cast<uintptr_t>(seq_lens) & 3u)) return LOKI_ERR_ALIGNMENT;
+  const void* words[] = {seq_lens, weights_in, weights_out};
+  for (const void* p : words)
+    if (reinterpret_cast<uintptr_t>(p) & 3u) return LOKI_ERR_ALIGNMENT;
+  if (!aligned256(workspace)) return LOKI_ERR_ALIGNMENT;
   s.S = S_max;
   s.rg.seq_lens = seq_lens;
   const int nsplit = weigh_splits(s);

@@ -140,7 +140,7 @@ template <bool GATHER, int KSTEPS, int QT, bool STREAM_V, typename Steps, typena
 __device__ __forceinline__ void am_attend_rows(const AmAddr<KSTEPS>& ad,
                                                const am_bf16x8_t (&bq)[KSTEPS][QT],
                                                const int32_t* s_idx, int r0, Steps steps, AmState& st, Complete complete,
-                                               Logits&& logits = {}) {
+                                               Logits logits = {}) {
   const int lane = threadIdx.x & 63;
   const int r16 = lane & 15, kgrp = lane >> 4;
   int base, end;
@@ -265,7 +265,7 @@ __device__ __forceinline__ void am_attend_rows(const AmAddr<KSTEPS>& ad,
       st.o[c] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a_hi, bv, st.o[c], 0, 0, 0);
     }
     issue_v(base, end);
-    if constexpr (std::remove_reference_t<Logits>::kAny) {  // entries b0 + 16 t + 4 kgrp .. + 3 of head r16; those at or past r1 are not there
+    if constexpr (Logits::kAny) {  // entries b0 + 16 t + 4 kgrp .. + 3 of head r16; those at or past r1 are not there
 #pragma unroll
       for (int t = 0; t < 2; ++t) logits(r16, 16 * t + 4 * kgrp, make_float4(logit[t][0], logit[t][1], logit[t][2], logit[t][3]));
       logits.step(b0);

@@ -76,7 +76,15 @@ __global__ __launch_bounds__(kEvThreads) void evict_select_kernel(EvictArgs a, i
       for (int i = 0; i < NK; ++i)
         if (i < rounds) f(i, reg[i]);
     } else {
-      for (int i = 0; i < rounds; ++i) f(i, key_of(i, load(i)));
+      constexpr int U = 16;
+      for (int i0 = 0; i0 < rounds; i0 += U) {
+        float x[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) x[u] = load(i0 + u);
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+          if (i0 + u < rounds) f(i0 + u, key_of(i0 + u, x[u]));
+      }
     }
   };
 
@@ -126,6 +134,8 @@ __global__ __launch_bounds__(kEvThreads) void evict_select_kernel(EvictArgs a, i
     all_equal = s_pick[2] == left;
   }
 
+  // (totals that change while they are read again, as those of more rows than registers hold are, cannot leave the list:
+  // its places are checked below, and its rows where they are moved)
   // kept rows of every wave's segment, then each wave writes its part of the list; equal keys that do not all stay are
   // counted too
   if (all_equal && need > 0u) --last;  // (a key is at least 1) all of them are above it then
@@ -142,7 +152,8 @@ __global__ __launch_bounds__(kEvThreads) void evict_select_kernel(EvictArgs a, i
   if (all_equal) {
     each([&](int i, uint32_t key) {
       const unsigned long long m = __ballot(key > last);
-      if (key > last) out[at + __builtin_amdgcn_mbcnt_hi((uint32_t)(m >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)m, 0u))] = first + 64 * i;
+      const uint32_t to = at + __builtin_amdgcn_mbcnt_hi((uint32_t)(m >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)m, 0u));
+      if (key > last && to < (uint32_t)kept) out[to] = first + 64 * i;
       at += (uint32_t)__popcll(m);
     });
     return;
@@ -154,7 +165,8 @@ __global__ __launch_bounds__(kEvThreads) void evict_select_kernel(EvictArgs a, i
     const unsigned long long m_equal = __ballot(key == last);
     const bool keep = key > last || (key == last && eq + (uint32_t)__popcll(m_equal & below) < equal_kept);
     const unsigned long long m = __ballot(keep);
-    if (keep) out[at + (uint32_t)__popcll(m & below)] = first + 64 * i;
+    const uint32_t to = at + (uint32_t)__popcll(m & below);
+    if (keep && to < (uint32_t)kept) out[to] = first + 64 * i;
     at += (uint32_t)__popcll(m);
     eq += (uint32_t)__popcll(m_equal);
   });
@@ -180,7 +192,7 @@ template <int CHUNKS, int FORM>  // CHUNKS: of 16 bytes, of a key and a value ro
 __global__ __launch_bounds__(kMvThreads) void evict_copy_kernel(EvictArgs a, const int32_t* __restrict__ list,
                                                                 const int32_t* __restrict__ kept_rows, int rows) {
   const int unit = blockIdx.y, b = unit / a.Hkv, h = unit - b * a.Hkv, tid = threadIdx.x;
-  const int j0 = blockIdx.x * rows, j1 = min(a.budget, j0 + rows);
+  const int j0 = blockIdx.x * rows, j1 = min(min(a.budget, a.S_max), j0 + rows);
   if (blockIdx.x == 0 && h == 0 && tid == 0 && a.lens_out != nullptr) a.lens_out[b] = kept_rows[unit];
   const int32_t* from = list + (size_t)unit * a.budget;
   if (from[j0] < 0) return;  // uniform for the block
@@ -196,7 +208,7 @@ __global__ __launch_bounds__(kMvThreads) void evict_copy_kernel(EvictArgs a, con
 #pragma unroll
     for (int u = 0; u < kMvInFlight; ++u)
       x[u] = load16_hint<FORM != kThroughCaches>(
-          evict_chunk(src, cache_row(a.pg, b, h, a.Hkv, a.S_cap, max(at[u], 0)), (i0 + u * kMvThreads) % CHUNKS, CHUNKS / 2, a.nlo));
+          evict_chunk(src, cache_row(a.pg, b, h, a.Hkv, a.S_cap, min(max(at[u], 0), a.S_max - 1)), (i0 + u * kMvThreads) % CHUNKS, CHUNKS / 2, a.nlo));
 #pragma unroll
     for (int u = 0; u < kMvInFlight; ++u) {
       const int i = i0 + u * kMvThreads;
@@ -204,7 +216,8 @@ __global__ __launch_bounds__(kMvThreads) void evict_copy_kernel(EvictArgs a, con
     }
   }
   if (a.weights_out != nullptr)
-    for (int j = j0 + tid; j < j1 && from[j] >= 0; j += kMvThreads) a.weights_out[out0 + j] = a.weights[(size_t)unit * a.S_cap + from[j]];
+    for (int j = j0 + tid; j < j1 && from[j] >= 0; j += kMvThreads)
+      a.weights_out[out0 + j] = a.weights[(size_t)unit * a.S_cap + min(from[j], a.S_max - 1)];
 }
 
 // Every source of a run has been read, by all waves, before one of its rows is overwritten.
@@ -232,7 +245,7 @@ __global__ __launch_bounds__(kIpThreads) void evict_compact_kernel(EvictArgs a, 
 #pragma unroll
       for (int u = 0; u < 4; ++u) {
         const int j = j0 + u * kIpThreads + tid;
-        x[u] = j < kept ? w[from[j]] : 0.f;
+        x[u] = w[min(max(from[min(j, kept - 1)], 0), a.S_max - 1)];
       }
       evict_all_read();
 #pragma unroll
@@ -253,11 +266,12 @@ __global__ __launch_bounds__(kIpThreads) void evict_compact_kernel(EvictArgs a, 
 #pragma unroll
     for (int u = 0; u < U; ++u) {
       const int j = j0 + u * kIpRows + r;
-      at[u] = j < kept ? from[j] : j;
+      at[u] = from[min(j, kept - 1)];
     }
 #pragma unroll
     for (int u = 0; u < U; ++u) {
       const int j = j0 + u * kIpRows + r;
+      at[u] = j < kept ? min(max(at[u], 0), a.S_max - 1) : j;
       if (at[u] != j) y[u] = load16(evict_chunk(x, cache_row(a.pg, b, h, a.Hkv, a.S_cap, at[u]), c, nk, a.nlo));
     }
     evict_all_read();
@@ -289,10 +303,11 @@ hipError_t launch_evict_move(const Shape& s, const EvictArgs& a, const int32_t* 
     return hipGetLastError();
   }
   const int rows = kMvThreads * kMvInFlight / chunks;
-  const dim3 grid((a.budget + rows - 1) / rows, units), block(kMvThreads);
+  const int most = a.budget < a.S_max ? a.budget : a.S_max;
+  const dim3 grid((most + rows - 1) / rows, units), block(kMvThreads);
   // By the bytes that go on: rows read once, from 48 MB past the caches, from 120 MB written past them too.  us through /
   // loads / both past: 34 MB 21.8 / 23.0 / 22.5, 67 39.4 / 33.5 / 35.2, 92 52.4 / 44.8 / 46.8, 134 72.2 / 68.6 / 64.1.
-  const double moved = (double)units * (a.budget < a.S_max ? a.budget : a.S_max) * 16 * chunks;
+  const double moved = (double)units * most * 16 * chunks;
   const int form = moved < 48e6 ? kThroughCaches : moved < 120e6 ? kPastCaches : kBothPast;
 #define LOKI_EVICT_COPY(C)                                                                                            \
   if (form == kThroughCaches)                                                                                         \

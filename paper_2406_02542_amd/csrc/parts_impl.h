@@ -83,6 +83,14 @@ __device__ __forceinline__ int first_run(const Ragged& rg, int S_max, int run, i
   return at;
 }
 
+template <typename Keep>
+struct KeepIn {  // (handed over by value: the rows' loop is compiled for callers without logits too)
+  static constexpr bool kAny = true;
+  Keep* keep;
+  __device__ __forceinline__ void operator()(int g, int row, const float4& x) const { (*keep)(g, row, x); }
+  __device__ __forceinline__ void step(int b0) const { keep->step(b0); }
+};
+
 template <typename T, int NH>
 constexpr bool parts_mfma() {  // four heads and more on a bf16 cache: matrix cores (as attend_mfma_applies)
   return T::EPC == 8 && NH >= 4;
@@ -98,9 +106,9 @@ struct StoreLogits {
     if (writer && ok) p[g * pitch + row] = x;
   }
 };
-// On the matrix cores a wave keeps those of some steps in LDS and stores them together, whole lines: memory
-// operations are waited for in their order, so a store of every step is waited for with the next rows (16 sequences of 32/8
-// heads up to 16384 rows: the launch 142 us with a store in every step, NNN so, 115 without the weights).
+// On the matrix cores a wave keeps those of some steps in LDS and stores them together, whole lines: memory operations are
+// waited for in their order, so a store of every step is waited for with the next rows.  16 sequences of 32/8 heads up to
+// 16384 rows: the launch 142 us with a store in every step, 136, 130 and 131 for runs of 4, 16 and 32 steps; 118 with the stores left out.
 template <int NH>
 constexpr int kept_steps() {
   return 64 / NH;
@@ -158,7 +166,7 @@ __device__ __forceinline__ void parts_body(MergeSmem<WAVES, NH>& s_merge, float*
     st.init();
     if constexpr (LOGITS) {
       KeepLogits<NH, WAVES> keep{lg, pitch, kept + (tid >> 6) * (kept_steps<NH>() * NH * kAmRows)};
-      am_attend_rows<false, 4, 1, STREAM>(ad, bq, nullptr, r0, AmRoundRobin<WAVES>(r0, r1), st, [] {}, keep);
+      am_attend_rows<false, 4, 1, STREAM>(ad, bq, nullptr, r0, AmRoundRobin<WAVES>(r0, r1), st, [] {}, KeepIn<KeepLogits<NH, WAVES>>{&keep});
       keep.flush();
     } else
       am_attend_rows<false, 4, 1, STREAM>(ad, bq, nullptr, r0, AmRoundRobin<WAVES>(r0, r1), st, [] {});

@@ -35,7 +35,8 @@ __device__ __forceinline__ size_t prefix_head(int r, int h, int G, int Hq) {
 //   O^T[column, query] += V^T P^T   the weights as they come out of the first product are operand i's keys 4 c + i; lane (m, c)
 //                                   loads 16 bytes of each of these rows, columns 4 m .. + 3 of either half
 // A step's keys and values are in registers before it begins.  The block's waves take steps in turn and are joined in LDS.
-// 64 sequences of 64/8 heads behind 16384 rows: 324 us, 106 TFLOP/s.
+// Two groups at most, so that two waves share a SIMD: 64 sequences of 64/8 heads behind 16384 rows with one, two and four groups
+// 400, 353, 371 us (two: 103 TFLOP/s; a large fp32 product reaches 134 on this card), 16 of 32/8 behind 8192 49, 40, 50.
 typedef float pf_f32x4_t __attribute__((ext_vector_type(4)));
 constexpr int kPfSteps = 16;       // keys of a step
 constexpr float kPfGrowth = 256.0f;  // the reference of the exponentials follows the maximum when weights sum up to more
@@ -458,7 +459,7 @@ struct OwnArgs {
 // runs of the prefix, so the tiles of a run, which read the same rows, go to one XCD where the runs are a multiple of 8.)
 // KIND: bf16: WQ; fp32: -QG.
 template <typename T, int NH, int WAVES, int KIND>
-__global__ __launch_bounds__(64 * WAVES, KIND == -1 ? 3 : KIND == -4 ? 1 : 2) void shared_kernel(const void* __restrict__ q, PrefixArgs pa, OwnArgs oa) {
+__global__ __launch_bounds__(64 * WAVES, KIND == -1 ? 3 : 2) void shared_kernel(const void* __restrict__ q, PrefixArgs pa, OwnArgs oa) {
   extern __shared__ __align__(16) char smem[];
   const int prefix_blocks = pa.splits * pa.tiles * oa.Hkv;
   if ((int)blockIdx.x < prefix_blocks) {
@@ -489,7 +490,7 @@ struct PrefixShape {
 };
 static PrefixShape prefix_shape(const Shape& s) {
   const int M = s.B * s.G;
-  if (s.dtype == 0) return M <= 16 ? PrefixShape{16, 64, 3} : M <= 32 ? PrefixShape{32, 64, 2} : PrefixShape{64, 64, 1};
+  if (s.dtype == 0) return M <= 16 ? PrefixShape{16, 64, 3} : PrefixShape{32, 64, 2};
   if (M <= 32) return {32, 128, 1};
   if (M <= 64) return {64, 128, 1};
   if (M <= 128) return {128, 64, 1};
@@ -555,8 +556,7 @@ static hipError_t launch_shared_nh(const Shape& s, const void* q, const PrefixAr
   const int nq = prefix_shape(s).queries;
   if (s.dtype == 0) {
     if (nq == 16) return launch_shared_k<F32, NH, 4, -1>(s, q, pa, oa, st);
-    if (nq == 32) return launch_shared_k<F32, NH, 4, -2>(s, q, pa, oa, st);
-    return launch_shared_k<F32, NH, 4, -4>(s, q, pa, oa, st);
+    return launch_shared_k<F32, NH, 4, -2>(s, q, pa, oa, st);
   }
   if (nq == 32) return launch_shared_k<BF16, NH, 4, 1>(s, q, pa, oa, st);
   if (nq == 64) return launch_shared_k<BF16, NH, 8, 2>(s, q, pa, oa, st);

@@ -102,3 +102,69 @@ def test_a_batch_behind_a_prefix_is_the_dense_step_over_both(dtype):
             ref, _, bound, _ = attend64(last[b, h * G:(h + 1) * G], kk[b, h, :n], vv[b, h, :n], ONE_TERM[dtype])
             assert worst(out[b, h * G:(h + 1) * G], ref, bound, dtype) <= 0
             assert worst(dense[b, h * G:(h + 1) * G], ref, bound, dtype) <= 0
+
+
+def test_two_graphs_on_one_workspace():
+    """Captured weights and a captured shared step take turns on one workspace; neither leaves anything the other needs."""
+    B, Hq, Hkv, S, P = 2, 8, 2, 700, 500
+    rand = lambda *s: torch.randn(s, device="cuda").bfloat16()
+    q, k, v, kp, vp = rand(B, Hq, 128), rand(B, Hkv, S, 128), rand(B, Hkv, S, 128), rand(Hkv, P, 128), rand(Hkv, P, 128)
+    lay = api.make_layout(B, Hq, Hkv, 128, 128, S, torch.bfloat16)
+    lens = torch.tensor([S, 33], dtype=torch.int32, device="cuda")
+    ws = torch.full((max(api.dense_weights_workspace_bytes(lay, S), api.dense_shared_workspace_bytes(lay, P, S)),), 255, dtype=torch.uint8, device="cuda")
+    out, w, both = torch.empty_like(q), torch.zeros((B, Hkv, S), device="cuda"), torch.empty_like(q)
+    calls = [lambda: api.dense_decode_weights(lay, q, k, v, S, lens, None, w, ws, out),
+             lambda: api.dense_decode_shared(lay, q, kp, vp, P, k, v, S, lens, ws, both)]
+    graphs = []
+    for call in calls:
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            call()
+        graphs.append(g)
+    for step in range(4):
+        q.copy_(rand(B, Hq, 128))
+        lens.copy_(torch.tensor([S - 100 * step, 33 * step], dtype=torch.int32))
+        w.zero_()
+        for g in graphs if step % 2 else graphs[::-1]:
+            g.replay()
+        torch.cuda.synchronize()
+        got = [t.clone() for t in (out, w, both)]
+        w.zero_()
+        for call in calls:
+            call()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(got, (out, w, both)))
+
+
+def test_two_streams_with_their_own_workspaces():
+    B, Hq, Hkv, S, keep = 4, 16, 4, 3000, 500
+    lay = api.make_layout(B, Hq, Hkv, 128, 128, S, torch.bfloat16)
+    rand = lambda *s: torch.randn(s, device="cuda").bfloat16()
+    sets = []
+    for i in range(2):
+        s = dict(q=rand(B, Hq, 128), k=rand(B, Hkv, S, 128), v=rand(B, Hkv, S, 128), w=torch.rand((B, Hkv, S), device="cuda"),
+                 out=torch.empty((B, Hq, 128), dtype=torch.bfloat16, device="cuda"), idx=torch.empty((B, Hkv, keep), dtype=torch.int32, device="cuda"),
+                 ws=torch.empty(api.dense_weights_workspace_bytes(lay, S), dtype=torch.uint8, device="cuda"),
+                 we=torch.empty(api.loki_evict_workspace_bytes(lay, S, keep), dtype=torch.uint8, device="cuda"))
+        s["total"] = torch.empty_like(s["w"])
+        sets.append(s)
+
+    def work(s, k, v):
+        api.dense_decode_weights(lay, s["q"], k, v, S, None, s["w"], s["total"], s["ws"], s["out"])
+        api.loki_evict(lay, s["total"], k, None, v, S, keep, 4, 100, s["we"], out_idx=s["idx"])
+
+    alone = []
+    for s in sets:
+        k, v = s["k"].clone(), s["v"].clone()
+        work(s, k, v)
+        torch.cuda.synchronize()
+        alone.append([t.clone() for t in (s["out"], s["total"], s["idx"], k, v)])
+    streams = [torch.cuda.Stream() for _ in sets]
+    caches = [(s["k"].clone(), s["v"].clone()) for s in sets]
+    torch.cuda.synchronize()
+    for st, s, (k, v) in zip(streams, sets, caches):
+        with torch.cuda.stream(st):
+            work(s, k, v)
+    torch.cuda.synchronize()
+    for s, (k, v), ref in zip(sets, caches, alone):
+        assert all(torch.equal(a, b) for a, b in zip((s["out"], s["total"], s["idx"], k, v), ref))

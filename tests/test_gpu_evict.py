@@ -141,6 +141,13 @@ def test_pages(dtype, d, into):
     check(3, 2, 1500, 1400, [1400, 257, 900], 300, 4, 50, dtype, d, into=into, page_rows=256)
 
 
+@pytest.mark.parametrize("into", [None, 300])
+@pytest.mark.parametrize("budget", [300, 301, 5000])
+def test_nothing_has_to_go(budget, into):
+    """A bound at or beyond the rows there can be: everything stays, a shorter cache takes S_max rows."""
+    check(3, 2, 310, 300, [300, 17, 0], budget, 4, 50, "bf16", 32, into=into)
+
+
 def test_lengths_written_where_they_are_read():
     check(4, 3, 900, 900, [900, 10, 300, 301], 300, 4, 50, "bf16", 32, lens_in_place=True)
 

@@ -131,6 +131,19 @@ def test_inverse_is_the_gradient_and_undoes():
     assert float((back - x).abs().max()) <= float(x.abs().max()) * 2 * 2.0 ** -19
 
 
+def test_input_broadcast_over_heads():
+    """One key for all heads, a stride of zero."""
+    B, n, H = 2, 5, 6
+    one, pos = torch.randn((B, n, 1, 128), device="cuda").bfloat16(), torch.arange(B * n, dtype=torch.int32, device="cuda").view(B, n)
+    f, _ = api.loki_rotary_frequencies(128, 10000.0)
+    lay = api.make_layout(B, H, H, 128, 128, 64, torch.bfloat16)
+    k, k_out = one.expand(B, n, H, 128), torch.empty((B, H, n, 128), dtype=torch.bfloat16, device="cuda")
+    api.loki_rotary(lay, pos, f, k=k, k_out=k_out)
+    torch.cuda.synchronize()
+    ref, e = turned(k, pos, f, 128, False, False, 1.0)
+    check(k_out.transpose(1, 2), ref, e, "bf16", 128)
+
+
 def test_stream_and_graph():
     """On a stream of its own, captured once and replayed with new positions between."""
     B, n, Hq, Hkv = 2, 1, 8, 2
