@@ -486,15 +486,15 @@ __global__ __launch_bounds__(64 * WAVES, KIND == -1 ? 3 : 2) void shared_kernel(
 // The block's queries and tiles for M query rows: as few blocks of queries as possible, and waves on different keys where
 // they do not fill them.
 struct PrefixShape {
-  int queries, keys, blocks_per_cu;  // of a block; keys: what a run is a multiple of
+  int queries, keys;  // of a block; keys: what a run is a multiple of
 };
 static PrefixShape prefix_shape(const Shape& s) {
   const int M = s.B * s.G;
-  if (s.dtype == 0) return M <= 16 ? PrefixShape{16, 64, 3} : PrefixShape{32, 64, 2};
-  if (M <= 32) return {32, 128, 1};
-  if (M <= 64) return {64, 128, 1};
-  if (M <= 128) return {128, 64, 1};
-  return {256, 64, 1};
+  if (s.dtype == 0) return M <= 16 ? PrefixShape{16, 64} : PrefixShape{32, 64};
+  if (M <= 32) return {32, 128};
+  if (M <= 64) return {64, 128};
+  if (M <= 128) return {128, 64};
+  return {256, 64};
 }
 
 static int prefix_tiles(const Shape& s) {
@@ -503,10 +503,19 @@ static int prefix_tiles(const Shape& s) {
 }
 
 static int prefix_run(const Shape& s, int rows) {
+  // A block for every CU, also where more would fit: more runs mean more parts to write and to merge.  us with one, two and
+  // three or four per CU, fp32: 5 sequences of 16/8 heads behind 5777 rows 16.0, 16.9, 19.0, behind 20000 37.3, 38.3, 39.7; 64 of 64/8
+  // behind 6000 124, 150.
   const PrefixShape ps = prefix_shape(s);
-  int n = ps.blocks_per_cu * device_cus() / (s.Hkv * prefix_tiles(s));
+  int n = device_cus() / (s.Hkv * prefix_tiles(s));
   if (n < 1) n = 1;
-  const int run = (rows + n - 1) / n;
+  int run = (rows + n - 1) / n;
+  // Many query heads, whose parts weigh more than their products: runs of at least 256 rows from 600 heads of the batch on, of 384
+  // from 2048.  bf16, us with runs as they come / of 256 / 384 / 512: 256 heads behind 2048 rows 11.9 / 12.7 / 14.5 / 15.5, 512
+  // behind 1000 13.6 / 14.6 / 15.9 / 16.8, 640 behind 2000 23.8 / 19.9 / 17.3 / 17.5, 1024 behind 4000 22.5 / 18.2 / 19.5 / 21.3, 4096
+  // behind 2000 33.6 / 30.2 / 30.0 / 32.0, behind 4000 38.1 / 37.9 / 35.5 / 34.5.
+  const int heads = s.B * s.Hq, least = s.dtype == 0 || heads < 600 ? 1 : heads < 2048 ? 256 : 384;
+  if (run < least) run = least;
   return (run + ps.keys - 1) / ps.keys * ps.keys;
 }
 
@@ -524,13 +533,14 @@ static bool in_one_launch(const Shape& s) {
   return (double)s.B * s.Hkv * s.S * (2 * kD * s.elem_bytes) < 24e6;
 }
 
-// Runs of a sequence's own rows: blocks of 8 waves take 256 rows to have a step for each.
+// Runs of a sequence's own rows: two steps for every wave in bf16, one in fp32 (8 sequences of 32/8 bf16 heads with 300 rows
+// behind 2048: one step 14.0 us, two 11.8; 5 of 16/8 fp32 heads with 131 behind 5777 16.1, 17.1).
 int shared_own_splits(const Shape& s) {
   if (s.S < 1) return 0;
   if (!in_one_launch(s)) return weigh_splits(s);
   const int units = s.B * s.Hkv, waves = s.dtype == 0 || prefix_shape(s).queries == 32 ? 4 : 8;
   int n = ((s.dtype == 0 ? 8 : 24 / waves) * device_cus() + units - 1) / units;
-  const int most = (s.S + 32 * waves - 1) / (32 * waves);
+  const int rows = (s.dtype == 0 ? 32 : 64) * waves, most = (s.S + rows - 1) / rows;
   if (n > most) n = most;
   return n < 1 ? 1 : n;
 }
