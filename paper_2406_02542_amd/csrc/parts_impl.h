@@ -92,8 +92,8 @@ struct KeepIn {  // (handed over by value: the rows' loop is compiled for caller
 };
 
 template <typename T, int NH>
-constexpr bool parts_mfma() {  // four heads and more on a bf16 cache: matrix cores (as attend_mfma_applies)
-  return T::EPC == 8 && NH >= 4;
+constexpr bool parts_mfma() {  // four heads and more: matrix cores (fp32, with the merge: 16 sequences of 64/8 heads with 4096 rows
+  return NH >= 4;              // 181 us on the vector units, 113 so, of 32/8 113, 107; one of 32/4 with 16384 rows 37, 21)
 }
 
 // The logits of the unit's heads, [head][pitch]: on the vector units one lane of a row's group stores them.
@@ -106,7 +106,18 @@ struct StoreLogits {
     if (writer && ok) p[g * pitch + row] = x;
   }
 };
-// On the matrix cores a wave keeps those of some steps in LDS and stores them together, whole lines: memory operations are
+// fp32 on the matrix cores: four rows of a head at a time (the rows of the sequence's last step past its end lie inside the pitch,
+// which is a multiple of 32).
+template <int NH>
+struct StoreSteps {
+  static constexpr bool kAny = true;
+  float* p;
+  size_t pitch;
+  __device__ __forceinline__ void operator()(int g, int row, const float4& x) const {
+    if (g < NH) *reinterpret_cast<float4*>(p + g * pitch + row) = x;
+  }
+};
+// bf16 on the matrix cores: a wave keeps those of some steps in LDS and stores them together, whole lines: memory operations are
 // waited for in their order, so a store of every step is waited for with the next rows.  16 sequences of 32/8 heads up to
 // 16384 rows: the launch 142 us with a store in every step, 136, 130 and 131 for runs of 4, 16 and 32 steps; 118 with the stores left out.
 template <int NH>
@@ -140,9 +151,196 @@ struct KeepLogits {
   }
 };
 
+// ---- fp32 on the matrix cores, straight from registers --------------------------------------------------------------
+// A wave takes steps of 16 keys and holds QG groups of 16 query rows:
+//   S^T[key, query] = K Q^T         v_mfma_f32_16x16x4_f32; lane (key, c) loads 16 bytes of its key's row at a time, columns
+//                                   16 j + 4 c .. + 3, one for each of four products, and the queries the same columns
+//   O^T[column, query] += V^T P^T   the weights as they come out of the first product are operand i's keys 4 c + i; lane (m, c)
+//                                   loads 16 bytes of each of these rows, columns 4 m .. + 3 of either half
+// A step's keys and values are in registers before it begins.  The block's waves take steps in turn and are joined in LDS.
+// STREAM: the values come past the caches, whole lines; a key's line comes in two halves (64/8 heads, 32 sequences of 8192 rows 433 us,
+// with the keys past the caches too 454).
+// Two groups at most, so that two waves share a SIMD: 64 sequences of 64/8 heads behind 16384 rows with one, two and four groups
+// 400, 353, 371 us (two: 103 TFLOP/s; a large fp32 product reaches 134 on this card), 16 of 32/8 behind 8192 49, 40, 50.
+// The reference of the exponentials follows the maximum only when a step's weights sum up to more than 2^8.
+typedef float pf_f32x4_t __attribute__((ext_vector_type(4)));
+constexpr int kF32Keys = 16;         // of a step
+constexpr float kPfGrowth = 256.0f;
+
+template <int QG, int WAVES>
+struct AttendF32Smem {
+  float o[WAVES / 2][QG][32][64];
+  float2 ml[WAVES][QG][16];
+};
+
+// Rows [r0, r1) (r0 < r1) of the cache at k, v, by the whole block.  query(i): query row i < 16 QG; part(i): where its part goes, or
+// null; logits: as attend_rows', four rows of one query at a time (those at or past r1 are not there).
+template <int QG, int WAVES, bool STREAM, typename Query, typename Part, typename Logits>
+__device__ __forceinline__ void attend_f32(AttendF32Smem<QG, WAVES>& sm, const float* __restrict__ k, const float* __restrict__ v, int r0,
+                                           int r1, Query query, Part part, Logits logits) {
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+  const int l16 = lane & 15, c4 = lane >> 4;
+  const float *kh = k + 4 * c4, *vh = v + 4 * l16;
+
+  float4 q[QG][8];
+#pragma unroll
+  for (int g = 0; g < QG; ++g) {
+    const float* src = query(16 * g + l16) + 4 * c4;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) q[g][j] = *reinterpret_cast<const float4*>(src + 16 * j);
+  }
+  float m[QG], l[QG];
+  pf_f32x4_t o[QG][8];
+#pragma unroll
+  for (int g = 0; g < QG; ++g) {
+    m[g] = kNegBig;
+    l[g] = 0.f;
+#pragma unroll
+    for (int c = 0; c < 8; ++c) o[g][c] = pf_f32x4_t{};
+  }
+  float4 kr[8], vr[4][2];
+  auto load_k = [&](int at) __attribute__((always_inline)) {  // (past the end: the last row again)
+    const float* p = kh + (size_t)min(at + l16, r1 - 1) * kD;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) kr[j] = *reinterpret_cast<const float4*>(p + 16 * j);
+  };
+  auto load_v = [&](int at) __attribute__((always_inline)) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const float* p = vh + (size_t)min(at + 4 * c4 + i, r1 - 1) * kD;
+      vr[i][0] = __builtin_bit_cast(float4, load16_hint<STREAM>(p));
+      vr[i][1] = __builtin_bit_cast(float4, load16_hint<STREAM>(p + 64));
+    }
+  };
+  int at = r0 + wave * kF32Keys;
+  if (at < r1) {  // (uniform for the wave)
+    load_k(at);
+    load_v(at);
+  }
+  for (; at < r1; at += WAVES * kF32Keys) {
+    pf_f32x4_t s[QG];
+#pragma unroll
+    for (int g = 0; g < QG; ++g) s[g] = pf_f32x4_t{};
+#pragma unroll
+    for (int j = 0; j < 8; ++j)
+#pragma unroll
+      for (int g = 0; g < QG; ++g) {
+        s[g] = __builtin_amdgcn_mfma_f32_16x16x4f32(kr[j].x, q[g][j].x, s[g], 0, 0, 0);
+        s[g] = __builtin_amdgcn_mfma_f32_16x16x4f32(kr[j].y, q[g][j].y, s[g], 0, 0, 0);
+        s[g] = __builtin_amdgcn_mfma_f32_16x16x4f32(kr[j].z, q[g][j].z, s[g], 0, 0, 0);
+        s[g] = __builtin_amdgcn_mfma_f32_16x16x4f32(kr[j].w, q[g][j].w, s[g], 0, 0, 0);
+      }
+    load_k(at + WAVES * kF32Keys);
+#pragma unroll
+    for (int g = 0; g < QG; ++g) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) s[g][i] = at + 4 * c4 + i < r1 ? s[g][i] * kSoftmaxScaleLog2 : kNegBig;
+      if constexpr (Logits::kAny) logits(16 * g + l16, at + 4 * c4, make_float4(s[g][0], s[g][1], s[g][2], s[g][3]));
+      float p[4], sum;
+      auto weights = [&]() __attribute__((always_inline)) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) p[i] = fast_exp2(s[g][i] - m[g]);
+        sum = (p[0] + p[1]) + (p[2] + p[3]);
+      };
+      weights();
+      if (__ballot(!(sum <= kPfGrowth)) != 0ull) {
+        float top = fmaxf(fmaxf(s[g][0], s[g][1]), fmaxf(s[g][2], s[g][3]));
+        top = fmaxf(top, __shfl_xor(top, 16));
+        top = fmaxf(top, __shfl_xor(top, 32));
+        const float mn = fmaxf(m[g], top), corr = fast_exp2(m[g] - mn);
+        m[g] = mn;
+        l[g] *= corr;
+#pragma unroll
+        for (int c = 0; c < 8; ++c)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) o[g][c][i] *= corr;
+        weights();
+      }
+      l[g] += sum;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) s[g][i] = p[i];
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+      for (int g = 0; g < QG; ++g)
+#pragma unroll
+        for (int c = 0; c < 2; ++c) {
+          o[g][4 * c] = __builtin_amdgcn_mfma_f32_16x16x4f32(vr[i][c].x, s[g][i], o[g][4 * c], 0, 0, 0);
+          o[g][4 * c + 1] = __builtin_amdgcn_mfma_f32_16x16x4f32(vr[i][c].y, s[g][i], o[g][4 * c + 1], 0, 0, 0);
+          o[g][4 * c + 2] = __builtin_amdgcn_mfma_f32_16x16x4f32(vr[i][c].z, s[g][i], o[g][4 * c + 2], 0, 0, 0);
+          o[g][4 * c + 3] = __builtin_amdgcn_mfma_f32_16x16x4f32(vr[i][c].w, s[g][i], o[g][4 * c + 3], 0, 0, 0);
+        }
+    load_v(at + WAVES * kF32Keys);
+  }
+
+  // the waves' shares of the keys
+#pragma unroll
+  for (int g = 0; g < QG; ++g) {
+    l[g] += __shfl_xor(l[g], 16);
+    l[g] += __shfl_xor(l[g], 32);
+    if (c4 == 0) sm.ml[wave][g][l16] = make_float2(m[g], l[g]);
+  }
+  __syncthreads();
+#pragma unroll
+  for (int g = 0; g < QG; ++g) {
+    float mn = kNegBig, ls = 0.f;
+#pragma unroll
+    for (int w = 0; w < WAVES; ++w) mn = fmaxf(mn, sm.ml[w][g][l16].x);
+#pragma unroll
+    for (int w = 0; w < WAVES; ++w) ls = fmaf(sm.ml[w][g][l16].y, fast_exp2(sm.ml[w][g][l16].x - mn), ls);
+    const float f = fast_exp2(m[g] - mn);
+    m[g] = mn;
+    l[g] = ls;
+#pragma unroll
+    for (int c = 0; c < 8; ++c)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) o[g][c][i] *= f;
+  }
+#pragma unroll
+  for (int n = WAVES / 2; n >= 1; n /= 2) {
+    if (wave >= n && wave < 2 * n) {
+#pragma unroll
+      for (int g = 0; g < QG; ++g)
+#pragma unroll
+        for (int c = 0; c < 8; ++c)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) sm.o[wave - n][g][4 * c + i][lane] = o[g][c][i];
+    }
+    __syncthreads();
+    if (wave < n) {
+#pragma unroll
+      for (int g = 0; g < QG; ++g)
+#pragma unroll
+        for (int c = 0; c < 8; ++c)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) o[g][c][i] += sm.o[wave][g][4 * c + i][lane];
+    }
+    __syncthreads();
+  }
+  if (wave != 0) return;
+  // o[4 c + t][i] is column 64 c + 4 (4 c4 + i) + t of query l16
+#pragma unroll
+  for (int g = 0; g < QG; ++g) {
+    float* pr = part(16 * g + l16);
+    if (pr == nullptr) continue;
+#pragma unroll
+    for (int c = 0; c < 2; ++c)
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        *reinterpret_cast<float4*>(pr + 64 * c + 16 * c4 + 4 * i) =
+            make_float4(o[g][4 * c][i], o[g][4 * c + 1][i], o[g][4 * c + 2][i], o[g][4 * c + 3][i]);
+    if (c4 == 0) *reinterpret_cast<float2*>(pr + kD) = make_float2(m[g], l[g]);
+  }
+}
+
+// What a run's waves are joined through.
+template <typename T, int NH, int WAVES>
+using PartsSmem = std::conditional_t<T::EPC == 4 && parts_mfma<T, NH>(), AttendF32Smem<1, WAVES>, MergeSmem<WAVES, NH>>;
+
 // One run by a block of WAVES waves: part `x` of the X that each query head of KV head h has.
 template <typename T, int NH, bool LOGITS, bool STREAM, int WAVES>
-__device__ __forceinline__ void parts_body(MergeSmem<WAVES, NH>& s_merge, float* kept, const RunAt& at, int run, int h, int x, int X,
+__device__ __forceinline__ void parts_body(PartsSmem<T, NH, WAVES>& s_merge, float* kept, const RunAt& at, int run, int h, int x, int X,
                                            const void* __restrict__ k, const void* __restrict__ v, const void* __restrict__ qv,
                                            float* __restrict__ partial, float* __restrict__ logits, size_t pitch, int Hkv, int S_cap) {
   using ST = typename T::store_t;
@@ -152,7 +350,16 @@ __device__ __forceinline__ void parts_body(MergeSmem<WAVES, NH>& s_merge, float*
   const size_t head0 = (size_t)unit * NH;
   const ST* q = static_cast<const ST*>(qv) + head0 * kD;
   float* lg = logits + head0 * pitch;
-  if constexpr (MFMA) {
+  if constexpr (MFMA && T::EPC == 4) {
+    auto query = [&](int i) { return q + (size_t)min(i, NH - 1) * kD; };
+    auto part = [&](int i) { return i < NH ? partial + ((size_t)(h * NH + i) * X + x) * kPartStride : nullptr; };
+    const float *ku = static_cast<const float*>(k) + (size_t)unit * S_cap * kD, *vu = static_cast<const float*>(v) + (size_t)unit * S_cap * kD;
+    auto& sm = s_merge;
+    if constexpr (LOGITS)
+      attend_f32<1, WAVES, STREAM>(sm, ku, vu, r0, r1, query, part, StoreSteps<NH>{lg, pitch});
+    else
+      attend_f32<1, WAVES, STREAM>(sm, ku, vu, r0, r1, query, part, NoLogits{});
+  } else if constexpr (MFMA) {
     const int lane = tid & 63, r16 = lane & 15, kgrp = lane >> 4;
     am_bf16x8_t bq[4][1];
 #pragma unroll
@@ -188,15 +395,17 @@ __device__ __forceinline__ void parts_body(MergeSmem<WAVES, NH>& s_merge, float*
       attend_rows<T, NH, WAVES * RPW, false, false, false, false, STREAM>(acc, qr, ra, nullptr, nullptr, gid, r0, r1);
     attend_publish<T, NH, WAVES>(acc, s_merge);
   }
+  if constexpr (!(MFMA && T::EPC == 4)) {
     for (int i = tid; i < NH * kD; i += (64 * WAVES)) {
-    const int g = i / kD, col = i % kD;
-    float mn, ls, os;
-    attend_merged<WAVES, NH>(s_merge, g, col, mn, ls, os);
-    float* pr = partial + ((size_t)(h * NH + g) * X + x) * kPartStride;
-    pr[col] = os;
-    if (col == 0) {
-      pr[kD] = mn;
-      pr[kD + 1] = ls;
+      const int g = i / kD, col = i % kD;
+      float mn, ls, os;
+      attend_merged<WAVES, NH>(s_merge, g, col, mn, ls, os);
+      float* pr = partial + ((size_t)(h * NH + g) * X + x) * kPartStride;
+      pr[col] = os;
+      if (col == 0) {
+        pr[kD] = mn;
+        pr[kD + 1] = ls;
+      }
     }
   }
 }

@@ -28,186 +28,16 @@ __device__ __forceinline__ size_t prefix_head(int r, int h, int G, int Hq) {
   return (size_t)(r >> (31 - __builtin_clz(G))) * Hq + h * G + (r & (G - 1));
 }
 
-// ---- fp32: matrix cores straight from registers ------------------------------------------------------------------
-// A wave takes steps of 16 keys and holds QG groups of 16 query rows:
-//   S^T[key, query] = K Q^T         v_mfma_f32_16x16x4_f32; lane (key, c) loads 16 bytes of its key's row at a time, columns
-//                                   16 j + 4 c .. + 3, one for each of four products, and the queries the same columns
-//   O^T[column, query] += V^T P^T   the weights as they come out of the first product are operand i's keys 4 c + i; lane (m, c)
-//                                   loads 16 bytes of each of these rows, columns 4 m .. + 3 of either half
-// A step's keys and values are in registers before it begins.  The block's waves take steps in turn and are joined in LDS.
-// Two groups at most, so that two waves share a SIMD: 64 sequences of 64/8 heads behind 16384 rows with one, two and four groups
-// 400, 353, 371 us (two: 103 TFLOP/s; a large fp32 product reaches 134 on this card), 16 of 32/8 behind 8192 49, 40, 50.
-typedef float pf_f32x4_t __attribute__((ext_vector_type(4)));
-constexpr int kPfSteps = 16;       // keys of a step
-constexpr float kPfGrowth = 256.0f;  // the reference of the exponentials follows the maximum when weights sum up to more
-
-template <int QG>
-struct PrefixF32Smem {
-  float o[kPfWaves / 2][QG][32][64];
-  float2 ml[kPfWaves][QG][16];
-};
+// ---- fp32: the loop of parts_impl.h over 16 or 32 query rows of the batch at a time -------------------------------------
 template <int QG>
 __device__ __forceinline__ void prefix_f32_body(char* smem, const PrefixAt& block, const float* __restrict__ qv, const PrefixArgs& a) {
-  auto& s_o = reinterpret_cast<PrefixF32Smem<QG>*>(smem)->o;
-  auto& s_ml = reinterpret_cast<PrefixF32Smem<QG>*>(smem)->ml;
-  const int M = a.M, G = a.G, Hq = a.Hq;
-  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int l16 = lane & 15, c4 = lane >> 4;
-  const int split = block.split, h = block.h, q0 = block.tile * (QG * 16);
-  const int r0 = split * a.run, r1 = min(a.rows, r0 + a.run);
-  const float* kh = static_cast<const float*>(a.k) + (size_t)h * a.cap * kD + 4 * c4;
-  const float* vh = static_cast<const float*>(a.v) + (size_t)h * a.cap * kD + 4 * l16;
-
-  float4 q[QG][8];
-#pragma unroll
-  for (int g = 0; g < QG; ++g) {
-    const float* src = qv + prefix_head(min(q0 + 16 * g + l16, M - 1), h, G, Hq) * kD + 4 * c4;
-#pragma unroll
-    for (int j = 0; j < 8; ++j) q[g][j] = *reinterpret_cast<const float4*>(src + 16 * j);
-  }
-  float m[QG], l[QG];
-  pf_f32x4_t o[QG][8];
-#pragma unroll
-  for (int g = 0; g < QG; ++g) {
-    m[g] = kNegBig;
-    l[g] = 0.f;
-#pragma unroll
-    for (int c = 0; c < 8; ++c) o[g][c] = pf_f32x4_t{};
-  }
-  float4 kr[8], vr[4][2];
-  auto load_k = [&](int at) __attribute__((always_inline)) {  // (past the end: the last row again)
-    const float* p = kh + (size_t)min(at + l16, r1 - 1) * kD;
-#pragma unroll
-    for (int j = 0; j < 8; ++j) kr[j] = *reinterpret_cast<const float4*>(p + 16 * j);
-  };
-  auto load_v = [&](int at) __attribute__((always_inline)) {
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const float* p = vh + (size_t)min(at + 4 * c4 + i, r1 - 1) * kD;
-      vr[i][0] = *reinterpret_cast<const float4*>(p);
-      vr[i][1] = *reinterpret_cast<const float4*>(p + 64);
-    }
-  };
-  int at = r0 + wave * kPfSteps;
-  if (at < r1) {  // (uniform for the wave)
-    load_k(at);
-    load_v(at);
-  }
-  for (; at < r1; at += kPfWaves * kPfSteps) {
-    pf_f32x4_t s[QG];
-#pragma unroll
-    for (int g = 0; g < QG; ++g) s[g] = pf_f32x4_t{};
-#pragma unroll
-    for (int j = 0; j < 8; ++j)
-#pragma unroll
-      for (int g = 0; g < QG; ++g) {
-        s[g] = __builtin_amdgcn_mfma_f32_16x16x4f32(kr[j].x, q[g][j].x, s[g], 0, 0, 0);
-        s[g] = __builtin_amdgcn_mfma_f32_16x16x4f32(kr[j].y, q[g][j].y, s[g], 0, 0, 0);
-        s[g] = __builtin_amdgcn_mfma_f32_16x16x4f32(kr[j].z, q[g][j].z, s[g], 0, 0, 0);
-        s[g] = __builtin_amdgcn_mfma_f32_16x16x4f32(kr[j].w, q[g][j].w, s[g], 0, 0, 0);
-      }
-    load_k(at + kPfWaves * kPfSteps);
-#pragma unroll
-    for (int g = 0; g < QG; ++g) {
-#pragma unroll
-      for (int i = 0; i < 4; ++i) s[g][i] = at + 4 * c4 + i < r1 ? s[g][i] * kSoftmaxScaleLog2 : kNegBig;
-      float p[4], sum;
-      auto weights = [&]() __attribute__((always_inline)) {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) p[i] = fast_exp2(s[g][i] - m[g]);
-        sum = (p[0] + p[1]) + (p[2] + p[3]);
-      };
-      weights();
-      if (__ballot(!(sum <= kPfGrowth)) != 0ull) {
-        float top = fmaxf(fmaxf(s[g][0], s[g][1]), fmaxf(s[g][2], s[g][3]));
-        top = fmaxf(top, __shfl_xor(top, 16));
-        top = fmaxf(top, __shfl_xor(top, 32));
-        const float mn = fmaxf(m[g], top), corr = fast_exp2(m[g] - mn);
-        m[g] = mn;
-        l[g] *= corr;
-#pragma unroll
-        for (int c = 0; c < 8; ++c)
-#pragma unroll
-          for (int i = 0; i < 4; ++i) o[g][c][i] *= corr;
-        weights();
-      }
-      l[g] += sum;
-#pragma unroll
-      for (int i = 0; i < 4; ++i) s[g][i] = p[i];
-    }
-#pragma unroll
-    for (int i = 0; i < 4; ++i)
-#pragma unroll
-      for (int g = 0; g < QG; ++g)
-#pragma unroll
-        for (int c = 0; c < 2; ++c) {
-          o[g][4 * c] = __builtin_amdgcn_mfma_f32_16x16x4f32(vr[i][c].x, s[g][i], o[g][4 * c], 0, 0, 0);
-          o[g][4 * c + 1] = __builtin_amdgcn_mfma_f32_16x16x4f32(vr[i][c].y, s[g][i], o[g][4 * c + 1], 0, 0, 0);
-          o[g][4 * c + 2] = __builtin_amdgcn_mfma_f32_16x16x4f32(vr[i][c].z, s[g][i], o[g][4 * c + 2], 0, 0, 0);
-          o[g][4 * c + 3] = __builtin_amdgcn_mfma_f32_16x16x4f32(vr[i][c].w, s[g][i], o[g][4 * c + 3], 0, 0, 0);
-        }
-    load_v(at + kPfWaves * kPfSteps);
-  }
-
-  // the four waves' shares of the keys
-#pragma unroll
-  for (int g = 0; g < QG; ++g) {
-    l[g] += __shfl_xor(l[g], 16);
-    l[g] += __shfl_xor(l[g], 32);
-    if (c4 == 0) s_ml[wave][g][l16] = make_float2(m[g], l[g]);
-  }
-  __syncthreads();
-#pragma unroll
-  for (int g = 0; g < QG; ++g) {
-    float mn = kNegBig, ls = 0.f;
-#pragma unroll
-    for (int w = 0; w < kPfWaves; ++w) mn = fmaxf(mn, s_ml[w][g][l16].x);
-#pragma unroll
-    for (int w = 0; w < kPfWaves; ++w) ls = fmaf(s_ml[w][g][l16].y, fast_exp2(s_ml[w][g][l16].x - mn), ls);
-    const float f = fast_exp2(m[g] - mn);
-    m[g] = mn;
-    l[g] = ls;
-#pragma unroll
-    for (int c = 0; c < 8; ++c)
-#pragma unroll
-      for (int i = 0; i < 4; ++i) o[g][c][i] *= f;
-  }
-#pragma unroll
-  for (int n = kPfWaves / 2; n >= 1; n /= 2) {
-    if (wave >= n && wave < 2 * n) {
-#pragma unroll
-      for (int g = 0; g < QG; ++g)
-#pragma unroll
-        for (int c = 0; c < 8; ++c)
-#pragma unroll
-          for (int i = 0; i < 4; ++i) s_o[wave - n][g][4 * c + i][lane] = o[g][c][i];
-    }
-    __syncthreads();
-    if (wave < n) {
-#pragma unroll
-      for (int g = 0; g < QG; ++g)
-#pragma unroll
-        for (int c = 0; c < 8; ++c)
-#pragma unroll
-          for (int i = 0; i < 4; ++i) o[g][c][i] += s_o[wave][g][4 * c + i][lane];
-    }
-    __syncthreads();
-  }
-  if (wave != 0) return;
-  // o[4 c + t][i] is column 64 c + 4 (4 c4 + i) + t of query l16
-#pragma unroll
-  for (int g = 0; g < QG; ++g) {
-    const int r = q0 + 16 * g + l16;
-    if (r >= M) continue;
-    float* pr = a.partial + (prefix_head(r, h, G, Hq) * a.splits + split) * kPartStride;
-#pragma unroll
-    for (int c = 0; c < 2; ++c)
-#pragma unroll
-      for (int i = 0; i < 4; ++i)
-        *reinterpret_cast<float4*>(pr + 64 * c + 16 * c4 + 4 * i) =
-            make_float4(o[g][4 * c][i], o[g][4 * c + 1][i], o[g][4 * c + 2][i], o[g][4 * c + 3][i]);
-    if (c4 == 0) *reinterpret_cast<float2*>(pr + kD) = make_float2(m[g], l[g]);
-  }
+  const int q0 = block.tile * (QG * 16), r0 = block.split * a.run, r1 = min(a.rows, r0 + a.run);
+  attend_f32<QG, kPfWaves, false>(
+      *reinterpret_cast<AttendF32Smem<QG, kPfWaves>*>(smem), static_cast<const float*>(a.k) + (size_t)block.h * a.cap * kD,
+      static_cast<const float*>(a.v) + (size_t)block.h * a.cap * kD, r0, r1,
+      [&](int i) { return qv + prefix_head(min(q0 + i, a.M - 1), block.h, a.G, a.Hq) * kD; },
+      [&](int i) { return q0 + i < a.M ? a.partial + (prefix_head(q0 + i, block.h, a.G, a.Hq) * a.splits + block.split) * kPartStride : nullptr; },
+      NoLogits{});
 }
 
 // ---- bf16: matrix cores on tiles that the block's waves share ------------------------------------------------------
@@ -476,7 +306,7 @@ __global__ __launch_bounds__(64 * WAVES, KIND == -1 ? 3 : 2) void shared_kernel(
   const RunAt at = find_run(oa.rg, oa.B, oa.S_max, d.run, x);
   if (at.b >= oa.B) return;  // uniform for the block
   const int form_now = oa.rg.loads.form == kByLengths ? form_of(oa.rg.loads, {d.total, 0.f}) : oa.rg.loads.form;
-  auto& s_merge = *reinterpret_cast<MergeSmem<WAVES, NH>*>(smem);
+  auto& s_merge = *reinterpret_cast<PartsSmem<T, NH, WAVES>*>(smem);
   with_form<kPastCaches>(form_now, [&](auto form) __attribute__((always_inline)) {
     parts_body<T, NH, false, decltype(form)::value != kThroughCaches, WAVES>(s_merge, nullptr, at, d.run, h, x, X, oa.k, oa.v, q, oa.partial,
                                                                              nullptr, 0, oa.Hkv, oa.S_cap);
@@ -548,11 +378,11 @@ int shared_own_splits(const Shape& s) {
 template <typename T, int NH, int WAVES, int KIND>
 static hipError_t launch_shared_k(const Shape& s, const void* q, const PrefixArgs& pa, const OwnArgs& oa, hipStream_t st) {
   static std::atomic<unsigned long long> raised{0};
-  int bytes = (int)sizeof(MergeSmem<WAVES, NH>);
+  int bytes = (int)sizeof(PartsSmem<T, NH, WAVES>);
   if constexpr (T::EPC == 8)
     bytes = max(bytes, pf_lds_bytes<WAVES, KIND>());
   else
-    bytes = max(bytes, (int)sizeof(PrefixF32Smem<-KIND>));
+    bytes = max(bytes, (int)sizeof(AttendF32Smem<-KIND, kPfWaves>));
   const hipError_t e = allow_dynamic_lds(reinterpret_cast<const void*>(&shared_kernel<T, NH, WAVES, KIND>), bytes, raised);
   if (e != hipSuccess) return e;
   const int blocks = pa.splits * pa.tiles * s.Hkv + oa.nsplit * s.B * s.Hkv;

@@ -20,8 +20,8 @@ __global__ __launch_bounds__(kPtThreads) void parts_kernel(const void* __restric
                                                            const void* __restrict__ qv, float* __restrict__ partial,
                                                            float* __restrict__ logits, size_t pitch, int B, int Hkv, int S_cap,
                                                            int S_max, int nsplit, Ragged rg) {
-  __shared__ __align__(16) MergeSmem<kPtWaves, NH> s_merge;
-  __shared__ __align__(16) float s_kept[LOGITS && parts_mfma<T, NH>() ? kPtWaves * kept_steps<NH>() * NH * kAmRows : 1];
+  __shared__ __align__(16) PartsSmem<T, NH, kPtWaves> s_merge;
+  __shared__ __align__(16) float s_kept[LOGITS && T::EPC == 8 && parts_mfma<T, NH>() ? kPtWaves * kept_steps<NH>() * NH * kAmRows : 1];
   const Dealt d = deal_runs(rg, B, S_max, nsplit);
   const RunAt at = find_run(rg, B, S_max, d.run, blockIdx.x);
   if (at.b >= B) return;  // uniform for the block; the merge knows how many runs there are
@@ -151,15 +151,19 @@ __global__ __launch_bounds__(kMgThreads) void weigh_merge_kernel(const float* __
   }
 }
 
-// Runs of a sequence: about four blocks per CU in bf16, eight in fp32, of at least 64 rows or 128.  us with 2, 4, 6, 8 and 12
-// per CU: 16 sequences of 32/8 bf16 heads up to 16384 rows 162, 144, 147, 145, 148; 5 of 24 fp32 heads up to 2311 rows
-// 43.5, 41.2, 38.4, 38.3, 38.8.
+// Runs of a sequence, at most as many as leave each wave two steps (bf16: 128 rows on the matrix cores) or 64 rows.
+// Matrix cores: two blocks per CU, as many as are resident, where a sequence then has eight runs and more (of the runs one per
+// sequence stays part empty); else four, whose smaller runs even out lengths better.  us with 1, 2, 3, 4 per CU, bf16: one sequence of
+// 32/4 heads, 32768 rows 19.8, 20.4, 25.5, 26.2, 4 of 32/8 with 8192 29.0, 28.8, 32.5, 30.3; with 2, 4, 6, 8: 16 of 32/8 up to 16384
+// 162, 144, 147, 145.  fp32, with 2 and 8: one of 32/4, 16384 rows 20.5, 25.6, 4 of 64/8 up to 2000 17.9, 22.2; with 2, 4 and 8: 16 of 32/8
+// with 4096 114, 116, 120.
+// Vector units: four per CU in bf16, eight in fp32 (5 sequences of 24 fp32 heads up to 2311 rows with 2, 4, 6, 8 and 12 per CU
+// 43.5, 41.2, 38.4, 38.3, 38.8; one of 24 bf16 heads, 8192 rows, with 2, 3, 4 25.9, 23.1, 24.6).
 int weigh_splits(const Shape& s) {
-  const int units = s.B * s.Hkv;
-  int n = ((s.dtype == 1 ? 4 : 8) * device_cus() + units - 1) / units;
-  const int rows = s.dtype == 1 && s.G >= 4 ? 128 : 64;  // a step of the matrix cores for every wave
-  const int most = (s.S + rows - 1) / rows;
-  if (n > most) n = most;
+  const int units = s.B * s.Hkv, slots = 2 * device_cus();
+  const bool mfma = s.G >= 4;
+  const int blocks = !mfma ? (s.dtype == 1 ? 2 : 4) * slots : slots >= 8 * units ? slots : 2 * slots;
+  const int rows = mfma && s.dtype == 1 ? 128 : 64, n = min((blocks + units - 1) / units, (s.S + rows - 1) / rows);
   return n < 1 ? 1 : n;
 }
 
