@@ -300,7 +300,7 @@ int dense_decode_step(const loki_layout* layout, const void* q, const void* k_fu
  *             least 0; two tokens' or heads' outputs must not overlap).  out may be in with the same strides, else the two
  *             must not overlap.  q_out as the decode calls take it is [B, Hq, D], k_new of
  *             loki_rotate_keys [B, Hkv, n_new, D], k_new of loki_decode_step [B, m, Hkv, D].
- *   positions device int32 [B, n_new]
+ *   positions device int32 [B, n_new]; B n_new <= 2^24
  *   rows      device int32 [B, n_new] or NULL.  When given, token j's key and value go to row
  *             rows[b, j] in place of j along out_token, straight into a cache [B, Hkv, n_rows, D]; a row outside
  *             [0, n_rows) is not written (padded tokens).  Two tokens of a sequence must not share a row.
@@ -378,7 +378,7 @@ int dense_decode_weights(const loki_layout* layout, const void* q, const void* k
  *   page_table .. as in loki_step_args: klo, khi, v are paged pools (out caches are never; weights neither). A
  *              page belongs to one sequence when in place.
  *   workspace  >= loki_evict_workspace_bytes(layout, S_max, budget), 256-byte aligned
- * 0 <= sinks, 0 <= recent, 1 <= budget, sinks + recent <= budget.
+ * 0 <= sinks, 0 <= recent, 1 <= budget <= 2^30, sinks + recent <= budget.
  */
 typedef struct {
   const int32_t* seq_lens;
@@ -407,7 +407,7 @@ int loki_evict(const loki_layout* layout, const loki_evict_args* args, int S_max
  * dense_decode_step for sequences that all begin with the same prefix_rows rows (a system prompt, a document),
  * held once: sequence b attends over the prefix and its own first seq_lens[b] rows,
  *     out = softmax(q [K_prefix; K_b]^T / sqrt(D)) [V_prefix; V_b].
- *   k_prefix, v_prefix  [Hkv, prefix_cap, D]; 0 <= prefix_rows <= prefix_cap, NULL allowed for 0 rows
+ *   k_prefix, v_prefix  [Hkv, prefix_cap, D]; 0 <= prefix_rows <= min(prefix_cap, 2^30), NULL allowed for 0 rows
  *   k_full, v           [B, Hkv, S_cap, D], the sequences' own rows; NULL allowed for S_max = 0
  *   S_max, seq_lens     0 <= S_max <= S_cap; device int32 [B], 0 <= seq_lens[b] <= S_max (clamped); NULL: S_max.
  *                       A sequence with no row at all gives zeros.

@@ -699,7 +699,7 @@ int loki_rotary(const loki_layout* layout, int n_new, const loki_rotary_args* ar
   L.d_split = 128;  // not used
   int rc = check_layout(&L, &s);
   if (rc != LOKI_OK) return rc;
-  if (n_new < 1 || (long long)n_new * s.B > (1 << 30)) return LOKI_ERR_INVALID_ARG;
+  if (n_new < 1 || (long long)n_new * s.B > (1 << 24)) return LOKI_ERR_INVALID_ARG;  // (a grid's threads are counted in 32 bits)
   if (!args->positions || !args->frequencies) return LOKI_ERR_INVALID_ARG;
   if (args->rotary_dims < 2 || args->rotary_dims > 128 || args->rotary_dims % 2 != 0) return LOKI_ERR_INVALID_ARG;
   if (!args->q.in && !args->k.in && !args->v.in) return LOKI_ERR_INVALID_ARG;
@@ -772,6 +772,8 @@ static int check_dense_layout(const loki_layout* layout, Shape* s) {
   return check_layout(&L, s);
 }
 
+constexpr int kMostRows = 1 << 30;  // of a budget or a prefix: row numbers with a step added stay within 32 bits
+
 struct PartsPlan {
   float *partial, *prefix, *logits;
   size_t total;
@@ -839,7 +841,7 @@ int loki_evict_workspace_bytes(const loki_layout* layout, int S_max, int budget,
   Shape s;
   const int rc = check_layout(layout, &s);
   if (rc != LOKI_OK) return rc;
-  if (!bytes || S_max < 1 || S_max > s.S_cap || budget < 1) return LOKI_ERR_INVALID_ARG;
+  if (!bytes || S_max < 1 || S_max > s.S_cap || budget < 1 || budget > kMostRows) return LOKI_ERR_INVALID_ARG;
   *bytes = evict_list_bytes(s, budget) + align_up((size_t)s.B * s.Hkv * sizeof(int32_t), 256);
   return LOKI_OK;
 }
@@ -911,7 +913,7 @@ int dense_shared_workspace_bytes(const loki_layout* layout, int prefix_rows, int
   Shape s;
   const int rc = check_dense_layout(layout, &s);
   if (rc != LOKI_OK) return rc;
-  if (!bytes || prefix_rows < 0 || S_max < 0 || S_max > s.S_cap) return LOKI_ERR_INVALID_ARG;
+  if (!bytes || prefix_rows < 0 || prefix_rows > kMostRows || S_max < 0 || S_max > s.S_cap) return LOKI_ERR_INVALID_ARG;
   s.S = S_max;
   *bytes = plan_parts(s, shared_own_splits(s), prefix_splits(s, prefix_rows), false, nullptr).total;
   return LOKI_OK;
@@ -924,7 +926,7 @@ int dense_decode_shared(const loki_layout* layout, const void* q, const void* k_
   const int rc = check_dense_layout(layout, &s);
   if (rc != LOKI_OK) return rc;
   if (!q || !out || !workspace) return LOKI_ERR_INVALID_ARG;
-  if (prefix_rows < 0 || prefix_rows > prefix_cap || S_max < 0 || S_max > s.S_cap) return LOKI_ERR_INVALID_ARG;
+  if (prefix_rows < 0 || prefix_rows > prefix_cap || prefix_rows > kMostRows || S_max < 0 || S_max > s.S_cap) return LOKI_ERR_INVALID_ARG;
   if ((prefix_rows > 0 && (!k_prefix || !v_prefix)) || (S_max > 0 && (!k_full || !v))) return LOKI_ERR_INVALID_ARG;
   if (!aligned16(q) || !aligned16(k_prefix) || !aligned16(v_prefix) || !aligned16(k_full) || !aligned16(v) || !aligned16(out))
     return LOKI_ERR_ALIGNMENT;

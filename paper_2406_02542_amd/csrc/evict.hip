@@ -4,9 +4,9 @@
 //
 // Two launches.  (1) evict_select_kernel, one block per unit: the totals as order-preserving integers in
 // registers, the smallest one kept found by three radix passes over LDS histograms, the list written in
-// ascending order.  Latency bounds it: a pass is a few barriers.  (2) evict_move_kernel: the listed rows to
-// their new places, bound by memory; a row is read once and written once.  In place row j comes from list[j]
-// >= j: a block owns a slice of the unit's columns, walks the list upwards and writes a run of rows only when
+// ascending order.  Latency bounds it: a pass is a few barriers.  (2) evict_copy_kernel or evict_compact_kernel: the
+// listed rows to their new places, bound by memory; a row is read once and written once.  In place row j comes from
+// list[j] >= j: a block owns a slice of the unit's columns, walks the list upwards and writes a run of rows only when
 // all of its sources have been read; the sources of later runs lie behind it.
 #include "common.h"
 

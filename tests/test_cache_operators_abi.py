@@ -211,6 +211,18 @@ def test_shared_refusals():
     assert L.dense_shared_workspace_bytes(by(lay), 0, 513, by(n)) == 1
 
 
+def test_sizes_past_what_the_kernels_count_are_refused():
+    L, lay, n = api.lib(), _layout(), ctypes.c_size_t()
+    most, ev = 1 << 30, api.EvictArgs(weights=P, klo=P, khi=P, v=P)
+    assert L.loki_rotary(by(lay), (1 << 23) + 1, by(_rotary_args()), None) == 1  # two sequences
+    assert L.loki_evict_workspace_bytes(by(lay), 512, most, by(n)) == 0 and n.value == 4 * most * 4 + 256
+    assert L.loki_evict_workspace_bytes(by(lay), 512, most + 1, by(n)) == 1
+    assert L.loki_evict(by(lay), by(ev), 512, most + 1, 0, 0, P, BIG, None) == 1
+    assert L.dense_shared_workspace_bytes(by(lay), most, 512, by(n)) == 0
+    assert L.dense_shared_workspace_bytes(by(lay), most + 1, 512, by(n)) == 1
+    assert L.dense_decode_shared(by(lay), P, P, P, most + 1, most + 1, P, P, 512, None, P, BIG, P, None) == 1
+
+
 @pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
 def test_workspace_of_the_longest_length_serves_shorter_ones(dtype):
     for B, Hq, Hkv in ((1, 8, 8), (6, 32, 8), (16, 64, 8), (48, 32, 32)):
