@@ -13,7 +13,8 @@ def attend64(q, k, v, weight_step=2.0 ** -16):
 
     A logit is a sum of D products: in any order its rounding is at most D 2^-24 of the sum of their magnitudes, and two
     roundings of the scale; a weight 2^x moves by that much relative to itself, numerator and denominator, and by the
-    exponential's own 2^-22 each, and the denominator by a sum of n terms, of which no chain is longer than n / 8 + 64.  An
+    exponential's own 2^-22 each, and the denominator by a sum of n terms, of which no chain is longer than n / 4 + 64: the
+    four waves of a block have different keys, or (where they have different queries) each adds two at a time for a lane and its partner.  An
     output is a sum of n products of such weights, relative to the sum of the products' magnitudes.  weight_step: what
     the weights are off as a matrix product takes them: 2^-16 in two bf16 terms of 8 bits each, 2 2^-8 in one (half a
     step, 2^-8, of every weight in the numerator, and as much in the denominator, which adds up the rounded ones)."""
@@ -25,7 +26,7 @@ def attend64(q, k, v, weight_step=2.0 ** -16):
     a = q @ k.t().contiguous() / math.sqrt(D)
     p = torch.softmax(a, dim=-1)
     size = float((q.abs() @ k.abs().t().contiguous()).max()) / math.sqrt(D)
-    chain = (n / 8 + 64) * 2.0 ** -24
+    chain = (n / 4 + 64) * 2.0 ** -24
     rel = 2 * ((D + 2) * 2.0 ** -24 * size + 2.0 ** -22) + chain
     return p @ v, p, (p @ v.abs()) * (rel + chain + weight_step), rel
 

@@ -74,6 +74,13 @@ def test_large_batches_and_long_sequences(Hq, Hkv, B, S):
     check(B, Hq, Hkv, S, S, lens, "bf16")
 
 
+@pytest.mark.parametrize("Hq,Hkv,B,S", [(32, 8, 16, 3500), (64, 8, 70, 600), (4, 1, 1, 60000), (8, 1, 1030, 90), (16, 4, 300, 77)])
+def test_large_fp32_batches_of_groups(Hq, Hkv, B, S):
+    """Rows through and past the caches, one run and many of a sequence, more units than blocks are resident."""
+    lens = [max(0, S - (b * 977) % (S + 1)) for b in range(B)]
+    check(B, Hq, Hkv, S, S, lens, "f32")
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 def test_peaked_attention(dtype):
     """Logits of hundreds: one row takes all, the others' weights vanish without a NaN."""
