@@ -152,17 +152,17 @@ __global__ __launch_bounds__(kMgThreads) void weigh_merge_kernel(const float* __
 }
 
 // Runs of a sequence, at most as many as leave each wave two steps (bf16: 128 rows on the matrix cores) or 64 rows.
-// Matrix cores: two blocks per CU, as many as are resident, where a sequence then has eight runs and more (of the runs one per
-// sequence stays part empty); else four, whose smaller runs even out lengths better.  us with 1, 2, 3, 4 per CU, bf16: one sequence of
-// 32/4 heads, 32768 rows 19.8, 20.4, 25.5, 26.2, 4 of 32/8 with 8192 29.0, 28.8, 32.5, 30.3; with 2, 4, 6, 8: 16 of 32/8 up to 16384
-// 162, 144, 147, 145.  fp32, with 2 and 8: one of 32/4, 16384 rows 20.5, 25.6, 4 of 64/8 up to 2000 17.9, 22.2; with 2, 4 and 8: 16 of 32/8
-// with 4096 114, 116, 120.
+// Matrix cores: two blocks per CU, as many as are resident, where a sequence then has four runs and more, else four, which even
+// out lengths better.  us with 1, 2, 3, 4 per CU: one of 32/4 bf16 heads, 32768 rows 19.8, 20.4, 25.5, 26.2; with 2, 4, 8: 20 of 32/4 up to
+// 5000 31.5, 34.5, -, 16 of 32/8 up to 16384 146, 144, 145, 50 of 32/8 up to 2500 83.3, 76.5, -, 48 of 64/8 up to 300 25.5, 24.2, 24.2, 64
+// of 64/8 up to 1024 50.3, 51.4, 54.5 (but all of 600 40.5, 44.7, 54.1); fp32: 16 of 32/8, 4096 rows 114, 116, 120, 32 of 64/8 up to 2000
+// 87.4, 86.3, 85.0.
 // Vector units: four per CU in bf16, eight in fp32 (5 sequences of 24 fp32 heads up to 2311 rows with 2, 4, 6, 8 and 12 per CU
 // 43.5, 41.2, 38.4, 38.3, 38.8; one of 24 bf16 heads, 8192 rows, with 2, 3, 4 25.9, 23.1, 24.6).
 int weigh_splits(const Shape& s) {
   const int units = s.B * s.Hkv, slots = 2 * device_cus();
   const bool mfma = s.G >= 4;
-  const int blocks = !mfma ? (s.dtype == 1 ? 2 : 4) * slots : slots >= 8 * units ? slots : 2 * slots;
+  const int blocks = !mfma ? (s.dtype == 1 ? 2 : 4) * slots : slots >= 4 * units ? slots : 2 * slots;
   const int rows = mfma && s.dtype == 1 ? 128 : 64, n = min((blocks + units - 1) / units, (s.S + rows - 1) / rows);
   return n < 1 ? 1 : n;
 }
