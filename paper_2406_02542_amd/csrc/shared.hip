@@ -60,6 +60,9 @@ __device__ __forceinline__ void prefix_f32_body(char* smem, const PrefixAt& bloc
 // maximum nor an exchange between lanes is needed in the other steps.
 // Measured: 64 sequences of 64/8 heads behind P rows, 18 us + 1.9 us per 1024 rows (1.1 PFLOP/s; a large product reaches 1.2
 // on this card): the constant part is a launch, the queries, and 528 bytes per query row and run written.
+// Of the 46 us of 24576 such rows the products alone, on operands that do not change, take 20, with the LDS reads 38, with the
+// exponentials but no reads 42.  Halves of the waves a phase apart by barriers, one in products while the other is in exponentials,
+// take 48; priorities for one half or for the products change 1 %.
 typedef float pf_f32x16_t __attribute__((ext_vector_type(16)));
 typedef short pf_s16x4_t __attribute__((ext_vector_type(4)));
 typedef __attribute__((address_space(3))) pf_s16x4_t pf_lds_s16x4_t;
