@@ -304,14 +304,14 @@ __global__ __launch_bounds__(64 * WAVES, KIND == -1 ? 3 : 2) void shared_kernel(
       prefix_f32_body<-KIND>(smem, block, static_cast<const float*>(q), pa);
     return;
   }
-  const int X = oa.nsplit * oa.B, id = (int)blockIdx.x - prefix_blocks, h = id / X, x = id - h * X;
+  const int X = oa.nsplit * oa.B, id = (int)blockIdx.x - prefix_blocks, x = id / oa.Hkv, h = id - x * oa.Hkv;
   const Dealt d = deal_runs(oa.rg, oa.B, oa.S_max, oa.nsplit);
   const RunAt at = find_run(oa.rg, oa.B, oa.S_max, d.run, x);
   if (at.b >= oa.B) return;  // uniform for the block
   const int form_now = oa.rg.loads.form == kByLengths ? form_of(oa.rg.loads, {d.total, 0.f}) : oa.rg.loads.form;
   auto& s_merge = *reinterpret_cast<PartsSmem<T, NH, WAVES>*>(smem);
   with_form<kPastCaches>(form_now, [&](auto form) __attribute__((always_inline)) {
-    parts_body<T, NH, false, decltype(form)::value != kThroughCaches, WAVES>(s_merge, nullptr, at, d.run, h, x, X, oa.k, oa.v, q, oa.partial,
+    parts_body<T, NH, false, decltype(form)::value != kThroughCaches, WAVES>(s_merge, nullptr, at, d.run, h, X, oa.k, oa.v, q, oa.partial,
                                                                              nullptr, 0, oa.Hkv, oa.S_cap);
   });
 }

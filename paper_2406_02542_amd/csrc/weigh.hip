@@ -23,11 +23,12 @@ __global__ __launch_bounds__(kPtThreads) void parts_kernel(const void* __restric
   __shared__ __align__(16) PartsSmem<T, NH, kPtWaves> s_merge;
   __shared__ __align__(16) float s_kept[LOGITS && T::EPC == 8 && parts_mfma<T, NH>() ? kPtWaves * kept_steps<NH>() * NH * kAmRows : 1];
   const Dealt d = deal_runs(rg, B, S_max, nsplit);
-  const RunAt at = find_run(rg, B, S_max, d.run, blockIdx.x);
+  const int x = blockIdx.x / Hkv, h = blockIdx.x - x * Hkv;  // (a run's heads next to each other: whole runs of all heads first)
+  const RunAt at = find_run(rg, B, S_max, d.run, x);
   if (at.b >= B) return;  // uniform for the block; the merge knows how many runs there are
   const int form_now = rg.loads.form == kByLengths ? form_of(rg.loads, {d.total, 0.f}) : rg.loads.form;
   with_form<kPastCaches>(form_now, [&](auto form) __attribute__((always_inline)) {
-    parts_body<T, NH, LOGITS, decltype(form)::value != kThroughCaches, kPtWaves>(s_merge, s_kept, at, d.run, blockIdx.y, blockIdx.x, gridDim.x,
+    parts_body<T, NH, LOGITS, decltype(form)::value != kThroughCaches, kPtWaves>(s_merge, s_kept, at, d.run, h, nsplit * B,
                                                                                k, v, qv, partial, logits, pitch, Hkv, S_cap);
   });
 }
@@ -152,17 +153,16 @@ __global__ __launch_bounds__(kMgThreads) void weigh_merge_kernel(const float* __
 }
 
 // Runs of a sequence, at most as many as leave each wave two steps (bf16: 128 rows on the matrix cores) or 64 rows.
-// Matrix cores: two blocks per CU, as many as are resident, where a sequence then has four runs and more, else four, which even
-// out lengths better.  us with 1, 2, 3, 4 per CU: one of 32/4 bf16 heads, 32768 rows 19.8, 20.4, 25.5, 26.2; with 2, 4, 8: 20 of 32/4 up to
-// 5000 31.5, 34.5, -, 16 of 32/8 up to 16384 146, 144, 145, 50 of 32/8 up to 2500 83.3, 76.5, -, 48 of 64/8 up to 300 25.5, 24.2, 24.2, 64
-// of 64/8 up to 1024 50.3, 51.4, 54.5 (but all of 600 40.5, 44.7, 54.1); fp32: 16 of 32/8, 4096 rows 114, 116, 120, 32 of 64/8 up to 2000
-// 87.4, 86.3, 85.0.
+// Matrix cores: two blocks per CU, as many as are resident, where a sequence then has six runs and more, else four, which even
+// out lengths better.  us with 2, 4, 8 per CU, bf16: one of 32/8 heads, 20000 rows 20.9, 25.0, 26.7, 10 of 32/4 up to 9000 28.9, 32.0, 40.1,
+// 20 of 32/4 up to 5000 31.5, 34.5, 42.4, 16 of 32/8 up to 16384 149, 141, 142, 24 up to 7000 94.0, 90.7, 93.6, 50 up to 2500 80.5, 74.0, 75.9
+// (but 64 of 64/8, all of 600 40.5, 44.5, 53.2); fp32: 13 of 32/8 up to 3000 48.7, 48.0, 50.5.
 // Vector units: four per CU in bf16, eight in fp32 (5 sequences of 24 fp32 heads up to 2311 rows with 2, 4, 6, 8 and 12 per CU
 // 43.5, 41.2, 38.4, 38.3, 38.8; one of 24 bf16 heads, 8192 rows, with 2, 3, 4 25.9, 23.1, 24.6).
 int weigh_splits(const Shape& s) {
   const int units = s.B * s.Hkv, slots = 2 * device_cus();
   const bool mfma = s.G >= 4;
-  const int blocks = !mfma ? (s.dtype == 1 ? 2 : 4) * slots : slots >= 4 * units ? slots : 2 * slots;
+  const int blocks = !mfma ? (s.dtype == 1 ? 2 : 4) * slots : slots >= 6 * units ? slots : 2 * slots;
   const int rows = mfma && s.dtype == 1 ? 128 : 64, n = min((blocks + units - 1) / units, (s.S + rows - 1) / rows);
   return n < 1 ? 1 : n;
 }
@@ -171,7 +171,7 @@ size_t weigh_logits_pitch(int S_max) { return ((size_t)S_max + 31) / 32 * 32; }
 
 hipError_t launch_parts(const Shape& s, int nsplit, const void* q, const void* k, const void* v, float* partial, float* logits,
                         hipStream_t st) {
-  const dim3 grid(nsplit * s.B, s.Hkv), block(kPtThreads);
+  const dim3 grid(nsplit * s.B * s.Hkv), block(kPtThreads);
   const Ragged rg = with_loads(s, kEveryRow);
 #define LOKI_PARTS(T, NH)                                                                                               \
   if (logits != nullptr)                                                                                                \
