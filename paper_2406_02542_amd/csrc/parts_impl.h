@@ -131,7 +131,7 @@ struct StoreSteps {
 };
 // bf16 on the matrix cores: a wave keeps those of some steps in LDS and stores them together, whole lines: memory operations are
 // waited for in their order, so a store of every step is waited for with the next rows.  16 sequences of 32/8 heads up to
-// 16384 rows: the launch 142 us with a store in every step, 136, 130 and 131 for runs of 4, 16 and 32 steps; 118 with the stores left out.
+// 16384 rows: the launch 136, 134, 130 and 130 us for runs of 2, 4, 16 and 32 steps; 118 with the stores left out.
 template <int NH>
 constexpr int kept_steps() {
   return 64 / NH;
