@@ -103,7 +103,7 @@ struct KeepIn {  // (handed over by value: the rows' loop is compiled for caller
   __device__ __forceinline__ void step(int b0) const { keep->step(b0); }
 };
 
-template <typename T, int NH>
+template <int NH>
 constexpr bool parts_mfma() {  // four heads and more: matrix cores (fp32, with the merge: 16 sequences of 64/8 heads with 4096 rows
   return NH >= 4;              // 181 us on the vector units, 113 so, of 32/8 113, 107; one of 32/4 with 16384 rows 37, 21)
 }
@@ -356,7 +356,7 @@ __device__ __forceinline__ void attend_f32(AttendF32Smem<QG, WAVES>& sm, const f
 
 // What a run's waves are joined through.
 template <typename T, int NH, int WAVES>
-using PartsSmem = std::conditional_t<T::EPC == 4 && parts_mfma<T, NH>(), AttendF32Smem<1, WAVES>, MergeSmem<WAVES, NH>>;
+using PartsSmem = std::conditional_t<T::EPC == 4 && parts_mfma<NH>(), AttendF32Smem<1, WAVES>, MergeSmem<WAVES, NH>>;
 
 // One run by a block of WAVES waves: part at.place of the X that each query head of KV head h has.
 template <typename T, int NH, bool LOGITS, bool STREAM, int WAVES>
@@ -364,7 +364,7 @@ __device__ __forceinline__ void parts_body(PartsSmem<T, NH, WAVES>& s_merge, flo
                                            const void* __restrict__ k, const void* __restrict__ v, const void* __restrict__ qv,
                                            float* __restrict__ partial, float* __restrict__ logits, size_t pitch, int Hkv, int S_cap) {
   using ST = typename T::store_t;
-  constexpr bool MFMA = parts_mfma<T, NH>();
+  constexpr bool MFMA = parts_mfma<NH>();
   const int tid = threadIdx.x, unit = at.b * Hkv + h;
   const int r0 = at.i * run, r1 = min(at.len, r0 + run);
   const size_t head0 = (size_t)unit * NH;

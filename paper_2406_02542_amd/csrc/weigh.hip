@@ -21,7 +21,7 @@ __global__ __launch_bounds__(kPtThreads) void parts_kernel(const void* __restric
                                                            float* __restrict__ logits, size_t pitch, int B, int Hkv, int S_cap,
                                                            int S_max, int nsplit, Ragged rg) {
   __shared__ __align__(16) PartsSmem<T, NH, kPtWaves> s_merge;
-  __shared__ __align__(16) float s_kept[LOGITS && T::EPC == 8 && parts_mfma<T, NH>() ? kPtWaves * kept_steps<NH>() * NH * kAmRows : 1];
+  __shared__ __align__(16) float s_kept[LOGITS && T::EPC == 8 && parts_mfma<NH>() ? kPtWaves * kept_steps<NH>() * NH * kAmRows : 1];
   const Dealt d = deal_runs(rg, B, S_max, nsplit);
   const int x = blockIdx.x / Hkv, h = blockIdx.x - x * Hkv;  // (a run's heads next to each other: whole runs of all heads first)
   const RunAt at = find_run(rg, B, S_max, d.run, x);
