@@ -95,7 +95,8 @@ enum { LOKI_PATH_SPLIT = 0x100, LOKI_PATH_FUSED = 0x200, LOKI_PATH_CLUSTER = 0x3
 /* Optional bit OR-ed into select_mode: the caller vouches that the workspace was filled with
  * zeros after it was allocated and that nothing but calls of this library (any shapes) has
  * written to it since.  LOKI_PATH_CLUSTER keeps a few control words at the start of the
- * workspace that must be zero when a launch starts; every finished launch leaves them zero, so
+ * workspace that must be zero when a launch starts; every finished launch leaves them zero and every
+ * other call that takes a workspace leaves them alone, so
  * with this bit the clearing kernel in front of the launch (about 5 us) is left out.  Without the
  * bit the workspace needs no initialisation at all.  A launch whose blocks gave up waiting
  * (NaN outputs) leaves a mark there: with the bit, later LOKI_PATH_CLUSTER launches on that

@@ -204,10 +204,11 @@ Workspace plan_workspace(const Shape& s, int select_mode, int nsplit, void* base
     off += align_up(bytes, 256);
     return r;
   };
+  // at offset 0 for every shape, and left alone by the calls that launch no cluster: a workspace may serve all of them in turn
+  if (select_mode != -1 || nsplit > 1) w.cluster_ctl = reinterpret_cast<uint32_t*>(take(kClusterCtlBytes));
   if (select_mode == -2) w.qhat = reinterpret_cast<float*>(take(heads_q * kD * sizeof(float)));
   if (select_mode >= 0) {
     const size_t heads_sel = (select_mode == 1) ? (size_t)s.B * s.Hkv : heads_q;
-    w.cluster_ctl = reinterpret_cast<uint32_t*>(take(kClusterCtlBytes));  // at offset 0 for every shape
     w.qhat = reinterpret_cast<float*>(take(heads_q * kD * sizeof(float)));
     w.scores = reinterpret_cast<float*>(take(heads_sel * s.S * sizeof(float)));
     w.sel_idx = reinterpret_cast<int32_t*>(take(heads_sel * s.k * sizeof(int32_t)));
@@ -778,19 +779,20 @@ struct PartsPlan {
   float *partial, *prefix, *logits;
   size_t total;
 };
-// Parts of every head's result, nsplit of its sequence and `shared` of the prefix, and for the weights every row's logits.
+// Behind the control words, which these calls leave alone (plan_workspace): parts of every head's result, nsplit of its sequence and
+// `shared` of the prefix, and for the weights every row's logits.
 static PartsPlan plan_parts(const Shape& s, int nsplit, int shared, bool weights, void* base) {
   PartsPlan w{};
   const size_t heads = (size_t)s.B * s.Hq;
   const size_t own = align_up(heads * nsplit * kPartStride * sizeof(float), 256);
   const size_t prefix = align_up(heads * shared * kPartStride * sizeof(float), 256);
-  char* p = static_cast<char*>(base);
-  if (p) {
+  if (base) {
+    char* p = static_cast<char*>(base) + kClusterCtlBytes;
     w.partial = reinterpret_cast<float*>(p);
     w.prefix = reinterpret_cast<float*>(p + own);
     w.logits = weights ? reinterpret_cast<float*>(p + own + prefix) : nullptr;
   }
-  w.total = own + prefix + (weights ? align_up(heads * weigh_logits_pitch(s.S) * sizeof(float), 256) : 0);
+  w.total = kClusterCtlBytes + own + prefix + (weights ? align_up(heads * weigh_logits_pitch(s.S) * sizeof(float), 256) : 0);
   return w;
 }
 
@@ -835,14 +837,35 @@ int dense_decode_weights(const loki_layout* layout, const void* q, const void* k
   return e == hipSuccess ? LOKI_OK : LOKI_ERR_HIP;
 }
 
-static size_t evict_list_bytes(const Shape& s, int budget) { return align_up((size_t)s.B * s.Hkv * budget * sizeof(int32_t), 256); }
+struct EvictPlan {
+  int32_t *list, *kept;
+  int pitch;  // entries of a unit's list
+  size_t total;
+};
+// Behind the control words, which the call leaves alone (plan_workspace): every unit's list of the rows that go on, at most all there
+// are, unless the caller has one of his own, and their numbers.  (Never less than lists of the whole budget, of which there was no
+// more once: workspaces of that size still serve.)
+static EvictPlan plan_evict(const Shape& s, int S_max, int budget, void* base) {
+  EvictPlan w{};
+  const size_t units = (size_t)s.B * s.Hkv, kept = align_up(units * sizeof(int32_t), 256);
+  w.pitch = budget < S_max ? budget : S_max;
+  const size_t lists = kClusterCtlBytes + units * w.pitch * sizeof(int32_t), whole = units * budget * sizeof(int32_t);
+  const size_t front = align_up(lists > whole ? lists : whole, 256);
+  if (base) {
+    char* p = static_cast<char*>(base);
+    w.list = reinterpret_cast<int32_t*>(p + kClusterCtlBytes);
+    w.kept = reinterpret_cast<int32_t*>(p + front);
+  }
+  w.total = front + kept;
+  return w;
+}
 
 int loki_evict_workspace_bytes(const loki_layout* layout, int S_max, int budget, size_t* bytes) {
   Shape s;
   const int rc = check_layout(layout, &s);
   if (rc != LOKI_OK) return rc;
   if (!bytes || S_max < 1 || S_max > s.S_cap || budget < 1 || budget > kMostRows) return LOKI_ERR_INVALID_ARG;
-  *bytes = evict_list_bytes(s, budget) + align_up((size_t)s.B * s.Hkv * sizeof(int32_t), 256);
+  *bytes = plan_evict(s, S_max, budget, nullptr).total;
   return LOKI_OK;
 }
 
@@ -895,16 +918,17 @@ int loki_evict(const loki_layout* layout, const loki_evict_args* args, int S_max
   a.sinks = sinks;
   a.recent = recent;
   a.nlo = s.d * s.elem_bytes / 16;
-  int32_t* kept = reinterpret_cast<int32_t*>(static_cast<char*>(workspace) + evict_list_bytes(s, budget));
-  int32_t* list = args->out_idx ? args->out_idx : static_cast<int32_t*>(workspace);
+  const EvictPlan w = plan_evict(s, S_max, budget, workspace);
+  int32_t* list = args->out_idx ? args->out_idx : w.list;
+  a.list_pitch = args->out_idx ? budget : w.pitch;
   hipStream_t st = static_cast<hipStream_t>(stream);
   StageTimer tm(st);
   tm.begin("evict_select");
-  hipError_t e = launch_evict_select(s, a, list, kept, st);
+  hipError_t e = launch_evict_select(s, a, list, w.kept, st);
   tm.end();
   if (e != hipSuccess) return LOKI_ERR_HIP;
   tm.begin("evict_move");
-  e = launch_evict_move(s, a, list, kept, st);
+  e = launch_evict_move(s, a, list, w.kept, st);
   tm.end();
   return e == hipSuccess ? LOKI_OK : LOKI_ERR_HIP;
 }
@@ -989,7 +1013,7 @@ int loki_pca_workspace_bytes(const loki_layout* layout, long long n_rows, size_t
   const int rc = check_layout(layout, &s);
   if (rc != LOKI_OK) return rc;
   if (!bytes || n_rows < 2 || n_rows > (1LL << 40)) return LOKI_ERR_INVALID_ARG;
-  *bytes = pca_workspace_bytes(s.Hkv, n_rows);
+  *bytes = kClusterCtlBytes + pca_workspace_bytes(s.Hkv, n_rows);  // (the control words are left alone: plan_workspace)
   return LOKI_OK;
 }
 
@@ -1002,7 +1026,8 @@ int loki_pca_fit(const loki_layout* layout, const void* keys, long long n_rows, 
   if (n_rows < 2 || n_rows > (1LL << 40)) return LOKI_ERR_INVALID_ARG;
   if (!aligned16(keys) || !aligned16(P) || !aligned16(eigenvalues)) return LOKI_ERR_ALIGNMENT;
   if (!aligned256(workspace)) return LOKI_ERR_ALIGNMENT;
-  if (pca_workspace_bytes(s.Hkv, n_rows) > workspace_bytes) return LOKI_ERR_WORKSPACE;
+  if (kClusterCtlBytes + pca_workspace_bytes(s.Hkv, n_rows) > workspace_bytes) return LOKI_ERR_WORKSPACE;
+  workspace = static_cast<char*>(workspace) + kClusterCtlBytes;
   hipStream_t st = static_cast<hipStream_t>(stream);
   StageTimer tm(st);
   static const char* const kStageNames[3] = {"pca_gram", "pca_covariance", "pca_eigensolve"};

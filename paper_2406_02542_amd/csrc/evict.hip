@@ -34,7 +34,7 @@ __device__ __forceinline__ uint32_t before_wave(const uint32_t* s_wave, int wave
 
 // NK: keys per lane held in registers (rows up to 1024 NK); 0: read again in every pass.
 template <int NK>
-__global__ __launch_bounds__(kEvThreads) void evict_select_kernel(EvictArgs a, int32_t* __restrict__ list /* [units, budget] */,
+__global__ __launch_bounds__(kEvThreads) void evict_select_kernel(EvictArgs a, int32_t* __restrict__ list /* [units, list_pitch] */,
                                                                   int32_t* __restrict__ kept_rows /* [units] */) {
   __shared__ uint32_t s_hist[kEvBins];
   __shared__ uint32_t s_wave[2][kEvWaves];
@@ -42,9 +42,9 @@ __global__ __launch_bounds__(kEvThreads) void evict_select_kernel(EvictArgs a, i
   const int unit = blockIdx.x, b = unit / a.Hkv;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int len = evict_rows(a.seq_lens, b, a.S_max), kept = min(len, a.budget);
-  int32_t* out = list + (size_t)unit * a.budget;
+  int32_t* out = list + (size_t)unit * a.list_pitch;
   if (tid == 0) kept_rows[unit] = kept;
-  for (int i = kept + tid; i < a.budget; i += kEvThreads) out[i] = -1;
+  for (int i = kept + tid; i < a.list_pitch; i += kEvThreads) out[i] = -1;
   if (len <= a.budget) {  // (uniform for the block)
     for (int i = tid; i < len; i += kEvThreads) out[i] = i;
     return;
@@ -194,7 +194,7 @@ __global__ __launch_bounds__(kMvThreads) void evict_copy_kernel(EvictArgs a, con
   const int unit = blockIdx.y, b = unit / a.Hkv, h = unit - b * a.Hkv, tid = threadIdx.x;
   const int j0 = blockIdx.x * rows, j1 = min(min(a.budget, a.S_max), j0 + rows);
   if (blockIdx.x == 0 && h == 0 && tid == 0 && a.lens_out != nullptr) a.lens_out[b] = kept_rows[unit];
-  const int32_t* from = list + (size_t)unit * a.budget;
+  const int32_t* from = list + (size_t)unit * a.list_pitch;
   if (from[j0] < 0) return;  // uniform for the block
   const EvictSide src{(char*)a.klo, (char*)a.khi, (char*)a.v, a.S_cap};
   const EvictSide dst{(char*)a.klo_out, (char*)a.khi_out, (char*)a.v_out, a.S_cap_out};
@@ -236,7 +236,7 @@ __global__ __launch_bounds__(kIpThreads) void evict_compact_kernel(EvictArgs a, 
   const int unit = blockIdx.y, b = unit / a.Hkv, h = unit - b * a.Hkv, tid = threadIdx.x;
   const int kept = kept_rows[unit];
   const int slices = chunks / kIpSlice;
-  const int32_t* from = list + (size_t)unit * a.budget;
+  const int32_t* from = list + (size_t)unit * a.list_pitch;
   if ((int)blockIdx.x == slices) {
     if (h == 0 && tid == 0 && a.lens_out != nullptr) a.lens_out[b] = kept;
     float* w = a.weights + (size_t)unit * a.S_cap;

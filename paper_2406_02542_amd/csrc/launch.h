@@ -120,7 +120,7 @@ struct Workspace {
   size_t ticket_words;    // its padded length in words
   uint32_t* sel_scratch;  // long sequences only: chunk histograms, candidates, bookkeeping
   float* partial;    // [B*Hq, nsplit, 130]
-  uint32_t* cluster_ctl;  // first bytes of every Loki workspace (kClusterCtlBytes): the arrival flags and tickets
+  uint32_t* cluster_ctl;  // first bytes of every workspace (kClusterCtlBytes): the arrival flags and tickets
                           // of the several-blocks-per-unit launch, at the same place whatever the shape
   void* cluster;     // exchange area of the several-blocks-per-unit launch (fused_gqa_cluster.hip), or null
   size_t total_bytes;
@@ -262,6 +262,7 @@ struct EvictArgs {
   float* weights_out;
   int32_t* lens_out;
   int Hkv, S_cap, S_cap_out, S_max, budget, sinks, recent, nlo;  // nlo: 16-byte chunks of a row of klo
+  int list_pitch;  // entries of a unit's list: at least min(budget, S_max)
   Paging pg;       // of the source
 };
 hipError_t launch_evict_select(const Shape& s, const EvictArgs& a, int32_t* list, int32_t* kept, hipStream_t st);
