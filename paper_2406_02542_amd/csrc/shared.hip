@@ -52,21 +52,22 @@ __device__ __forceinline__ void prefix_f32_body(char* smem, const PrefixAt& bloc
 // places exchanged by the row's number, so that neither the key rows (stride 256 bytes) nor the four rows of a transposing
 // load meet in a bank (no conflict is counted).  Eight waves of 32 queries keep two on a SIMD, whose products and
 // exponentials overlap: four waves of 64 queries, each with the registers of a SIMD to itself, take 130 us where these take 113.
-// The weights enter the second product as ONE bf16 each: half a step, 2^-8, of each weight, which their sum, that of the
-// rounded weights, shares; over many rows the errors average to the size of the output's own rounding.  In two terms, as where
-// memory bounds an attention, the second product is twice as long (64 sequences of 64/8 heads behind 32768 rows: 97 us, 79 so).
+// The weights enter the second product in two bf16 terms, as in the library's other attention over whole caches, and their sum in 32
+// bits: 2^-17 of each weight.  One term makes that product half as long, but is off by 2^-9 of each weight, which
+// outputs whose large rows cancel do not hide: then whole outputs are wrong by their own size (tests/test_gpu_weight_precision.py).
+// us in one / two terms, without rows of their own: 4 sequences of 32/8 heads behind 65536 rows 52.3 / 52.9, 16 of them 55.8 / 56.6, 32
+// 63.6 / 70.2, 64 of 64/8 behind 4096 29.9 / 33.2, 32768 84.6 / 104.2.
 // The reference of the exponentials follows the running maximum only when a step's weights sum up to more than 2^8: the
 // outputs are rescaled a few times per run instead of in most steps, weights up to 2^8 lose nothing, and neither the
 // maximum nor an exchange between lanes is needed in the other steps.
-// Measured: 64 sequences of 64/8 heads behind P rows, 18 us + 1.9 us per 1024 rows (1.1 PFLOP/s; a large product reaches 1.2
-// on this card): the constant part is a launch, the queries, and 528 bytes per query row and run written.
-// Of the 46 us of 24576 such rows the products alone, on operands that do not change, take 20, with the LDS reads 38, with the
-// exponentials but no reads 42.  Halves of the waves a phase apart by barriers, one in products while the other is in exponentials,
-// take 48; priorities for one half or for the products change 1 %.
+// Measured: 64 sequences of 64/8 heads behind P rows, 14 us + 2.8 us per 1024 rows (0.77 PFLOP/s of the attention, 1.15 of products
+// with the second term; a large product reaches 1.2 on this card): the constant part is a launch, the queries, 528 bytes per query
+// row and run written, and their merge.  In one term, of the 46 us of 24576 such rows, the products alone, on operands that do not
+// change, took 20, with the LDS reads 38, with the exponentials but no reads 42; halves of the waves a phase apart by barriers,
+// one in products while the other is in exponentials, took 48; priorities for one half or for the products changed 1 %.
 typedef float pf_f32x16_t __attribute__((ext_vector_type(16)));
 typedef short pf_s16x4_t __attribute__((ext_vector_type(4)));
 typedef __attribute__((address_space(3))) pf_s16x4_t pf_lds_s16x4_t;
-typedef __bf16 pf_bf16x2_t __attribute__((ext_vector_type(2)));
 
 template <int WAVES, int WQ>
 constexpr int pf_tile_keys() {
@@ -153,15 +154,18 @@ __device__ __forceinline__ void prefix_mfma_body(char* smem /* [2][K tile, V til
       for (int i = 0; i < 16; ++i)
         if (8 * (i >> 2) + 4 * half + (i & 3) >= there) s[i] = kNegBig;
     }
-    uint32_t w[8];
-    float sum;
+    float p[16], sum;
     auto weights = [&]() __attribute__((always_inline)) {
-      sum = 0.f;
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        w[i] = BF16::round2(fast_exp2(fmaf(s[2 * i], kSoftmaxScaleLog2, -m)), fast_exp2(fmaf(s[2 * i + 1], kSoftmaxScaleLog2, -m)));
-        sum = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(pf_bf16x2_t, w[i]), __builtin_bit_cast(pf_bf16x2_t, 0x3f803f80u), sum, false);
+      for (int i = 0; i < 16; ++i) p[i] = fast_exp2(fmaf(s[i], kSoftmaxScaleLog2, -m));
+      float odd = p[1];
+      sum = p[0];
+#pragma unroll
+      for (int i = 2; i < 16; i += 2) {
+        sum += p[i];
+        odd += p[i + 1];
       }
+      sum += odd;
     };
     weights();
     if (__ballot(!(sum <= kPfGrowth)) != 0ull) {
@@ -179,12 +183,20 @@ __device__ __forceinline__ void prefix_mfma_body(char* smem /* [2][K tile, V til
       weights();
     }
     l += sum;
+    uint32_t w[2][8];  // the weights' two terms
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      w[0][i] = BF16::round2(p[2 * i], p[2 * i + 1]);
+      w[1][i] = BF16::round2(p[2 * i] - __uint_as_float(w[0][i] << 16), p[2 * i + 1] - __uint_as_float(w[0][i] & 0xffff0000u));
+    }
 #pragma unroll
     for (int ks = 0; ks < 2; ++ks)
 #pragma unroll
-      for (int c = 0; c < 4; ++c)
-        o[c] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(va[ks][c], __builtin_bit_cast(am_bf16x8_t, make_uint4(w[4 * ks], w[4 * ks + 1], w[4 * ks + 2], w[4 * ks + 3])),
-                                                       o[c], 0, 0, 0);
+      for (int t = 0; t < 2; ++t)
+#pragma unroll
+        for (int c = 0; c < 4; ++c)
+          o[c] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
+              va[ks][c], __builtin_bit_cast(am_bf16x8_t, make_uint4(w[t][4 * ks], w[t][4 * ks + 1], w[t][4 * ks + 2], w[t][4 * ks + 3])), o[c], 0, 0, 0);
   };
 
   load(0);
@@ -290,9 +302,9 @@ struct OwnArgs {
 
 // Blocks [0, splits tiles Hkv): the prefix; behind them X = nsplit B blocks for every KV head.  (Neighbours in the grid are
 // runs of the prefix, so the tiles of a run, which read the same rows, go to one XCD where the runs are a multiple of 8.)
-// KIND: bf16: WQ; fp32: -QG.
+// KIND: bf16: WQ; fp32: -QG.  (KIND 1: its 128 KB of LDS leave a CU one block of four waves, so each may have all registers of its SIMD.)
 template <typename T, int NH, int WAVES, int KIND>
-__global__ __launch_bounds__(64 * WAVES, KIND == -1 ? 3 : 2) void shared_kernel(const void* __restrict__ q, PrefixArgs pa, OwnArgs oa) {
+__global__ __launch_bounds__(64 * WAVES, KIND == -1 ? 3 : KIND == 1 ? 1 : 2) void shared_kernel(const void* __restrict__ q, PrefixArgs pa, OwnArgs oa) {
   extern __shared__ __align__(16) char smem[];
   const int prefix_blocks = pa.splits * pa.tiles * oa.Hkv;
   if ((int)blockIdx.x < prefix_blocks) {

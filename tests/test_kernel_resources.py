@@ -55,3 +55,13 @@ def test_selection_and_attention_in_one_launch_keep_their_registers(kernels):
         assert scratch == 0, name
         if "BF16ELi1E" in name or "F32ELi1E" in name:
             assert regs <= 128, name
+
+
+def test_prefix_tiles_stay_in_registers(kernels):
+    """Eight waves of a block, two on a SIMD: at most 256 of its 512 registers each, and nothing in scratch; four waves, one on
+    each SIMD: all of them."""
+    found = {k: v for k, v in kernels.items() if "13shared_kernel" in k}
+    assert found
+    for name, (regs, scratch) in found.items():
+        assert scratch == 0, name
+        assert regs <= (256 if re.search(r"BF16ELi\dELi8E", name) else 512), name
