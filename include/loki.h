@@ -413,7 +413,8 @@ int loki_evict(const loki_layout* layout, const loki_evict_args* args, int S_max
  *   S_max, seq_lens     0 <= S_max <= S_cap; device int32 [B], 0 <= seq_lens[b] <= S_max (clamped); NULL: S_max.
  *                       A sequence with no row at all gives zeros.
  *   workspace           >= dense_shared_workspace_bytes(layout, prefix_rows, S_max), 256-byte aligned
- * The prefix is read once for the whole batch.  Batches with several prefixes take one call for each.
+ * The prefix is read once for the whole batch.  Batches with several prefixes take one call for each.  A workspace sized for
+ * a prefix_rows and an S_max also serves shorter ones of the same batch.
  */
 int dense_shared_workspace_bytes(const loki_layout* layout, int prefix_rows, int S_max, size_t* bytes);
 int dense_decode_shared(const loki_layout* layout, const void* q, const void* k_prefix, const void* v_prefix, int prefix_rows,

@@ -939,7 +939,7 @@ int dense_shared_workspace_bytes(const loki_layout* layout, int prefix_rows, int
   if (rc != LOKI_OK) return rc;
   if (!bytes || prefix_rows < 0 || prefix_rows > kMostRows || S_max < 0 || S_max > s.S_cap) return LOKI_ERR_INVALID_ARG;
   s.S = S_max;
-  *bytes = plan_parts(s, shared_own_splits(s), prefix_splits(s, prefix_rows), false, nullptr).total;
+  *bytes = plan_parts(s, shared_own_splits_at_most(s), prefix_splits_at_most(s, prefix_rows), false, nullptr).total;
   return LOKI_OK;
 }
 
@@ -958,8 +958,9 @@ int dense_decode_shared(const loki_layout* layout, const void* q, const void* k_
   s.S = S_max;
   s.rg.seq_lens = seq_lens;
   const int nsplit = shared_own_splits(s), shared = prefix_splits(s, prefix_rows);
+  if (plan_parts(s, shared_own_splits_at_most(s), prefix_splits_at_most(s, prefix_rows), false, nullptr).total > workspace_bytes)
+    return LOKI_ERR_WORKSPACE;
   const PartsPlan w = plan_parts(s, nsplit, shared, false, workspace);
-  if (w.total > workspace_bytes) return LOKI_ERR_WORKSPACE;
   hipStream_t st = static_cast<hipStream_t>(stream);
   StageTimer tm(st);
   tm.begin("shared_parts");

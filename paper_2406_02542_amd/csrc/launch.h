@@ -281,6 +281,9 @@ hipError_t launch_weigh_merge(const Shape& s, int nsplit, int shared, const floa
 // heads, nsplit B places for each query head's own.
 int prefix_splits(const Shape& s, int prefix_rows);
 int shared_own_splits(const Shape& s);
+// The most of either at any length up to this one, which a workspace is sized for.
+int prefix_splits_at_most(const Shape& s, int prefix_rows);
+int shared_own_splits_at_most(const Shape& s);
 hipError_t launch_shared(const Shape& s, int splits, int nsplit, const void* q, const void* k_prefix, const void* v_prefix,
                          int prefix_rows, int prefix_cap, const void* k, const void* v, float* prefix, float* partial, hipStream_t st);
 hipError_t launch_rotate(const Shape& s, const void* k_new, const float* P, void* klo, void* khi,

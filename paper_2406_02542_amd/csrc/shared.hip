@@ -347,21 +347,29 @@ static int prefix_tiles(const Shape& s) {
   return (s.B * s.G + nq - 1) / nq;
 }
 
-static int prefix_run(const Shape& s, int rows) {
-  // A block for every CU, also where more would fit: more runs mean more parts to write and to merge.  us with one, two and
-  // three or four per CU, fp32: 5 sequences of 16/8 heads behind 5777 rows 16.0, 16.9, 19.0, behind 20000 37.3, 38.3, 39.7; 64 of 64/8
-  // behind 6000 124, 150.
-  const PrefixShape ps = prefix_shape(s);
-  int n = device_cus() / (s.Hkv * prefix_tiles(s));
-  if (n < 1) n = 1;
-  int run = (rows + n - 1) / n;
-  // Many query heads, whose parts weigh more than their products: runs of at least 256 rows from 600 heads of the batch on, of 384
-  // from 2048.  bf16, us with runs as they come / of 256 / 384 / 512: 256 heads behind 2048 rows 11.9 / 12.7 / 14.5 / 15.5, 512
-  // behind 1000 13.6 / 14.6 / 15.9 / 16.8, 640 behind 2000 23.8 / 19.9 / 17.3 / 17.5, 1024 behind 4000 22.5 / 18.2 / 19.5 / 21.3, 4096
-  // behind 2000 33.6 / 30.2 / 30.0 / 32.0, behind 4000 38.1 / 37.9 / 35.5 / 34.5.
+// Runs of the prefix at most: a block for every CU, also where more would fit: more runs mean more parts to write and to merge.  us with
+// one, two and three or four per CU, fp32: 5 sequences of 16/8 heads behind 5777 rows 16.0, 16.9, 19.0, behind 20000 37.3, 38.3,
+// 39.7; 64 of 64/8 behind 6000 124, 150.
+static int prefix_most(const Shape& s) {
+  const int n = device_cus() / (s.Hkv * prefix_tiles(s));
+  return n < 1 ? 1 : n;
+}
+
+// Rows of a run at least.  Many query heads, whose parts weigh more than their products: 256 rows from 600 heads of the batch on, 384
+// from 2048.  bf16, us with runs as they come / of 256 / 384 / 512: 256 heads behind 2048 rows 11.9 / 12.7 / 14.5 / 15.5, 512
+// behind 1000 13.6 / 14.6 / 15.9 / 16.8, 640 behind 2000 23.8 / 19.9 / 17.3 / 17.5, 1024 behind 4000 22.5 / 18.2 / 19.5 / 21.3, 4096
+// behind 2000 33.6 / 30.2 / 30.0 / 32.0, behind 4000 38.1 / 37.9 / 35.5 / 34.5.
+static int prefix_least(const Shape& s) {
   const int heads = s.B * s.Hq, least = s.dtype == 0 || heads < 600 ? 1 : heads < 2048 ? 256 : 384;
+  const int keys = prefix_shape(s).keys;
+  return (least + keys - 1) / keys * keys;
+}
+
+static int prefix_run(const Shape& s, int rows) {
+  const int n = prefix_most(s), least = prefix_least(s), keys = prefix_shape(s).keys;
+  int run = (rows + n - 1) / n;
   if (run < least) run = least;
-  return (run + ps.keys - 1) / ps.keys * ps.keys;
+  return (run + keys - 1) / keys * keys;
 }
 
 int prefix_splits(const Shape& s, int prefix_rows) {
@@ -370,24 +378,41 @@ int prefix_splits(const Shape& s, int prefix_rows) {
   return (prefix_rows + run - 1) / run;
 }
 
+int prefix_splits_at_most(const Shape& s, int prefix_rows) {
+  if (prefix_rows < 1) return 0;
+  const int n = prefix_most(s), least = prefix_least(s), whole = (prefix_rows + least - 1) / least;
+  return whole < n ? whole : n;
+}
+
 // One launch for the prefix and the sequences' own rows while the latter are few: a launch less, but their blocks then have
 // the registers and LDS of the prefix's and eight waves fill a CU.  us in one / in two launches: 3 sequences of 32/8 heads behind
 // 700 rows with 30 of their own 10.4 / 15.4, 8 behind 2048 with 300 (10 MB) 14.2 / 18.6; 8 of 32/16 heads behind 4096 with 500
 // (33 MB) 23.5 / 22.0, 32 of 32/8 with 1500 (197 MB) 44.5 / 41.3, 16 of 32/32 with 2048 (537 MB) 99.6 / 76.6.
-static bool in_one_launch(const Shape& s) {
-  return (double)s.B * s.Hkv * s.S * (2 * kD * s.elem_bytes) < 24e6;
-}
+constexpr double kOneLaunchBytes = 24e6;
+static double own_bytes(const Shape& s, int rows) { return (double)s.B * s.Hkv * rows * (2 * kD * s.elem_bytes); }
+static bool in_one_launch(const Shape& s) { return own_bytes(s, s.S) < kOneLaunchBytes; }
 
-// Runs of a sequence's own rows: two steps for every wave in bf16, one in fp32 (8 sequences of 32/8 bf16 heads with 300 rows
-// behind 2048: one step 14.0 us, two 11.8; 5 of 16/8 fp32 heads with 131 behind 5777 16.1, 17.1).
-int shared_own_splits(const Shape& s) {
-  if (s.S < 1) return 0;
-  if (!in_one_launch(s)) return weigh_splits(s);
+// Runs of a sequence's own rows in that one launch: two steps for every wave in bf16, one in fp32 (8 sequences of 32/8 bf16 heads with
+// 300 rows behind 2048: one step 14.0 us, two 11.8; 5 of 16/8 fp32 heads with 131 behind 5777 16.1, 17.1).
+static int one_launch_splits(const Shape& s, int own_rows) {
   const int units = s.B * s.Hkv, waves = s.dtype == 0 || prefix_shape(s).queries == 32 ? 4 : 8;
   int n = ((s.dtype == 0 ? 8 : 24 / waves) * device_cus() + units - 1) / units;
-  const int rows = (s.dtype == 0 ? 32 : 64) * waves, most = (s.S + rows - 1) / rows;
+  const int rows = (s.dtype == 0 ? 32 : 64) * waves, most = (own_rows + rows - 1) / rows;
   if (n > most) n = most;
   return n < 1 ? 1 : n;
+}
+
+int shared_own_splits(const Shape& s) {
+  if (s.S < 1) return 0;
+  return in_one_launch(s) ? one_launch_splits(s, s.S) : weigh_splits(s);
+}
+
+int shared_own_splits_at_most(const Shape& s) {
+  if (s.S < 1) return 0;
+  if (in_one_launch(s)) return one_launch_splits(s, s.S);
+  // the longest rows of one launch, or one more
+  const int apart = weigh_splits(s), together = one_launch_splits(s, (int)(kOneLaunchBytes / own_bytes(s, 1)) + 1);
+  return apart > together ? apart : together;
 }
 
 template <typename T, int NH, int WAVES, int KIND>

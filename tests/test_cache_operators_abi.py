@@ -248,3 +248,15 @@ def test_binding_refuses_what_does_not_fit():
         api.dense_decode_weights(lay, t, t, t, 64, None, None, t, t, t)
     with pytest.raises(ValueError, match="GPU"):
         api.dense_decode_shared(lay, t, t, t, 1, None, None, 0, None, t, t)
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("B,Hq,Hkv", [(1, 8, 8), (3, 4, 1), (8, 32, 8), (44, 64, 8), (64, 64, 8), (20, 32, 32), (130, 8, 1)])
+def test_shared_workspace_of_the_longest_lengths_serves_shorter_ones(B, Hq, Hkv, dtype):
+    """Of the prefix and of the sequences' own rows: runs get longer in steps, and the own rows have two rules."""
+    lay = api.make_layout(B, Hq, Hkv, 128, 128, 16384, dtype)
+    prefixes = (0, 1, 127, 128, 129, 500, 1000, 2048, 4096, 4097, 8192, 8193, 20000, 33000, 1 << 20)
+    lens = (0, 1, 63, 64, 65, 300, 301, 700, 1171, 1172, 1500, 2048, 4186, 8192, 16384)
+    size = [[api.dense_shared_workspace_bytes(lay, P, S) for S in lens] for P in prefixes]
+    assert all(row == sorted(row) for row in size)
+    assert all(list(col) == sorted(col) for col in zip(*size))

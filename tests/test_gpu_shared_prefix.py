@@ -99,3 +99,28 @@ def test_same_result_every_time_and_on_a_replayed_graph():
         graph.replay()
         torch.cuda.synchronize()
         assert torch.equal(out, eager())
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("B,Hq,Hkv", [(8, 32, 8), (40, 16, 2)])
+def test_one_workspace_for_growing_prefixes_and_sequences(B, Hq, Hkv, dtype):
+    """Sized once for the longest of both; nothing behind it is written."""
+    P, S, G, dt = 9000, 700, Hq // Hkv, DT[dtype]
+    gen = torch.Generator(device="cuda").manual_seed(9)
+    rand = lambda *s: torch.randn(s, generator=gen, device="cuda").to(dt)
+    q, kp, vp, k, v = rand(B, Hq, 128), rand(Hkv, P, 128), rand(Hkv, P, 128), rand(B, Hkv, S, 128), rand(B, Hkv, S, 128)
+    lay = api.make_layout(B, Hq, Hkv, 128, 128, S, dt)
+    need = api.dense_shared_workspace_bytes(lay, P, S)
+    buf = torch.full((need + 4096,), 255, dtype=torch.uint8, device="cuda")
+    out = torch.empty_like(q)
+    for rows, own in ((P, S), (8193, 5), (8192, 300), (4097, S), (4096, 64), (4096, 0), (129, 33), (1, 1), (0, S)):
+        print("case", B, Hq, Hkv, dtype, rows, own, flush=True)
+        assert api.dense_shared_workspace_bytes(lay, rows, own) <= need
+        api.dense_decode_shared(lay, q, kp, vp, rows, k, v, own, None, buf[:need], out)
+        torch.cuda.synchronize()
+        assert bool((buf[need:] == 255).all())
+        for b in (0, B - 1):
+            for h in (0, Hkv - 1):
+                kk, vv = torch.cat([kp[h, :rows], k[b, h, :own]]), torch.cat([vp[h, :rows], v[b, h, :own]])
+                ref, _, bound, _ = attend64(q[b, h * G:(h + 1) * G], kk, vv, {"bf16": 2.0 ** -16, "f32": 0.0}[dtype])
+                assert worst(out[b, h * G:(h + 1) * G], ref, bound, dtype) <= 0, (b, h)
