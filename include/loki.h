@@ -354,7 +354,9 @@ int loki_rotary_frequencies(int rotary_dims, double base, int scaling, double fa
  * for the rows s < seq_lens[b]; later entries of weights_out are not written.
  *   seq_lens    device int32 [B], 0 <= seq_lens[b] <= S_max (clamped); NULL: S_max.  A sequence without rows
  *               gives zeros in `out`.
- *   weights_in  device fp32 [B, Hkv, S_cap] or NULL (zeros); weights_out likewise, may be weights_in
+ *   weights_in  device fp32 [B, Hkv, S_cap] or NULL (zeros); weights_out likewise, may be weights_in.  The total of a row that
+ *               is new begins with what its place holds: the caller sets it to zero when the row is appended (behind
+ *               an eviction in place that is the total of the row which was there)
  *   workspace   >= dense_weights_workspace_bytes(layout, S_max), 256-byte aligned
  * A workspace sized for an S_max also serves shorter ones.
  */
@@ -373,7 +375,8 @@ int dense_decode_weights(const loki_layout* layout, const void* q, const void* k
  *   weights    device fp32 [B, Hkv, S_cap] (no NaN); moved along with the rows when in place
  *   klo_out .. weights_out   the cache that the kept rows go to, rows 0 .. of [B, Hkv, S_cap_out, .],
  *              S_cap_out >= min(budget, S_max); later rows are not written.  weights_out may be NULL.  The two caches must
- *              not overlap.  All NULL: in place, row j from row idx[j] >= j; later rows stay as they are.
+ *              not overlap.  All NULL: in place, row j from row idx[j] >= j; later rows stay as they are, and so do
+ *              their weights, which the caller sets to zero where rows are appended
  *   lens_out   device int32 [B] or NULL: rows kept, min(seq_lens[b], budget).  May be seq_lens.
  *   out_idx    device int32 [B, Hkv, budget] or NULL: the rows kept, ascending, -1 behind them
  *   page_table .. as in loki_step_args: klo, khi, v are paged pools (out caches are never; weights neither). A

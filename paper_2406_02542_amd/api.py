@@ -484,7 +484,9 @@ def dense_weights_workspace_bytes(layout: Layout, S_max: int) -> int:
 def dense_decode_weights(layout: Layout, q: torch.Tensor, k_full: torch.Tensor, v: torch.Tensor, S_max: int,
                          seq_lens: Optional[torch.Tensor], weights_in: Optional[torch.Tensor], weights_out: torch.Tensor,
                          workspace: torch.Tensor, out: torch.Tensor, stream=None) -> None:
-    """``dense_decode_step`` that adds every row's softmax weight to its running total [B, Hkv, S_cap]."""
+    """``dense_decode_step`` that adds every row's softmax weight to its running total [B, Hkv, S_cap].  A new row's total
+    begins with what ``weights_in`` holds there: set it to zero with the append, for instance
+    ``weights.scatter_(2, rows.long()[:, None, None].expand(-1, Hkv, 1), 0.0)`` for the rows [B] that are written."""
     dt = _torch_dtype(layout)
     rows = layout.B * layout.Hkv * layout.S_cap
     nq = layout.B * layout.Hq * layout.D

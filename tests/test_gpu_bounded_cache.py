@@ -168,3 +168,51 @@ def test_two_streams_with_their_own_workspaces():
     torch.cuda.synchronize()
     for s, (k, v), ref in zip(sets, caches, alone):
         assert all(torch.equal(a, b) for a, b in zip((s["out"], s["total"], s["idx"], k, v), ref))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_totals_of_rows_appended_behind_an_eviction(dtype):
+    """A new row's place holds the total of the row that was there; cleared with the append, on the device, a row has gathered
+    what its own steps gave it, over several evictions; left alone it begins with the old total."""
+    B, Hq, Hkv, cap, budget, sinks, recent = 2, 4, 2, 48, 32, 2, 8
+    dt, G = DT[dtype], Hq // Hkv
+    lay = api.make_layout(B, Hq, Hkv, 128, 128, cap, dt)
+    gen = torch.Generator(device="cuda").manual_seed(17)
+    rand = lambda *s: torch.randn(s, generator=gen, device="cuda").to(dt)
+    k, v = rand(B, Hkv, cap, 128), rand(B, Hkv, cap, 128)
+    w, total = torch.zeros((B, Hkv, cap), device="cuda"), torch.zeros((B, Hkv, cap), dtype=torch.float64, device="cuda")
+    lens = torch.full((B,), 20, dtype=torch.int32, device="cuda")
+    ws = torch.empty(max(api.dense_weights_workspace_bytes(lay, cap), api.loki_evict_workspace_bytes(lay, cap, budget)), dtype=torch.uint8,
+                     device="cuda")
+    idx = torch.empty((B, Hkv, budget), dtype=torch.int32, device="cuda")
+    out, off, evictions = torch.empty((B, Hq, 128), dtype=dt, device="cuda"), 0.0, 0
+    for step in range(80):
+        at = lens.long()[:, None, None].expand(-1, Hkv, 1)
+        k.scatter_(2, at[..., None].expand(-1, -1, -1, 128), rand(B, Hkv, 1, 128))
+        v.scatter_(2, at[..., None].expand(-1, -1, -1, 128), rand(B, Hkv, 1, 128))
+        inherited = w.gather(2, at).clone()
+        if step == 79:  # the last one keeps what it finds
+            assert float(inherited.min()) > 0
+        else:
+            w.scatter_(2, at, 0.0)
+            total.scatter_(2, at, 0.0)
+        lens += 1
+        q = rand(B, Hq, 128)
+        api.dense_decode_weights(lay, q, k, v, cap, lens, w, w, ws, out)
+        torch.cuda.synchronize()
+        n = int(lens[0])
+        if step == 79:
+            total.scatter_(2, at, inherited.double())
+        rels = []
+        for b in range(B):
+            for h in range(Hkv):
+                _, p, _, rel = attend64(q[b, h * G:(h + 1) * G], k[b, h, :n], v[b, h, :n])
+                total[b, h, :n] += p.sum(0)
+                rels.append(rel)
+        off += max(rels) + (G + 1) * 2.0 ** -24  # of each step, relative to a total that only grows
+        assert bool(((w - total).abs()[:, :, :n] <= off * total[:, :, :n]).all()), step
+        if n == cap:
+            evictions += 1
+            api.loki_evict(lay, w, k, None, v, cap, budget, sinks, recent, ws, seq_lens=lens, lens_out=lens, out_idx=idx)
+            total[:, :, :budget] = total.gather(2, idx.long())
+    assert evictions >= 3
