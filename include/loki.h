@@ -341,7 +341,8 @@ int loki_rotary(const loki_layout* layout, int n_new, const loki_rotary_args* ar
  *   BANDS   by the turns n_i = original_context f_i / (2 pi) a pair makes in the original context: above `high`
  *           as they are, below `low` divided by factor, between them a mix linear in n_i (low < high)
  *   RAMP    a mix linear in i, from as they are up to the pair that makes `high` turns (rounded down) to divided
- *           by factor from the pair that makes `low` turns (rounded up); *scale = 0.1 ln(factor) + 1
+ *           by factor from the pair that makes `low` turns (rounded up), both as real numbers, also outside the pairs
+ *           there are; *scale = 0.1 ln(factor) + 1
  * frequencies: host fp64 [rotary_dims / 2]; scale: host, may be NULL, 1 unless stated.  factor >= 1, base > 1.
  */
 enum { LOKI_ROTARY_NONE = 0, LOKI_ROTARY_LINEAR = 1, LOKI_ROTARY_BASE = 2, LOKI_ROTARY_BANDS = 3, LOKI_ROTARY_RAMP = 4 };

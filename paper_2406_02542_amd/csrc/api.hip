@@ -743,14 +743,12 @@ int loki_rotary_frequencies(int rotary_dims, double base, int scaling, double fa
   if (scaling == LOKI_ROTARY_BASE && R == 2) return LOKI_ERR_INVALID_ARG;
   const double two_pi = 6.283185307179586476925;
   if (scaling == LOKI_ROTARY_BASE) base *= pow(factor, (double)R / (R - 2));
-  double from = 0.0, to = 0.0;  // RAMP: the pairs between which the mix changes
+  double from = 0.0, to = 0.0;  // RAMP: the pairs between which the mix changes, which need not be there
   if (scaling == LOKI_ROTARY_RAMP) {
     // pair i makes original_context base^(-2 i / R) / (2 pi) turns
     from = floor(R * log(original_context / (two_pi * high)) / (2.0 * log(base)));
     to = ceil(R * log(original_context / (two_pi * low)) / (2.0 * log(base)));
-    from = from < 0.0 ? 0.0 : from;
-    to = to > R - 1.0 ? R - 1.0 : to;
-    if (!(to > from)) to = from + 0.001;  // a step
+    if (!(to > from)) to = from + 1.0;  // (high > low, so only where the two logarithms are the same)
   }
   for (int i = 0; i < R / 2; ++i) {
     const double f = pow(base, -2.0 * i / R);

@@ -260,3 +260,20 @@ def test_shared_workspace_of_the_longest_lengths_serves_shorter_ones(B, Hq, Hkv,
     size = [[api.dense_shared_workspace_bytes(lay, P, S) for S in lens] for P in prefixes]
     assert all(row == sorted(row) for row in size)
     assert all(list(col) == sorted(col) for col in zip(*size))
+
+
+@pytest.mark.parametrize("R,base,factor,ctx,low,high", [(128, 10000.0, 4.0, 100.0, 1.0, 32.0), (128, 10000.0, 4.0, 1e9, 1.0, 32.0),
+                                                        (64, 500000.0, 8.0, 4.0, 1.0, 4.0), (64, 10000.0, 2.0, 1e-3, 1.0, 4.0),
+                                                        (20, 100.0, 16.0, 1e12, 1.0, 2.0), (2, 10000.0, 4.0, 50.0, 1.0, 32.0),
+                                                        (128, 10000.0, 4.0, 4096.0, 1.0, 1.0 + 1e-12)])
+def test_frequencies_ramp_with_ends_outside_the_pairs(R, base, factor, ctx, low, high):
+    """The mix is linear between the pairs that make `high` and `low` turns, also where there are no such pairs: contexts in which
+    even the first pair makes fewer turns, or the last one more."""
+    f, _ = _freqs(R, base)
+    g, _ = _freqs(R, base, api.ROTARY_RAMP, factor, ctx, low, high)
+    pair = lambda turns: R * math.log(ctx / (2 * math.pi * turns)) / (2 * math.log(base))
+    a, b = math.floor(pair(high)), math.ceil(pair(low))
+    assert a < b
+    for i, (x, y) in enumerate(zip(f, g)):
+        r = min(max((i - a) / (b - a), 0.0), 1.0)
+        assert y == pytest.approx(x * (1 - r) + x / factor * r, rel=1e-12), i
