@@ -430,6 +430,8 @@ def _rotary_tensor(name: str, x: Optional[torch.Tensor], y: Optional[torch.Tenso
     """The members of a ``loki_rotary_tensor``: x [B, n, heads, D] to y, of the same shape or head-major
     [B, heads, rows, D], both with any strides of whole rows."""
     if x is None:
+        if y is not None:
+            raise ValueError(f"{name}_out without {name}")
         return _NOT_THERE
     if y is not None and x.is_cuda and y.is_cuda and x.dtype is dt and y.dtype is dt and x.shape == shape and y.shape == out_shape:
         ib, it, ih, ic = x.stride()
@@ -510,6 +512,13 @@ def loki_evict_workspace_bytes(layout: Layout, S_max: int, budget: int) -> int:
     return n.value
 
 
+def _same_rows(units: int, rows: int, *parts) -> None:
+    """Every part (name, tensor or None, width) of a cache holds exactly `rows` rows for each unit: one stride goes for all."""
+    for name, t, width in parts:
+        if t is not None and t.numel() != units * rows * width:
+            raise ValueError(f"{name} holds {t.numel()} elements, {rows} rows of {width} for {units} heads have {units * rows * width}")
+
+
 _evict_pack = struct.Struct("P" * 12 + "iiii").pack  # EvictArgs
 
 
@@ -526,6 +535,9 @@ def loki_evict(layout: Layout, weights: torch.Tensor, klo: torch.Tensor, khi: Op
     units, D, d = layout.B * layout.Hkv, layout.D, layout.d_split
     cache_rows = (n_pages * layout.Hkv * page_rows) if page_table is not None else units * layout.S_cap
     cap_out = klo_out.numel() // (units * d) if klo_out is not None else 0
+    if klo_out is not None:
+        _same_rows(units, cap_out, ("klo_out", klo_out, d), ("khi_out", khi_out if d < D else None, D - d), ("v_out", v_out, D),
+                   ("weights_out", weights_out, 1))
     args = _evict_pack(
         _ptr(seq_lens, "seq_lens", torch.int32, layout.B) or 0,
         _ptr(weights, "weights", torch.float32, units * layout.S_cap),
@@ -559,7 +571,10 @@ def dense_decode_shared(layout: Layout, q: torch.Tensor, k_prefix: Optional[torc
     H, D = layout.Hkv, layout.D
     rows = layout.B * H * layout.S_cap if S_max > 0 else 0
     nq = layout.B * layout.Hq * D
+    if (k_prefix is None) != (v_prefix is None):
+        raise ValueError("k_prefix and v_prefix go together")
     cap = k_prefix.numel() // (H * D) if k_prefix is not None else 0
+    _same_rows(H, cap, ("k_prefix", k_prefix, D), ("v_prefix", v_prefix, D))
     _check(lib().dense_decode_shared(
         ctypes.byref(layout),
         _ptr(q, "q", dt, nq),

@@ -277,3 +277,34 @@ def test_frequencies_ramp_with_ends_outside_the_pairs(R, base, factor, ctx, low,
     for i, (x, y) in enumerate(zip(f, g)):
         r = min(max((i - a) / (b - a), 0.0), 1.0)
         assert y == pytest.approx(x * (1 - r) + x / factor * r, rel=1e-12), i
+
+
+def test_binding_refuses_caches_of_different_lengths():
+    """The calls take one number of rows for all parts of a cache; what would be read or written at the wrong places is refused."""
+    lay, units = api.make_layout(2, 4, 4, 128, 32, 64, torch.bfloat16), 8
+    t = lambda rows, x: torch.zeros(units * rows * x, dtype=torch.bfloat16)
+    w, ws = torch.zeros(units * 64), torch.zeros(1 << 20, dtype=torch.uint8)
+    evict = lambda **kw: api.loki_evict(lay, w, t(64, 32), t(64, 96), t(64, 128), 64, 8, 0, 0, ws, **kw)
+    ok = dict(klo_out=t(10, 32), khi_out=t(10, 96), v_out=t(10, 128), weights_out=torch.zeros(units * 10))
+    for name, other in (("klo_out", t(10, 32)[:-8]), ("khi_out", t(11, 96)), ("khi_out", t(9, 96)), ("v_out", t(11, 128)), ("v_out", t(9, 128)),
+                        ("weights_out", torch.zeros(units * 11)), ("weights_out", torch.zeros(units * 64))):
+        with pytest.raises(ValueError, match=name):
+            evict(**{**ok, name: other})
+    with pytest.raises(ValueError, match="GPU"):
+        evict(**ok)
+    q, out = torch.zeros(2, 4, 128, dtype=torch.bfloat16), torch.zeros(2, 4, 128, dtype=torch.bfloat16)
+    p = lambda rows: torch.zeros(4, rows, 128, dtype=torch.bfloat16)
+    shared = lambda kp, vp: api.dense_decode_shared(lay, q, kp, vp, 8, None, None, 0, None, ws, out)
+    for kp, vp in ((p(8), p(9)), (p(9), p(8)), (p(8).flatten()[:-1], p(8)), (p(8), None), (None, p(8))):
+        with pytest.raises(ValueError, match="_prefix"):
+            shared(kp, vp)
+    with pytest.raises(ValueError, match="GPU"):
+        shared(p(8), p(8))
+
+
+def test_binding_refuses_rotary_outputs_without_their_inputs():
+    lay = api.make_layout(1, 1, 1, 128, 128, 64, torch.float32)
+    t, pos, f = torch.zeros(1, 2, 1, 128), torch.zeros(1, 2, dtype=torch.int32), torch.zeros(64, dtype=torch.float64)
+    for name in "qkv":
+        with pytest.raises(ValueError, match=f"{name}_out"):
+            api.loki_rotary(lay, pos, f, **{name + "_out": t})
