@@ -355,13 +355,12 @@ static int prefix_most(const Shape& s) {
   return n < 1 ? 1 : n;
 }
 
-// Rows of a run at least.  Many query heads, whose parts weigh more than their products: 256 rows from 600 heads of the batch on, 384
-// from 2048.  bf16, us with runs as they come / of 256 / 384 / 512: 256 heads behind 2048 rows 11.9 / 12.7 / 14.5 / 15.5, 512
-// behind 1000 13.6 / 14.6 / 15.9 / 16.8, 640 behind 2000 23.8 / 19.9 / 17.3 / 17.5, 1024 behind 4000 22.5 / 18.2 / 19.5 / 21.3, 4096
-// behind 2000 33.6 / 30.2 / 30.0 / 32.0, behind 4000 38.1 / 37.9 / 35.5 / 34.5.
+// Rows of a run at least: 256 from 600 heads of the batch on, whose parts weigh more than their products.  bf16, us with runs as they
+// come / of 256 / of 384, behind 1000, 2000 and 4000 rows with a few of their own: 640 heads 14.1 / 15.5 / 17.3, 20.1 / 16.2 / 18.2, 21.2 /
+// 17.2 / 18.9; 1024 16.1 / 16.4 / 18.4, 21.6 / 17.5 / 19.4, 22.5 / 18.3 / 20.1; 1536 18.5 / 21.1 / 24.4, 25.6 / 22.2 / 26.0, 25.5 /
+// 22.4 / 25.9; 4096 41.9 / 43.2 / 47.3, 44.7 / 45.3 / 48.7, 50.1 / 50.2 / 51.0; 256 heads behind 2048 rows 12.2 / 11.9 / 12.2.
 static int prefix_least(const Shape& s) {
-  const int heads = s.B * s.Hq, least = s.dtype == 0 || heads < 600 ? 1 : heads < 2048 ? 256 : 384;
-  const int keys = prefix_shape(s).keys;
+  const int least = s.dtype == 0 || s.B * s.Hq < 600 ? 1 : 256, keys = prefix_shape(s).keys;
   return (least + keys - 1) / keys * keys;
 }
 
