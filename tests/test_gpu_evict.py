@@ -196,3 +196,40 @@ def test_replayed_graph():
                 keep = kept_rows(host[b, h], S, budget, 4, 20)
                 assert np.array_equal(idx[b, h].cpu().numpy(), keep)
                 assert torch.equal(v[b, h, :budget], v0[b, h][torch.from_numpy(keep).cuda()])
+
+
+@pytest.mark.parametrize("into", [None, 900])
+@pytest.mark.parametrize("page_rows", [0, 256])
+@pytest.mark.parametrize("budget", [1, 100, 899, 900, 901, 40000])
+def test_lists_of_the_workspace(budget, page_rows, into):
+    """Without out_idx the lists lie in the workspace, no longer than the rows there can be; nothing behind it is written."""
+    B, H, S, cap, lens = 3, 2, 900, 910, [900, 0, 333]
+    print("case", budget, page_rows, into, flush=True)
+    gen = torch.Generator(device="cuda").manual_seed(budget + page_rows)
+    lay = api.make_layout(B, H, H, 128, 32, cap, torch.bfloat16)
+    w = weights("few", B, H, cap, budget)
+    rand = lambda *s: torch.randn(s, generator=gen, device="cuda").bfloat16()
+    paged, lead = {}, (B, H, cap)
+    if page_rows:
+        table = torch.randperm(12, generator=torch.Generator().manual_seed(3)).to(torch.int32).reshape(B, 4)
+        paged, lead = dict(page_table=table.cuda(), page_rows=page_rows, n_pages=12), (12, H, page_rows)
+    cache = [rand(*lead, x) for x in (32, 96, 128)]
+
+    def rows_of(t):
+        return t[table.long().cuda().flatten()].reshape(B, 4, H, page_rows, -1).transpose(1, 2).reshape(B, H, 4 * page_rows, -1) if page_rows else t
+
+    before, w0 = [rows_of(t).clone() for t in cache], w.cpu().numpy()
+    outs = [torch.zeros((B, H, into, x), dtype=torch.bfloat16, device="cuda") for x in (32, 96, 128)] if into else [None] * 3
+    need = api.loki_evict_workspace_bytes(lay, S, budget)
+    buf = torch.full((need + 4096,), 255, dtype=torch.uint8, device="cuda")
+    recent = min(20, budget)
+    api.loki_evict(lay, w, *cache, S, budget, 0, recent, buf[:need], seq_lens=torch.tensor(lens, dtype=torch.int32, device="cuda"),
+                   klo_out=outs[0], khi_out=outs[1], v_out=outs[2], **paged)
+    torch.cuda.synchronize()
+    assert bool((buf[need:] == 255).all())
+    for b, n in enumerate(lens):
+        for h in range(H):
+            at = torch.from_numpy(kept_rows(w0[b, h], n, budget, 0, recent)).cuda()
+            for t, old, new in zip(cache, before, outs):
+                got = new[b, h] if into else rows_of(t)[b, h]
+                assert torch.equal(got[:len(at)], old[b, h][at])
