@@ -298,8 +298,8 @@ int dense_decode_step(const loki_layout* layout, const void* q, const void* k_fu
  *   q, k, v   the tensors to take along (in == NULL: not there; v is carried over unturned). Element
  *             (b, token j, head h, column c) lies at in + b in_batch + j in_token + h in_head + c and goes
  *             to the same sum of the out strides (elements of the storage type, multiples of 16 bytes, at
- *             least 0; two tokens' or heads' outputs must not overlap).  out may be in with the same strides, else the two
- *             must not overlap.  q_out as the decode calls take it is [B, Hq, D], k_new of
+ *             least 0; two tokens' or heads' outputs must not overlap).  out may be in with the same strides, without
+ *             rows, else the two must not overlap.  q_out as the decode calls take it is [B, Hq, D], k_new of
  *             loki_rotate_keys [B, Hkv, n_new, D], k_new of loki_decode_step [B, m, Hkv, D].
  *   positions device int32 [B, n_new]; B n_new <= 2^24
  *   rows      device int32 [B, n_new] or NULL.  When given, token j's key and value go to row

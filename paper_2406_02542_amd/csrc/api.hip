@@ -679,7 +679,7 @@ int dense_decode_step(const loki_layout* layout, const void* q, const void* k_fu
 }
 
 // ---- rotary positions, weighed rows and their eviction, shared prefixes ---------------------------
-static int rotary_tensor(const loki_rotary_tensor& x, int heads, int epc, RotaryTensor* t) {
+static int rotary_tensor(const loki_rotary_tensor& x, int B, int n, int heads, int epc, bool by_rows, RotaryTensor* t) {
   if (x.in == nullptr) return LOKI_OK;
   if (x.out == nullptr) return LOKI_ERR_INVALID_ARG;
   const int64_t st[6] = {x.in_batch, x.in_token, x.in_head, x.out_batch, x.out_token, x.out_head};
@@ -688,6 +688,9 @@ static int rotary_tensor(const loki_rotary_tensor& x, int heads, int epc, Rotary
     if (v % epc != 0) return LOKI_ERR_ALIGNMENT;
   }
   if (!aligned16(x.in) || !aligned16(x.out)) return LOKI_ERR_ALIGNMENT;
+  // in place: every row where it lies, else one is written that another block has yet to read
+  const bool moves = by_rows || (B > 1 && st[0] != st[3]) || (n > 1 && st[1] != st[4]) || (heads > 1 && st[2] != st[5]);
+  if (x.in == x.out && moves) return LOKI_ERR_INVALID_ARG;
   *t = RotaryTensor{x.in, x.out, heads, x.in_batch, x.in_token, x.in_head, x.out_batch, x.out_token, x.out_head};
   return LOKI_OK;
 }
@@ -710,9 +713,10 @@ int loki_rotary(const loki_layout* layout, int n_new, const loki_rotary_args* ar
     return LOKI_ERR_ALIGNMENT;
   RotaryArgs a{};
   const int epc = 16 / s.elem_bytes;
-  if ((rc = rotary_tensor(args->q, s.Hq, epc, &a.q)) != LOKI_OK) return rc;
-  if ((rc = rotary_tensor(args->k, s.Hkv, epc, &a.k)) != LOKI_OK) return rc;
-  if ((rc = rotary_tensor(args->v, s.Hkv, epc, &a.v)) != LOKI_OK) return rc;
+  const bool by_rows = args->rows != nullptr;
+  if ((rc = rotary_tensor(args->q, s.B, n_new, s.Hq, epc, false, &a.q)) != LOKI_OK) return rc;
+  if ((rc = rotary_tensor(args->k, s.B, n_new, s.Hkv, epc, by_rows, &a.k)) != LOKI_OK) return rc;
+  if ((rc = rotary_tensor(args->v, s.B, n_new, s.Hkv, epc, by_rows, &a.v)) != LOKI_OK) return rc;
   a.positions = args->positions;
   a.rows = args->rows;
   a.freqs = args->frequencies;

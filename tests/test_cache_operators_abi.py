@@ -308,3 +308,10 @@ def test_binding_refuses_rotary_outputs_without_their_inputs():
     for name in "qkv":
         with pytest.raises(ValueError, match=f"{name}_out"):
             api.loki_rotary(lay, pos, f, **{name + "_out": t})
+
+
+def test_rotary_refuses_to_move_rows_in_place():
+    """A block that writes a token's row may not be another's that has yet to be read: in place only where it lies."""
+    call = lambda n, lay=_layout(), **kw: api.lib().loki_rotary(by(lay), n, by(_rotary_args(**kw)), None)
+    for kw in (dict(rows=P, n_rows=64), dict(k__out_token=512, k__out_head=1024), dict(q__out_batch=1 << 20), dict(v__out_head=256)):
+        assert call(4, **kw) == 1, kw
