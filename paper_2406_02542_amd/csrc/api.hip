@@ -700,7 +700,8 @@ int loki_rotary(const loki_layout* layout, int n_new, const loki_rotary_args* ar
   loki_layout L;
   if (!layout || !args) return LOKI_ERR_INVALID_ARG;
   L = *layout;
-  L.d_split = 128;  // not used
+  L.d_split = 128;  // not used, as the rows
+  L.S_cap = 1;
   int rc = check_layout(&L, &s);
   if (rc != LOKI_OK) return rc;
   if (n_new < 1 || (long long)n_new * s.B > (1 << 24)) return LOKI_ERR_INVALID_ARG;  // (a grid's threads are counted in 32 bits)

@@ -315,3 +315,9 @@ def test_rotary_refuses_to_move_rows_in_place():
     call = lambda n, lay=_layout(), **kw: api.lib().loki_rotary(by(lay), n, by(_rotary_args(**kw)), None)
     for kw in (dict(rows=P, n_rows=64), dict(k__out_token=512, k__out_head=1024), dict(q__out_batch=1 << 20), dict(v__out_head=256)):
         assert call(4, **kw) == 1, kw
+
+
+def test_rotary_uses_no_more_of_the_layout_than_it_says():
+    """The rows of a cache and its split are no concern of a call that may know of no cache: what is refused is what follows."""
+    for lay in (_layout(S_cap=0), _layout(S_cap=-1, d_split=0), _layout(d_split=200)):
+        assert api.lib().loki_rotary(by(lay), 4, by(_rotary_args(positions=P + 2)), None) == 3
