@@ -198,6 +198,12 @@ _current_device = getattr(torch._C, "_cuda_getDevice", None)
 _current_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
 
 
+def _on_current_device(t: torch.Tensor, name: str) -> None:
+    """Kernels run on the current device: one of another would read addresses that are not its own."""
+    if _current_device is not None and t.get_device() != _current_device():
+        raise ValueError(f"{name} must live on the current device ({_current_device()}), got {t.device}")
+
+
 def _stream_ptr(stream) -> int:
     if stream is not None:
         return stream.cuda_stream
@@ -474,6 +480,7 @@ def loki_rotary(layout: Layout, positions: torch.Tensor, frequencies: torch.Tens
         0 if rows is None else _ptr(rows, "rows", torch.int32, B * n),
         _ptr(frequencies, "frequencies", torch.float64, 1),
         n_rows, 2 * frequencies.numel(), interleaved, inverse, scale)
+    _on_current_device(positions, "positions")
     _check(lib().loki_rotary(ctypes.byref(layout), n, args, _stream_ptr(stream)), "loki_rotary")
 
 
@@ -492,9 +499,11 @@ def dense_decode_weights(layout: Layout, q: torch.Tensor, k_full: torch.Tensor, 
     dt = _torch_dtype(layout)
     rows = layout.B * layout.Hkv * layout.S_cap
     nq = layout.B * layout.Hq * layout.D
+    q_ptr = _ptr(q, "q", dt, nq)
+    _on_current_device(q, "q")
     _check(lib().dense_decode_weights(
         ctypes.byref(layout),
-        _ptr(q, "q", dt, nq),
+        q_ptr,
         _ptr(k_full, "k_full", dt, rows * layout.D),
         _ptr(v, "v", dt, rows * layout.D),
         S_max,
@@ -512,8 +521,8 @@ def loki_evict_workspace_bytes(layout: Layout, S_max: int, budget: int) -> int:
     return n.value
 
 
-def _same_rows(units: int, rows: int, *parts) -> None:
-    """Every part (name, tensor or None, width) of a cache holds exactly `rows` rows for each unit: one stride goes for all."""
+def _refuse_rows(units: int, rows: int, *parts) -> None:
+    """Every part (name, tensor or None, width) of a cache has to hold exactly `rows` rows for each unit: one stride goes for all."""
     for name, t, width in parts:
         if t is not None and t.numel() != units * rows * width:
             raise ValueError(f"{name} holds {t.numel()} elements, {rows} rows of {width} for {units} heads have {units * rows * width}")
@@ -536,8 +545,12 @@ def loki_evict(layout: Layout, weights: torch.Tensor, klo: torch.Tensor, khi: Op
     cache_rows = (n_pages * layout.Hkv * page_rows) if page_table is not None else units * layout.S_cap
     cap_out = klo_out.numel() // (units * d) if klo_out is not None else 0
     if klo_out is not None:
-        _same_rows(units, cap_out, ("klo_out", klo_out, d), ("khi_out", khi_out if d < D else None, D - d), ("v_out", v_out, D),
-                   ("weights_out", weights_out, 1))
+        rows = units * cap_out
+        if (klo_out.numel() != rows * d or (v_out is not None and v_out.numel() != rows * D) or
+                (weights_out is not None and weights_out.numel() != rows) or
+                (khi_out is not None and d < D and khi_out.numel() != rows * (D - d))):
+            _refuse_rows(units, cap_out, ("klo_out", klo_out, d), ("khi_out", khi_out if d < D else None, D - d), ("v_out", v_out, D),
+                         ("weights_out", weights_out, 1))
     args = _evict_pack(
         _ptr(seq_lens, "seq_lens", torch.int32, layout.B) or 0,
         _ptr(weights, "weights", torch.float32, units * layout.S_cap),
@@ -552,6 +565,7 @@ def loki_evict(layout: Layout, weights: torch.Tensor, klo: torch.Tensor, khi: Op
         _ptr(out_idx, "out_idx", torch.int32, units * budget) or 0,
         _ptr(page_table, "page_table", torch.int32, layout.B) or 0,
         cap_out, page_rows, (page_table.numel() // layout.B) if page_table is not None else 0, n_pages)
+    _on_current_device(weights, "weights")
     _check(lib().loki_evict(ctypes.byref(layout), args, S_max, budget, sinks, recent,
                             _ptr(workspace, "workspace", torch.uint8), workspace.numel(), _stream_ptr(stream)), "loki_evict")
 
@@ -574,10 +588,13 @@ def dense_decode_shared(layout: Layout, q: torch.Tensor, k_prefix: Optional[torc
     if (k_prefix is None) != (v_prefix is None):
         raise ValueError("k_prefix and v_prefix go together")
     cap = k_prefix.numel() // (H * D) if k_prefix is not None else 0
-    _same_rows(H, cap, ("k_prefix", k_prefix, D), ("v_prefix", v_prefix, D))
+    if k_prefix is not None and (k_prefix.numel() != H * cap * D or v_prefix.numel() != H * cap * D):
+        _refuse_rows(H, cap, ("k_prefix", k_prefix, D), ("v_prefix", v_prefix, D))
+    q_ptr = _ptr(q, "q", dt, nq)
+    _on_current_device(q, "q")
     _check(lib().dense_decode_shared(
         ctypes.byref(layout),
-        _ptr(q, "q", dt, nq),
+        q_ptr,
         _ptr(k_prefix, "k_prefix", dt, H * cap * D),
         _ptr(v_prefix, "v_prefix", dt, H * cap * D),
         prefix_rows, cap,

@@ -216,3 +216,22 @@ def test_totals_of_rows_appended_behind_an_eviction(dtype):
             api.loki_evict(lay, w, k, None, v, cap, budget, sinks, recent, ws, seq_lens=lens, lens_out=lens, out_idx=idx)
             total[:, :, :budget] = total.gather(2, idx.long())
     assert evictions >= 3
+
+
+def test_tensors_of_another_device_are_refused(monkeypatch):
+    """The kernels would be launched on the current device with addresses of another."""
+    lay = api.make_layout(1, 2, 2, 128, 128, 16, torch.float32)
+    t, w, ws = torch.zeros((1, 2, 16, 128), device="cuda"), torch.zeros((1, 2, 16), device="cuda"), torch.zeros(1 << 20, dtype=torch.uint8, device="cuda")
+    q, out = torch.zeros((1, 2, 128), device="cuda"), torch.full((1, 2, 128), 7.0, device="cuda")
+    pos, f = torch.zeros((1, 1), dtype=torch.int32, device="cuda"), torch.zeros(64, dtype=torch.float64, device="cuda")
+    stream = torch.cuda.current_stream()
+    monkeypatch.setattr(api, "_current_device", lambda: t.get_device() + 1)
+    for call in (lambda **kw: api.loki_rotary(lay, pos, f, q=q[:, None], q_out=out[:, None], **kw),
+                 lambda **kw: api.dense_decode_weights(lay, q, t, t, 16, None, None, w, ws, out, **kw),
+                 lambda **kw: api.loki_evict(lay, w, t, None, t, 16, 4, 0, 0, ws, **kw),
+                 lambda **kw: api.dense_decode_shared(lay, q, None, None, 0, t, t, 16, None, ws, out, **kw)):
+        for kw in ({}, dict(stream=stream)):
+            with pytest.raises(ValueError, match="current device"):
+                call(**kw)
+    torch.cuda.synchronize()
+    assert bool((out == 7.0).all())
