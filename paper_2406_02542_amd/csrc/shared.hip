@@ -4,8 +4,8 @@
 //
 // One launch of two kinds of blocks: a run of the prefix for a tile of query rows (below), and a run of a sequence's own rows
 // for its G heads (parts_impl.h).  Each leaves (max, sum, output) per query row, which weigh_merge_kernel joins.  Few
-// query rows: memory bounds it (16 of 32/8 heads behind 65536 rows: 268 MB in 43 us).  From about 200 on the
-// matrix cores do: the prefix is then read once by the chip for 4 M D operations a row.
+// query rows: memory bounds it (16 sequences of 32/8 heads behind 65536 rows: 268 MB, the call 57 us).  From about 120 on the
+// matrix cores do: the prefix is then read once by the chip for 6 M D operations a row.
 #include "parts_impl.h"
 
 namespace loki {
@@ -53,14 +53,14 @@ __device__ __forceinline__ void prefix_f32_body(char* smem, const PrefixAt& bloc
 // load meet in a bank (no conflict is counted).  Eight waves of 32 queries keep two on a SIMD, whose products and
 // exponentials overlap: four waves of 64 queries, each with the registers of a SIMD to itself, take 130 us where these take 113.
 // The weights enter the second product in two bf16 terms, as in the library's other attention over whole caches, and their sum in 32
-// bits: 2^-17 of each weight.  One term makes that product half as long, but is off by 2^-9 of each weight, which
+// bits: 2^-16 of each weight.  One term makes that product half as long, but is off by up to 2^-8 of each weight, which
 // outputs whose large rows cancel do not hide: then whole outputs are wrong by their own size (tests/test_gpu_weight_precision.py).
 // us in one / two terms, without rows of their own: 4 sequences of 32/8 heads behind 65536 rows 52.3 / 52.9, 16 of them 55.8 / 56.6, 32
 // 63.6 / 70.2, 64 of 64/8 behind 4096 29.9 / 33.2, 32768 84.6 / 104.2.
 // The reference of the exponentials follows the running maximum only when a step's weights sum up to more than 2^8: the
 // outputs are rescaled a few times per run instead of in most steps, weights up to 2^8 lose nothing, and neither the
 // maximum nor an exchange between lanes is needed in the other steps.
-// Measured: 64 sequences of 64/8 heads behind P rows, 14 us + 2.8 us per 1024 rows (0.77 PFLOP/s of the attention, 1.15 of products
+// Measured: 64 sequences of 64/8 heads behind P rows, 12 us + 2.9 us per 1024 rows (0.74 PFLOP/s of the attention, 1.1 of products
 // with the second term; a large product reaches 1.2 on this card): the constant part is a launch, the queries, 528 bytes per query
 // row and run written, and their merge.  In one term, of the 46 us of 24576 such rows, the products alone, on operands that do not
 // change, took 20, with the LDS reads 38, with the exponentials but no reads 42; halves of the waves a phase apart by barriers,
@@ -391,8 +391,8 @@ constexpr double kOneLaunchBytes = 24e6;
 static double own_bytes(const Shape& s, int rows) { return (double)s.B * s.Hkv * rows * (2 * kD * s.elem_bytes); }
 static bool in_one_launch(const Shape& s) { return own_bytes(s, s.S) < kOneLaunchBytes; }
 
-// Runs of a sequence's own rows in that one launch: two steps for every wave in bf16, one in fp32 (8 sequences of 32/8 bf16 heads with
-// 300 rows behind 2048: one step 14.0 us, two 11.8; 5 of 16/8 fp32 heads with 131 behind 5777 16.1, 17.1).
+// Runs of a sequence's own rows in that one launch: 64 rows for every wave in bf16, 32 in fp32 (with 32 and 64, 8 sequences of 32/8 bf16
+// heads with 300 rows behind 2048 14.0 and 11.8 us, 5 of 16/8 fp32 heads with 131 behind 5777 16.1 and 17.1).
 static int one_launch_splits(const Shape& s, int own_rows) {
   const int units = s.B * s.Hkv, waves = s.dtype == 0 || prefix_shape(s).queries == 32 ? 4 : 8;
   int n = ((s.dtype == 0 ? 8 : 24 / waves) * device_cus() + units - 1) / units;

@@ -152,13 +152,15 @@ __global__ __launch_bounds__(kMgThreads) void weigh_merge_kernel(const float* __
   }
 }
 
-// Runs of a sequence, at most as many as leave each wave two steps (bf16: 128 rows on the matrix cores) or 64 rows.
+// Runs of a sequence, at most as many as leave each of a block's four waves a step of 32 rows (bf16 on the matrix cores) or 16 rows.
 // Matrix cores: two blocks per CU, as many as are resident, where a sequence then has six runs and more, else four, which even
 // out lengths better.  us with 2, 4, 8 per CU, bf16: one of 32/8 heads, 20000 rows 20.9, 25.0, 26.7, 10 of 32/4 up to 9000 28.9, 32.0, 40.1,
 // 20 of 32/4 up to 5000 31.5, 34.5, 42.4, 16 of 32/8 up to 16384 149, 141, 142, 24 up to 7000 94.0, 90.7, 93.6, 50 up to 2500 80.5, 74.0, 75.9
 // (but 64 of 64/8, all of 600 40.5, 44.5, 53.2); fp32: 13 of 32/8 up to 3000 48.7, 48.0, 50.5.
-// Vector units: four per CU in bf16, eight in fp32 (5 sequences of 24 fp32 heads up to 2311 rows with 2, 4, 6, 8 and 12 per CU
-// 43.5, 41.2, 38.4, 38.3, 38.8; one of 24 bf16 heads, 8192 rows, with 2, 3, 4 25.9, 23.1, 24.6).
+// Vector units: eight per CU in fp32 (5 sequences of 24 fp32 heads up to 2311 rows with 2, 4, 6, 8 and 12 per CU 43.5, 41.2, 38.4,
+// 38.3, 38.8), four in bf16, where no count is best for all.  With 2, 3 and 4: 40 of 16 heads up to 2000 rows 81.4, 74.0, 74.1, 7 of 24 up to
+// 3000 42.2, 38.4, 37.8; 16 of 32 with 4096 178, 182, 182, up to 4096 131, 134, 134; 4 of 32/16 with 4096 27.8, 30.0, 28.2, 9 up to 5000
+// 56.4, 61.4, 59.3; 4 of 32 up to 4096 42.5, 45.5, 48.2; one of 32 with 8192 27.4, 27.5, 31.0, of 24 22.2, 22.2, 22.2.
 int weigh_splits(const Shape& s) {
   const int units = s.B * s.Hkv, slots = 2 * device_cus();
   const bool mfma = s.G >= 4;
