@@ -426,6 +426,79 @@ int dense_decode_shared(const loki_layout* layout, const void* q, const void* k_
                         size_t workspace_bytes, void* out, void* stream);
 
 /*
+ * A cache held whole: keys as the decode calls without a basis take them, and values.
+ *   k, v        rows of D elements of the storage type, [B, Hkv, S_cap, D] or, on pages, [n_pages, Hkv, page_rows, D]
+ *   k_scales, v_scales  NULL, or both: the cache is in 4 bits.  k and v are then rows of 16 words of 32 bits (in place of D), the scales rows
+ *               [4][2] of fp16: (step, lowest) of the row's columns 32 g .. 32 g + 31, g < 4.  With lowest = fp16(the smallest of the
+ *               group) and step = fp16((largest - smallest) / 15) the code of x is (x - lowest) / step rounded to nearest, ties to even,
+ *               within 0 .. 15 (step 0: 0) and stands for lowest + code * step: within half a step of x, plus what fp16 leaves
+ *               of lowest (2^-11 of it) and 15 of step (2^-11 of the range).  Word m holds columns 32 g + 2 m (bits 4 g ..) and 32 g + 2 m + 1
+ *               (bits 16 + 4 g ..).  160 bytes a row of keys and values; bf16 has 512.  Values beyond 65504 are held as if they were that.
+ *   page_table  NULL, or device int32 [B, pages_per_seq]: row s of sequence b lies in page page_table[b, s / page_rows] at row
+ *               s % page_rows.  page_rows: a power of two >= 16 (256 where loki_decode_step or loki_evict take the pools too);
+ *               pages_per_seq * page_rows >= S_cap; n_pages * Hkv * page_rows < 2^31
+ */
+typedef struct {
+  void* k;
+  void* v;
+  void* k_scales;
+  void* v_scales;
+  const int32_t* page_table;
+  int32_t page_rows;
+  int32_t pages_per_seq;
+  int32_t n_pages;
+} loki_cache;
+
+/*
+ * Keys and values of new tokens into such a cache, in the storage type or in 4 bits, the keys turned by their positions on
+ * the way, and the queries of the same tokens beside them, in one launch.  The members of args mean what they mean in loki_rotary, but
+ *   k, v      both there; their `out` are NULL and its strides not used: token j's go to row args->rows[b, j] of sequence b
+ *   q         may be missing
+ *   rows      device int32 [B, n_new]; a row outside [0, S_cap) or whose page entry is outside [0, n_pages) is not written (padded
+ *             tokens, pages not there yet).  Two tokens must not share a row (nor two sequences a page that both write)
+ *   rotary_dims  0: nothing is turned, positions and frequencies are not used, queries and keys are carried over as they are
+ *   n_rows    not used
+ * In 4 bits the turned fp32 key is rounded once, to its code.
+ */
+int loki_append(const loki_layout* layout, const loki_cache* cache, int n_new, const loki_rotary_args* args, void* stream);
+
+/*
+ * Rows of such a cache as tensors: row rows[b, j] of sequence b to k_out and v_out [B, Hkv, n, D] (storage type; either may be NULL).
+ * In 4 bits the values that the codes stand for, rounded once.  Where rows[b, j] is outside [0, S_cap) or its page entry outside
+ * [0, n_pages) nothing is written.  B n <= 2^24, B n Hkv <= 2^27.
+ */
+int loki_read_rows(const loki_layout* layout, const loki_cache* cache, int n, const int32_t* rows, void* k_out, void* v_out,
+                   void* stream);
+
+/*
+ * Attention over such a cache, for one or several tokens of every sequence, each over all of its rows or over the last ones and the
+ * first few: a token that sees L rows, itself in row L - 1, attends over the rows s < L with
+ *     s < sinks  or  s >= L - window            (window 0: all rows, and sinks is not used)
+ *     out = softmax(q K^T / sqrt(D)) V          over them; L = 0: zeros.
+ *   q, out      [B, m, Hq, D], m = queries_per_seq (0 or 1: one)
+ *   seq_lens    device int32 [B, m], 0 <= seq_lens[b, j] <= S_max (clamped): L of token j, 0 for a padded one.  NULL: S_max - (m - 1 - j),
+ *               at least 0.  The tokens of a sequence are expected next to each other, in their order: rows are read from the shortest's
+ *               window on to the longest's end (for up to 256 query rows of a KV head at a time)
+ *   S_max       1 <= S_max <= min(S_cap, 2^30)
+ *   window, sinks  >= 0
+ *   workspace   >= dense_cache_workspace_bytes(layout, cache, S_max, args), 256-byte aligned; a workspace sized for an S_max also
+ *               serves shorter ones, with the same args
+ * Rows that no token sees, before the window or behind the end, are not read, and their pages' entries may be any (entries that are
+ * read are clamped into [0, n_pages)).  m may be thousands (a chunk of prompts): B m <= 2^24, B m Hq <= 2^27.
+ */
+typedef struct {
+  const int32_t* seq_lens;
+  int32_t queries_per_seq;
+  int32_t window;
+  int32_t sinks;
+} loki_span_args;
+
+int dense_cache_workspace_bytes(const loki_layout* layout, const loki_cache* cache, int S_max, const loki_span_args* args,
+                                size_t* bytes);
+int dense_decode_cache(const loki_layout* layout, const void* q, const loki_cache* cache, int S_max, const loki_span_args* args,
+                       void* workspace, size_t workspace_bytes, void* out, void* stream);
+
+/*
  * Appendix E, Algorithm 2 (PCAAttn, the variant the paper tried and set aside): the
  * attention weights come from the first d rotated columns alone, over all S rows,
  *   out = softmax(qhat[:d] Klo^T / sqrt(D)) V,

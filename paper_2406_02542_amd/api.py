@@ -59,6 +59,17 @@ class EvictArgs(ctypes.Structure):
         (n, ctypes.c_int32) for n in ("S_cap_out", "page_rows", "pages_per_seq", "n_pages")]
 
 
+class CacheArgs(ctypes.Structure):
+    """Mirror of ``loki_cache``."""
+    _fields_ = [(n, ctypes.c_void_p) for n in ("k", "v", "k_scales", "v_scales", "page_table")] + [
+        (n, ctypes.c_int32) for n in ("page_rows", "pages_per_seq", "n_pages")]
+
+
+class SpanArgs(ctypes.Structure):
+    """Mirror of ``loki_span_args``."""
+    _fields_ = [("seq_lens", ctypes.c_void_p)] + [(n, ctypes.c_int32) for n in ("queries_per_seq", "window", "sinks")]
+
+
 _lib = None
 
 
@@ -123,6 +134,15 @@ def lib() -> ctypes.CDLL:
     L.dense_shared_workspace_bytes.argtypes = [LP, i32, i32, ctypes.POINTER(sz)]
     L.dense_decode_shared.restype = i32
     L.dense_decode_shared.argtypes = [LP, vp, vp, vp, i32, i32, vp, vp, i32, vp, vp, sz, vp, vp]
+    CP, SP = ctypes.POINTER(CacheArgs), ctypes.POINTER(SpanArgs)
+    L.loki_append.restype = i32
+    L.loki_append.argtypes = [LP, CP, i32, vp, vp]
+    L.loki_read_rows.restype = i32
+    L.loki_read_rows.argtypes = [LP, CP, i32, vp, vp, vp, vp]
+    L.dense_cache_workspace_bytes.restype = i32
+    L.dense_cache_workspace_bytes.argtypes = [LP, CP, i32, SP, ctypes.POINTER(sz)]
+    L.dense_decode_cache.restype = i32
+    L.dense_decode_cache.argtypes = [LP, vp, CP, i32, SP, vp, sz, vp, vp]
     L.dense_decode_attn.restype = i32
     L.dense_decode_attn.argtypes = [LP, vp, vp, vp, i32, vp, sz, vp, vp]
     L.loki_profile_create.restype = i32
@@ -740,3 +760,138 @@ class Profile:
             self.close()
         except Exception:
             pass
+
+
+class Cache:
+    """A cache held whole (``loki_cache``), checked once and kept with its tensors: ``k``, ``v`` [B, Hkv, S_cap, 128] of the
+    layout's type or, with ``page_table`` [B, pages_per_seq] (int32), pools [n_pages, Hkv, page_rows, 128]; in 4 bits int32
+    [.., 16] with ``k_scales``, ``v_scales`` fp16 [.., 4, 2].  See ``alloc_whole_cache``."""
+
+    def __init__(self, layout: Layout, k: torch.Tensor, v: torch.Tensor, k_scales: Optional[torch.Tensor] = None,
+                 v_scales: Optional[torch.Tensor] = None, page_table: Optional[torch.Tensor] = None):
+        if (k_scales is None) != (v_scales is None):
+            raise ValueError("k_scales and v_scales come together")
+        dt, tail = (_torch_dtype(layout), (128,)) if k_scales is None else (torch.int32, (16,))
+        B, H = layout.B, layout.Hkv
+        pages = rows = per_seq = 0
+        if page_table is not None:
+            if page_table.dim() != 2 or page_table.shape[0] != B:
+                raise ValueError(f"page_table must be [{B}, pages_per_seq], got {tuple(page_table.shape)}")
+            if k.dim() != 4:
+                raise ValueError(f"k must be [n_pages, {H}, page_rows, {tail[0]}], got {tuple(k.shape)}")
+            (pages, rows), per_seq = (k.shape[0], k.shape[2]), page_table.shape[1]
+        shape = (pages, H, rows) if page_table is not None else (B, H, layout.S_cap)
+        parts = [("k", k, dt, shape + tail), ("v", v, dt, shape + tail)]
+        if k_scales is not None:
+            parts += [(n, t, torch.float16, shape + (4, 2)) for n, t in (("k_scales", k_scales), ("v_scales", v_scales))]
+        for name, t, want, size in parts:
+            if t.shape != size:
+                raise ValueError(f"{name} must be {list(size)}, got {tuple(t.shape)}")
+            _ptr(t, name, want)
+            if t.get_device() != k.get_device():
+                raise ValueError(f"{name} and k must live on the same device")
+        self.tensors = (k, v, k_scales, v_scales, page_table)
+        self.k = k
+        self.args = CacheArgs(k.data_ptr(), v.data_ptr(), None if k_scales is None else k_scales.data_ptr(),
+                              None if v_scales is None else v_scales.data_ptr(), _ptr(page_table, "page_table", torch.int32),
+                              rows, per_seq, pages)
+        self.shape = (B, H, layout.S_cap, layout.dtype)
+
+    def _of(self, layout: Layout):
+        if self.shape != (layout.B, layout.Hkv, layout.S_cap, layout.dtype):
+            raise ValueError(f"the cache is one of (B, Hkv, S_cap, dtype) = {self.shape}")
+        _on_current_device(self.k, "cache")
+        return ctypes.byref(self.args)
+
+
+def alloc_whole_cache(layout: Layout, four_bits: bool = False, page_table: Optional[torch.Tensor] = None, page_rows: int = 0,
+                      n_pages: int = 0, device="cuda") -> Cache:
+    """A ``Cache`` of the layout (zero-filled), contiguous or as pools of ``n_pages`` pages."""
+    lead = (layout.B, layout.Hkv, layout.S_cap) if page_table is None else (n_pages, layout.Hkv, page_rows)
+    make = lambda tail, dt: torch.zeros(lead + tail, dtype=dt, device=device)
+    if not four_bits:
+        return Cache(layout, make((128,), _torch_dtype(layout)), make((128,), _torch_dtype(layout)), page_table=page_table)
+    return Cache(layout, make((16,), torch.int32), make((16,), torch.int32), make((4, 2), torch.float16),
+                 make((4, 2), torch.float16), page_table=page_table)
+
+
+def _strided(name: str, x: torch.Tensor, shape, dt: torch.dtype):
+    """(pointer, three strides) of x [B, n, heads, D], rows of whole columns."""
+    if not x.is_cuda:
+        raise ValueError(f"{name} must live on the GPU")
+    if x.dtype is not dt or x.shape != shape:
+        raise ValueError(f"{name} must be {list(shape)} of {dt}, got {tuple(x.shape)} of {x.dtype}")
+    b, t, h, c = x.stride()
+    if c != 1:
+        raise ValueError(f"{name}: the columns of a row must be next to each other")
+    return x.data_ptr(), b, t, h
+
+
+def loki_append(layout: Layout, cache: Cache, rows: torch.Tensor, k: torch.Tensor, v: torch.Tensor,
+                positions: Optional[torch.Tensor] = None, frequencies: Optional[torch.Tensor] = None,
+                q: Optional[torch.Tensor] = None, q_out: Optional[torch.Tensor] = None, interleaved: bool = False,
+                inverse: bool = False, scale: float = 1.0, stream=None) -> None:
+    """Tokens' ``k``, ``v`` [B, n, Hkv, D] (any strides of whole rows) into the rows ``rows`` [B, n] of the cache, ``k`` and ``q``
+    [B, n, Hq, D] turned by ``positions`` [B, n] (as ``loki_rotary``; without ``frequencies`` nothing is turned)."""
+    if rows.dim() != 2 or rows.shape[0] != layout.B:
+        raise ValueError(f"rows must be [{layout.B}, n], got {tuple(rows.shape)}")
+    B, n = rows.shape
+    dt = _torch_dtype(layout)
+    if (q is None) != (q_out is None):
+        raise ValueError("q and q_out come together")
+    if (positions is None) != (frequencies is None):
+        raise ValueError("positions and frequencies come together")
+    shape = (B, n, layout.Hkv, 128)
+    kp, vp = _strided("k", k, shape, dt), _strided("v", v, shape, dt)
+    qs = _NOT_THERE
+    if q is not None:
+        q_shape = (B, n, layout.Hq, 128)
+        qi, qo = _strided("q", q, q_shape, dt), _strided("q_out", q_out, q_shape, dt)
+        qs = (qi[0], qo[0]) + qi[1:] + qo[1:]
+    pos = freq = R = 0
+    if frequencies is not None:
+        pos, freq = _ptr(positions, "positions", torch.int32, B * n), _ptr(frequencies, "frequencies", torch.float64, 1)
+        R = 2 * frequencies.numel()
+    args = _rotary_pack(*qs, kp[0], 0, *kp[1:], 0, 0, 0, vp[0], 0, *vp[1:], 0, 0, 0, pos, _ptr(rows, "rows", torch.int32), freq,
+                        0, R, interleaved, inverse, scale)
+    cache_args = cache._of(layout)
+    _on_current_device(rows, "rows")
+    _check(lib().loki_append(ctypes.byref(layout), cache_args, n, args, _stream_ptr(stream)), "loki_append")
+
+
+def loki_read_rows(layout: Layout, cache: Cache, rows: torch.Tensor, k_out: Optional[torch.Tensor] = None,
+                   v_out: Optional[torch.Tensor] = None, stream=None) -> None:
+    """Rows ``rows`` [B, n] of the cache to ``k_out``, ``v_out`` [B, Hkv, n, D]."""
+    if rows.dim() != 2 or rows.shape[0] != layout.B:
+        raise ValueError(f"rows must be [{layout.B}, n], got {tuple(rows.shape)}")
+    n = rows.shape[1]
+    dt, need = _torch_dtype(layout), layout.B * layout.Hkv * n * 128
+    cache_args = cache._of(layout)
+    _on_current_device(rows, "rows")
+    _check(lib().loki_read_rows(ctypes.byref(layout), cache_args, n, _ptr(rows, "rows", torch.int32), _ptr(k_out, "k_out", dt, need),
+                                _ptr(v_out, "v_out", dt, need), _stream_ptr(stream)), "loki_read_rows")
+
+
+def dense_cache_workspace_bytes(layout: Layout, cache: Cache, S_max: int, queries_per_seq: int = 1, window: int = 0, sinks: int = 0) -> int:
+    n = ctypes.c_size_t()
+    args = SpanArgs(None, queries_per_seq, window, sinks)
+    _check(lib().dense_cache_workspace_bytes(ctypes.byref(layout), cache._of(layout), S_max, ctypes.byref(args), ctypes.byref(n)),
+           "dense_cache_workspace_bytes")
+    return n.value
+
+
+def dense_decode_cache(layout: Layout, cache: Cache, q: torch.Tensor, S_max: int, workspace: torch.Tensor, out: torch.Tensor,
+                       seq_lens: Optional[torch.Tensor] = None, queries_per_seq: int = 1, window: int = 0, sinks: int = 0,
+                       stream=None) -> None:
+    """Attention of ``q`` [B, m, Hq, D] over the cache's rows, or with ``window`` over the last of them and the first ``sinks``;
+    ``seq_lens`` [B, m] (int32): the rows that every token sees, itself the last, 0 for a padded one."""
+    dt = _torch_dtype(layout)
+    m = max(1, queries_per_seq)
+    nq = layout.B * m * layout.Hq * layout.D
+    args = SpanArgs(_ptr(seq_lens, "seq_lens", torch.int32, layout.B * m), queries_per_seq, window, sinks)
+    cache_args = cache._of(layout)
+    q_ptr = _ptr(q, "q", dt, nq)
+    _on_current_device(q, "q")
+    _check(lib().dense_decode_cache(ctypes.byref(layout), q_ptr, cache_args, S_max, ctypes.byref(args),
+                                    _ptr(workspace, "workspace", torch.uint8), workspace.numel(), _ptr(out, "out", dt, nq),
+                                    _stream_ptr(stream)), "dense_decode_cache")

@@ -393,11 +393,11 @@ int loki_workspace_bytes(const loki_layout* layout, int S, int d, int k, int sel
 }
 
 static int paging_from_args(const int32_t* page_table, int page_rows, int pages_per_seq, int n_pages,
-                            int Hkv, long long rows_needed, Paging* pg) {
+                            int Hkv, long long rows_needed, Paging* pg, int least_lg = 8) {
   int lg = 0;
   while (lg < 31 && (1 << lg) < page_rows) ++lg;
   if (page_rows < 1 || (1 << lg) != page_rows) return LOKI_ERR_INVALID_ARG;
-  if (lg < 8 || lg > 24 || pages_per_seq < 1 || n_pages < 1) return LOKI_ERR_INVALID_ARG;
+  if (lg < least_lg || lg > 24 || pages_per_seq < 1 || n_pages < 1) return LOKI_ERR_INVALID_ARG;
   if ((long long)pages_per_seq * page_rows < rows_needed) return LOKI_ERR_INVALID_ARG;
   if ((long long)n_pages * Hkv * page_rows > 0x7fffffffLL) return LOKI_ERR_UNSUPPORTED;
   if (reinterpret_cast<uintptr_t>(page_table) & 3u) return LOKI_ERR_ALIGNMENT;
@@ -972,6 +972,124 @@ int dense_decode_shared(const loki_layout* layout, const void* q, const void* k_
   if (e != hipSuccess) return LOKI_ERR_HIP;
   tm.begin("merge");
   e = launch_weigh_merge(s, nsplit, shared, w.partial, w.prefix, nullptr, nullptr, nullptr, out, st);
+  tm.end();
+  return e == hipSuccess ? LOKI_OK : LOKI_ERR_HIP;
+}
+
+// ---- caches held whole ----------------------------------------------------------------------------
+static int check_cache(const loki_layout* layout, const loki_cache* cache, Shape* s, CacheView* c) {
+  int rc = check_dense_layout(layout, s);
+  if (rc != LOKI_OK) return rc;
+  if (!cache || !cache->k || !cache->v || !cache->k_scales != !cache->v_scales) return LOKI_ERR_INVALID_ARG;
+  if (!aligned16(cache->k) || !aligned16(cache->v) || !aligned16(cache->k_scales) || !aligned16(cache->v_scales)) return LOKI_ERR_ALIGNMENT;
+  *c = CacheView{cache->k, cache->v, cache->k_scales, cache->v_scales, Paging{}, s->S_cap};
+  if (!cache->page_table) return LOKI_OK;
+  return paging_from_args(cache->page_table, cache->page_rows, cache->pages_per_seq, cache->n_pages, s->Hkv, s->S_cap, &c->pg, 4);
+}
+
+int loki_append(const loki_layout* layout, const loki_cache* cache, int n_new, const loki_rotary_args* args, void* stream) {
+  Shape s;
+  AppendArgs a{};
+  int rc = check_cache(layout, cache, &s, &a.cache);
+  if (rc != LOKI_OK) return rc;
+  if (!args || n_new < 1 || (long long)n_new * s.B > (1 << 24)) return LOKI_ERR_INVALID_ARG;  // (a grid's threads are counted in 32 bits)
+  if (!args->k.in || !args->v.in || args->k.out || args->v.out || !args->rows) return LOKI_ERR_INVALID_ARG;
+  if (args->rotary_dims < 0 || args->rotary_dims > 128 || args->rotary_dims % 2 != 0) return LOKI_ERR_INVALID_ARG;
+  if (args->rotary_dims > 0 && (!args->positions || !args->frequencies)) return LOKI_ERR_INVALID_ARG;
+  if ((reinterpret_cast<uintptr_t>(args->positions) & 3u) || (reinterpret_cast<uintptr_t>(args->rows) & 3u) ||
+      (reinterpret_cast<uintptr_t>(args->frequencies) & 7u))
+    return LOKI_ERR_ALIGNMENT;
+  const int epc = 16 / s.elem_bytes;
+  if ((rc = rotary_tensor(args->q, s.B, n_new, s.Hq, epc, false, &a.r.q)) != LOKI_OK) return rc;
+  for (int i = 0; i < 2; ++i) {  // to the cache: only where they come from is the caller's
+    loki_rotary_tensor x = i ? args->v : args->k;
+    x.out = i ? cache->v : cache->k;
+    x.out_batch = x.out_token = x.out_head = 0;
+    if ((rc = rotary_tensor(x, s.B, n_new, s.Hkv, epc, true, i ? &a.r.v : &a.r.k)) != LOKI_OK) return rc;
+  }
+  a.r.positions = args->positions;
+  a.r.rows = args->rows;
+  a.r.freqs = args->frequencies;
+  a.r.n = n_new;
+  a.r.total = n_new * s.B;
+  a.r.R = args->rotary_dims;
+  a.r.interleaved = args->interleaved != 0;
+  a.r.inverse = args->inverse != 0;
+  a.r.scale = args->scale;
+  hipStream_t st = static_cast<hipStream_t>(stream);
+  StageTimer tm(st);
+  tm.begin("append");
+  const hipError_t e = launch_append(s, a, st);
+  tm.end();
+  return e == hipSuccess ? LOKI_OK : LOKI_ERR_HIP;
+}
+
+int loki_read_rows(const loki_layout* layout, const loki_cache* cache, int n, const int32_t* rows, void* k_out, void* v_out, void* stream) {
+  Shape s;
+  CacheView c{};
+  const int rc = check_cache(layout, cache, &s, &c);
+  if (rc != LOKI_OK) return rc;
+  if (!rows || (!k_out && !v_out) || n < 1 || (long long)n * s.B > (1 << 24) || (long long)n * s.B * s.Hkv > (1 << 27)) return LOKI_ERR_INVALID_ARG;
+  if (!aligned16(k_out) || !aligned16(v_out) || (reinterpret_cast<uintptr_t>(rows) & 3u)) return LOKI_ERR_ALIGNMENT;
+  hipStream_t st = static_cast<hipStream_t>(stream);
+  StageTimer tm(st);
+  tm.begin("read_rows");
+  const hipError_t e = launch_read_rows(s, c, rows, n, k_out, v_out, st);
+  tm.end();
+  return e == hipSuccess ? LOKI_OK : LOKI_ERR_HIP;
+}
+
+static int check_span(const loki_layout* layout, const loki_cache* cache, int S_max, const loki_span_args* args, Shape* s, SpanArgs* a) {
+  const int rc = check_cache(layout, cache, s, &a->cache);
+  if (rc != LOKI_OK) return rc;
+  if (!args || S_max < 1 || S_max > s->S_cap || S_max > kMostRows) return LOKI_ERR_INVALID_ARG;
+  if (args->queries_per_seq < 0 || args->window < 0 || args->sinks < 0) return LOKI_ERR_INVALID_ARG;
+  a->m = args->queries_per_seq > 0 ? args->queries_per_seq : 1;
+  if ((long long)a->m * s->B > (1 << 24) || (long long)a->m * s->B * s->Hq > (1 << 27)) return LOKI_ERR_INVALID_ARG;
+  if (reinterpret_cast<uintptr_t>(args->seq_lens) & 3u) return LOKI_ERR_ALIGNMENT;
+  s->S = S_max;
+  a->lens = args->seq_lens;
+  a->B = s->B;
+  a->G = s->G;
+  a->Hq = s->Hq;
+  a->Hkv = s->Hkv;
+  a->S_max = S_max;
+  a->window = args->window;
+  a->sinks = args->sinks;
+  return LOKI_OK;
+}
+// Behind the control words, which the call leaves alone (plan_workspace): the parts, where there are any.
+static size_t span_bytes(const Shape& s, const SpanArgs& a, const SpanPlan& plan) {
+  const size_t parts = plan.nsplit > 1 ? (size_t)a.B * a.m * a.Hq * plan.nsplit * kPartStride * sizeof(float) : 0;
+  return kClusterCtlBytes + align_up(parts, 256);
+}
+
+int dense_cache_workspace_bytes(const loki_layout* layout, const loki_cache* cache, int S_max, const loki_span_args* args, size_t* bytes) {
+  Shape s;
+  SpanArgs a{};
+  const int rc = check_span(layout, cache, S_max, args, &s, &a);
+  if (rc != LOKI_OK) return rc;
+  if (!bytes) return LOKI_ERR_INVALID_ARG;
+  *bytes = span_bytes(s, a, span_plan(s, a.m, a.window, a.sinks, a.cache.k_scales != nullptr));
+  return LOKI_OK;
+}
+
+int dense_decode_cache(const loki_layout* layout, const void* q, const loki_cache* cache, int S_max, const loki_span_args* args,
+                       void* workspace, size_t workspace_bytes, void* out, void* stream) {
+  Shape s;
+  SpanArgs a{};
+  const int rc = check_span(layout, cache, S_max, args, &s, &a);
+  if (rc != LOKI_OK) return rc;
+  if (!q || !out || !workspace) return LOKI_ERR_INVALID_ARG;
+  if (!aligned16(q) || !aligned16(out) || !aligned256(workspace)) return LOKI_ERR_ALIGNMENT;
+  if (span_bytes(s, a, span_plan(s, a.m, a.window, a.sinks, a.cache.k_scales != nullptr)) > workspace_bytes) return LOKI_ERR_WORKSPACE;
+  a.q = q;
+  a.out = out;
+  a.partial = reinterpret_cast<float*>(static_cast<char*>(workspace) + kClusterCtlBytes);
+  hipStream_t st = static_cast<hipStream_t>(stream);
+  StageTimer tm(st);
+  tm.begin("cache_attend");
+  const hipError_t e = launch_span(s, a, st);
   tm.end();
   return e == hipSuccess ? LOKI_OK : LOKI_ERR_HIP;
 }

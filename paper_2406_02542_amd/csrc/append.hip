@@ -1,0 +1,274 @@
+// Keys and values of new tokens into a cache held whole, contiguous or on pages, in the storage type or in 4 bits, the keys and the
+// queries beside them turned by their positions on the way (in front of Algorithm 1 line 2 of arXiv 2406.02542); and rows of such a
+// cache back.
+//
+// The rotation is that of rotary.hip, and so is the split: a block owns a few tokens (or some heads of one), works their angles
+// out once, into LDS, and lane groups take heads of one token in turn.  Memory bounds it.
+// In 4 bits the turned row goes through LDS in 32 bits, from the lanes that hold pairs to the lanes that hold words, and is rounded
+// once, to its code.
+#include "cache_impl.h"
+#include "rotary_impl.h"
+
+namespace loki {
+
+constexpr int kApThreads = 256;
+constexpr int kApMaxTokens = 4;  // of a block: one angle per thread with 64 pairs
+
+// Where a token's row goes, from the start of the pool of head 0, and the rows between two heads'; not there: first < 0.
+struct RowTarget {
+  long long first, between;
+};
+__device__ __forceinline__ RowTarget row_target(const CacheView& c, int b, int Hkv, int row) {
+  if (row < 0 || row >= c.S_cap) return {-1, 0};
+  if (c.pg.table == nullptr) return {(long long)b * Hkv * c.S_cap + row, c.S_cap};
+  const int page = c.pg.table[(long long)b * c.pg.pages_per_seq + (row >> c.pg.lg_rows)];
+  if (page < 0 || page >= c.pg.n_pages) return {-1, 0};
+  return {(((long long)page * Hkv) << c.pg.lg_rows) + (row & ((1 << c.pg.lg_rows) - 1)), 1LL << c.pg.lg_rows};
+}
+
+// Code of x: the quotient is rounded as IEEE division has it, so values half-way between two codes go to the even one.
+__device__ __forceinline__ uint32_t q4_code(float x, float low, float step) {
+  const float n = step > 0.f ? rintf((x - low) / step) : 0.f;
+  return (uint32_t)fminf(fmaxf(n, 0.f), 15.f);
+}
+
+// The row in `row` (LDS, 128 floats, complete) as codes and scales, by the LANES lanes of a group; p: the lane's number.
+template <int LANES>
+__device__ __forceinline__ void store_q4(const float* row, int p, uint32_t* codes, uint32_t* scales) {
+  constexpr int W = kQ4Words / LANES;
+  float2 x[W][kQ4Groups];
+  uint32_t word[W] = {};
+#pragma unroll
+  for (int w = 0; w < W; ++w)
+#pragma unroll
+    for (int g = 0; g < kQ4Groups; ++g) x[w][g] = *reinterpret_cast<const float2*>(row + 32 * g + 2 * (W * p + w));
+#pragma unroll
+  for (int g = 0; g < kQ4Groups; ++g) {
+    float lo = x[0][g].x, hi = lo;
+#pragma unroll
+    for (int w = 0; w < W; ++w) {
+      lo = fminf(lo, fminf(x[w][g].x, x[w][g].y));
+      hi = fmaxf(hi, fmaxf(x[w][g].x, x[w][g].y));
+    }
+    lo = -group_allreduce_max<LANES>(-lo);
+    hi = group_allreduce_max<LANES>(hi);
+    // (a range past fp16's is clamped to its largest)
+    const cache_half2_t sc = {(_Float16)fminf((hi - lo) / 15.f, 65504.f), (_Float16)fminf(fmaxf(lo, -65504.f), 65504.f)};
+    const float step = (float)sc.x, low = (float)sc.y;
+#pragma unroll
+    for (int w = 0; w < W; ++w) word[w] |= q4_code(x[w][g].x, low, step) << (4 * g) | q4_code(x[w][g].y, low, step) << (16 + 4 * g);
+    if (p == g) scales[g] = __builtin_bit_cast(uint32_t, sc);
+  }
+#pragma unroll
+  for (int w = 0; w < W; ++w) codes[W * p + w] = word[w];
+}
+
+// STYLE as rotary_kernel's.
+template <typename T, int STYLE, bool BITS4>
+__global__ __launch_bounds__(kApThreads) void append_kernel(AppendArgs args) {
+  using ST = typename T::store_t;
+  constexpr int EPC = T::EPC;
+  constexpr int kLanes = kD / EPC / 2;  // lanes of a row: two chunks each
+  constexpr int kGroups = kApThreads / kLanes;
+  constexpr int U = BITS4 ? 2 : 4;  // rows of a lane group in flight
+  const RotaryArgs& a = args.r;
+  __shared__ float2 s_cs[kApMaxTokens][kD / 2];
+  __shared__ __align__(16) float s_row[BITS4 ? kGroups : 1][kD + 4];
+  const int tid = threadIdx.x, p = tid % kLanes, gid = tid / kLanes;
+  const int pairs = a.R / 2, tok0 = blockIdx.x * a.tokens, ntok = min(a.tokens, a.total - tok0);
+  // this lane group's token, and its heads h0 + first, h0 + first + step, ..
+  const int mine = gid & (a.tokens - 1), first = gid / a.tokens, step = kGroups / a.tokens;
+  const int Hkv = a.k.heads, heads = a.q.heads + 2 * Hkv;
+  const int h0 = blockIdx.y * a.heads_per_block, h1 = min(h0 + a.heads_per_block, heads);
+  const int t = tok0 + min(mine, ntok - 1), b = t / a.n, j = t - b * a.n;
+  const RowTarget to = row_target(args.cache, b, Hkv, a.rows[t]);
+
+  for (int i = tid; i < ntok * pairs; i += kApThreads) {
+    const int u = i / pairs, f = i - u * pairs;
+    const double quarters = (double)a.positions[tok0 + u] * (a.freqs[f] * 0.63661977236758134308);  // 2 / pi
+    float2 cs = cos_sin_quarters(quarters);
+    cs.x *= a.scale;
+    cs.y *= a.inverse ? -a.scale : a.scale;
+    s_cs[u][f] = cs;
+  }
+  __syncthreads();
+  if (mine >= ntok) return;
+
+  // the two chunks of this lane: a pair of rotated ones, or two of the columns behind R
+  int c0 = p, c1 = p + kLanes;
+  if (STYLE == 0) {
+    const int np = pairs / EPC;
+    c0 = p < np ? p : p + np;
+    c1 = p < np ? p + np : p + kLanes;
+  }
+  const bool in_r = a.R > 0 && (STYLE != 0 || c1 * EPC < a.R);  // (STYLE 0: both chunks or none)
+
+  for (int i0 = h0 + first; i0 < h1; i0 += step * U) {
+    uint4 raw[U][2];
+    const ST* src[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      int h = min(i0 + u * step, h1 - 1);
+      const RotaryTensor& x = h < a.q.heads ? a.q : h < a.q.heads + Hkv ? a.k : a.v;
+      if (h >= a.q.heads) h = h - a.q.heads < Hkv ? h - a.q.heads : h - a.q.heads - Hkv;
+      src[u] = static_cast<const ST*>(x.in) + (b * x.in_batch + j * x.in_token + h * x.in_head);
+      raw[u][0] = load16(src[u] + c0 * EPC);
+      raw[u][1] = load16(src[u] + c1 * EPC);
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int i = i0 + u * step;
+      if (i >= h1) break;
+      const bool is_q = i < a.q.heads, is_v = i >= a.q.heads + Hkv;
+      const int h = is_q ? i : is_v ? i - a.q.heads - Hkv : i - a.q.heads;
+      if (!is_q && to.first < 0) continue;  // padded token
+      float x0[EPC], x1[EPC], y0[EPC], y1[EPC];
+      T::unpack(raw[u][0], x0);
+      T::unpack(raw[u][1], x1);
+#pragma unroll
+      for (int e = 0; e < EPC; ++e) {
+        y0[e] = x0[e];
+        y1[e] = x1[e];
+      }
+      if (in_r && !is_v) {
+        if constexpr (STYLE == 0) {
+#pragma unroll
+          for (int e = 0; e < EPC; ++e) {
+            const float2 cs = s_cs[mine][c0 * EPC + e];
+            y0[e] = x0[e] * cs.x - x1[e] * cs.y;
+            y1[e] = x1[e] * cs.x + x0[e] * cs.y;
+          }
+        } else {
+          auto turn = [&](int c, const float(&x)[EPC], float(&y)[EPC]) __attribute__((always_inline)) {
+#pragma unroll
+            for (int e = 0; e < EPC; ++e) {
+              const int col = c * EPC + e;
+              if (col >= a.R) continue;
+              if constexpr (STYLE == 1) {
+                const float2 cs = s_cs[mine][col / 2];
+                y[e] = e % 2 == 0 ? x[e] * cs.x - x[e ^ 1] * cs.y : x[e] * cs.x + x[e ^ 1] * cs.y;
+              } else {  // partners that no chunk boundary respects, element by element
+                const bool lower = col < pairs;
+                const float2 cs = s_cs[mine][lower ? col : col - pairs];
+                const float other = T::load1(src[u] + (lower ? col + pairs : col - pairs));
+                y[e] = lower ? x[e] * cs.x - other * cs.y : x[e] * cs.x + other * cs.y;
+              }
+            }
+          };
+          turn(c0, x0, y0);
+          turn(c1, x1, y1);
+        }
+      }
+      if (is_q || !BITS4) {
+        const long long row = to.first + h * to.between;
+        ST* dst = is_q ? static_cast<ST*>(a.q.out) + (b * a.q.out_batch + j * a.q.out_token + h * a.q.out_head)
+                       : static_cast<ST*>(is_v ? args.cache.v : args.cache.k) + row * kD;
+        *reinterpret_cast<uint4*>(dst + c0 * EPC) = pack_chunk<T>(y0);
+        *reinterpret_cast<uint4*>(dst + c1 * EPC) = pack_chunk<T>(y1);
+      } else if constexpr (BITS4) {
+        const long long row = to.first + h * to.between;
+        float* mid = s_row[gid];
+#pragma unroll
+        for (int e = 0; e < EPC; e += 4) {
+          *reinterpret_cast<float4*>(mid + c0 * EPC + e) = make_float4(y0[e], y0[e + 1], y0[e + 2], y0[e + 3]);
+          *reinterpret_cast<float4*>(mid + c1 * EPC + e) = make_float4(y1[e], y1[e + 1], y1[e + 2], y1[e + 3]);
+        }
+        __builtin_amdgcn_wave_barrier();  // (the group's lanes are of one wave, whose LDS operations keep their order)
+        store_q4<kLanes>(mid, p, static_cast<uint32_t*>(is_v ? args.cache.v : args.cache.k) + row * kQ4Words,
+                         static_cast<uint32_t*>(is_v ? args.cache.v_scales : args.cache.k_scales) + row * kQ4Groups);
+        __builtin_amdgcn_wave_barrier();
+      }
+    }
+  }
+}
+
+template <typename T, bool BITS4>
+static hipError_t launch_append_t(const AppendArgs& a, dim3 grid, int style, hipStream_t st) {
+  const dim3 block(kApThreads);
+  if (style == 0)
+    hipLaunchKernelGGL((append_kernel<T, 0, BITS4>), grid, block, 0, st, a);
+  else if (style == 1)
+    hipLaunchKernelGGL((append_kernel<T, 1, BITS4>), grid, block, 0, st, a);
+  else
+    hipLaunchKernelGGL((append_kernel<T, 2, BITS4>), grid, block, 0, st, a);
+  return hipGetLastError();
+}
+
+hipError_t launch_append(const Shape& s, AppendArgs args, hipStream_t st) {
+  RotaryArgs& a = args.r;
+  const int epc = 16 / s.elem_bytes, heads = a.q.heads + 2 * s.Hkv;
+  // few tokens: the heads of a token are spread over blocks (as launch_rotary)
+  const int tokens = s.dtype == 0 ? 2 : kApMaxTokens;
+  a.tokens = a.total >= tokens * device_cus() ? tokens : 1;
+  a.heads_per_block = heads;
+  const int groups = kApThreads / (kD / epc / 2);
+  if (a.tokens == 1) {
+    int splits = device_cus() / a.total;
+    const int most = (heads + groups - 1) / groups;
+    if (splits > most) splits = most;
+    if (splits > 1) a.heads_per_block = (heads + splits - 1) / splits;
+  }
+  const dim3 grid((a.total + a.tokens - 1) / a.tokens, (heads + a.heads_per_block - 1) / a.heads_per_block);
+  const int style = a.interleaved ? 1 : (a.R / 2) % epc == 0 ? 0 : 2;
+  const bool bits4 = args.cache.k_scales != nullptr;
+  if (s.dtype == 0) return bits4 ? launch_append_t<F32, true>(args, grid, style, st) : launch_append_t<F32, false>(args, grid, style, st);
+  return bits4 ? launch_append_t<BF16, true>(args, grid, style, st) : launch_append_t<BF16, false>(args, grid, style, st);
+}
+
+// ---- rows of a cache back --------------------------------------------------------------------------------------
+// 16 lanes take a row: in 4 bits a word each, so a store instruction takes the pairs of one group of 4 rows; else 16-byte chunks.
+template <typename T, bool BITS4>
+__global__ __launch_bounds__(256) void read_rows_kernel(CacheView c, const int32_t* __restrict__ rows, int B, int n, int Hkv,
+                                                        typename T::store_t* __restrict__ k_out, typename T::store_t* __restrict__ v_out) {
+  constexpr int kRows = 16, kChunks = kD / T::EPC;
+  const long long at = (long long)blockIdx.x * kRows + (threadIdx.x >> 4), all = (long long)B * n * Hkv;
+  const int m = threadIdx.x & 15;
+  if (at >= all) return;
+  const int j = (int)(at % n), h = (int)(at / n % Hkv), b = (int)(at / n / Hkv);
+  const RowTarget from = row_target(c, b, Hkv, rows[(long long)b * n + j]);
+  if (from.first < 0) return;
+  const long long row = from.first + h * from.between;
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    typename T::store_t* dst = (i ? v_out : k_out) + at * kD;
+    if (i ? v_out == nullptr : k_out == nullptr) continue;
+    if constexpr (BITS4) {
+      const uint32_t word = static_cast<const uint32_t*>(i ? c.v : c.k)[row * kQ4Words + m];
+      const uint4 sc = load16(static_cast<const uint4*>(i ? c.v_scales : c.k_scales) + row);
+      const uint32_t scales[kQ4Groups] = {sc.x, sc.y, sc.z, sc.w};
+#pragma unroll
+      for (int g = 0; g < kQ4Groups; ++g) {
+        const cache_half2_t x = __builtin_bit_cast(cache_half2_t, scales[g]);
+        const float lo = fmaf((float)(word >> (4 * g) & 15u), (float)x.x, (float)x.y);
+        const float hi = fmaf((float)(word >> (16 + 4 * g) & 15u), (float)x.x, (float)x.y);
+        if constexpr (T::EPC == 8)
+          *reinterpret_cast<uint32_t*>(dst + 32 * g + 2 * m) = BF16::round2(lo, hi);
+        else
+          *reinterpret_cast<float2*>(dst + 32 * g + 2 * m) = make_float2(lo, hi);
+      }
+    } else {
+      const uint4* src = reinterpret_cast<const uint4*>(static_cast<const typename T::store_t*>(i ? c.v : c.k) + row * kD);
+#pragma unroll
+      for (int e = 0; e < kChunks / 16; ++e) reinterpret_cast<uint4*>(dst)[16 * e + m] = src[16 * e + m];
+    }
+  }
+}
+
+hipError_t launch_read_rows(const Shape& s, const CacheView& cache, const int32_t* rows, int n, void* k_out, void* v_out, hipStream_t st) {
+  const dim3 grid((unsigned)(((long long)s.B * n * s.Hkv + 15) / 16)), block(256);
+  const bool bits4 = cache.k_scales != nullptr;
+#define LOKI_READ(T, BITS4)                                                                                              \
+  hipLaunchKernelGGL((read_rows_kernel<T, BITS4>), grid, block, 0, st, cache, rows, s.B, n, s.Hkv, static_cast<T::store_t*>(k_out), \
+                     static_cast<T::store_t*>(v_out))
+  if (s.dtype == 0) {
+    if (bits4) LOKI_READ(F32, true);
+    else LOKI_READ(F32, false);
+  } else {
+    if (bits4) LOKI_READ(BF16, true);
+    else LOKI_READ(BF16, false);
+  }
+#undef LOKI_READ
+  return hipGetLastError();
+}
+
+}  // namespace loki

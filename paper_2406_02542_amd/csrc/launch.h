@@ -286,6 +286,36 @@ int prefix_splits_at_most(const Shape& s, int prefix_rows);
 int shared_own_splits_at_most(const Shape& s);
 hipError_t launch_shared(const Shape& s, int splits, int nsplit, const void* q, const void* k_prefix, const void* v_prefix,
                          int prefix_rows, int prefix_cap, const void* k, const void* v, float* prefix, float* partial, hipStream_t st);
+// A cache held whole (append.hip, span.hip, span_q4.hip): keys and values in the storage type, or with scales in 4 bits.
+struct CacheView {
+  void *k, *v;                // rows of 128 elements, or of 16 words of 8 codes
+  void *k_scales, *v_scales;  // null, or rows of 4 groups of (step, lowest) in fp16
+  Paging pg;                  // pages of at least 16 rows
+  int S_cap;
+};
+struct AppendArgs {
+  RotaryArgs r;  // k, v: their inputs; rows; R 0: nothing is turned
+  CacheView cache;
+};
+hipError_t launch_append(const Shape& s, AppendArgs a, hipStream_t st);
+hipError_t launch_read_rows(const Shape& s, const CacheView& cache, const int32_t* rows, int n, void* k_out, void* v_out, hipStream_t st);
+// Attention over such a cache: tokens of a sequence, each over the last `window` of its rows and the first `sinks`.
+struct SpanArgs {
+  CacheView cache;
+  const void* q;
+  void* out;              // [B, m, Hq, 128] as q
+  float* partial;         // [B m Hq][nsplit] parts, with more than one split
+  const int32_t* lens;    // [B, m] or null: S_max less the tokens behind
+  int B, m, G, Hq, Hkv, S_max, window, sinks;
+  int tiles, nsplit;      // tiles of query rows of a sequence and KV head; parts of a tile's rows
+};
+// How a call is cut: the workspace's size and the launch go by it.
+struct SpanPlan {
+  int rows;   // query rows of a tile
+  int tiles, nsplit;
+};
+SpanPlan span_plan(const Shape& s, int m, int window, int sinks, bool bits4);
+hipError_t launch_span(const Shape& s, SpanArgs a, hipStream_t st);
 hipError_t launch_rotate(const Shape& s, const void* k_new, const float* P, void* klo, void* khi,
                          int pos, int n_new, hipStream_t st);
 

@@ -13,40 +13,13 @@
 // 8 x 2048 tokens of 32/8 bf16 heads: 403 MB in 68 us (5.9 TB/s), pairs half a head apart or side by side.  Where half of the columns
 // is no whole number of chunks (STYLE 2) a lane's partners lie in other lanes' chunks and are loaded one by one: 136 us with 20 columns,
 // 185 with 126; 3 x 1111 tokens of 24/24 fp32 heads 72 us with 20, 47 with 64.
-#include "common.h"
+#include "rotary_impl.h"
 
 namespace loki {
 
 constexpr int kRotThreads = 256;
 constexpr int kRotInFlight = 6;
 constexpr int kRotMaxTokens = 4;  // of a block: one angle per thread with 64 pairs
-
-// cos and sin of x quarter turns, |x| reduced here; fp32 results.  Taylor polynomials on [-pi/4, pi/4]: the first
-// term left out is below 2^-29.
-__device__ __forceinline__ float2 cos_sin_quarters(double x) {
-  const double k = rint(x);
-  const float th = (float)(x - k) * 1.57079632679489662f, t2 = th * th;
-  float s = fmaf(t2, 2.7557319224e-6f, -1.9841269841e-4f);
-  s = fmaf(s, t2, 8.3333333333e-3f);
-  s = fmaf(s, t2, -1.6666666667e-1f);
-  s = fmaf(s * t2, th, th);
-  float c = fmaf(t2, -2.7557319224e-7f, 2.4801587302e-5f);
-  c = fmaf(c, t2, -1.3888888889e-3f);
-  c = fmaf(c, t2, 4.1666666667e-2f);
-  c = fmaf(c, t2, -0.5f);
-  c = fmaf(c, t2, 1.0f);
-  const int quarter = (int)((long long)k & 3);
-  const float cs = quarter & 1 ? s : c, sn = quarter & 1 ? c : s;
-  return make_float2(quarter == 1 || quarter == 2 ? -cs : cs, quarter >= 2 ? -sn : sn);
-}
-
-template <typename T>
-__device__ __forceinline__ uint4 pack_chunk(const float (&f)[T::EPC]) {
-  if constexpr (T::EPC == 8)
-    return make_uint4(BF16::round2(f[0], f[1]), BF16::round2(f[2], f[3]), BF16::round2(f[4], f[5]), BF16::round2(f[6], f[7]));
-  else
-    return make_uint4(__float_as_uint(f[0]), __float_as_uint(f[1]), __float_as_uint(f[2]), __float_as_uint(f[3]));
-}
 
 // STYLE: 0 pairs (i, i + R / 2), R / 2 a multiple of a chunk; 1 pairs (2 i, 2 i + 1); 2 as 0, any even R.
 // STREAM: rows are loaded and stored past the caches (launch_rotary).

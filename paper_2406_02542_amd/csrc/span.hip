@@ -1,0 +1,352 @@
+// Attention over a cache held whole, contiguous or on pages (Section 2, Eq. 1 of arXiv 2406.02542), each token over the last rows of its
+// sequence and the first few (span_impl.h): one token of every sequence, several, or chunks of prompts.
+//
+// Up to 16 query rows of a KV head (span_rows_kernel, span_f32_kernel): memory bounds it, a wave takes steps of rows straight from
+// registers, a block's waves take steps in turn.  More, in bf16 (span_tiles_kernel): the matrix cores bound it, tiles of keys and
+// values go through LDS for all of the block's query rows.
+#include "span_impl.h"
+
+namespace loki {
+
+constexpr int kSpWaves = 4;
+
+// ---- bf16, up to 16 query rows ------------------------------------------------------------------------------------
+// A wave takes steps of 32 rows:
+//   S[row, query] = K Q^T           v_mfma_f32_16x16x32_bf16, A = 16 bytes of a row for each lane (row, c), two tiles of 16 rows
+//   O^T[column, query] += V^T P^T   lane (m, c) loads 16 bytes, columns 8 m .., of the 8 rows whose weights its own column of P has, and pairs
+//                                   rows up (v_perm_b32); the weights in two bf16 terms, 2^-16 of each (as the library's other attention)
+// so a query's maximum, sum and outputs are its own lanes'.  The reference of the exponentials follows the maximum only when a
+// lane's weights of a step sum up to more than 2^8.
+__global__ __launch_bounds__(64 * kSpWaves) void span_rows_kernel(SpanArgs a) {
+  constexpr int KEYS = 32;
+  __shared__ __align__(16) SpanMerge<16, kSpWaves> sm;
+  const SpanTile tile = span_tile(a);
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), r16 = lane & 15, kgrp = lane >> 4;
+  const int M = a.m * a.G, r0 = tile.tile * 16, live = min(16, M - r0), lg = 31 - __builtin_clz(a.G);
+  const SpanRows rows = span_rows(a, tile.b, r0 >> lg, (r0 + live - 1) >> lg);
+  const SpanSteps<KEYS> steps(rows);
+  const int each = (steps.total + a.nsplit - 1) / a.nsplit, s1 = min(steps.total, (tile.split + 1) * each);
+  const RowPlaces places(a.cache, tile.b, tile.h, a.Hkv);
+  const int len = r16 < live ? span_len(a, tile.b, (r0 + r16) >> lg) : 0;
+
+  am_bf16x8_t bq[4];
+  {
+    const uint16_t* src = static_cast<const uint16_t*>(a.q) + span_place(a, tile.b, tile.h, r0 + min(r16, live - 1)) * kD + 8 * kgrp;
+#pragma unroll
+    for (int s = 0; s < 4; ++s) bq[s] = __builtin_bit_cast(am_bf16x8_t, load16(src + 32 * s));
+  }
+  float m = kNegBig, l = 0.f;
+  am_f32x4_t o[8];
+#pragma unroll
+  for (int c = 0; c < 8; ++c) o[c] = am_f32x4_t{};
+  const char* kb = static_cast<const char*>(a.cache.k) + 16 * kgrp;
+  const char* vb = static_cast<const char*>(a.cache.v) + 16 * r16;
+  uint4 kraw[2][4], vraw[8];
+  long long place[2];
+  auto find = [&](const SpanStep& st) __attribute__((always_inline)) {
+#pragma unroll
+    for (int t = 0; t < 2; ++t) place[t] = places(min(max(st.at + 16 * t, st.lo), st.hi - 1));
+  };
+  auto load_k = [&](const SpanStep& st) __attribute__((always_inline)) {
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+      const char* p = kb + (place[t] + min(max(st.at + 16 * t + r16, st.lo), st.hi - 1)) * (kD * 2);
+#pragma unroll
+      for (int s = 0; s < 4; ++s) kraw[t][s] = load16(p + 64 * s);
+    }
+  };
+  auto load_v = [&](const SpanStep& st) __attribute__((always_inline)) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+      vraw[e] = load16(vb + (place[e / 4] + min(max(st.at + 16 * (e / 4) + 4 * kgrp + e % 4, st.lo), st.hi - 1)) * (kD * 2));
+  };
+  int s = tile.split * each + wave;
+  if (s < s1) {  // (uniform for the wave)
+    const SpanStep st = span_step(steps, rows, s);
+    find(st);
+    load_k(st);
+    load_v(st);
+  }
+  for (; s < s1; s += kSpWaves) {
+    const SpanStep st = span_step(steps, rows, s), next = span_step(steps, rows, min(s + kSpWaves, steps.total - 1));
+    am_f32x4_t acc[2];
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+      acc[t] = am_f32x4_t{};
+#pragma unroll
+      for (int i = 0; i < 4; ++i) acc[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(am_bf16x8_t, kraw[t][i]), bq[i], acc[t], 0, 0, 0);
+    }
+    find(next);
+    load_k(next);
+    uint32_t seen = 0xffu;
+    if (!span_full(a, rows, st, KEYS)) {  // (uniform)
+      seen = 0;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) seen |= (span_sees(a, st, len, st.at + 16 * (e / 4) + 4 * kgrp + e % 4) ? 1u : 0u) << e;
+    }
+    float p[8], sum;
+    auto weights = [&]() __attribute__((always_inline)) {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) p[e] = seen >> e & 1u ? fast_exp2(fmaf(acc[e / 4][e % 4], kSoftmaxScaleLog2, -m)) : 0.f;
+      sum = ((p[0] + p[1]) + (p[2] + p[3])) + ((p[4] + p[5]) + (p[6] + p[7]));
+    };
+    weights();
+    if (__ballot(!(sum <= kPfGrowth)) != 0ull) {
+      float top = kNegBig;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) top = fmaxf(top, seen >> e & 1u ? acc[e / 4][e % 4] * kSoftmaxScaleLog2 : kNegBig);
+      top = fmaxf(top, __shfl_xor(top, 16));
+      top = fmaxf(top, __shfl_xor(top, 32));
+      const float mn = fmaxf(m, top), corr = fast_exp2(m - mn);
+      m = mn;
+      l *= corr;
+#pragma unroll
+      for (int c = 0; c < 8; ++c)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) o[c][i] *= corr;
+      weights();
+    }
+    l += sum;
+    uint32_t w[2][4];  // the weights' two terms
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      w[0][i] = BF16::round2(p[2 * i], p[2 * i + 1]);
+      w[1][i] = BF16::round2(p[2 * i] - __uint_as_float(w[0][i] << 16), p[2 * i + 1] - __uint_as_float(w[0][i] & 0xffff0000u));
+    }
+    const am_bf16x8_t b_hi = __builtin_bit_cast(am_bf16x8_t, make_uint4(w[0][0], w[0][1], w[0][2], w[0][3]));
+    const am_bf16x8_t b_lo = __builtin_bit_cast(am_bf16x8_t, make_uint4(w[1][0], w[1][1], w[1][2], w[1][3]));
+#pragma unroll
+    for (int c = 0; c < 8; ++c) {
+      uint32_t x[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        x[i] = __builtin_amdgcn_perm(am_word(vraw[2 * i + 1], c / 2), am_word(vraw[2 * i], c / 2), c % 2 ? 0x07060302u : 0x05040100u);
+      const am_bf16x8_t av = __builtin_bit_cast(am_bf16x8_t, make_uint4(x[0], x[1], x[2], x[3]));
+      o[c] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(av, b_lo, o[c], 0, 0, 0);
+      o[c] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(av, b_hi, o[c], 0, 0, 0);
+    }
+    load_v(next);
+  }
+  l += __shfl_xor(l, 16);
+  l += __shfl_xor(l, 32);
+  if (len == 0) l = 0.f;  // (a padded token's lanes took whatever full steps gave)
+  if (kgrp == 0) sm.ml[wave][r16] = make_float2(m, l);
+  // o[c][i] is column 8 (4 kgrp + i) + c
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    float4* dst = reinterpret_cast<float4*>(&sm.o[wave][r16][8 * (4 * kgrp + i)]);
+    dst[0] = make_float4(o[0][i], o[1][i], o[2][i], o[3][i]);
+    dst[1] = make_float4(o[4][i], o[5][i], o[6][i], o[7][i]);
+  }
+  span_store<BF16>(a, sm, tile, r0, live);
+}
+
+// ---- fp32 -----------------------------------------------------------------------------------------------------------
+// The products of parts_impl.h's attend_f32, v_mfma_f32_16x16x4_f32, straight from registers, for QG groups of 16 query rows; steps of 16 rows.
+template <int QG>
+__global__ __launch_bounds__(64 * kSpWaves, 2) void span_f32_kernel(SpanArgs a) {
+  constexpr int KEYS = 16;
+  __shared__ __align__(16) SpanMerge<16 * QG, kSpWaves> sm;
+  const SpanTile tile = span_tile(a);
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), l16 = lane & 15, c4 = lane >> 4;
+  const int M = a.m * a.G, r0 = tile.tile * (16 * QG), live = min(16 * QG, M - r0), lg = 31 - __builtin_clz(a.G);
+  const SpanRows rows = span_rows(a, tile.b, r0 >> lg, (r0 + live - 1) >> lg);
+  const SpanSteps<KEYS> steps(rows);
+  const int each = (steps.total + a.nsplit - 1) / a.nsplit, s1 = min(steps.total, (tile.split + 1) * each);
+  const RowPlaces places(a.cache, tile.b, tile.h, a.Hkv);
+
+  int len[QG];
+  float4 q[QG][8];
+  float m[QG], l[QG];
+  pf_f32x4_t o[QG][8];
+#pragma unroll
+  for (int g = 0; g < QG; ++g) {
+    const int r = 16 * g + l16;
+    len[g] = r < live ? span_len(a, tile.b, (r0 + r) >> lg) : 0;
+    const float* src = static_cast<const float*>(a.q) + span_place(a, tile.b, tile.h, r0 + min(r, live - 1)) * kD + 4 * c4;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) q[g][j] = *reinterpret_cast<const float4*>(src + 16 * j);
+    m[g] = kNegBig;
+    l[g] = 0.f;
+#pragma unroll
+    for (int c = 0; c < 8; ++c) o[g][c] = pf_f32x4_t{};
+  }
+  const float* kb = static_cast<const float*>(a.cache.k) + 4 * c4;
+  const float* vb = static_cast<const float*>(a.cache.v) + 4 * l16;
+  float4 kr[8], vr[4][2];
+  long long place;
+  auto load_k = [&](const SpanStep& st) __attribute__((always_inline)) {
+    const float* p = kb + (place + min(max(st.at + l16, st.lo), st.hi - 1)) * kD;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) kr[j] = *reinterpret_cast<const float4*>(p + 16 * j);
+  };
+  auto load_v = [&](const SpanStep& st) __attribute__((always_inline)) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const float* p = vb + (place + min(max(st.at + 4 * c4 + i, st.lo), st.hi - 1)) * kD;
+      vr[i][0] = *reinterpret_cast<const float4*>(p);
+      vr[i][1] = *reinterpret_cast<const float4*>(p + 64);
+    }
+  };
+  int s = tile.split * each + wave;
+  if (s < s1) {  // (uniform for the wave)
+    const SpanStep st = span_step(steps, rows, s);
+    place = places(min(max(st.at, st.lo), st.hi - 1));
+    load_k(st);
+    load_v(st);
+  }
+  for (; s < s1; s += kSpWaves) {
+    const SpanStep st = span_step(steps, rows, s), next = span_step(steps, rows, min(s + kSpWaves, steps.total - 1));
+    pf_f32x4_t p[QG], chain[QG][4];
+#pragma unroll
+    for (int g = 0; g < QG; ++g)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) chain[g][e] = pf_f32x4_t{};
+#pragma unroll
+    for (int j = 0; j < 8; ++j)
+#pragma unroll
+      for (int g = 0; g < QG; ++g) {
+        chain[g][0] = __builtin_amdgcn_mfma_f32_16x16x4f32(kr[j].x, q[g][j].x, chain[g][0], 0, 0, 0);
+        chain[g][1] = __builtin_amdgcn_mfma_f32_16x16x4f32(kr[j].y, q[g][j].y, chain[g][1], 0, 0, 0);
+        chain[g][2] = __builtin_amdgcn_mfma_f32_16x16x4f32(kr[j].z, q[g][j].z, chain[g][2], 0, 0, 0);
+        chain[g][3] = __builtin_amdgcn_mfma_f32_16x16x4f32(kr[j].w, q[g][j].w, chain[g][3], 0, 0, 0);
+      }
+    place = places(min(max(next.at, next.lo), next.hi - 1));
+    load_k(next);
+    const bool full = span_full(a, rows, st, KEYS);
+#pragma unroll
+    for (int g = 0; g < QG; ++g) {
+      float x[4], sum;
+      bool seen[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        x[i] = ((chain[g][0][i] + chain[g][1][i]) + (chain[g][2][i] + chain[g][3][i])) * kSoftmaxScaleLog2;
+        seen[i] = full || span_sees(a, st, len[g], st.at + 4 * c4 + i);
+      }
+      auto weights = [&]() __attribute__((always_inline)) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) p[g][i] = seen[i] ? fast_exp2(x[i] - m[g]) : 0.f;
+        sum = (p[g][0] + p[g][1]) + (p[g][2] + p[g][3]);
+      };
+      weights();
+      if (__ballot(!(sum <= kPfGrowth)) != 0ull) {
+        float top = kNegBig;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) top = fmaxf(top, seen[i] ? x[i] : kNegBig);
+        top = fmaxf(top, __shfl_xor(top, 16));
+        top = fmaxf(top, __shfl_xor(top, 32));
+        const float mn = fmaxf(m[g], top), corr = fast_exp2(m[g] - mn);
+        m[g] = mn;
+        l[g] *= corr;
+#pragma unroll
+        for (int c = 0; c < 8; ++c)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) o[g][c][i] *= corr;
+        weights();
+      }
+      l[g] += sum;
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+      for (int g = 0; g < QG; ++g)
+#pragma unroll
+        for (int c = 0; c < 2; ++c) {
+          o[g][4 * c] = __builtin_amdgcn_mfma_f32_16x16x4f32(vr[i][c].x, p[g][i], o[g][4 * c], 0, 0, 0);
+          o[g][4 * c + 1] = __builtin_amdgcn_mfma_f32_16x16x4f32(vr[i][c].y, p[g][i], o[g][4 * c + 1], 0, 0, 0);
+          o[g][4 * c + 2] = __builtin_amdgcn_mfma_f32_16x16x4f32(vr[i][c].z, p[g][i], o[g][4 * c + 2], 0, 0, 0);
+          o[g][4 * c + 3] = __builtin_amdgcn_mfma_f32_16x16x4f32(vr[i][c].w, p[g][i], o[g][4 * c + 3], 0, 0, 0);
+        }
+    load_v(next);
+  }
+#pragma unroll
+  for (int g = 0; g < QG; ++g) {
+    l[g] += __shfl_xor(l[g], 16);
+    l[g] += __shfl_xor(l[g], 32);
+    if (len[g] == 0) l[g] = 0.f;
+    const int r = 16 * g + l16;
+    if (c4 == 0) sm.ml[wave][r] = make_float2(m[g], l[g]);
+    // o[4 c + t][i] is column 64 c + 4 (4 c4 + i) + t
+#pragma unroll
+    for (int c = 0; c < 2; ++c)
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        *reinterpret_cast<float4*>(&sm.o[wave][r][64 * c + 16 * c4 + 4 * i]) = make_float4(o[g][4 * c][i], o[g][4 * c + 1][i], o[g][4 * c + 2][i], o[g][4 * c + 3][i]);
+  }
+  span_store<F32>(a, sm, tile, r0, live);
+}
+
+// ---- parts joined ---------------------------------------------------------------------------------------------------
+// 32 lanes take a query row, 16 bytes of each of its parts.
+template <typename T>
+__global__ __launch_bounds__(256) void span_merge_kernel(const float* __restrict__ partial, typename T::store_t* __restrict__ out,
+                                                         long long rows, int nsplit) {
+  const long long r = (long long)blockIdx.x * 8 + (threadIdx.x >> 5);
+  const int lane = threadIdx.x & 31;
+  if (r >= rows) return;
+  float mn = kNegBig, ls = 0.f;
+  float4 os = make_float4(0.f, 0.f, 0.f, 0.f);
+  for (int i = 0; i < nsplit; ++i) {
+    const float* p = partial + (r * nsplit + i) * kPartStride;
+    const float2 ml = *reinterpret_cast<const float2*>(p + kD);
+    const float4 x = *reinterpret_cast<const float4*>(p + 4 * lane);
+    const float top = fmaxf(mn, ml.x), c = fast_exp2(mn - top), f = fast_exp2(ml.x - top);
+    mn = top;
+    ls = fmaf(ls, c, ml.y * f);
+    os = make_float4(fmaf(os.x, c, x.x * f), fmaf(os.y, c, x.y * f), fmaf(os.z, c, x.z * f), fmaf(os.w, c, x.w * f));
+  }
+  const float inv = ls > 0.f ? 1.0f / ls : 0.f;  // (a token without rows: zeros)
+  if constexpr (T::EPC == 8)
+    *reinterpret_cast<uint2*>(out + r * kD + 4 * lane) = make_uint2(BF16::round2(os.x * inv, os.y * inv), BF16::round2(os.z * inv, os.w * inv));
+  else
+    *reinterpret_cast<float4*>(out + r * kD + 4 * lane) = make_float4(os.x * inv, os.y * inv, os.z * inv, os.w * inv);
+}
+
+// ---- the launch -----------------------------------------------------------------------------------------------------
+SpanPlan span_plan(const Shape& s, int m, int window, int sinks, bool bits4) {
+  SpanPlan p{16, 0, 1};
+  const long long M = (long long)m * s.G;
+  if (s.dtype == 0 && !bits4 && M > 16) p.rows = 32;
+  p.tiles = (int)((M + p.rows - 1) / p.rows);
+  // rows of a tile at most, and the parts of at least 128 of them that give every CU two blocks
+  const long long most = window > 0 ? (long long)window + sinks + (p.rows + s.G - 1) / s.G + 32 : s.S;
+  const long long read = most < s.S ? most : s.S, blocks = (long long)s.B * s.Hkv * p.tiles;
+  long long n = (2LL * device_cus() + blocks - 1) / blocks;
+  if (n > (read + 127) / 128) n = (read + 127) / 128;
+  p.nsplit = n < 1 ? 1 : (int)n;
+  return p;
+}
+
+hipError_t launch_span_q4(const Shape& s, const SpanArgs& a, int rows, hipStream_t st);
+
+hipError_t launch_span(const Shape& s, SpanArgs a, hipStream_t st) {
+  const bool bits4 = a.cache.k_scales != nullptr;
+  const SpanPlan plan = span_plan(s, a.m, a.window, a.sinks, bits4);
+  if (a.window == 0) {
+    a.window = 0x7fffffff;
+    a.sinks = 0;
+  }
+  a.tiles = plan.tiles;
+  a.nsplit = plan.nsplit;
+  const dim3 grid((unsigned)((long long)a.B * a.Hkv * a.tiles * a.nsplit)), block(64 * kSpWaves);
+  hipError_t e = hipSuccess;
+  if (bits4)
+    e = launch_span_q4(s, a, plan.rows, st);
+  else if (s.dtype == 1)
+    hipLaunchKernelGGL(span_rows_kernel, grid, block, 0, st, a);
+  else if (plan.rows == 16)
+    hipLaunchKernelGGL((span_f32_kernel<1>), grid, block, 0, st, a);
+  else
+    hipLaunchKernelGGL((span_f32_kernel<2>), grid, block, 0, st, a);
+  if (e == hipSuccess) e = hipGetLastError();
+  if (e != hipSuccess || a.nsplit == 1) return e;
+  const long long rows = (long long)a.B * a.m * a.Hq;
+  const dim3 merge((unsigned)((rows + 7) / 8));
+  if (s.dtype == 0)
+    hipLaunchKernelGGL((span_merge_kernel<F32>), merge, dim3(256), 0, st, a.partial, static_cast<float*>(a.out), rows, a.nsplit);
+  else
+    hipLaunchKernelGGL((span_merge_kernel<BF16>), merge, dim3(256), 0, st, a.partial, static_cast<uint16_t*>(a.out), rows, a.nsplit);
+  return hipGetLastError();
+}
+
+}  // namespace loki

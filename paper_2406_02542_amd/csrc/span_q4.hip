@@ -1,0 +1,240 @@
+// Attention over a cache held whole in 4 bits (cache_impl.h), contiguous or on pages (Section 2, Eq. 1 of arXiv 2406.02542), each token over
+// the last rows of its sequence and the first few (span_impl.h).
+//
+// A value is lowest + step n with one (step, lowest) for a row's group g of 32 columns, so
+//   logit[row] = sum over g of 16 step_g[row] sum over c in g of q[c] n[row, c] / 16 + lowest_g[row] sum over c in g of q[c]
+//   out[c]     = sum over rows of (16 p step_g)[row] n[row, c] / 16 + sum over rows of (p lowest_g)[row]          for c in g
+// and the codes go to the matrix cores as they are: the bits 0x3f80 | n << 3 are the bf16 number 1 + n / 16, exactly, a shift and a bit
+// select for two of them.  The ones' share is taken off in advance (the first product begins with minus the group's sum of q) or
+// at the end (sum over rows of 16 p step_g).
+#include "span_impl.h"
+
+namespace loki {
+
+constexpr int kQ4Waves = 4;
+
+// Codes g of a word's halves as two bf16 numbers 1 + n / 16.
+__device__ __forceinline__ uint32_t q4_pair(uint32_t x, int g) {
+  const uint32_t y = g == 0 ? x << 3 : x >> (4 * g - 3);
+  return (y & 0x00780078u) | 0x3f803f80u;
+}
+
+// x0, x1 as TERMS pairs of bf16 numbers that add up to them.
+template <int TERMS>
+__device__ __forceinline__ void q4_terms(float x0, float x1, uint32_t (&w)[TERMS]) {
+#pragma unroll
+  for (int t = 0; t < TERMS; ++t) {
+    w[t] = BF16::round2(x0, x1);
+    x0 -= __uint_as_float(w[t] << 16);  // exact in fp32
+    x1 -= __uint_as_float(w[t] & 0xffff0000u);
+  }
+}
+
+// QG groups of 16 query rows.  bf16: q is one term, the weights two (2^-16 of each, as the library's other attention); fp32: three each.
+template <typename T, int QG>
+__global__ __launch_bounds__(64 * kQ4Waves) void span_q4_kernel(SpanArgs a) {
+  constexpr int KEYS = 32, QT = T::EPC == 8 ? 1 : 3, PT = T::EPC == 8 ? 2 : 3;
+  __shared__ __align__(16) SpanMerge<16 * QG, kQ4Waves> sm;
+  const SpanTile tile = span_tile(a);
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), r16 = lane & 15, kgrp = lane >> 4;
+  const int M = a.m * a.G, r0 = tile.tile * (16 * QG), live = min(16 * QG, M - r0), lg = 31 - __builtin_clz(a.G);
+  const SpanRows rows = span_rows(a, tile.b, r0 >> lg, (r0 + live - 1) >> lg);
+  const SpanSteps<KEYS> steps(rows);
+  const int each = (steps.total + a.nsplit - 1) / a.nsplit, s1 = min(steps.total, (tile.split + 1) * each);
+  const RowPlaces places(a.cache, tile.b, tile.h, a.Hkv);
+
+  int len[QG];
+  am_bf16x8_t bq[QG][kQ4Groups][QT];
+  float qsum[QG][kQ4Groups];  // of a group's columns
+  float m[QG], l[QG], low[QG][kQ4Groups], ones[QG][kQ4Groups];
+  am_f32x4_t o[QG][8];
+#pragma unroll
+  for (int u = 0; u < QG; ++u) {
+    const int r = 16 * u + r16;
+    len[u] = r < live ? span_len(a, tile.b, (r0 + r) >> lg) : 0;
+    const typename T::store_t* src = static_cast<const typename T::store_t*>(a.q) + span_place(a, tile.b, tile.h, r0 + min(r, live - 1)) * kD + 8 * kgrp;
+#pragma unroll
+    for (int g = 0; g < kQ4Groups; ++g) {
+      float x[8];
+#pragma unroll
+      for (int e = 0; e < 8; e += T::EPC) T::unpack(load16(src + 32 * g + e), *reinterpret_cast<float(*)[T::EPC]>(x + e));
+      uint32_t w[4][QT];
+      float sum = 0.f;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        q4_terms<QT>(x[2 * i], x[2 * i + 1], w[i]);
+        sum += x[2 * i] + x[2 * i + 1];
+      }
+#pragma unroll
+      for (int t = 0; t < QT; ++t) bq[u][g][t] = __builtin_bit_cast(am_bf16x8_t, make_uint4(w[0][t], w[1][t], w[2][t], w[3][t]));
+      sum += __shfl_xor(sum, 16);
+      qsum[u][g] = sum + __shfl_xor(sum, 32);
+      low[u][g] = ones[u][g] = 0.f;
+    }
+    m[u] = kNegBig;
+    l[u] = 0.f;
+#pragma unroll
+    for (int c = 0; c < 8; ++c) o[u][c] = am_f32x4_t{};
+  }
+
+  const char *kb = static_cast<const char*>(a.cache.k) + 16 * kgrp, *vb = static_cast<const char*>(a.cache.v) + 4 * r16;
+  const char *ks = static_cast<const char*>(a.cache.k_scales), *vs = static_cast<const char*>(a.cache.v_scales);
+  uint4 kraw[2], ksc[8], vsc[8];
+  uint32_t vraw[8];
+  long long place[2];
+  auto row_of = [&](const SpanStep& st, int e) __attribute__((always_inline)) {  // row e of the 8 whose weights this lane has
+    return place[e / 4] + min(max(st.at + 16 * (e / 4) + 4 * kgrp + e % 4, st.lo), st.hi - 1);
+  };
+  auto find = [&](const SpanStep& st) __attribute__((always_inline)) {
+#pragma unroll
+    for (int t = 0; t < 2; ++t) place[t] = places(min(max(st.at + 16 * t, st.lo), st.hi - 1));
+  };
+  auto load_k = [&](const SpanStep& st) __attribute__((always_inline)) {
+#pragma unroll
+    for (int t = 0; t < 2; ++t) kraw[t] = load16(kb + (place[t] + min(max(st.at + 16 * t + r16, st.lo), st.hi - 1)) * kQ4RowBytes);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) ksc[e] = load16(ks + row_of(st, e) * kQ4ScaleBytes);
+  };
+  auto load_v = [&](const SpanStep& st) __attribute__((always_inline)) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      vraw[e] = *reinterpret_cast<const uint32_t*>(vb + row_of(st, e) * kQ4RowBytes);
+      vsc[e] = load16(vs + row_of(st, e) * kQ4ScaleBytes);
+    }
+  };
+  int s = tile.split * each + wave;
+  if (s < s1) {  // (uniform for the wave)
+    const SpanStep st = span_step(steps, rows, s);
+    find(st);
+    load_k(st);
+    load_v(st);
+  }
+  for (; s < s1; s += kQ4Waves) {
+    const SpanStep st = span_step(steps, rows, s), next = span_step(steps, rows, min(s + kQ4Waves, steps.total - 1));
+    float x[QG][8];
+#pragma unroll
+    for (int u = 0; u < QG; ++u)
+#pragma unroll
+      for (int e = 0; e < 8; ++e) x[u][e] = 0.f;
+#pragma unroll
+    for (int t = 0; t < 2; ++t)
+#pragma unroll
+      for (int g = 0; g < kQ4Groups; ++g) {
+        const am_bf16x8_t ka = __builtin_bit_cast(am_bf16x8_t, make_uint4(q4_pair(kraw[t].x, g), q4_pair(kraw[t].y, g), q4_pair(kraw[t].z, g), q4_pair(kraw[t].w, g)));
+#pragma unroll
+        for (int u = 0; u < QG; ++u) {
+          am_f32x4_t acc = {-qsum[u][g], -qsum[u][g], -qsum[u][g], -qsum[u][g]};
+#pragma unroll
+          for (int i = QT - 1; i >= 0; --i) acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ka, bq[u][g][i], acc, 0, 0, 0);
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const cache_half2_t sc = __builtin_bit_cast(cache_half2_t, am_word(ksc[4 * t + i], g));
+            x[u][4 * t + i] = fmaf(acc[i], 16.f * (float)sc.x, fmaf(qsum[u][g], (float)sc.y, x[u][4 * t + i]));
+          }
+        }
+      }
+    const bool full = span_full(a, rows, st, KEYS);
+    float p[QG][8];
+#pragma unroll
+    for (int u = 0; u < QG; ++u) {
+      uint32_t seen = 0xffu;
+      if (!full) {  // (uniform)
+        seen = 0;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) seen |= (span_sees(a, st, len[u], st.at + 16 * (e / 4) + 4 * kgrp + e % 4) ? 1u : 0u) << e;
+      }
+      float sum;
+      auto weights = [&]() __attribute__((always_inline)) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) p[u][e] = seen >> e & 1u ? fast_exp2(fmaf(x[u][e], kSoftmaxScaleLog2, -m[u])) : 0.f;
+        sum = ((p[u][0] + p[u][1]) + (p[u][2] + p[u][3])) + ((p[u][4] + p[u][5]) + (p[u][6] + p[u][7]));
+      };
+      weights();
+      if (__ballot(!(sum <= kPfGrowth)) != 0ull) {
+        float top = kNegBig;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) top = fmaxf(top, seen >> e & 1u ? x[u][e] * kSoftmaxScaleLog2 : kNegBig);
+        top = fmaxf(top, __shfl_xor(top, 16));
+        top = fmaxf(top, __shfl_xor(top, 32));
+        const float mn = fmaxf(m[u], top), corr = fast_exp2(m[u] - mn);
+        m[u] = mn;
+        l[u] *= corr;
+#pragma unroll
+        for (int g = 0; g < kQ4Groups; ++g) {
+          low[u][g] *= corr;
+          ones[u][g] *= corr;
+        }
+#pragma unroll
+        for (int c = 0; c < 8; ++c)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) o[u][c][i] *= corr;
+        weights();
+      }
+      l[u] += sum;
+    }
+#pragma unroll
+    for (int g = 0; g < kQ4Groups; ++g) {
+      // tile c of group g: column 32 g + 2 m + c of lane m's word
+      am_bf16x8_t av[2];
+#pragma unroll
+      for (int c = 0; c < 2; ++c) {
+        uint32_t y[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) y[i] = q4_pair(__builtin_amdgcn_perm(vraw[2 * i + 1], vraw[2 * i], c ? 0x07060302u : 0x05040100u), g);
+        av[c] = __builtin_bit_cast(am_bf16x8_t, make_uint4(y[0], y[1], y[2], y[3]));
+      }
+#pragma unroll
+      for (int u = 0; u < QG; ++u) {
+        uint32_t w[4][PT];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const cache_half2_t s0 = __builtin_bit_cast(cache_half2_t, am_word(vsc[2 * i], g)), s1 = __builtin_bit_cast(cache_half2_t, am_word(vsc[2 * i + 1], g));
+          const float p0 = p[u][2 * i], p1 = p[u][2 * i + 1], x0 = p0 * (float)s0.x, x1 = p1 * (float)s1.x;
+          ones[u][g] += x0 + x1;
+          low[u][g] = fmaf(p0, (float)s0.y, fmaf(p1, (float)s1.y, low[u][g]));
+          q4_terms<PT>(x0, x1, w[i]);
+        }
+#pragma unroll
+        for (int t = PT - 1; t >= 0; --t) {
+          const am_bf16x8_t b = __builtin_bit_cast(am_bf16x8_t, make_uint4(w[0][t], w[1][t], w[2][t], w[3][t]));
+#pragma unroll
+          for (int c = 0; c < 2; ++c) o[u][2 * g + c] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(av[c], b, o[u][2 * g + c], 0, 0, 0);
+        }
+      }
+    }
+    find(next);
+    load_k(next);
+    load_v(next);
+  }
+#pragma unroll
+  for (int u = 0; u < QG; ++u) {
+    const int r = 16 * u + r16;
+    l[u] += __shfl_xor(l[u], 16);
+    l[u] += __shfl_xor(l[u], 32);
+    if (len[u] == 0) l[u] = 0.f;  // (a padded token's lanes took whatever full steps gave)
+    if (kgrp == 0) sm.ml[wave][r] = make_float2(m[u], l[u]);
+    // o[2 g + c][i] is column 32 g + 2 (4 kgrp + i) + c
+#pragma unroll
+    for (int g = 0; g < kQ4Groups; ++g) {
+      float base = low[u][g] - 16.f * ones[u][g];
+      base += __shfl_xor(base, 16);
+      base += __shfl_xor(base, 32);
+#pragma unroll
+      for (int i = 0; i < 4; i += 2)
+        *reinterpret_cast<float4*>(&sm.o[wave][r][32 * g + 8 * kgrp + 2 * i]) =
+            make_float4(fmaf(16.f, o[u][2 * g][i], base), fmaf(16.f, o[u][2 * g + 1][i], base), fmaf(16.f, o[u][2 * g][i + 1], base), fmaf(16.f, o[u][2 * g + 1][i + 1], base));
+    }
+  }
+  span_store<T>(a, sm, tile, r0, live);
+}
+
+hipError_t launch_span_q4(const Shape& s, const SpanArgs& a, int rows, hipStream_t st) {
+  const dim3 grid((unsigned)((long long)a.B * a.Hkv * a.tiles * a.nsplit)), block(64 * kQ4Waves);
+  if (s.dtype == 0)
+    hipLaunchKernelGGL((span_q4_kernel<F32, 1>), grid, block, 0, st, a);
+  else
+    hipLaunchKernelGGL((span_q4_kernel<BF16, 1>), grid, block, 0, st, a);
+  return hipGetLastError();
+}
+
+}  // namespace loki
