@@ -787,6 +787,7 @@ class Cache:
         for name, t, want, size in parts:
             if t.shape != size:
                 raise ValueError(f"{name} must be {list(size)}, got {tuple(t.shape)}")
+        for name, t, want, _ in parts:
             _ptr(t, name, want)
             if t.get_device() != k.get_device():
                 raise ValueError(f"{name} and k must live on the same device")

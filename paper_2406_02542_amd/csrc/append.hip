@@ -32,6 +32,37 @@ __device__ __forceinline__ uint32_t q4_code(float x, float low, float step) {
   return (uint32_t)fminf(fmaxf(n, 0.f), 15.f);
 }
 
+// cos and sin of an angle, formed in 64 bits and rounded once: pi / 2 in two terms takes the quarter turns off, Taylor polynomials on
+// [-pi / 4, pi / 4], whose first terms left out are below 2^-54.
+__device__ __forceinline__ float2 cos_sin_rounded(double x) {
+  const double k = rint(x * 0.63661977236758134308), t = fma(-k, 6.123233995736766e-17, fma(-k, 1.5707963267948966, x)), t2 = t * t;
+  double s = -1.0 / 1307674368000.0, c = 1.0 / 20922789888000.0;
+  s = fma(s, t2, 1.0 / 6227020800.0);
+  s = fma(s, t2, -1.0 / 39916800.0);
+  s = fma(s, t2, 1.0 / 362880.0);
+  s = fma(s, t2, -1.0 / 5040.0);
+  s = fma(s, t2, 1.0 / 120.0);
+  s = fma(s, t2, -1.0 / 6.0);
+  s = fma(s * t2, t, t);
+  c = fma(c, t2, -1.0 / 87178291200.0);
+  c = fma(c, t2, 1.0 / 479001600.0);
+  c = fma(c, t2, -1.0 / 3628800.0);
+  c = fma(c, t2, 1.0 / 40320.0);
+  c = fma(c, t2, -1.0 / 720.0);
+  c = fma(c, t2, 1.0 / 24.0);
+  c = fma(c, t2, -0.5);
+  c = fma(c, t2, 1.0);
+  const int quarter = (int)((long long)k & 3);
+  const float cs = (float)(quarter & 1 ? s : c), sn = (float)(quarter & 1 ? c : s);
+  return make_float2(quarter == 1 || quarter == 2 ? -cs : cs, quarter >= 2 ? -sn : sn);
+}
+
+// a x + b y, each product rounded by itself: what a value becomes, and with it its code, does not turn on which product is fused.
+__device__ __forceinline__ float turned(float a, float x, float b, float y) {
+#pragma clang fp contract(off)
+  return a * x + b * y;
+}
+
 // The row in `row` (LDS, 128 floats, complete) as codes and scales, by the LANES lanes of a group; p: the lane's number.
 template <int LANES>
 __device__ __forceinline__ void store_q4(const float* row, int p, uint32_t* codes, uint32_t* scales) {
@@ -85,8 +116,7 @@ __global__ __launch_bounds__(kApThreads) void append_kernel(AppendArgs args) {
 
   for (int i = tid; i < ntok * pairs; i += kApThreads) {
     const int u = i / pairs, f = i - u * pairs;
-    const double quarters = (double)a.positions[tok0 + u] * (a.freqs[f] * 0.63661977236758134308);  // 2 / pi
-    float2 cs = cos_sin_quarters(quarters);
+    float2 cs = cos_sin_rounded((double)a.positions[tok0 + u] * a.freqs[f]);
     cs.x *= a.scale;
     cs.y *= a.inverse ? -a.scale : a.scale;
     s_cs[u][f] = cs;
@@ -135,8 +165,8 @@ __global__ __launch_bounds__(kApThreads) void append_kernel(AppendArgs args) {
 #pragma unroll
           for (int e = 0; e < EPC; ++e) {
             const float2 cs = s_cs[mine][c0 * EPC + e];
-            y0[e] = x0[e] * cs.x - x1[e] * cs.y;
-            y1[e] = x1[e] * cs.x + x0[e] * cs.y;
+            y0[e] = turned(x0[e], cs.x, x1[e], -cs.y);
+            y1[e] = turned(x1[e], cs.x, x0[e], cs.y);
           }
         } else {
           auto turn = [&](int c, const float(&x)[EPC], float(&y)[EPC]) __attribute__((always_inline)) {
@@ -146,12 +176,12 @@ __global__ __launch_bounds__(kApThreads) void append_kernel(AppendArgs args) {
               if (col >= a.R) continue;
               if constexpr (STYLE == 1) {
                 const float2 cs = s_cs[mine][col / 2];
-                y[e] = e % 2 == 0 ? x[e] * cs.x - x[e ^ 1] * cs.y : x[e] * cs.x + x[e ^ 1] * cs.y;
+                y[e] = turned(x[e], cs.x, x[e ^ 1], e % 2 == 0 ? -cs.y : cs.y);
               } else {  // partners that no chunk boundary respects, element by element
                 const bool lower = col < pairs;
                 const float2 cs = s_cs[mine][lower ? col : col - pairs];
                 const float other = T::load1(src[u] + (lower ? col + pairs : col - pairs));
-                y[e] = lower ? x[e] * cs.x - other * cs.y : x[e] * cs.x + other * cs.y;
+                y[e] = turned(x[e], cs.x, other, lower ? -cs.y : cs.y);
               }
             }
           };
