@@ -276,6 +276,273 @@ __global__ __launch_bounds__(64 * kSpWaves, 2) void span_f32_kernel(SpanArgs a) 
   span_store<F32>(a, sm, tile, r0, live);
 }
 
+// ---- bf16, more query rows: tiles through LDS -------------------------------------------------------------------------
+// The products of shared.hip's prefix kernel: a wave holds 32 query rows and takes steps of 32 keys, S^T = K Q^T and O^T += V^T P^T by
+// v_mfma_f32_32x32x16_bf16, the weights in two bf16 terms as they come out of the first product.  Tiles of KT keys and values go through LDS
+// once for the block's waves, WQ of which hold different queries and WK = WAVES / WQ different keys of the tile; the next tile is loaded into
+// registers while this one is used.  What is masked is decided for a wave's step as a whole: nothing to see, everything, or each on its own.
+typedef short sp_s16x4_t __attribute__((ext_vector_type(4)));
+typedef float sp_f32x16_t __attribute__((ext_vector_type(16)));
+typedef __attribute__((address_space(3))) sp_s16x4_t sp_lds_s16x4_t;
+
+constexpr float kUnseen = -3.0e38f;  // a logit that no maximum follows and whose weight is 0 whatever the maximum is
+
+template <int WAVES, int WQ>
+constexpr int span_tile_keys() {
+  return WAVES / WQ == 4 ? 128 : 64;
+}
+// Two pairs of tiles; at the end, where waves have other keys of the same queries, what half of them hand over, or the outputs.
+template <int WAVES, int WQ>
+constexpr int span_lds_bytes() {
+  const int tiles = 4 * span_tile_keys<WAVES, WQ>() * 256, merge = WQ == WAVES ? 0 : WAVES * 32 * 8 + WAVES / 2 * 64 * 256;
+  return tiles > merge ? tiles : merge;
+}
+
+template <int WAVES, int WQ>
+__global__ __launch_bounds__(64 * WAVES, WAVES == 4 ? 1 : 2) void span_tiles_kernel(SpanArgs a) {
+  extern __shared__ __align__(16) char smem[];  // [2][K tile, V tile]
+  constexpr int kThreads = 64 * WAVES, WK = WAVES / WQ, KT = span_tile_keys<WAVES, WQ>(), kSteps = KT / (32 * WK), kChunks = KT * 16 / kThreads;
+  constexpr int kTileBytes = KT * 256;
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int l32 = lane & 31, half = lane >> 5, l16 = lane & 15;
+  const int wq = wave % WQ, wk = wave / WQ;
+  SpanTile tile = span_tile(a);
+  tile.tile = a.tiles - 1 - tile.tile;  // (the last tokens see the most)
+  const int M = a.m * a.G, r0 = tile.tile * (32 * WQ), live = min(32 * WQ, M - r0), lg = 31 - __builtin_clz(a.G);
+  const SpanRows rows = span_rows(a, tile.b, r0 >> lg, (r0 + live - 1) >> lg);
+  const SpanSteps<KT> steps(rows);
+  const int each = (steps.total + a.nsplit - 1) / a.nsplit, s0 = tile.split * each, s1 = min(steps.total, s0 + each);
+  const RowPlaces places(a.cache, tile.b, tile.h, a.Hkv);
+  // this wave's queries, and its lane's
+  const int q0 = wq * 32, mine = min(32, live - q0), row = q0 + l32;
+  SpanRows own{0, 0, 0, 0};
+  if (mine > 0) own = span_rows(a, tile.b, (r0 + q0) >> lg, (r0 + q0 + mine - 1) >> lg);
+  const int len = row < live ? span_len(a, tile.b, (r0 + row) >> lg) : 0;
+
+  am_bf16x8_t q[8];
+  {
+    const uint16_t* src = static_cast<const uint16_t*>(a.q) + span_place(a, tile.b, tile.h, r0 + min(row, live - 1)) * kD + 8 * half;
+#pragma unroll
+    for (int ks = 0; ks < 8; ++ks) q[ks] = __builtin_bit_cast(am_bf16x8_t, load16(src + 16 * ks));
+  }
+  const uint16_t* kb = static_cast<const uint16_t*>(a.cache.k) + l16 * 8;
+  const uint16_t* vb = static_cast<const uint16_t*>(a.cache.v) + l16 * 8;
+  uint4 kst[kChunks], vst[kChunks];
+  auto load = [&](int s) __attribute__((always_inline)) {  // (a wave's four rows of a chunk lie in one page)
+    const SpanStep st = span_step(steps, rows, s);
+#pragma unroll
+    for (int j = 0; j < kChunks; ++j) {
+      const int first = st.at + 4 * wave + kThreads / 16 * j;
+      const long long off = (places(min(max(first, st.lo), st.hi - 1)) + min(max(first + (lane >> 4), st.lo), st.hi - 1)) * kD;
+      kst[j] = load16(kb + off);
+      vst[j] = load16(vb + off);
+    }
+  };
+  auto store = [&](int b) __attribute__((always_inline)) {
+    char* base = smem + b * 2 * kTileBytes;
+#pragma unroll
+    for (int j = 0; j < kChunks; ++j) {
+      const int at = tid + kThreads * j, r = at >> 4, c = at & 15;
+      *reinterpret_cast<uint4*>(base + r * 256 + ((c ^ (r & 15)) * 16)) = kst[j];
+      *reinterpret_cast<uint4*>(base + kTileBytes + r * 256 + ((c ^ ((r & 3) << 2)) * 16)) = vst[j];
+    }
+  };
+
+  float m = kNegBig, l = 0.f;
+  sp_f32x16_t o[4];
+#pragma unroll
+  for (int c = 0; c < 4; ++c) o[c] = sp_f32x16_t{};
+  const int k_at = l32 * 256 + ((half ^ l16) * 16);
+  const int v_row = 4 * half + (l16 >> 2);
+  const int v_at = kTileBytes + v_row * 256 + (((((lane >> 4) & 1) * 2 + ((l16 & 3) >> 1)) ^ ((v_row & 3) << 2)) * 16) + (l16 & 1) * 8;
+
+  // 32 keys of the tile in buffer `base`, rows st.at ..; MASKED: each query on its own
+  auto step = [&](const char* base, const SpanStep& st, auto masked) __attribute__((always_inline)) {
+    am_bf16x8_t ka[8], va[2][4];
+#pragma unroll
+    for (int ks = 0; ks < 8; ++ks) ka[ks] = __builtin_bit_cast(am_bf16x8_t, *reinterpret_cast<const uint4*>(base + (k_at ^ (ks * 32))));
+    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+    for (int ks = 0; ks < 2; ++ks)
+#pragma unroll
+      for (int c = 0; c < 4; ++c) {
+        const char* at = base + (v_at ^ (c * 64)) + ks * 4096;
+        const sp_s16x4_t x = __builtin_amdgcn_ds_read_tr16_b64_v4i16((sp_lds_s16x4_t*)(at));
+        const sp_s16x4_t y = __builtin_amdgcn_ds_read_tr16_b64_v4i16((sp_lds_s16x4_t*)(at + 2048));
+        va[ks][c] = __builtin_bit_cast(am_bf16x8_t, __builtin_shufflevector(x, y, 0, 1, 2, 3, 4, 5, 6, 7));
+      }
+    sp_f32x16_t s = sp_f32x16_t{};
+#pragma unroll
+    for (int ks = 0; ks < 8; ++ks) s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(ka[ks], q[ks], s, 0, 0, 0);
+    __builtin_amdgcn_sched_barrier(0);
+    if constexpr (decltype(masked)::value) {
+#pragma unroll
+      for (int i = 0; i < 16; ++i)
+        if (!span_sees(a, st, len, st.at + 8 * (i >> 2) + 4 * half + (i & 3))) s[i] = kUnseen;
+    }
+    float p[16], sum;
+    auto weights = [&]() __attribute__((always_inline)) {
+#pragma unroll
+      for (int i = 0; i < 16; ++i) p[i] = fast_exp2(fmaf(s[i], kSoftmaxScaleLog2, -m));
+      float odd = p[1];
+      sum = p[0];
+#pragma unroll
+      for (int i = 2; i < 16; i += 2) {
+        sum += p[i];
+        odd += p[i + 1];
+      }
+      sum += odd;
+    };
+    weights();
+    if (__ballot(!(sum <= kPfGrowth)) != 0ull) {
+      float top = s[0];
+#pragma unroll
+      for (int i = 1; i < 16; ++i) top = fmaxf(top, s[i]);
+      top = fmaxf(top, __shfl_xor(top, 32)) * kSoftmaxScaleLog2;
+      const float mn = fmaxf(m, top), corr = fast_exp2(m - mn);
+      m = mn;
+      l *= corr;
+#pragma unroll
+      for (int c = 0; c < 4; ++c)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) o[c][i] *= corr;
+      weights();
+    }
+    l += sum;
+    uint32_t w[2][8];  // the weights' two terms
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      w[0][i] = BF16::round2(p[2 * i], p[2 * i + 1]);
+      w[1][i] = BF16::round2(p[2 * i] - __uint_as_float(w[0][i] << 16), p[2 * i + 1] - __uint_as_float(w[0][i] & 0xffff0000u));
+    }
+#pragma unroll
+    for (int ks = 0; ks < 2; ++ks)
+#pragma unroll
+      for (int t = 0; t < 2; ++t)
+#pragma unroll
+        for (int c = 0; c < 4; ++c)
+          o[c] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
+              va[ks][c], __builtin_bit_cast(am_bf16x8_t, make_uint4(w[t][4 * ks], w[t][4 * ks + 1], w[t][4 * ks + 2], w[t][4 * ks + 3])), o[c], 0, 0, 0);
+  };
+
+  if (s0 < s1) {
+    load(s0);
+    store(0);
+    __syncthreads();
+    for (int t = s0; t < s1; ++t) {
+      if (t + 1 < s1) load(t + 1);
+      const char* base = smem + ((t - s0) & 1) * 2 * kTileBytes;
+      const SpanStep whole = span_step(steps, rows, t);
+#pragma unroll
+      for (int s = 0; s < kSteps; ++s) {
+        const int key = (s * WK + wk) * 32;
+        const SpanStep st{whole.at + key, whole.lo, whole.hi};
+        // (all uniform for the wave)
+        if (st.at >= min(st.hi, own.hi) || st.at + 32 <= st.lo || (st.at + 32 <= own.lo && st.at >= a.sinks)) continue;
+        if (span_full(a, own, st, 32))
+          step(base + key * 256, st, std::false_type{});
+        else
+          step(base + key * 256, st, std::true_type{});
+      }
+      if (t + 1 < s1) store((t + 1 - s0) & 1);
+      __syncthreads();
+    }
+  }
+
+  // both halves of a query's keys; then the waves that had other keys of the same queries
+  l += __shfl_xor(l, 32);
+  if constexpr (WK > 1) {
+    float2* ml = reinterpret_cast<float2*>(smem);                   // [wave][32] (max, sum)
+    float4* ob = reinterpret_cast<float4*>(smem + WAVES * 32 * 8);  // [wave of the upper half][4][4][lane]
+    if (half == 0) ml[wave * 32 + l32] = make_float2(m, l);
+    __syncthreads();
+    float mn = kNegBig, ls = 0.f;
+#pragma unroll
+    for (int w = 0; w < WK; ++w) mn = fmaxf(mn, ml[(w * WQ + wq) * 32 + l32].x);
+#pragma unroll
+    for (int w = 0; w < WK; ++w) {
+      const float2 x = ml[(w * WQ + wq) * 32 + l32];
+      ls = fmaf(x.y, fast_exp2(x.x - mn), ls);
+    }
+    const float f = fast_exp2(m - mn);
+    m = mn;
+    l = ls;
+#pragma unroll
+    for (int c = 0; c < 4; ++c)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) o[c][i] *= f;
+#pragma unroll
+    for (int n = WK / 2; n >= 1; n /= 2) {
+      if (wk >= n && wk < 2 * n) {
+        float4* dst = ob + ((wk - n) * WQ + wq) * 16 * 64;
+#pragma unroll
+        for (int c = 0; c < 4; ++c)
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+            dst[(c * 4 + i) * 64 + lane] = make_float4(o[c][4 * i], o[c][4 * i + 1], o[c][4 * i + 2], o[c][4 * i + 3]);
+      }
+      __syncthreads();
+      if (wk < n) {
+        const float4* src = ob + (wk * WQ + wq) * 16 * 64;
+#pragma unroll
+        for (int c = 0; c < 4; ++c)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const float4 x = src[(c * 4 + i) * 64 + lane];
+            o[c][4 * i] += x.x;
+            o[c][4 * i + 1] += x.y;
+            o[c][4 * i + 2] += x.z;
+            o[c][4 * i + 3] += x.w;
+          }
+      }
+      __syncthreads();
+    }
+    if (wk != 0) return;
+  }
+  if (len == 0) l = 0.f;  // (a padded token's lanes took whatever full steps gave)
+  const float inv = l > 0.f ? 1.0f / l : 0.f;  // (a token without rows: zeros)
+  const bool parts = a.nsplit > 1;
+  // a lane has four columns of one query at a time: through LDS, so that a store takes four half rows
+  char* at = smem + wave * 8192;  // [32 queries][64 columns], 16-byte chunks exchanged as the keys'
+#pragma unroll
+  for (int pass = 0; pass < 2; ++pass) {
+#pragma unroll
+    for (int c = 0; c < 2; ++c)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const sp_f32x16_t& x = o[2 * pass + c];
+        const float f = parts ? 1.0f : inv;
+        *reinterpret_cast<float4*>(at + l32 * 256 + (((8 * c + 2 * i + half) ^ l16) * 16)) = make_float4(x[4 * i] * f, x[4 * i + 1] * f, x[4 * i + 2] * f, x[4 * i + 3] * f);
+      }
+    __builtin_amdgcn_wave_barrier();
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      const int r = 4 * j + (lane >> 4);
+      const float4 x = *reinterpret_cast<const float4*>(at + r * 256 + ((l16 ^ (r & 15)) * 16));
+      if (q0 + r < live) {
+        const long long place = span_place(a, tile.b, tile.h, r0 + q0 + r);
+        if (parts)
+          *reinterpret_cast<float4*>(a.partial + (place * a.nsplit + tile.split) * kPartStride + 64 * pass + 4 * l16) = x;
+        else
+          *reinterpret_cast<uint2*>(static_cast<uint16_t*>(a.out) + place * kD + 64 * pass + 4 * l16) = make_uint2(BF16::round2(x.x, x.y), BF16::round2(x.z, x.w));
+      }
+    }
+    __builtin_amdgcn_wave_barrier();
+  }
+  if (parts && half == 0 && row < live)
+    *reinterpret_cast<float2*>(a.partial + (span_place(a, tile.b, tile.h, r0 + row) * a.nsplit + tile.split) * kPartStride + kD) = make_float2(m, l);
+}
+
+template <int WAVES, int WQ>
+static hipError_t launch_tiles(const SpanArgs& a, dim3 grid, hipStream_t st) {
+  static std::atomic<unsigned long long> raised{0};
+  constexpr int bytes = span_lds_bytes<WAVES, WQ>();
+  const hipError_t e = allow_dynamic_lds(reinterpret_cast<const void*>(&span_tiles_kernel<WAVES, WQ>), bytes, raised);
+  if (e != hipSuccess) return e;
+  hipLaunchKernelGGL((span_tiles_kernel<WAVES, WQ>), grid, dim3(64 * WAVES), bytes, st, a);
+  return hipGetLastError();
+}
+
 // ---- parts joined ---------------------------------------------------------------------------------------------------
 // 32 lanes take a query row, 16 bytes of each of its parts.
 template <typename T>
@@ -307,12 +574,15 @@ SpanPlan span_plan(const Shape& s, int m, int window, int sinks, bool bits4) {
   SpanPlan p{16, 0, 1};
   const long long M = (long long)m * s.G;
   if (s.dtype == 0 && !bits4 && M > 16) p.rows = 32;
+  const bool lds = s.dtype == 1 && !bits4 && M > 16;
+  if (lds) p.rows = M <= 32 ? 32 : M <= 64 ? 64 : M <= 128 ? 128 : 256;
   p.tiles = (int)((M + p.rows - 1) / p.rows);
-  // rows of a tile at most, and the parts of at least 128 of them that give every CU two blocks
+  // rows of a tile at most, and the parts of at least `least` of them that give every CU two blocks, or one of the larger
   const long long most = window > 0 ? (long long)window + sinks + (p.rows + s.G - 1) / s.G + 32 : s.S;
   const long long read = most < s.S ? most : s.S, blocks = (long long)s.B * s.Hkv * p.tiles;
-  long long n = (2LL * device_cus() + blocks - 1) / blocks;
-  if (n > (read + 127) / 128) n = (read + 127) / 128;
+  const int least = lds ? 256 : 128;
+  long long n = ((lds ? 1LL : 2LL) * device_cus() + blocks - 1) / blocks;
+  if (n > (read + least - 1) / least) n = (read + least - 1) / least;
   p.nsplit = n < 1 ? 1 : (int)n;
   return p;
 }
@@ -332,6 +602,14 @@ hipError_t launch_span(const Shape& s, SpanArgs a, hipStream_t st) {
   hipError_t e = hipSuccess;
   if (bits4)
     e = launch_span_q4(s, a, plan.rows, st);
+  else if (s.dtype == 1 && plan.rows == 32)
+    e = launch_tiles<4, 1>(a, grid, st);
+  else if (s.dtype == 1 && plan.rows == 64)
+    e = launch_tiles<8, 2>(a, grid, st);
+  else if (s.dtype == 1 && plan.rows == 128)
+    e = launch_tiles<8, 4>(a, grid, st);
+  else if (s.dtype == 1 && plan.rows == 256)
+    e = launch_tiles<8, 8>(a, grid, st);
   else if (s.dtype == 1)
     hipLaunchKernelGGL(span_rows_kernel, grid, block, 0, st, a);
   else if (plan.rows == 16)
