@@ -356,8 +356,8 @@ __global__ __launch_bounds__(64 * WAVES, WAVES == 4 ? 1 : 2) void span_tiles_ker
   const int v_row = 4 * half + (l16 >> 2);
   const int v_at = kTileBytes + v_row * 256 + (((((lane >> 4) & 1) * 2 + ((l16 & 3) >> 1)) ^ ((v_row & 3) << 2)) * 16) + (l16 & 1) * 8;
 
-  // 32 keys of the tile in buffer `base`, rows st.at ..; MASKED: each query on its own
-  auto step = [&](const char* base, const SpanStep& st, auto masked) __attribute__((always_inline)) {
+  // 32 keys of the tile in buffer `base`, rows st.at ..; full: all of them are seen by all of the wave's queries
+  auto step = [&](const char* base, const SpanStep& st, bool full) __attribute__((always_inline)) {
     am_bf16x8_t ka[8], va[2][4];
 #pragma unroll
     for (int ks = 0; ks < 8; ++ks) ka[ks] = __builtin_bit_cast(am_bf16x8_t, *reinterpret_cast<const uint4*>(base + (k_at ^ (ks * 32))));
@@ -375,7 +375,7 @@ __global__ __launch_bounds__(64 * WAVES, WAVES == 4 ? 1 : 2) void span_tiles_ker
 #pragma unroll
     for (int ks = 0; ks < 8; ++ks) s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(ka[ks], q[ks], s, 0, 0, 0);
     __builtin_amdgcn_sched_barrier(0);
-    if constexpr (decltype(masked)::value) {
+    if (!full) {  // (uniform)
 #pragma unroll
       for (int i = 0; i < 16; ++i)
         if (!span_sees(a, st, len, st.at + 8 * (i >> 2) + 4 * half + (i & 3))) s[i] = kUnseen;
@@ -433,16 +433,13 @@ __global__ __launch_bounds__(64 * WAVES, WAVES == 4 ? 1 : 2) void span_tiles_ker
       if (t + 1 < s1) load(t + 1);
       const char* base = smem + ((t - s0) & 1) * 2 * kTileBytes;
       const SpanStep whole = span_step(steps, rows, t);
-#pragma unroll
+#pragma unroll 1
       for (int s = 0; s < kSteps; ++s) {
         const int key = (s * WK + wk) * 32;
         const SpanStep st{whole.at + key, whole.lo, whole.hi};
         // (all uniform for the wave)
         if (st.at >= min(st.hi, own.hi) || st.at + 32 <= st.lo || (st.at + 32 <= own.lo && st.at >= a.sinks)) continue;
-        if (span_full(a, own, st, 32))
-          step(base + key * 256, st, std::false_type{});
-        else
-          step(base + key * 256, st, std::true_type{});
+        step(base + key * 256, st, span_full(a, own, st, 32));
       }
       if (t + 1 < s1) store((t + 1 - s0) & 1);
       __syncthreads();
