@@ -307,12 +307,12 @@ struct SpanArgs {
   float* partial;         // [B m Hq][nsplit] parts, with more than one split
   const int32_t* lens;    // [B, m] or null: S_max less the tokens behind
   int B, m, G, Hq, Hkv, S_max, window, sinks;
-  int tiles, nsplit;      // tiles of query rows of a sequence and KV head; parts of a tile's rows
+  int tiles, nsplit, run; // tiles of query rows of a sequence and KV head; parts of a tile's rows at most, and the rows of one
 };
 // How a call is cut: the workspace's size and the launch go by it.
 struct SpanPlan {
   int rows;   // query rows of a tile
-  int tiles, nsplit;
+  int tiles, nsplit, run;
 };
 SpanPlan span_plan(const Shape& s, int m, int window, int sinks, bool bits4);
 hipError_t launch_span(const Shape& s, SpanArgs a, hipStream_t st);

@@ -25,7 +25,12 @@ __global__ __launch_bounds__(64 * kSpWaves) void span_rows_kernel(SpanArgs a) {
   const int M = a.m * a.G, r0 = tile.tile * 16, live = min(16, M - r0), lg = 31 - __builtin_clz(a.G);
   const SpanRows rows = span_rows(a, tile.b, r0 >> lg, (r0 + live - 1) >> lg);
   const SpanSteps<KEYS> steps(rows);
-  const int each = (steps.total + a.nsplit - 1) / a.nsplit, s1 = min(steps.total, (tile.split + 1) * each);
+  const SpanRun<KEYS> run(a, steps, tile.split);
+  const int s1 = run.s1;
+  if (run.s0 >= s1 && tile.split > 0) {  // (uniform for the block)
+    span_none(a, tile, r0, live);
+    return;
+  }
   const RowPlaces places(a.cache, tile.b, tile.h, a.Hkv);
   const int len = r16 < live ? span_len(a, tile.b, (r0 + r16) >> lg) : 0;
 
@@ -60,7 +65,7 @@ __global__ __launch_bounds__(64 * kSpWaves) void span_rows_kernel(SpanArgs a) {
     for (int e = 0; e < 8; ++e)
       vraw[e] = load16(vb + (place[e / 4] + min(max(st.at + 16 * (e / 4) + 4 * kgrp + e % 4, st.lo), st.hi - 1)) * (kD * 2));
   };
-  int s = tile.split * each + wave;
+  int s = run.s0 + wave;
   if (s < s1) {  // (uniform for the wave)
     const SpanStep st = span_step(steps, rows, s);
     find(st);
@@ -152,7 +157,12 @@ __global__ __launch_bounds__(64 * kSpWaves, 2) void span_f32_kernel(SpanArgs a) 
   const int M = a.m * a.G, r0 = tile.tile * (16 * QG), live = min(16 * QG, M - r0), lg = 31 - __builtin_clz(a.G);
   const SpanRows rows = span_rows(a, tile.b, r0 >> lg, (r0 + live - 1) >> lg);
   const SpanSteps<KEYS> steps(rows);
-  const int each = (steps.total + a.nsplit - 1) / a.nsplit, s1 = min(steps.total, (tile.split + 1) * each);
+  const SpanRun<KEYS> run(a, steps, tile.split);
+  const int s1 = run.s1;
+  if (run.s0 >= s1 && tile.split > 0) {  // (uniform for the block)
+    span_none(a, tile, r0, live);
+    return;
+  }
   const RowPlaces places(a.cache, tile.b, tile.h, a.Hkv);
 
   int len[QG];
@@ -188,7 +198,7 @@ __global__ __launch_bounds__(64 * kSpWaves, 2) void span_f32_kernel(SpanArgs a) 
       vr[i][1] = *reinterpret_cast<const float4*>(p + 64);
     }
   };
-  int s = tile.split * each + wave;
+  int s = run.s0 + wave;
   if (s < s1) {  // (uniform for the wave)
     const SpanStep st = span_step(steps, rows, s);
     place = places(min(max(st.at, st.lo), st.hi - 1));
@@ -285,8 +295,6 @@ typedef short sp_s16x4_t __attribute__((ext_vector_type(4)));
 typedef float sp_f32x16_t __attribute__((ext_vector_type(16)));
 typedef __attribute__((address_space(3))) sp_s16x4_t sp_lds_s16x4_t;
 
-constexpr float kUnseen = -3.0e38f;  // a logit that no maximum follows and whose weight is 0 whatever the maximum is
-
 template <int WAVES, int WQ>
 constexpr int span_tile_keys() {
   return WAVES / WQ == 4 ? 128 : 64;
@@ -311,7 +319,12 @@ __global__ __launch_bounds__(64 * WAVES, WAVES == 4 ? 1 : 2) void span_tiles_ker
   const int M = a.m * a.G, r0 = tile.tile * (32 * WQ), live = min(32 * WQ, M - r0), lg = 31 - __builtin_clz(a.G);
   const SpanRows rows = span_rows(a, tile.b, r0 >> lg, (r0 + live - 1) >> lg);
   const SpanSteps<KT> steps(rows);
-  const int each = (steps.total + a.nsplit - 1) / a.nsplit, s0 = tile.split * each, s1 = min(steps.total, s0 + each);
+  const SpanRun<KT> run(a, steps, tile.split);
+  const int s0 = run.s0, s1 = run.s1;
+  if (s0 >= s1 && tile.split > 0) {  // (uniform for the block)
+    span_none(a, tile, r0, live);
+    return;
+  }
   const RowPlaces places(a.cache, tile.b, tile.h, a.Hkv);
   // this wave's queries, and its lane's
   const int q0 = wq * 32, mine = min(32, live - q0), row = q0 + l32;
@@ -541,50 +554,104 @@ static hipError_t launch_tiles(const SpanArgs& a, dim3 grid, hipStream_t st) {
 }
 
 // ---- parts joined ---------------------------------------------------------------------------------------------------
-// 32 lanes take a query row, 16 bytes of each of its parts.
-template <typename T>
+// 32 lanes take a query row, 16 bytes of each of its parts; GROUPS of them share a row's parts, four each at a time.
+template <typename T, int GROUPS>
 __global__ __launch_bounds__(256) void span_merge_kernel(const float* __restrict__ partial, typename T::store_t* __restrict__ out,
                                                          long long rows, int nsplit) {
-  const long long r = (long long)blockIdx.x * 8 + (threadIdx.x >> 5);
-  const int lane = threadIdx.x & 31;
-  if (r >= rows) return;
-  float mn = kNegBig, ls = 0.f;
-  float4 os = make_float4(0.f, 0.f, 0.f, 0.f);
-  for (int i = 0; i < nsplit; ++i) {
-    const float* p = partial + (r * nsplit + i) * kPartStride;
-    const float2 ml = *reinterpret_cast<const float2*>(p + kD);
-    const float4 x = *reinterpret_cast<const float4*>(p + 4 * lane);
-    const float top = fmaxf(mn, ml.x), c = fast_exp2(mn - top), f = fast_exp2(ml.x - top);
-    mn = top;
-    ls = fmaf(ls, c, ml.y * f);
-    os = make_float4(fmaf(os.x, c, x.x * f), fmaf(os.y, c, x.y * f), fmaf(os.z, c, x.z * f), fmaf(os.w, c, x.w * f));
+  constexpr int U = 4;
+  __shared__ __align__(16) float s_o[GROUPS > 1 ? GROUPS : 1][kD];
+  __shared__ float2 s_ml[GROUPS];
+  const int lane = threadIdx.x & 31, grp = threadIdx.x >> 5;
+  const long long r = GROUPS > 1 ? (long long)blockIdx.x : (long long)blockIdx.x * 8 + grp;
+  if (GROUPS == 1 && r >= rows) return;
+  float m = kNegBig, l = 0.f;
+  float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+  for (int i0 = GROUPS > 1 ? grp : 0; i0 < nsplit; i0 += GROUPS * U) {
+    float2 ml[U];
+    float4 x[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int i = i0 + u * GROUPS;
+      const float* p = partial + (r * nsplit + (i < nsplit ? i : i0)) * kPartStride;
+      ml[u] = *reinterpret_cast<const float2*>(p + kD);
+      x[u] = *reinterpret_cast<const float4*>(p + 4 * lane);
+      if (i >= nsplit) ml[u] = make_float2(kNegBig, 0.f);
+    }
+    float mn = m;
+#pragma unroll
+    for (int u = 0; u < U; ++u) mn = fmaxf(mn, ml[u].x);
+    const float c = fast_exp2(m - mn);
+    m = mn;
+    l *= c;
+    o = make_float4(o.x * c, o.y * c, o.z * c, o.w * c);
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const float f = fast_exp2(ml[u].x - mn);
+      if (ml[u].y > 0.f) {  // (a part without rows has no outputs)
+        l = fmaf(ml[u].y, f, l);
+        o = make_float4(fmaf(x[u].x, f, o.x), fmaf(x[u].y, f, o.y), fmaf(x[u].z, f, o.z), fmaf(x[u].w, f, o.w));
+      }
+    }
   }
-  const float inv = ls > 0.f ? 1.0f / ls : 0.f;  // (a token without rows: zeros)
+  if constexpr (GROUPS > 1) {
+    *reinterpret_cast<float4*>(&s_o[grp][4 * lane]) = o;
+    if (lane == 0) s_ml[grp] = make_float2(m, l);
+    __syncthreads();
+    if (grp != 0) return;
+    float mn = kNegBig;
+#pragma unroll
+    for (int g = 0; g < GROUPS; ++g) mn = fmaxf(mn, s_ml[g].x);
+    l = 0.f;
+    o = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+    for (int g = 0; g < GROUPS; ++g) {
+      const float f = fast_exp2(s_ml[g].x - mn);
+      const float4 x = *reinterpret_cast<const float4*>(&s_o[g][4 * lane]);
+      l = fmaf(s_ml[g].y, f, l);
+      o = make_float4(fmaf(x.x, f, o.x), fmaf(x.y, f, o.y), fmaf(x.z, f, o.z), fmaf(x.w, f, o.w));
+    }
+  }
+  const float inv = l > 0.f ? 1.0f / l : 0.f;  // (a token without rows: zeros)
   if constexpr (T::EPC == 8)
-    *reinterpret_cast<uint2*>(out + r * kD + 4 * lane) = make_uint2(BF16::round2(os.x * inv, os.y * inv), BF16::round2(os.z * inv, os.w * inv));
+    *reinterpret_cast<uint2*>(out + r * kD + 4 * lane) = make_uint2(BF16::round2(o.x * inv, o.y * inv), BF16::round2(o.z * inv, o.w * inv));
   else
-    *reinterpret_cast<float4*>(out + r * kD + 4 * lane) = make_float4(os.x * inv, os.y * inv, os.z * inv, os.w * inv);
+    *reinterpret_cast<float4*>(out + r * kD + 4 * lane) = make_float4(o.x * inv, o.y * inv, o.z * inv, o.w * inv);
 }
 
 // ---- the launch -----------------------------------------------------------------------------------------------------
 SpanPlan span_plan(const Shape& s, int m, int window, int sinks, bool bits4) {
-  SpanPlan p{16, 0, 1};
+  SpanPlan p{16, 0, 1, 0};
   const long long M = (long long)m * s.G;
-  if (s.dtype == 0 && !bits4 && M > 16) p.rows = 32;
   const bool lds = s.dtype == 1 && !bits4 && M > 16;
-  if (lds) p.rows = M <= 32 ? 32 : M <= 64 ? 64 : M <= 128 ? 128 : 256;
+  if (lds)
+    p.rows = M <= 32 ? 32 : M <= 64 ? 64 : M <= 128 ? 128 : 256;
+  else if (bits4)
+    p.rows = M <= 4 ? 4 : M <= 8 && s.dtype == 1 ? 8 : M <= 16 ? 16 : 32;
+  else if (s.dtype == 0 && M > 16)
+    p.rows = 32;
   p.tiles = (int)((M + p.rows - 1) / p.rows);
-  // rows of a tile at most, and the parts of at least `least` of them that give every CU two blocks, or one of the larger
-  const long long most = window > 0 ? (long long)window + sinks + (p.rows + s.G - 1) / s.G + 32 : s.S;
-  const long long read = most < s.S ? most : s.S, blocks = (long long)s.B * s.Hkv * p.tiles;
+  // a tile's rows at most: its tokens' windows and the sinks
+  const long long tokens = p.rows < M ? (p.rows + s.G - 1) / s.G + 1 : m, most = (long long)window + tokens - 1 + sinks;
+  const long long read = window > 0 && most < s.S ? most : s.S, blocks = (long long)s.B * s.Hkv * p.tiles;
   const int least = lds ? 256 : 128;
   long long n = ((lds ? 1LL : 2LL) * device_cus() + blocks - 1) / blocks;
   if (n > (read + least - 1) / least) n = (read + least - 1) / least;
-  p.nsplit = n < 1 ? 1 : (int)n;
+  p.run = (int)((read + n - 1) / n);
+  p.nsplit = (int)n;
   return p;
 }
 
 hipError_t launch_span_q4(const Shape& s, const SpanArgs& a, int rows, hipStream_t st);
+
+template <typename T>
+static void launch_span_merge(const SpanArgs& a, hipStream_t st) {
+  const long long rows = (long long)a.B * a.m * a.Hq;
+  auto* out = static_cast<typename T::store_t*>(a.out);
+  if (a.nsplit <= 4)
+    hipLaunchKernelGGL((span_merge_kernel<T, 1>), dim3((unsigned)((rows + 7) / 8)), dim3(256), 0, st, a.partial, out, rows, a.nsplit);
+  else
+    hipLaunchKernelGGL((span_merge_kernel<T, 8>), dim3((unsigned)rows), dim3(256), 0, st, a.partial, out, rows, a.nsplit);
+}
 
 hipError_t launch_span(const Shape& s, SpanArgs a, hipStream_t st) {
   const bool bits4 = a.cache.k_scales != nullptr;
@@ -595,32 +662,31 @@ hipError_t launch_span(const Shape& s, SpanArgs a, hipStream_t st) {
   }
   a.tiles = plan.tiles;
   a.nsplit = plan.nsplit;
+  a.run = plan.run;
   const dim3 grid((unsigned)((long long)a.B * a.Hkv * a.tiles * a.nsplit)), block(64 * kSpWaves);
   hipError_t e = hipSuccess;
   if (bits4)
     e = launch_span_q4(s, a, plan.rows, st);
-  else if (s.dtype == 1 && plan.rows == 32)
-    e = launch_tiles<4, 1>(a, grid, st);
-  else if (s.dtype == 1 && plan.rows == 64)
-    e = launch_tiles<8, 2>(a, grid, st);
-  else if (s.dtype == 1 && plan.rows == 128)
-    e = launch_tiles<8, 4>(a, grid, st);
-  else if (s.dtype == 1 && plan.rows == 256)
-    e = launch_tiles<8, 8>(a, grid, st);
-  else if (s.dtype == 1)
-    hipLaunchKernelGGL(span_rows_kernel, grid, block, 0, st, a);
-  else if (plan.rows == 16)
+  else if (s.dtype == 0 && plan.rows == 16)
     hipLaunchKernelGGL((span_f32_kernel<1>), grid, block, 0, st, a);
-  else
+  else if (s.dtype == 0)
     hipLaunchKernelGGL((span_f32_kernel<2>), grid, block, 0, st, a);
+  else if (plan.rows == 16)
+    hipLaunchKernelGGL(span_rows_kernel, grid, block, 0, st, a);
+  else if (plan.rows == 32)
+    e = launch_tiles<4, 1>(a, grid, st);
+  else if (plan.rows == 64)
+    e = launch_tiles<8, 2>(a, grid, st);
+  else if (plan.rows == 128)
+    e = launch_tiles<8, 4>(a, grid, st);
+  else
+    e = launch_tiles<8, 8>(a, grid, st);
   if (e == hipSuccess) e = hipGetLastError();
   if (e != hipSuccess || a.nsplit == 1) return e;
-  const long long rows = (long long)a.B * a.m * a.Hq;
-  const dim3 merge((unsigned)((rows + 7) / 8));
   if (s.dtype == 0)
-    hipLaunchKernelGGL((span_merge_kernel<F32>), merge, dim3(256), 0, st, a.partial, static_cast<float*>(a.out), rows, a.nsplit);
+    launch_span_merge<F32>(a, st);
   else
-    hipLaunchKernelGGL((span_merge_kernel<BF16>), merge, dim3(256), 0, st, a.partial, static_cast<uint16_t*>(a.out), rows, a.nsplit);
+    launch_span_merge<BF16>(a, st);
   return hipGetLastError();
 }
 

@@ -12,6 +12,8 @@
 
 namespace loki {
 
+constexpr float kUnseen = -3.0e38f;  // a logit that no maximum follows and whose weight is 0 whatever the maximum is
+
 struct SpanTile {
   int b, h, tile, split;
 };
@@ -77,10 +79,28 @@ __device__ __forceinline__ bool span_full(const SpanArgs& a, const SpanRows& r, 
   return st.at >= st.lo && st.at + keys <= min(st.hi, r.len_min) && (st.at >= r.hi - a.window || st.at + keys <= a.sinks);
 }
 
+// The steps of this block's run: the same number for every tile, so that blocks have equal work whatever the lengths; a tile has as many
+// runs as its rows fill (more rows than expected, of tokens that do not lie next to each other, make its runs longer).
+template <int KEYS>
+struct SpanRun {
+  int s0, s1;
+  __device__ __forceinline__ SpanRun(const SpanArgs& a, const SpanSteps<KEYS>& n, int split) {
+    const int each = max((a.run + KEYS - 1) / KEYS, (n.total + a.nsplit - 1) / a.nsplit);
+    s0 = split * each;
+    s1 = min(n.total, s0 + each);
+  }
+};
+
 // Query row r of a sequence: its place among the rows of q, of out and of the parts.
 __device__ __forceinline__ long long span_place(const SpanArgs& a, int b, int h, int r) {
   const int j = r >> (31 - __builtin_clz(a.G));
   return ((long long)b * a.m + j) * a.Hq + h * a.G + (r & (a.G - 1));
+}
+
+// A run that no row is left for: its parts say so, which the merge asks for in front of their outputs.
+__device__ __forceinline__ void span_none(const SpanArgs& a, const SpanTile& tile, int r0, int live) {
+  for (int r = threadIdx.x; r < live; r += blockDim.x)
+    *reinterpret_cast<float2*>(a.partial + (span_place(a, tile.b, tile.h, r0 + r) * a.nsplit + tile.split) * kPartStride + kD) = make_float2(kNegBig, 0.f);
 }
 
 // A wave's state after its steps, for 16 query rows: lane (row r16, kgrp) holds maximum m and sum l of its row (l its own share of the

@@ -30,6 +30,229 @@ __device__ __forceinline__ void q4_terms(float x0, float x1, uint32_t (&w)[TERMS
   }
 }
 
+// Up to 4 NS query rows, as most calls with one token have.  Lane n = 4 r + g of the matrix cores' 16 columns is row r in group g, NS sets of them:
+//   first product   column n holds q[r] in the columns of group g and zeros elsewhere, so that the four products add up to each lane's own
+//                   group's sum, which takes one step and one lowest for a row; the four lanes of a query add theirs (DPP)
+//   second          column n holds p step_g, so a lane forms its own group's only; it keeps the two output tiles of its group
+// which leaves a quarter of the scaling and of the splitting into terms that whole columns for a query would ask of every lane: 24
+// vector instructions a row of keys and values for all 64 lanes against 40 of the kernel below.
+template <typename T, int NS>
+__global__ __launch_bounds__(64 * kQ4Waves, 2) void span_q4_few_kernel(SpanArgs a) {
+  constexpr int KEYS = 32, QT = T::EPC == 8 ? 1 : 3, PT = T::EPC == 8 ? 2 : 3, ROWS = 4 * NS;
+  __shared__ __align__(16) SpanMerge<ROWS, kQ4Waves> sm;
+  const SpanTile tile = span_tile(a);
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), r16 = lane & 15, kgrp = lane >> 4;
+  const int g = r16 & 3, hd = r16 >> 2;
+  const int M = a.m * a.G, r0 = tile.tile * ROWS, live = min(ROWS, M - r0), lg = 31 - __builtin_clz(a.G);
+  const SpanRows rows = span_rows(a, tile.b, r0 >> lg, (r0 + live - 1) >> lg);
+  const SpanSteps<KEYS> steps(rows);
+  const SpanRun<KEYS> run(a, steps, tile.split);
+  const int s1 = run.s1;
+  if (run.s0 >= s1 && tile.split > 0) {  // (uniform for the block)
+    span_none(a, tile, r0, live);
+    return;
+  }
+  const RowPlaces places(a.cache, tile.b, tile.h, a.Hkv);
+
+  const char *kb = static_cast<const char*>(a.cache.k), *vb = static_cast<const char*>(a.cache.v);
+  const char *ks = static_cast<const char*>(a.cache.k_scales), *vs = static_cast<const char*>(a.cache.v_scales);
+  const unsigned k_at = r16 * kQ4RowBytes + 16 * kgrp, v_at = 4 * kgrp * kQ4RowBytes + 4 * r16, s_at = 4 * kgrp * kQ4ScaleBytes + 4 * g;
+  uint4 kraw[2];
+  uint32_t ksc[8], vsc[8], vraw[8];
+  long long place[2];
+  auto find = [&](const SpanStep& st) __attribute__((always_inline)) {
+#pragma unroll
+    for (int t = 0; t < 2; ++t) place[t] = places(min(max(st.at + 16 * t, st.lo), st.hi - 1));
+  };
+  // The rows of a step, from uniform addresses; a step that the range's end cuts takes the range's own rows again for those outside.
+  auto load = [&](const SpanStep& st, auto values) __attribute__((always_inline)) {
+    const char *codes = decltype(values)::value ? vb : kb, *scales = decltype(values)::value ? vs : ks;
+    uint32_t(&sc)[8] = decltype(values)::value ? vsc : ksc;
+    if (st.at >= st.lo && st.at + KEYS <= st.hi) {  // (uniform)
+#pragma unroll
+      for (int t = 0; t < 2; ++t) {
+        const char *c = codes + (place[t] + st.at + 16 * t) * kQ4RowBytes, *x = scales + (place[t] + st.at + 16 * t) * kQ4ScaleBytes;
+        if constexpr (!decltype(values)::value) kraw[t] = load16(c + k_at);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          sc[4 * t + i] = *reinterpret_cast<const uint32_t*>(x + s_at + i * kQ4ScaleBytes);
+          if constexpr (decltype(values)::value) vraw[4 * t + i] = *reinterpret_cast<const uint32_t*>(c + v_at + i * kQ4RowBytes);
+        }
+      }
+    } else {
+#pragma unroll
+      for (int t = 0; t < 2; ++t) {
+        if constexpr (!decltype(values)::value)
+          kraw[t] = load16(codes + (place[t] + min(max(st.at + 16 * t + r16, st.lo), st.hi - 1)) * kQ4RowBytes + 16 * kgrp);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const long long row = place[t] + min(max(st.at + 16 * t + 4 * kgrp + i, st.lo), st.hi - 1);
+          sc[4 * t + i] = *reinterpret_cast<const uint32_t*>(scales + row * kQ4ScaleBytes + 4 * g);
+          if constexpr (decltype(values)::value) vraw[4 * t + i] = *reinterpret_cast<const uint32_t*>(codes + row * kQ4RowBytes + 4 * r16);
+        }
+      }
+    }
+  };
+  int s = run.s0 + wave;
+  if (s < s1) {  // (uniform for the wave)
+    const SpanStep st = span_step(steps, rows, s);
+    find(st);
+    load(st, std::false_type{});
+    load(st, std::true_type{});
+    find(span_step(steps, rows, min(s + kQ4Waves, steps.total - 1)));
+  }
+
+  int len[NS];
+  am_bf16x8_t bq[NS][kQ4Groups][QT];
+  float qsum[NS], m[NS], l[NS], low[NS], ones[NS];  // qsum: of the group's columns
+  am_f32x4_t o[NS][8];
+#pragma unroll
+  for (int u = 0; u < NS; ++u) {
+    const int r = 4 * u + hd;
+    len[u] = r < live ? span_len(a, tile.b, (r0 + r) >> lg) : 0;
+    const typename T::store_t* src =
+        static_cast<const typename T::store_t*>(a.q) + span_place(a, tile.b, tile.h, r0 + min(r, live - 1)) * kD + 32 * g + 8 * kgrp;
+    float x[8];
+#pragma unroll
+    for (int e = 0; e < 8; e += T::EPC) T::unpack(load16(src + e), *reinterpret_cast<float(*)[T::EPC]>(x + e));
+    uint32_t w[4][QT];
+    float sum = 0.f;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      q4_terms<QT>(x[2 * i], x[2 * i + 1], w[i]);
+      sum += x[2 * i] + x[2 * i + 1];
+    }
+#pragma unroll
+    for (int G = 0; G < kQ4Groups; ++G)
+#pragma unroll
+      for (int t = 0; t < QT; ++t)
+        bq[u][G][t] = __builtin_bit_cast(am_bf16x8_t, G == g ? make_uint4(w[0][t], w[1][t], w[2][t], w[3][t]) : make_uint4(0, 0, 0, 0));
+    sum += __shfl_xor(sum, 16);
+    qsum[u] = sum + __shfl_xor(sum, 32);
+    m[u] = kNegBig;
+    l[u] = low[u] = ones[u] = 0.f;
+#pragma unroll
+    for (int c = 0; c < 8; ++c) o[u][c] = am_f32x4_t{};
+  }
+
+  for (; s < s1; s += kQ4Waves) {
+    const SpanStep st = span_step(steps, rows, s), next = span_step(steps, rows, min(s + kQ4Waves, steps.total - 1));
+    float x[NS][8];  // a sixteenth of the logits
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+      am_f32x4_t acc[NS];
+#pragma unroll
+      for (int u = 0; u < NS; ++u) acc[u] = am_f32x4_t{-qsum[u], -qsum[u], -qsum[u], -qsum[u]};
+#pragma unroll
+      for (int G = 0; G < kQ4Groups; ++G) {
+        const am_bf16x8_t ka = __builtin_bit_cast(am_bf16x8_t, make_uint4(q4_pair(kraw[t].x, G), q4_pair(kraw[t].y, G), q4_pair(kraw[t].z, G), q4_pair(kraw[t].w, G)));
+#pragma unroll
+        for (int u = 0; u < NS; ++u)
+#pragma unroll
+          for (int i = QT - 1; i >= 0; --i) acc[u] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ka, bq[u][G][i], acc[u], 0, 0, 0);
+      }
+#pragma unroll
+      for (int u = 0; u < NS; ++u)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const cache_half2_t sc = __builtin_bit_cast(cache_half2_t, ksc[4 * t + i]);
+          x[u][4 * t + i] = group_allreduce_sum<4>(fmaf((float)sc.x, acc[u][i], (float)sc.y * (qsum[u] * 0.0625f)));
+        }
+    }
+    load(next, std::false_type{});
+    const bool full = span_full(a, rows, st, KEYS);
+    float p[NS][8];
+#pragma unroll
+    for (int u = 0; u < NS; ++u) {
+      if (!full) {  // (uniform)
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+          if (!span_sees(a, st, len[u], st.at + 16 * (e / 4) + 4 * kgrp + e % 4)) x[u][e] = kUnseen;
+      }
+      float sum;
+      auto weights = [&]() __attribute__((always_inline)) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) p[u][e] = fast_exp2(fmaf(x[u][e], 16.f * kSoftmaxScaleLog2, -m[u]));
+        sum = ((p[u][0] + p[u][1]) + (p[u][2] + p[u][3])) + ((p[u][4] + p[u][5]) + (p[u][6] + p[u][7]));
+      };
+      weights();
+      if (__ballot(!(sum <= kPfGrowth)) != 0ull) {
+        float top = x[u][0];
+#pragma unroll
+        for (int e = 1; e < 8; ++e) top = fmaxf(top, x[u][e]);
+        top = fmaxf(top, __shfl_xor(top, 16));
+        top = fmaxf(top, __shfl_xor(top, 32)) * (16.f * kSoftmaxScaleLog2);
+        const float mn = fmaxf(m[u], top), corr = fast_exp2(m[u] - mn);
+        m[u] = mn;
+        l[u] *= corr;
+        low[u] *= corr;
+        ones[u] *= corr;
+#pragma unroll
+        for (int c = 0; c < 8; ++c)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) o[u][c][i] *= corr;
+        weights();
+      }
+      l[u] += sum;
+    }
+    am_bf16x8_t b[NS][PT];
+#pragma unroll
+    for (int u = 0; u < NS; ++u) {
+      uint32_t w[4][PT];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const cache_half2_t sc0 = __builtin_bit_cast(cache_half2_t, vsc[2 * i]), sc1 = __builtin_bit_cast(cache_half2_t, vsc[2 * i + 1]);
+        const float p0 = p[u][2 * i], p1 = p[u][2 * i + 1], x0 = p0 * (float)sc0.x, x1 = p1 * (float)sc1.x;
+        ones[u] += x0 + x1;
+        low[u] = fmaf(p0, (float)sc0.y, fmaf(p1, (float)sc1.y, low[u]));
+        q4_terms<PT>(x0, x1, w[i]);
+      }
+#pragma unroll
+      for (int t = 0; t < PT; ++t) b[u][t] = __builtin_bit_cast(am_bf16x8_t, make_uint4(w[0][t], w[1][t], w[2][t], w[3][t]));
+    }
+#pragma unroll
+    for (int c = 0; c < 2; ++c) {
+      uint32_t y[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) y[i] = __builtin_amdgcn_perm(vraw[2 * i + 1], vraw[2 * i], c ? 0x07060302u : 0x05040100u);
+#pragma unroll
+      for (int G = 0; G < kQ4Groups; ++G) {
+        const am_bf16x8_t av = __builtin_bit_cast(am_bf16x8_t, make_uint4(q4_pair(y[0], G), q4_pair(y[1], G), q4_pair(y[2], G), q4_pair(y[3], G)));
+#pragma unroll
+        for (int u = 0; u < NS; ++u)
+#pragma unroll
+          for (int t = PT - 1; t >= 0; --t) o[u][2 * G + c] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(av, b[u][t], o[u][2 * G + c], 0, 0, 0);
+      }
+    }
+    load(next, std::true_type{});
+    find(span_step(steps, rows, min(s + 2 * kQ4Waves, steps.total - 1)));
+  }
+#pragma unroll
+  for (int u = 0; u < NS; ++u) {
+    const int r = 4 * u + hd;
+    l[u] += __shfl_xor(l[u], 16);
+    l[u] += __shfl_xor(l[u], 32);
+    if (len[u] == 0) l[u] = 0.f;  // (a padded token's lanes took whatever full steps gave)
+    if (kgrp == 0 && g == 0) sm.ml[wave][r] = make_float2(m[u], l[u]);
+    float base = low[u] - 16.f * ones[u];
+    base += __shfl_xor(base, 16);
+    base += __shfl_xor(base, 32);
+    // o[2 g + c][i] is column 32 g + 2 (4 kgrp + i) + c
+    float y[2][4];
+#pragma unroll
+    for (int c = 0; c < 2; ++c)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const float mine = g < 2 ? (g == 0 ? o[u][c][i] : o[u][2 + c][i]) : (g == 2 ? o[u][4 + c][i] : o[u][6 + c][i]);
+        y[c][i] = fmaf(16.f, mine, base);
+      }
+#pragma unroll
+    for (int i = 0; i < 4; i += 2)
+      *reinterpret_cast<float4*>(&sm.o[wave][r][32 * g + 8 * kgrp + 2 * i]) = make_float4(y[0][i], y[1][i], y[0][i + 1], y[1][i + 1]);
+  }
+  span_store<T>(a, sm, tile, r0, live);
+}
+
 // QG groups of 16 query rows.  bf16: q is one term, the weights two (2^-16 of each, as the library's other attention); fp32: three each.
 template <typename T, int QG>
 __global__ __launch_bounds__(64 * kQ4Waves) void span_q4_kernel(SpanArgs a) {
@@ -40,7 +263,12 @@ __global__ __launch_bounds__(64 * kQ4Waves) void span_q4_kernel(SpanArgs a) {
   const int M = a.m * a.G, r0 = tile.tile * (16 * QG), live = min(16 * QG, M - r0), lg = 31 - __builtin_clz(a.G);
   const SpanRows rows = span_rows(a, tile.b, r0 >> lg, (r0 + live - 1) >> lg);
   const SpanSteps<KEYS> steps(rows);
-  const int each = (steps.total + a.nsplit - 1) / a.nsplit, s1 = min(steps.total, (tile.split + 1) * each);
+  const SpanRun<KEYS> run(a, steps, tile.split);
+  const int s1 = run.s1;
+  if (run.s0 >= s1 && tile.split > 0) {  // (uniform for the block)
+    span_none(a, tile, r0, live);
+    return;
+  }
   const RowPlaces places(a.cache, tile.b, tile.h, a.Hkv);
 
   int len[QG];
@@ -102,7 +330,7 @@ __global__ __launch_bounds__(64 * kQ4Waves) void span_q4_kernel(SpanArgs a) {
       vsc[e] = load16(vs + row_of(st, e) * kQ4ScaleBytes);
     }
   };
-  int s = tile.split * each + wave;
+  int s = run.s0 + wave;
   if (s < s1) {  // (uniform for the wave)
     const SpanStep st = span_step(steps, rows, s);
     find(st);
@@ -228,13 +456,22 @@ __global__ __launch_bounds__(64 * kQ4Waves) void span_q4_kernel(SpanArgs a) {
   span_store<T>(a, sm, tile, r0, live);
 }
 
-hipError_t launch_span_q4(const Shape& s, const SpanArgs& a, int rows, hipStream_t st) {
+template <typename T>
+static hipError_t launch_span_q4_t(const SpanArgs& a, int rows, hipStream_t st) {
   const dim3 grid((unsigned)((long long)a.B * a.Hkv * a.tiles * a.nsplit)), block(64 * kQ4Waves);
-  if (s.dtype == 0)
-    hipLaunchKernelGGL((span_q4_kernel<F32, 1>), grid, block, 0, st, a);
+  if (rows == 4)
+    hipLaunchKernelGGL((span_q4_few_kernel<T, 1>), grid, block, 0, st, a);
+  else if (T::EPC == 8 && rows == 8)  // (fp32: its three terms for two sets do not fit in the registers of two waves)
+    hipLaunchKernelGGL((span_q4_few_kernel<BF16, 2>), grid, block, 0, st, a);
+  else if (rows == 16)
+    hipLaunchKernelGGL((span_q4_kernel<T, 1>), grid, block, 0, st, a);
   else
-    hipLaunchKernelGGL((span_q4_kernel<BF16, 1>), grid, block, 0, st, a);
+    hipLaunchKernelGGL((span_q4_kernel<T, 2>), grid, block, 0, st, a);
   return hipGetLastError();
+}
+
+hipError_t launch_span_q4(const Shape& s, const SpanArgs& a, int rows, hipStream_t st) {
+  return s.dtype == 0 ? launch_span_q4_t<F32>(a, rows, st) : launch_span_q4_t<BF16>(a, rows, st);
 }
 
 }  // namespace loki
