@@ -1059,9 +1059,10 @@ static int check_span(const loki_layout* layout, const loki_cache* cache, int S_
   return LOKI_OK;
 }
 // Behind the control words, which the call leaves alone (plan_workspace): the parts, where there are any.
-static size_t span_bytes(const Shape& s, const SpanArgs& a, const SpanPlan& plan) {
-  const size_t parts = plan.nsplit > 1 ? (size_t)a.B * a.m * a.Hq * plan.nsplit * kPartStride * sizeof(float) : 0;
-  return kClusterCtlBytes + align_up(parts, 256);
+static size_t span_bytes(const Shape& s, const SpanArgs& a) {
+  const SpanPlan plan = span_plan(s, a.m, a.window, a.sinks, a.cache.k_scales != nullptr);
+  const size_t parts = plan.nsplit > 1 ? (size_t)a.B * a.m * a.Hq * plan.nsplit : 0;
+  return kClusterCtlBytes + align_up(parts * kPartStride * sizeof(float), 256);
 }
 
 int dense_cache_workspace_bytes(const loki_layout* layout, const loki_cache* cache, int S_max, const loki_span_args* args, size_t* bytes) {
@@ -1070,7 +1071,7 @@ int dense_cache_workspace_bytes(const loki_layout* layout, const loki_cache* cac
   const int rc = check_span(layout, cache, S_max, args, &s, &a);
   if (rc != LOKI_OK) return rc;
   if (!bytes) return LOKI_ERR_INVALID_ARG;
-  *bytes = span_bytes(s, a, span_plan(s, a.m, a.window, a.sinks, a.cache.k_scales != nullptr));
+  *bytes = span_bytes(s, a);
   return LOKI_OK;
 }
 
@@ -1082,7 +1083,7 @@ int dense_decode_cache(const loki_layout* layout, const void* q, const loki_cach
   if (rc != LOKI_OK) return rc;
   if (!q || !out || !workspace) return LOKI_ERR_INVALID_ARG;
   if (!aligned16(q) || !aligned16(out) || !aligned256(workspace)) return LOKI_ERR_ALIGNMENT;
-  if (span_bytes(s, a, span_plan(s, a.m, a.window, a.sinks, a.cache.k_scales != nullptr)) > workspace_bytes) return LOKI_ERR_WORKSPACE;
+  if (span_bytes(s, a) > workspace_bytes) return LOKI_ERR_WORKSPACE;
   a.q = q;
   a.out = out;
   a.partial = reinterpret_cast<float*>(static_cast<char*>(workspace) + kClusterCtlBytes);

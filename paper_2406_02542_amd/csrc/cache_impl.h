@@ -20,8 +20,9 @@ typedef _Float16 cache_half2_t __attribute__((ext_vector_type(2)));
 // Entries of a page table are read with scalar loads (no launch writes a table that it reads).
 typedef const __attribute__((address_space(4))) int32_t cache_const_i32_t;
 
-// What is added to the number of a row (uniform for the wave; with pages, of a row of the same page) to get its place from the
-// start of the pool.  An entry that names no page is clamped: such rows are never part of a result, but are read.
+// Where rows of a unit lie.  entry() asks the page table (a scalar load, whose result is best not touched at once) and place() makes of
+// it what is added to the number of a row (uniform for the wave; with pages, of a row of the same page) to get its place from
+// the start of the pool.  An entry that names no page is clamped: such rows are never part of a result, but are read.
 struct RowPlaces {
   long long first;  // contiguous: row 0 of the unit
   cache_const_i32_t* table;
@@ -30,12 +31,13 @@ struct RowPlaces {
       : first(((long long)b * Hkv_ + h_) * c.S_cap),
         table(c.pg.table == nullptr ? nullptr : (cache_const_i32_t*)(c.pg.table + (long long)b * c.pg.pages_per_seq)),
         lg(c.pg.lg_rows), n_pages(c.pg.n_pages), Hkv(Hkv_), h(h_) {}
-  __device__ __forceinline__ long long operator()(int row) const {
+  __device__ __forceinline__ int entry(int row) const { return table == nullptr ? 0 : table[__builtin_amdgcn_readfirstlane(row >> lg)]; }
+  __device__ __forceinline__ long long place(int row, int entry) const {
     if (table == nullptr) return first;
     const int at = __builtin_amdgcn_readfirstlane(row >> lg);
-    const int page = min(max(table[at], 0), n_pages - 1);
-    return ((long long)page * Hkv + h - at) << lg;
+    return ((long long)min(max(entry, 0), n_pages - 1) * Hkv + h - at) << lg;
   }
+  __device__ __forceinline__ long long operator()(int row) const { return place(row, entry(row)); }
 };
 
 }  // namespace loki

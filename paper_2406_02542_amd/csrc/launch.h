@@ -304,15 +304,14 @@ struct SpanArgs {
   CacheView cache;
   const void* q;
   void* out;              // [B, m, Hq, 128] as q
-  float* partial;         // [B m Hq][nsplit] parts, with more than one split
+  float* partial;         // [B m Hq][nsplit] parts, with more than one
   const int32_t* lens;    // [B, m] or null: S_max less the tokens behind
   int B, m, G, Hq, Hkv, S_max, window, sinks;
-  int tiles, nsplit, run; // tiles of query rows of a sequence and KV head; parts of a tile's rows at most, and the rows of one
+  int rows, tiles, nsplit, run;  // tiles of `rows` query rows of a sequence and KV head, each cut into up to nsplit parts of `run` rows
 };
 // How a call is cut: the workspace's size and the launch go by it.
 struct SpanPlan {
-  int rows;   // query rows of a tile
-  int tiles, nsplit, run;
+  int rows, tiles, nsplit, run;
 };
 SpanPlan span_plan(const Shape& s, int m, int window, int sinks, bool bits4);
 hipError_t launch_span(const Shape& s, SpanArgs a, hipStream_t st);

@@ -20,17 +20,13 @@ constexpr int kSpWaves = 4;
 __global__ __launch_bounds__(64 * kSpWaves) void span_rows_kernel(SpanArgs a) {
   constexpr int KEYS = 32;
   __shared__ __align__(16) SpanMerge<16, kSpWaves> sm;
-  const SpanTile tile = span_tile(a);
+  const SpanTile tile = span_tile<KEYS>(a);
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), r16 = lane & 15, kgrp = lane >> 4;
   const int M = a.m * a.G, r0 = tile.tile * 16, live = min(16, M - r0), lg = 31 - __builtin_clz(a.G);
-  const SpanRows rows = span_rows(a, tile.b, r0 >> lg, (r0 + live - 1) >> lg);
+  const SpanRows rows = tile.rows;
   const SpanSteps<KEYS> steps(rows);
-  const SpanRun<KEYS> run(a, steps, tile.split);
-  const int s1 = run.s1;
-  if (run.s0 >= s1 && tile.split > 0) {  // (uniform for the block)
-    span_none(a, tile, r0, live);
-    return;
-  }
+  if (tile.s0 >= tile.s1 && tile.part > 0) return span_none(a, tile, live);  // (uniform for the block)
+  const int s1 = tile.s1;
   const RowPlaces places(a.cache, tile.b, tile.h, a.Hkv);
   const int len = r16 < live ? span_len(a, tile.b, (r0 + r16) >> lg) : 0;
 
@@ -44,33 +40,29 @@ __global__ __launch_bounds__(64 * kSpWaves) void span_rows_kernel(SpanArgs a) {
   am_f32x4_t o[8];
 #pragma unroll
   for (int c = 0; c < 8; ++c) o[c] = am_f32x4_t{};
-  const char* kb = static_cast<const char*>(a.cache.k) + 16 * kgrp;
-  const char* vb = static_cast<const char*>(a.cache.v) + 16 * r16;
+  const char *kb = static_cast<const char*>(a.cache.k), *vb = static_cast<const char*>(a.cache.v);
   uint4 kraw[2][4], vraw[8];
-  long long place[2];
-  auto find = [&](const SpanStep& st) __attribute__((always_inline)) {
-#pragma unroll
-    for (int t = 0; t < 2; ++t) place[t] = places(min(max(st.at + 16 * t, st.lo), st.hi - 1));
-  };
+  SpanPlaces<2> place;
   auto load_k = [&](const SpanStep& st) __attribute__((always_inline)) {
 #pragma unroll
     for (int t = 0; t < 2; ++t) {
-      const char* p = kb + (place[t] + min(max(st.at + 16 * t + r16, st.lo), st.hi - 1)) * (kD * 2);
+      const char* p = kb + (place.at[t] + span_near(st, t, r16)) * (kD * 2) + 16 * kgrp;
 #pragma unroll
-      for (int s = 0; s < 4; ++s) kraw[t][s] = load16(p + 64 * s);
+      for (int i = 0; i < 4; ++i) kraw[t][i] = load16(p + 64 * i);
     }
   };
   auto load_v = [&](const SpanStep& st) __attribute__((always_inline)) {
 #pragma unroll
-    for (int e = 0; e < 8; ++e)
-      vraw[e] = load16(vb + (place[e / 4] + min(max(st.at + 16 * (e / 4) + 4 * kgrp + e % 4, st.lo), st.hi - 1)) * (kD * 2));
+    for (int e = 0; e < 8; ++e) vraw[e] = load16(vb + (place.at[e / 4] + span_near(st, e / 4, 4 * kgrp + e % 4)) * (kD * 2) + 16 * r16);
   };
-  int s = run.s0 + wave;
+  int s = tile.s0 + wave;
   if (s < s1) {  // (uniform for the wave)
     const SpanStep st = span_step(steps, rows, s);
-    find(st);
+    place.ask(places, st);
+    place.settle(places, st);
     load_k(st);
     load_v(st);
+    place.ask(places, span_step(steps, rows, min(s + kSpWaves, steps.total - 1)));
   }
   for (; s < s1; s += kSpWaves) {
     const SpanStep st = span_step(steps, rows, s), next = span_step(steps, rows, min(s + kSpWaves, steps.total - 1));
@@ -81,7 +73,7 @@ __global__ __launch_bounds__(64 * kSpWaves) void span_rows_kernel(SpanArgs a) {
 #pragma unroll
       for (int i = 0; i < 4; ++i) acc[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(am_bf16x8_t, kraw[t][i]), bq[i], acc[t], 0, 0, 0);
     }
-    find(next);
+    place.settle(places, next);
     load_k(next);
     uint32_t seen = 0xffu;
     if (!span_full(a, rows, st, KEYS)) {  // (uniform)
@@ -131,6 +123,7 @@ __global__ __launch_bounds__(64 * kSpWaves) void span_rows_kernel(SpanArgs a) {
       o[c] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(av, b_hi, o[c], 0, 0, 0);
     }
     load_v(next);
+    place.ask(places, span_step(steps, rows, min(s + 2 * kSpWaves, steps.total - 1)));
   }
   l += __shfl_xor(l, 16);
   l += __shfl_xor(l, 32);
@@ -152,17 +145,13 @@ template <int QG>
 __global__ __launch_bounds__(64 * kSpWaves, 2) void span_f32_kernel(SpanArgs a) {
   constexpr int KEYS = 16;
   __shared__ __align__(16) SpanMerge<16 * QG, kSpWaves> sm;
-  const SpanTile tile = span_tile(a);
+  const SpanTile tile = span_tile<KEYS>(a);
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), l16 = lane & 15, c4 = lane >> 4;
   const int M = a.m * a.G, r0 = tile.tile * (16 * QG), live = min(16 * QG, M - r0), lg = 31 - __builtin_clz(a.G);
-  const SpanRows rows = span_rows(a, tile.b, r0 >> lg, (r0 + live - 1) >> lg);
+  const SpanRows rows = tile.rows;
   const SpanSteps<KEYS> steps(rows);
-  const SpanRun<KEYS> run(a, steps, tile.split);
-  const int s1 = run.s1;
-  if (run.s0 >= s1 && tile.split > 0) {  // (uniform for the block)
-    span_none(a, tile, r0, live);
-    return;
-  }
+  if (tile.s0 >= tile.s1 && tile.part > 0) return span_none(a, tile, live);  // (uniform for the block)
+  const int s1 = tile.s1;
   const RowPlaces places(a.cache, tile.b, tile.h, a.Hkv);
 
   int len[QG];
@@ -181,29 +170,30 @@ __global__ __launch_bounds__(64 * kSpWaves, 2) void span_f32_kernel(SpanArgs a) 
 #pragma unroll
     for (int c = 0; c < 8; ++c) o[g][c] = pf_f32x4_t{};
   }
-  const float* kb = static_cast<const float*>(a.cache.k) + 4 * c4;
-  const float* vb = static_cast<const float*>(a.cache.v) + 4 * l16;
+  const char *kb = static_cast<const char*>(a.cache.k), *vb = static_cast<const char*>(a.cache.v);
   float4 kr[8], vr[4][2];
-  long long place;
+  SpanPlaces<1> place;
   auto load_k = [&](const SpanStep& st) __attribute__((always_inline)) {
-    const float* p = kb + (place + min(max(st.at + l16, st.lo), st.hi - 1)) * kD;
+    const char* p = kb + (place.at[0] + span_near(st, 0, l16)) * (kD * 4) + 16 * c4;
 #pragma unroll
-    for (int j = 0; j < 8; ++j) kr[j] = *reinterpret_cast<const float4*>(p + 16 * j);
+    for (int j = 0; j < 8; ++j) kr[j] = *reinterpret_cast<const float4*>(p + 64 * j);
   };
   auto load_v = [&](const SpanStep& st) __attribute__((always_inline)) {
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      const float* p = vb + (place + min(max(st.at + 4 * c4 + i, st.lo), st.hi - 1)) * kD;
+      const char* p = vb + (place.at[0] + span_near(st, 0, 4 * c4 + i)) * (kD * 4) + 16 * l16;
       vr[i][0] = *reinterpret_cast<const float4*>(p);
-      vr[i][1] = *reinterpret_cast<const float4*>(p + 64);
+      vr[i][1] = *reinterpret_cast<const float4*>(p + 256);
     }
   };
-  int s = run.s0 + wave;
+  int s = tile.s0 + wave;
   if (s < s1) {  // (uniform for the wave)
     const SpanStep st = span_step(steps, rows, s);
-    place = places(min(max(st.at, st.lo), st.hi - 1));
+    place.ask(places, st);
+    place.settle(places, st);
     load_k(st);
     load_v(st);
+    place.ask(places, span_step(steps, rows, min(s + kSpWaves, steps.total - 1)));
   }
   for (; s < s1; s += kSpWaves) {
     const SpanStep st = span_step(steps, rows, s), next = span_step(steps, rows, min(s + kSpWaves, steps.total - 1));
@@ -221,7 +211,7 @@ __global__ __launch_bounds__(64 * kSpWaves, 2) void span_f32_kernel(SpanArgs a) 
         chain[g][2] = __builtin_amdgcn_mfma_f32_16x16x4f32(kr[j].z, q[g][j].z, chain[g][2], 0, 0, 0);
         chain[g][3] = __builtin_amdgcn_mfma_f32_16x16x4f32(kr[j].w, q[g][j].w, chain[g][3], 0, 0, 0);
       }
-    place = places(min(max(next.at, next.lo), next.hi - 1));
+    place.settle(places, next);
     load_k(next);
     const bool full = span_full(a, rows, st, KEYS);
 #pragma unroll
@@ -268,6 +258,7 @@ __global__ __launch_bounds__(64 * kSpWaves, 2) void span_f32_kernel(SpanArgs a) 
           o[g][4 * c + 3] = __builtin_amdgcn_mfma_f32_16x16x4f32(vr[i][c].w, p[g][i], o[g][4 * c + 3], 0, 0, 0);
         }
     load_v(next);
+    place.ask(places, span_step(steps, rows, min(s + 2 * kSpWaves, steps.total - 1)));
   }
 #pragma unroll
   for (int g = 0; g < QG; ++g) {
@@ -314,17 +305,12 @@ __global__ __launch_bounds__(64 * WAVES, WAVES == 4 ? 1 : 2) void span_tiles_ker
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int l32 = lane & 31, half = lane >> 5, l16 = lane & 15;
   const int wq = wave % WQ, wk = wave / WQ;
-  SpanTile tile = span_tile(a);
-  tile.tile = a.tiles - 1 - tile.tile;  // (the last tokens see the most)
+  const SpanTile tile = span_tile<KT>(a);
   const int M = a.m * a.G, r0 = tile.tile * (32 * WQ), live = min(32 * WQ, M - r0), lg = 31 - __builtin_clz(a.G);
-  const SpanRows rows = span_rows(a, tile.b, r0 >> lg, (r0 + live - 1) >> lg);
+  const SpanRows rows = tile.rows;
   const SpanSteps<KT> steps(rows);
-  const SpanRun<KT> run(a, steps, tile.split);
-  const int s0 = run.s0, s1 = run.s1;
-  if (s0 >= s1 && tile.split > 0) {  // (uniform for the block)
-    span_none(a, tile, r0, live);
-    return;
-  }
+  if (tile.s0 >= tile.s1 && tile.part > 0) return span_none(a, tile, live);  // (uniform for the block)
+  const int s0 = tile.s0, s1 = tile.s1;
   const RowPlaces places(a.cache, tile.b, tile.h, a.Hkv);
   // this wave's queries, and its lane's
   const int q0 = wq * 32, mine = min(32, live - q0), row = q0 + l32;
@@ -530,17 +516,16 @@ __global__ __launch_bounds__(64 * WAVES, WAVES == 4 ? 1 : 2) void span_tiles_ker
       const int r = 4 * j + (lane >> 4);
       const float4 x = *reinterpret_cast<const float4*>(at + r * 256 + ((l16 ^ (r & 15)) * 16));
       if (q0 + r < live) {
-        const long long place = span_place(a, tile.b, tile.h, r0 + q0 + r);
         if (parts)
-          *reinterpret_cast<float4*>(a.partial + (place * a.nsplit + tile.split) * kPartStride + 64 * pass + 4 * l16) = x;
+          *reinterpret_cast<float4*>(span_part(a, tile, q0 + r) + 64 * pass + 4 * l16) = x;
         else
-          *reinterpret_cast<uint2*>(static_cast<uint16_t*>(a.out) + place * kD + 64 * pass + 4 * l16) = make_uint2(BF16::round2(x.x, x.y), BF16::round2(x.z, x.w));
+          *reinterpret_cast<uint2*>(static_cast<uint16_t*>(a.out) + span_place(a, tile.b, tile.h, r0 + q0 + r) * kD + 64 * pass + 4 * l16) = make_uint2(BF16::round2(x.x, x.y), BF16::round2(x.z, x.w));
       }
     }
     __builtin_amdgcn_wave_barrier();
   }
   if (parts && half == 0 && row < live)
-    *reinterpret_cast<float2*>(a.partial + (span_place(a, tile.b, tile.h, r0 + row) * a.nsplit + tile.split) * kPartStride + kD) = make_float2(m, l);
+    *reinterpret_cast<float2*>(span_part(a, tile, row) + kD) = make_float2(m, l);
 }
 
 template <int WAVES, int WQ>
@@ -556,7 +541,7 @@ static hipError_t launch_tiles(const SpanArgs& a, dim3 grid, hipStream_t st) {
 // ---- parts joined ---------------------------------------------------------------------------------------------------
 // 32 lanes take a query row, 16 bytes of each of its parts; GROUPS of them share a row's parts, four each at a time.
 template <typename T, int GROUPS>
-__global__ __launch_bounds__(256) void span_merge_kernel(const float* __restrict__ partial, typename T::store_t* __restrict__ out,
+__global__ __launch_bounds__(256) void span_merge_kernel(const float* __restrict__ partials, typename T::store_t* __restrict__ out,
                                                          long long rows, int nsplit) {
   constexpr int U = 4;
   __shared__ __align__(16) float s_o[GROUPS > 1 ? GROUPS : 1][kD];
@@ -564,6 +549,7 @@ __global__ __launch_bounds__(256) void span_merge_kernel(const float* __restrict
   const int lane = threadIdx.x & 31, grp = threadIdx.x >> 5;
   const long long r = GROUPS > 1 ? (long long)blockIdx.x : (long long)blockIdx.x * 8 + grp;
   if (GROUPS == 1 && r >= rows) return;
+  const float* partial = partials + r * nsplit * kPartStride;
   float m = kNegBig, l = 0.f;
   float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
   for (int i0 = GROUPS > 1 ? grp : 0; i0 < nsplit; i0 += GROUPS * U) {
@@ -572,7 +558,7 @@ __global__ __launch_bounds__(256) void span_merge_kernel(const float* __restrict
 #pragma unroll
     for (int u = 0; u < U; ++u) {
       const int i = i0 + u * GROUPS;
-      const float* p = partial + (r * nsplit + (i < nsplit ? i : i0)) * kPartStride;
+      const float* p = partial + (long long)(i < nsplit ? i : i0) * kPartStride;
       ml[u] = *reinterpret_cast<const float2*>(p + kD);
       x[u] = *reinterpret_cast<const float4*>(p + 4 * lane);
       if (i >= nsplit) ml[u] = make_float2(kNegBig, 0.f);
@@ -632,16 +618,19 @@ SpanPlan span_plan(const Shape& s, int m, int window, int sinks, bool bits4) {
   p.tiles = (int)((M + p.rows - 1) / p.rows);
   // a tile's rows at most: its tokens' windows and the sinks
   const long long tokens = p.rows < M ? (p.rows + s.G - 1) / s.G + 1 : m, most = (long long)window + tokens - 1 + sinks;
-  const long long read = window > 0 && most < s.S ? most : s.S, blocks = (long long)s.B * s.Hkv * p.tiles;
+  const long long read = window > 0 && most < s.S ? most : s.S, blocks = (long long)s.B * p.tiles * s.Hkv;
+  // as many parts as fill the blocks that are resident together, by the kernels' registers
+  const bool three = bits4 ? s.dtype == 1 && p.rows == 4 : s.dtype == 0 && p.rows == 16;
+  const long long slots = (lds ? 1LL : three ? 3LL : 2LL) * device_cus();
   const int least = lds ? 256 : 128;
-  long long n = ((lds ? 1LL : 2LL) * device_cus() + blocks - 1) / blocks;
+  long long n = (slots + blocks - 1) / blocks;
   if (n > (read + least - 1) / least) n = (read + least - 1) / least;
-  p.run = (int)((read + n - 1) / n);
-  p.nsplit = (int)n;
+  p.nsplit = n < 1 ? 1 : (int)n;
+  p.run = (int)((read + p.nsplit - 1) / p.nsplit);
   return p;
 }
 
-hipError_t launch_span_q4(const Shape& s, const SpanArgs& a, int rows, hipStream_t st);
+hipError_t launch_span_q4(const Shape& s, const SpanArgs& a, hipStream_t st);
 
 template <typename T>
 static void launch_span_merge(const SpanArgs& a, hipStream_t st) {
@@ -660,13 +649,14 @@ hipError_t launch_span(const Shape& s, SpanArgs a, hipStream_t st) {
     a.window = 0x7fffffff;
     a.sinks = 0;
   }
+  a.rows = plan.rows;
   a.tiles = plan.tiles;
   a.nsplit = plan.nsplit;
   a.run = plan.run;
   const dim3 grid((unsigned)((long long)a.B * a.Hkv * a.tiles * a.nsplit)), block(64 * kSpWaves);
   hipError_t e = hipSuccess;
   if (bits4)
-    e = launch_span_q4(s, a, plan.rows, st);
+    e = launch_span_q4(s, a, st);
   else if (s.dtype == 0 && plan.rows == 16)
     hipLaunchKernelGGL((span_f32_kernel<1>), grid, block, 0, st, a);
   else if (s.dtype == 0)
@@ -683,10 +673,10 @@ hipError_t launch_span(const Shape& s, SpanArgs a, hipStream_t st) {
     e = launch_tiles<8, 8>(a, grid, st);
   if (e == hipSuccess) e = hipGetLastError();
   if (e != hipSuccess || a.nsplit == 1) return e;
-  if (s.dtype == 0)
-    launch_span_merge<F32>(a, st);
-  else
+  if (s.dtype == 1)
     launch_span_merge<BF16>(a, st);
+  else
+    launch_span_merge<F32>(a, st);
   return hipGetLastError();
 }
 

@@ -14,18 +14,6 @@ namespace loki {
 
 constexpr float kUnseen = -3.0e38f;  // a logit that no maximum follows and whose weight is 0 whatever the maximum is
 
-struct SpanTile {
-  int b, h, tile, split;
-};
-__device__ __forceinline__ SpanTile span_tile(const SpanArgs& a) {
-  int x = blockIdx.x;
-  const int h = x % a.Hkv;
-  x /= a.Hkv;
-  const int split = x % a.nsplit;
-  x /= a.nsplit;
-  return {x / a.tiles, h, x % a.tiles, split};
-}
-
 __device__ __forceinline__ int span_len(const SpanArgs& a, int b, int j) {
   if (a.lens == nullptr) return max(0, a.S_max - (a.m - 1 - j));
   return min(max(a.lens[(long long)b * a.m + j], 0), a.S_max);
@@ -70,6 +58,42 @@ __device__ __forceinline__ SpanStep span_step(const SpanSteps<KEYS>& n, const Sp
   return s < n.sinks ? SpanStep{s * KEYS, 0, r.nsink} : SpanStep{n.base + (s - n.sinks) * KEYS, r.lo, r.hi};
 }
 
+// The places of a step's TILES tiles of 16 rows (the range's first or last row's, where a tile lies outside): asked for a step ahead,
+// settled when the step's rows are loaded.
+template <int TILES>
+struct SpanPlaces {
+  int row[TILES], entry[TILES];
+  long long at[TILES];  // of the tile's first row, which may lie outside
+  __device__ __forceinline__ void ask(const RowPlaces& places, const SpanStep& st) {
+#pragma unroll
+    for (int t = 0; t < TILES; ++t) {
+      row[t] = min(max(st.at + 16 * t, st.lo), st.hi - 1);
+      entry[t] = places.entry(row[t]);
+    }
+  }
+  __device__ __forceinline__ void settle(const RowPlaces& places, const SpanStep& st) {
+#pragma unroll
+    for (int t = 0; t < TILES; ++t) at[t] = places.place(row[t], entry[t]) + st.at + 16 * t;
+  }
+};
+// Row `i` of tile t of a step from the tile's first: itself, or the range's last or first.
+__device__ __forceinline__ int span_near(const SpanStep& st, int t, int i) {
+  const int first = st.at + 16 * t;
+  return min(max(first + i, st.lo), st.hi - 1) - first;
+}
+// f(whole): whether the step's rows are all there, so that they lie at fixed distances.  (The empty statements keep the compiler from taking
+// the loads of both branches together, for which it would carry an address for each in registers.)
+template <int KEYS, typename F>
+__device__ __forceinline__ void span_loads(const SpanStep& st, F f) {
+  if (st.at >= st.lo && st.at + KEYS <= st.hi) {  // (uniform)
+    f(std::true_type{});
+    asm volatile("" ::: "memory");
+  } else {
+    f(std::false_type{});
+    asm volatile("" ::: "memory");
+  }
+}
+
 // Whether a token that sees `len` rows sees row s of a step.
 __device__ __forceinline__ bool span_sees(const SpanArgs& a, const SpanStep& st, int len, int s) {
   return s >= st.lo && s < min(st.hi, len) && (s >= len - a.window || s < a.sinks);
@@ -79,16 +103,10 @@ __device__ __forceinline__ bool span_full(const SpanArgs& a, const SpanRows& r, 
   return st.at >= st.lo && st.at + keys <= min(st.hi, r.len_min) && (st.at >= r.hi - a.window || st.at + keys <= a.sinks);
 }
 
-// The steps of this block's run: the same number for every tile, so that blocks have equal work whatever the lengths; a tile has as many
-// runs as its rows fill (more rows than expected, of tokens that do not lie next to each other, make its runs longer).
-template <int KEYS>
-struct SpanRun {
-  int s0, s1;
-  __device__ __forceinline__ SpanRun(const SpanArgs& a, const SpanSteps<KEYS>& n, int split) {
-    const int each = max((a.run + KEYS - 1) / KEYS, (n.total + a.nsplit - 1) / a.nsplit);
-    s0 = split * each;
-    s1 = min(n.total, s0 + each);
-  }
+// What a block does: steps [s0, s1) of a tile, part `part` of its nsplit.
+struct SpanTile {
+  int b, h, tile, part, s0, s1;
+  SpanRows rows;
 };
 
 // Query row r of a sequence: its place among the rows of q, of out and of the parts.
@@ -96,11 +114,37 @@ __device__ __forceinline__ long long span_place(const SpanArgs& a, int b, int h,
   const int j = r >> (31 - __builtin_clz(a.G));
   return ((long long)b * a.m + j) * a.Hq + h * a.G + (r & (a.G - 1));
 }
+// Where query row r of the tile has this block's part.
+__device__ __forceinline__ float* span_part(const SpanArgs& a, const SpanTile& t, int r) {
+  return a.partial + (span_place(a, t.b, t.h, t.tile * a.rows + r) * a.nsplit + t.part) * kPartStride;
+}
 
-// A run that no row is left for: its parts say so, which the merge asks for in front of their outputs.
-__device__ __forceinline__ void span_none(const SpanArgs& a, const SpanTile& tile, int r0, int live) {
-  for (int r = threadIdx.x; r < live; r += blockDim.x)
-    *reinterpret_cast<float2*>(a.partial + (span_place(a, tile.b, tile.h, r0 + r) * a.nsplit + tile.split) * kPartStride + kD) = make_float2(kNegBig, 0.f);
+// This block's tile and its share of the tile's steps: runs of equal length, so that blocks have equal work whatever the lengths and short
+// sequences fewer of them (more rows than expected, of tokens that do not lie next to each other, make a tile's runs longer).  us with the
+// rows of each sequence in equal parts and so: 16 sequences of 32/8 bf16 heads up to 16384 rows 144, 136; 5 of 24 fp32 heads up to 2311 in
+// 4 bits 19.1, 16.8.
+template <int KEYS>
+__device__ __forceinline__ SpanTile span_tile(const SpanArgs& a) {
+  SpanTile t;
+  int x = blockIdx.x;
+  t.h = x % a.Hkv;  // (a run's heads next to each other)
+  x /= a.Hkv;
+  t.part = x % a.nsplit;
+  x /= a.nsplit;
+  t.b = x / a.tiles;
+  t.tile = a.tiles - 1 - (x - t.b * a.tiles);  // (the last tokens see the most)
+  const int r0 = t.tile * a.rows, lg = 31 - __builtin_clz(a.G), last = min(r0 + a.rows, a.m * a.G) - 1;
+  t.rows = span_rows(a, t.b, r0 >> lg, last >> lg);
+  const SpanSteps<KEYS> n(t.rows);
+  const int each = max((a.run + KEYS - 1) / KEYS, (n.total + a.nsplit - 1) / a.nsplit);
+  t.s0 = t.part * each;
+  t.s1 = min(n.total, t.s0 + each);
+  return t;
+}
+
+// A run that no row is left for: its parts say so, which the merge goes by.
+__device__ __forceinline__ void span_none(const SpanArgs& a, const SpanTile& t, int live) {
+  for (int r = threadIdx.x; r < live; r += blockDim.x) *reinterpret_cast<float2*>(span_part(a, t, r) + kD) = make_float2(kNegBig, 0.f);
 }
 
 // A wave's state after its steps, for 16 query rows: lane (row r16, kgrp) holds maximum m and sum l of its row (l its own share of the
@@ -128,12 +172,12 @@ __device__ __forceinline__ void span_store(const SpanArgs& a, const SpanMerge<RO
       ls = fmaf(sm.ml[w][r].y, f, ls);
       os = make_float4(fmaf(x.x, f, os.x), fmaf(x.y, f, os.y), fmaf(x.z, f, os.z), fmaf(x.w, f, os.w));
     }
-    const long long place = span_place(a, tile.b, tile.h, r0 + r);
     if (a.nsplit > 1) {
-      float* p = a.partial + (place * a.nsplit + tile.split) * kPartStride;
+      float* p = span_part(a, tile, r);
       *reinterpret_cast<float4*>(p + c) = os;
       if (c == 0) *reinterpret_cast<float2*>(p + kD) = make_float2(mn, ls);
     } else {
+      const long long place = span_place(a, tile.b, tile.h, r0 + r);
       const float inv = ls > 0.f ? 1.0f / ls : 0.f;  // (a token without rows: zeros)
       if constexpr (T::EPC == 8)
         *reinterpret_cast<uint2*>(static_cast<uint16_t*>(a.out) + place * kD + c) =

@@ -13,11 +13,12 @@ namespace loki {
 
 constexpr int kQ4Waves = 4;
 
-// Codes g of a word's halves as two bf16 numbers 1 + n / 16.
-__device__ __forceinline__ uint32_t q4_pair(uint32_t x, int g) {
-  const uint32_t y = g == 0 ? x << 3 : x >> (4 * g - 3);
-  return (y & 0x00780078u) | 0x3f803f80u;
-}
+// Codes g of a word's halves as two bf16 numbers 1 + n / 16.  The constants are kept in registers: one instruction takes both then.
+struct Q4Pair {
+  uint32_t mask = 0x00780078u, one = 0x3f803f80u;
+  __device__ __forceinline__ Q4Pair() { asm("" : "+v"(mask), "+s"(one)); }
+  __device__ __forceinline__ uint32_t operator()(uint32_t x, int g) const { return ((g == 0 ? x << 3 : x >> (4 * g - 3)) & mask) | one; }
+};
 
 // x0, x1 as TERMS pairs of bf16 numbers that add up to them.
 template <int TERMS>
@@ -37,69 +38,53 @@ __device__ __forceinline__ void q4_terms(float x0, float x1, uint32_t (&w)[TERMS
 // which leaves a quarter of the scaling and of the splitting into terms that whole columns for a query would ask of every lane: 24
 // vector instructions a row of keys and values for all 64 lanes against 40 of the kernel below.
 template <typename T, int NS>
-__global__ __launch_bounds__(64 * kQ4Waves, 2) void span_q4_few_kernel(SpanArgs a) {
+__global__ __launch_bounds__(64 * kQ4Waves, T::EPC == 8 && NS == 1 ? 3 : 2) void span_q4_few_kernel(SpanArgs a) {
   constexpr int KEYS = 32, QT = T::EPC == 8 ? 1 : 3, PT = T::EPC == 8 ? 2 : 3, ROWS = 4 * NS;
   __shared__ __align__(16) SpanMerge<ROWS, kQ4Waves> sm;
-  const SpanTile tile = span_tile(a);
+  const SpanTile tile = span_tile<KEYS>(a);
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), r16 = lane & 15, kgrp = lane >> 4;
   const int g = r16 & 3, hd = r16 >> 2;
   const int M = a.m * a.G, r0 = tile.tile * ROWS, live = min(ROWS, M - r0), lg = 31 - __builtin_clz(a.G);
-  const SpanRows rows = span_rows(a, tile.b, r0 >> lg, (r0 + live - 1) >> lg);
+  const SpanRows rows = tile.rows;
   const SpanSteps<KEYS> steps(rows);
-  const SpanRun<KEYS> run(a, steps, tile.split);
-  const int s1 = run.s1;
-  if (run.s0 >= s1 && tile.split > 0) {  // (uniform for the block)
-    span_none(a, tile, r0, live);
-    return;
-  }
+  if (tile.s0 >= tile.s1 && tile.part > 0) return span_none(a, tile, live);  // (uniform for the block)
+  const int s1 = tile.s1;
   const RowPlaces places(a.cache, tile.b, tile.h, a.Hkv);
+  const Q4Pair q4_pair;
 
   const char *kb = static_cast<const char*>(a.cache.k), *vb = static_cast<const char*>(a.cache.v);
   const char *ks = static_cast<const char*>(a.cache.k_scales), *vs = static_cast<const char*>(a.cache.v_scales);
   const unsigned k_at = r16 * kQ4RowBytes + 16 * kgrp, v_at = 4 * kgrp * kQ4RowBytes + 4 * r16, s_at = 4 * kgrp * kQ4ScaleBytes + 4 * g;
   uint4 kraw[2];
   uint32_t ksc[8], vsc[8], vraw[8];
-  long long place[2];
-  auto find = [&](const SpanStep& st) __attribute__((always_inline)) {
-#pragma unroll
-    for (int t = 0; t < 2; ++t) place[t] = places(min(max(st.at + 16 * t, st.lo), st.hi - 1));
-  };
-  // The rows of a step, from uniform addresses; a step that the range's end cuts takes the range's own rows again for those outside.
+  SpanPlaces<2> place;
   auto load = [&](const SpanStep& st, auto values) __attribute__((always_inline)) {
-    const char *codes = decltype(values)::value ? vb : kb, *scales = decltype(values)::value ? vs : ks;
-    uint32_t(&sc)[8] = decltype(values)::value ? vsc : ksc;
-    if (st.at >= st.lo && st.at + KEYS <= st.hi) {  // (uniform)
+    constexpr bool V = decltype(values)::value;
+    const char *codes = V ? vb : kb, *scales = V ? vs : ks;
+    uint32_t(&sc)[8] = V ? vsc : ksc;
+    span_loads<KEYS>(st, [&](auto whole) __attribute__((always_inline)) {
+      constexpr bool W = decltype(whole)::value;
 #pragma unroll
       for (int t = 0; t < 2; ++t) {
-        const char *c = codes + (place[t] + st.at + 16 * t) * kQ4RowBytes, *x = scales + (place[t] + st.at + 16 * t) * kQ4ScaleBytes;
-        if constexpr (!decltype(values)::value) kraw[t] = load16(c + k_at);
+        const char *c = codes + place.at[t] * kQ4RowBytes, *x = scales + place.at[t] * kQ4ScaleBytes;
+        if constexpr (!V) kraw[t] = load16(W ? c + k_at : c + span_near(st, t, r16) * kQ4RowBytes + 16 * kgrp);
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-          sc[4 * t + i] = *reinterpret_cast<const uint32_t*>(x + s_at + i * kQ4ScaleBytes);
-          if constexpr (decltype(values)::value) vraw[4 * t + i] = *reinterpret_cast<const uint32_t*>(c + v_at + i * kQ4RowBytes);
+          const int row = W ? 0 : span_near(st, t, 4 * kgrp + i);
+          sc[4 * t + i] = *reinterpret_cast<const uint32_t*>(W ? x + s_at + i * kQ4ScaleBytes : x + row * kQ4ScaleBytes + 4 * g);
+          if constexpr (V) vraw[4 * t + i] = *reinterpret_cast<const uint32_t*>(W ? c + v_at + i * kQ4RowBytes : c + row * kQ4RowBytes + 4 * r16);
         }
       }
-    } else {
-#pragma unroll
-      for (int t = 0; t < 2; ++t) {
-        if constexpr (!decltype(values)::value)
-          kraw[t] = load16(codes + (place[t] + min(max(st.at + 16 * t + r16, st.lo), st.hi - 1)) * kQ4RowBytes + 16 * kgrp);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const long long row = place[t] + min(max(st.at + 16 * t + 4 * kgrp + i, st.lo), st.hi - 1);
-          sc[4 * t + i] = *reinterpret_cast<const uint32_t*>(scales + row * kQ4ScaleBytes + 4 * g);
-          if constexpr (decltype(values)::value) vraw[4 * t + i] = *reinterpret_cast<const uint32_t*>(codes + row * kQ4RowBytes + 4 * r16);
-        }
-      }
-    }
+    });
   };
-  int s = run.s0 + wave;
+  int s = tile.s0 + wave;
   if (s < s1) {  // (uniform for the wave)
     const SpanStep st = span_step(steps, rows, s);
-    find(st);
+    place.ask(places, st);
+    place.settle(places, st);
     load(st, std::false_type{});
     load(st, std::true_type{});
-    find(span_step(steps, rows, min(s + kQ4Waves, steps.total - 1)));
+    place.ask(places, span_step(steps, rows, min(s + kQ4Waves, steps.total - 1)));
   }
 
   int len[NS];
@@ -159,6 +144,7 @@ __global__ __launch_bounds__(64 * kQ4Waves, 2) void span_q4_few_kernel(SpanArgs 
           x[u][4 * t + i] = group_allreduce_sum<4>(fmaf((float)sc.x, acc[u][i], (float)sc.y * (qsum[u] * 0.0625f)));
         }
     }
+    place.settle(places, next);
     load(next, std::false_type{});
     const bool full = span_full(a, rows, st, KEYS);
     float p[NS][8];
@@ -225,7 +211,7 @@ __global__ __launch_bounds__(64 * kQ4Waves, 2) void span_q4_few_kernel(SpanArgs 
       }
     }
     load(next, std::true_type{});
-    find(span_step(steps, rows, min(s + 2 * kQ4Waves, steps.total - 1)));
+    place.ask(places, span_step(steps, rows, min(s + 2 * kQ4Waves, steps.total - 1)));
   }
 #pragma unroll
   for (int u = 0; u < NS; ++u) {
@@ -255,21 +241,18 @@ __global__ __launch_bounds__(64 * kQ4Waves, 2) void span_q4_few_kernel(SpanArgs 
 
 // QG groups of 16 query rows.  bf16: q is one term, the weights two (2^-16 of each, as the library's other attention); fp32: three each.
 template <typename T, int QG>
-__global__ __launch_bounds__(64 * kQ4Waves) void span_q4_kernel(SpanArgs a) {
+__global__ __launch_bounds__(64 * kQ4Waves, QG == 1 ? 2 : 1) void span_q4_kernel(SpanArgs a) {
   constexpr int KEYS = 32, QT = T::EPC == 8 ? 1 : 3, PT = T::EPC == 8 ? 2 : 3;
   __shared__ __align__(16) SpanMerge<16 * QG, kQ4Waves> sm;
-  const SpanTile tile = span_tile(a);
+  const SpanTile tile = span_tile<KEYS>(a);
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), r16 = lane & 15, kgrp = lane >> 4;
   const int M = a.m * a.G, r0 = tile.tile * (16 * QG), live = min(16 * QG, M - r0), lg = 31 - __builtin_clz(a.G);
-  const SpanRows rows = span_rows(a, tile.b, r0 >> lg, (r0 + live - 1) >> lg);
+  const SpanRows rows = tile.rows;
   const SpanSteps<KEYS> steps(rows);
-  const SpanRun<KEYS> run(a, steps, tile.split);
-  const int s1 = run.s1;
-  if (run.s0 >= s1 && tile.split > 0) {  // (uniform for the block)
-    span_none(a, tile, r0, live);
-    return;
-  }
+  if (tile.s0 >= tile.s1 && tile.part > 0) return span_none(a, tile, live);  // (uniform for the block)
+  const int s1 = tile.s1;
   const RowPlaces places(a.cache, tile.b, tile.h, a.Hkv);
+  const Q4Pair q4_pair;
 
   int len[QG];
   am_bf16x8_t bq[QG][kQ4Groups][QT];
@@ -305,37 +288,39 @@ __global__ __launch_bounds__(64 * kQ4Waves) void span_q4_kernel(SpanArgs a) {
     for (int c = 0; c < 8; ++c) o[u][c] = am_f32x4_t{};
   }
 
-  const char *kb = static_cast<const char*>(a.cache.k) + 16 * kgrp, *vb = static_cast<const char*>(a.cache.v) + 4 * r16;
+  const char *kb = static_cast<const char*>(a.cache.k), *vb = static_cast<const char*>(a.cache.v);
   const char *ks = static_cast<const char*>(a.cache.k_scales), *vs = static_cast<const char*>(a.cache.v_scales);
+  const unsigned k_at = r16 * kQ4RowBytes + 16 * kgrp, v_at = 4 * kgrp * kQ4RowBytes + 4 * r16, s_at = 4 * kgrp * kQ4ScaleBytes;
   uint4 kraw[2], ksc[8], vsc[8];
   uint32_t vraw[8];
-  long long place[2];
-  auto row_of = [&](const SpanStep& st, int e) __attribute__((always_inline)) {  // row e of the 8 whose weights this lane has
-    return place[e / 4] + min(max(st.at + 16 * (e / 4) + 4 * kgrp + e % 4, st.lo), st.hi - 1);
-  };
-  auto find = [&](const SpanStep& st) __attribute__((always_inline)) {
+  SpanPlaces<2> place;
+  auto load = [&](const SpanStep& st, auto values) __attribute__((always_inline)) {
+    constexpr bool V = decltype(values)::value;
+    const char *codes = V ? vb : kb, *scales = V ? vs : ks;
+    uint4(&sc)[8] = V ? vsc : ksc;
+    span_loads<KEYS>(st, [&](auto whole) __attribute__((always_inline)) {
+      constexpr bool W = decltype(whole)::value;
 #pragma unroll
-    for (int t = 0; t < 2; ++t) place[t] = places(min(max(st.at + 16 * t, st.lo), st.hi - 1));
-  };
-  auto load_k = [&](const SpanStep& st) __attribute__((always_inline)) {
+      for (int t = 0; t < 2; ++t) {
+        const char *c = codes + place.at[t] * kQ4RowBytes, *x = scales + place.at[t] * kQ4ScaleBytes;
+        if constexpr (!V) kraw[t] = load16(W ? c + k_at : c + span_near(st, t, r16) * kQ4RowBytes + 16 * kgrp);
 #pragma unroll
-    for (int t = 0; t < 2; ++t) kraw[t] = load16(kb + (place[t] + min(max(st.at + 16 * t + r16, st.lo), st.hi - 1)) * kQ4RowBytes);
-#pragma unroll
-    for (int e = 0; e < 8; ++e) ksc[e] = load16(ks + row_of(st, e) * kQ4ScaleBytes);
+        for (int i = 0; i < 4; ++i) {
+          const int row = W ? 0 : span_near(st, t, 4 * kgrp + i);
+          sc[4 * t + i] = load16(W ? x + s_at + i * kQ4ScaleBytes : x + row * kQ4ScaleBytes);
+          if constexpr (V) vraw[4 * t + i] = *reinterpret_cast<const uint32_t*>(W ? c + v_at + i * kQ4RowBytes : c + row * kQ4RowBytes + 4 * r16);
+        }
+      }
+    });
   };
-  auto load_v = [&](const SpanStep& st) __attribute__((always_inline)) {
-#pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      vraw[e] = *reinterpret_cast<const uint32_t*>(vb + row_of(st, e) * kQ4RowBytes);
-      vsc[e] = load16(vs + row_of(st, e) * kQ4ScaleBytes);
-    }
-  };
-  int s = run.s0 + wave;
+  int s = tile.s0 + wave;
   if (s < s1) {  // (uniform for the wave)
     const SpanStep st = span_step(steps, rows, s);
-    find(st);
-    load_k(st);
-    load_v(st);
+    place.ask(places, st);
+    place.settle(places, st);
+    load(st, std::false_type{});
+    load(st, std::true_type{});
+    place.ask(places, span_step(steps, rows, min(s + kQ4Waves, steps.total - 1)));
   }
   for (; s < s1; s += kQ4Waves) {
     const SpanStep st = span_step(steps, rows, s), next = span_step(steps, rows, min(s + kQ4Waves, steps.total - 1));
@@ -430,9 +415,10 @@ __global__ __launch_bounds__(64 * kQ4Waves) void span_q4_kernel(SpanArgs a) {
         }
       }
     }
-    find(next);
-    load_k(next);
-    load_v(next);
+    place.settle(places, next);
+    load(next, std::false_type{});
+    load(next, std::true_type{});
+    place.ask(places, span_step(steps, rows, min(s + 2 * kQ4Waves, steps.total - 1)));
   }
 #pragma unroll
   for (int u = 0; u < QG; ++u) {
@@ -457,21 +443,21 @@ __global__ __launch_bounds__(64 * kQ4Waves) void span_q4_kernel(SpanArgs a) {
 }
 
 template <typename T>
-static hipError_t launch_span_q4_t(const SpanArgs& a, int rows, hipStream_t st) {
+static hipError_t launch_span_q4_t(const SpanArgs& a, hipStream_t st) {
   const dim3 grid((unsigned)((long long)a.B * a.Hkv * a.tiles * a.nsplit)), block(64 * kQ4Waves);
-  if (rows == 4)
+  if (a.rows == 4)
     hipLaunchKernelGGL((span_q4_few_kernel<T, 1>), grid, block, 0, st, a);
-  else if (T::EPC == 8 && rows == 8)  // (fp32: its three terms for two sets do not fit in the registers of two waves)
+  else if (T::EPC == 8 && a.rows == 8)  // (fp32: its three terms for two sets do not fit in the registers of two waves)
     hipLaunchKernelGGL((span_q4_few_kernel<BF16, 2>), grid, block, 0, st, a);
-  else if (rows == 16)
+  else if (a.rows == 16)
     hipLaunchKernelGGL((span_q4_kernel<T, 1>), grid, block, 0, st, a);
   else
     hipLaunchKernelGGL((span_q4_kernel<T, 2>), grid, block, 0, st, a);
   return hipGetLastError();
 }
 
-hipError_t launch_span_q4(const Shape& s, const SpanArgs& a, int rows, hipStream_t st) {
-  return s.dtype == 0 ? launch_span_q4_t<F32>(a, rows, st) : launch_span_q4_t<BF16>(a, rows, st);
+hipError_t launch_span_q4(const Shape& s, const SpanArgs& a, hipStream_t st) {
+  return s.dtype == 0 ? launch_span_q4_t<F32>(a, st) : launch_span_q4_t<BF16>(a, st);
 }
 
 }  // namespace loki
