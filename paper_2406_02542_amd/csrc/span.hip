@@ -17,6 +17,7 @@ constexpr int kSpWaves = 4;
 //                                   rows up (v_perm_b32); the weights in two bf16 terms, 2^-16 of each (as the library's other attention)
 // so a query's maximum, sum and outputs are its own lanes'.  The reference of the exponentials follows the maximum only when a
 // lane's weights of a step sum up to more than 2^8.
+template <bool STREAM>
 __global__ __launch_bounds__(64 * kSpWaves) void span_rows_kernel(SpanArgs a) {
   constexpr int KEYS = 32;
   __shared__ __align__(16) SpanMerge<16, kSpWaves> sm;
@@ -53,7 +54,7 @@ __global__ __launch_bounds__(64 * kSpWaves) void span_rows_kernel(SpanArgs a) {
   };
   auto load_v = [&](const SpanStep& st) __attribute__((always_inline)) {
 #pragma unroll
-    for (int e = 0; e < 8; ++e) vraw[e] = load16(vb + (place.at[e / 4] + span_near(st, e / 4, 4 * kgrp + e % 4)) * (kD * 2) + 16 * r16);
+    for (int e = 0; e < 8; ++e) vraw[e] = load16_hint<STREAM>(vb + (place.at[e / 4] + span_near(st, e / 4, 4 * kgrp + e % 4)) * (kD * 2) + 16 * r16);
   };
   int s = tile.s0 + wave;
   if (s < s1) {  // (uniform for the wave)
@@ -141,7 +142,7 @@ __global__ __launch_bounds__(64 * kSpWaves) void span_rows_kernel(SpanArgs a) {
 
 // ---- fp32 -----------------------------------------------------------------------------------------------------------
 // The products of parts_impl.h's attend_f32, v_mfma_f32_16x16x4_f32, straight from registers, for QG groups of 16 query rows; steps of 16 rows.
-template <int QG>
+template <int QG, bool STREAM>
 __global__ __launch_bounds__(64 * kSpWaves, 2) void span_f32_kernel(SpanArgs a) {
   constexpr int KEYS = 16;
   __shared__ __align__(16) SpanMerge<16 * QG, kSpWaves> sm;
@@ -182,8 +183,8 @@ __global__ __launch_bounds__(64 * kSpWaves, 2) void span_f32_kernel(SpanArgs a) 
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       const char* p = vb + (place.at[0] + span_near(st, 0, 4 * c4 + i)) * (kD * 4) + 16 * l16;
-      vr[i][0] = *reinterpret_cast<const float4*>(p);
-      vr[i][1] = *reinterpret_cast<const float4*>(p + 256);
+      vr[i][0] = __builtin_bit_cast(float4, load16_hint<STREAM>(p));
+      vr[i][1] = __builtin_bit_cast(float4, load16_hint<STREAM>(p + 256));
     }
   };
   int s = tile.s0 + wave;
@@ -655,14 +656,22 @@ hipError_t launch_span(const Shape& s, SpanArgs a, hipStream_t st) {
   a.run = plan.run;
   const dim3 grid((unsigned)((long long)a.B * a.Hkv * a.tiles * a.nsplit)), block(64 * kSpWaves);
   hipError_t e = hipSuccess;
+  // From 90 MB of rows on, of which none is read twice, values are loaded past the caches (row_loads in api.hip).  us through / past: 64
+  // sequences of 64/8 heads with 4100 rows each 180 / 163, 16 of 32/8 with 16384 186 / 166, 13 with 4000 51.4 / 47.8, with 1500 (80 MB) 21.3 / 21.6;
+  // fp32, 16 of 24 heads with 1000 rows 74.5 / 68.1, 5 with 703 (86 MB) 22.7 / 23.4.
+  const bool past = plan.tiles == 1 && (double)a.B * a.Hkv * plan.nsplit * plan.run * (2 * kD * s.elem_bytes) >= kPastBytes;
   if (bits4)
     e = launch_span_q4(s, a, st);
+  else if (s.dtype == 0 && plan.rows == 16 && past)
+    hipLaunchKernelGGL((span_f32_kernel<1, true>), grid, block, 0, st, a);
   else if (s.dtype == 0 && plan.rows == 16)
-    hipLaunchKernelGGL((span_f32_kernel<1>), grid, block, 0, st, a);
+    hipLaunchKernelGGL((span_f32_kernel<1, false>), grid, block, 0, st, a);
   else if (s.dtype == 0)
-    hipLaunchKernelGGL((span_f32_kernel<2>), grid, block, 0, st, a);
+    hipLaunchKernelGGL((span_f32_kernel<2, false>), grid, block, 0, st, a);
+  else if (plan.rows == 16 && past)
+    hipLaunchKernelGGL((span_rows_kernel<true>), grid, block, 0, st, a);
   else if (plan.rows == 16)
-    hipLaunchKernelGGL(span_rows_kernel, grid, block, 0, st, a);
+    hipLaunchKernelGGL((span_rows_kernel<false>), grid, block, 0, st, a);
   else if (plan.rows == 32)
     e = launch_tiles<4, 1>(a, grid, st);
   else if (plan.rows == 64)

@@ -20,6 +20,12 @@ struct Q4Pair {
   __device__ __forceinline__ uint32_t operator()(uint32_t x, int g) const { return ((g == 0 ? x << 3 : x >> (4 * g - 3)) & mask) | one; }
 };
 
+template <bool STREAM>
+__device__ __forceinline__ uint32_t load4_hint(const void* p) {
+  if constexpr (STREAM) return __builtin_nontemporal_load(static_cast<const uint32_t*>(p));
+  return *static_cast<const uint32_t*>(p);
+}
+
 // x0, x1 as TERMS pairs of bf16 numbers that add up to them.
 template <int TERMS>
 __device__ __forceinline__ void q4_terms(float x0, float x1, uint32_t (&w)[TERMS]) {
@@ -37,7 +43,7 @@ __device__ __forceinline__ void q4_terms(float x0, float x1, uint32_t (&w)[TERMS
 //   second          column n holds p step_g, so a lane forms its own group's only; it keeps the two output tiles of its group
 // which leaves a quarter of the scaling and of the splitting into terms that whole columns for a query would ask of every lane: 24
 // vector instructions a row of keys and values for all 64 lanes against 40 of the kernel below.
-template <typename T, int NS>
+template <typename T, int NS, bool STREAM>
 __global__ __launch_bounds__(64 * kQ4Waves, T::EPC == 8 && NS == 1 ? 3 : 2) void span_q4_few_kernel(SpanArgs a) {
   constexpr int KEYS = 32, QT = T::EPC == 8 ? 1 : 3, PT = T::EPC == 8 ? 2 : 3, ROWS = 4 * NS;
   __shared__ __align__(16) SpanMerge<ROWS, kQ4Waves> sm;
@@ -54,7 +60,8 @@ __global__ __launch_bounds__(64 * kQ4Waves, T::EPC == 8 && NS == 1 ? 3 : 2) void
 
   const char *kb = static_cast<const char*>(a.cache.k), *vb = static_cast<const char*>(a.cache.v);
   const char *ks = static_cast<const char*>(a.cache.k_scales), *vs = static_cast<const char*>(a.cache.v_scales);
-  const unsigned k_at = r16 * kQ4RowBytes + 16 * kgrp, v_at = 4 * kgrp * kQ4RowBytes + 4 * r16, s_at = 4 * kgrp * kQ4ScaleBytes + 4 * g;
+  const int k_row = 4 * (r16 & 3) + (r16 >> 2);  // (see the head of this file)
+  const unsigned k_at = k_row * kQ4RowBytes + 16 * kgrp, v_at = kgrp * kQ4RowBytes + 4 * r16, s_at = kgrp * kQ4ScaleBytes + 4 * g;
   uint4 kraw[2];
   uint32_t ksc[8], vsc[8], vraw[8];
   SpanPlaces<2> place;
@@ -67,12 +74,12 @@ __global__ __launch_bounds__(64 * kQ4Waves, T::EPC == 8 && NS == 1 ? 3 : 2) void
 #pragma unroll
       for (int t = 0; t < 2; ++t) {
         const char *c = codes + place.at[t] * kQ4RowBytes, *x = scales + place.at[t] * kQ4ScaleBytes;
-        if constexpr (!V) kraw[t] = load16(W ? c + k_at : c + span_near(st, t, r16) * kQ4RowBytes + 16 * kgrp);
+        if constexpr (!V) kraw[t] = load16_hint<STREAM>(W ? c + k_at : c + span_near(st, t, k_row) * kQ4RowBytes + 16 * kgrp);
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-          const int row = W ? 0 : span_near(st, t, 4 * kgrp + i);
-          sc[4 * t + i] = *reinterpret_cast<const uint32_t*>(W ? x + s_at + i * kQ4ScaleBytes : x + row * kQ4ScaleBytes + 4 * g);
-          if constexpr (V) vraw[4 * t + i] = *reinterpret_cast<const uint32_t*>(W ? c + v_at + i * kQ4RowBytes : c + row * kQ4RowBytes + 4 * r16);
+          const int row = W ? 0 : span_near(st, t, 4 * i + kgrp);
+          sc[4 * t + i] = *reinterpret_cast<const uint32_t*>(W ? x + s_at + 4 * i * kQ4ScaleBytes : x + row * kQ4ScaleBytes + 4 * g);
+          if constexpr (V) vraw[4 * t + i] = load4_hint<STREAM>(W ? c + v_at + 4 * i * kQ4RowBytes : c + row * kQ4RowBytes + 4 * r16);
         }
       }
     });
@@ -153,7 +160,7 @@ __global__ __launch_bounds__(64 * kQ4Waves, T::EPC == 8 && NS == 1 ? 3 : 2) void
       if (!full) {  // (uniform)
 #pragma unroll
         for (int e = 0; e < 8; ++e)
-          if (!span_sees(a, st, len[u], st.at + 16 * (e / 4) + 4 * kgrp + e % 4)) x[u][e] = kUnseen;
+          if (!span_sees(a, st, len[u], st.at + 16 * (e / 4) + 4 * (e % 4) + kgrp)) x[u][e] = kUnseen;
       }
       float sum;
       auto weights = [&]() __attribute__((always_inline)) {
@@ -290,7 +297,8 @@ __global__ __launch_bounds__(64 * kQ4Waves, QG == 1 ? 2 : 1) void span_q4_kernel
 
   const char *kb = static_cast<const char*>(a.cache.k), *vb = static_cast<const char*>(a.cache.v);
   const char *ks = static_cast<const char*>(a.cache.k_scales), *vs = static_cast<const char*>(a.cache.v_scales);
-  const unsigned k_at = r16 * kQ4RowBytes + 16 * kgrp, v_at = 4 * kgrp * kQ4RowBytes + 4 * r16, s_at = 4 * kgrp * kQ4ScaleBytes;
+  const int k_row = 4 * (r16 & 3) + (r16 >> 2);
+  const unsigned k_at = k_row * kQ4RowBytes + 16 * kgrp, v_at = kgrp * kQ4RowBytes + 4 * r16, s_at = kgrp * kQ4ScaleBytes;
   uint4 kraw[2], ksc[8], vsc[8];
   uint32_t vraw[8];
   SpanPlaces<2> place;
@@ -303,12 +311,12 @@ __global__ __launch_bounds__(64 * kQ4Waves, QG == 1 ? 2 : 1) void span_q4_kernel
 #pragma unroll
       for (int t = 0; t < 2; ++t) {
         const char *c = codes + place.at[t] * kQ4RowBytes, *x = scales + place.at[t] * kQ4ScaleBytes;
-        if constexpr (!V) kraw[t] = load16(W ? c + k_at : c + span_near(st, t, r16) * kQ4RowBytes + 16 * kgrp);
+        if constexpr (!V) kraw[t] = load16(W ? c + k_at : c + span_near(st, t, k_row) * kQ4RowBytes + 16 * kgrp);
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-          const int row = W ? 0 : span_near(st, t, 4 * kgrp + i);
-          sc[4 * t + i] = load16(W ? x + s_at + i * kQ4ScaleBytes : x + row * kQ4ScaleBytes);
-          if constexpr (V) vraw[4 * t + i] = *reinterpret_cast<const uint32_t*>(W ? c + v_at + i * kQ4RowBytes : c + row * kQ4RowBytes + 4 * r16);
+          const int row = W ? 0 : span_near(st, t, 4 * i + kgrp);
+          sc[4 * t + i] = load16(W ? x + s_at + 4 * i * kQ4ScaleBytes : x + row * kQ4ScaleBytes);
+          if constexpr (V) vraw[4 * t + i] = *reinterpret_cast<const uint32_t*>(W ? c + v_at + 4 * i * kQ4RowBytes : c + row * kQ4RowBytes + 4 * r16);
         }
       }
     });
@@ -354,7 +362,7 @@ __global__ __launch_bounds__(64 * kQ4Waves, QG == 1 ? 2 : 1) void span_q4_kernel
       if (!full) {  // (uniform)
         seen = 0;
 #pragma unroll
-        for (int e = 0; e < 8; ++e) seen |= (span_sees(a, st, len[u], st.at + 16 * (e / 4) + 4 * kgrp + e % 4) ? 1u : 0u) << e;
+        for (int e = 0; e < 8; ++e) seen |= (span_sees(a, st, len[u], st.at + 16 * (e / 4) + 4 * (e % 4) + kgrp) ? 1u : 0u) << e;
       }
       float sum;
       auto weights = [&]() __attribute__((always_inline)) {
@@ -445,10 +453,15 @@ __global__ __launch_bounds__(64 * kQ4Waves, QG == 1 ? 2 : 1) void span_q4_kernel
 template <typename T>
 static hipError_t launch_span_q4_t(const SpanArgs& a, hipStream_t st) {
   const dim3 grid((unsigned)((long long)a.B * a.Hkv * a.tiles * a.nsplit)), block(64 * kQ4Waves);
-  if (a.rows == 4)
-    hipLaunchKernelGGL((span_q4_few_kernel<T, 1>), grid, block, 0, st, a);
-  else if (T::EPC == 8 && a.rows == 8)  // (fp32: its three terms for two sets do not fit in the registers of two waves)
-    hipLaunchKernelGGL((span_q4_few_kernel<BF16, 2>), grid, block, 0, st, a);
+  const bool past = a.tiles == 1 && (double)a.B * a.Hkv * a.nsplit * a.run * (2 * (kQ4RowBytes + kQ4ScaleBytes)) >= kPastBytes;
+  if (a.rows == 4 && past)
+    hipLaunchKernelGGL((span_q4_few_kernel<T, 1, true>), grid, block, 0, st, a);
+  else if (a.rows == 4)
+    hipLaunchKernelGGL((span_q4_few_kernel<T, 1, false>), grid, block, 0, st, a);
+  else if (T::EPC == 8 && a.rows == 8 && past)  // (fp32: its three terms for two sets do not fit in the registers of two waves)
+    hipLaunchKernelGGL((span_q4_few_kernel<BF16, 2, true>), grid, block, 0, st, a);
+  else if (T::EPC == 8 && a.rows == 8)
+    hipLaunchKernelGGL((span_q4_few_kernel<BF16, 2, false>), grid, block, 0, st, a);
   else if (a.rows == 16)
     hipLaunchKernelGGL((span_q4_kernel<T, 1>), grid, block, 0, st, a);
   else
