@@ -613,7 +613,7 @@ SpanPlan span_plan(const Shape& s, int m, int window, int sinks, bool bits4) {
   if (lds)
     p.rows = M <= 32 ? 32 : M <= 64 ? 64 : M <= 128 ? 128 : 256;
   else if (bits4)
-    p.rows = M <= 4 ? 4 : M <= 8 && s.dtype == 1 ? 8 : M <= 16 ? 16 : 32;
+    p.rows = M <= 4 ? 4 : M <= 8 ? 8 : M <= 16 ? 16 : 32;
   else if (s.dtype == 0 && M > 16)
     p.rows = 32;
   p.tiles = (int)((M + p.rows - 1) / p.rows);
@@ -621,8 +621,7 @@ SpanPlan span_plan(const Shape& s, int m, int window, int sinks, bool bits4) {
   const long long tokens = p.rows < M ? (p.rows + s.G - 1) / s.G + 1 : m, most = (long long)window + tokens - 1 + sinks;
   const long long read = window > 0 && most < s.S ? most : s.S, blocks = (long long)s.B * p.tiles * s.Hkv;
   // as many parts as fill the blocks that are resident together, by the kernels' registers
-  const bool three = bits4 ? s.dtype == 1 && p.rows == 4 : s.dtype == 0 && p.rows == 16;
-  const long long slots = (lds ? 1LL : three ? 3LL : 2LL) * device_cus();
+  const long long slots = (lds ? 1LL : bits4 ? span_q4_waves(s.dtype == 1, p.rows) : s.dtype == 0 && p.rows == 16 ? 3LL : 2LL) * device_cus();
   const int least = lds ? 256 : 128;
   long long n = (slots + blocks - 1) / blocks;
   if (n > (read + least - 1) / least) n = (read + least - 1) / least;
