@@ -26,10 +26,16 @@ __device__ __forceinline__ RowTarget row_target(const CacheView& c, int b, int H
   return {(((long long)page * Hkv) << c.pg.lg_rows) + (row & ((1 << c.pg.lg_rows) - 1)), 1LL << c.pg.lg_rows};
 }
 
-// Code of x: the quotient is rounded as IEEE division has it, so values half-way between two codes go to the even one.
-__device__ __forceinline__ uint32_t q4_code(float x, float low, float step) {
-  const float n = step > 0.f ? rintf((x - low) / step) : 0.f;
-  return (uint32_t)fminf(fmaxf(n, 0.f), 15.f);
+// Code of x: the quotient's nearest whole number, the even one half-way.  A product with the rounded reciprocal is off by less than 2^-18 there, and
+// what it leaves of x - lowest, exact but for one rounding, says on which side of half a step that was.
+__device__ __forceinline__ uint32_t q4_code(float x, float low, float step, float inv) {
+  const float t = x - low;
+  float n = rintf(t * inv);
+  const float rest = fmaf(-n, step, t), half = 0.5f * step;
+  const bool odd = ((int)n & 1) != 0;
+  if (rest > half || (rest == half && odd)) n += 1.f;
+  if (rest < -half || (rest == -half && odd)) n -= 1.f;
+  return step > 0.f ? (uint32_t)fminf(fmaxf(n, 0.f), 15.f) : 0u;
 }
 
 // cos and sin of an angle, formed in 64 bits and rounded once: pi / 2 in two terms takes the quarter turns off, Taylor polynomials on
@@ -85,23 +91,24 @@ __device__ __forceinline__ void store_q4(const float* row, int p, uint32_t* code
     hi = group_allreduce_max<LANES>(hi);
     // (a range past fp16's is clamped to its largest)
     const cache_half2_t sc = {(_Float16)fminf((hi - lo) / 15.f, 65504.f), (_Float16)fminf(fmaxf(lo, -65504.f), 65504.f)};
-    const float step = (float)sc.x, low = (float)sc.y;
+    const float step = (float)sc.x, low = (float)sc.y, inv = 1.0f / step;
 #pragma unroll
-    for (int w = 0; w < W; ++w) word[w] |= q4_code(x[w][g].x, low, step) << (4 * g) | q4_code(x[w][g].y, low, step) << (16 + 4 * g);
+    for (int w = 0; w < W; ++w) word[w] |= q4_code(x[w][g].x, low, step, inv) << (4 * g) | q4_code(x[w][g].y, low, step, inv) << (16 + 4 * g);
     if (p == g) scales[g] = __builtin_bit_cast(uint32_t, sc);
   }
 #pragma unroll
   for (int w = 0; w < W; ++w) codes[W * p + w] = word[w];
 }
 
-// STYLE as rotary_kernel's.
-template <typename T, int STYLE, bool BITS4>
+// STYLE and STREAM as rotary_kernel's.
+template <typename T, int STYLE, bool BITS4, bool STREAM>
 __global__ __launch_bounds__(kApThreads) void append_kernel(AppendArgs args) {
   using ST = typename T::store_t;
   constexpr int EPC = T::EPC;
   constexpr int kLanes = kD / EPC / 2;  // lanes of a row: two chunks each
   constexpr int kGroups = kApThreads / kLanes;
-  constexpr int U = BITS4 ? 2 : 4;  // rows of a lane group in flight
+  constexpr int kAngles = STYLE == 2 ? 1 : EPC;  // of a lane
+  constexpr int U = BITS4 ? 4 : 6;               // rows of a lane group in flight
   const RotaryArgs& a = args.r;
   __shared__ float2 s_cs[kApMaxTokens][kD / 2];
   __shared__ __align__(16) float s_row[BITS4 ? kGroups : 1][kD + 4];
@@ -124,34 +131,49 @@ __global__ __launch_bounds__(kApThreads) void append_kernel(AppendArgs args) {
   __syncthreads();
   if (mine >= ntok) return;
 
-  // the two chunks of this lane: a pair of rotated ones, or two of the columns behind R
+  // the two chunks of this lane: a pair of rotated ones, or two of the columns behind R; and their angles
   int c0 = p, c1 = p + kLanes;
   if (STYLE == 0) {
     const int np = pairs / EPC;
     c0 = p < np ? p : p + np;
     c1 = p < np ? p + np : p + kLanes;
   }
+  float2 cs[kAngles];
+#pragma unroll
+  for (int e = 0; e < kAngles; ++e) {
+    if (STYLE == 0) cs[e] = s_cs[mine][max(0, min(c0 * EPC + e, pairs - 1))];
+    if (STYLE == 1) cs[e] = s_cs[mine][max(0, min((e < EPC / 2 ? c0 : c1) * (EPC / 2) + e % (EPC / 2), pairs - 1))];
+  }
   const bool in_r = a.R > 0 && (STYLE != 0 || c1 * EPC < a.R);  // (STYLE 0: both chunks or none)
 
   for (int i0 = h0 + first; i0 < h1; i0 += step * U) {
     uint4 raw[U][2];
-    const ST* src[U];
-#pragma unroll
-    for (int u = 0; u < U; ++u) {
-      int h = min(i0 + u * step, h1 - 1);
-      const RotaryTensor& x = h < a.q.heads ? a.q : h < a.q.heads + Hkv ? a.k : a.v;
-      if (h >= a.q.heads) h = h - a.q.heads < Hkv ? h - a.q.heads : h - a.q.heads - Hkv;
-      src[u] = static_cast<const ST*>(x.in) + (b * x.in_batch + j * x.in_token + h * x.in_head);
-      raw[u][0] = load16(src[u] + c0 * EPC);
-      raw[u][1] = load16(src[u] + c1 * EPC);
-    }
+    ST* dst[U];           // null: not there; in 4 bits of the queries only
+    long long at[U];      // in 4 bits, of keys and values: their row, negative: not there
+    const ST* src[U];     // (STYLE 2)
+    bool turn[U], is_v[U];
 #pragma unroll
     for (int u = 0; u < U; ++u) {
       const int i = i0 + u * step;
-      if (i >= h1) break;
-      const bool is_q = i < a.q.heads, is_v = i >= a.q.heads + Hkv;
-      const int h = is_q ? i : is_v ? i - a.q.heads - Hkv : i - a.q.heads;
-      if (!is_q && to.first < 0) continue;  // padded token
+      int h = min(i, h1 - 1);
+      const bool is_q = h < a.q.heads;
+      if (!is_q) h -= a.q.heads;
+      is_v[u] = !is_q && h >= Hkv;
+      if (is_v[u]) h -= Hkv;
+      const RotaryTensor& x = is_q ? a.q : is_v[u] ? a.v : a.k;
+      src[u] = static_cast<const ST*>(x.in) + (b * x.in_batch + j * x.in_token + h * x.in_head);
+      raw[u][0] = load16_hint<STREAM>(src[u] + c0 * EPC);
+      raw[u][1] = load16_hint<STREAM>(src[u] + c1 * EPC);
+      turn[u] = in_r && !is_v[u];
+      const bool there = i < h1 && (is_q || to.first >= 0);  // (else padded)
+      const long long row = to.first + h * to.between;
+      at[u] = there && !is_q ? row : -1;
+      dst[u] = is_q ? static_cast<ST*>(a.q.out) + (b * a.q.out_batch + j * a.q.out_token + h * a.q.out_head)
+                    : static_cast<ST*>(is_v[u] ? args.cache.v : args.cache.k) + row * kD;
+      if (!there || (BITS4 && !is_q)) dst[u] = nullptr;
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
       float x0[EPC], x1[EPC], y0[EPC], y1[EPC];
       T::unpack(raw[u][0], x0);
       T::unpack(raw[u][1], x1);
@@ -160,67 +182,66 @@ __global__ __launch_bounds__(kApThreads) void append_kernel(AppendArgs args) {
         y0[e] = x0[e];
         y1[e] = x1[e];
       }
-      if (in_r && !is_v) {
+      if (turn[u]) {
         if constexpr (STYLE == 0) {
 #pragma unroll
           for (int e = 0; e < EPC; ++e) {
-            const float2 cs = s_cs[mine][c0 * EPC + e];
-            y0[e] = turned(x0[e], cs.x, x1[e], -cs.y);
-            y1[e] = turned(x1[e], cs.x, x0[e], cs.y);
+            y0[e] = turned(x0[e], cs[e].x, x1[e], -cs[e].y);
+            y1[e] = turned(x1[e], cs[e].x, x0[e], cs[e].y);
           }
-        } else {
-          auto turn = [&](int c, const float(&x)[EPC], float(&y)[EPC]) __attribute__((always_inline)) {
+        } else if constexpr (STYLE == 1) {
+#pragma unroll
+          for (int e = 0; e < EPC; ++e) {
+            const float2 z0 = cs[e / 2], z1 = cs[(EPC + e) / 2];
+            if (c0 * EPC + e < a.R) y0[e] = turned(x0[e], z0.x, x0[e ^ 1], e % 2 == 0 ? -z0.y : z0.y);
+            if (c1 * EPC + e < a.R) y1[e] = turned(x1[e], z1.x, x1[e ^ 1], e % 2 == 0 ? -z1.y : z1.y);
+          }
+        } else {  // partners that no chunk boundary respects, element by element
+#pragma unroll
+          for (int half = 0; half < 2; ++half)
 #pragma unroll
             for (int e = 0; e < EPC; ++e) {
-              const int col = c * EPC + e;
-              if (col >= a.R) continue;
-              if constexpr (STYLE == 1) {
-                const float2 cs = s_cs[mine][col / 2];
-                y[e] = turned(x[e], cs.x, x[e ^ 1], e % 2 == 0 ? -cs.y : cs.y);
-              } else {  // partners that no chunk boundary respects, element by element
+              const int col = (half ? c1 : c0) * EPC + e;
+              if (col < a.R) {
                 const bool lower = col < pairs;
-                const float2 cs = s_cs[mine][lower ? col : col - pairs];
+                const float2 z = s_cs[mine][lower ? col : col - pairs];
                 const float other = T::load1(src[u] + (lower ? col + pairs : col - pairs));
-                y[e] = turned(x[e], cs.x, other, lower ? -cs.y : cs.y);
+                (half ? y1[e] : y0[e]) = turned(half ? x1[e] : x0[e], z.x, other, lower ? -z.y : z.y);
               }
             }
-          };
-          turn(c0, x0, y0);
-          turn(c1, x1, y1);
         }
       }
-      if (is_q || !BITS4) {
-        const long long row = to.first + h * to.between;
-        ST* dst = is_q ? static_cast<ST*>(a.q.out) + (b * a.q.out_batch + j * a.q.out_token + h * a.q.out_head)
-                       : static_cast<ST*>(is_v ? args.cache.v : args.cache.k) + row * kD;
-        *reinterpret_cast<uint4*>(dst + c0 * EPC) = pack_chunk<T>(y0);
-        *reinterpret_cast<uint4*>(dst + c1 * EPC) = pack_chunk<T>(y1);
-      } else if constexpr (BITS4) {
-        const long long row = to.first + h * to.between;
-        float* mid = s_row[gid];
+      if (dst[u] != nullptr) {
+        store16_hint<STREAM>(dst[u] + c0 * EPC, pack_chunk<T>(y0));
+        store16_hint<STREAM>(dst[u] + c1 * EPC, pack_chunk<T>(y1));
+      }
+      if constexpr (BITS4) {
+        if (at[u] >= 0) {  // (the same for the lanes of a group)
+          float* mid = s_row[gid];
 #pragma unroll
-        for (int e = 0; e < EPC; e += 4) {
-          *reinterpret_cast<float4*>(mid + c0 * EPC + e) = make_float4(y0[e], y0[e + 1], y0[e + 2], y0[e + 3]);
-          *reinterpret_cast<float4*>(mid + c1 * EPC + e) = make_float4(y1[e], y1[e + 1], y1[e + 2], y1[e + 3]);
+          for (int e = 0; e < EPC; e += 4) {
+            *reinterpret_cast<float4*>(mid + c0 * EPC + e) = make_float4(y0[e], y0[e + 1], y0[e + 2], y0[e + 3]);
+            *reinterpret_cast<float4*>(mid + c1 * EPC + e) = make_float4(y1[e], y1[e + 1], y1[e + 2], y1[e + 3]);
+          }
+          __builtin_amdgcn_wave_barrier();  // (the group's lanes are of one wave, whose LDS operations keep their order)
+          store_q4<kLanes>(mid, p, static_cast<uint32_t*>(is_v[u] ? args.cache.v : args.cache.k) + at[u] * kQ4Words,
+                           static_cast<uint32_t*>(is_v[u] ? args.cache.v_scales : args.cache.k_scales) + at[u] * kQ4Groups);
+          __builtin_amdgcn_wave_barrier();
         }
-        __builtin_amdgcn_wave_barrier();  // (the group's lanes are of one wave, whose LDS operations keep their order)
-        store_q4<kLanes>(mid, p, static_cast<uint32_t*>(is_v ? args.cache.v : args.cache.k) + row * kQ4Words,
-                         static_cast<uint32_t*>(is_v ? args.cache.v_scales : args.cache.k_scales) + row * kQ4Groups);
-        __builtin_amdgcn_wave_barrier();
       }
     }
   }
 }
 
-template <typename T, bool BITS4>
+template <typename T, bool BITS4, bool STREAM>
 static hipError_t launch_append_t(const AppendArgs& a, dim3 grid, int style, hipStream_t st) {
   const dim3 block(kApThreads);
   if (style == 0)
-    hipLaunchKernelGGL((append_kernel<T, 0, BITS4>), grid, block, 0, st, a);
+    hipLaunchKernelGGL((append_kernel<T, 0, BITS4, STREAM>), grid, block, 0, st, a);
   else if (style == 1)
-    hipLaunchKernelGGL((append_kernel<T, 1, BITS4>), grid, block, 0, st, a);
+    hipLaunchKernelGGL((append_kernel<T, 1, BITS4, STREAM>), grid, block, 0, st, a);
   else
-    hipLaunchKernelGGL((append_kernel<T, 2, BITS4>), grid, block, 0, st, a);
+    hipLaunchKernelGGL((append_kernel<T, 2, BITS4, false>), grid, block, 0, st, a);
   return hipGetLastError();
 }
 
@@ -240,9 +261,12 @@ hipError_t launch_append(const Shape& s, AppendArgs args, hipStream_t st) {
   }
   const dim3 grid((a.total + a.tokens - 1) / a.tokens, (heads + a.heads_per_block - 1) / a.heads_per_block);
   const int style = a.interleaved ? 1 : (a.R / 2) % epc == 0 ? 0 : 2;
-  const bool bits4 = args.cache.k_scales != nullptr;
-  if (s.dtype == 0) return bits4 ? launch_append_t<F32, true>(args, grid, style, st) : launch_append_t<F32, false>(args, grid, style, st);
-  return bits4 ? launch_append_t<BF16, true>(args, grid, style, st) : launch_append_t<BF16, false>(args, grid, style, st);
+  // From 100 MB read and written on, past the caches (as launch_rotary); not in 4 bits, whose short rows are written piece by piece.
+  const bool past = 2.0 * a.total * heads * kD * s.elem_bytes >= 100e6;
+  if (args.cache.k_scales != nullptr)
+    return s.dtype == 0 ? launch_append_t<F32, true, false>(args, grid, style, st) : launch_append_t<BF16, true, false>(args, grid, style, st);
+  if (s.dtype == 0) return past ? launch_append_t<F32, false, true>(args, grid, style, st) : launch_append_t<F32, false, false>(args, grid, style, st);
+  return past ? launch_append_t<BF16, false, true>(args, grid, style, st) : launch_append_t<BF16, false, false>(args, grid, style, st);
 }
 
 // ---- rows of a cache back --------------------------------------------------------------------------------------
