@@ -108,7 +108,7 @@ __global__ __launch_bounds__(kApThreads) void append_kernel(AppendArgs args) {
   constexpr int kLanes = kD / EPC / 2;  // lanes of a row: two chunks each
   constexpr int kGroups = kApThreads / kLanes;
   constexpr int kAngles = STYLE == 2 ? 1 : EPC;  // of a lane
-  constexpr int U = BITS4 ? 4 : 6;               // rows of a lane group in flight
+  constexpr int U = BITS4 ? 2 : 6;               // rows of a lane group in flight
   const RotaryArgs& a = args.r;
   __shared__ float2 s_cs[kApMaxTokens][kD / 2];
   __shared__ __align__(16) float s_row[BITS4 ? kGroups : 1][kD + 4];
@@ -248,8 +248,10 @@ static hipError_t launch_append_t(const AppendArgs& a, dim3 grid, int style, hip
 hipError_t launch_append(const Shape& s, AppendArgs args, hipStream_t st) {
   RotaryArgs& a = args.r;
   const int epc = 16 / s.elem_bytes, heads = a.q.heads + 2 * s.Hkv;
-  // few tokens: the heads of a token are spread over blocks (as launch_rotary)
-  const int tokens = s.dtype == 0 ? 2 : kApMaxTokens;
+  // few tokens: the heads of a token are spread over blocks (as launch_rotary).  In 4 bits, us with 4 rows of a lane group in flight and 4 tokens a
+  // block, 4 and 2, 2 and 2, 2 and 4, 3 and 1: 4 x 1111 tokens of 32/8 bf16 heads 36.6, 33.7, 33.2, 33.1, 41.6, 2 x 512 15.9, 13.5, 13.4, 15.1, 13.4.
+  const bool bits4 = args.cache.k_scales != nullptr;
+  const int tokens = s.dtype == 0 || bits4 ? 2 : kApMaxTokens;
   a.tokens = a.total >= tokens * device_cus() ? tokens : 1;
   a.heads_per_block = heads;
   const int groups = kApThreads / (kD / epc / 2);
@@ -261,12 +263,16 @@ hipError_t launch_append(const Shape& s, AppendArgs args, hipStream_t st) {
   }
   const dim3 grid((a.total + a.tokens - 1) / a.tokens, (heads + a.heads_per_block - 1) / a.heads_per_block);
   const int style = a.interleaved ? 1 : (a.R / 2) % epc == 0 ? 0 : 2;
-  // From 100 MB read and written on, past the caches (as launch_rotary); not in 4 bits, whose short rows are written piece by piece.
+  // From 100 MB read and written on, past the caches (as launch_rotary), but for codes and scales, which are written piece by piece.
   const bool past = 2.0 * a.total * heads * kD * s.elem_bytes >= 100e6;
-  if (args.cache.k_scales != nullptr)
-    return s.dtype == 0 ? launch_append_t<F32, true, false>(args, grid, style, st) : launch_append_t<BF16, true, false>(args, grid, style, st);
-  if (s.dtype == 0) return past ? launch_append_t<F32, false, true>(args, grid, style, st) : launch_append_t<F32, false, false>(args, grid, style, st);
-  return past ? launch_append_t<BF16, false, true>(args, grid, style, st) : launch_append_t<BF16, false, false>(args, grid, style, st);
+#define LOKI_APPEND(T, BITS4) return past ? launch_append_t<T, BITS4, true>(args, grid, style, st) : launch_append_t<T, BITS4, false>(args, grid, style, st)
+  if (bits4) {
+    if (s.dtype == 0) LOKI_APPEND(F32, true);
+    LOKI_APPEND(BF16, true);
+  }
+  if (s.dtype == 0) LOKI_APPEND(F32, false);
+  LOKI_APPEND(BF16, false);
+#undef LOKI_APPEND
 }
 
 // ---- rows of a cache back --------------------------------------------------------------------------------------
