@@ -309,10 +309,10 @@ struct SpanArgs {
   int B, m, G, Hq, Hkv, S_max, window, sinks;
   int rows, tiles, nsplit, run;  // tiles of `rows` query rows of a sequence and KV head, each cut into up to nsplit parts of `run` rows
 };
-// Blocks of the 4-bit kernels that a CU holds, by the registers of tiles of `rows` query rows.  us with more (their registers then less, with
-// some in scratch): 16 sequences of 32/8 bf16 heads with 16384 rows (4 rows) three 65.0, four 70.0; 64 of 64/8 with 4096 (8) two 78.3,
-// three 92.8; 16 of 64/8 with 8000 and two tokens each (16) one 71.1, two 65.6; fp32, 16 of 32/8 with 8000, four tokens (16) one 79, two 105.
-__host__ __device__ constexpr int span_q4_waves(bool bf16, int rows) { return rows == 32 ? 1 : rows == 16 ? (bf16 ? 2 : 1) : rows == 4 && bf16 ? 3 : 2; }
+// Blocks of the 4-bit kernels that a CU holds, by the registers of tiles of `rows` query rows.  us with more or fewer: 16 sequences of 32/8 bf16 heads up
+// to 16384 rows (4 rows) four 57.7, three 60.7; 64 of 64/8 up to 4096 (8) two 68.1, three 75.6; fp32, 16 of 8/8 up to 8000 (4) three 39.6, two
+// 43.0; 16 of 32/8 with 8000, four tokens (16) two 57.2, one 75.3.
+__host__ __device__ constexpr int span_q4_waves(bool bf16, int rows) { return rows == 4 ? (bf16 ? 4 : 3) : 2; }
 // How a call is cut: the workspace's size and the launch go by it.
 struct SpanPlan {
   int rows, tiles, nsplit, run;

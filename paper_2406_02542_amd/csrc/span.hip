@@ -613,7 +613,7 @@ SpanPlan span_plan(const Shape& s, int m, int window, int sinks, bool bits4) {
   if (lds)
     p.rows = M <= 32 ? 32 : M <= 64 ? 64 : M <= 128 ? 128 : 256;
   else if (bits4)
-    p.rows = M <= 4 ? 4 : M <= 8 ? 8 : M <= 16 ? 16 : 32;
+    p.rows = M <= 4 ? 4 : M <= 8 ? 8 : 16;
   else if (s.dtype == 0 && M > 16)
     p.rows = 32;
   p.tiles = (int)((M + p.rows - 1) / p.rows);
