@@ -4,7 +4,7 @@
 // Up to 16 query rows of a KV head (span_rows_kernel, span_f32_kernel): memory bounds it, a wave takes steps of rows straight from
 // registers, a block's waves take steps in turn.  More, in bf16 (span_tiles_kernel): the matrix cores bound it, tiles of keys and
 // values go through LDS for all of the block's query rows.
-#include "span_impl.h"
+#include "span_tiles_impl.h"
 
 namespace loki {
 
@@ -278,267 +278,6 @@ __global__ __launch_bounds__(64 * kSpWaves, 2) void span_f32_kernel(SpanArgs a) 
   span_store<F32>(a, sm, tile, r0, live);
 }
 
-// ---- bf16, more query rows: tiles through LDS -------------------------------------------------------------------------
-// The products of shared.hip's prefix kernel: a wave holds 32 query rows and takes steps of 32 keys, S^T = K Q^T and O^T += V^T P^T by
-// v_mfma_f32_32x32x16_bf16, the weights in two bf16 terms as they come out of the first product.  Tiles of KT keys and values go through LDS
-// once for the block's waves, WQ of which hold different queries and WK = WAVES / WQ different keys of the tile; the next tile is loaded into
-// registers while this one is used.  What is masked is decided for a wave's step as a whole: nothing to see, everything, or each on its own.
-typedef short sp_s16x4_t __attribute__((ext_vector_type(4)));
-typedef float sp_f32x16_t __attribute__((ext_vector_type(16)));
-typedef __attribute__((address_space(3))) sp_s16x4_t sp_lds_s16x4_t;
-
-template <int WAVES, int WQ>
-constexpr int span_tile_keys() {
-  return WAVES / WQ == 4 ? 128 : 64;
-}
-// Two pairs of tiles; at the end, where waves have other keys of the same queries, what half of them hand over, or the outputs.
-template <int WAVES, int WQ>
-constexpr int span_lds_bytes() {
-  const int tiles = 4 * span_tile_keys<WAVES, WQ>() * 256, merge = WQ == WAVES ? 0 : WAVES * 32 * 8 + WAVES / 2 * 64 * 256;
-  return tiles > merge ? tiles : merge;
-}
-
-template <int WAVES, int WQ>
-__global__ __launch_bounds__(64 * WAVES, WAVES == 4 ? 1 : 2) void span_tiles_kernel(SpanArgs a) {
-  extern __shared__ __align__(16) char smem[];  // [2][K tile, V tile]
-  constexpr int kThreads = 64 * WAVES, WK = WAVES / WQ, KT = span_tile_keys<WAVES, WQ>(), kSteps = KT / (32 * WK), kChunks = KT * 16 / kThreads;
-  constexpr int kTileBytes = KT * 256;
-  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int l32 = lane & 31, half = lane >> 5, l16 = lane & 15;
-  const int wq = wave % WQ, wk = wave / WQ;
-  const SpanTile tile = span_tile<KT>(a);
-  const int M = a.m * a.G, r0 = tile.tile * (32 * WQ), live = min(32 * WQ, M - r0), lg = 31 - __builtin_clz(a.G);
-  const SpanRows rows = tile.rows;
-  const SpanSteps<KT> steps(rows);
-  if (tile.s0 >= tile.s1 && tile.part > 0) return span_none(a, tile, live);  // (uniform for the block)
-  const int s0 = tile.s0, s1 = tile.s1;
-  const RowPlaces places(a.cache, tile.b, tile.h, a.Hkv);
-  // this wave's queries, and its lane's
-  const int q0 = wq * 32, mine = min(32, live - q0), row = q0 + l32;
-  SpanRows own{0, 0, 0, 0};
-  if (mine > 0) own = span_rows(a, tile.b, (r0 + q0) >> lg, (r0 + q0 + mine - 1) >> lg);
-  const int len = row < live ? span_len(a, tile.b, (r0 + row) >> lg) : 0;
-
-  am_bf16x8_t q[8];
-  {
-    const uint16_t* src = static_cast<const uint16_t*>(a.q) + span_place(a, tile.b, tile.h, r0 + min(row, live - 1)) * kD + 8 * half;
-#pragma unroll
-    for (int ks = 0; ks < 8; ++ks) q[ks] = __builtin_bit_cast(am_bf16x8_t, load16(src + 16 * ks));
-  }
-  const uint16_t* kb = static_cast<const uint16_t*>(a.cache.k) + l16 * 8;
-  const uint16_t* vb = static_cast<const uint16_t*>(a.cache.v) + l16 * 8;
-  uint4 kst[kChunks], vst[kChunks];
-  auto load = [&](int s) __attribute__((always_inline)) {  // (a wave's four rows of a chunk lie in one page)
-    const SpanStep st = span_step(steps, rows, s);
-#pragma unroll
-    for (int j = 0; j < kChunks; ++j) {
-      const int first = st.at + 4 * wave + kThreads / 16 * j;
-      const long long off = (places(min(max(first, st.lo), st.hi - 1)) + min(max(first + (lane >> 4), st.lo), st.hi - 1)) * kD;
-      kst[j] = load16(kb + off);
-      vst[j] = load16(vb + off);
-    }
-  };
-  auto store = [&](int b) __attribute__((always_inline)) {
-    char* base = smem + b * 2 * kTileBytes;
-#pragma unroll
-    for (int j = 0; j < kChunks; ++j) {
-      const int at = tid + kThreads * j, r = at >> 4, c = at & 15;
-      *reinterpret_cast<uint4*>(base + r * 256 + ((c ^ (r & 15)) * 16)) = kst[j];
-      *reinterpret_cast<uint4*>(base + kTileBytes + r * 256 + ((c ^ ((r & 3) << 2)) * 16)) = vst[j];
-    }
-  };
-
-  float m = kNegBig, l = 0.f;
-  sp_f32x16_t o[4];
-#pragma unroll
-  for (int c = 0; c < 4; ++c) o[c] = sp_f32x16_t{};
-  const int k_at = l32 * 256 + ((half ^ l16) * 16);
-  const int v_row = 4 * half + (l16 >> 2);
-  const int v_at = kTileBytes + v_row * 256 + (((((lane >> 4) & 1) * 2 + ((l16 & 3) >> 1)) ^ ((v_row & 3) << 2)) * 16) + (l16 & 1) * 8;
-
-  // 32 keys of the tile in buffer `base`, rows st.at ..; full: all of them are seen by all of the wave's queries
-  auto step = [&](const char* base, const SpanStep& st, bool full) __attribute__((always_inline)) {
-    am_bf16x8_t ka[8], va[2][4];
-#pragma unroll
-    for (int ks = 0; ks < 8; ++ks) ka[ks] = __builtin_bit_cast(am_bf16x8_t, *reinterpret_cast<const uint4*>(base + (k_at ^ (ks * 32))));
-    __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-    for (int ks = 0; ks < 2; ++ks)
-#pragma unroll
-      for (int c = 0; c < 4; ++c) {
-        const char* at = base + (v_at ^ (c * 64)) + ks * 4096;
-        const sp_s16x4_t x = __builtin_amdgcn_ds_read_tr16_b64_v4i16((sp_lds_s16x4_t*)(at));
-        const sp_s16x4_t y = __builtin_amdgcn_ds_read_tr16_b64_v4i16((sp_lds_s16x4_t*)(at + 2048));
-        va[ks][c] = __builtin_bit_cast(am_bf16x8_t, __builtin_shufflevector(x, y, 0, 1, 2, 3, 4, 5, 6, 7));
-      }
-    sp_f32x16_t s = sp_f32x16_t{};
-#pragma unroll
-    for (int ks = 0; ks < 8; ++ks) s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(ka[ks], q[ks], s, 0, 0, 0);
-    __builtin_amdgcn_sched_barrier(0);
-    if (!full) {  // (uniform)
-#pragma unroll
-      for (int i = 0; i < 16; ++i)
-        if (!span_sees(a, st, len, st.at + 8 * (i >> 2) + 4 * half + (i & 3))) s[i] = kUnseen;
-    }
-    float p[16], sum;
-    auto weights = [&]() __attribute__((always_inline)) {
-#pragma unroll
-      for (int i = 0; i < 16; ++i) p[i] = fast_exp2(fmaf(s[i], kSoftmaxScaleLog2, -m));
-      float odd = p[1];
-      sum = p[0];
-#pragma unroll
-      for (int i = 2; i < 16; i += 2) {
-        sum += p[i];
-        odd += p[i + 1];
-      }
-      sum += odd;
-    };
-    weights();
-    if (__ballot(!(sum <= kPfGrowth)) != 0ull) {
-      float top = s[0];
-#pragma unroll
-      for (int i = 1; i < 16; ++i) top = fmaxf(top, s[i]);
-      top = fmaxf(top, __shfl_xor(top, 32)) * kSoftmaxScaleLog2;
-      const float mn = fmaxf(m, top), corr = fast_exp2(m - mn);
-      m = mn;
-      l *= corr;
-#pragma unroll
-      for (int c = 0; c < 4; ++c)
-#pragma unroll
-        for (int i = 0; i < 16; ++i) o[c][i] *= corr;
-      weights();
-    }
-    l += sum;
-    uint32_t w[2][8];  // the weights' two terms
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      w[0][i] = BF16::round2(p[2 * i], p[2 * i + 1]);
-      w[1][i] = BF16::round2(p[2 * i] - __uint_as_float(w[0][i] << 16), p[2 * i + 1] - __uint_as_float(w[0][i] & 0xffff0000u));
-    }
-#pragma unroll
-    for (int ks = 0; ks < 2; ++ks)
-#pragma unroll
-      for (int t = 0; t < 2; ++t)
-#pragma unroll
-        for (int c = 0; c < 4; ++c)
-          o[c] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
-              va[ks][c], __builtin_bit_cast(am_bf16x8_t, make_uint4(w[t][4 * ks], w[t][4 * ks + 1], w[t][4 * ks + 2], w[t][4 * ks + 3])), o[c], 0, 0, 0);
-  };
-
-  if (s0 < s1) {
-    load(s0);
-    store(0);
-    __syncthreads();
-    for (int t = s0; t < s1; ++t) {
-      if (t + 1 < s1) load(t + 1);
-      const char* base = smem + ((t - s0) & 1) * 2 * kTileBytes;
-      const SpanStep whole = span_step(steps, rows, t);
-#pragma unroll 1
-      for (int s = 0; s < kSteps; ++s) {
-        const int key = (s * WK + wk) * 32;
-        const SpanStep st{whole.at + key, whole.lo, whole.hi};
-        // (all uniform for the wave)
-        if (st.at >= min(st.hi, own.hi) || st.at + 32 <= st.lo || (st.at + 32 <= own.lo && st.at >= a.sinks)) continue;
-        step(base + key * 256, st, span_full(a, own, st, 32));
-      }
-      if (t + 1 < s1) store((t + 1 - s0) & 1);
-      __syncthreads();
-    }
-  }
-
-  // both halves of a query's keys; then the waves that had other keys of the same queries
-  l += __shfl_xor(l, 32);
-  if constexpr (WK > 1) {
-    float2* ml = reinterpret_cast<float2*>(smem);                   // [wave][32] (max, sum)
-    float4* ob = reinterpret_cast<float4*>(smem + WAVES * 32 * 8);  // [wave of the upper half][4][4][lane]
-    if (half == 0) ml[wave * 32 + l32] = make_float2(m, l);
-    __syncthreads();
-    float mn = kNegBig, ls = 0.f;
-#pragma unroll
-    for (int w = 0; w < WK; ++w) mn = fmaxf(mn, ml[(w * WQ + wq) * 32 + l32].x);
-#pragma unroll
-    for (int w = 0; w < WK; ++w) {
-      const float2 x = ml[(w * WQ + wq) * 32 + l32];
-      ls = fmaf(x.y, fast_exp2(x.x - mn), ls);
-    }
-    const float f = fast_exp2(m - mn);
-    m = mn;
-    l = ls;
-#pragma unroll
-    for (int c = 0; c < 4; ++c)
-#pragma unroll
-      for (int i = 0; i < 16; ++i) o[c][i] *= f;
-#pragma unroll
-    for (int n = WK / 2; n >= 1; n /= 2) {
-      if (wk >= n && wk < 2 * n) {
-        float4* dst = ob + ((wk - n) * WQ + wq) * 16 * 64;
-#pragma unroll
-        for (int c = 0; c < 4; ++c)
-#pragma unroll
-          for (int i = 0; i < 4; ++i)
-            dst[(c * 4 + i) * 64 + lane] = make_float4(o[c][4 * i], o[c][4 * i + 1], o[c][4 * i + 2], o[c][4 * i + 3]);
-      }
-      __syncthreads();
-      if (wk < n) {
-        const float4* src = ob + (wk * WQ + wq) * 16 * 64;
-#pragma unroll
-        for (int c = 0; c < 4; ++c)
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            const float4 x = src[(c * 4 + i) * 64 + lane];
-            o[c][4 * i] += x.x;
-            o[c][4 * i + 1] += x.y;
-            o[c][4 * i + 2] += x.z;
-            o[c][4 * i + 3] += x.w;
-          }
-      }
-      __syncthreads();
-    }
-    if (wk != 0) return;
-  }
-  if (len == 0) l = 0.f;  // (a padded token's lanes took whatever full steps gave)
-  const float inv = l > 0.f ? 1.0f / l : 0.f;  // (a token without rows: zeros)
-  const bool parts = a.nsplit > 1;
-  // a lane has four columns of one query at a time: through LDS, so that a store takes four half rows
-  char* at = smem + wave * 8192;  // [32 queries][64 columns], 16-byte chunks exchanged as the keys'
-#pragma unroll
-  for (int pass = 0; pass < 2; ++pass) {
-#pragma unroll
-    for (int c = 0; c < 2; ++c)
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const sp_f32x16_t& x = o[2 * pass + c];
-        const float f = parts ? 1.0f : inv;
-        *reinterpret_cast<float4*>(at + l32 * 256 + (((8 * c + 2 * i + half) ^ l16) * 16)) = make_float4(x[4 * i] * f, x[4 * i + 1] * f, x[4 * i + 2] * f, x[4 * i + 3] * f);
-      }
-    __builtin_amdgcn_wave_barrier();
-#pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      const int r = 4 * j + (lane >> 4);
-      const float4 x = *reinterpret_cast<const float4*>(at + r * 256 + ((l16 ^ (r & 15)) * 16));
-      if (q0 + r < live) {
-        if (parts)
-          *reinterpret_cast<float4*>(span_part(a, tile, q0 + r) + 64 * pass + 4 * l16) = x;
-        else
-          *reinterpret_cast<uint2*>(static_cast<uint16_t*>(a.out) + span_place(a, tile.b, tile.h, r0 + q0 + r) * kD + 64 * pass + 4 * l16) = make_uint2(BF16::round2(x.x, x.y), BF16::round2(x.z, x.w));
-      }
-    }
-    __builtin_amdgcn_wave_barrier();
-  }
-  if (parts && half == 0 && row < live)
-    *reinterpret_cast<float2*>(span_part(a, tile, row) + kD) = make_float2(m, l);
-}
-
-template <int WAVES, int WQ>
-static hipError_t launch_tiles(const SpanArgs& a, dim3 grid, hipStream_t st) {
-  static std::atomic<unsigned long long> raised{0};
-  constexpr int bytes = span_lds_bytes<WAVES, WQ>();
-  const hipError_t e = allow_dynamic_lds(reinterpret_cast<const void*>(&span_tiles_kernel<WAVES, WQ>), bytes, raised);
-  if (e != hipSuccess) return e;
-  hipLaunchKernelGGL((span_tiles_kernel<WAVES, WQ>), grid, dim3(64 * WAVES), bytes, st, a);
-  return hipGetLastError();
-}
-
 // ---- parts joined ---------------------------------------------------------------------------------------------------
 // 32 lanes take a query row, 16 bytes of each of its parts; GROUPS of them share a row's parts, four each at a time.
 template <typename T, int GROUPS>
@@ -606,12 +345,18 @@ __global__ __launch_bounds__(256) void span_merge_kernel(const float* __restrict
 }
 
 // ---- the launch -----------------------------------------------------------------------------------------------------
+// Which kernel and how many blocks.  Tiles through LDS from 65 query rows of a KV head on, and from 33 on where more than 33 MB are read, us
+// 16 rows at a time / so: 1 x 64 tokens of 8/8 heads, window 512 9.1 / 14.9, 2 x 8 of 64/8, window 1000 13.7 / 17.5, 4000 (33 MB) 19.6 / 20.1, 8 x 16 of
+// 32/8 up to 8192 rows 92.5 / 54.1; with 32 query rows 8 x 4 of 64/8, window 1000 14.9 / 17.6, 2000 23.1 / 25.6, 8192 59.8 / 58.0; in 4 bits, 8192 rows, 8 x 8 tokens of
+// 64/8 (64 query rows) 79 / 91, 4 x 20 of 32/8 (80) 65.6 / 53.2, 4 x 64 of 32/8 (256) 143 / 92.
 SpanPlan span_plan(const Shape& s, int m, int window, int sinks, bool bits4) {
   SpanPlan p{16, 0, 1, 0};
   const long long M = (long long)m * s.G;
-  const bool lds = s.dtype == 1 && !bits4 && M > 16;
+  const long long tokens_read = window > 0 ? (long long)window + m - 1 + sinks : s.S, most_read = tokens_read < s.S ? tokens_read : s.S;
+  const double bytes = (double)s.B * s.Hkv * most_read * (2 * kD * s.elem_bytes);
+  const bool lds = s.dtype == 1 && (M > 64 || (!bits4 && M > 32 && bytes > 33e6));
   if (lds)
-    p.rows = M <= 32 ? 32 : M <= 64 ? 64 : M <= 128 ? 128 : 256;
+    p.rows = M <= 64 ? 64 : M <= 128 ? 128 : 256;
   else if (bits4)
     p.rows = M <= 4 ? 4 : M <= 8 ? 8 : 16;
   else if (s.dtype == 0 && M > 16)
@@ -622,7 +367,8 @@ SpanPlan span_plan(const Shape& s, int m, int window, int sinks, bool bits4) {
   const long long read = window > 0 && most < s.S ? most : s.S, blocks = (long long)s.B * p.tiles * s.Hkv;
   // as many parts as fill the blocks that are resident together, by the kernels' registers
   const long long slots = (lds ? 1LL : bits4 ? span_q4_waves(s.dtype == 1, p.rows) : s.dtype == 0 && p.rows == 16 ? 3LL : 2LL) * device_cus();
-  const int least = lds ? 256 : 128;
+  // (the more the longer S is, also over the change to tiles of 64 rows, one for every three or four of 16: a workspace for a length serves shorter ones)
+  const int least = 128;
   long long n = (slots + blocks - 1) / blocks;
   if (n > (read + least - 1) / least) n = (read + least - 1) / least;
   p.nsplit = n < 1 ? 1 : (int)n;
@@ -671,14 +417,12 @@ hipError_t launch_span(const Shape& s, SpanArgs a, hipStream_t st) {
     hipLaunchKernelGGL((span_rows_kernel<true>), grid, block, 0, st, a);
   else if (plan.rows == 16)
     hipLaunchKernelGGL((span_rows_kernel<false>), grid, block, 0, st, a);
-  else if (plan.rows == 32)
-    e = launch_tiles<4, 1>(a, grid, st);
   else if (plan.rows == 64)
-    e = launch_tiles<8, 2>(a, grid, st);
+    e = launch_span_tiles<8, 2, false>(a, st);
   else if (plan.rows == 128)
-    e = launch_tiles<8, 4>(a, grid, st);
+    e = launch_span_tiles<8, 4, false>(a, st);
   else
-    e = launch_tiles<8, 8>(a, grid, st);
+    e = launch_span_tiles<8, 8, false>(a, st);
   if (e == hipSuccess) e = hipGetLastError();
   if (e != hipSuccess || a.nsplit == 1) return e;
   if (s.dtype == 1)

@@ -7,18 +7,11 @@
 // and the codes go to the matrix cores as they are: the bits 0x3f80 | n << 3 are the bf16 number 1 + n / 16, exactly, a shift and a bit
 // select for two of them.  The ones' share is taken off in advance (the first product begins with minus the group's sum of q) or
 // at the end (sum over rows of p (lowest_g - 16 step_g), with the lowest values' share).
-#include "span_impl.h"
+#include "span_tiles_impl.h"
 
 namespace loki {
 
 constexpr int kQ4Waves = 4;
-
-// Codes g of a word's halves as two bf16 numbers 1 + n / 16.  The constants are kept in registers: one instruction takes both then.
-struct Q4Pair {
-  uint32_t mask = 0x00780078u, one = 0x3f803f80u;
-  __device__ __forceinline__ Q4Pair() { asm("" : "+v"(mask), "+s"(one)); }
-  __device__ __forceinline__ uint32_t operator()(uint32_t x, int g) const { return ((g == 0 ? x << 3 : x >> (4 * g - 3)) & mask) | one; }
-};
 
 template <bool STREAM>
 __device__ __forceinline__ uint32_t load4_hint(const void* p) {
@@ -32,17 +25,6 @@ struct alignas(4 * N) Q4Scales {
   uint32_t w[N];
   __device__ __forceinline__ cache_half2_t at(int n) const { return __builtin_bit_cast(cache_half2_t, w[n]); }
 };
-
-// x0, x1 as TERMS pairs of bf16 numbers that add up to them.
-template <int TERMS>
-__device__ __forceinline__ void q4_terms(float x0, float x1, uint32_t (&w)[TERMS]) {
-#pragma unroll
-  for (int t = 0; t < TERMS; ++t) {
-    w[t] = BF16::round2(x0, x1);
-    x0 -= __uint_as_float(w[t] << 16);  // exact in fp32
-    x1 -= __uint_as_float(w[t] & 0xffff0000u);
-  }
-}
 
 // A lane's column of the matrix cores' 16 is query row n / CG in CG ways: with the NS = 4 / CG groups n % CG * NS ..  Up to 4 query rows take
 // CG = 4, up to 8 two, more one, 16 at a time.
@@ -274,6 +256,8 @@ template <typename T>
 static hipError_t launch_span_q4_t(const SpanArgs& a, hipStream_t st) {
   const dim3 grid((unsigned)((long long)a.B * a.Hkv * a.tiles * a.nsplit)), block(64 * kQ4Waves);
   const bool past = a.tiles == 1 && (double)a.B * a.Hkv * a.nsplit * a.run * (2 * (kQ4RowBytes + kQ4ScaleBytes)) >= kPastBytes;
+  if (T::EPC == 8 && a.rows == 128) return launch_span_tiles<8, 4, true>(a, st);
+  if (T::EPC == 8 && a.rows == 256) return launch_span_tiles<8, 8, true>(a, st);
   if (a.rows == 4 && past)
     hipLaunchKernelGGL((span_q4_kernel<T, 4, true>), grid, block, 0, st, a);
   else if (a.rows == 4)

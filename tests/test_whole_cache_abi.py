@@ -92,7 +92,7 @@ def test_read_refusals():
 
 @pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
 @pytest.mark.parametrize("scales", [None, P])
-@pytest.mark.parametrize("B,Hq,Hkv", [(1, 8, 8), (3, 8, 1), (64, 64, 8)])
+@pytest.mark.parametrize("B,Hq,Hkv", [(1, 8, 8), (3, 8, 1), (64, 64, 8), (2, 64, 8), (5, 32, 8)])
 def test_workspace_of_the_longest_length_serves_shorter_ones(B, Hq, Hkv, scales, dtype):
     lay = api.make_layout(B, Hq, Hkv, 128, 128, 1 << 20, dtype)
     c, n = _cache(k_scales=scales, v_scales=scales), ctypes.c_size_t()
@@ -101,7 +101,7 @@ def test_workspace_of_the_longest_length_serves_shorter_ones(B, Hq, Hkv, scales,
         assert api.lib().dense_cache_workspace_bytes(by(lay), by(c), S, by(api.SpanArgs(**kw)), by(n)) == 0
         return n.value
 
-    for kw in (dict(), dict(window=1), dict(window=1000, sinks=4), dict(queries_per_seq=5), dict(queries_per_seq=300, window=4096), dict(queries_per_seq=3000)):
+    for kw in (dict(), dict(window=1), dict(window=1000, sinks=4), dict(queries_per_seq=5), dict(queries_per_seq=8), dict(queries_per_seq=13, window=20000), dict(queries_per_seq=300, window=4096), dict(queries_per_seq=3000)):
         sizes = [size(S, **kw) for S in (1, 2, 31, 64, 65, 127, 128, 129, 255, 700, 1100, 4186, 8192, 16384, 100000, 1 << 20)]
         assert sizes == sorted(sizes), kw
 
