@@ -25,17 +25,18 @@ typedef const __attribute__((address_space(4))) int32_t cache_const_i32_t;
 // the start of the pool.  An entry that names no page is clamped: such rows are never part of a result, but are read.
 struct RowPlaces {
   long long first;  // contiguous: row 0 of the unit
-  cache_const_i32_t* table;
+  cache_const_i32_t* table;  // (contiguous: the keys, of which one word is read and not used, in place of a branch)
+  bool paged;
   int lg, n_pages, Hkv, h;
   __device__ __forceinline__ RowPlaces(const CacheView& c, int b, int h_, int Hkv_)
       : first(((long long)b * Hkv_ + h_) * c.S_cap),
-        table(c.pg.table == nullptr ? nullptr : (cache_const_i32_t*)(c.pg.table + (long long)b * c.pg.pages_per_seq)),
-        lg(c.pg.lg_rows), n_pages(c.pg.n_pages), Hkv(Hkv_), h(h_) {}
-  __device__ __forceinline__ int entry(int row) const { return table == nullptr ? 0 : table[__builtin_amdgcn_readfirstlane(row >> lg)]; }
+        table((cache_const_i32_t*)(c.pg.table == nullptr ? static_cast<const int32_t*>(c.k) : c.pg.table + (long long)b * c.pg.pages_per_seq)),
+        paged(c.pg.table != nullptr), lg(c.pg.lg_rows), n_pages(c.pg.n_pages), Hkv(Hkv_), h(h_) {}
+  __device__ __forceinline__ int entry(int row) const { return table[__builtin_amdgcn_readfirstlane(paged ? row >> lg : 0)]; }
   __device__ __forceinline__ long long place(int row, int entry) const {
-    if (table == nullptr) return first;
     const int at = __builtin_amdgcn_readfirstlane(row >> lg);
-    return ((long long)min(max(entry, 0), n_pages - 1) * Hkv + h - at) << lg;
+    const long long in_page = ((long long)min(max(entry, 0), n_pages - 1) * Hkv + h - at) << lg;
+    return paged ? in_page : first;
   }
   __device__ __forceinline__ long long operator()(int row) const { return place(row, entry(row)); }
 };
