@@ -6,7 +6,7 @@
 //   out[c]     = sum over rows of (16 p step_g)[row] n[row, c] / 16 + sum over rows of (p lowest_g)[row]          for c in g
 // and the codes go to the matrix cores as they are: the bits 0x3f80 | n << 3 are the bf16 number 1 + n / 16, exactly, a shift and a bit
 // select for two of them.  The ones' share is taken off in advance (the first product begins with minus the group's sum of q) or
-// at the end (sum over rows of p (lowest_g - 16 step_g), with the lowest values' share).
+// at the end (the product of the same terms with ones).
 #include "span_tiles_impl.h"
 
 namespace loki {
@@ -25,6 +25,13 @@ struct alignas(4 * N) Q4Scales {
   uint32_t w[N];
   __device__ __forceinline__ cache_half2_t at(int n) const { return __builtin_bit_cast(cache_half2_t, w[n]); }
 };
+
+// p times a row's step, from its half of the scales' word (which v_fma_mix_f32 takes as it is, and the compiler converts first).
+__device__ __forceinline__ float q4_times_step(float p, uint32_t scales) {
+  float x;
+  asm("v_fma_mix_f32 %0, %1, %2, 0 op_sel_hi:[0,1,0]" : "=v"(x) : "v"(p), "v"(scales));
+  return x;
+}
 
 // A lane's column of the matrix cores' 16 is query row n / CG in CG ways: with the NS = 4 / CG groups n % CG * NS ..  Up to 4 query rows take
 // CG = 4, up to 8 two, more one, 16 at a time.
@@ -106,7 +113,8 @@ __global__ __launch_bounds__(64 * kQ4Waves, span_q4_waves(T::EPC == 8, 16 / CG))
   am_bf16x8_t bq[kQ4Groups][QT];
   float qsum[NS], low[NS];  // qsum: of a group's columns
   float m = kNegBig, l = 0.f;
-  am_f32x4_t o[NS][2];
+  am_f32x4_t o[NS][2], ones[NS];  // ones: the sum of the numbers that multiply codes, in every element
+  const am_bf16x8_t one = __builtin_bit_cast(am_bf16x8_t, make_uint4(0x3f803f80u, 0x3f803f80u, 0x3f803f80u, 0x3f803f80u));
   const typename T::store_t* src =
       static_cast<const typename T::store_t*>(a.q) + span_place(a, tile.b, tile.h, r0 + min(r, live - 1)) * kD + 32 * g0 + 8 * kgrp;
 #pragma unroll
@@ -129,7 +137,7 @@ __global__ __launch_bounds__(64 * kQ4Waves, span_q4_waves(T::EPC == 8, 16 / CG))
     sum += __shfl_xor(sum, 16);
     qsum[n] = sum + __shfl_xor(sum, 32);
     low[n] = 0.f;
-    o[n][0] = o[n][1] = am_f32x4_t{};
+    o[n][0] = o[n][1] = ones[n] = am_f32x4_t{};
   }
 
   for (; s < s1; s += kQ4Waves) {
@@ -191,6 +199,7 @@ __global__ __launch_bounds__(64 * kQ4Waves, span_q4_waves(T::EPC == 8, 16 / CG))
         for (int i = 0; i < 4; ++i) {
           o[n][0][i] *= corr;
           o[n][1][i] *= corr;
+          ones[n][i] *= corr;
         }
       }
       weights();
@@ -210,12 +219,13 @@ __global__ __launch_bounds__(64 * kQ4Waves, span_q4_waves(T::EPC == 8, 16 / CG))
       uint32_t w[4][PT];
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        const cache_half2_t c0 = sc[2 * i].at(n), c1 = sc[2 * i + 1].at(n);
         const float p0 = p[2 * i], p1 = p[2 * i + 1];
-        // lowest - 16 step: a code's value less its number 1 + n / 16 times 16 step
-        low[n] = fmaf(p0, fmaf(-16.f, (float)c0.x, (float)c0.y), fmaf(p1, fmaf(-16.f, (float)c1.x, (float)c1.y), low[n]));
-        q4_terms<PT>(p0 * (float)c0.x, p1 * (float)c1.x, w[i]);
+        low[n] = fmaf(p0, (float)sc[2 * i].at(n).y, fmaf(p1, (float)sc[2 * i + 1].at(n).y, low[n]));
+        q4_terms<PT>(q4_times_step(p0, sc[2 * i].w[n]), q4_times_step(p1, sc[2 * i + 1].w[n]), w[i]);
       }
+#pragma unroll
+      for (int t = PT - 1; t >= 0; --t)
+        ones[n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(one, __builtin_bit_cast(am_bf16x8_t, make_uint4(w[0][t], w[1][t], w[2][t], w[3][t])), ones[n], 0, 0, 0);
 #pragma unroll
       for (int k = 0; k < CG; ++k) {
         const int g = k * NS + n;
@@ -244,10 +254,14 @@ __global__ __launch_bounds__(64 * kQ4Waves, span_q4_waves(T::EPC == 8, 16 / CG))
     float base = low[n];
     base += __shfl_xor(base, 16);
     base += __shfl_xor(base, 32);
+    float y[2][4];
+#pragma unroll
+    for (int c = 0; c < 2; ++c)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) y[c][i] = fmaf(16.f, o[n][c][i] - ones[n][i], base);
 #pragma unroll
     for (int i = 0; i < 4; i += 2)
-      *reinterpret_cast<float4*>(&sm.o[wave][r][32 * (g0 + n) + 8 * kgrp + 2 * i]) =
-          make_float4(fmaf(16.f, o[n][0][i], base), fmaf(16.f, o[n][1][i], base), fmaf(16.f, o[n][0][i + 1], base), fmaf(16.f, o[n][1][i + 1], base));
+      *reinterpret_cast<float4*>(&sm.o[wave][r][32 * (g0 + n) + 8 * kgrp + 2 * i]) = make_float4(y[0][i], y[1][i], y[0][i + 1], y[1][i + 1]);
   }
   span_store<T>(a, sm, tile, r0, live);
 }
