@@ -121,6 +121,31 @@ __global__ __launch_bounds__(kApThreads) void append_kernel(AppendArgs args) {
   const int t = tok0 + min(mine, ntok - 1), b = t / a.n, j = t - b * a.n;
   const RowTarget to = row_target(args.cache, b, Hkv, a.rows[t]);
 
+  // the two chunks of this lane: a pair of rotated ones, or two of the columns behind R; and their angles
+  int c0 = p, c1 = p + kLanes;
+  if (STYLE == 0) {
+    const int np = pairs / EPC;
+    c0 = p < np ? p : p + np;
+    c1 = p < np ? p + np : p + kLanes;
+  }
+  uint4 raw[U][2];
+  const ST* src[U];  // (STYLE 2)
+  auto fetch = [&](int i0) __attribute__((always_inline)) {
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      int h = min(i0 + u * step, h1 - 1);
+      const bool is_q = h < a.q.heads;
+      if (!is_q) h -= a.q.heads;
+      const bool is_v = !is_q && h >= Hkv;
+      if (is_v) h -= Hkv;
+      const RotaryTensor& x = is_q ? a.q : is_v ? a.v : a.k;
+      src[u] = static_cast<const ST*>(x.in) + (b * x.in_batch + j * x.in_token + h * x.in_head);
+      raw[u][0] = load16_hint<STREAM>(src[u] + c0 * EPC);
+      raw[u][1] = load16_hint<STREAM>(src[u] + c1 * EPC);
+    }
+  };
+  fetch(h0 + first);  // (before the angles, which they need not wait for; lane groups without a token take another's)
+
   for (int i = tid; i < ntok * pairs; i += kApThreads) {
     const int u = i / pairs, f = i - u * pairs;
     float2 cs = cos_sin_rounded((double)a.positions[tok0 + u] * a.freqs[f]);
@@ -131,13 +156,6 @@ __global__ __launch_bounds__(kApThreads) void append_kernel(AppendArgs args) {
   __syncthreads();
   if (mine >= ntok) return;
 
-  // the two chunks of this lane: a pair of rotated ones, or two of the columns behind R; and their angles
-  int c0 = p, c1 = p + kLanes;
-  if (STYLE == 0) {
-    const int np = pairs / EPC;
-    c0 = p < np ? p : p + np;
-    c1 = p < np ? p + np : p + kLanes;
-  }
   float2 cs[kAngles];
 #pragma unroll
   for (int e = 0; e < kAngles; ++e) {
@@ -147,10 +165,8 @@ __global__ __launch_bounds__(kApThreads) void append_kernel(AppendArgs args) {
   const bool in_r = a.R > 0 && (STYLE != 0 || c1 * EPC < a.R);  // (STYLE 0: both chunks or none)
 
   for (int i0 = h0 + first; i0 < h1; i0 += step * U) {
-    uint4 raw[U][2];
-    ST* dst[U];           // null: not there; in 4 bits of the queries only
-    long long at[U];      // in 4 bits, of keys and values: their row, negative: not there
-    const ST* src[U];     // (STYLE 2)
+    ST* dst[U];         // null: not there; in 4 bits of the queries only
+    long long at[U];    // in 4 bits, of keys and values: their row, negative: not there
     bool turn[U], is_v[U];
 #pragma unroll
     for (int u = 0; u < U; ++u) {
@@ -160,10 +176,6 @@ __global__ __launch_bounds__(kApThreads) void append_kernel(AppendArgs args) {
       if (!is_q) h -= a.q.heads;
       is_v[u] = !is_q && h >= Hkv;
       if (is_v[u]) h -= Hkv;
-      const RotaryTensor& x = is_q ? a.q : is_v[u] ? a.v : a.k;
-      src[u] = static_cast<const ST*>(x.in) + (b * x.in_batch + j * x.in_token + h * x.in_head);
-      raw[u][0] = load16_hint<STREAM>(src[u] + c0 * EPC);
-      raw[u][1] = load16_hint<STREAM>(src[u] + c1 * EPC);
       turn[u] = in_r && !is_v[u];
       const bool there = i < h1 && (is_q || to.first >= 0);  // (else padded)
       const long long row = to.first + h * to.between;
@@ -230,6 +242,7 @@ __global__ __launch_bounds__(kApThreads) void append_kernel(AppendArgs args) {
         }
       }
     }
+    if (i0 + step * U < h1) fetch(i0 + step * U);
   }
 }
 
