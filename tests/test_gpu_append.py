@@ -147,6 +147,39 @@ def test_codes_and_scales_are_those_of_the_definition(dtype):
             float((back[i].double() - values64(got, cache.tensors[2 + i])).abs().max()) <= 2.0 ** -8 * float(back[i].abs().max())
 
 
+@pytest.mark.parametrize("bits", [0, 4])
+@pytest.mark.parametrize("dtype,B,n,Hq,Hkv,R,interleaved", [("bf16", 6, 1300, 32, 8, 128, False), ("f32", 3, 1100, 32, 8, 64, True), ("bf16", 7, 1030, 32, 8, 20, False)])
+def test_large_appends(dtype, B, n, Hq, Hkv, R, interleaved, bits):
+    """Enough for rows past the caches."""
+    x = Tokens(B, n, Hq, Hkv, dtype, R, 100000)
+    S = n + 30
+    gen = torch.Generator(device="cuda").manual_seed(8)
+    lay = api.make_layout(B, Hq, Hkv, 128, 128, S, DT[dtype])
+    table, n_pages = make_table(B, S, 64, gen)
+    cache = api.alloc_whole_cache(lay, bits == 4, table, 64, n_pages)
+    rows = (17 + torch.arange(n, device="cuda", dtype=torch.int32))[None].repeat(B, 1)
+    rows[1, n // 2:] = -1
+    q_out = torch.empty_like(x.q)
+    api.loki_append(lay, cache, rows, x.k, x.v, q=x.q, q_out=q_out, interleaved=interleaved, **x.rot)
+    k, e = turned(x.k, x.positions, x.f, R, interleaved, False, 1.0)
+    assert within(q_out, *turned(x.q, x.positions, x.f, R, interleaved, False, 1.0), dtype)
+    held = [None if t is None else unpaged(t, table, S) for t in cache.tensors[:4]]
+    for b in range(B):
+        m = n // 2 if b == 1 else n
+        at = slice(17, 17 + m)
+        if not bits:
+            assert within(held[0][b, :, at], k[b, :m].transpose(0, 1), e[b, :m].transpose(0, 1), dtype)
+            assert torch.equal(held[1][b, :, at], x.v[b, :m].transpose(0, 1))
+        else:
+            for t, y, off in ((0, k, e), (1, x.v.double(), torch.zeros_like(e))):
+                y, off = y[b, :m].transpose(0, 1), off[b, :m].transpose(0, 1)
+                got = values64(unpack(held[t][b, :, at]), held[2 + t][b, :, at])
+                lo, hi = y.unflatten(-1, (4, 32)).amin(-1, True), y.unflatten(-1, (4, 32)).amax(-1, True)
+                near = (hi - lo) / 15 * (0.5 + 15 * 2.0 ** -11 + 2.0 ** -10) + lo.abs() * 2.0 ** -10 + 2.0 ** -24  # (as above)
+                assert bool(((got - y).abs() <= near.expand(*near.shape[:-1], 32).flatten(-2) + 2 * off).all())
+    assert bool((held[0][1, :, 17 + n // 2:] == 0).all()) and bool((held[1][:, :, :17] == 0).all())
+
+
 def test_reads_of_one_tensor_and_of_rows_that_are_not_there():
     c = Case(2, 4, 2, 50, "bf16", 16)
     rows = torch.tensor([[49, 0, 0, 50], [-1, 17, 2 ** 31 - 1, -2 ** 31]], dtype=torch.int32, device="cuda")

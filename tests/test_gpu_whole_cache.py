@@ -106,6 +106,19 @@ def test_lengths_are_clamped_and_default_to_the_longest(dtype, bits):
 
 
 @pytest.mark.parametrize("dtype,bits", KINDS)
+@pytest.mark.parametrize("m", [2, 30, 200])
+def test_tokens_that_do_not_lie_next_to_each_other(m, dtype, bits):
+    """Lengths in no order and far apart: slower, since rows between the shortest's window and the longest's end are read, but right."""
+    B, G, Hkv, S = 2, 4, 2, 1500
+    c = Case(B, G * Hkv, Hkv, S, dtype, 16, bits, seed=m)
+    gen = torch.Generator(device="cuda").manual_seed(m)
+    lens = torch.randint(0, S + 1, (B, m), generator=gen, device="cuda", dtype=torch.int32)
+    lens[0, 0], lens[0, 1], lens[1, m - 1] = 1, S, 0
+    for window, sinks in ((40, 3), (1, 0), (0, 0)):
+        check(c, c.queries(m), lens, S, window, sinks, dtype)
+
+
+@pytest.mark.parametrize("dtype,bits", KINDS)
 @pytest.mark.parametrize("m", [1, 4, 40])
 def test_weights_over_many_orders_of_magnitude(m, dtype, bits):
     """Logits that grow along the rows, so that the reference of the exponentials moves many times, and large ones throughout."""
@@ -163,6 +176,27 @@ def test_in_a_graph_with_other_lengths_and_tables(m, dtype, bits):
             torch.cuda.synchronize()
             assert torch.equal(outs[i], c.attend(q, lens, 1500, 200 * i, 4 * i)), (totals, i)
     check(c, q, lens, 1500, 200, 4, dtype, outs[1])
+
+
+@pytest.mark.parametrize("dtype,bits,B,m,Hq,Hkv,S,window,sinks,page_rows", [
+    ("bf16", 0, 12, 1, 32, 8, 2100, 0, 0, 0), ("bf16", 0, 9, 2, 16, 16, 4000, 1300, 5, 256), ("f32", 0, 6, 1, 16, 16, 1100, 0, 0, 64),
+    ("f32", 0, 3, 6, 16, 4, 9000, 0, 0, 0), ("bf16", 4, 10, 1, 32, 8, 7100, 0, 0, 256), ("bf16", 4, 5, 1, 64, 8, 15000, 0, 0, 0),
+    ("f32", 4, 10, 1, 16, 8, 7100, 0, 0, 16), ("f32", 4, 9, 1, 64, 8, 9000, 8000, 3, 0), ("bf16", 0, 2, 11, 32, 8, 4300, 0, 0, 64),
+    ("bf16", 0, 3, 8, 64, 8, 9000, 3000, 4, 0), ("bf16", 4, 2, 20, 32, 8, 1500, 700, 4, 64), ("bf16", 4, 2, 70, 32, 8, 900, 0, 0, 0)])
+def test_large_calls(dtype, bits, B, m, Hq, Hkv, S, window, sinks, page_rows):
+    """Calls large enough for rows past the caches and for tiles of 64, 128 and 256 query rows; some units of them."""
+    print("case", dtype, bits, B, m, Hq, Hkv, S, window, sinks, page_rows, flush=True)
+    c = Case(B, Hq, Hkv, S, dtype, page_rows, bits)
+    q, lens = c.queries(m), last_tokens([S, S // 2, S - 77, 300][:min(B, 4)] + [S] * (B - 4), m)
+    out = c.attend(q, lens, S, window, sinks)
+    units = {(0, 0), (1, Hkv - 1), (B - 1, Hkv // 2)}
+    ref, bound = reference(q, c.k, c.v, lens.cpu(), window, sinks, c.scales, units)
+    torch.cuda.synchronize()
+    G = Hq // Hkv
+    assert bool(torch.isfinite(out).all())
+    for b, h in units:
+        at = (b, slice(None), slice(h * G, h * G + G))
+        assert worst(out[at], ref[at], bound[at], dtype) <= 0, (b, h)
 
 
 @pytest.mark.parametrize("dtype,bits", [("bf16", 0), ("bf16", 4)])

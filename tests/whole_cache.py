@@ -68,8 +68,8 @@ def seen(L, window, sinks):
     return (s[(s < sinks) | (s >= L - window)] if window else s).cuda()
 
 
-def reference(q, k, v, lens, window, sinks, scales=None):
-    """(out, bound) [B, m, Hq, 128] in 64 bits; k, v [B, H, S, 128]; scales: (k's, v's) of caches in 4 bits."""
+def reference(q, k, v, lens, window, sinks, scales=None, units=None):
+    """(out, bound) [B, m, Hq, 128] in 64 bits; k, v [B, H, S, 128]; scales: (k's, v's) of caches in 4 bits; units: only those (b, KV head)."""
     B, m, Hq, _ = q.shape
     G = Hq // k.shape[1]
     out, bound = (torch.zeros(q.shape, dtype=torch.float64, device=q.device) for _ in range(2))
@@ -77,6 +77,8 @@ def reference(q, k, v, lens, window, sinks, scales=None):
         for j in range(m):
             rows = seen(int(lens[b, j]), window, sinks)
             for h in range(k.shape[1]):
+                if units is not None and (b, h) not in units:
+                    continue
                 at = (b, j, slice(h * G, (h + 1) * G))
                 if scales is None:
                     step = 2.0 ** -16 if q.dtype == torch.bfloat16 else 0.0
