@@ -433,7 +433,7 @@ int dense_decode_shared(const loki_layout* layout, const void* q, const void* k_
  *               group) and step = fp16((largest - smallest) / 15) the code of x is (x - lowest) / step rounded to nearest, ties to even,
  *               within 0 .. 15 (step 0: 0) and stands for lowest + code * step: within half a step of x, plus what fp16 leaves
  *               of lowest (2^-11 of it) and 15 of step (2^-11 of the range).  Word m holds columns 32 g + 2 m (bits 4 g ..) and 32 g + 2 m + 1
- *               (bits 16 + 4 g ..).  160 bytes a row of keys and values; bf16 has 512.  Values beyond 65504 are held as if they were that.
+ *               (bits 16 + 4 g ..).  160 bytes a row of keys and values; bf16 has 512.  Beyond fp16's range lowest and step are its largest number, 65504.
  *   page_table  NULL, or device int32 [B, pages_per_seq]: row s of sequence b lies in page page_table[b, s / page_rows] at row
  *               s % page_rows.  page_rows: a power of two >= 16 (256 where loki_decode_step or loki_evict take the pools too);
  *               pages_per_seq * page_rows >= S_cap; n_pages * Hkv * page_rows < 2^31
@@ -452,7 +452,8 @@ typedef struct {
 /*
  * Keys and values of new tokens into such a cache, in the storage type or in 4 bits, the keys turned by their positions on
  * the way, and the queries of the same tokens beside them, in one launch.  The members of args mean what they mean in loki_rotary, but
- *   k, v      both there; their `out` are NULL and its strides not used: token j's go to row args->rows[b, j] of sequence b
+ *   k, v      both there, outside the cache; their `out` are NULL and its strides not used: token j's go to row args->rows[b, j] of
+ *             sequence b
  *   q         may be missing
  *   rows      device int32 [B, n_new]; a row outside [0, S_cap) or whose page entry is outside [0, n_pages) is not written (padded
  *             tokens, pages not there yet).  Two tokens must not share a row (nor two sequences a page that both write)

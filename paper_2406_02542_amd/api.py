@@ -763,7 +763,8 @@ class Profile:
 
 
 class Cache:
-    """A cache held whole (``loki_cache``), checked once and kept with its tensors: ``k``, ``v`` [B, Hkv, S_cap, 128] of the
+    """A cache held whole (``loki_cache``), checked once and kept with its tensors (another page table is another ``Cache``; its
+    entries may change): ``k``, ``v`` [B, Hkv, S_cap, 128] of the
     layout's type or, with ``page_table`` [B, pages_per_seq] (int32), pools [n_pages, Hkv, page_rows, 128]; in 4 bits int32
     [.., 16] with ``k_scales``, ``v_scales`` fp16 [.., 4, 2].  See ``alloc_whole_cache``."""
 
@@ -787,15 +788,15 @@ class Cache:
         for name, t, want, size in parts:
             if t.shape != size:
                 raise ValueError(f"{name} must be {list(size)}, got {tuple(t.shape)}")
+        if page_table is not None:
+            parts.append(("page_table", page_table, torch.int32, page_table.shape))
         for name, t, want, _ in parts:
             _ptr(t, name, want)
             if t.get_device() != k.get_device():
                 raise ValueError(f"{name} and k must live on the same device")
         self.tensors = (k, v, k_scales, v_scales, page_table)
         self.k = k
-        self.args = CacheArgs(k.data_ptr(), v.data_ptr(), None if k_scales is None else k_scales.data_ptr(),
-                              None if v_scales is None else v_scales.data_ptr(), _ptr(page_table, "page_table", torch.int32),
-                              rows, per_seq, pages)
+        self.args = CacheArgs(*(None if t is None else t.data_ptr() for t in self.tensors), rows, per_seq, pages)
         self.shape = (B, H, layout.S_cap, layout.dtype)
 
     def _of(self, layout: Layout):

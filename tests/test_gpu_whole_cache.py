@@ -199,6 +199,19 @@ def test_large_calls(dtype, bits, B, m, Hq, Hkv, S, window, sinks, page_rows):
         assert worst(out[at], ref[at], bound[at], dtype) <= 0, (b, h)
 
 
+@pytest.mark.parametrize("dtype,bits", KINDS)
+@pytest.mark.parametrize("m", [1, 90])
+def test_the_control_words_at_the_start_of_a_workspace_are_left_alone(m, dtype, bits):
+    ctl = (128 * 9 * 16 + 64) * 4  # as the calls that rely on them count them
+    c = Case(2, 8, 2, 900, dtype, 0, bits)
+    need = api.dense_cache_workspace_bytes(c.lay, c.cache, 900, m)
+    assert need >= ctl
+    ws = torch.zeros(need, dtype=torch.uint8, device="cuda")
+    q, lens = c.queries(m), last_tokens([900, 500], m)
+    check(c, q, lens, 900, 0, 0, dtype, c.attend(q, lens, 900, ws=ws))
+    assert not bool(ws[:ctl].any())
+
+
 @pytest.mark.parametrize("dtype,bits", [("bf16", 0), ("bf16", 4)])
 def test_rows_past_32_bits(dtype, bits):
     """A cache whose rows begin more than 2^32 bytes in."""
