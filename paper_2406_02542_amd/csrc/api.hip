@@ -1060,8 +1060,9 @@ static int check_span(const loki_layout* layout, const loki_cache* cache, int S_
 }
 // Behind the control words, which the call leaves alone (plan_workspace): the parts, where there are any.
 static size_t span_bytes(const Shape& s, const SpanArgs& a) {
-  const SpanPlan plan = span_plan(s, a.m, a.window, a.sinks, a.cache.k_scales != nullptr);
-  const size_t parts = plan.nsplit > 1 ? (size_t)a.B * a.m * a.Hq * plan.nsplit : 0;
+  const bool bits4 = a.cache.k_scales != nullptr;
+  const int x = span_plan(s, a.m, a.window, a.sinks, bits4).nsplit, y = span_plan(s, a.m, a.window, a.sinks, bits4, true).nsplit, n = x > y ? x : y;
+  const size_t parts = n > 1 ? (size_t)a.B * a.m * a.Hq * n : 0;
   return kClusterCtlBytes + align_up(parts * kPartStride * sizeof(float), 256);
 }
 

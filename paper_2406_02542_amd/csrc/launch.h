@@ -317,7 +317,8 @@ __host__ __device__ constexpr int span_q4_waves(bool bf16, int rows) { return ro
 struct SpanPlan {
   int rows, tiles, nsplit, run;
 };
-SpanPlan span_plan(const Shape& s, int m, int window, int sinks, bool bits4);
+// short_rows: as a call with fewer rows would be cut, where the kernel turns on them.
+SpanPlan span_plan(const Shape& s, int m, int window, int sinks, bool bits4, bool short_rows = false);
 hipError_t launch_span(const Shape& s, SpanArgs a, hipStream_t st);
 hipError_t launch_rotate(const Shape& s, const void* k_new, const float* P, void* klo, void* khi,
                          int pos, int n_new, hipStream_t st);

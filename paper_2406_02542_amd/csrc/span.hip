@@ -345,16 +345,35 @@ __global__ __launch_bounds__(256) void span_merge_kernel(const float* __restrict
 }
 
 // ---- the launch -----------------------------------------------------------------------------------------------------
+// Parts of a tile's rows, of at least 128: as many as make whole rounds of the blocks that are resident together, since one block more than a round
+// costs another (up to a few rounds; 3 % of a round for the parts that more of them write and the merge reads).  us with the fewest that fill a round / so:
+// 13 sequences of 32/8 bf16 heads with 4000 rows 49.2 / 42.3, 5 of 24 51.8 / 45.9, in 4 bits 24.3 / 21.4, 700 tokens of 32/8 behind 8192 rows 207 / 175; but
+// where lengths leave some of the blocks without rows, 5 of 24 fp32 heads up to 2311 in 4 bits 17.4 / 18.4.  Never fewer for more rows.
+static int span_splits(long long blocks, long long slots, long long most) {
+  const long long fill = (slots + blocks - 1) / blocks, top = 3 * fill < most ? 3 * fill : most;
+  if (blocks >= 2 * slots) return 1;
+  double best = 1e30;
+  int n = 1;
+  for (long long i = 1; i <= top; ++i) {
+    const double cost = (double)((blocks * i + slots - 1) / slots) / (double)i + 0.03 * (double)((i - 1) * blocks) / (double)slots;
+    if (cost < best) {
+      best = cost;
+      n = (int)i;
+    }
+  }
+  return n;
+}
+
 // Which kernel and how many blocks.  Tiles through LDS from 65 query rows of a KV head on, and from 33 on where more than 33 MB are read, us
 // 16 rows at a time / so: 1 x 64 tokens of 8/8 heads, window 512 9.1 / 14.9, 2 x 8 of 64/8, window 1000 13.7 / 17.5, 4000 (33 MB) 19.6 / 20.1, 8 x 16 of
 // 32/8 up to 8192 rows 92.5 / 54.1; with 32 query rows 8 x 4 of 64/8, window 1000 14.9 / 17.6, 2000 23.1 / 25.6, 8192 59.8 / 58.0; in 4 bits, 8192 rows, 8 x 8 tokens of
 // 64/8 (64 query rows) 79 / 91, 4 x 20 of 32/8 (80) 65.6 / 53.2, 4 x 64 of 32/8 (256) 143 / 92.
-SpanPlan span_plan(const Shape& s, int m, int window, int sinks, bool bits4) {
+SpanPlan span_plan(const Shape& s, int m, int window, int sinks, bool bits4, bool short_rows) {
   SpanPlan p{16, 0, 1, 0};
   const long long M = (long long)m * s.G;
   const long long tokens_read = window > 0 ? (long long)window + m - 1 + sinks : s.S, most_read = tokens_read < s.S ? tokens_read : s.S;
   const double bytes = (double)s.B * s.Hkv * most_read * (2 * kD * s.elem_bytes);
-  const bool lds = s.dtype == 1 && (M > 64 || (!bits4 && M > 32 && bytes > 33e6));
+  const bool lds = s.dtype == 1 && (M > 64 || (!bits4 && M > 32 && bytes > 33e6 && !short_rows));
   if (lds)
     p.rows = M <= 64 ? 64 : M <= 128 ? 128 : 256;
   else if (bits4)
@@ -367,11 +386,7 @@ SpanPlan span_plan(const Shape& s, int m, int window, int sinks, bool bits4) {
   const long long read = window > 0 && most < s.S ? most : s.S, blocks = (long long)s.B * p.tiles * s.Hkv;
   // as many parts as fill the blocks that are resident together, by the kernels' registers
   const long long slots = (lds ? 1LL : bits4 ? span_q4_waves(s.dtype == 1, p.rows) : s.dtype == 0 && p.rows == 16 ? 3LL : 2LL) * device_cus();
-  // (the more the longer S is, also over the change to tiles of 64 rows, one for every three or four of 16: a workspace for a length serves shorter ones)
-  const int least = 128;
-  long long n = (slots + blocks - 1) / blocks;
-  if (n > (read + least - 1) / least) n = (read + least - 1) / least;
-  p.nsplit = n < 1 ? 1 : (int)n;
+  p.nsplit = span_splits(blocks, slots, (read + 127) / 128);
   p.run = (int)((read + p.nsplit - 1) / p.nsplit);
   return p;
 }
