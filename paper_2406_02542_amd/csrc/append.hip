@@ -79,6 +79,12 @@ __device__ __forceinline__ void store_q4(const float* row, int p, uint32_t* code
   for (int w = 0; w < W; ++w)
 #pragma unroll
     for (int g = 0; g < kQ4Groups; ++g) x[w][g] = *reinterpret_cast<const float2*>(row + 32 * g + 2 * (W * p + w));
+  bool odd = false;  // minima and maxima pass over what is no number
+#pragma unroll
+  for (int w = 0; w < W; ++w)
+#pragma unroll
+    for (int g = 0; g < kQ4Groups; ++g) odd |= __builtin_isunordered(x[w][g].x, x[w][g].y);
+  const bool any = __ballot(odd) != 0ull;
 #pragma unroll
   for (int g = 0; g < kQ4Groups; ++g) {
     float lo = x[0][g].x, hi = lo;
@@ -90,7 +96,14 @@ __device__ __forceinline__ void store_q4(const float* row, int p, uint32_t* code
     lo = -group_allreduce_max<LANES>(-lo);
     hi = group_allreduce_max<LANES>(hi);
     // (a range past fp16's is clamped to its largest)
-    const cache_half2_t sc = {(_Float16)fminf((hi - lo) / 15.f, 65504.f), (_Float16)fminf(fmaxf(lo, -65504.f), 65504.f)};
+    cache_half2_t sc = {(_Float16)fminf((hi - lo) / 15.f, 65504.f), (_Float16)fminf(fmaxf(lo, -65504.f), 65504.f)};
+    if (any) {  // (uniform) a group with such a value stands for no numbers
+      bool own = false;
+#pragma unroll
+      for (int w = 0; w < W; ++w) own |= __builtin_isunordered(x[w][g].x, x[w][g].y);
+      const int lane = threadIdx.x & 63;
+      if ((__ballot(own) >> (lane & ~(LANES - 1)) & ((1ull << LANES) - 1)) != 0ull) sc = cache_half2_t{(_Float16)__builtin_nanf(""), (_Float16)__builtin_nanf("")};
+    }
     const float step = (float)sc.x, low = (float)sc.y, inv = 1.0f / step;
 #pragma unroll
     for (int w = 0; w < W; ++w) word[w] |= q4_code(x[w][g].x, low, step, inv) << (4 * g) | q4_code(x[w][g].y, low, step, inv) << (16 + 4 * g);

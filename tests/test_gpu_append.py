@@ -260,3 +260,47 @@ def test_a_prompt_and_then_token_by_token(dtype, bits):
         ref, bound = reference(q_out, k, v, sees.cpu(), window, sinks, scales)
         assert worst(out, ref, bound, dtype) <= 0, turn
         start += real
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_groups_with_a_value_that_is_no_number(dtype):
+    """In 4 bits their step and lowest are NaN; the other groups, rows and heads are as without."""
+    B, H, n = 2, 3, 37
+    dt = DT[dtype]
+    gen = torch.Generator(device="cuda").manual_seed(5)
+    k, v = (torch.randn((B, n, H, 128), generator=gen, device="cuda").to(dt) for _ in "kv")
+    spoilt = torch.zeros((B, H, n, 4), dtype=torch.bool, device="cuda")
+    for b, j, h, col in ((0, 0, 0, 0), (0, 5, 2, 31), (1, 36, 1, 32), (1, 20, 0, 127), (1, 20, 0, 70)):
+        spoilt[b, h, j, col // 32] = True
+        v[b, j, h, col] = float("nan")
+    lay = api.make_layout(B, H, H, 128, 128, n, dt)
+    rows = torch.arange(n, dtype=torch.int32, device="cuda").repeat(B, 1)
+    held = []
+    for x in (v, torch.nan_to_num(v, nan=0.0)):
+        cache = api.alloc_whole_cache(lay, four_bits=True)
+        api.loki_append(lay, cache, rows, k, x)
+        held.append(cache.tensors)
+    torch.cuda.synchronize()
+    assert torch.equal(held[0][0], held[1][0]) and torch.equal(held[0][2], held[1][2])
+    assert bool(torch.isnan(held[0][3][spoilt]).all())
+    assert torch.equal(held[0][3][~spoilt], held[1][3][~spoilt])
+    clean = (~spoilt).repeat_interleave(32, -1)
+    assert torch.equal(unpack(held[0][1])[clean], unpack(held[1][1])[clean])
+
+
+@pytest.mark.parametrize("bits", [0, 4])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("interleaved,R", [(False, 128), (True, 96), (False, 20)])
+def test_queries_turned_in_place(interleaved, R, dtype, bits):
+    B, n, Hq, H = 2, 300, 8, 2
+    t = Tokens(B, n, Hq, H, dtype, R, 5000)
+    lay = api.make_layout(B, Hq, H, 128, 128, n, DT[dtype])
+    rows = torch.arange(n, dtype=torch.int32, device="cuda").repeat(B, 1)
+    q_out, q = torch.empty_like(t.q), t.q.clone()
+    caches = [api.alloc_whole_cache(lay, four_bits=bits == 4) for _ in range(2)]
+    api.loki_append(lay, caches[0], rows, t.k, t.v, q=t.q, q_out=q_out, interleaved=interleaved, **t.rot)
+    api.loki_append(lay, caches[1], rows, t.k, t.v, q=q, q_out=q, interleaved=interleaved, **t.rot)
+    torch.cuda.synchronize()
+    assert torch.equal(q, q_out)
+    for x, y in zip(caches[0].tensors[:4], caches[1].tensors[:4]):
+        assert x is None or torch.equal(x, y)
