@@ -81,6 +81,30 @@ __global__ __launch_bounds__(64 * kSpWaves) void span_rows_kernel(SpanArgs a) {
       seen = 0;
 #pragma unroll
       for (int e = 0; e < 8; ++e) seen |= (span_sees(a, st, len, st.at + 16 * (e / 4) + 4 * kgrp + e % 4) ? 1u : 0u) << e;
+      uint32_t odd = 0;
+#pragma unroll
+      for (int e = 0; e < 8; ++e)
+#pragma unroll
+        for (int w = 0; w < 4; ++w) odd |= bf16_not_finite(am_word(vraw[e], w));
+      if (__ballot(odd != 0) != 0ull) {  // (span_mark)
+        uint32_t ones[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) ones[i] = (seen >> (2 * i) & 1u ? 0x3f80u : 0u) | (seen >> (2 * i + 1) & 1u ? 0x3f800000u : 0u);
+#pragma unroll
+        for (int c = 0; c < 8; ++c) {
+          uint32_t x[4];
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+            x[i] = bf16_marks(__builtin_amdgcn_perm(am_word(vraw[2 * i + 1], c / 2), am_word(vraw[2 * i], c / 2), c % 2 ? 0x07060302u : 0x05040100u));
+          const am_f32x4_t count = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(am_bf16x8_t, make_uint4(x[0], x[1], x[2], x[3])),
+                                                                           __builtin_bit_cast(am_bf16x8_t, make_uint4(ones[0], ones[1], ones[2], ones[3])), am_f32x4_t{}, 0, 0, 0);
+#pragma unroll
+          for (int i = 0; i < 4; ++i) o[c][i] = span_mark(o[c][i], count[i]);
+          __builtin_amdgcn_sched_barrier(0);
+        }
+#pragma unroll
+        for (int e = 0; e < 8; ++e) vraw[e] = make_uint4(bf16_finite(vraw[e].x), bf16_finite(vraw[e].y), bf16_finite(vraw[e].z), bf16_finite(vraw[e].w));
+      }
     }
     float p[8], sum;
     auto weights = [&]() __attribute__((always_inline)) {
@@ -128,7 +152,11 @@ __global__ __launch_bounds__(64 * kSpWaves) void span_rows_kernel(SpanArgs a) {
   }
   l += __shfl_xor(l, 16);
   l += __shfl_xor(l, 32);
-  if (len == 0) l = 0.f;  // (a padded token's lanes took whatever full steps gave)
+  if (len == 0) {  // (a padded token's lanes took whatever full steps gave)
+    l = 0.f;
+#pragma unroll
+    for (int c = 0; c < 8; ++c) o[c] = am_f32x4_t{};
+  }
   if (kgrp == 0) sm.ml[wave][r16] = make_float2(m, l);
   // o[c][i] is column 8 (4 kgrp + i) + c
 #pragma unroll
@@ -247,6 +275,48 @@ __global__ __launch_bounds__(64 * kSpWaves, 2) void span_f32_kernel(SpanArgs a) 
       }
       l[g] += sum;
     }
+    if (!full) {  // (uniform)
+      uint32_t odd = 0;
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int c = 0; c < 2; ++c) odd |= f32_not_finite(vr[i][c].x) | f32_not_finite(vr[i][c].y) | f32_not_finite(vr[i][c].z) | f32_not_finite(vr[i][c].w);
+      if (__ballot(odd != 0) != 0ull) {  // (span_mark)
+        uint32_t mine[QG];  // bit i: whether the lane's token sees the row
+#pragma unroll
+        for (int g = 0; g < QG; ++g) {
+          mine[g] = 0;
+#pragma unroll
+          for (int i = 0; i < 4; ++i) mine[g] |= span_sees(a, st, len[g], st.at + 4 * c4 + i) ? 1u << i : 0u;
+          asm volatile("" : "+v"(mine[g]));  // (else their masks stay in scalar registers, which there are too few of)
+        }
+#pragma unroll
+        for (int c = 0; c < 2; ++c) {
+#pragma unroll
+          for (int t = 0; t < 4; ++t) {
+            float ones[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              float& x = t == 0 ? vr[i][c].x : t == 1 ? vr[i][c].y : t == 2 ? vr[i][c].z : vr[i][c].w;
+              asm volatile("" : "+v"(x));  // (else what was found above is kept, in as many registers)
+              const uint32_t bad = f32_not_finite(x);
+              ones[i] = (float)bad;
+              x = __uint_as_float(__float_as_uint(x) & (bad - 1u));
+            }
+#pragma unroll
+            for (int g = 0; g < QG; ++g) {
+              pf_f32x4_t count = pf_f32x4_t{};
+#pragma unroll
+              for (int i = 0; i < 4; ++i)
+                count = __builtin_amdgcn_mfma_f32_16x16x4f32(ones[i], (float)(mine[g] >> i & 1u), count, 0, 0, 0);
+#pragma unroll
+              for (int i = 0; i < 4; ++i) o[g][4 * c + t][i] = span_mark(o[g][4 * c + t][i], count[i]);
+            }
+            __builtin_amdgcn_sched_barrier(0);
+          }
+        }
+      }
+    }
 #pragma unroll
     for (int i = 0; i < 4; ++i)
 #pragma unroll
@@ -265,7 +335,11 @@ __global__ __launch_bounds__(64 * kSpWaves, 2) void span_f32_kernel(SpanArgs a) 
   for (int g = 0; g < QG; ++g) {
     l[g] += __shfl_xor(l[g], 16);
     l[g] += __shfl_xor(l[g], 32);
-    if (len[g] == 0) l[g] = 0.f;
+    if (len[g] == 0) {
+      l[g] = 0.f;
+#pragma unroll
+      for (int c = 0; c < 8; ++c) o[g][c] = pf_f32x4_t{};
+    }
     const int r = 16 * g + l16;
     if (c4 == 0) sm.ml[wave][r] = make_float2(m[g], l[g]);
     // o[4 c + t][i] is column 64 c + 4 (4 c4 + i) + t
@@ -313,7 +387,7 @@ __global__ __launch_bounds__(256) void span_merge_kernel(const float* __restrict
 #pragma unroll
     for (int u = 0; u < U; ++u) {
       const float f = fast_exp2(ml[u].x - mn);
-      if (ml[u].y > 0.f) {  // (a part without rows has no outputs)
+      if (ml[u].y != 0.f) {  // (a part without rows has no outputs)
         l = fmaf(ml[u].y, f, l);
         o = make_float4(fmaf(x[u].x, f, o.x), fmaf(x[u].y, f, o.y), fmaf(x[u].z, f, o.z), fmaf(x[u].w, f, o.w));
       }
@@ -337,7 +411,7 @@ __global__ __launch_bounds__(256) void span_merge_kernel(const float* __restrict
       o = make_float4(fmaf(x.x, f, o.x), fmaf(x.y, f, o.y), fmaf(x.z, f, o.z), fmaf(x.w, f, o.w));
     }
   }
-  const float inv = l > 0.f ? 1.0f / l : 0.f;  // (a token without rows: zeros)
+  const float inv = l == 0.f ? 0.f : 1.0f / l;  // (a token without rows: zeros)
   if constexpr (T::EPC == 8)
     *reinterpret_cast<uint2*>(out + r * kD + 4 * lane) = make_uint2(BF16::round2(o.x * inv, o.y * inv), BF16::round2(o.z * inv, o.w * inv));
   else

@@ -103,6 +103,17 @@ __device__ __forceinline__ bool span_full(const SpanArgs& a, const SpanRows& r, 
   return st.at >= st.lo && st.at + keys <= min(st.hi, r.len_min) && (st.at >= r.hi - a.window || st.at + keys <= a.sinks);
 }
 
+// A row that a token does not see may hold anything, and a product with a weight of zero is no zero where it holds no finite number.  So in
+// steps that are masked such values are cleared, and which of them a token sees is a product of its own, of ones: a column's count, and where
+// it is not zero the output is no number.
+__device__ __forceinline__ float span_mark(float o, float count) { return count > 0.f ? __builtin_nanf("") : o; }
+// The halves of x that are no finite bf16 number (all ones as exponents, which one more carries into the sign's place): in bits 0 and 16;
+// as ones; and x with zeros for them.
+__device__ __forceinline__ uint32_t bf16_not_finite(uint32_t x) { return ((x & 0x7f807f80u) + 0x00800080u) >> 15 & 0x00010001u; }
+__device__ __forceinline__ uint32_t bf16_marks(uint32_t x) { return bf16_not_finite(x) * 0x3f80u; }
+__device__ __forceinline__ uint32_t bf16_finite(uint32_t x) { return x & ~(bf16_not_finite(x) * 0xffffu); }
+__device__ __forceinline__ uint32_t f32_not_finite(float x) { return ((__float_as_uint(x) & 0x7f800000u) + 0x00800000u) >> 31; }
+
 // What a block does: steps [s0, s1) of a tile, part `part` of its nsplit.
 struct SpanTile {
   int b, h, tile, part, s0, s1;
@@ -178,7 +189,7 @@ __device__ __forceinline__ void span_store(const SpanArgs& a, const SpanMerge<RO
       if (c == 0) *reinterpret_cast<float2*>(p + kD) = make_float2(mn, ls);
     } else {
       const long long place = span_place(a, tile.b, tile.h, r0 + r);
-      const float inv = ls > 0.f ? 1.0f / ls : 0.f;  // (a token without rows: zeros)
+      const float inv = ls == 0.f ? 0.f : 1.0f / ls;  // (a token without rows: zeros)
       if constexpr (T::EPC == 8)
         *reinterpret_cast<uint2*>(static_cast<uint16_t*>(a.out) + place * kD + c) =
             make_uint2(BF16::round2(os.x * inv, os.y * inv), BF16::round2(os.z * inv, os.w * inv));

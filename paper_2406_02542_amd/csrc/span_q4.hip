@@ -171,7 +171,8 @@ __global__ __launch_bounds__(64 * kQ4Waves, span_q4_waves(T::EPC == 8, 16 / CG))
     }
     place.settle(places, next);
     load_k(next);
-    if (!span_full(a, rows, st, KEYS)) {  // (uniform)
+    const bool full = span_full(a, rows, st, KEYS);
+    if (!full) {  // (uniform)
 #pragma unroll
       for (int e = 0; e < 8; ++e)
         if (!span_sees(a, st, len, st.at + 16 * (e / 4) + 4 * (e % 4) + kgrp)) x[e] = kUnseen;
@@ -213,6 +214,11 @@ __global__ __launch_bounds__(64 * kQ4Waves, span_q4_waves(T::EPC == 8, 16 / CG))
     Q4Scales<NS> sc[8];
 #pragma unroll
     for (int e = 0; e < 8; ++e) sc[e] = scales(1, e);
+    if (!full) {  // (a row that the token does not see may hold no numbers)
+#pragma unroll
+      for (int e = 0; e < 8; ++e)
+        if (!span_sees(a, st, len, st.at + 16 * (e / 4) + 4 * (e % 4) + kgrp)) sc[e] = Q4Scales<NS>{};
+    }
     __builtin_amdgcn_wave_barrier();
 #pragma unroll
     for (int n = 0; n < NS; ++n) {
@@ -246,7 +252,14 @@ __global__ __launch_bounds__(64 * kQ4Waves, span_q4_waves(T::EPC == 8, 16 / CG))
   }
   l += __shfl_xor(l, 16);
   l += __shfl_xor(l, 32);
-  if (len == 0) l = 0.f;  // (a padded token's lanes took whatever full steps gave)
+  if (len == 0) {  // (a padded token's lanes took whatever full steps gave)
+    l = 0.f;
+#pragma unroll
+    for (int n = 0; n < NS; ++n) {
+      o[n][0] = o[n][1] = ones[n] = am_f32x4_t{};
+      low[n] = 0.f;
+    }
+  }
   if (kgrp == 0 && gl == 0) sm.ml[wave][r] = make_float2(m, l);
   // o[n][c][i] is column 32 (g0 + n) + 2 (4 kgrp + i) + c
 #pragma unroll

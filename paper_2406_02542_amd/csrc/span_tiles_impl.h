@@ -179,10 +179,48 @@ __global__ __launch_bounds__(64 * WAVES, WAVES == 4 ? 1 : 2) void span_tiles_ker
 #pragma unroll
     for (int ks = 0; ks < 8; ++ks) s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(ka[ks], q[ks], s, 0, 0, 0);
     __builtin_amdgcn_sched_barrier(0);
+    // whether any of the values in registers is no finite number (span_mark)
+    auto odd = [&]() __attribute__((always_inline)) {
+      uint32_t x = 0;
+#pragma unroll
+      for (int ks = 0; ks < 2; ++ks)
+#pragma unroll
+        for (int c = 0; c < 4; ++c)
+#pragma unroll
+          for (int w = 0; w < 4; ++w) x |= bf16_not_finite(am_word(__builtin_bit_cast(uint4, va[ks][c]), w));
+      return __ballot(x != 0) != 0ull;
+    };
     if (!full) {  // (uniform)
 #pragma unroll
       for (int i = 0; i < 16; ++i)
         if (!span_sees(a, st, len, st.at + 8 * (i >> 2) + 4 * half + (i & 3))) s[i] = kUnseen;
+      if (odd()) {
+        uint32_t ones[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          float x = s[2 * i], y = s[2 * i + 1];
+          asm volatile("" : "+v"(x), "+v"(y));  // (else the masks of all of them stay in scalar registers, which there are too few of)
+          ones[i] = (x != kUnseen ? 0x3f80u : 0u) | (y != kUnseen ? 0x3f800000u : 0u);
+        }
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {
+          sp_f32x16_t count = sp_f32x16_t{};
+#pragma unroll
+          for (int ks = 0; ks < 2; ++ks) {
+            uint4 x = __builtin_bit_cast(uint4, va[ks][c]);
+            asm volatile("" : "+v"(x.x), "+v"(x.y), "+v"(x.z), "+v"(x.w));  // (else what was found above is kept, in as many registers)
+            const uint4 bad = make_uint4(bf16_marks(x.x), bf16_marks(x.y), bf16_marks(x.z), bf16_marks(x.w));
+            count = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
+                __builtin_bit_cast(am_bf16x8_t, bad),
+                __builtin_bit_cast(am_bf16x8_t, make_uint4(ones[4 * ks], ones[4 * ks + 1], ones[4 * ks + 2], ones[4 * ks + 3])), count, 0, 0, 0);
+            va[ks][c] = __builtin_bit_cast(am_bf16x8_t, make_uint4(bf16_finite(x.x), bf16_finite(x.y), bf16_finite(x.z), bf16_finite(x.w)));
+            __builtin_amdgcn_sched_barrier(0);
+          }
+#pragma unroll
+          for (int i = 0; i < 16; ++i) o[c][i] = span_mark(o[c][i], count[i]);
+          __builtin_amdgcn_sched_barrier(0);
+        }
+      }
     }
     float p[16], sum;
     auto weights = [&]() __attribute__((always_inline)) {
@@ -229,6 +267,15 @@ __global__ __launch_bounds__(64 * WAVES, WAVES == 4 ? 1 : 2) void span_tiles_ker
               va[ks][c], __builtin_bit_cast(am_bf16x8_t, make_uint4(w[t][4 * ks], w[t][4 * ks + 1], w[t][4 * ks + 2], w[t][4 * ks + 3])), o[c], 0, 0, 0);
     if constexpr (BITS4) {  // (the two second terms' product is 2^-18 of the first two's)
       values(1);
+      if (!full && odd()) {
+#pragma unroll
+        for (int ks = 0; ks < 2; ++ks)
+#pragma unroll
+          for (int c = 0; c < 4; ++c) {
+            const uint4 x = __builtin_bit_cast(uint4, va[ks][c]);
+            va[ks][c] = __builtin_bit_cast(am_bf16x8_t, make_uint4(bf16_finite(x.x), bf16_finite(x.y), bf16_finite(x.z), bf16_finite(x.w)));
+          }
+      }
 #pragma unroll
       for (int ks = 0; ks < 2; ++ks)
 #pragma unroll
@@ -261,6 +308,11 @@ __global__ __launch_bounds__(64 * WAVES, WAVES == 4 ? 1 : 2) void span_tiles_ker
 
   // both halves of a query's keys; then the waves that had other keys of the same queries
   l += __shfl_xor(l, 32);
+  if (len == 0) {  // (a padded token's lanes took whatever full steps gave)
+    l = 0.f;
+#pragma unroll
+    for (int c = 0; c < 4; ++c) o[c] = sp_f32x16_t{};
+  }
   if constexpr (WK > 1) {
     float2* ml = reinterpret_cast<float2*>(smem);                   // [wave][32] (max, sum)
     float4* ob = reinterpret_cast<float4*>(smem + WAVES * 32 * 8);  // [wave of the upper half][4][4][lane]
@@ -309,8 +361,7 @@ __global__ __launch_bounds__(64 * WAVES, WAVES == 4 ? 1 : 2) void span_tiles_ker
     }
     if (wk != 0) return;
   }
-  if (len == 0) l = 0.f;  // (a padded token's lanes took whatever full steps gave)
-  const float inv = l > 0.f ? 1.0f / l : 0.f;  // (a token without rows: zeros)
+  const float inv = l == 0.f ? 0.f : 1.0f / l;  // (a token without rows: zeros)
   const bool parts = a.nsplit > 1;
   // a lane has four columns of one query at a time: through LDS, so that a store takes four half rows
   char* at = smem + wave * 8192;  // [32 queries][64 columns], 16-byte chunks exchanged as the keys'
