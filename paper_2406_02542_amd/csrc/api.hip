@@ -1058,12 +1058,13 @@ static int check_span(const loki_layout* layout, const loki_cache* cache, int S_
   a->sinks = args->sinks;
   return LOKI_OK;
 }
-// Behind the control words, which the call leaves alone (plan_workspace): the parts, where there are any.
+// Behind the control words, which the call leaves alone (plan_workspace): which runs the tiles have, and the parts.
+static size_t span_dealt_bytes(const SpanPlan& p) { return align_up(p.dealt * sizeof(int2), 256); }
+static size_t span_bytes(const SpanPlan& p) { return kClusterCtlBytes + span_dealt_bytes(p) + align_up(p.parts * kPartStride * sizeof(float), 256); }
 static size_t span_bytes(const Shape& s, const SpanArgs& a) {
   const bool bits4 = a.cache.k_scales != nullptr;
-  const int x = span_plan(s, a.m, a.window, a.sinks, bits4).nsplit, y = span_plan(s, a.m, a.window, a.sinks, bits4, true).nsplit, n = x > y ? x : y;
-  const size_t parts = n > 1 ? (size_t)a.B * a.m * a.Hq * n : 0;
-  return kClusterCtlBytes + align_up(parts * kPartStride * sizeof(float), 256);
+  const size_t x = span_bytes(span_plan(s, a.m, a.window, a.sinks, bits4)), y = span_bytes(span_plan(s, a.m, a.window, a.sinks, bits4, true));
+  return x > y ? x : y;
 }
 
 int dense_cache_workspace_bytes(const loki_layout* layout, const loki_cache* cache, int S_max, const loki_span_args* args, size_t* bytes) {
@@ -1087,11 +1088,13 @@ int dense_decode_cache(const loki_layout* layout, const void* q, const loki_cach
   if (span_bytes(s, a) > workspace_bytes) return LOKI_ERR_WORKSPACE;
   a.q = q;
   a.out = out;
-  a.partial = reinterpret_cast<float*>(static_cast<char*>(workspace) + kClusterCtlBytes);
+  const SpanPlan plan = span_plan(s, a.m, a.window, a.sinks, a.cache.k_scales != nullptr);
+  a.dealt = plan.cap > 0 && a.lens != nullptr ? reinterpret_cast<int2*>(static_cast<char*>(workspace) + kClusterCtlBytes) : nullptr;
+  a.partial = reinterpret_cast<float*>(static_cast<char*>(workspace) + kClusterCtlBytes + span_dealt_bytes(plan));
   hipStream_t st = static_cast<hipStream_t>(stream);
   StageTimer tm(st);
   tm.begin("cache_attend");
-  const hipError_t e = launch_span(s, a, st);
+  const hipError_t e = launch_span(s, a, plan, st);
   tm.end();
   return e == hipSuccess ? LOKI_OK : LOKI_ERR_HIP;
 }

@@ -304,10 +304,13 @@ struct SpanArgs {
   CacheView cache;
   const void* q;
   void* out;              // [B, m, Hq, 128] as q
-  float* partial;         // [B m Hq][nsplit] parts, with more than one
+  float* partial;         // [B m Hq][nsplit] parts; dealt: [run][Hkv][rows]
+  int2* dealt;            // [B tiles] (first run, runs): the blocks deal runs by the lengths, up to cap; null: each tile in nsplit runs
   const int32_t* lens;    // [B, m] or null: S_max less the tokens behind
   int B, m, G, Hq, Hkv, S_max, window, sinks;
-  int rows, tiles, nsplit, run;  // tiles of `rows` query rows of a sequence and KV head, each cut into up to nsplit parts of `run` rows
+  int rows, tiles;        // tiles of `rows` query rows of a sequence and KV head
+  int nsplit, run;        // runs of a tile, of `run` rows
+  int cap;                // runs of a KV head that are resident together
 };
 // Blocks of the 4-bit kernels that a CU holds, by the registers of tiles of `rows` query rows.  us with more or fewer: 16 sequences of 32/8 bf16 heads up
 // to 16384 rows (4 rows) four 57.7, three 60.7; 64 of 64/8 up to 4096 (8) two 68.1, three 75.6; fp32, 16 of 8/8 up to 8000 (4) three 39.6, two
@@ -315,11 +318,13 @@ struct SpanArgs {
 __host__ __device__ constexpr int span_q4_waves(bool bf16, int rows) { return rows == 4 ? (bf16 ? 4 : 3) : 2; }
 // How a call is cut: the workspace's size and the launch go by it.
 struct SpanPlan {
-  int rows, tiles, nsplit, run;
+  int rows, tiles, nsplit, run, cap;  // cap 0: not dealt
+  size_t parts, dealt;                // what the workspace holds of each
+  bool past;                          // values are loaded past the caches
 };
 // short_rows: as a call with fewer rows would be cut, where the kernel turns on them.
 SpanPlan span_plan(const Shape& s, int m, int window, int sinks, bool bits4, bool short_rows = false);
-hipError_t launch_span(const Shape& s, SpanArgs a, hipStream_t st);
+hipError_t launch_span(const Shape& s, SpanArgs a, const SpanPlan& plan, hipStream_t st);
 hipError_t launch_rotate(const Shape& s, const void* k_new, const float* P, void* klo, void* khi,
                          int pos, int n_new, hipStream_t st);
 

@@ -17,16 +17,17 @@ constexpr int kSpWaves = 4;
 //                                   rows up (v_perm_b32); the weights in two bf16 terms, 2^-16 of each (as the library's other attention)
 // so a query's maximum, sum and outputs are its own lanes'.  The reference of the exponentials follows the maximum only when a
 // lane's weights of a step sum up to more than 2^8.
-template <bool STREAM>
+template <bool STREAM, bool DEALT>
 __global__ __launch_bounds__(64 * kSpWaves) void span_rows_kernel(SpanArgs a) {
   constexpr int KEYS = 32;
   __shared__ __align__(16) SpanMerge<16, kSpWaves> sm;
-  const SpanTile tile = span_tile<KEYS>(a);
+  const SpanTile tile = span_tile<KEYS, DEALT>(a);
+  if (tile.h < 0) return;  // (uniform for the block)
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), r16 = lane & 15, kgrp = lane >> 4;
   const int M = a.m * a.G, r0 = tile.tile * 16, live = min(16, M - r0), lg = 31 - __builtin_clz(a.G);
   const SpanRows rows = tile.rows;
   const SpanSteps<KEYS> steps(rows);
-  if (tile.s0 >= tile.s1 && tile.part > 0) return span_none(a, tile, live);  // (uniform for the block)
+  if (tile.s0 >= tile.s1 && tile.part > 0) return span_none<DEALT>(a, tile, live);  // (uniform for the block)
   const int s1 = tile.s1;
   const RowPlaces places(a.cache, tile.b, tile.h, a.Hkv);
   const int len = r16 < live ? span_len(a, tile.b, (r0 + r16) >> lg) : 0;
@@ -165,7 +166,7 @@ __global__ __launch_bounds__(64 * kSpWaves) void span_rows_kernel(SpanArgs a) {
     dst[0] = make_float4(o[0][i], o[1][i], o[2][i], o[3][i]);
     dst[1] = make_float4(o[4][i], o[5][i], o[6][i], o[7][i]);
   }
-  span_store<BF16>(a, sm, tile, r0, live);
+  span_store<BF16, DEALT>(a, sm, tile, r0, live);
 }
 
 // ---- fp32 -----------------------------------------------------------------------------------------------------------
@@ -174,12 +175,12 @@ template <int QG, bool STREAM>
 __global__ __launch_bounds__(64 * kSpWaves, 2) void span_f32_kernel(SpanArgs a) {
   constexpr int KEYS = 16;
   __shared__ __align__(16) SpanMerge<16 * QG, kSpWaves> sm;
-  const SpanTile tile = span_tile<KEYS>(a);
+  const SpanTile tile = span_tile<KEYS, false>(a);
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), l16 = lane & 15, c4 = lane >> 4;
   const int M = a.m * a.G, r0 = tile.tile * (16 * QG), live = min(16 * QG, M - r0), lg = 31 - __builtin_clz(a.G);
   const SpanRows rows = tile.rows;
   const SpanSteps<KEYS> steps(rows);
-  if (tile.s0 >= tile.s1 && tile.part > 0) return span_none(a, tile, live);  // (uniform for the block)
+  if (tile.s0 >= tile.s1 && tile.part > 0) return span_none<false>(a, tile, live);  // (uniform for the block)
   const int s1 = tile.s1;
   const RowPlaces places(a.cache, tile.b, tile.h, a.Hkv);
 
@@ -349,21 +350,32 @@ __global__ __launch_bounds__(64 * kSpWaves, 2) void span_f32_kernel(SpanArgs a) 
       for (int i = 0; i < 4; ++i)
         *reinterpret_cast<float4*>(&sm.o[wave][r][64 * c + 16 * c4 + 4 * i]) = make_float4(o[g][4 * c][i], o[g][4 * c + 1][i], o[g][4 * c + 2][i], o[g][4 * c + 3][i]);
   }
-  span_store<F32>(a, sm, tile, r0, live);
+  span_store<F32, false>(a, sm, tile, r0, live);
 }
 
 // ---- parts joined ---------------------------------------------------------------------------------------------------
 // 32 lanes take a query row, 16 bytes of each of its parts; GROUPS of them share a row's parts, four each at a time.
-template <typename T, int GROUPS>
-__global__ __launch_bounds__(256) void span_merge_kernel(const float* __restrict__ partials, typename T::store_t* __restrict__ out,
-                                                         long long rows, int nsplit) {
+template <typename T, int GROUPS, bool DEALT>
+__global__ __launch_bounds__(256) void span_merge_kernel(SpanArgs a) {
   constexpr int U = 4;
   __shared__ __align__(16) float s_o[GROUPS > 1 ? GROUPS : 1][kD];
   __shared__ float2 s_ml[GROUPS];
   const int lane = threadIdx.x & 31, grp = threadIdx.x >> 5;
-  const long long r = GROUPS > 1 ? (long long)blockIdx.x : (long long)blockIdx.x * 8 + grp;
-  if (GROUPS == 1 && r >= rows) return;
-  const float* partial = partials + r * nsplit * kPartStride;
+  const int r = GROUPS > 1 ? (int)blockIdx.x : (int)blockIdx.x * 8 + grp;
+  if (GROUPS == 1 && r >= a.B * a.m * a.Hq) return;
+  int nsplit = a.nsplit;
+  long long between = kPartStride;
+  const float* partial = a.partial + (long long)r * nsplit * kPartStride;
+  if constexpr (DEALT) {
+    const int per = a.m * a.Hq, b = r / per, j = (r - b * per) / a.Hq, head = r - b * per - j * a.Hq, h = head >> (31 - __builtin_clz(a.G));
+    const int row = j * a.G + (head & (a.G - 1)), tile = row >> (31 - __builtin_clz(a.rows));
+    const int2 dealt = a.dealt[b * a.tiles + a.tiles - 1 - tile];
+    nsplit = dealt.y;
+    if (nsplit == 1) return;  // (written already)
+    between = (long long)a.Hkv * a.rows * kPartStride;
+    partial = a.partial + dealt.x * between + ((long long)h * a.rows + (row & (a.rows - 1))) * kPartStride;
+  }
+  typename T::store_t* out = static_cast<typename T::store_t*>(a.out) + (long long)r * kD;
   float m = kNegBig, l = 0.f;
   float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
   for (int i0 = GROUPS > 1 ? grp : 0; i0 < nsplit; i0 += GROUPS * U) {
@@ -372,7 +384,7 @@ __global__ __launch_bounds__(256) void span_merge_kernel(const float* __restrict
 #pragma unroll
     for (int u = 0; u < U; ++u) {
       const int i = i0 + u * GROUPS;
-      const float* p = partial + (long long)(i < nsplit ? i : i0) * kPartStride;
+      const float* p = partial + (i < nsplit ? i : i0) * between;
       ml[u] = *reinterpret_cast<const float2*>(p + kD);
       x[u] = *reinterpret_cast<const float4*>(p + 4 * lane);
       if (i >= nsplit) ml[u] = make_float2(kNegBig, 0.f);
@@ -413,9 +425,9 @@ __global__ __launch_bounds__(256) void span_merge_kernel(const float* __restrict
   }
   const float inv = l == 0.f ? 0.f : 1.0f / l;  // (a token without rows: zeros)
   if constexpr (T::EPC == 8)
-    *reinterpret_cast<uint2*>(out + r * kD + 4 * lane) = make_uint2(BF16::round2(o.x * inv, o.y * inv), BF16::round2(o.z * inv, o.w * inv));
+    *reinterpret_cast<uint2*>(out + 4 * lane) = make_uint2(BF16::round2(o.x * inv, o.y * inv), BF16::round2(o.z * inv, o.w * inv));
   else
-    *reinterpret_cast<float4*>(out + r * kD + 4 * lane) = make_float4(o.x * inv, o.y * inv, o.z * inv, o.w * inv);
+    *reinterpret_cast<float4*>(out + 4 * lane) = make_float4(o.x * inv, o.y * inv, o.z * inv, o.w * inv);
 }
 
 // ---- the launch -----------------------------------------------------------------------------------------------------
@@ -443,7 +455,8 @@ static int span_splits(long long blocks, long long slots, long long most) {
 // 32/8 up to 8192 rows 92.5 / 54.1; with 32 query rows 8 x 4 of 64/8, window 1000 14.9 / 17.6, 2000 23.1 / 25.6, 8192 59.8 / 58.0; in 4 bits, 8192 rows, 8 x 8 tokens of
 // 64/8 (64 query rows) 79 / 91, 4 x 20 of 32/8 (80) 65.6 / 53.2, 4 x 64 of 32/8 (256) 143 / 92.
 SpanPlan span_plan(const Shape& s, int m, int window, int sinks, bool bits4, bool short_rows) {
-  SpanPlan p{16, 0, 1, 0};
+  SpanPlan p{};
+  p.rows = 16;
   const long long M = (long long)m * s.G;
   const long long tokens_read = window > 0 ? (long long)window + m - 1 + sinks : s.S, most_read = tokens_read < s.S ? tokens_read : s.S;
   const double bytes = (double)s.B * s.Hkv * most_read * (2 * kD * s.elem_bytes);
@@ -460,26 +473,49 @@ SpanPlan span_plan(const Shape& s, int m, int window, int sinks, bool bits4, boo
   const long long read = window > 0 && most < s.S ? most : s.S, blocks = (long long)s.B * p.tiles * s.Hkv;
   // as many parts as fill the blocks that are resident together, by the kernels' registers
   const long long slots = (lds ? 1LL : bits4 ? span_q4_waves(s.dtype == 1, p.rows) : s.dtype == 0 && p.rows == 16 ? 3LL : 2LL) * device_cus();
+  // From 90 MB of rows on, of which none is read twice, values are loaded past the caches (row_loads in api.hip).  us through / past: 64
+  // sequences of 64/8 heads with 4100 rows each 180 / 163, 16 of 32/8 with 16384 186 / 166, 13 with 4000 51.4 / 47.8, with 1500 (80 MB) 21.3 / 21.6;
+  // fp32, 16 of 24 heads with 1000 rows 74.5 / 68.1, 5 with 703 (86 MB) 22.7 / 23.4.
+  const bool large = (double)blocks * read * (bits4 ? 2.0 * (kQ4RowBytes + kQ4ScaleBytes) : 2.0 * kD * s.elem_bytes) >= kPastBytes;
+  p.past = p.tiles == 1 && large;
   p.nsplit = span_splits(blocks, slots, (read + 127) / 128);
   p.run = (int)((read + p.nsplit - 1) / p.nsplit);
+  p.parts = p.nsplit > 1 ? (size_t)s.B * m * s.G * s.Hkv * p.nsplit : 0;
+  // Runs are dealt by the lengths where a round of blocks holds two and more of each tile and the call is long enough for what it costs, about 1 us: us
+  // by the longest length / so, with lengths from a quarter of it on: in 4 bits, 16 sequences of 32/8 bf16 heads up to 16384 rows 53.1 / 44.5, 40 up to 3000
+  // 31.8 / 26.3, of 8 fp32 heads 38.3 / 30.1, 8 of 64/8 up to 4000 (41 MB) 17.0 / 16.6, up to 2000 13.0 / 14.0, 4 of 32/8 up to 4096 (21 MB) 12.8 / 13.2; in bf16, 16 of
+  // 32/8 up to 16384 129 / 124, 5 up to 8000 29.0 / 28.0; in fp32 none gained, 8 of 8 up to 2000 25.8 / 26.6.
+  const bool deals = bits4 ? !lds && (double)blocks * read * 2.0 * (kQ4RowBytes + kQ4ScaleBytes) >= 33e6 : s.dtype == 1 && p.rows == 16 && p.past;
+  const long long tiles = (long long)s.B * p.tiles, all = tiles * ((read + 127) / 128), round = slots / s.Hkv, cap = round < all ? round : all;
+  if (tiles > 1 && tiles <= 64) {
+    if (deals && cap >= 2 * tiles) p.cap = (int)cap;
+    p.dealt = (size_t)tiles;
+    const size_t parts = (size_t)cap * s.Hkv * p.rows;
+    if (p.parts < parts) p.parts = parts;
+  }
   return p;
 }
 
-hipError_t launch_span_q4(const Shape& s, const SpanArgs& a, hipStream_t st);
+hipError_t launch_span_q4(const Shape& s, const SpanArgs& a, unsigned blocks, bool past, hipStream_t st);
 
-template <typename T>
-static void launch_span_merge(const SpanArgs& a, hipStream_t st) {
-  const long long rows = (long long)a.B * a.m * a.Hq;
-  auto* out = static_cast<typename T::store_t*>(a.out);
-  if (a.nsplit <= 4)
-    hipLaunchKernelGGL((span_merge_kernel<T, 1>), dim3((unsigned)((rows + 7) / 8)), dim3(256), 0, st, a.partial, out, rows, a.nsplit);
+template <typename T, bool DEALT>
+static void launch_span_merge(const SpanArgs& a, int runs, hipStream_t st) {
+  const unsigned rows = (unsigned)(a.B * a.m * a.Hq);
+  if (runs <= 4 * a.B * a.tiles)
+    hipLaunchKernelGGL((span_merge_kernel<T, 1, DEALT>), dim3((rows + 7) / 8), dim3(256), 0, st, a);
   else
-    hipLaunchKernelGGL((span_merge_kernel<T, 8>), dim3((unsigned)rows), dim3(256), 0, st, a.partial, out, rows, a.nsplit);
+    hipLaunchKernelGGL((span_merge_kernel<T, 8, DEALT>), dim3(rows), dim3(256), 0, st, a);
+}
+template <typename T>
+static void launch_span_merge(const SpanArgs& a, int runs, hipStream_t st) {
+  if (a.dealt != nullptr)
+    launch_span_merge<T, true>(a, runs, st);
+  else
+    launch_span_merge<T, false>(a, runs, st);
 }
 
-hipError_t launch_span(const Shape& s, SpanArgs a, hipStream_t st) {
+hipError_t launch_span(const Shape& s, SpanArgs a, const SpanPlan& plan, hipStream_t st) {
   const bool bits4 = a.cache.k_scales != nullptr;
-  const SpanPlan plan = span_plan(s, a.m, a.window, a.sinks, bits4);
   if (a.window == 0) {
     a.window = 0x7fffffff;
     a.sinks = 0;
@@ -488,36 +524,37 @@ hipError_t launch_span(const Shape& s, SpanArgs a, hipStream_t st) {
   a.tiles = plan.tiles;
   a.nsplit = plan.nsplit;
   a.run = plan.run;
-  const dim3 grid((unsigned)((long long)a.B * a.Hkv * a.tiles * a.nsplit)), block(64 * kSpWaves);
+  a.cap = plan.cap;
+  const int tiles = a.B * a.tiles, runs = a.dealt != nullptr ? a.cap : tiles * a.nsplit;
+  const unsigned blocks = (unsigned)((long long)runs * a.Hkv);
+  const dim3 grid(blocks), block(64 * kSpWaves);
   hipError_t e = hipSuccess;
-  // From 90 MB of rows on, of which none is read twice, values are loaded past the caches (row_loads in api.hip).  us through / past: 64
-  // sequences of 64/8 heads with 4100 rows each 180 / 163, 16 of 32/8 with 16384 186 / 166, 13 with 4000 51.4 / 47.8, with 1500 (80 MB) 21.3 / 21.6;
-  // fp32, 16 of 24 heads with 1000 rows 74.5 / 68.1, 5 with 703 (86 MB) 22.7 / 23.4.
-  const bool past = plan.tiles == 1 && (double)a.B * a.Hkv * plan.nsplit * plan.run * (2 * kD * s.elem_bytes) >= kPastBytes;
   if (bits4)
-    e = launch_span_q4(s, a, st);
-  else if (s.dtype == 0 && plan.rows == 16 && past)
+    e = launch_span_q4(s, a, blocks, plan.past, st);
+  else if (s.dtype == 0 && plan.rows == 16 && plan.past)
     hipLaunchKernelGGL((span_f32_kernel<1, true>), grid, block, 0, st, a);
   else if (s.dtype == 0 && plan.rows == 16)
     hipLaunchKernelGGL((span_f32_kernel<1, false>), grid, block, 0, st, a);
   else if (s.dtype == 0)
     hipLaunchKernelGGL((span_f32_kernel<2, false>), grid, block, 0, st, a);
-  else if (plan.rows == 16 && past)
-    hipLaunchKernelGGL((span_rows_kernel<true>), grid, block, 0, st, a);
+  else if (plan.rows == 16 && a.dealt != nullptr)
+    hipLaunchKernelGGL((span_rows_kernel<true, true>), grid, block, 0, st, a);
+  else if (plan.rows == 16 && plan.past)
+    hipLaunchKernelGGL((span_rows_kernel<true, false>), grid, block, 0, st, a);
   else if (plan.rows == 16)
-    hipLaunchKernelGGL((span_rows_kernel<false>), grid, block, 0, st, a);
+    hipLaunchKernelGGL((span_rows_kernel<false, false>), grid, block, 0, st, a);
   else if (plan.rows == 64)
-    e = launch_span_tiles<8, 2, false>(a, st);
+    e = launch_span_tiles<8, 2, false>(a, blocks, st);
   else if (plan.rows == 128)
-    e = launch_span_tiles<8, 4, false>(a, st);
+    e = launch_span_tiles<8, 4, false>(a, blocks, st);
   else
-    e = launch_span_tiles<8, 8, false>(a, st);
+    e = launch_span_tiles<8, 8, false>(a, blocks, st);
   if (e == hipSuccess) e = hipGetLastError();
-  if (e != hipSuccess || a.nsplit == 1) return e;
+  if (e != hipSuccess || (a.dealt == nullptr && a.nsplit == 1)) return e;
   if (s.dtype == 1)
-    launch_span_merge<BF16>(a, st);
+    launch_span_merge<BF16>(a, runs, st);
   else
-    launch_span_merge<F32>(a, st);
+    launch_span_merge<F32>(a, runs, st);
   return hipGetLastError();
 }
 

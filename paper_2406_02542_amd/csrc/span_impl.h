@@ -23,6 +23,15 @@ struct SpanRows {
   int lo, hi, nsink;  // of the tile
   int len_min;        // the shortest token's rows (not 0), hi the longest's
 };
+// Of tokens that see from `least` to `most` rows.
+__device__ __forceinline__ SpanRows span_rows_of(const SpanArgs& a, int least, int most) {
+  SpanRows r;
+  r.hi = most;
+  r.len_min = least;
+  r.lo = most > 0 ? max(0, least - a.window) : 0;
+  r.nsink = min(a.sinks, r.lo);
+  return r;
+}
 // Of tokens j0 .. j1 of sequence b; every wave for itself.
 __device__ __forceinline__ SpanRows span_rows(const SpanArgs& a, int b, int j0, int j1) {
   int most = 0, least = 0;  // least: S_max less the shortest
@@ -32,12 +41,8 @@ __device__ __forceinline__ SpanRows span_rows(const SpanArgs& a, int b, int j0, 
     most = max(most, len);
     least = max(least, len > 0 ? a.S_max - len : 0);
   }
-  SpanRows r;
-  r.hi = wave_max_i32(most);
-  r.len_min = a.S_max - wave_max_i32(least);
-  r.lo = r.hi > 0 ? max(0, r.len_min - a.window) : 0;
-  r.nsink = min(a.sinks, r.lo);
-  return r;
+  const int hi = wave_max_i32(most);
+  return span_rows_of(a, a.S_max - wave_max_i32(least), hi);
 }
 
 // Steps of a tile: those of the sinks, then those of the window.
@@ -114,9 +119,10 @@ __device__ __forceinline__ uint32_t bf16_marks(uint32_t x) { return bf16_not_fin
 __device__ __forceinline__ uint32_t bf16_finite(uint32_t x) { return x & ~(bf16_not_finite(x) * 0xffffu); }
 __device__ __forceinline__ uint32_t f32_not_finite(float x) { return ((__float_as_uint(x) & 0x7f800000u) + 0x00800000u) >> 31; }
 
-// What a block does: steps [s0, s1) of a tile, part `part` of its nsplit.
+// What a block does: steps [s0, s1) of a tile, run `part` of its `parts`.
 struct SpanTile {
-  int b, h, tile, part, s0, s1;
+  int b, h, tile, part, parts, s0, s1;  // h < 0: nothing
+  int slot;  // the run's number
   SpanRows rows;
 };
 
@@ -126,36 +132,101 @@ __device__ __forceinline__ long long span_place(const SpanArgs& a, int b, int h,
   return ((long long)b * a.m + j) * a.Hq + h * a.G + (r & (a.G - 1));
 }
 // Where query row r of the tile has this block's part.
+template <bool DEALT>
 __device__ __forceinline__ float* span_part(const SpanArgs& a, const SpanTile& t, int r) {
-  return a.partial + (span_place(a, t.b, t.h, t.tile * a.rows + r) * a.nsplit + t.part) * kPartStride;
+  const long long at = DEALT ? ((long long)t.slot * a.Hkv + t.h) * a.rows + r : span_place(a, t.b, t.h, t.tile * a.rows + r) * a.nsplit + t.part;
+  return a.partial + at * kPartStride;
 }
 
-// This block's tile and its share of the tile's steps: runs of equal length, so that blocks have equal work whatever the lengths and short
-// sequences fewer of them (more rows than expected, of tokens that do not lie next to each other, make a tile's runs longer).  us with the
-// rows of each sequence in equal parts and so: 16 sequences of 32/8 bf16 heads up to 16384 rows 144, 136; 5 of 24 fp32 heads up to 2311 in
-// 4 bits 19.1, 16.8.
-template <int KEYS>
+// Tiles in the order in which runs are dealt: b tiles + i, the last tokens first, which see the most.
+__device__ __forceinline__ void span_tile_at(const SpanArgs& a, int t, int& b, int& tile) {
+  b = t / a.tiles;
+  tile = a.tiles - 1 - (t - b * a.tiles);
+}
+// This block's run.  Without lengths, and for one or many tiles, a tile is cut into nsplit runs of `run` rows, as the longest length asks for (more rows
+// than expected, of tokens that do not lie next to each other, make a tile's runs longer).  Else the blocks deal the runs, each for itself, since lengths
+// are on the device only: all runs are of about one length, the least of a few with which they fit the blocks that are resident together, so that sequences
+// of all lengths keep every CU as busy as equal ones would.  A tile's lane takes as many as its length asks for, and where they begin is the
+// sum of the lanes before (figures at span_plan).
+template <int KEYS, bool DEALT>
 __device__ __forceinline__ SpanTile span_tile(const SpanArgs& a) {
   SpanTile t;
-  int x = blockIdx.x;
-  t.h = x % a.Hkv;  // (a run's heads next to each other)
-  x /= a.Hkv;
-  t.part = x % a.nsplit;
-  x /= a.nsplit;
-  t.b = x / a.tiles;
-  t.tile = a.tiles - 1 - (x - t.b * a.tiles);  // (the last tokens see the most)
-  const int r0 = t.tile * a.rows, lg = 31 - __builtin_clz(a.G), last = min(r0 + a.rows, a.m * a.G) - 1;
-  t.rows = span_rows(a, t.b, r0 >> lg, last >> lg);
+  const int i = blockIdx.x / a.Hkv, lg = 31 - __builtin_clz(a.G);
+  t.h = blockIdx.x - i * a.Hkv;  // (a run's heads next to each other)
+  t.slot = i;
+  bool known = false;
+  int each = 0;
+  if constexpr (!DEALT) {
+    const int at = i / a.nsplit;
+    t.parts = a.nsplit;
+    t.part = i - at * a.nsplit;
+    span_tile_at(a, at, t.b, t.tile);
+    each = (a.run + KEYS - 1) / KEYS;
+  } else {
+    constexpr int kUnit = KEYS >= 64 ? 1 : 4;  // steps of a run: a multiple of the waves that take them in turn, and at least 128 rows
+    const int lane = threadIdx.x & 63, all = a.B * a.tiles;  // (up to 64)
+    int b, tile, n = 0, most, least;
+    span_tile_at(a, min(lane, all - 1), b, tile);
+    const int r0 = tile * a.rows, j0 = r0 >> lg, j1 = (min(r0 + a.rows, a.m * a.G) - 1) >> lg;
+    most = least = span_len(a, b, j0);
+    known = a.rows <= 8 << lg;  // (else by the tile's first and last token and some between)
+    if (a.m > 1) {
+      least = least > 0 ? least : 0x7fffffff;
+#pragma unroll
+      for (int u = 1; u < 8; ++u) {
+        const int len = span_len(a, b, u == 7 ? j1 : min(j0 + u, j1));
+        most = max(most, len);
+        least = min(least, len > 0 ? len : 0x7fffffff);
+      }
+      least = min(least, most);
+    }
+    if (lane < all) n = SpanSteps<KEYS>(span_rows_of(a, least, most)).total;
+    const float longest = (float)wave_max_i32(n), total = wave_sum_f32((float)n);
+    // a run's length, from the least that may do to one that does
+    const float low = total * __builtin_amdgcn_rcpf((float)a.cap), high = fminf(total * __builtin_amdgcn_rcpf((float)(a.cap - all)), longest);
+    uint32_t c[4], incl[2];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      const float run = fmaxf(ceilf(fmaf(high - low, (float)k / 3.f, low) * (1.0f / kUnit)) * kUnit, 128.f / KEYS);
+      c[k] = lane < all ? (uint32_t)fmaxf(ceilf(fmaf((float)n, __builtin_amdgcn_rcpf(run), -1e-4f)), 1.f) : 0u;
+    }
+    incl[0] = wave_inclusive_scan_u32(c[0] | c[1] << 16);
+    incl[1] = wave_inclusive_scan_u32(c[2] | c[3] << 16);
+    uint32_t mine = lane < all ? 1u : 0u, sum = min(lane + 1, all);  // (a run each)
+#pragma unroll
+    for (int k = 3; k >= 0; --k) {
+      const uint32_t x = incl[k / 2] >> (16 * (k % 2)) & 0xffffu;
+      if (__builtin_amdgcn_readlane((int)x, 63) <= a.cap) {
+        mine = c[k];
+        sum = x;
+      }
+    }
+    const int found = __popcll(__ballot((int)sum <= i)), at = min(found, all - 1);
+    if (found >= all) t.h = -1;
+    t.parts = __builtin_amdgcn_readlane((int)mine, at);
+    t.part = i - __builtin_amdgcn_readlane((int)(sum - mine), at);
+    t.b = __builtin_amdgcn_readlane(b, at);
+    t.tile = __builtin_amdgcn_readlane(tile, at);
+    t.rows = span_rows_of(a, __builtin_amdgcn_readlane(least, at), __builtin_amdgcn_readlane(most, at));
+    if (t.h == 0 && t.part == 0 && threadIdx.x == 0) a.dealt[at] = make_int2(i, t.parts);
+  }
+  if (!known) {
+    const int r0 = t.tile * a.rows, last = min(r0 + a.rows, a.m * a.G) - 1;
+    t.rows = span_rows(a, t.b, r0 >> lg, last >> lg);
+  }
   const SpanSteps<KEYS> n(t.rows);
-  const int each = max((a.run + KEYS - 1) / KEYS, (n.total + a.nsplit - 1) / a.nsplit);
-  t.s0 = t.part * each;
+  each = max(each, (n.total + t.parts - 1) / t.parts);
+  t.s0 = min(n.total, t.part * each);
   t.s1 = min(n.total, t.s0 + each);
+  for (int* x : {&t.b, &t.h, &t.tile, &t.part, &t.parts, &t.slot, &t.s0, &t.s1, &t.rows.lo, &t.rows.hi, &t.rows.nsink, &t.rows.len_min})
+    *x = __builtin_amdgcn_readfirstlane(*x);  // (uniform, which the compiler does not see)
   return t;
 }
 
 // A run that no row is left for: its parts say so, which the merge goes by.
+template <bool DEALT>
 __device__ __forceinline__ void span_none(const SpanArgs& a, const SpanTile& t, int live) {
-  for (int r = threadIdx.x; r < live; r += blockDim.x) *reinterpret_cast<float2*>(span_part(a, t, r) + kD) = make_float2(kNegBig, 0.f);
+  for (int r = threadIdx.x; r < live; r += blockDim.x) *reinterpret_cast<float2*>(span_part<DEALT>(a, t, r) + kD) = make_float2(kNegBig, 0.f);
 }
 
 // A wave's state after its steps, for 16 query rows: lane (row r16, kgrp) holds maximum m and sum l of its row (l its own share of the
@@ -167,7 +238,7 @@ struct SpanMerge {
 };
 
 // The waves' results joined: `live` query rows of the tile, out or as parts.  Begins with a barrier.
-template <typename T, int ROWS, int WAVES>
+template <typename T, bool DEALT, int ROWS, int WAVES>
 __device__ __forceinline__ void span_store(const SpanArgs& a, const SpanMerge<ROWS, WAVES>& sm, const SpanTile& tile, int r0, int live) {
   __syncthreads();
   for (int i = threadIdx.x; i < live * (kD / 4); i += 64 * WAVES) {
@@ -183,8 +254,8 @@ __device__ __forceinline__ void span_store(const SpanArgs& a, const SpanMerge<RO
       ls = fmaf(sm.ml[w][r].y, f, ls);
       os = make_float4(fmaf(x.x, f, os.x), fmaf(x.y, f, os.y), fmaf(x.z, f, os.z), fmaf(x.w, f, os.w));
     }
-    if (a.nsplit > 1) {
-      float* p = span_part(a, tile, r);
+    if (tile.parts > 1) {
+      float* p = span_part<DEALT>(a, tile, r);
       *reinterpret_cast<float4*>(p + c) = os;
       if (c == 0) *reinterpret_cast<float2*>(p + kD) = make_float2(mn, ls);
     } else {

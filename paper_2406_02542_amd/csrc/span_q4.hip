@@ -44,18 +44,19 @@ __device__ __forceinline__ float q4_times_step(float p, uint32_t scales) {
 // (CG = 2) 78.3, 72.5, 16 of 64/8 with 8000 and two tokens (1) 65.6, 48.4, 16 of 32/8 with 16384 (4) 65.0, 63.5.  (16 rows' products for two groups
 // of queries at a time, which unpack codes half as often, leave a SIMD one wave: 50.6 us where these take 43.9.)
 // bf16: q is one term, the weights two (2^-16 of each, as the library's other attention); fp32: three each.
-template <typename T, int CG, bool STREAM>
+template <typename T, int CG, bool STREAM, bool DEALT>
 __global__ __launch_bounds__(64 * kQ4Waves, span_q4_waves(T::EPC == 8, 16 / CG)) void span_q4_kernel(SpanArgs a) {
   constexpr int KEYS = 32, QT = T::EPC == 8 ? 1 : 3, PT = T::EPC == 8 ? 2 : 3, NS = kQ4Groups / CG, ROWS = 16 / CG;
   __shared__ __align__(16) SpanMerge<ROWS, kQ4Waves> sm;
   __shared__ uint4 s_scales[kQ4Waves][2 * KEYS];  // of a step's keys, and values
-  const SpanTile tile = span_tile<KEYS>(a);
+  const SpanTile tile = span_tile<KEYS, DEALT>(a);
+  if (tile.h < 0) return;  // (uniform for the block)
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), r16 = lane & 15, kgrp = lane >> 4;
   const int gl = r16 % CG, g0 = gl * NS, r = r16 / CG;
   const int M = a.m * a.G, r0 = tile.tile * ROWS, live = min(ROWS, M - r0), lg = 31 - __builtin_clz(a.G);
   const SpanRows rows = tile.rows;
   const SpanSteps<KEYS> steps(rows);
-  if (tile.s0 >= tile.s1 && tile.part > 0) return span_none(a, tile, live);  // (uniform for the block)
+  if (tile.s0 >= tile.s1 && tile.part > 0) return span_none<DEALT>(a, tile, live);  // (uniform for the block)
   const int s1 = tile.s1;
   const RowPlaces places(a.cache, tile.b, tile.h, a.Hkv);
   const Q4Pair q4_pair;
@@ -140,7 +141,18 @@ __global__ __launch_bounds__(64 * kQ4Waves, span_q4_waves(T::EPC == 8, 16 / CG))
     o[n][0] = o[n][1] = ones[n] = am_f32x4_t{};
   }
 
+  // The waves of a SIMD, of different blocks, are to end together: those that are behind go first.  (The oldest go first otherwise, and a SIMD is left
+  // to the last one: blocks of equal work took 34 to 65 us where these take 49 to 61.)  us without / so: 16 sequences of 32/8 heads
+  // with 16384 rows 64.1 / 60.9, four tokens of 8 of 64/8 44.3 / 42.4.
+  const int quarter = (s1 - s) >> 2, marks[3] = {s + quarter, s + 2 * quarter, s + 3 * quarter};
+  __builtin_amdgcn_s_setprio(3);
   for (; s < s1; s += kQ4Waves) {
+    if (s >= marks[2])
+      __builtin_amdgcn_s_setprio(0);
+    else if (s >= marks[1])
+      __builtin_amdgcn_s_setprio(1);
+    else if (s >= marks[0])
+      __builtin_amdgcn_s_setprio(2);
     const SpanStep st = span_step(steps, rows, s), next = span_step(steps, rows, min(s + kQ4Waves, steps.total - 1));
     s_scales[wave][lane] = sraw;
     __builtin_amdgcn_wave_barrier();
@@ -276,30 +288,36 @@ __global__ __launch_bounds__(64 * kQ4Waves, span_q4_waves(T::EPC == 8, 16 / CG))
     for (int i = 0; i < 4; i += 2)
       *reinterpret_cast<float4*>(&sm.o[wave][r][32 * (g0 + n) + 8 * kgrp + 2 * i]) = make_float4(y[0][i], y[1][i], y[0][i + 1], y[1][i + 1]);
   }
-  span_store<T>(a, sm, tile, r0, live);
+  span_store<T, DEALT>(a, sm, tile, r0, live);
 }
 
 template <typename T>
-static hipError_t launch_span_q4_t(const SpanArgs& a, hipStream_t st) {
-  const dim3 grid((unsigned)((long long)a.B * a.Hkv * a.tiles * a.nsplit)), block(64 * kQ4Waves);
-  const bool past = a.tiles == 1 && (double)a.B * a.Hkv * a.nsplit * a.run * (2 * (kQ4RowBytes + kQ4ScaleBytes)) >= kPastBytes;
-  if (T::EPC == 8 && a.rows == 128) return launch_span_tiles<8, 4, true>(a, st);
-  if (T::EPC == 8 && a.rows == 256) return launch_span_tiles<8, 8, true>(a, st);
-  if (a.rows == 4 && past)
-    hipLaunchKernelGGL((span_q4_kernel<T, 4, true>), grid, block, 0, st, a);
-  else if (a.rows == 4)
-    hipLaunchKernelGGL((span_q4_kernel<T, 4, false>), grid, block, 0, st, a);
-  else if (a.rows == 8 && past)
-    hipLaunchKernelGGL((span_q4_kernel<T, 2, true>), grid, block, 0, st, a);
-  else if (a.rows == 8)
-    hipLaunchKernelGGL((span_q4_kernel<T, 2, false>), grid, block, 0, st, a);
-  else
-    hipLaunchKernelGGL((span_q4_kernel<T, 1, false>), grid, block, 0, st, a);
+static hipError_t launch_span_q4_t(const SpanArgs& a, unsigned blocks, bool past, hipStream_t st) {
+  const dim3 grid(blocks), block(64 * kQ4Waves);
+  if (T::EPC == 8 && a.rows == 128) return launch_span_tiles<8, 4, true>(a, blocks, st);
+  if (T::EPC == 8 && a.rows == 256) return launch_span_tiles<8, 8, true>(a, blocks, st);
+#define LOKI_SPAN_Q4(CG, STREAM)                                                            \
+  if (a.dealt != nullptr)                                                                   \
+    hipLaunchKernelGGL((span_q4_kernel<T, CG, STREAM, true>), grid, block, 0, st, a);       \
+  else                                                                                      \
+    hipLaunchKernelGGL((span_q4_kernel<T, CG, STREAM, false>), grid, block, 0, st, a)
+  if (a.rows == 4 && past) {
+    LOKI_SPAN_Q4(4, true);
+  } else if (a.rows == 4) {
+    LOKI_SPAN_Q4(4, false);
+  } else if (a.rows == 8 && past) {
+    LOKI_SPAN_Q4(2, true);
+  } else if (a.rows == 8) {
+    LOKI_SPAN_Q4(2, false);
+  } else {
+    LOKI_SPAN_Q4(1, false);
+  }
+#undef LOKI_SPAN_Q4
   return hipGetLastError();
 }
 
-hipError_t launch_span_q4(const Shape& s, const SpanArgs& a, hipStream_t st) {
-  return s.dtype == 0 ? launch_span_q4_t<F32>(a, st) : launch_span_q4_t<BF16>(a, st);
+hipError_t launch_span_q4(const Shape& s, const SpanArgs& a, unsigned blocks, bool past, hipStream_t st) {
+  return s.dtype == 0 ? launch_span_q4_t<F32>(a, blocks, past, st) : launch_span_q4_t<BF16>(a, blocks, past, st);
 }
 
 }  // namespace loki

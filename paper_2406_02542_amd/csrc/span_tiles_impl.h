@@ -72,11 +72,11 @@ __global__ __launch_bounds__(64 * WAVES, WAVES == 4 ? 1 : 2) void span_tiles_ker
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int l32 = lane & 31, half = lane >> 5, l16 = lane & 15;
   const int wq = wave % WQ, wk = wave / WQ;
-  const SpanTile tile = span_tile<KT>(a);
+  const SpanTile tile = span_tile<KT, false>(a);
   const int M = a.m * a.G, r0 = tile.tile * (32 * WQ), live = min(32 * WQ, M - r0), lg = 31 - __builtin_clz(a.G);
   const SpanRows rows = tile.rows;
   const SpanSteps<KT> steps(rows);
-  if (tile.s0 >= tile.s1 && tile.part > 0) return span_none(a, tile, live);  // (uniform for the block)
+  if (tile.s0 >= tile.s1 && tile.part > 0) return span_none<false>(a, tile, live);  // (uniform for the block)
   const int s0 = tile.s0, s1 = tile.s1;
   const RowPlaces places(a.cache, tile.b, tile.h, a.Hkv);
   // this wave's queries, and its lane's
@@ -362,7 +362,7 @@ __global__ __launch_bounds__(64 * WAVES, WAVES == 4 ? 1 : 2) void span_tiles_ker
     if (wk != 0) return;
   }
   const float inv = l == 0.f ? 0.f : 1.0f / l;  // (a token without rows: zeros)
-  const bool parts = a.nsplit > 1;
+  const bool parts = tile.parts > 1;
   // a lane has four columns of one query at a time: through LDS, so that a store takes four half rows
   char* at = smem + wave * 8192;  // [32 queries][64 columns], 16-byte chunks exchanged as the keys'
 #pragma unroll
@@ -382,7 +382,7 @@ __global__ __launch_bounds__(64 * WAVES, WAVES == 4 ? 1 : 2) void span_tiles_ker
       const float4 x = *reinterpret_cast<const float4*>(at + r * 256 + ((l16 ^ (r & 15)) * 16));
       if (q0 + r < live) {
         if (parts)
-          *reinterpret_cast<float4*>(span_part(a, tile, q0 + r) + 64 * pass + 4 * l16) = x;
+          *reinterpret_cast<float4*>(span_part<false>(a, tile, q0 + r) + 64 * pass + 4 * l16) = x;
         else
           *reinterpret_cast<uint2*>(static_cast<uint16_t*>(a.out) + span_place(a, tile.b, tile.h, r0 + q0 + r) * kD + 64 * pass + 4 * l16) = make_uint2(BF16::round2(x.x, x.y), BF16::round2(x.z, x.w));
       }
@@ -390,16 +390,16 @@ __global__ __launch_bounds__(64 * WAVES, WAVES == 4 ? 1 : 2) void span_tiles_ker
     __builtin_amdgcn_wave_barrier();
   }
   if (parts && half == 0 && row < live)
-    *reinterpret_cast<float2*>(span_part(a, tile, row) + kD) = make_float2(m, l);
+    *reinterpret_cast<float2*>(span_part<false>(a, tile, row) + kD) = make_float2(m, l);
 }
 
 template <int WAVES, int WQ, bool BITS4>
-static hipError_t launch_span_tiles(const SpanArgs& a, hipStream_t st) {
+static hipError_t launch_span_tiles(const SpanArgs& a, unsigned blocks, hipStream_t st) {
   static std::atomic<unsigned long long> raised{0};
   constexpr int bytes = span_lds_bytes<WAVES, WQ, BITS4>();
   const hipError_t e = allow_dynamic_lds(reinterpret_cast<const void*>(&span_tiles_kernel<WAVES, WQ, BITS4>), bytes, raised);
   if (e != hipSuccess) return e;
-  const dim3 grid((unsigned)((long long)a.B * a.Hkv * a.tiles * a.nsplit));
+  const dim3 grid(blocks);
   hipLaunchKernelGGL((span_tiles_kernel<WAVES, WQ, BITS4>), grid, dim3(64 * WAVES), bytes, st, a);
   return hipGetLastError();
 }
