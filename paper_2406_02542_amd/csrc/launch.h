@@ -311,6 +311,7 @@ struct SpanArgs {
   int rows, tiles;        // tiles of `rows` query rows of a sequence and KV head
   int nsplit, run;        // runs of a tile, of `run` rows
   int cap;                // runs of a KV head that are resident together
+  int halves;             // tiles of 256 rows without parts: blocks that are resident together, of which the last may take half a tile; 0: none does
 };
 // Blocks of the 4-bit kernels that a CU holds, by the registers of tiles of `rows` query rows.  us with more or fewer: 16 sequences of 32/8 bf16 heads up
 // to 16384 rows (4 rows) four 57.7, three 60.7; 64 of 64/8 up to 4096 (8) two 68.1, three 75.6; fp32, 16 of 8/8 up to 8000 (4) three 39.6, two
@@ -318,7 +319,7 @@ struct SpanArgs {
 __host__ __device__ constexpr int span_q4_waves(bool bf16, int rows) { return rows == 4 ? (bf16 ? 4 : 3) : 2; }
 // How a call is cut: the workspace's size and the launch go by it.
 struct SpanPlan {
-  int rows, tiles, nsplit, run, cap;  // cap 0: not dealt
+  int rows, tiles, nsplit, run, cap, halves;  // cap 0: not dealt
   size_t parts, dealt;                // what the workspace holds of each
   bool past;                          // values are loaded past the caches
 };

@@ -479,6 +479,10 @@ SpanPlan span_plan(const Shape& s, int m, int window, int sinks, bool bits4, boo
   const bool large = (double)blocks * read * (bits4 ? 2.0 * (kQ4RowBytes + kQ4ScaleBytes) : 2.0 * kD * s.elem_bytes) >= kPastBytes;
   p.past = p.tiles == 1 && large;
   p.nsplit = span_splits(blocks, slots, (read + 127) / 128);
+  if (p.rows == 256 && blocks >= slots && blocks <= 8 * slots) {
+    p.nsplit = 1;
+    p.halves = (int)slots;
+  }
   p.run = (int)((read + p.nsplit - 1) / p.nsplit);
   p.parts = p.nsplit > 1 ? (size_t)s.B * m * s.G * s.Hkv * p.nsplit : 0;
   // Runs are dealt by the lengths where a round of blocks holds two and more of each tile and the call is long enough for what it costs, about 1 us: us
@@ -525,8 +529,9 @@ hipError_t launch_span(const Shape& s, SpanArgs a, const SpanPlan& plan, hipStre
   a.nsplit = plan.nsplit;
   a.run = plan.run;
   a.cap = plan.cap;
+  a.halves = plan.halves;
   const int tiles = a.B * a.tiles, runs = a.dealt != nullptr ? a.cap : tiles * a.nsplit;
-  const unsigned blocks = (unsigned)((long long)runs * a.Hkv);
+  const unsigned blocks = (unsigned)((long long)runs * a.Hkv) + a.halves / 2;
   const dim3 grid(blocks), block(64 * kSpWaves);
   hipError_t e = hipSuccess;
   if (bits4)
@@ -547,8 +552,10 @@ hipError_t launch_span(const Shape& s, SpanArgs a, const SpanPlan& plan, hipStre
     e = launch_span_tiles<8, 2, false>(a, blocks, st);
   else if (plan.rows == 128)
     e = launch_span_tiles<8, 4, false>(a, blocks, st);
-  else
+  else if (a.halves == 0)
     e = launch_span_tiles<8, 8, false>(a, blocks, st);
+  else
+    e = launch_span_tiles<8, 8, false, true>(a, blocks, st);
   if (e == hipSuccess) e = hipGetLastError();
   if (e != hipSuccess || (a.dealt == nullptr && a.nsplit == 1)) return e;
   if (s.dtype == 1)

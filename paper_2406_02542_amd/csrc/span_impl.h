@@ -123,6 +123,7 @@ __device__ __forceinline__ uint32_t f32_not_finite(float x) { return ((__float_a
 struct SpanTile {
   int b, h, tile, part, parts, s0, s1;  // h < 0: nothing
   int slot;  // the run's number
+  int half;  // 0, or of a tile's rows the first (1) or the second (2) half
   SpanRows rows;
 };
 
@@ -143,6 +144,60 @@ __device__ __forceinline__ void span_tile_at(const SpanArgs& a, int t, int& b, i
   b = t / a.tiles;
   tile = a.tiles - 1 - (t - b * a.tiles);
 }
+// Of 64 tiles t0 .. those whose first token sees rows, and those that there are.
+__device__ __forceinline__ unsigned long long span_there(const SpanArgs& a, int t0, unsigned long long& tiles) {
+  const int at = t0 + (int)(threadIdx.x & 63), all = a.B * a.tiles;
+  int b, tile;
+  span_tile_at(a, min(at, all - 1), b, tile);
+  tiles = __ballot(at < all);
+  return __ballot(at < all && span_len(a, b, tile * a.rows >> (31 - __builtin_clz(a.G))) > 0);
+}
+// Blocks of tiles without parts, of which a CU holds one: whole rounds of tiles, and what is left, if it is no more than half a round, in halves of
+// their query rows, which take half the time (tiles of that few rows do so anyway).  Tiles of padded tokens come last.  us without / so: 16 chunks
+// of up to 100 tokens of 64/8 heads, window 2048 186 / 156, 4 of up to 700 of 32/8, window 4096 303 / 288, 2 of up to 2048 (of three
+// pairs of lengths one leaves that little) 358 / 336.
+__device__ __forceinline__ SpanTile span_tile_halves(const SpanArgs& a) {
+  SpanTile t{};
+  const int all = a.B * a.tiles, lg = 31 - __builtin_clz(a.G);
+  unsigned long long tiles;
+  int there = 0;
+  for (int t0 = 0; t0 < all; t0 += 64) there += __popcll(span_there(a, t0, tiles));
+  const int blocks = there * a.Hkv, whole = blocks / a.halves * a.halves, rest = blocks - whole;
+  const bool cut = 2 * rest <= a.halves;
+  const int busy = cut ? whole + 2 * rest : blocks;
+  int x = blockIdx.x;
+  const bool padded = x >= busy;
+  if (padded) {
+    x -= busy;
+  } else if (cut && x >= whole) {
+    t.half = x < whole + rest ? 1 : 2;
+    x -= t.half == 2 ? rest : 0;
+  }
+  int n = x / a.Hkv, at = -1;  // the n-th of those tiles
+  t.h = x - n * a.Hkv;
+  for (int t0 = 0; t0 < all; t0 += 64) {
+    unsigned long long mask = span_there(a, t0, tiles);
+    if (padded) mask = tiles & ~mask;
+    const int c = __popcll(mask);
+    if (at < 0 && n < c) {
+      const int lane = threadIdx.x & 63;
+      at = t0 + __builtin_ctzll(__ballot((mask >> lane & 1ull) != 0ull && __popcll(mask & ((1ull << lane) - 1)) == n));
+    }
+    n -= c;
+  }
+  if (at < 0) t.h = -1;
+  span_tile_at(a, max(at, 0), t.b, t.tile);
+  t.parts = 1;
+  if (t.half == 0 && a.m * a.G - t.tile * a.rows <= a.rows / 2) t.half = 1;
+  const int r0 = t.tile * a.rows + (t.half == 2 ? a.rows / 2 : 0), last = min(r0 + (t.half != 0 ? a.rows / 2 : a.rows), a.m * a.G) - 1;
+  if (r0 > last) t.h = -1;  // (the second half of what has no such rows)
+  t.rows = span_rows(a, t.b, min(r0, last) >> lg, last >> lg);
+  t.s1 = SpanSteps<64>(t.rows).total;
+  for (int* x : {&t.b, &t.h, &t.tile, &t.half, &t.s1, &t.rows.lo, &t.rows.hi, &t.rows.nsink, &t.rows.len_min})
+    *x = __builtin_amdgcn_readfirstlane(*x);  // (uniform, which the compiler does not see)
+  return t;
+}
+
 // This block's run.  Without lengths, and for one or many tiles, a tile is cut into nsplit runs of `run` rows, as the longest length asks for (more rows
 // than expected, of tokens that do not lie next to each other, make a tile's runs longer).  Else the blocks deal the runs, each for itself, since lengths
 // are on the device only: all runs are of about one length, the least of a few with which they fit the blocks that are resident together, so that sequences
@@ -154,6 +209,7 @@ __device__ __forceinline__ SpanTile span_tile(const SpanArgs& a) {
   const int i = blockIdx.x / a.Hkv, lg = 31 - __builtin_clz(a.G);
   t.h = blockIdx.x - i * a.Hkv;  // (a run's heads next to each other)
   t.slot = i;
+  t.half = 0;
   bool known = false;
   int each = 0;
   if constexpr (!DEALT) {

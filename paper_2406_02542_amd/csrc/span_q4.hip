@@ -295,7 +295,7 @@ template <typename T>
 static hipError_t launch_span_q4_t(const SpanArgs& a, unsigned blocks, bool past, hipStream_t st) {
   const dim3 grid(blocks), block(64 * kQ4Waves);
   if (T::EPC == 8 && a.rows == 128) return launch_span_tiles<8, 4, true>(a, blocks, st);
-  if (T::EPC == 8 && a.rows == 256) return launch_span_tiles<8, 8, true>(a, blocks, st);
+  if (T::EPC == 8 && a.rows == 256) return a.halves == 0 ? launch_span_tiles<8, 8, true>(a, blocks, st) : launch_span_tiles<8, 8, true, true>(a, blocks, st);
 #define LOKI_SPAN_Q4(CG, STREAM)                                                            \
   if (a.dealt != nullptr)                                                                   \
     hipLaunchKernelGGL((span_q4_kernel<T, CG, STREAM, true>), grid, block, 0, st, a);       \

@@ -59,11 +59,11 @@ struct SpanQ4Chunk {
 // Two pairs of tiles; at the end, where waves have other keys of the same queries, what half of them hand over, or the outputs.
 template <int WAVES, int WQ, bool BITS4>
 constexpr int span_lds_bytes() {
-  const int tiles = (BITS4 ? 8 : 4) * span_tile_keys<WAVES, WQ>() * 256, merge = WQ == WAVES ? 0 : WAVES * 32 * 8 + WAVES / 2 * 64 * 256;
+  const int tiles = (BITS4 ? 8 : 4) * span_tile_keys<WAVES, WQ>() * 256, merge = WAVES * 32 * 8 + WAVES / 2 * 64 * 256;
   return tiles > merge ? tiles : merge;
 }
 
-template <int WAVES, int WQ, bool BITS4>
+template <int WAVES, int WQ, bool BITS4, bool HALVES>
 __global__ __launch_bounds__(64 * WAVES, WAVES == 4 ? 1 : 2) void span_tiles_kernel(SpanArgs a) {
   extern __shared__ __align__(16) char smem[];  // [2][K tile, V tile], in 4 bits [2][K tile's terms, V tile's terms]
   constexpr int kThreads = 64 * WAVES, WK = WAVES / WQ, KT = span_tile_keys<WAVES, WQ>(), kSteps = KT / (32 * WK);
@@ -71,9 +71,18 @@ __global__ __launch_bounds__(64 * WAVES, WAVES == 4 ? 1 : 2) void span_tiles_ker
   constexpr int kTileBytes = KT * 256, kBufferBytes = (BITS4 ? 4 : 2) * kTileBytes, kValues = kBufferBytes / 2;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int l32 = lane & 31, half = lane >> 5, l16 = lane & 15;
-  const int wq = wave % WQ, wk = wave / WQ;
-  const SpanTile tile = span_tile<KT, false>(a);
-  const int M = a.m * a.G, r0 = tile.tile * (32 * WQ), live = min(32 * WQ, M - r0), lg = 31 - __builtin_clz(a.G);
+  SpanTile tile;
+  if constexpr (HALVES) {
+    tile = span_tile_halves(a);
+    if (tile.h < 0) return;  // (uniform for the block)
+  } else {
+    tile = span_tile<KT, false>(a);
+  }
+  // half of a tile: as WQ / 2 waves of queries, and two of keys
+  const bool half_tile = HALVES && tile.half != 0;
+  const int wq = half_tile ? wave % (WQ / 2) : wave % WQ, wk = half_tile ? wave / (WQ / 2) : wave / WQ;
+  const int M = a.m * a.G, r0 = tile.tile * (32 * WQ) + (tile.half == 2 ? 16 * WQ : 0), lg = 31 - __builtin_clz(a.G);
+  const int live = min(half_tile ? 16 * WQ : 32 * WQ, M - r0);
   const SpanRows rows = tile.rows;
   const SpanSteps<KT> steps(rows);
   if (tile.s0 >= tile.s1 && tile.part > 0) return span_none<false>(a, tile, live);  // (uniform for the block)
@@ -294,8 +303,8 @@ __global__ __launch_bounds__(64 * WAVES, WAVES == 4 ? 1 : 2) void span_tiles_ker
       const char* base = smem + ((t - s0) & 1) * kBufferBytes;
       const SpanStep whole = span_step(steps, rows, t);
 #pragma unroll 1
-      for (int s = 0; s < kSteps; ++s) {
-        const int key = (s * WK + wk) * 32;
+      for (int s = 0; s < (half_tile ? kSteps / 2 : kSteps); ++s) {
+        const int key = half_tile ? (2 * s + wk) * 32 : (s * WK + wk) * 32;
         const SpanStep st{whole.at + key, whole.lo, whole.hi};
         // (all uniform for the wave)
         if (st.at >= min(st.hi, own.hi) || st.at + 32 <= st.lo || (st.at + 32 <= own.lo && st.at >= a.sinks)) continue;
@@ -313,17 +322,18 @@ __global__ __launch_bounds__(64 * WAVES, WAVES == 4 ? 1 : 2) void span_tiles_ker
 #pragma unroll
     for (int c = 0; c < 4; ++c) o[c] = sp_f32x16_t{};
   }
-  if constexpr (WK > 1) {
+  if ((HALVES && half_tile) || WK > 1) {  // (uniform)
+    constexpr int Q = HALVES ? WQ / 2 : WQ, K = WAVES / Q;
     float2* ml = reinterpret_cast<float2*>(smem);                   // [wave][32] (max, sum)
     float4* ob = reinterpret_cast<float4*>(smem + WAVES * 32 * 8);  // [wave of the upper half][4][4][lane]
     if (half == 0) ml[wave * 32 + l32] = make_float2(m, l);
     __syncthreads();
     float mn = kNegBig, ls = 0.f;
 #pragma unroll
-    for (int w = 0; w < WK; ++w) mn = fmaxf(mn, ml[(w * WQ + wq) * 32 + l32].x);
+    for (int w = 0; w < K; ++w) mn = fmaxf(mn, ml[(w * Q + wq) * 32 + l32].x);
 #pragma unroll
-    for (int w = 0; w < WK; ++w) {
-      const float2 x = ml[(w * WQ + wq) * 32 + l32];
+    for (int w = 0; w < K; ++w) {
+      const float2 x = ml[(w * Q + wq) * 32 + l32];
       ls = fmaf(x.y, fast_exp2(x.x - mn), ls);
     }
     const float f = fast_exp2(m - mn);
@@ -334,9 +344,9 @@ __global__ __launch_bounds__(64 * WAVES, WAVES == 4 ? 1 : 2) void span_tiles_ker
 #pragma unroll
       for (int i = 0; i < 16; ++i) o[c][i] *= f;
 #pragma unroll
-    for (int n = WK / 2; n >= 1; n /= 2) {
+    for (int n = K / 2; n >= 1; n /= 2) {
       if (wk >= n && wk < 2 * n) {
-        float4* dst = ob + ((wk - n) * WQ + wq) * 16 * 64;
+        float4* dst = ob + ((wk - n) * Q + wq) * 16 * 64;
 #pragma unroll
         for (int c = 0; c < 4; ++c)
 #pragma unroll
@@ -345,7 +355,7 @@ __global__ __launch_bounds__(64 * WAVES, WAVES == 4 ? 1 : 2) void span_tiles_ker
       }
       __syncthreads();
       if (wk < n) {
-        const float4* src = ob + (wk * WQ + wq) * 16 * 64;
+        const float4* src = ob + (wk * Q + wq) * 16 * 64;
 #pragma unroll
         for (int c = 0; c < 4; ++c)
 #pragma unroll
@@ -393,14 +403,14 @@ __global__ __launch_bounds__(64 * WAVES, WAVES == 4 ? 1 : 2) void span_tiles_ker
     *reinterpret_cast<float2*>(span_part<false>(a, tile, row) + kD) = make_float2(m, l);
 }
 
-template <int WAVES, int WQ, bool BITS4>
+template <int WAVES, int WQ, bool BITS4, bool HALVES = false>
 static hipError_t launch_span_tiles(const SpanArgs& a, unsigned blocks, hipStream_t st) {
   static std::atomic<unsigned long long> raised{0};
   constexpr int bytes = span_lds_bytes<WAVES, WQ, BITS4>();
-  const hipError_t e = allow_dynamic_lds(reinterpret_cast<const void*>(&span_tiles_kernel<WAVES, WQ, BITS4>), bytes, raised);
+  const hipError_t e = allow_dynamic_lds(reinterpret_cast<const void*>(&span_tiles_kernel<WAVES, WQ, BITS4, HALVES>), bytes, raised);
   if (e != hipSuccess) return e;
   const dim3 grid(blocks);
-  hipLaunchKernelGGL((span_tiles_kernel<WAVES, WQ, BITS4>), grid, dim3(64 * WAVES), bytes, st, a);
+  hipLaunchKernelGGL((span_tiles_kernel<WAVES, WQ, BITS4, HALVES>), grid, dim3(64 * WAVES), bytes, st, a);
   return hipGetLastError();
 }
 

@@ -96,3 +96,25 @@ def test_a_captured_call_deals_by_the_lengths_of_each_replay(dtype, bits, B, m, 
         eager = c.attend(q, lens, S)
         torch.cuda.synchronize()
         assert torch.equal(got, eager), kind
+
+
+@pytest.mark.parametrize("bits", [0, 4])
+@pytest.mark.parametrize("B,m,Hq,Hkv,S,window,page_rows", [
+    (16, 70, 32, 8, 300, 0, 16), (17, 130, 16, 16, 400, 100, 0), (9, 300, 32, 8, 420, 130, 64), (3, 700, 64, 8, 900, 0, 256), (65, 40, 32, 4, 250, 50, 0)])
+def test_tiles_of_many_query_rows_in_whole_rounds_and_halves(B, m, Hq, Hkv, S, window, page_rows, bits):
+    """Chunks of prompts, some of them padded, one empty, one whose first tokens see nothing: as many tiles with rows as leave a round half empty, or full."""
+    print("case", B, m, Hq, Hkv, S, window, page_rows, bits, flush=True)
+    c = Case(B, Hq, Hkv, S, "bf16", page_rows, bits, seed=m)
+    q = c.queries(m)
+    for padded in (0.0, 0.3, 0.6, 0.95):
+        lens = last_tokens([S - (3 * b) % 40 for b in range(B)], m)
+        for b in range(B):
+            if padded:
+                lens[b, max(1, int(m * (1 - padded * ((b % 4) + 1) / 4))):] = 0
+        lens[1] = 0
+        lens[2] = last_tokens([m // 2], m)[0]
+        out = c.attend(q, lens, S, window, 3)
+        again = c.attend(q, lens, S, window, 3)
+        torch.cuda.synchronize()
+        assert torch.equal(out, again)
+        check(c, q, out, lens, window, 3, "bf16", {(0, 0), (2, Hkv - 1), (B - 1, Hkv // 2)})

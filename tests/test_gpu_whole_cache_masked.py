@@ -8,9 +8,9 @@ from tests.whole_cache import Case, reference, seen
 
 pytestmark = pytest.mark.gpu
 NAN, INF = float("nan"), float("inf")
-# (B, m, Hq, Hkv, S): up to 4, 8, 16, 32, 64, 128 and 256 query rows of a KV head, and several tiles of them; the one before the last reads 69 MB
+# (B, m, Hq, Hkv, S): up to 4, 8, 16, 32, 64, 128 and 256 query rows of a KV head, and several tiles of them, 69 MB and more read, and whole rounds of tiles
 SHAPES = [(2, 3, 2, 2, 300), (2, 2, 8, 2, 300), (1, 1, 8, 2, 2100), (2, 4, 8, 2, 2100), (2, 7, 8, 2, 700), (1, 16, 8, 2, 600), (1, 30, 8, 2, 500), (2, 60, 8, 2, 900), (1, 300, 4, 2, 700),
-          (4, 16, 32, 8, 4200), (1, 64, 8, 2, 5000)]
+          (4, 16, 32, 8, 4200), (1, 64, 8, 2, 5000), (16, 70, 32, 8, 300), (2, 1, 32, 8, 16500)]
 
 
 @pytest.mark.parametrize("dtype,bits", KINDS)
