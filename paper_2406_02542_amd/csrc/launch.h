@@ -314,8 +314,8 @@ struct SpanArgs {
   int halves;             // tiles of 256 rows without parts: blocks that are resident together, of which the last may take half a tile; 0: none does
 };
 // Blocks of the 4-bit kernels that a CU holds, by the registers of tiles of `rows` query rows.  us with more or fewer: 16 sequences of 32/8 bf16 heads up
-// to 16384 rows (4 rows) four 57.7, three 60.7; 64 of 64/8 up to 4096 (8) two 68.1, three 75.6; fp32, 16 of 8/8 up to 8000 (4) three 39.6, two
-// 43.0; 16 of 32/8 with 8000, four tokens (16) two 57.2, one 75.3.
+// to 16384 rows (4 rows) four 46.0, three 46.8; 64 of 64/8 with 4096 (8) two 73.9, three 75.8; fp32, 16 of 8/8 up to 8000 (4) three 31.5, two
+// 36.3; 16 of 32/8 with 8000, four tokens (16) two 49.6, one 69.5.
 __host__ __device__ constexpr int span_q4_waves(bool bf16, int rows) { return rows == 4 ? (bf16 ? 4 : 3) : 2; }
 // How a call is cut: the workspace's size and the launch go by it.
 struct SpanPlan {

@@ -450,17 +450,17 @@ static int span_splits(long long blocks, long long slots, long long most) {
   return n;
 }
 
-// Which kernel and how many blocks.  Tiles through LDS from 65 query rows of a KV head on, and from 33 on where more than 33 MB are read, us
-// 16 rows at a time / so: 1 x 64 tokens of 8/8 heads, window 512 9.1 / 14.9, 2 x 8 of 64/8, window 1000 13.7 / 17.5, 4000 (33 MB) 19.6 / 20.1, 8 x 16 of
-// 32/8 up to 8192 rows 92.5 / 54.1; with 32 query rows 8 x 4 of 64/8, window 1000 14.9 / 17.6, 2000 23.1 / 25.6, 8192 59.8 / 58.0; in 4 bits, 8192 rows, 8 x 8 tokens of
-// 64/8 (64 query rows) 79 / 91, 4 x 20 of 32/8 (80) 65.6 / 53.2, 4 x 64 of 32/8 (256) 143 / 92.
+// Which kernel and how many blocks.  Tiles through LDS from 65 query rows of a KV head on (in 4 bits from 81), and from 33 on where more than 33 MB
+// are read, us 16 rows at a time / so: 1 x 64 tokens of 8/8 heads, window 512 9.3 / 13.5, 2 x 8 of 64/8, window 1000 13.7 / 16.5, 4000 (33 MB) 19.3 / 19.9,
+// 8 x 16 of 32/8 up to 8192 rows 93.2 / 54.8; with 32 query rows 8 x 4 of 64/8, window 1000 15.9 / 18.6, 2000 22.4 / 24.2, 8192 60.1 / 57.5; in 4 bits, 8192
+// rows, 4 x 20 tokens of 32/8 (80 query rows) 54.0 / 52.9, of lengths from a quarter on 45.1 / 52.3, 4 x 32 (128) of such 72.8 / 54.7, 4 x 64 132 / 92.8.
 SpanPlan span_plan(const Shape& s, int m, int window, int sinks, bool bits4, bool short_rows) {
   SpanPlan p{};
   p.rows = 16;
   const long long M = (long long)m * s.G;
   const long long tokens_read = window > 0 ? (long long)window + m - 1 + sinks : s.S, most_read = tokens_read < s.S ? tokens_read : s.S;
   const double bytes = (double)s.B * s.Hkv * most_read * (2 * kD * s.elem_bytes);
-  const bool lds = s.dtype == 1 && (M > 64 || (!bits4 && M > 32 && bytes > 33e6 && !short_rows));
+  const bool lds = s.dtype == 1 && (M > (bits4 ? 80 : 64) || (!bits4 && M > 32 && bytes > 33e6 && !short_rows));
   if (lds)
     p.rows = M <= 64 ? 64 : M <= 128 ? 128 : 256;
   else if (bits4)

@@ -39,10 +39,10 @@ __device__ __forceinline__ float q4_times_step(float p, uint32_t scales) {
 //                   a place s = g % NS add up to each lane's own; the lanes of a query add theirs (DPP)
 //   second          for group g, column n holds p step_g if g is its own, else zeros: the outputs of CG groups share an accumulator too
 // so a lane scales and splits into terms only what its own groups ask: vector instructions for 32 rows of keys and values, of which 136 unpack
-// codes: CG = 4 280, 2 340, 1 430.  The scales go through the wave's own part of LDS: a load takes them for all of a step's rows, and no
-// lane holds 16 (CG = 4) to 64 registers of them while it waits; us in registers / LDS: 64 sequences of 64/8 heads with 4096 rows
+// codes: CG = 4 308, 2 356, 1 409.  The scales go through the wave's own part of LDS: a load takes them for all of a step's rows, and no
+// lane holds 16 (CG = 4) to 64 registers of them while it waits; us in registers / LDS (before runs were dealt by the lengths): 64 sequences of 64/8 heads with 4096 rows
 // (CG = 2) 78.3, 72.5, 16 of 64/8 with 8000 and two tokens (1) 65.6, 48.4, 16 of 32/8 with 16384 (4) 65.0, 63.5.  (16 rows' products for two groups
-// of queries at a time, which unpack codes half as often, leave a SIMD one wave: 50.6 us where these take 43.9.)
+// of queries at a time, which unpack codes half as often, leave a SIMD one wave: 50.6 us where these took 43.9.)
 // bf16: q is one term, the weights two (2^-16 of each, as the library's other attention); fp32: three each.
 template <typename T, int CG, bool STREAM, bool DEALT>
 __global__ __launch_bounds__(64 * kQ4Waves, span_q4_waves(T::EPC == 8, 16 / CG)) void span_q4_kernel(SpanArgs a) {
@@ -143,7 +143,7 @@ __global__ __launch_bounds__(64 * kQ4Waves, span_q4_waves(T::EPC == 8, 16 / CG))
 
   // The waves of a SIMD, of different blocks, are to end together: those that are behind go first.  (The oldest go first otherwise, and a SIMD is left
   // to the last one: blocks of equal work took 34 to 65 us where these take 49 to 61.)  us without / so: 16 sequences of 32/8 heads
-  // with 16384 rows 64.1 / 60.9, four tokens of 8 of 64/8 44.3 / 42.4.
+  // with 16384 rows 64.1 / 60.9, four tokens of 8 of 64/8 44.3 / 42.4 (each in equal parts).
   const int quarter = (s1 - s) >> 2, marks[3] = {s + quarter, s + 2 * quarter, s + 3 * quarter};
   __builtin_amdgcn_s_setprio(3);
   for (; s < s1; s += kQ4Waves) {
