@@ -113,8 +113,10 @@ __device__ __forceinline__ void store_q4(const float* row, int p, uint32_t* code
   for (int w = 0; w < W; ++w) codes[W * p + w] = word[w];
 }
 
-// STYLE and STREAM as rotary_kernel's.
-template <typename T, int STYLE, bool BITS4, bool STREAM>
+// STYLE as rotary_kernel's; LOADS and STORES: past the caches.  Stores past them are of whole lines: where a lane's chunks of a row leave holes, the row
+// goes through LDS in front of them; us through the caches / past them with holes / so: 16 x 512 tokens of 32/8 bf16 heads, 96 columns turned 47.3 / 57.9 /
+// 36.5, 64 46.6 / 44.4 / 36.3.
+template <typename T, int STYLE, bool BITS4, bool LOADS, bool STORES>
 __global__ __launch_bounds__(kApThreads) void append_kernel(AppendArgs args) {
   using ST = typename T::store_t;
   constexpr int EPC = T::EPC;
@@ -124,7 +126,9 @@ __global__ __launch_bounds__(kApThreads) void append_kernel(AppendArgs args) {
   constexpr int U = BITS4 ? 2 : 6;               // rows of a lane group in flight
   const RotaryArgs& a = args.r;
   __shared__ float2 s_cs[kApMaxTokens][kD / 2];
+  constexpr bool kLines = STYLE == 0 && STORES;
   __shared__ __align__(16) float s_row[BITS4 ? kGroups : 1][kD + 4];
+  __shared__ uint4 s_line[kLines ? kGroups : 1][kD / EPC];
   const int tid = threadIdx.x, p = tid % kLanes, gid = tid / kLanes;
   const int pairs = a.R / 2, tok0 = blockIdx.x * a.tokens, ntok = min(a.tokens, a.total - tok0);
   // this lane group's token, and its heads h0 + first, h0 + first + step, ..
@@ -153,8 +157,8 @@ __global__ __launch_bounds__(kApThreads) void append_kernel(AppendArgs args) {
       if (is_v) h -= Hkv;
       const RotaryTensor& x = is_q ? a.q : is_v ? a.v : a.k;
       src[u] = static_cast<const ST*>(x.in) + (b * x.in_batch + j * x.in_token + h * x.in_head);
-      raw[u][0] = load16_hint<STREAM>(src[u] + c0 * EPC);
-      raw[u][1] = load16_hint<STREAM>(src[u] + c1 * EPC);
+      raw[u][0] = load16_hint<LOADS>(src[u] + c0 * EPC);
+      raw[u][1] = load16_hint<LOADS>(src[u] + c1 * EPC);
     }
   };
   fetch(h0 + first);  // (before the angles, which they need not wait for; lane groups without a token take another's)
@@ -175,6 +179,7 @@ __global__ __launch_bounds__(kApThreads) void append_kernel(AppendArgs args) {
     if (STYLE == 0) cs[e] = s_cs[mine][max(0, min(c0 * EPC + e, pairs - 1))];
     if (STYLE == 1) cs[e] = s_cs[mine][max(0, min((e < EPC / 2 ? c0 : c1) * (EPC / 2) + e % (EPC / 2), pairs - 1))];
   }
+  const bool holes = kLines && a.R > 0 && a.R < kD;  // (uniform)
   const bool in_r = a.R > 0 && (STYLE != 0 || c1 * EPC < a.R);  // (STYLE 0: both chunks or none)
 
   for (int i0 = h0 + first; i0 < h1; i0 += step * U) {
@@ -237,8 +242,20 @@ __global__ __launch_bounds__(kApThreads) void append_kernel(AppendArgs args) {
         }
       }
       if (dst[u] != nullptr) {
-        store16_hint<STREAM>(dst[u] + c0 * EPC, pack_chunk<T>(y0));
-        store16_hint<STREAM>(dst[u] + c1 * EPC, pack_chunk<T>(y1));
+        uint4 z0 = pack_chunk<T>(y0), z1 = pack_chunk<T>(y1);
+        int at0 = c0, at1 = c1;
+        if (holes) {
+          at0 = p;
+          at1 = p + kLanes;
+          s_line[gid][c0] = z0;
+          s_line[gid][c1] = z1;
+          __builtin_amdgcn_wave_barrier();  // (the group's lanes are of one wave, whose LDS operations keep their order)
+          z0 = s_line[gid][at0];
+          z1 = s_line[gid][at1];
+          __builtin_amdgcn_wave_barrier();
+        }
+        store16_hint<STORES>(dst[u] + at0 * EPC, z0);
+        store16_hint<STORES>(dst[u] + at1 * EPC, z1);
       }
       if constexpr (BITS4) {
         if (at[u] >= 0) {  // (the same for the lanes of a group)
@@ -248,7 +265,7 @@ __global__ __launch_bounds__(kApThreads) void append_kernel(AppendArgs args) {
             *reinterpret_cast<float4*>(mid + c0 * EPC + e) = make_float4(y0[e], y0[e + 1], y0[e + 2], y0[e + 3]);
             *reinterpret_cast<float4*>(mid + c1 * EPC + e) = make_float4(y1[e], y1[e + 1], y1[e + 2], y1[e + 3]);
           }
-          __builtin_amdgcn_wave_barrier();  // (the group's lanes are of one wave, whose LDS operations keep their order)
+          __builtin_amdgcn_wave_barrier();
           store_q4<kLanes>(mid, p, static_cast<uint32_t*>(is_v[u] ? args.cache.v : args.cache.k) + at[u] * kQ4Words,
                            static_cast<uint32_t*>(is_v[u] ? args.cache.v_scales : args.cache.k_scales) + at[u] * kQ4Groups);
           __builtin_amdgcn_wave_barrier();
@@ -259,15 +276,15 @@ __global__ __launch_bounds__(kApThreads) void append_kernel(AppendArgs args) {
   }
 }
 
-template <typename T, bool BITS4, bool STREAM>
+template <typename T, bool BITS4, bool LOADS, bool STORES>
 static hipError_t launch_append_t(const AppendArgs& a, dim3 grid, int style, hipStream_t st) {
   const dim3 block(kApThreads);
   if (style == 0)
-    hipLaunchKernelGGL((append_kernel<T, 0, BITS4, STREAM>), grid, block, 0, st, a);
+    hipLaunchKernelGGL((append_kernel<T, 0, BITS4, LOADS, STORES>), grid, block, 0, st, a);
   else if (style == 1)
-    hipLaunchKernelGGL((append_kernel<T, 1, BITS4, STREAM>), grid, block, 0, st, a);
+    hipLaunchKernelGGL((append_kernel<T, 1, BITS4, LOADS, STORES>), grid, block, 0, st, a);
   else
-    hipLaunchKernelGGL((append_kernel<T, 2, BITS4, false>), grid, block, 0, st, a);
+    hipLaunchKernelGGL((append_kernel<T, 2, BITS4, false, false>), grid, block, 0, st, a);
   return hipGetLastError();
 }
 
@@ -289,9 +306,15 @@ hipError_t launch_append(const Shape& s, AppendArgs args, hipStream_t st) {
   }
   const dim3 grid((a.total + a.tokens - 1) / a.tokens, (heads + a.heads_per_block - 1) / a.heads_per_block);
   const int style = a.interleaved ? 1 : (a.R / 2) % epc == 0 ? 0 : 2;
-  // From 100 MB read and written on, past the caches (as launch_rotary), but for codes and scales, which are written piece by piece.
-  const bool past = 2.0 * a.total * heads * kD * s.elem_bytes >= 100e6;
-#define LOKI_APPEND(T, BITS4) return past ? launch_append_t<T, BITS4, true>(args, grid, style, st) : launch_append_t<T, BITS4, false>(args, grid, style, st)
+  // From 100 MB read and written on, rows are stored past the caches (but for codes and scales, which are written piece by piece); from 90 MB of rows on
+  // they are loaded past them, but for half lines: us through / past: 4 x 1111 tokens of 32/8 bf16 heads into 4 bits (55 MB) with their rows read
+  // back 27.1 / 32.8, 16 x 512 (101 MB) 62.4 / 56.9; into bf16, 8 x 2048 (201 MB) 70.2 / 68.4, 16 x 512 36.1 / 36.6, 96 columns turned 36.5 / 41.6.
+  const double bytes = (double)a.total * heads * kD * s.elem_bytes;
+  const bool holes = style == 0 && a.R > 0 && a.R < kD, stores = 2.0 * bytes >= 100e6, loads = bytes >= kPastBytes && (bits4 || !holes);
+#define LOKI_APPEND(T, BITS4)                                                              \
+  return loads    ? launch_append_t<T, BITS4, true, true>(args, grid, style, st)           \
+         : stores ? launch_append_t<T, BITS4, false, true>(args, grid, style, st)          \
+                  : launch_append_t<T, BITS4, false, false>(args, grid, style, st)
   if (bits4) {
     if (s.dtype == 0) LOKI_APPEND(F32, true);
     LOKI_APPEND(BF16, true);

@@ -148,7 +148,8 @@ def test_codes_and_scales_are_those_of_the_definition(dtype):
 
 
 @pytest.mark.parametrize("bits", [0, 4])
-@pytest.mark.parametrize("dtype,B,n,Hq,Hkv,R,interleaved", [("bf16", 6, 1300, 32, 8, 128, False), ("f32", 3, 1100, 32, 8, 64, True), ("bf16", 7, 1030, 32, 8, 20, False)])
+@pytest.mark.parametrize("dtype,B,n,Hq,Hkv,R,interleaved", [("bf16", 6, 1300, 32, 8, 128, False), ("f32", 3, 1100, 32, 8, 64, True), ("bf16", 7, 1030, 32, 8, 20, False),
+                                                               ("bf16", 6, 1100, 32, 8, 96, False), ("bf16", 9, 1000, 32, 8, 16, False), ("f32", 3, 1100, 32, 8, 48, False)])
 def test_large_appends(dtype, B, n, Hq, Hkv, R, interleaved, bits):
     """Enough for rows past the caches."""
     x = Tokens(B, n, Hq, Hkv, dtype, R, 100000)
