@@ -798,12 +798,13 @@ class Cache:
         self.k = k
         self.args = CacheArgs(*(None if t is None else t.data_ptr() for t in self.tensors), rows, per_seq, pages)
         self.shape = (B, H, layout.S_cap, layout.dtype)
+        self.ref = ctypes.byref(self.args)
 
     def _of(self, layout: Layout):
         if self.shape != (layout.B, layout.Hkv, layout.S_cap, layout.dtype):
             raise ValueError(f"the cache is one of (B, Hkv, S_cap, dtype) = {self.shape}")
         _on_current_device(self.k, "cache")
-        return ctypes.byref(self.args)
+        return self.ref
 
 
 def alloc_whole_cache(layout: Layout, four_bits: bool = False, page_table: Optional[torch.Tensor] = None, page_rows: int = 0,
@@ -817,16 +818,23 @@ def alloc_whole_cache(layout: Layout, four_bits: bool = False, page_table: Optio
                  make((4, 2), torch.float16), page_table=page_table)
 
 
-def _strided(name: str, x: torch.Tensor, shape, dt: torch.dtype):
-    """(pointer, three strides) of x [B, n, heads, D], rows of whole columns."""
+def _refuse_strided(name: str, x: torch.Tensor, shape, dt: torch.dtype):
     if not x.is_cuda:
         raise ValueError(f"{name} must live on the GPU")
     if x.dtype is not dt or x.shape != shape:
         raise ValueError(f"{name} must be {list(shape)} of {dt}, got {tuple(x.shape)} of {x.dtype}")
-    b, t, h, c = x.stride()
-    if c != 1:
-        raise ValueError(f"{name}: the columns of a row must be next to each other")
-    return x.data_ptr(), b, t, h
+    raise ValueError(f"{name}: the columns of a row must be next to each other")
+
+
+def _strided(names, x: torch.Tensor, y: torch.Tensor, shape, dt: torch.dtype):
+    """(pointer, strides of a batch, a token and a head) of x, and of y, [B, n, heads, D], rows of whole columns."""
+    if x.is_cuda and y.is_cuda and x.dtype is dt and y.dtype is dt and x.shape == shape and y.shape == shape:
+        xb, xt, xh, xc = x.stride()
+        yb, yt, yh, yc = y.stride()
+        if xc == 1 and yc == 1:
+            return x.data_ptr(), xb, xt, xh, y.data_ptr(), yb, yt, yh
+    x_right = x.is_cuda and x.dtype is dt and x.shape == shape and x.stride(3) == 1
+    _refuse_strided(names[x_right], (x, y)[x_right], shape, dt)
 
 
 def loki_append(layout: Layout, cache: Cache, rows: torch.Tensor, k: torch.Tensor, v: torch.Tensor,
@@ -843,19 +851,15 @@ def loki_append(layout: Layout, cache: Cache, rows: torch.Tensor, k: torch.Tenso
         raise ValueError("q and q_out come together")
     if (positions is None) != (frequencies is None):
         raise ValueError("positions and frequencies come together")
-    shape = (B, n, layout.Hkv, 128)
-    kp, vp = _strided("k", k, shape, dt), _strided("v", v, shape, dt)
-    qs = _NOT_THERE
+    kp, kb, kt, kh, vp, vb, vt, vh = _strided(("k", "v"), k, v, (B, n, layout.Hkv, 128), dt)
+    qp = qb = qt = qh = op = ob = ot = oh = pos = freq = R = 0
     if q is not None:
-        q_shape = (B, n, layout.Hq, 128)
-        qi, qo = _strided("q", q, q_shape, dt), _strided("q_out", q_out, q_shape, dt)
-        qs = (qi[0], qo[0]) + qi[1:] + qo[1:]
-    pos = freq = R = 0
+        qp, qb, qt, qh, op, ob, ot, oh = _strided(("q", "q_out"), q, q_out, (B, n, layout.Hq, 128), dt)
     if frequencies is not None:
         pos, freq = _ptr(positions, "positions", torch.int32, B * n), _ptr(frequencies, "frequencies", torch.float64, 1)
         R = 2 * frequencies.numel()
-    args = _rotary_pack(*qs, kp[0], 0, *kp[1:], 0, 0, 0, vp[0], 0, *vp[1:], 0, 0, 0, pos, _ptr(rows, "rows", torch.int32), freq,
-                        0, R, interleaved, inverse, scale)
+    args = _rotary_pack(qp, op, qb, qt, qh, ob, ot, oh, kp, 0, kb, kt, kh, 0, 0, 0, vp, 0, vb, vt, vh, 0, 0, 0, pos,
+                        _ptr(rows, "rows", torch.int32), freq, 0, R, interleaved, inverse, scale)
     cache_args = cache._of(layout)
     _on_current_device(rows, "rows")
     _check(lib().loki_append(ctypes.byref(layout), cache_args, n, args, _stream_ptr(stream)), "loki_append")

@@ -1061,9 +1061,10 @@ static int check_span(const loki_layout* layout, const loki_cache* cache, int S_
 // Behind the control words, which the call leaves alone (plan_workspace): which runs the tiles have, and the parts.
 static size_t span_dealt_bytes(const SpanPlan& p) { return align_up(p.dealt * sizeof(int2), 256); }
 static size_t span_bytes(const SpanPlan& p) { return kClusterCtlBytes + span_dealt_bytes(p) + align_up(p.parts * kPartStride * sizeof(float), 256); }
-static size_t span_bytes(const Shape& s, const SpanArgs& a) {
-  const bool bits4 = a.cache.k_scales != nullptr;
-  const size_t x = span_bytes(span_plan(s, a.m, a.window, a.sinks, bits4)), y = span_bytes(span_plan(s, a.m, a.window, a.sinks, bits4, true));
+static size_t span_bytes(const Shape& s, const SpanArgs& a, const SpanPlan& plan) {
+  const size_t x = span_bytes(plan), M = (size_t)a.m * s.G;
+  if (a.cache.k_scales != nullptr || M <= 32 || M > 64) return x;  // (the only ones that are cut another way with fewer rows)
+  const size_t y = span_bytes(span_plan(s, a.m, a.window, a.sinks, false, true));
   return x > y ? x : y;
 }
 
@@ -1073,7 +1074,7 @@ int dense_cache_workspace_bytes(const loki_layout* layout, const loki_cache* cac
   const int rc = check_span(layout, cache, S_max, args, &s, &a);
   if (rc != LOKI_OK) return rc;
   if (!bytes) return LOKI_ERR_INVALID_ARG;
-  *bytes = span_bytes(s, a);
+  *bytes = span_bytes(s, a, span_plan(s, a.m, a.window, a.sinks, a.cache.k_scales != nullptr));
   return LOKI_OK;
 }
 
@@ -1085,10 +1086,10 @@ int dense_decode_cache(const loki_layout* layout, const void* q, const loki_cach
   if (rc != LOKI_OK) return rc;
   if (!q || !out || !workspace) return LOKI_ERR_INVALID_ARG;
   if (!aligned16(q) || !aligned16(out) || !aligned256(workspace)) return LOKI_ERR_ALIGNMENT;
-  if (span_bytes(s, a) > workspace_bytes) return LOKI_ERR_WORKSPACE;
+  const SpanPlan plan = span_plan(s, a.m, a.window, a.sinks, a.cache.k_scales != nullptr);
+  if (span_bytes(s, a, plan) > workspace_bytes) return LOKI_ERR_WORKSPACE;
   a.q = q;
   a.out = out;
-  const SpanPlan plan = span_plan(s, a.m, a.window, a.sinks, a.cache.k_scales != nullptr);
   a.dealt = plan.cap > 0 && a.lens != nullptr ? reinterpret_cast<int2*>(static_cast<char*>(workspace) + kClusterCtlBytes) : nullptr;
   a.partial = reinterpret_cast<float*>(static_cast<char*>(workspace) + kClusterCtlBytes + span_dealt_bytes(plan));
   hipStream_t st = static_cast<hipStream_t>(stream);

@@ -6,6 +6,8 @@
 // values go through LDS for all of the block's query rows.
 #include "span_tiles_impl.h"
 
+#include <cmath>
+
 namespace loki {
 
 constexpr int kSpWaves = 4;
@@ -436,15 +438,19 @@ __global__ __launch_bounds__(256) void span_merge_kernel(SpanArgs a) {
 // 13 sequences of 32/8 bf16 heads with 4000 rows 49.2 / 42.3, 5 of 24 51.8 / 45.9, in 4 bits 24.3 / 21.4, 700 tokens of 32/8 behind 8192 rows 207 / 175; but
 // where lengths leave some of the blocks without rows, 5 of 24 fp32 heads up to 2311 in 4 bits 17.4 / 18.4.  Never fewer for more rows.
 static int span_splits(long long blocks, long long slots, long long most) {
-  const long long fill = (slots + blocks - 1) / blocks, top = 3 * fill < most ? 3 * fill : most;
   if (blocks >= 2 * slots) return 1;
+  const double share = (double)slots / (double)blocks;
   double best = 1e30;
   int n = 1;
-  for (long long i = 1; i <= top; ++i) {
-    const double cost = (double)((blocks * i + slots - 1) / slots) / (double)i + 0.03 * (double)((i - 1) * blocks) / (double)slots;
+  for (int rounds = 1; rounds <= 3; ++rounds) {
+    double parts = floor(rounds * share);
+    if (parts > sqrt(rounds * share / 0.03)) parts = floor(sqrt(rounds * share / 0.03));  // (where one more costs what it gains)
+    if (parts > (double)most) parts = (double)most;
+    if (parts < 1.0) continue;
+    const double cost = rounds / parts + 0.03 * (parts - 1.0) / share;
     if (cost < best) {
       best = cost;
-      n = (int)i;
+      n = (int)parts;
     }
   }
   return n;
