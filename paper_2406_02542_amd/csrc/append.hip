@@ -6,6 +6,8 @@
 // out once, into LDS, and lane groups take heads of one token in turn.  Memory bounds it.
 // In 4 bits the turned row goes through LDS in 32 bits, from the lanes that hold pairs to the lanes that hold words, and is rounded
 // once, to its code.
+// 8 x up to 2048 tokens of 32/8 bf16 heads (369 MB) 68 us, 5.4 TB/s, 16 x 512 (201 MB) 36 us; 4 x up to 1111 into 4 bits, half of the columns turned 21.7 us (105 MB);
+// one token 4.9 us, a launch.
 #include "cache_impl.h"
 #include "rotary_impl.h"
 
@@ -291,7 +293,7 @@ static hipError_t launch_append_t(const AppendArgs& a, dim3 grid, int style, hip
 hipError_t launch_append(const Shape& s, AppendArgs args, hipStream_t st) {
   RotaryArgs& a = args.r;
   const int epc = 16 / s.elem_bytes, heads = a.q.heads + 2 * s.Hkv;
-  // few tokens: the heads of a token are spread over blocks (as launch_rotary).  In 4 bits, us with 4 rows of a lane group in flight and 4 tokens a
+  // few tokens: the heads of a token are spread over blocks (as launch_rotary).  In 4 bits, us (loading past the caches) with 4 rows of a lane group in flight and 4 tokens a
   // block, 4 and 2, 2 and 2, 2 and 4, 3 and 1: 4 x 1111 tokens of 32/8 bf16 heads 36.6, 33.7, 33.2, 33.1, 41.6, 2 x 512 15.9, 13.5, 13.4, 15.1, 13.4.
   const bool bits4 = args.cache.k_scales != nullptr;
   const int tokens = s.dtype == 0 || bits4 ? 2 : kApMaxTokens;
@@ -325,7 +327,8 @@ hipError_t launch_append(const Shape& s, AppendArgs args, hipStream_t st) {
 }
 
 // ---- rows of a cache back --------------------------------------------------------------------------------------
-// 16 lanes take a row: in 4 bits a word each, so a store instruction takes the pairs of one group of 4 rows; else 16-byte chunks.
+// 16 lanes take a row: in 4 bits a word each, so a store instruction takes the pairs of one group of 4 rows; else 16-byte chunks.  Memory bounds it: 4 x up to 1111
+// rows of 8 heads out of 4 bits (20 MB) 5.8 us.
 template <typename T, bool BITS4>
 __global__ __launch_bounds__(256) void read_rows_kernel(CacheView c, const int32_t* __restrict__ rows, int B, int n, int Hkv,
                                                         typename T::store_t* __restrict__ k_out, typename T::store_t* __restrict__ v_out) {
