@@ -286,7 +286,7 @@ static hipError_t launch_append_t(const AppendArgs& a, dim3 grid, int style, hip
   else if (style == 1)
     hipLaunchKernelGGL((append_kernel<T, 1, BITS4, LOADS, STORES>), grid, block, 0, st, a);
   else
-    hipLaunchKernelGGL((append_kernel<T, 2, BITS4, false, false>), grid, block, 0, st, a);
+    hipLaunchKernelGGL((append_kernel<T, 2, BITS4, false, STORES>), grid, block, 0, st, a);
   return hipGetLastError();
 }
 

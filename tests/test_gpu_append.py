@@ -305,3 +305,46 @@ def test_queries_turned_in_place(interleaved, R, dtype, bits):
     assert torch.equal(q, q_out)
     for x, y in zip(caches[0].tensors[:4], caches[1].tensors[:4]):
         assert x is None or torch.equal(x, y)
+
+
+@pytest.mark.parametrize("bits", [0, 4])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("n", [1, 40])
+def test_captured_with_other_rows_positions_and_pages_at_each_replay(n, dtype, bits):
+    """Appends and reads of a graph that is replayed, on a stream of their own, give what the same calls give one by one."""
+    B, Hq, H, S = 3, 8, 2, 200
+    gen = torch.Generator(device="cuda").manual_seed(n)
+    lay = api.make_layout(B, Hq, H, 128, 128, S, DT[dtype])
+    table, n_pages = make_table(B, S, 16, gen)
+    t = Tokens(B, n, Hq, H, dtype, 64, 3000)
+    rows = torch.zeros((B, n), dtype=torch.int32, device="cuda")
+
+    def state():
+        cache = api.alloc_whole_cache(lay, bits == 4, table, 16, n_pages)
+        return cache, torch.zeros_like(t.q), [torch.zeros((B, H, n, 128), dtype=DT[dtype], device="cuda") for _ in "kv"]
+
+    def call(s, stream=None):
+        api.loki_append(lay, s[0], rows, t.k, t.v, q=t.q, q_out=s[1], stream=stream, **t.rot)
+        api.loki_read_rows(lay, s[0], rows, *s[2], stream=stream)
+
+    mine, other = state(), state()
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=side):
+        call(mine, side)
+    torch.cuda.synchronize()
+    for i in range(4):
+        for b in range(B):
+            rows[b] = torch.randperm(S, generator=gen, device="cuda")[:n].int()
+        rows[i % B, n // 2:] = -1
+        t.positions.copy_(torch.randint(0, 100000, (B, n), generator=gen, device="cuda", dtype=torch.int32))
+        t.k.normal_(generator=gen)
+        table.copy_(table.flatten()[torch.randperm(table.numel(), generator=gen, device="cuda")].view_as(table))
+        graph.replay()
+        torch.cuda.synchronize()
+        call(other)
+        torch.cuda.synchronize()
+        assert torch.equal(mine[1], other[1])
+        for x, y in zip((*mine[0].tensors[:4], *mine[2]), (*other[0].tensors[:4], *other[2])):
+            assert x is None or torch.equal(x, y)
