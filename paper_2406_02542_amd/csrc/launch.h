@@ -312,6 +312,7 @@ struct SpanArgs {
   int nsplit, run;        // runs of a tile, of `run` rows
   int cap;                // runs of a KV head that are resident together
   int halves;             // tiles of 256 rows without parts: blocks that are resident together, of which the last may take half a tile; 0: none does
+  int halves_all;         // there are blocks for halves of all tiles
 };
 // Blocks of the 4-bit kernels that a CU holds, by the registers of tiles of `rows` query rows.  us with more or fewer: 16 sequences of 32/8 bf16 heads up
 // to 16384 rows (4 rows) four 46.0, three 46.8; 64 of 64/8 with 4096 (8) two 73.9, three 75.8; fp32, 16 of 8/8 up to 8000 (4) three 31.5, two

@@ -373,7 +373,7 @@ __global__ __launch_bounds__(256) void span_merge_kernel(SpanArgs a) {
   if constexpr (DEALT) {
     const int per = a.m * a.Hq, b = r / per, j = (r - b * per) / a.Hq, head = r - b * per - j * a.Hq, h = head >> (31 - __builtin_clz(a.G));
     const int row = j * a.G + (head & (a.G - 1)), tile = row >> (31 - __builtin_clz(a.rows));
-    const int2 dealt = a.dealt[b * a.tiles + a.tiles - 1 - tile];
+    const int2 dealt = a.dealt[span_tile_index(a, b, tile)];
     nsplit = dealt.y;
     if (nsplit == 1) return;  // (written already)
     between = (long long)a.Hkv * a.rows * kPartStride;
@@ -539,7 +539,8 @@ hipError_t launch_span(const Shape& s, SpanArgs a, const SpanPlan& plan, hipStre
   a.cap = plan.cap;
   a.halves = plan.halves;
   const int tiles = a.B * a.tiles, runs = a.dealt != nullptr ? a.cap : tiles * a.nsplit;
-  const unsigned blocks = (unsigned)((long long)runs * a.Hkv) + a.halves / 2;
+  a.halves_all = a.halves > 0 && a.window == 0x7fffffff && runs * a.Hkv < 2 * a.halves;  // (only tiles that see all rows differ that much)
+  const unsigned blocks = (unsigned)((long long)runs * a.Hkv) + (a.halves_all ? runs * a.Hkv : a.halves / 2);
   const dim3 grid(blocks), block(64 * kSpWaves);
   hipError_t e = hipSuccess;
   if (bits4)

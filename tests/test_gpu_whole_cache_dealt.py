@@ -100,7 +100,7 @@ def test_a_captured_call_deals_by_the_lengths_of_each_replay(dtype, bits, B, m, 
 
 @pytest.mark.parametrize("bits", [0, 4])
 @pytest.mark.parametrize("B,m,Hq,Hkv,S,window,page_rows", [
-    (16, 70, 32, 8, 300, 0, 16), (17, 130, 16, 16, 400, 100, 0), (9, 300, 32, 8, 420, 130, 64), (3, 700, 64, 8, 900, 0, 256), (65, 40, 32, 4, 250, 50, 0)])
+    (16, 70, 32, 8, 300, 0, 16), (17, 130, 16, 16, 400, 100, 0), (9, 300, 32, 8, 420, 130, 64), (3, 700, 64, 8, 900, 0, 256), (65, 40, 32, 4, 250, 50, 0), (4, 520, 32, 16, 520, 0, 64)])
 def test_tiles_of_many_query_rows_in_whole_rounds_and_halves(B, m, Hq, Hkv, S, window, page_rows, bits):
     """Chunks of prompts, some of them padded, one empty, one whose first tokens see nothing: as many tiles with rows as leave a round half empty, or full."""
     print("case", B, m, Hq, Hkv, S, window, page_rows, bits, flush=True)
