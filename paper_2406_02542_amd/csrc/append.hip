@@ -29,14 +29,11 @@ __device__ __forceinline__ RowTarget row_target(const CacheView& c, int b, int H
 }
 
 // Code of x: the quotient's nearest whole number, the even one half-way.  A product with the rounded reciprocal is off by less than 2^-18 there, and
-// what it leaves of x - lowest, exact but for one rounding, says on which side of half a step that was.
+// what it leaves of x - lowest, which 64 bits hold exactly, says on which side of half a step that was.
 __device__ __forceinline__ uint32_t q4_code(float x, float low, float step, float inv) {
-  const float t = x - low;
-  float n = rintf(t * inv);
-  const float rest = fmaf(-n, step, t), half = 0.5f * step;
-  const bool odd = ((int)n & 1) != 0;
-  if (rest > half || (rest == half && odd)) n += 1.f;
-  if (rest < -half || (rest == -half && odd)) n -= 1.f;
+  float n = rintf((x - low) * inv);
+  const double rest = fma(-(double)n, (double)step, (double)x - (double)low), over = fabs(rest) - 0.5 * (double)step;
+  if (over > 0.0 || (over == 0.0 && ((int)n & 1) != 0)) n += copysignf(1.f, (float)rest);
   return step > 0.f ? (uint32_t)fminf(fmaxf(n, 0.f), 15.f) : 0u;
 }
 
@@ -98,7 +95,7 @@ __device__ __forceinline__ void store_q4(const float* row, int p, uint32_t* code
     lo = -group_allreduce_max<LANES>(-lo);
     hi = group_allreduce_max<LANES>(hi);
     // (a range past fp16's is clamped to its largest)
-    cache_half2_t sc = {(_Float16)fminf((hi - lo) / 15.f, 65504.f), (_Float16)fminf(fmaxf(lo, -65504.f), 65504.f)};
+    cache_half2_t sc = {(_Float16)fminf((hi - lo) * (1.0f / 15.0f), 65504.f), (_Float16)fminf(fmaxf(lo, -65504.f), 65504.f)};
     if (any) {  // (uniform) a group with such a value stands for no numbers
       bool own = false;
 #pragma unroll

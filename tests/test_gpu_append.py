@@ -348,3 +348,34 @@ def test_captured_with_other_rows_positions_and_pages_at_each_replay(n, dtype, b
         assert torch.equal(mine[1], other[1])
         for x, y in zip((*mine[0].tensors[:4], *mine[2]), (*other[0].tensors[:4], *other[2])):
             assert x is None or torch.equal(x, y)
+
+
+def test_codes_next_to_their_borders():
+    """Values half-way between two codes, and the fp32 numbers next to those: the codes are those of 64 bits, whatever the lowest value is."""
+    n, H = 512, 4
+    gen = torch.Generator(device="cuda").manual_seed(3)
+    lay = api.make_layout(1, H, H, 128, 128, n, torch.float32)
+    rows = torch.arange(n, dtype=torch.int32, device="cuda")[None]
+    k = torch.randn((1, n, H, 128), generator=gen, device="cuda") * torch.exp(3 * torch.randn((1, n, H, 1), generator=gen, device="cuda"))
+    k += 20 * torch.randn((1, n, H, 1), generator=gen, device="cuda") * (torch.rand((1, n, H, 1), generator=gen, device="cuda") < 0.3)
+    cache = api.alloc_whole_cache(lay, four_bits=True)
+    api.loki_append(lay, cache, rows, k, k)
+    torch.cuda.synchronize()
+    scales = cache.tensors[2].double().transpose(1, 2)  # [1, n, H, 4, 2]
+    step, low = scales[..., :1], scales[..., 1:]
+    g = k.unflatten(-1, (4, 32)).clone()
+    lo, hi = g.amin(-1, True), g.amax(-1, True)
+    at = torch.randint(0, 15, g.shape, generator=gen, device="cuda") + 0.5
+    near = (low + at * step).float()
+    for _ in range(3):  # up to three fp32 numbers off, in either direction
+        move = torch.randint(-1, 2, g.shape, generator=gen, device="cuda")
+        near = torch.where(move == 0, near, torch.nextafter(near, torch.where(move > 0, 1e30, -1e30).float()))
+    keep = (g == lo) | (g == hi)  # the group's lowest and largest stay, and with them its scales
+    g = torch.where(keep, g, torch.minimum(torch.maximum(near, lo), hi))
+    k2 = g.flatten(-2).contiguous()
+    api.loki_append(lay, cache, rows, k2, k2)
+    torch.cuda.synchronize()
+    assert torch.equal(cache.tensors[2].double().transpose(1, 2), scales)
+    want = torch.where(step > 0, torch.round((g.double() - low) / torch.where(step > 0, step, 1.0)), 0.0).clamp(0, 15).long().flatten(-2)
+    for t in cache.tensors[:2]:
+        assert torch.equal(unpack(t).transpose(1, 2), want)
