@@ -486,8 +486,9 @@ int loki_read_rows(const loki_layout* layout, const loki_cache* cache, int n, co
  *   workspace   >= dense_cache_workspace_bytes(layout, cache, S_max, args), 256-byte aligned; a workspace sized for an S_max also
  *               serves shorter ones, with the same args
  * Rows that no token sees, before the window or behind the end, are not read, and their pages' entries may be any (entries that are
- * read are clamped into [0, n_pages)).  What a token does not see does not reach its output, whatever it holds; a value that it sees and that is no
- * finite number makes that column (in 4 bits, such a step or lowest the group's columns) of its output NaN or infinite, such a key all of it.  m may be thousands (a chunk of prompts): B m <= 2^24, B m Hq <= 2^27.
+ * read are clamped into [0, n_pages)).  What a token does not see does not reach its output, whatever it holds; a value that it sees and
+ * that is no finite number makes that column (in 4 bits, such a step or lowest the group's columns) of its output NaN or infinite, such a
+ * key all of it.  m may be thousands (a chunk of prompts): B m <= 2^24, B m Hq <= 2^27.
  */
 typedef struct {
   const int32_t* seq_lens;

@@ -238,7 +238,7 @@ __device__ __forceinline__ SpanTile span_tile(const SpanArgs& a) {
     span_tile_at(a, at, t.b, t.tile);
     each = (a.run + KEYS - 1) / KEYS;
   } else {
-    constexpr int kUnit = KEYS >= 64 ? 1 : 4;  // steps of a run: a multiple of the waves that take them in turn, and at least 128 rows
+    constexpr int kUnit = 4;  // steps of a run: a multiple of the waves that take them in turn, and at least 128 rows
     const int lane = threadIdx.x & 63, all = a.B * a.tiles;  // (up to 64)
     int b, tile, n = 0, most, least;
     span_tile_at(a, min(lane, all - 1), b, tile);
