@@ -156,7 +156,8 @@ __global__ __launch_bounds__(64 * kSpWaves) void span_rows_kernel(SpanArgs a) {
   }
   l += __shfl_xor(l, 16);
   l += __shfl_xor(l, 32);
-  if (len == 0) {  // (a padded token's lanes took whatever full steps gave)
+  if (len == 0) {  // (a padded token's lanes took whatever full steps gave: a maximum too, which may be infinite)
+    m = kNegBig;
     l = 0.f;
 #pragma unroll
     for (int c = 0; c < 8; ++c) o[c] = am_f32x4_t{};
@@ -341,6 +342,7 @@ __global__ __launch_bounds__(64 * kSpWaves, 2) void span_f32_kernel(SpanArgs a) 
     l[g] += __shfl_xor(l[g], 16);
     l[g] += __shfl_xor(l[g], 32);
     if (len[g] == 0) {
+      m[g] = kNegBig;
       l[g] = 0.f;
 #pragma unroll
       for (int c = 0; c < 8; ++c) o[g][c] = pf_f32x4_t{};

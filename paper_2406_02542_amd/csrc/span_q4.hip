@@ -286,7 +286,8 @@ __global__ __launch_bounds__(64 * kQ4Waves, span_q4_waves(T::EPC == 8, 16 / CG))
   }
   l += __shfl_xor(l, 16);
   l += __shfl_xor(l, 32);
-  if (len == 0) {  // (a padded token's lanes took whatever full steps gave)
+  if (len == 0) {  // (a padded token's lanes took whatever full steps gave: a maximum too, which may be infinite)
+    m = kNegBig;
     l = 0.f;
 #pragma unroll
     for (int n = 0; n < NS; ++n) {

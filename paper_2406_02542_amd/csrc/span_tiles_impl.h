@@ -319,7 +319,8 @@ __global__ __launch_bounds__(64 * WAVES, 2) void span_tiles_kernel(SpanArgs a) {
 
   // both halves of a query's keys; then the waves that had other keys of the same queries
   l += __shfl_xor(l, 32);
-  if (len == 0) {  // (a padded token's lanes took whatever full steps gave)
+  if (len == 0) {  // (a padded token's lanes took whatever full steps gave: a maximum too, which may be infinite)
+    m = kNegBig;
     l = 0.f;
 #pragma unroll
     for (int c = 0; c < 4; ++c) o[c] = sp_f32x16_t{};
