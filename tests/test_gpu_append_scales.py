@@ -1,0 +1,83 @@
+"""loki_append into 4 bits: steps and lowest values are those of the format's definition, bit for bit, and so are the codes."""
+import numpy as np
+import pytest
+import torch
+
+from paper_2406_02542_amd import api
+from tests.attention_bound import DT
+from tests.whole_cache import unpack
+
+pytestmark = pytest.mark.gpu
+
+
+def defined(x):
+    """(step, lowest) as fp16 [.., 4] and codes [.., 128] of fp32 numbers x [.., 128]: the range and its quotient in 32 bits, codes in 64."""
+    g = x.reshape(*x.shape[:-1], 4, 32)
+    lo, hi = g.min(-1), g.max(-1)
+    with np.errstate(over="ignore"):
+        step = np.minimum((hi - lo) / np.float32(15), np.float32(65504)).astype(np.float16)
+    low = np.clip(lo, np.float32(-65504), np.float32(65504)).astype(np.float16)
+    s, n = step.astype(np.float64)[..., None], low.astype(np.float64)[..., None]
+    codes = np.where(s > 0, np.clip(np.rint((g.astype(np.float64) - n) / np.where(s > 0, s, 1.0)), 0, 15), 0.0)
+    return step, low, codes.reshape(x.shape).astype(np.int64)
+
+
+def ranges(kind, n, rng):
+    """n ranges, fp32."""
+    if kind == "any":
+        return rng.uniform(0.01, 100.0, n)
+    if kind == "small":  # steps among fp16's smallest numbers, and below them
+        return np.exp2(rng.uniform(-24.0, -9.0, n))
+    if kind == "huge":
+        return np.exp2(rng.uniform(15.0, 21.0, n))
+    low = rng.uniform(0.01, 100.0, n).astype(np.float16)  # fifteenths half-way between two fp16 numbers, and next to that
+    half = (low.astype(np.float64) + np.nextafter(low, np.float16(np.inf)).astype(np.float64)) / 2
+    r = (15.0 * half).astype(np.float32)
+    move = rng.integers(-1, 2, n)
+    return np.where(move == 0, r, np.nextafter(r, np.where(move > 0, np.inf, -np.inf).astype(np.float32)))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("kind", ["any", "half-way", "small", "huge"])
+@pytest.mark.parametrize("lowest", [0.0, -1.0])
+def test_steps_and_lowest_values_are_the_quotients_of_the_definition(lowest, kind, dtype):
+    print("case", lowest, kind, dtype, flush=True)
+    n, H = 600, 8
+    rng = np.random.default_rng([3, int(lowest < 0), len(kind)])
+    r = np.asarray(ranges(kind, n * H * 4, rng), np.float32).reshape(n, H, 4, 1)
+    lo = (np.float32(lowest) * r * rng.uniform(0.0, 1.0, r.shape).astype(np.float32)).astype(np.float32)
+    x = lo + r * rng.uniform(0.0, 1.0, (n, H, 4, 32)).astype(np.float32)
+    x[..., 7], x[..., 21] = lo[..., 0], lo[..., 0] + r[..., 0]
+    x = torch.from_numpy(x.reshape(1, n, H, 128)).to(DT[dtype])
+    step, low, codes = defined(x.float().numpy())
+    lay = api.make_layout(1, H, H, 128, 128, n, DT[dtype])
+    cache = api.alloc_whole_cache(lay, four_bits=True)
+    rows = torch.arange(n, dtype=torch.int32, device="cuda")[None]
+    x = x.cuda()
+    api.loki_append(lay, cache, rows, x, x.flip(1).contiguous())
+    torch.cuda.synchronize()
+    for i in range(2):
+        words, scales = (t.transpose(1, 2) for t in (cache.tensors[i], cache.tensors[2 + i]))
+        if i:
+            words, scales = words.flip(1), scales.flip(1)
+        scales = scales.cpu().numpy()
+        assert int((scales[..., 0] != step).sum()) == 0
+        assert int((scales[..., 1] != low).sum()) == 0
+        assert int((unpack(words).cpu().numpy() != codes).sum()) == 0
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_infinite_values_take_the_largest_steps_and_lowest_values(dtype):
+    """Groups with an infinity of either sign, of infinities alone, of both."""
+    x = torch.linspace(-2.0, 2.0, 128).repeat(1, 1, 4, 1)
+    x[0, 0, 0, 40], x[0, 0, 1, 3], x[0, 0, 2, 96:], x[0, 0, 3, 64:66] = float("inf"), -float("inf"), float("inf"), torch.tensor([float("inf"), -float("inf")])
+    x = x.to(DT[dtype]).cuda()
+    lay = api.make_layout(1, 4, 4, 128, 128, 1, DT[dtype])
+    cache = api.alloc_whole_cache(lay, four_bits=True)
+    api.loki_append(lay, cache, torch.zeros((1, 1), dtype=torch.int32, device="cuda"), x, x)
+    torch.cuda.synchronize()
+    scales, codes = cache.tensors[2][0, :, 0].float(), unpack(cache.tensors[0])[0, :, 0]
+    assert scales[0, 1].tolist() == [65504.0, float(x[0, 0, 0, 32].half())] and int(codes[0, 40]) == 15 and int(codes[0, 32]) == 0
+    assert scales[1, 0].tolist() == [65504.0, -65504.0] and int(codes[1, 3]) == 0 and int(codes[1, 4]) == 1
+    assert scales[2, 3].tolist() == [65504.0, 65504.0] and codes[2, 96:].unique().tolist() == [15]
+    assert scales[3, 2].tolist() == [65504.0, -65504.0] and codes[3, 64:67].tolist() == [15, 0, 1]
