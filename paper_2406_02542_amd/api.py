@@ -224,6 +224,28 @@ def _on_current_device(t: torch.Tensor, name: str) -> None:
         raise ValueError(f"{name} must live on the current device ({_current_device()}), got {t.device}")
 
 
+def _here() -> int:
+    """The current device's number; where there is none, one that no tensor has (the host's have -1)."""
+    try:
+        return torch.cuda.current_device() if _current_device is None else _current_device()
+    except RuntimeError:
+        return -2
+
+
+def _ptr_here(here: int, t: Optional[torch.Tensor], name: str, dtype: torch.dtype, numel: int = 0) -> Optional[int]:
+    """``_ptr`` of a tensor of the current device."""
+    if t is None:
+        return None
+    if t.get_device() == here and t.dtype is dtype and t.numel() >= numel and t.is_contiguous():
+        return t.data_ptr()
+    _ptr(t, name, dtype, numel)
+    _refuse_device(here, t, name)
+
+
+def _refuse_device(here: int, t: torch.Tensor, name: str) -> None:
+    raise ValueError(f"{name} must live on the current device ({here}), got {t.device}")
+
+
 def _stream_ptr(stream) -> int:
     if stream is not None:
         return stream.cuda_stream
@@ -818,23 +840,25 @@ def alloc_whole_cache(layout: Layout, four_bits: bool = False, page_table: Optio
                  make((4, 2), torch.float16), page_table=page_table)
 
 
-def _refuse_strided(name: str, x: torch.Tensor, shape, dt: torch.dtype):
+def _refuse_strided(here: int, name: str, x: torch.Tensor, shape, dt: torch.dtype):
     if not x.is_cuda:
         raise ValueError(f"{name} must live on the GPU")
+    if x.get_device() != here:
+        _refuse_device(here, x, name)
     if x.dtype is not dt or x.shape != shape:
         raise ValueError(f"{name} must be {list(shape)} of {dt}, got {tuple(x.shape)} of {x.dtype}")
     raise ValueError(f"{name}: the columns of a row must be next to each other")
 
 
-def _strided(names, x: torch.Tensor, y: torch.Tensor, shape, dt: torch.dtype):
-    """(pointer, strides of a batch, a token and a head) of x, and of y, [B, n, heads, D], rows of whole columns."""
-    if x.is_cuda and y.is_cuda and x.dtype is dt and y.dtype is dt and x.shape == shape and y.shape == shape:
+def _strided(here: int, names, x: torch.Tensor, y: torch.Tensor, shape, dt: torch.dtype):
+    """(pointer, strides of a batch, a token and a head) of x, and of y, [B, n, heads, D], rows of whole columns, of the current device."""
+    if x.get_device() == here and y.get_device() == here and x.dtype is dt and y.dtype is dt and x.shape == shape and y.shape == shape:
         xb, xt, xh, xc = x.stride()
         yb, yt, yh, yc = y.stride()
         if xc == 1 and yc == 1:
             return x.data_ptr(), xb, xt, xh, y.data_ptr(), yb, yt, yh
-    x_right = x.is_cuda and x.dtype is dt and x.shape == shape and x.stride(3) == 1
-    _refuse_strided(names[x_right], (x, y)[x_right], shape, dt)
+    x_right = x.get_device() == here and x.dtype is dt and x.shape == shape and x.stride(3) == 1
+    _refuse_strided(here, names[x_right], (x, y)[x_right], shape, dt)
 
 
 def loki_append(layout: Layout, cache: Cache, rows: torch.Tensor, k: torch.Tensor, v: torch.Tensor,
@@ -851,17 +875,17 @@ def loki_append(layout: Layout, cache: Cache, rows: torch.Tensor, k: torch.Tenso
         raise ValueError("q and q_out come together")
     if (positions is None) != (frequencies is None):
         raise ValueError("positions and frequencies come together")
-    kp, kb, kt, kh, vp, vb, vt, vh = _strided(("k", "v"), k, v, (B, n, layout.Hkv, 128), dt)
+    here = _here()
+    kp, kb, kt, kh, vp, vb, vt, vh = _strided(here, ("k", "v"), k, v, (B, n, layout.Hkv, 128), dt)
     qp = qb = qt = qh = op = ob = ot = oh = pos = freq = R = 0
     if q is not None:
-        qp, qb, qt, qh, op, ob, ot, oh = _strided(("q", "q_out"), q, q_out, (B, n, layout.Hq, 128), dt)
+        qp, qb, qt, qh, op, ob, ot, oh = _strided(here, ("q", "q_out"), q, q_out, (B, n, layout.Hq, 128), dt)
     if frequencies is not None:
-        pos, freq = _ptr(positions, "positions", torch.int32, B * n), _ptr(frequencies, "frequencies", torch.float64, 1)
+        pos, freq = _ptr_here(here, positions, "positions", torch.int32, B * n), _ptr_here(here, frequencies, "frequencies", torch.float64, 1)
         R = 2 * frequencies.numel()
     args = _rotary_pack(qp, op, qb, qt, qh, ob, ot, oh, kp, 0, kb, kt, kh, 0, 0, 0, vp, 0, vb, vt, vh, 0, 0, 0, pos,
-                        _ptr(rows, "rows", torch.int32), freq, 0, R, interleaved, inverse, scale)
+                        _ptr_here(here, rows, "rows", torch.int32), freq, 0, R, interleaved, inverse, scale)
     cache_args = cache._of(layout)
-    _on_current_device(rows, "rows")
     _check(lib().loki_append(ctypes.byref(layout), cache_args, n, args, _stream_ptr(stream)), "loki_append")
 
 
@@ -872,10 +896,10 @@ def loki_read_rows(layout: Layout, cache: Cache, rows: torch.Tensor, k_out: Opti
         raise ValueError(f"rows must be [{layout.B}, n], got {tuple(rows.shape)}")
     n = rows.shape[1]
     dt, need = _torch_dtype(layout), layout.B * layout.Hkv * n * 128
-    cache_args = cache._of(layout)
-    _on_current_device(rows, "rows")
-    _check(lib().loki_read_rows(ctypes.byref(layout), cache_args, n, _ptr(rows, "rows", torch.int32), _ptr(k_out, "k_out", dt, need),
-                                _ptr(v_out, "v_out", dt, need), _stream_ptr(stream)), "loki_read_rows")
+    cache_args, here = cache._of(layout), _here()
+    _check(lib().loki_read_rows(ctypes.byref(layout), cache_args, n, _ptr_here(here, rows, "rows", torch.int32),
+                                _ptr_here(here, k_out, "k_out", dt, need), _ptr_here(here, v_out, "v_out", dt, need),
+                                _stream_ptr(stream)), "loki_read_rows")
 
 
 def dense_cache_workspace_bytes(layout: Layout, cache: Cache, S_max: int, queries_per_seq: int = 1, window: int = 0, sinks: int = 0) -> int:
@@ -894,10 +918,9 @@ def dense_decode_cache(layout: Layout, cache: Cache, q: torch.Tensor, S_max: int
     dt = _torch_dtype(layout)
     m = max(1, queries_per_seq)
     nq = layout.B * m * layout.Hq * layout.D
-    args = SpanArgs(_ptr(seq_lens, "seq_lens", torch.int32, layout.B * m), queries_per_seq, window, sinks)
+    here = _here()
+    args = SpanArgs(_ptr_here(here, seq_lens, "seq_lens", torch.int32, layout.B * m), queries_per_seq, window, sinks)
     cache_args = cache._of(layout)
-    q_ptr = _ptr(q, "q", dt, nq)
-    _on_current_device(q, "q")
-    _check(lib().dense_decode_cache(ctypes.byref(layout), q_ptr, cache_args, S_max, ctypes.byref(args),
-                                    _ptr(workspace, "workspace", torch.uint8), workspace.numel(), _ptr(out, "out", dt, nq),
-                                    _stream_ptr(stream)), "dense_decode_cache")
+    _check(lib().dense_decode_cache(ctypes.byref(layout), _ptr_here(here, q, "q", dt, nq), cache_args, S_max, ctypes.byref(args),
+                                    _ptr_here(here, workspace, "workspace", torch.uint8), workspace.numel(),
+                                    _ptr_here(here, out, "out", dt, nq), _stream_ptr(stream)), "dense_decode_cache")
