@@ -432,9 +432,10 @@ int dense_decode_shared(const loki_layout* layout, const void* q, const void* k_
  *               [4][2] of fp16: (step, lowest) of the row's columns 32 g .. 32 g + 31, g < 4.  With lowest = fp16(the smallest of the
  *               group) and step = fp16((largest - smallest) / 15, in 32 bits) the code of x is (x - lowest) / step rounded to nearest, ties to even,
  *               within 0 .. 15 (step 0: 0) and stands for lowest + code * step: within half a step of x, plus what fp16 leaves
- *               of lowest (2^-11 of it) and 15 of step (2^-11 of the range).  Word m holds columns 32 g + 2 m (bits 4 g ..) and 32 g + 2 m + 1
- *               (bits 16 + 4 g ..).  160 bytes a row of keys and values; bf16 has 512.  Beyond fp16's range lowest and step are its largest number, 65504;
- *               of a group that holds a NaN both are NaN
+ *               of lowest (2^-11 of it, or 2^-25) and 15 of step (2^-11 of the range, or 15 2^-25; a range up to 15 2^-25 has step 0).  Beyond fp16's
+ *               range lowest and step are its largest number, 65504, and what they do not reach is cut off; of a group that holds a NaN both
+ *               are NaN.  Word m holds columns 32 g + 2 m (bits 4 g ..) and 32 g + 2 m + 1 (bits 16 + 4 g ..).  160 bytes a row of keys and
+ *               values; bf16 has 512
  *   page_table  NULL, or device int32 [B, pages_per_seq]: row s of sequence b lies in page page_table[b, s / page_rows] at row
  *               s % page_rows.  page_rows: a power of two >= 16 (256 where loki_decode_step or loki_evict take the pools too);
  *               pages_per_seq * page_rows >= S_cap; n_pages * Hkv * page_rows < 2^31
@@ -486,9 +487,11 @@ int loki_read_rows(const loki_layout* layout, const loki_cache* cache, int n, co
  *   workspace   >= dense_cache_workspace_bytes(layout, cache, S_max, args), 256-byte aligned; a workspace sized for an S_max also
  *               serves shorter ones, with the same args
  * Rows that no token sees, before the window or behind the end, are not read, and their pages' entries may be any (entries that are
- * read are clamped into [0, n_pages)).  What a token does not see does not reach its output, whatever it holds; a value that it sees and
- * that is no finite number makes that column (in 4 bits, such a step or lowest the group's columns) of its output NaN or infinite, such a
- * key all of it.  m may be thousands (a chunk of prompts): B m <= 2^24, B m Hq <= 2^27.
+ * read are clamped into [0, n_pages)).  What a token does not see does not reach its output, whatever it holds, and the queries of padded
+ * tokens reach none.  A value that a token sees and that is no finite number makes that column (in 4 bits, such a step or lowest the
+ * group's columns) of its output NaN or infinite.  A key that it sees and that is no finite number gives a logit of NaN or plus infinity, and
+ * all of the output is NaN, or one of minus infinity, and has weight 0 (in 4 bits, either).  Zeros where all logits are below -6e29.
+ * m may be thousands (a chunk of prompts): B m <= 2^24, B m Hq <= 2^27.
  */
 typedef struct {
   const int32_t* seq_lens;

@@ -50,6 +50,11 @@ def test_steps_and_lowest_values_are_the_quotients_of_the_definition(lowest, kin
     x[..., 7], x[..., 21] = lo[..., 0], lo[..., 0] + r[..., 0]
     x = torch.from_numpy(x.reshape(1, n, H, 128)).to(DT[dtype])
     step, low, codes = defined(x.float().numpy())
+    if kind != "huge":  # what the format says of a value's distance; fp16's steps are 2^-24 at least
+        y, far = x.double().numpy().reshape(1, n, H, 4, 32), lambda part: np.maximum(2.0 ** -11 * np.abs(part), 2.0 ** -25)
+        stands = low.astype(np.float64)[..., None] + codes.reshape(y.shape) * step.astype(np.float64)[..., None]
+        bound = step.astype(np.float64) / 2 + far(y.min(-1)) + 15 * far((y.max(-1) - y.min(-1)) / 15)
+        assert bool((np.abs(stands - y) <= bound[..., None]).all())
     lay = api.make_layout(1, H, H, 128, 128, n, DT[dtype])
     cache = api.alloc_whole_cache(lay, four_bits=True)
     rows = torch.arange(n, dtype=torch.int32, device="cuda")[None]
