@@ -430,12 +430,13 @@ int dense_decode_shared(const loki_layout* layout, const void* q, const void* k_
  *   k, v        rows of D elements of the storage type, [B, Hkv, S_cap, D] or, on pages, [n_pages, Hkv, page_rows, D]
  *   k_scales, v_scales  NULL, or both: the cache is in 4 bits.  k and v are then rows of 16 words of 32 bits (in place of D), the scales rows
  *               [4][2] of fp16: (step, lowest) of the row's columns 32 g .. 32 g + 31, g < 4.  With lowest = fp16(the smallest of the
- *               group) and step = fp16((largest - smallest) / 15, in 32 bits) the code of x is (x - lowest) / step rounded to nearest, ties to even,
- *               within 0 .. 15 (step 0: 0) and stands for lowest + code * step: within half a step of x, plus what fp16 leaves
- *               of lowest (2^-11 of it, or 2^-25) and 15 of step (2^-11 of the range, or 15 2^-25; a range up to 15 2^-25 has step 0).  Beyond fp16's
- *               range lowest and step are its largest number, 65504, and what they do not reach is cut off; of a group that holds a NaN both
- *               are NaN.  Word m holds columns 32 g + 2 m (bits 4 g ..) and 32 g + 2 m + 1 (bits 16 + 4 g ..).  160 bytes a row of keys and
- *               values; bf16 has 512
+ *               group) and step = fp16((largest - smallest) * (1.0f / 15.0f)), in 32 bits, the code of x is (x - lowest) / step rounded to nearest,
+ *               ties to even, within 0 .. 15 (step 0: 0) and stands for lowest + code * step: within half a step of x, plus what fp16
+ *               leaves of lowest (2^-11 of it, or 2^-25) and 15 of step (2^-11 of the range, or 15 2^-25; a range up to 15 2^-25 has step 0).
+ *               (A division by 15 in the product's place gives another step for 1 group in 10 000, one fp16 number off.)  Beyond fp16's
+ *               range lowest and step are its largest number, 65504, and what they do not reach is cut off; of a group that holds a NaN
+ *               both are NaN.  Word m holds columns 32 g + 2 m (bits 4 g ..) and 32 g + 2 m + 1 (bits 16 + 4 g ..).  160 bytes a row of
+ *               keys and values; bf16 has 512
  *   page_table  NULL, or device int32 [B, pages_per_seq]: row s of sequence b lies in page page_table[b, s / page_rows] at row
  *               s % page_rows.  page_rows: a power of two >= 16 (256 where loki_decode_step or loki_evict take the pools too);
  *               pages_per_seq * page_rows >= S_cap; n_pages * Hkv * page_rows < 2^31

@@ -68,14 +68,6 @@ __device__ __forceinline__ float turned(float a, float x, float b, float y) {
   return a * x + b * y;
 }
 
-// x / 15 as a division rounds it: the product with the rounded reciprocal, and a fifteenth of what that leaves of x (the same for every mantissa, compared on the
-// host; below 2^-90, where it may not be, fp16 has only zero).  An infinite x gives a NaN, which fminf passes over.
-__device__ __forceinline__ float fifteenth(float x) {
-  constexpr float kInv = 1.0f / 15.0f;
-  const float t = x * kInv;
-  return fmaf(fmaf(-15.0f, t, x), kInv, t);
-}
-
 // The row in `row` (LDS, 128 floats, complete) as codes and scales, by the LANES lanes of a group; p: the lane's number.
 template <int LANES>
 __device__ __forceinline__ void store_q4(const float* row, int p, uint32_t* codes, uint32_t* scales) {
@@ -103,7 +95,7 @@ __device__ __forceinline__ void store_q4(const float* row, int p, uint32_t* code
     lo = -group_allreduce_max<LANES>(-lo);
     hi = group_allreduce_max<LANES>(hi);
     // (a range past fp16's is clamped to its largest)
-    cache_half2_t sc = {(_Float16)fminf(fifteenth(hi - lo), 65504.f), (_Float16)fminf(fmaxf(lo, -65504.f), 65504.f)};
+    cache_half2_t sc = {(_Float16)fminf((hi - lo) * (1.0f / 15.0f), 65504.f), (_Float16)fminf(fmaxf(lo, -65504.f), 65504.f)};
     if (any) {  // (uniform) a group with such a value stands for no numbers
       bool own = false;
 #pragma unroll

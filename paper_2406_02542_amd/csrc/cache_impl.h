@@ -1,6 +1,6 @@
 // A cache held whole, contiguous or on pages, in the storage type or in 4 bits: where its rows lie, and the 4-bit form.
 //
-// 4 bits: a row is four groups of 32 columns.  With lowest = fp16(min) and step = fp16((max - min) / 15) of a group, the code of x is
+// 4 bits: a row is four groups of 32 columns.  With lowest = fp16(min) and step = fp16((max - min) * (1 / 15)) of a group, the code of x is
 // (x - lowest) / step rounded to nearest (ties to even) within 0 .. 15, 0 where step is 0, and stands for lowest + code * step.  Word m of
 // a row's 16 holds columns 2 m and 2 m + 1 of every group, that of group g in bits 4 g .. and 16 + 4 g ..: one shift and one bit
 // select turn a word into a register of two matrix-core operands, neighbours of one group, with the same four for all groups.
