@@ -5,9 +5,9 @@
 // The rotation is that of rotary.hip, and so is the split: a block owns a few tokens (or some heads of one), works their angles
 // out once, into LDS, and lane groups take heads of one token in turn.  Memory bounds it.
 // In 4 bits the turned row goes through LDS in 32 bits, from the lanes that hold pairs to the lanes that hold words, and is rounded
-// once, to its code.
-// 8 x up to 2048 tokens of 32/8 bf16 heads (369 MB) 68 us, 5.4 TB/s, 16 x 512 (201 MB) 36 us; 4 x up to 1111 into 4 bits, half of the columns turned 23 us (105 MB);
-// one token 4.9 us, a launch.
+// once, to its code.  Vector instructions bound that: 79 % of the SIMDs' cycles.
+// 8 x up to 2048 tokens of 32/8 bf16 heads (369 MB) 68 us, 5.4 TB/s, 16 x 512 (201 MB) 36 us; 4 x up to 1111 into 4 bits, half of the columns turned 22 us (96 MB);
+// one token 4.8 us, a launch.
 #include "cache_impl.h"
 #include "rotary_impl.h"
 
@@ -307,7 +307,7 @@ hipError_t launch_append(const Shape& s, AppendArgs args, hipStream_t st) {
   const int style = a.interleaved ? 1 : (a.R / 2) % epc == 0 ? 0 : 2;
   // From 100 MB read and written on, rows are stored past the caches (but for codes and scales, which are written piece by piece); from 90 MB of rows on
   // they are loaded past them, but for half lines: us through / past: 4 x 1111 tokens of 32/8 bf16 heads into 4 bits (55 MB) with their rows read
-  // back 27.1 / 32.8, 16 x 512 (101 MB) 62.4 / 56.9 (both 1.3 us more by now); into bf16, 8 x 2048 (201 MB) 70.2 / 68.4, 16 x 512 36.1 / 36.6, 96 columns turned 36.5 / 41.6.
+  // back 28.1 / 33.2, 16 x 512 (101 MB) 63.1 / 57.5; into bf16, 8 x 2048 (201 MB) 70.2 / 68.4, 16 x 512 36.1 / 36.6, 96 columns turned 36.5 / 41.6.
   const double bytes = (double)a.total * heads * kD * s.elem_bytes;
   const bool holes = style == 0 && a.R > 0 && a.R < kD, stores = 2.0 * bytes >= 100e6, loads = bytes >= kPastBytes && (bits4 || !holes);
 #define LOKI_APPEND(T, BITS4)                                                              \

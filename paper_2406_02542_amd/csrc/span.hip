@@ -175,7 +175,8 @@ __global__ __launch_bounds__(64 * kSpWaves) void span_rows_kernel(SpanArgs a) {
 
 // ---- fp32 -----------------------------------------------------------------------------------------------------------
 // The products of parts_impl.h's attend_f32, v_mfma_f32_16x16x4_f32, straight from registers, for QG groups of 16 query rows; steps of 16 rows.
-// 5 x 3 tokens of 24 heads over 702 rows (86 MB, memory) 21.4 us with the merge; 2 x 512 tokens of 16/8 heads behind 4096 rows (the matrix cores) 316 us, 102 TFLOP/s.
+// 5 x 3 tokens of 24 heads over 702 rows (86 MB, memory) 21.5 us with the merge; 2 x 512 tokens of 16/8 heads behind 4096 rows (keys and
+// values again for each 32 query rows) 347 us, 105 TFLOP/s.
 template <int QG, bool STREAM>
 __global__ __launch_bounds__(64 * kSpWaves, 2) void span_f32_kernel(SpanArgs a) {
   constexpr int KEYS = 16;

@@ -46,8 +46,9 @@ __device__ __forceinline__ float q4_times_step(float p, uint32_t scales) {
 // (CG = 2) 78.3, 72.5, 16 of 64/8 with 8000 and two tokens (1) 65.6, 48.4, 16 of 32/8 with 16384 (4) 65.0, 63.5.  (16 rows' products for two groups
 // of queries at a time, which unpack codes half as often, leave a SIMD one wave: 50.6 us where these took 43.9.)
 // bf16: q is one term, the weights two (2^-16 of each, as the library's other attention); fp32: three each.
-// Vector instructions bound it: 16 sequences of 32/8 heads up to 16384 rows (210 MB) 45 us, 4.6 TB/s, all of 16384 60 us, 5.6; four tokens of 8 of 64/8 up
-// to 8192 39 us; 5 of 24 fp32 heads up to 2311 17 us; one of 32/8 over 8192 10 us, of which the merge 2.9.
+// Vector instructions bound it: 16 sequences of 32/8 heads up to 16384 rows (210 to 240 MB) 43 to 48 us, 72 % of the SIMDs' cycles beside 5.6 TB/s of memory, all
+// of 16384 60 us; four tokens of 8 of 64/8 up to 8192 35 to 38 us, 62 %; 5 of 24 fp32 heads up to 2311 17 us, 51 %; one of 32/8 over 8192 10 us, of which the
+// merge 3.
 template <typename T, int CG, bool STREAM, bool DEALT>
 __global__ __launch_bounds__(64 * kQ4Waves, span_q4_waves(T::EPC == 8, 16 / CG)) void span_q4_kernel(SpanArgs a) {
   constexpr bool MID = T::EPC == 4;
