@@ -68,6 +68,8 @@ __global__ __launch_bounds__(64 * kSpWaves) void span_rows_kernel(SpanArgs a) {
     load_k(st);
     load_v(st);
     place.ask(places, span_step(steps, rows, min(s + kSpWaves, steps.total - 1)));
+#pragma unroll
+    for (int i = 0; i < 4; ++i) bq[i] = __builtin_bit_cast(am_bf16x8_t, span_query(__builtin_bit_cast(uint4, bq[i]), len));  // (rows are on their way)
   }
   for (; s < s1; s += kSpWaves) {
     const SpanStep st = span_step(steps, rows, s), next = span_step(steps, rows, min(s + kSpWaves, steps.total - 1));
@@ -156,7 +158,7 @@ __global__ __launch_bounds__(64 * kSpWaves) void span_rows_kernel(SpanArgs a) {
   }
   l += __shfl_xor(l, 16);
   l += __shfl_xor(l, 32);
-  if (len == 0) {  // (a padded token's lanes took whatever full steps gave: a maximum too, which may be infinite)
+  if (len == 0) {  // (a padded token's lanes took whatever full steps gave, a maximum too)
     m = kNegBig;
     l = 0.f;
 #pragma unroll
@@ -230,6 +232,10 @@ __global__ __launch_bounds__(64 * kSpWaves, 2) void span_f32_kernel(SpanArgs a) 
     load_k(st);
     load_v(st);
     place.ask(places, span_step(steps, rows, min(s + kSpWaves, steps.total - 1)));
+#pragma unroll
+    for (int g = 0; g < QG; ++g)
+#pragma unroll
+      for (int j = 0; j < 8; ++j) q[g][j] = __builtin_bit_cast(float4, span_query(__builtin_bit_cast(uint4, q[g][j]), len[g]));  // (rows are on their way)
   }
   for (; s < s1; s += kSpWaves) {
     const SpanStep st = span_step(steps, rows, s), next = span_step(steps, rows, min(s + kSpWaves, steps.total - 1));

@@ -45,6 +45,12 @@ __device__ __forceinline__ SpanRows span_rows(const SpanArgs& a, int b, int j0, 
   return span_rows_of(a, a.S_max - wave_max_i32(least), hi);
 }
 
+// 16 bytes of the query of a token that sees `len` rows.  A padded token's lanes take part in steps that all others see whole: with zeros, so that no
+// reference of the exponentials, which a wave moves for all of its lanes at once, goes by what such a query holds.
+__device__ __forceinline__ uint4 span_query(uint4 x, int len) {
+  return len == 0 ? make_uint4(0, 0, 0, 0) : x;
+}
+
 // Steps of a tile: those of the sinks, then those of the window.
 template <int KEYS>
 struct SpanSteps {

@@ -129,7 +129,7 @@ __global__ __launch_bounds__(64 * kQ4Waves, span_q4_waves(T::EPC == 8, 16 / CG))
   for (int n = 0; n < NS; ++n) {
     float x[8];
 #pragma unroll
-    for (int e = 0; e < 8; e += T::EPC) T::unpack(load16(src + 32 * n + e), *reinterpret_cast<float(*)[T::EPC]>(x + e));
+    for (int e = 0; e < 8; e += T::EPC) T::unpack(span_query(load16(src + 32 * n + e), len), *reinterpret_cast<float(*)[T::EPC]>(x + e));
     uint32_t w[4][QT];
     std::conditional_t<MID, double, float> sum = 0;
 #pragma unroll
@@ -287,7 +287,7 @@ __global__ __launch_bounds__(64 * kQ4Waves, span_q4_waves(T::EPC == 8, 16 / CG))
   }
   l += __shfl_xor(l, 16);
   l += __shfl_xor(l, 32);
-  if (len == 0) {  // (a padded token's lanes took whatever full steps gave: a maximum too, which may be infinite)
+  if (len == 0) {  // (a padded token's lanes took whatever full steps gave, a maximum too)
     m = kNegBig;
     l = 0.f;
 #pragma unroll

@@ -100,7 +100,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void span_tiles_kernel(SpanArgs a) {
   {
     const uint16_t* src = static_cast<const uint16_t*>(a.q) + span_place(a, tile.b, tile.h, r0 + min(row, live - 1)) * kD + 8 * half;
 #pragma unroll
-    for (int ks = 0; ks < 8; ++ks) q[ks] = __builtin_bit_cast(am_bf16x8_t, load16(src + 16 * ks));
+    for (int ks = 0; ks < 8; ++ks) q[ks] = __builtin_bit_cast(am_bf16x8_t, span_query(load16(src + 16 * ks), len));
   }
   uint4 kst[BITS4 ? 1 : kChunks], vst[BITS4 ? 1 : kChunks];
   SpanQ4Chunk cst[BITS4 ? kChunks : 1];
@@ -319,7 +319,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void span_tiles_kernel(SpanArgs a) {
 
   // both halves of a query's keys; then the waves that had other keys of the same queries
   l += __shfl_xor(l, 32);
-  if (len == 0) {  // (a padded token's lanes took whatever full steps gave: a maximum too, which may be infinite)
+  if (len == 0) {  // (a padded token's lanes took whatever full steps gave, a maximum too)
     m = kNegBig;
     l = 0.f;
 #pragma unroll

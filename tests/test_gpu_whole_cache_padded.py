@@ -1,4 +1,4 @@
-"""dense_decode_cache where a padded token's query gives infinite logits: it gets zeros, and no other token anything of it."""
+"""dense_decode_cache where padded tokens' queries hold anything: they get zeros, and no other token anything of them."""
 import pytest
 import torch
 
@@ -40,3 +40,24 @@ def test_padded_tokens_with_infinite_logits(B, m, Hq, Hkv, S, dtype, bits):
             for b, h in units:
                 at = (b, slice(None), slice(h * G, (h + 1) * G))
                 assert worst(out[at], ref[at], bound[at], dtype) <= 0, (window, low, high)
+
+
+@pytest.mark.parametrize("dtype,bits", KINDS)
+@pytest.mark.parametrize("B,m,Hq,Hkv,S", SHAPES)
+def test_padded_queries_change_no_bit_of_other_tokens(B, m, Hq, Hkv, S, dtype, bits):
+    """Large logits of a padded token, or such that are no number, move no reference of the exponentials of the tokens beside it."""
+    print("case", B, m, Hq, Hkv, S, dtype, bits, flush=True)
+    c = Case(B, Hq, Hkv, S, dtype, 16, bits, seed=m)
+    lens = last_tokens([S - 5 * b for b in range(B)], m)
+    lens[0, m - (m + 2) // 3:] = 0
+    lens[B - 1, m // 2] = 0
+    q = c.queries(m)
+    for window, sinks in ((0, 0), (S - 30, 5)):
+        outs = []
+        for what in (0.0, 40.0, -40.0, float("nan"), INF):
+            given = q.clone()
+            given[lens == 0] = what * q[lens == 0]
+            outs.append(c.attend(given, lens, S, window, sinks))
+        torch.cuda.synchronize()
+        for out in outs[1:]:
+            assert torch.equal(out, outs[0]), (window,)
